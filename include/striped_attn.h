@@ -244,6 +244,104 @@ int sa_ring_bwd_tiled(const void* Q, const void* K, const void* V, const void* d
                       int32_t q_dev_only, float* step_ms, void* stream);
 
 /*
+ * Packed sequences: attention over whole sequences of different lengths, end to end in one tensor (documents in training,
+ * prompts in serving).  Row r of Q, O, dO, dQ is [r, head, 0..d) with d contiguous and strides stride_s (rows) and stride_h
+ * (heads) in elements; K, V, dK, dV have H_kv heads (H_kv divides H; query head h reads head h / (H / H_kv)) and strides of
+ * their own, under sa_shape's rules (heads apart or interleaved within a row step).  LSE and delta are fp32 [head, row], rows
+ * contiguous, heads stat_stride_h apart.  offsets: DEVICE int32, n_seq + 1 of them: sequence s is rows offsets[s] ..
+ * offsets[s + 1] - 1 and attends causally to itself.  Empty sequences are allowed, and so are rows in front of the first and
+ * behind the last sequence: nothing of them is read or written (but delta, which is scratch).  Offsets outside 0 .. rows count as
+ * the nearest of these, a sequence that ends before it begins as empty.
+ * n_seq, rows or max_len 0: success, nothing launched, pointers not looked at.
+ */
+typedef struct {
+    int32_t n_seq;         /* sequences */
+    int32_t rows;          /* rows of the tensors */
+    int32_t max_len;       /* no sequence is longer; of one that is, the rows from max_len on are left alone */
+    int32_t H, H_kv, d;    /* d: any multiple of 4 up to 256 */
+    int64_t stride_h, stride_s, kv_stride_h, kv_stride_s, stat_stride_h;
+    int32_t dtype;         /* sa_dtype of all but LSE and delta, which are fp32 */
+    float softmax_scale;   /* <= 0 selects 1/sqrt(d) */
+} sa_packed;
+
+/*
+ * Forward: O = softmax(scale Q K^T, causal within a sequence) V rounded once to `dtype`, LSE = the rows' log-sum-exp.  Infinities
+ * and NaN: as the ring step's blocks of 128 rows and more (fp32: as its fp32 storage); nothing of one sequence reaches another.
+ * Errors: NULL, DTYPE, ALIGN, SHAPE (also: bf16 and a sequence of max_len rows reaches over 2^31 bytes, or more workgroups than
+ * a launch takes for a single key/value head), HIP.
+ */
+int sa_attn_packed_fwd(const void* q, const void* k, const void* v, const int32_t* offsets, void* out, float* lse,
+                       const sa_packed* shape, void* stream);
+
+/*
+ * Backward: the gradient of the forward call for the gradient dout of O, given its q, k, v, out and lse.  dq, dk, dv are written
+ * in `dtype` (not added to), each rounded once; rows of no sequence are left as they are.  delta: scratch, [head, row] as LSE.
+ * Sums have a fixed order: the same inputs give the same bits.
+ */
+int sa_attn_packed_bwd(const void* q, const void* k, const void* v, const void* out, const void* dout, const float* lse,
+                       const int32_t* offsets, float* delta, void* dq, void* dk, void* dv, const sa_packed* shape, void* stream);
+
+/*
+ * Paged key/value cache: two tensors (keys, values) of one geometry, each a pool of pages of page_size tokens,
+ * [page, slot, head, 0..d) with d contiguous and strides in elements: heads interleaved within a token's step or apart.
+ * Which page holds which tokens of which sequence is the caller's: sa_cache_append goes by slot numbers, page * page_size +
+ * place in the page, sa_attn_decode by a table of page numbers.
+ */
+typedef struct {
+    int32_t n_pages;       /* n_pages * page_size below 2^31 */
+    int32_t page_size;     /* tokens; a multiple of 16 */
+    int32_t H_kv, d;       /* d: any multiple of 4 up to 256 */
+    int64_t stride_page, stride_s, stride_h;       /* pages, tokens, heads; multiples of 4, stride_s below 2^24 */
+    int32_t dtype;         /* sa_dtype of the cache and of what is appended to it or attends to it */
+} sa_cache;
+
+/* New rows: row r of q is [r, head, 0..d) with H heads, stride_s, stride_h; of k and v with the cache's heads and kv_stride_*;
+ * in elements, under sa_shape's rules */
+typedef struct {
+    int32_t rows, H;
+    int64_t stride_h, stride_s, kv_stride_h, kv_stride_s;
+    float rope_base;       /* above 1 where pos is given */
+} sa_append;
+
+/*
+ * Append: row r of k, rotated by the angles of position id pos[r] (pairing, angles and double precision as sa_rope), and row r of
+ * v are stored at slot[r]; each rotated value is rounded once.  Where slot[r] is no slot of the cache (negative: a padding row)
+ * nothing of the row is stored.  No two rows may have the same slot: what it then holds is not defined.
+ * q, q_out: rows of the same tokens' queries, rotated from one into the other (which may be the same); both NULL: none.
+ * k_out: where the rotated keys are wanted beside the cache, in k's strides (may be k); NULL: nowhere.
+ * pos: device int32 [rows]; NULL: nothing is rotated (q must be NULL then).  slot: device int32 [rows].
+ * rows 0: success, nothing launched.  Errors: NULL, DTYPE, SHAPE, ALIGN, HIP.
+ */
+int sa_cache_append(const void* q, void* q_out, const void* k, void* k_out, const void* v, const int32_t* pos, const int32_t* slot,
+                    void* k_cache, void* v_cache, const sa_append* rows, const sa_cache* cache, void* stream);
+
+/* One new token of each of B sequences: q and out are [B, H, 0..d), LSE fp32 [B, H] (heads contiguous); H a multiple of the
+ * cache's H_kv, query head h reads head h / (H / H_kv) */
+typedef struct {
+    int32_t B, H;
+    int32_t max_pages;     /* page numbers a sequence in the table; max_pages * page_size at most 2^30 */
+    int64_t stride_b, stride_h;        /* of q and out, multiples of 4 */
+    int64_t stat_stride_b;
+    int64_t table_stride;  /* page numbers between sequences in the table */
+    float softmax_scale;   /* <= 0 selects 1/sqrt(d) */
+} sa_decode;
+
+/*
+ * Attention of one new token a sequence over its cached tokens 0 .. lens[b] - 1 (its own among them, appended before); token t lies
+ * in page table[b, t / page_size].  lens: device int32 [B], taken as at most max_pages * page_size; of a sequence without a token
+ * (0 or less) out is zero and LSE -inf.  A page number that is none of the cache's is not looked at: its tokens are left out.
+ * Nothing behind a sequence's last token is read.  out is rounded once to the cache's dtype; lse may be NULL.  A key with score -inf has
+ * no weight; a sequence with no other is NaN, and so is one with a NaN or +inf score.
+ * workspace: sa_attn_decode_workspace(shape, cache) bytes, 16-byte aligned, of any content; it depends on H, H_kv, d and the
+ * type, not on the batch.  Calls that may run at the same time (other streams, captured graphs) need one each.
+ * The lengths and the table are read on the device: a captured call follows them.
+ * B 0: success, nothing launched.  Errors: NULL, DTYPE, SHAPE (also a workspace that is too small), ALIGN, HIP.
+ */
+int64_t sa_attn_decode_workspace(const sa_decode* shape, const sa_cache* cache);      /* or a negative sa_status */
+int sa_attn_decode(const void* q, const void* k_cache, const void* v_cache, const int32_t* table, const int32_t* lens, void* out,
+                   float* lse, void* workspace, int64_t workspace_bytes, const sa_decode* shape, const sa_cache* cache, void* stream);
+
+/*
  * Host-only helpers (no GPU work).
  * sa_step_mask: the step's mask, GetMask(q_dev, kv_dev) of Sec. 2.2 / 2.3 in local
  * indices.  Writes both outputs: *kind = 0 empty (nothing allowed) / 1 triangular (key b

@@ -87,6 +87,11 @@ def lib():
             "sa_attn_step_bwd_tiled": (i32, [vp] * 9 + [i32, i32, i32, i32, shp, i32, i32, vp]),
             "sa_ring_fwd_tiled": (i32, [vp] * 5 + [i32, i32, shp, i32, i32, i32, vp, vp]),
             "sa_ring_bwd_tiled": (i32, [vp] * 10 + [i32, i32, shp, i32, i32, i32, vp, vp]),
+            "sa_attn_packed_fwd": (i32, [vp] * 8),
+            "sa_attn_packed_bwd": (i32, [vp] * 13),
+            "sa_cache_append": (i32, [vp] * 12),
+            "sa_attn_decode_workspace": (i64, [vp, vp]),
+            "sa_attn_decode": (i32, [vp] * 8 + [i64] + [vp] * 3),
             "sa_step_tiles": (i32, [i32, i32, i32, i32, i64, i64, i64, ctypes.POINTER(i64),
                                     ctypes.POINTER(i64)]),
             "sa_step_mask": (i32, [i32, i32, i32, i32, ctypes.POINTER(i32), ctypes.POINTER(i32)]),
@@ -115,6 +120,7 @@ EXPORTS = ("sa_stripe_permute", "sa_unstripe_permute", "sa_rope", "sa_state_init
            "sa_attn_step_fwd_rope",
            "sa_finalize", "sa_bwd_preprocess", "sa_attn_step_bwd", "sa_ring_fwd", "sa_ring_bwd",
            "sa_attn_step_fwd_tiled", "sa_attn_step_bwd_tiled", "sa_ring_fwd_tiled", "sa_ring_bwd_tiled",
+           "sa_attn_packed_fwd", "sa_attn_packed_bwd", "sa_cache_append", "sa_attn_decode_workspace", "sa_attn_decode",
            "sa_step_tiles", "sa_step_mask", "sa_step_pairs", "sa_device_props", "sa_status_str")
 
 
@@ -134,6 +140,11 @@ def _stream():
     if _raw_stream is None or _device is None:
         return torch.cuda.current_stream().cuda_stream
     return _raw_stream(_device())
+
+
+def _here():
+    """The current device's number."""
+    return torch.cuda.current_device() if _device is None else _device()
 
 
 def _check(status, where):
@@ -282,6 +293,45 @@ def sa_ring_bwd_tiled(Q, K, V, dO, O, LSE, delta, dQ, dK, dV, N, layout, shape, 
                                    _ptr(dQ), _ptr(dK), _ptr(dV), N, layout, ctypes.byref(shape), skip_bq,
                                    skip_bk, q_dev_only, buf, _stream()), "sa_ring_bwd_tiled")
     return [[buf[i * N + j] for j in range(N)] for i in range(N)] if timed else None
+
+
+# ---- packed sequences and the paged cache: no shape structure, sizes and strides are the tensors'.  Tensors lie on the current
+# device (ValueError otherwise: the call goes to that device's stream).
+
+
+def sa_attn_packed_fwd(q, k, v, offsets, out, lse, max_len, scale=None):
+    """Causal attention of sequences packed end to end: q, out [rows, H, d], k, v [rows, H_kv, d] (any strides, d contiguous),
+    offsets int32 [n_seq + 1] on the GPU, lse fp32 [H, rows]; no sequence is longer than max_len."""
+    _check(_marshal.packed_fwd(_entry["sa_attn_packed_fwd"], q, k, v, offsets, out, lse, max_len, scale or 0.0, _here, _stream),
+           "sa_attn_packed_fwd")
+
+
+def sa_attn_packed_bwd(q, k, v, out, dout, lse, offsets, delta, dq, dk, dv, max_len, scale=None):
+    """The gradient of sa_attn_packed_fwd for the gradient dout of out; delta is scratch like lse."""
+    _check(_marshal.packed_bwd(_entry["sa_attn_packed_bwd"], q, k, v, out, dout, lse, offsets, delta, dq, dk, dv, max_len, scale or 0.0,
+                               _here, _stream), "sa_attn_packed_bwd")
+
+
+def sa_cache_append(k, v, slot, k_cache, v_cache, pos=None, k_out=None, q=None, q_out=None, base=10000.0):
+    """Rows k, v [rows, H_kv, d] into the slots slot (int32 [rows], negative: none) of the caches [pages, page size, H_kv, d], keys
+    rotated by their position ids pos (int32 [rows]; None: not rotated); the rotated keys also to k_out, q [rows, H, d] rotated
+    into q_out."""
+    _check(_marshal.append(_entry["sa_cache_append"], k, v, slot, k_cache, v_cache, pos, k_out, q, q_out, float(base), _here, _stream),
+           "sa_cache_append")
+
+
+def sa_attn_decode_workspace(q, k_cache):
+    """Bytes of workspace of sa_attn_decode for such q and cache; the same for any number of sequences."""
+    size = _marshal.decode_workspace(_entry["sa_attn_decode_workspace"], q, k_cache)
+    _check(min(size, 0), "sa_attn_decode_workspace")
+    return size
+
+
+def sa_attn_decode(q, k_cache, v_cache, table, lens, out, lse, workspace, scale=None):
+    """One new token a sequence, q, out [B, H, d], over the tokens 0 .. lens[b] - 1 in the pages table[b] (int32 [B, pages]) of the
+    caches [pages, page size, H_kv, d]; lse fp32 [B, H] or None."""
+    _check(_marshal.decode(_entry["sa_attn_decode"], q, k_cache, v_cache, table, lens, out, lse, workspace, scale or 0.0, _here, _stream),
+           "sa_attn_decode")
 
 
 def sa_step_tiles(q_dev, kv_dev, N, layout, c, skip_bq, skip_bk):

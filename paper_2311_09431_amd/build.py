@@ -21,7 +21,8 @@ OBJ_DIR = os.path.join(ROOT, "_build")
 
 SOURCES = ["api.hip", "permute.hip", "elementwise.hip", "f32_step.hip", "fwd_mfma.hip",
            "bwd_mfma.hip", "bwd_ring.hip", "split_mfma.hip", "f32x3_step.hip", "f32x3_split.hip", "f32_route.hip",
-           "rows_step.hip"]
+           "rows_step.hip", "packed_fwd.hip", "packed_bwd.hip", "packed_bwd_ring.hip", "packed_f32.hip", "cache_append.hip",
+           "decode.hip"]
 
 # Flags of single sources.  f32x3_step: score tiles are read by vector instructions right after
 # their products, so MFMA results stay out of the accumulation registers (forward 2.20 -> 2.10 ms,
@@ -31,7 +32,8 @@ SOURCE_FLAGS = {"f32x3_step.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
 
 # Sources with matrix instructions in asm statements, and their kernels whose accumulators are registers by
 # number: the assembly of these is looked over (asm_check.py).
-ASM_CHECKED = {"bwd_mfma.hip": ["bwd_dkdv_wide_kernel"], "bwd_ring.hip": ["bwd_dkdv_ring_kernel", "bwd_both_ring_kernel"], "split_mfma.hip": []}
+ASM_CHECKED = {"bwd_mfma.hip": ["bwd_dkdv_wide_kernel"], "bwd_ring.hip": ["bwd_dkdv_ring_kernel", "bwd_both_ring_kernel"], "split_mfma.hip": [],
+               "packed_bwd.hip": [], "packed_bwd_ring.hip": ["packed_dkdv_ring_kernel"]}
 
 # packed fp32 VALU forms are switched off on purpose for the test machines
 FLAGS = ["-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC", "-fno-gpu-rdc",
@@ -84,7 +86,7 @@ def build_marshal():
     cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC",
            "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI, "-I" + os.path.join(at, "include"),
            "-I" + os.path.join(at, "include", "torch", "csrc", "api", "include"),
-           "-I" + sysconfig.get_paths()["include"], os.path.join(CSRC, "marshal.cpp"), "-o", out,
+           "-I" + sysconfig.get_paths()["include"], "-I" + os.path.join(ROOT, "include"), os.path.join(CSRC, "marshal.cpp"), "-o", out,
            "-L" + os.path.join(at, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", "-Wl,-rpath," + os.path.join(at, "lib")]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode:

@@ -5,6 +5,8 @@
 #include <algorithm>
 #include <vector>
 
+#include "packed.h"
+#include "paged.h"
 #include "sa_internal.h"
 
 namespace {
@@ -189,6 +191,79 @@ int step_bwd(const void* q, const void* k, const void* v, const void* dout, cons
 // and when the caller wants each step's time, one launch per block and kernel.
 bool one_launch(const StepArgs& a, int N) {
     return (int64_t)N * a.c < (int64_t(1) << 31) && workgroups_per_kv_head(a) <= kMostWorkgroups;
+}
+
+// ---- packed sequences
+int check_packed(const sa_packed* s) {
+    if (!s) return SA_ERR_NULL;
+    if (s->dtype != SA_F32 && s->dtype != SA_BF16) return SA_ERR_DTYPE;
+    if (s->n_seq < 0 || s->rows < 0 || s->max_len < 0) return SA_ERR_SHAPE;
+    if (s->H < 1 || s->H > 65535 || s->H_kv < 1 || s->H % s->H_kv || s->d < 1 || s->d > 256 || s->d % 4) return SA_ERR_SHAPE;
+    const Geom q{s->H, 0, s->stride_h, s->stride_s}, kv{s->H_kv, 0, s->kv_stride_h, s->kv_stride_s};
+    if (s->stat_stride_h < s->rows) return SA_ERR_SHAPE;
+    if (int e = check_geom(q, 1, s->rows, s->d)) return e;
+    return check_geom(kv, 1, s->rows, s->d);
+}
+// The tile loads address a sequence through a buffer descriptor with 32-bit byte offsets: its last tile must end below 2^31
+// bytes from its first row (in `stride`, elements between rows).
+bool packed_in_reach(const sa_packed* s, int64_t stride) {
+    const int64_t rows = ((int64_t)std::min(s->max_len, s->rows) + 127) / 128 * 128;
+    return s->dtype == SA_F32 || stride < (int64_t(1) << 30) / (rows + 1);
+}
+// One launch, or several of whole key/value heads and their groups where a launch would hold too many workgroups.
+template <typename Launch>
+int play_packed(const sa_packed* s, const int32_t* offsets, sa::PackedArgs a, Launch launch) {
+    a.layout = SA_CONTIGUOUS; a.n_q = a.n_kv = 1; a.fresh = true;
+    a.B = 1; a.H = s->H; a.H_kv = s->H_kv; a.d = s->d;
+    a.stride_h = s->stride_h; a.stride_s = s->stride_s; a.kv_stride_h = s->kv_stride_h; a.kv_stride_s = s->kv_stride_s;
+    a.stat_stride_h = s->stat_stride_h;
+    a.scale = s->softmax_scale > 0.f ? s->softmax_scale : 1.0f / sqrtf((float)s->d);
+    a.offsets = offsets; a.n_seq = s->n_seq; a.rows = s->rows; a.max_len = std::min(s->max_len, s->rows);
+    a.es = (int)elt_size(s->dtype);
+    const int64_t each = ((int64_t)a.max_len + sa::PACKED_ROWS - 1) / sa::PACKED_ROWS;
+    const int64_t ranks = std::min((int64_t)s->rows / sa::PACKED_ROWS + s->n_seq, each * s->n_seq);
+    const int group = s->H / s->H_kv;
+    // per key/value head at most a workgroup for each tile and query head, and two for its keys (above 128 columns)
+    const int64_t fit = kMostWorkgroups / (ranks * (group + 2));
+    if (fit < 1) return SA_ERR_SHAPE;
+    a.n_ranks = (int)ranks;
+    const int heads = (int)std::min<int64_t>(fit, s->H_kv);
+    for (int h = 0; h < s->H_kv; h += heads) {
+        sa::PackedArgs part = a;
+        part.H_kv = std::min(heads, s->H_kv - h);
+        part.H = part.H_kv * group;
+        const int64_t q = (int64_t)h * group * a.stride_h * a.es, kv = (int64_t)h * a.kv_stride_h * a.es;
+        auto at = [](const void* p, int64_t bytes) { return p ? (char*)p + bytes : nullptr; };
+        part.q = at(a.q, q); part.k = at(a.k, kv); part.v = at(a.v, kv); part.dout = at(a.dout, q);
+        part.o = (float*)at(a.o, q); part.dq = (float*)at(a.dq, q); part.dk = (float*)at(a.dk, kv); part.dv = (float*)at(a.dv, kv);
+        part.lse = a.lse + (int64_t)h * group * a.stat_stride_h;
+        if (a.delta) part.delta = a.delta + (int64_t)h * group * a.stat_stride_h;
+        if (launch(part) != hipSuccess) return SA_ERR_HIP;
+    }
+    return SA_OK;
+}
+
+// ---- paged cache
+int check_cache(const sa_cache* c) {
+    if (!c) return SA_ERR_NULL;
+    if (c->dtype != SA_F32 && c->dtype != SA_BF16) return SA_ERR_DTYPE;
+    if (c->n_pages < 1 || c->page_size < 16 || c->page_size % 16 || c->H_kv < 1 || c->d < 1 || c->d > 256 || c->d % 4) return SA_ERR_SHAPE;
+    if ((int64_t)c->n_pages * c->page_size >= (int64_t(1) << 31)) return SA_ERR_SHAPE;
+    if (int e = check_geom({c->H_kv, c->stride_page, c->stride_h, c->stride_s}, 1, c->page_size, c->d)) return e;
+    // pages apart, and the tokens of a 16-row block within the 32-bit offsets of a descriptor
+    const bool heads_apart = c->stride_h >= c->page_size * c->stride_s;
+    if (c->n_pages > 1 && c->stride_page < (heads_apart ? c->H_kv * c->stride_h : c->page_size * c->stride_s)) return SA_ERR_SHAPE;
+    if (c->stride_s >= (int64_t(1) << 24)) return SA_ERR_SHAPE;
+    return c->stride_page % 4 ? SA_ERR_ALIGN : SA_OK;
+}
+int check_decode(const sa_decode* s, const sa_cache* c) {
+    if (!s) return SA_ERR_NULL;
+    if (int e = check_cache(c)) return e;
+    if (s->B < 0 || s->H < 1 || s->H % c->H_kv || s->max_pages < 0) return SA_ERR_SHAPE;
+    if ((int64_t)s->B * s->H > kMostWorkgroups || (int64_t)s->max_pages * c->page_size > (int64_t(1) << 30)) return SA_ERR_SHAPE;
+    if (s->stride_h < c->d || (s->B > 1 && (s->stride_b < s->H * s->stride_h || s->stat_stride_b < s->H))) return SA_ERR_SHAPE;
+    if (s->B > 1 && s->table_stride < s->max_pages) return SA_ERR_SHAPE;
+    return s->stride_b % 4 || s->stride_h % 4 ? SA_ERR_ALIGN : SA_OK;
 }
 
 // Event bookkeeping for the drivers' optional per-step timings.
@@ -441,6 +516,94 @@ int sa_ring_bwd(const void* Q, const void* K, const void* V, const void* dO, con
                 const sa_shape* shape, int32_t q_dev_only, float* step_ms, void* stream) {
     return sa_ring_bwd_tiled(Q, K, V, dO, O, LSE, delta, dQ, dK, dV, N, layout, shape, 0, 0, q_dev_only,
                              step_ms, stream);
+}
+
+int sa_attn_packed_fwd(const void* q, const void* k, const void* v, const int32_t* offsets, void* out, float* lse,
+                       const sa_packed* shape, void* stream) {
+    if (int e = check_packed(shape)) return e;
+    if (shape->n_seq == 0 || shape->rows == 0 || shape->max_len == 0) return SA_OK;
+    if (!q || !k || !v || !offsets || !out || !lse) return SA_ERR_NULL;
+    if (!packed_in_reach(shape, shape->kv_stride_s)) return SA_ERR_SHAPE;
+    if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out) || (reinterpret_cast<uintptr_t>(offsets) & 3u) ||
+        (reinterpret_cast<uintptr_t>(lse) & 3u))
+        return SA_ERR_ALIGN;
+    hipStream_t st = (hipStream_t)stream;
+    sa::PackedArgs a{};
+    a.q = q; a.k = k; a.v = v; a.o = (float*)out; a.lse = lse;
+    return play_packed(shape, offsets, a, [&](const sa::PackedArgs& p) {
+        return shape->dtype == SA_F32 ? sa::launch_packed_f32(p, false, st) : sa::launch_packed_fwd(p, st);
+    });
+}
+
+int sa_attn_packed_bwd(const void* q, const void* k, const void* v, const void* out, const void* dout, const float* lse,
+                       const int32_t* offsets, float* delta, void* dq, void* dk, void* dv, const sa_packed* shape, void* stream) {
+    if (int e = check_packed(shape)) return e;
+    if (shape->n_seq == 0 || shape->rows == 0 || shape->max_len == 0) return SA_OK;
+    if (!q || !k || !v || !out || !dout || !lse || !offsets || !delta || !dq || !dk || !dv) return SA_ERR_NULL;
+    if (!packed_in_reach(shape, shape->kv_stride_s) || !packed_in_reach(shape, shape->stride_s)) return SA_ERR_SHAPE;
+    if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out) || !aligned16(dout) || !aligned16(dq) || !aligned16(dk) ||
+        !aligned16(dv) || ((reinterpret_cast<uintptr_t>(offsets) | reinterpret_cast<uintptr_t>(lse) | reinterpret_cast<uintptr_t>(delta)) & 3u))
+        return SA_ERR_ALIGN;
+    hipStream_t st = (hipStream_t)stream;
+    sa::PackedArgs a{};
+    a.q = q; a.k = k; a.v = v; a.dout = dout; a.lse = const_cast<float*>(lse); a.delta = delta;
+    a.o = (float*)const_cast<void*>(out);
+    a.dq = (float*)dq; a.dk = (float*)dk; a.dv = (float*)dv;
+    return play_packed(shape, offsets, a, [&](const sa::PackedArgs& p) {
+        if (hipError_t e = sa::launch_packed_delta(p, p.o, shape->dtype, st)) return e;
+        return shape->dtype == SA_F32 ? sa::launch_packed_f32(p, true, st) : sa::launch_packed_bwd(p, st);
+    });
+}
+
+int sa_cache_append(const void* q, void* q_out, const void* k, void* k_out, const void* v, const int32_t* pos, const int32_t* slot,
+                    void* k_cache, void* v_cache, const sa_append* rows, const sa_cache* cache, void* stream) {
+    if (!rows) return SA_ERR_NULL;
+    if (int e = check_cache(cache)) return e;
+    if (rows->rows < 0) return SA_ERR_SHAPE;
+    if (rows->rows == 0) return SA_OK;
+    if (!k || !v || !slot || !k_cache || !v_cache || !q != !q_out || (q && !pos)) return SA_ERR_NULL;
+    if (q) {
+        if (rows->H < 1 || rows->H > 65535) return SA_ERR_SHAPE;
+        if (int e = check_geom({rows->H, 0, rows->stride_h, rows->stride_s}, 1, rows->rows, cache->d)) return e;
+    }
+    if (int e = check_geom({cache->H_kv, 0, rows->kv_stride_h, rows->kv_stride_s}, 1, rows->rows, cache->d)) return e;
+    if (pos && !(rows->rope_base > 1.f)) return SA_ERR_SHAPE;
+    for (const void* p : {q, (const void*)q_out, k, (const void*)k_out, v, (const void*)k_cache, (const void*)v_cache})
+        if (!aligned16(p)) return SA_ERR_ALIGN;
+    if ((reinterpret_cast<uintptr_t>(pos) | reinterpret_cast<uintptr_t>(slot)) & 3u) return SA_ERR_ALIGN;
+    sa::AppendArgs a{};
+    a.q = q; a.q_out = q_out; a.k = k; a.k_out = k_out; a.v = v; a.pos = pos; a.slot = slot; a.k_cache = k_cache; a.v_cache = v_cache;
+    a.rows = rows->rows; a.H = rows->H; a.H_kv = cache->H_kv; a.d = cache->d; a.page_size = cache->page_size;
+    a.n_slots = (int64_t)cache->n_pages * cache->page_size;
+    a.stride_h = rows->stride_h; a.stride_s = rows->stride_s; a.kv_stride_h = rows->kv_stride_h; a.kv_stride_s = rows->kv_stride_s;
+    a.stride_page = cache->stride_page; a.stride_slot = cache->stride_s; a.stride_head = cache->stride_h;
+    a.log2_base = pos ? log2((double)rows->rope_base) : 0.;
+    return sa::launch_cache_append(a, cache->dtype, (hipStream_t)stream) == hipSuccess ? SA_OK : SA_ERR_HIP;
+}
+
+int64_t sa_attn_decode_workspace(const sa_decode* shape, const sa_cache* cache) {
+    if (int e = check_decode(shape, cache)) return e;
+    return sa::decode_workspace(shape->H, cache->H_kv, cache->d, cache->dtype);
+}
+
+int sa_attn_decode(const void* q, const void* k_cache, const void* v_cache, const int32_t* table, const int32_t* lens, void* out,
+                   float* lse, void* workspace, int64_t workspace_bytes, const sa_decode* shape, const sa_cache* cache, void* stream) {
+    if (int e = check_decode(shape, cache)) return e;
+    if (shape->B == 0) return SA_OK;
+    if (!q || !k_cache || !v_cache || !lens || !out || !workspace || (!table && shape->max_pages > 0)) return SA_ERR_NULL;
+    if (workspace_bytes < sa::decode_workspace(shape->H, cache->H_kv, cache->d, cache->dtype)) return SA_ERR_SHAPE;
+    for (const void* p : {q, k_cache, v_cache, (const void*)out, (const void*)workspace})
+        if (!aligned16(p)) return SA_ERR_ALIGN;
+    if ((reinterpret_cast<uintptr_t>(table) | reinterpret_cast<uintptr_t>(lens) | reinterpret_cast<uintptr_t>(lse)) & 3u) return SA_ERR_ALIGN;
+    sa::DecodeArgs a{};
+    a.q = q; a.k_cache = k_cache; a.v_cache = v_cache; a.table = table; a.lens = lens; a.out = out; a.lse = lse;
+    a.parts = (float*)workspace;
+    a.B = shape->B; a.H = shape->H; a.H_kv = cache->H_kv; a.d = cache->d; a.n_pages = cache->n_pages; a.page_size = cache->page_size;
+    a.max_pages = shape->max_pages;
+    a.stride_b = shape->stride_b; a.stride_h = shape->stride_h; a.stat_stride_b = shape->stat_stride_b; a.table_stride = shape->table_stride;
+    a.stride_page = cache->stride_page; a.stride_slot = cache->stride_s; a.stride_head = cache->stride_h;
+    a.scale = shape->softmax_scale > 0.f ? shape->softmax_scale : 1.0f / sqrtf((float)cache->d);
+    return sa::launch_decode(a, cache->dtype, (hipStream_t)stream) == hipSuccess ? SA_OK : SA_ERR_HIP;
 }
 
 int sa_step_mask(int32_t q_dev, int32_t kv_dev, int32_t N, int32_t layout, int32_t* kind, int32_t* off) {

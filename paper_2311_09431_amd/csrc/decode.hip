@@ -1,0 +1,558 @@
+// Attention of one new token a sequence over its paged cache: O = softmax(scale q K^T) V over the sequence's cached rows.
+//
+// Bound by memory: the cache is read once, 2 d elements a token and key/value head, for 4 d operations of each of the G query
+// heads that share it.
+//
+// Work.  A unit is (sequence, key/value head, 16 query heads of its group); its tokens come in chunks of CHUNK, and all chunks of all
+// units, in order, are cut into equal shares, one a workgroup, however the lengths differ.  What a workgroup holds of a unit it
+// holds alone is written as result; of a unit that goes over into another workgroup's share it writes an unnormalised sum, its
+// reference and its row sum, and a second kernel joins them.  A share has at most two such pieces (its first and its last unit's),
+// so the workspace depends on neither the batch nor the lengths.
+//
+// Inside, a wavefront takes every fourth tile of TILE tokens and keeps its own reference, row sum and accumulators; the four meet in LDS
+// at the end of a unit.  Nothing is staged: K and V rows go from memory to the registers that the products want.
+//  * S^T = K Q^T by 16 x 16 tiles, tokens as rows: a lane holds 16 bytes of one token's row a product.  The tile's lane (16 j + n)
+//    register r is token 4 j + r of query head n.
+//  * O^T += V^T P^T: that register, as it stands, is the right operand where the contraction goes through the tokens in that
+//    order.  The left one wants, of one column, the lane's tokens: a lane loads a few columns of each of them (16 lanes a whole row, so
+//    memory sees whole rows) and turns the little block round in registers (bf16: two tokens a v_perm; fp32: nothing to do).
+// The next tile's K rows are requested as soon as this one's scores are formed, its V rows when they are used up.
+//
+// Probabilities: bf16 storage takes them as two bf16 terms (2^-17 relative; one term would put a second rounding of 2^-9 beside the
+// result's own), fp32 as they are; row sums in fp32.  The reference moves only when a lane's sum of a tile passes 2^24 or there is none yet.
+//
+// What must not be read is not: a 16-token block's descriptor ends with the last cached token, and one whose page number is none
+// has a range of zero; both deliver zeros, and the scores are masked.
+#include <hip/hip_bf16.h>
+
+#include "mfma_tiles.h"
+#include "paged.h"
+
+namespace sa {
+
+namespace {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int WAVES = 4, HEADS = 16;            // wavefronts a workgroup, query heads a unit
+constexpr float MOST = 16777216.f;              // 2^24: a lane's sum of a tile against a reference that stays
+
+// Of a storage type and DP columns computed: tokens a tile, columns of a V row a lane loads at once, loads a V row
+template <typename T, int DP> struct Of;
+template <int DP> struct Of<__hip_bfloat16, DP> {
+    static constexpr int TILE = 32, STEP = 32, CW = DP >= 128 ? 8 : 4, ES = 2;
+};
+template <int DP> struct Of<float, DP> {
+    static constexpr int TILE = 16, STEP = 16, CW = 4, ES = 4;
+};
+template <typename T> constexpr int CHUNK = WAVES * Of<T, 64>::TILE;
+
+__device__ inline f32x4 mfma_bf16(u32x4 a, u32x4 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+__device__ inline f32x4 mfma_f32(uint32_t a, uint32_t b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a), __uint_as_float(b), c, 0, 0, 0);
+}
+// over the four lanes that hold a query head
+__device__ inline float quad_max(float x) {
+    x = fmaxf(x, __shfl_xor(x, 16));
+    return fmaxf(x, __shfl_xor(x, 32));
+}
+__device__ inline float quad_sum(float x) {
+    x += __shfl_xor(x, 16);
+    return x + __shfl_xor(x, 32);
+}
+// Parts are joined against the largest reference, of parts without a token (or any weight) 0.  A row sum of -1 says that there were
+// tokens, all without weight (scores of -inf): nothing beside other parts, no number if there are none.
+__device__ inline float reference(float top) { return top == -INFINITY ? 0.f : top; }
+__device__ inline void add_sum(float& sum, bool& weightless, float l, float factor) {
+    weightless = weightless || l < 0.f;
+    sum += (l < 0.f ? 0.f : l) * factor;
+}
+__device__ inline int scalar(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ inline int64_t scalar64(int64_t x) {
+    return (int64_t)((uint64_t)(uint32_t)scalar((int)(x >> 32)) << 32 | (uint32_t)scalar((int)x));
+}
+
+template <typename T>
+__device__ inline int chunks_of(const DecodeArgs& p, int b) {
+    const int64_t room = (int64_t)p.max_pages * p.page_size;
+    const int len = (int)min((int64_t)max(p.lens[b], 0), room);
+    return (len + CHUNK<T> - 1) / CHUNK<T>;
+}
+__device__ inline int wave_scan(int x, int lane) {          // inclusive
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int y = __shfl_up(x, o);
+        if (lane >= o) x += y;
+    }
+    return x;
+}
+// units of a sequence
+__device__ inline int units_of(const DecodeArgs& p) { return p.H_kv * ((p.H / p.H_kv + HEADS - 1) / HEADS); }
+
+// Chunks of all sequences (a wavefront's lanes take them in turn), and the sequence in which chunk number `at` of them lies with the
+// chunks before it; found: at >= 0 and there is one.
+struct Where { int64_t all, before; int seq; };
+template <typename T>
+__device__ inline int64_t all_chunks(const DecodeArgs& p, int lane) {
+    int64_t n = 0;
+    for (int b0 = 0; b0 < p.B; b0 += 64) n += __shfl(wave_scan(b0 + lane < p.B ? chunks_of<T>(p, b0 + lane) : 0, lane), 63);
+    return n;
+}
+template <typename T>
+__device__ inline Where find_chunk(const DecodeArgs& p, int64_t at, int lane) {
+    int64_t before = 0;
+    for (int b0 = 0; b0 < p.B; b0 += 64) {
+        const int own = b0 + lane < p.B ? chunks_of<T>(p, b0 + lane) : 0, upto = wave_scan(own, lane);
+        const uint64_t past = __builtin_amdgcn_ballot_w64(before + upto > at);
+        if (past) {
+            const int l = (int)__builtin_ctzll(past);
+            return {0, before + __shfl(upto - own, l), b0 + l};
+        }
+        before += __shfl(upto, 63);
+    }
+    return {0, before, p.B};
+}
+
+// A unit's piece in the workspace: HEADS rows (as many as the group has) of DP columns, then references and row sums.
+__host__ __device__ inline int part_rows(int group) { return group < HEADS ? group : HEADS; }
+__host__ __device__ inline int64_t part_floats(int group, int DP) { return (int64_t)part_rows(group) * (DP + 2); }
+
+template <typename T, int DP>
+__global__ void __launch_bounds__(64 * WAVES, DP > 128 ? 1 : 2)
+decode_kernel(DecodeArgs p) {
+    using O = Of<T, DP>;
+    constexpr int TILE = O::TILE, CW = O::CW, ES = O::ES, KS = DP / O::STEP, NM = DP / (16 * CW), NB = DP / 16;
+    constexpr bool BF16 = ES == 2;
+    constexpr int BLOCKS = TILE / 16, TOKENS = 4 * BLOCKS;      // 16-token blocks of a tile, tokens a lane holds of it
+    constexpr int PITCH = DP + 4;
+    __shared__ __attribute__((aligned(16))) float o_lds[WAVES][HEADS][PITCH];
+    __shared__ float m_lds[WAVES][HEADS], l_lds[WAVES][HEADS];
+
+    const int lane = threadIdx.x & 63, n = lane & 15, j = lane >> 4;
+    const int wave = scalar((int)threadIdx.x >> 6);
+    const int group = p.H / p.H_kv, blocks = (group + HEADS - 1) / HEADS, units = p.H_kv * blocks, d = p.d;
+    const int64_t all = scalar64(all_chunks<T>(p, lane)) * units;
+    const int64_t share = (all + p.n_wgs - 1) / p.n_wgs;
+    int64_t at = (int64_t)blockIdx.x * share;
+    const int64_t end = min(at + share, all);
+    if (at >= end) return;
+    // where the share begins: sequence, unit of it, chunk of that
+    int b, unit, chunk, n_chunks, len;
+    const int64_t room = (int64_t)p.max_pages * p.page_size;
+    auto enter = [&]() {
+        len = scalar((int)min((int64_t)max(p.lens[b], 0), room));
+        n_chunks = (len + CHUNK<T> - 1) / CHUNK<T>;
+    };
+    {
+        // (a sequence's chunks, unit by unit, follow those of all sequences before it)
+        const Where w = find_chunk<T>(p, at / units, lane);
+        b = scalar(w.seq);
+        enter();
+        const int64_t in = at - scalar64(w.before) * units;
+        unit = (int)(in / n_chunks);
+        chunk = (int)(in - (int64_t)unit * n_chunks);
+    }
+    const float kappa = p.scale * LOG2E;
+    const int pitch = (int)p.stride_slot * ES;              // bytes between tokens of a page
+    // this lane's bytes of a K block (token n, its columns of each product) and of a V block (token 4 j + r, its columns)
+    uint32_t k_at[KS], v_at[4][NM];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+        const int col = O::STEP * ks + (BF16 ? 8 : 4) * j;
+        k_at[ks] = col < d ? n * pitch + col * ES : DT_OUT_OF_RANGE;
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int m = 0; m < NM; ++m) {
+            const int col = 16 * CW * m + CW * n;
+            v_at[r][m] = col < d ? (4 * j + r) * pitch + col * ES : DT_OUT_OF_RANGE;
+        }
+    // bf16, d % 8 == 4: the chunk that holds column d has four elements of whatever follows the row
+    const int part_ks = BF16 && d % 8 && ((d >> 3) & 3) == j ? d >> 5 : -1;
+
+    while (at < end) {
+        const int kvh = unit / blocks, h0 = kvh * group + (unit - kvh * blocks) * HEADS;
+        const int n_heads = min(HEADS, (kvh + 1) * group - h0);
+        const int first = chunk, last = (int)min((int64_t)n_chunks, chunk + (end - at));       // chunks of the unit in this share
+        u32x4 q[KS];
+        const bool has_head = n < n_heads;
+        const T* q_row = (const T*)p.q + b * p.stride_b + (h0 + (has_head ? n : 0)) * p.stride_h;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            constexpr int E = BF16 ? 8 : 4;
+            const int col = O::STEP * ks + E * j;
+            q[ks] = u32x4{0, 0, 0, 0};
+            if (has_head && col < d) {
+                if (!BF16 || col + 8 <= d) q[ks] = *reinterpret_cast<const u32x4*>(q_row + col);
+                else {
+                    const u32x2 x = *reinterpret_cast<const u32x2*>(q_row + col);
+                    q[ks][0] = x[0];
+                    q[ks][1] = x[1];
+                }
+            }
+        }
+        f32x4 acc[NB];
+#pragma unroll
+        for (int i = 0; i < NB; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+        float m = -INFINITY, l = 0.f;
+        bool seen = false;                      // some token of a page that is one
+
+        // this wavefront's tiles of the unit: tokens t0, t0 + CHUNK, ..., each in BLOCKS blocks of 16
+        const int t_end = min(len, last * CHUNK<T>);
+        int t0 = first * CHUNK<T> + wave * TILE;
+        // page and place in it of each block, counted on by CHUNK a tile
+        const int step_page = CHUNK<T> / p.page_size, step_in = CHUNK<T> - step_page * p.page_size;
+        int page[BLOCKS], in_page[BLOCKS];
+#pragma unroll
+        for (int i = 0; i < BLOCKS; ++i) {
+            page[i] = (t0 + 16 * i) / p.page_size;
+            in_page[i] = t0 + 16 * i - page[i] * p.page_size;
+        }
+        const int32_t* table = p.table + b * p.table_stride;
+        const int64_t head_at = (int64_t)kvh * p.stride_head;
+        u32x4 k[BLOCKS][KS];
+        uint32_t v[TOKENS][NM][CW * ES / 4];
+        int64_t at_k[BLOCKS], at_v[BLOCKS];         // bytes of the blocks in the caches, of the tile requested last / before it
+        int rows_k[BLOCKS], rows_v[BLOCKS];         // tokens that may be read (0: none)
+        auto place = [&](int t) {
+#pragma unroll
+            for (int i = 0; i < BLOCKS; ++i) {
+                const int token = t + 16 * i;
+                rows_k[i] = 0;
+                at_k[i] = 0;
+                if (token < len) {
+                    const int id = scalar(table[page[i]]);
+                    if (id >= 0 && id < p.n_pages) {
+                        rows_k[i] = min(16, len - token);
+                        at_k[i] = (id * p.stride_page + in_page[i] * p.stride_slot + head_at) * ES;
+                    }
+                }
+                page[i] += step_page;
+                in_page[i] += step_in;
+                if (in_page[i] >= p.page_size) {
+                    in_page[i] -= p.page_size;
+                    ++page[i];
+                }
+            }
+        };
+        auto rsrc = [&](const void* cache, int64_t bytes, int rows) {
+            return __builtin_amdgcn_make_buffer_rsrc((void*)((const char*)cache + bytes), 0, rows ? (rows - 1) * pitch + ES * d : 0, 0x00020000);
+        };
+        auto load_k = [&]() {
+#pragma unroll
+            for (int i = 0; i < BLOCKS; ++i) {
+                const auto s = rsrc(p.k_cache, at_k[i], rows_k[i]);
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) k[i][ks] = __builtin_amdgcn_raw_buffer_load_b128(s, k_at[ks], 0, 0);
+            }
+        };
+        auto load_v = [&]() {
+#pragma unroll
+            for (int i = 0; i < BLOCKS; ++i) {
+                const auto s = rsrc(p.v_cache, at_v[i], rows_v[i]);
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+#pragma unroll
+                    for (int x = 0; x < NM; ++x) {
+                        uint32_t(&to)[CW * ES / 4] = v[4 * i + r][x];
+                        if constexpr (CW * ES == 16) {
+                            const u32x4 y = __builtin_amdgcn_raw_buffer_load_b128(s, v_at[r][x], 0, 0);
+                            to[0] = y[0]; to[1] = y[1]; to[2] = y[2]; to[3] = y[3];
+                        } else {
+                            const u32x2 y = __builtin_amdgcn_raw_buffer_load_b64(s, v_at[r][x], 0, 0);
+                            to[0] = y[0]; to[1] = y[1];
+                        }
+                    }
+            }
+        };
+        auto keep_place = [&]() {
+#pragma unroll
+            for (int i = 0; i < BLOCKS; ++i) {
+                at_v[i] = at_k[i];
+                rows_v[i] = rows_k[i];
+            }
+        };
+        if (t0 < t_end) {
+            place(t0);
+            load_k();
+            keep_place();
+            load_v();
+        }
+        for (; t0 < t_end; t0 += CHUNK<T>) {
+            f32x4 s[BLOCKS];
+#pragma unroll
+            for (int i = 0; i < BLOCKS; ++i) {
+                s[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) {
+                    if constexpr (BF16) {
+                        u32x4 x = k[i][ks];
+                        if (d % 8) {
+                            x[2] = ks == part_ks ? 0 : x[2];
+                            x[3] = ks == part_ks ? 0 : x[3];
+                        }
+                        s[i] = mfma_bf16(x, q[ks], s[i]);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) s[i] = mfma_f32(k[i][ks][e], q[ks][e], s[i]);
+                    }
+                }
+            }
+            int rows[BLOCKS];
+            bool whole = true;
+#pragma unroll
+            for (int i = 0; i < BLOCKS; ++i) {
+                rows[i] = rows_k[i];
+                whole = whole && rows[i] == 16;
+                seen = seen || rows[i] > 0;
+            }
+            // the next tile's K rows (behind the last one: nothing, t0 is beyond the unit's tokens here)
+            const bool more = t0 + CHUNK<T> < t_end;
+            if (more) {
+                place(t0 + CHUNK<T>);
+                load_k();
+            }
+            if (!whole) {
+#pragma unroll
+                for (int i = 0; i < BLOCKS; ++i)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        if (4 * j + r >= rows[i]) s[i][r] = -INFINITY;
+            }
+            float pr[TOKENS], sum = 0.f;
+#pragma unroll
+            for (int x = 0; x < TOKENS; ++x) {
+                pr[x] = __builtin_amdgcn_exp2f(fmaf(s[x / 4][x % 4], kappa, -m));
+                sum += pr[x];
+            }
+            if (__builtin_amdgcn_ballot_w64(!(sum < MOST)) != 0) {          // wave-uniform and rare but for the first tile
+                float top = s[0][0];
+#pragma unroll
+                for (int x = 1; x < TOKENS; ++x) top = fmaxf(top, s[x / 4][x % 4]);
+                const float m_new = fmaxf(m, quad_max(top) * kappa), ref = m_new == -INFINITY ? 0.f : m_new;
+                const float alpha = __builtin_amdgcn_exp2f(m - ref);
+                m = m_new;
+                l *= alpha;
+#pragma unroll
+                for (int i = 0; i < NB; ++i) acc[i] *= alpha;
+                sum = 0.f;
+#pragma unroll
+                for (int x = 0; x < TOKENS; ++x) {
+                    pr[x] = __builtin_amdgcn_exp2f(fmaf(s[x / 4][x % 4], kappa, -ref));
+                    sum += pr[x];
+                }
+            }
+            l += sum;
+            if constexpr (BF16) {
+                bf16x8 hi, lo;
+#pragma unroll
+                for (int x = 0; x < 8; ++x) {
+                    hi[x] = (__bf16)pr[x];
+                    lo[x] = (__bf16)(pr[x] - (float)hi[x]);
+                }
+                const u32x4 ph = __builtin_bit_cast(u32x4, hi), pl = __builtin_bit_cast(u32x4, lo);
+#pragma unroll
+                for (int x = 0; x < NM; ++x)
+#pragma unroll
+                    for (int c = 0; c < CW; ++c) {
+                        u32x4 a;        // column c of the lane's, its eight tokens
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            a[e] = __builtin_amdgcn_perm(v[2 * e + 1][x][c / 2], v[2 * e][x][c / 2], c % 2 ? 0x07060302u : 0x05040100u);
+                        acc[x * CW + c] = mfma_bf16(a, ph, acc[x * CW + c]);
+                        acc[x * CW + c] = mfma_bf16(a, pl, acc[x * CW + c]);
+                    }
+            } else {
+#pragma unroll
+                for (int r = 0; r < TOKENS; ++r)
+#pragma unroll
+                    for (int x = 0; x < NM; ++x)
+#pragma unroll
+                        for (int c = 0; c < CW; ++c)
+                            acc[x * CW + c] = mfma_f32(v[r][x][c], __float_as_uint(pr[r]), acc[x * CW + c]);
+            }
+            if (more) {
+                keep_place();
+                load_v();
+            }
+        }
+
+        // the four wavefronts' parts
+        l = quad_sum(l);
+        if (l == 0.f && seen) l = -1.f;
+        if (j == 0) {
+            m_lds[wave][n] = m;
+            l_lds[wave][n] = l;
+        }
+        __syncthreads();
+        float top = m_lds[0][n];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) top = fmaxf(top, m_lds[w][n]);
+        const float own = __builtin_amdgcn_exp2f(m - reference(top));
+#pragma unroll
+        for (int x = 0; x < NM; ++x)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int c = 0; c < CW; c += 4) {
+                    float4 y;
+                    y.x = acc[x * CW + c][r] * own; y.y = acc[x * CW + c + 1][r] * own;
+                    y.z = acc[x * CW + c + 2][r] * own; y.w = acc[x * CW + c + 3][r] * own;
+                    *reinterpret_cast<float4*>(&o_lds[wave][n][16 * CW * x + CW * (4 * j + r) + c]) = y;
+                }
+        __syncthreads();
+        const bool complete = first == 0 && last == n_chunks;
+        // (a share's piece of a unit that began in another one is its first, of one that ends in another its last)
+        float* part = p.parts + ((int64_t)blockIdx.x * 2 + (first > 0 ? 0 : 1)) * part_floats(group, DP);
+        for (int i = threadIdx.x; i < n_heads * (DP / 4); i += 64 * WAVES) {
+            const int row = i / (DP / 4), col = 4 * (i - row * (DP / 4));
+            if (col >= d) continue;
+            float4 y = *reinterpret_cast<const float4*>(&o_lds[0][row][col]);
+            float mx = m_lds[0][row];
+#pragma unroll
+            for (int w = 1; w < WAVES; ++w) {
+                const float4 z = *reinterpret_cast<const float4*>(&o_lds[w][row][col]);
+                y.x += z.x; y.y += z.y; y.z += z.z; y.w += z.w;
+                mx = fmaxf(mx, m_lds[w][row]);
+            }
+            float sum = 0.f;
+            bool weightless = false;
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) add_sum(sum, weightless, l_lds[w][row], __builtin_amdgcn_exp2f(m_lds[w][row] - reference(mx)));
+            if (sum == 0.f && weightless) sum = -1.f;
+            if (complete) {
+                // no token: zeros; tokens without any weight: no number
+                const float inv = sum < 0.f ? NAN : sum == 0.f ? 0.f : 1.f / sum;
+                T* to = (T*)p.out + b * p.stride_b + (h0 + row) * p.stride_h + col;
+                if constexpr (BF16) {
+                    bf16x4 z = {(__bf16)(y.x * inv), (__bf16)(y.y * inv), (__bf16)(y.z * inv), (__bf16)(y.w * inv)};
+                    *reinterpret_cast<bf16x4*>(to) = z;
+                } else {
+                    *reinterpret_cast<float4*>(to) = make_float4(y.x * inv, y.y * inv, y.z * inv, y.w * inv);
+                }
+                if (p.lse && col == 0) p.lse[b * p.stat_stride_b + h0 + row] = sum < 0.f ? NAN : (mx + __builtin_amdgcn_logf(sum)) * LN2;
+            } else {
+                *reinterpret_cast<float4*>(part + row * DP + col) = y;
+                if (col == 0) {
+                    part[part_rows(group) * DP + row] = mx;
+                    part[part_rows(group) * (DP + 1) + row] = sum;
+                }
+            }
+        }
+        __syncthreads();
+        at += last - first;
+        chunk = 0;
+        if (++unit == units) {
+            unit = 0;
+            do ++b; while (at < end && (enter(), n_chunks == 0));
+        }
+    }
+}
+
+// Units whose pieces lie in several shares, and sequences without a token.  One workgroup a (sequence, unit, query head); its wavefronts
+// take the pieces in turn.
+template <typename T, int DP>
+__global__ void __launch_bounds__(64 * WAVES)
+decode_join_kernel(DecodeArgs p) {
+    constexpr int COLS = DP / 64;
+    __shared__ float o_lds[WAVES][DP], m_lds[WAVES], l_lds[WAVES];
+    const int lane = threadIdx.x & 63, wave = scalar((int)threadIdx.x >> 6);
+    const int group = p.H / p.H_kv, blocks = (group + HEADS - 1) / HEADS, units = p.H_kv * blocks;
+    const int b = (int)blockIdx.x / p.H, head = (int)blockIdx.x - b * p.H;
+    const int kvh = head / group, in_group = head - kvh * group, unit = kvh * blocks + in_group / HEADS, row = in_group % HEADS;
+    int64_t before = 0, all = 0;
+    for (int b0 = 0; b0 < p.B; b0 += 64) {
+        const int own = b0 + lane < p.B ? chunks_of<T>(p, b0 + lane) : 0, upto = wave_scan(own, lane);
+        if (b >= b0 && b < b0 + 64) before = all + __shfl(upto - own, b - b0);
+        all += __shfl(upto, 63);
+    }
+    before = scalar64(before);
+    all = scalar64(all) * units;
+    const int n = scalar(chunks_of<T>(p, b));
+    const int64_t share = max((int64_t)1, (all + p.n_wgs - 1) / p.n_wgs);
+    const int64_t from = before * units + (int64_t)unit * n;
+    const int g0 = (int)(from / share), g1 = n ? (int)((from + n - 1) / share) : g0;
+    if (n && g0 == g1) return;
+    float m = -INFINITY, l = 0.f, acc[COLS] = {};
+    bool weightless = false;
+    for (int g = n ? g0 + wave : g1 + 1; g <= g1; g += WAVES) {
+        const float* part = p.parts + ((int64_t)g * 2 + (g == g0 ? 1 : 0)) * part_floats(group, DP);
+        const float mg = part[part_rows(group) * DP + row], lg = part[part_rows(group) * (DP + 1) + row];
+        float x[COLS];
+#pragma unroll
+        for (int c = 0; c < COLS; ++c) x[c] = lane + 64 * c < p.d ? part[row * DP + lane + 64 * c] : 0.f;
+        const float top = fmaxf(m, mg), a = __builtin_amdgcn_exp2f(m - reference(top)), f = __builtin_amdgcn_exp2f(mg - reference(top));
+        l *= a;
+        add_sum(l, weightless, lg, f);
+#pragma unroll
+        for (int c = 0; c < COLS; ++c) acc[c] = acc[c] * a + x[c] * f;
+        m = top;
+    }
+#pragma unroll
+    for (int c = 0; c < COLS; ++c) o_lds[wave][lane + 64 * c] = acc[c];
+    if (lane == 0) {
+        m_lds[wave] = m;
+        l_lds[wave] = weightless && l == 0.f ? -1.f : l;
+    }
+    __syncthreads();
+    float top = m_lds[0];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) top = fmaxf(top, m_lds[w]);
+    float f[WAVES], sum = 0.f;
+    weightless = false;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+        f[w] = __builtin_amdgcn_exp2f(m_lds[w] - reference(top));
+        add_sum(sum, weightless, l_lds[w], f[w]);
+    }
+    if (sum == 0.f && weightless) sum = NAN;
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    for (int col = threadIdx.x; col < p.d; col += 64 * WAVES) {
+        float y = 0.f;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) y += o_lds[w][col] * f[w];
+        T* to = (T*)p.out + b * p.stride_b + head * p.stride_h + col;
+        if constexpr (sizeof(T) == 2) *reinterpret_cast<__bf16*>(to) = (__bf16)(y * inv);
+        else *to = y * inv;
+    }
+    if (p.lse && threadIdx.x == 0) p.lse[b * p.stat_stride_b + head] = (top + __builtin_amdgcn_logf(sum)) * LN2;
+}
+
+constexpr int columns(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
+// as many as the chip holds at once
+constexpr int workgroups(int DP) { return N_CU * (DP <= 128 ? 2 : 1); }
+
+template <typename T, int DP>
+hipError_t launch(DecodeArgs a, hipStream_t st) {
+    a.n_wgs = workgroups(DP);
+    hipLaunchKernelGGL((decode_kernel<T, DP>), dim3((unsigned)a.n_wgs), dim3(64 * WAVES), 0, st, a);
+    if (hipError_t e = hipGetLastError()) return e;
+    hipLaunchKernelGGL((decode_join_kernel<T, DP>), dim3((unsigned)a.B * a.H), dim3(64 * WAVES), 0, st, a);
+    return hipGetLastError();
+}
+template <typename T>
+hipError_t launch(const DecodeArgs& a, hipStream_t st) {
+    switch (columns(a.d)) {
+        case 64: return launch<T, 64>(a, st);
+        case 128: return launch<T, 128>(a, st);
+        default: return launch<T, 256>(a, st);
+    }
+}
+
+}  // namespace
+
+int64_t decode_workspace(int H, int H_kv, int d, int) {
+    const int DP = columns(d);
+    return (int64_t)workgroups(DP) * 2 * part_floats(H / H_kv, DP) * 4;
+}
+
+hipError_t launch_decode(DecodeArgs a, int dtype, hipStream_t st) {
+    return dtype == SA_F32 ? launch<float>(a, st) : launch<__hip_bfloat16>(a, st);
+}
+
+}  // namespace sa

@@ -17,6 +17,7 @@
 namespace sa {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr int TD = 128;          // tile columns: head dimensions up to 128 are zero-padded to it;
@@ -121,9 +122,9 @@ __device__ inline bf16x8 zero_beyond_d(bf16x8 x, bool is_last_chunk) {
     return __builtin_bit_cast(bf16x8, v);
 }
 // Only the k-steps that can hold column d need that: d > 64 for DP = 112 (k-steps 4..6), > 112 for
-// 128 (the last one).  32 heads, d 100, 8192 tokens, triangular step, selects on every k-step against
+// 128 (the last one).  (Above 128 columns, where any k-step can: all.)  32 heads, d 100, 8192 tokens, triangular step, selects on every k-step against
 // these: forward 0.604 / 0.585 ms, backward 1.91 / 1.84.
-constexpr int part_from(int DP) { return DP <= 64 ? 0 : DP <= 112 ? 4 : 7; }
+constexpr int part_from(int DP) { return DP <= 64 || DP > 128 ? 0 : DP <= 112 ? 4 : 7; }
 // The loads go through a buffer descriptor held in scalar registers: the tile's byte
 // offset within the (batch, head) matrix is a scalar operand and the lane offset a 32-bit
 // vector operand, so a load costs no address arithmetic at all.  The descriptor's range is
@@ -337,11 +338,16 @@ __device__ inline void decode_block(int linear, int n_tiles, int n_bh, int& rank
     bh = grp * HEAD_GROUP + (within - rank * heads);
 }
 
+// place and head found before (packed.h)
+__device__ inline void decode_given(int linear, int n_heads, int& rank, int& head) {
+    rank = linear / n_heads;
+    head = linear - rank * n_heads;
+}
+
 // Row of d <= 16 NF elements (d a multiple of 4) as B-operand fragments, NF k-steps of 16,
 // zero-padded to 16 NF columns.  Nothing beyond the row is read.
 template <int NF>
 __device__ inline void load_b_frags(bf16x8 (&f)[NF], const __bf16* __restrict__ row, int h, int d) {
-    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 #pragma unroll
     for (int ks = 0; ks < NF; ++ks) {
         const int col = 16 * ks + 8 * h;

@@ -1,0 +1,117 @@
+// Packed sequences: rows of n_seq sequences lie end to end, sequence s in rows offsets[s] .. offsets[s + 1] - 1, and attend
+// causally to themselves.  A sequence is one triangular block of the ring step's kernels; what is added here is how a
+// workgroup finds its own.
+#pragma once
+#include "mfma_tiles.h"
+#include "sa_internal.h"
+
+namespace sa {
+
+// StepArgs of one block (B = 1, one device, triangular), its pointers those of row 0; c is set by the workgroup
+struct PackedArgs : StepArgs {
+    const int32_t* offsets;     // device, n_seq + 1
+    int n_seq, rows, max_len;   // rows of the tensors; rows of a sequence beyond max_len are not looked at
+    int n_ranks;                // 128-row tiles of all sequences, at most
+    int es;                     // bytes of an element
+    bool by_rank;               // workgroup order: by ranks over all heads, or in groups of heads (decode_block)
+};
+
+constexpr int PACKED_ROWS = 128;        // rows of a tile
+
+// Rows first .. first + len - 1 of sequence s.  Whatever the offsets hold, they lie within the tensors: an offset below zero or
+// behind the last row is taken as the nearest one that is none, a sequence that ends before it begins is empty.
+struct Span { int first, len; };
+__device__ inline Span span_of(const PackedArgs& p, int s) {
+    const int first = min(max(p.offsets[s], 0), p.rows), end = min(max(p.offsets[s + 1], first), p.rows);
+    return {first, min(end - first, p.max_len)};
+}
+__device__ inline int tiles_of(Span x) { return (x.len + PACKED_ROWS - 1) / PACKED_ROWS; }
+
+__device__ inline int wave_add(int x) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o);
+    return x;
+}
+
+hipError_t launch_packed_fwd(PackedArgs p, hipStream_t st);
+hipError_t launch_packed_delta(const PackedArgs& p, const void* out, int dtype, hipStream_t st);
+hipError_t launch_packed_bwd(const PackedArgs& p, hipStream_t st);
+hipError_t launch_packed_bwd_ring(const PackedArgs& p, hipStream_t st);       // dK and dV at 65 to 128 columns
+hipError_t launch_packed_f32(PackedArgs p, bool backward, hipStream_t st);
+
+// Tile `rank` of all sequences' tiles, the heaviest first: a sequence of t tiles has one of each weight 1 .. t (query tile i
+// walks i + 1 key tiles, key tile i is walked by t - i query tiles).  C(w) = sum over sequences of max(0, t - w + 1) tiles weigh w or
+// more; the tile's weight is the largest w with C(w) > rank, found by halving, and among the sequences that have one of it the tile is
+// that of number rank - C(w + 1).  Every wavefront looks for itself, 64 sequences at a time in its lanes.  False: fewer tiles than that.
+__device__ inline bool find_tile(const PackedArgs& p, int rank, int& seq, int& weight) {
+    const int lane = threadIdx.x & 63;
+    const int own = lane < p.n_seq ? tiles_of(span_of(p, lane)) : 0;      // of the first 64 sequences
+    auto count = [&](int w) {
+        int n = max(0, own - w + 1);
+        for (int s = 64 + lane; s < p.n_seq; s += 64) n += max(0, tiles_of(span_of(p, s)) - w + 1);
+        return __builtin_amdgcn_readfirstlane(wave_add(n));
+    };
+    int behind = count(1);
+    if (rank >= behind) return false;
+    int lo = 1, hi = (p.max_len + PACKED_ROWS - 1) / PACKED_ROWS + 1;      // C(lo) > rank >= C(hi)
+    behind = 0;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1, c = count(mid);
+        if (c > rank) lo = mid;
+        else {
+            hi = mid;
+            behind = c;
+        }
+    }
+    weight = lo;
+    int left = rank - behind;           // so many sequences with such a tile come before it
+    for (int s0 = 0; s0 < p.n_seq; s0 += 64) {
+        const int t = s0 == 0 ? own : s0 + lane < p.n_seq ? tiles_of(span_of(p, s0 + lane)) : 0;
+        const uint64_t has = __builtin_amdgcn_ballot_w64(t >= lo);
+        const int n = __builtin_popcountll(has);
+        if (left < n) {
+            const int before = __builtin_amdgcn_mbcnt_hi((uint32_t)(has >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)has, 0));
+            const uint64_t mine = __builtin_amdgcn_ballot_w64(t >= lo && before == left);
+            seq = s0 + (int)__builtin_ctzll(mine);
+            return true;
+        }
+        left -= n;
+    }
+    return false;                       // (not reached: C counted them)
+}
+
+// The workgroup's sequence, tile and head: p becomes the arguments of a launch on that sequence alone, n_tiles its tiles,
+// rank the tile's place among them (0: the heaviest).  False: none, the launch has more workgroups than there are tiles.
+template <bool SNAKE>
+__device__ inline bool enter_sequence(PackedArgs& p, int linear, int n_heads, int& n_tiles, int& rank, int& head) {
+    if (p.by_rank) decode_block<SNAKE, true>(linear, p.n_ranks, n_heads, rank, head);
+    else decode_block<SNAKE, false>(linear, p.n_ranks, n_heads, rank, head);
+    int seq, weight;
+    if (!find_tile(p, rank, seq, weight)) return false;
+    const Span x = span_of(p, seq);
+    const int first = __builtin_amdgcn_readfirstlane(x.first);
+    p.c = __builtin_amdgcn_readfirstlane(x.len);
+    n_tiles = (p.c + PACKED_ROWS - 1) / PACKED_ROWS;
+    rank = n_tiles - weight;
+    const int64_t q = p.es * p.stride_s * first, kv = p.es * p.kv_stride_s * first;         // bytes
+    p.q = (const char*)p.q + q;
+    p.k = (const char*)p.k + kv;
+    p.v = (const char*)p.v + kv;
+    p.dout = (const char*)p.dout + q;
+    p.o = (float*)((char*)p.o + q);
+    p.dq = (float*)((char*)p.dq + q);
+    p.dk = (float*)((char*)p.dk + kv);
+    p.dv = (float*)((char*)p.dv + kv);
+    p.lse += first;
+    p.delta += first;
+    return true;
+}
+
+// arguments of a row that is done over (f32_rows.h): of a packed sequence the workgroup's own, not the launch's
+template <bool PACKED>
+__device__ inline const StepArgs& row_args(const StepArgs& launch, const StepArgs& own) {
+    if constexpr (PACKED) return own;
+    else return launch;
+}
+
+}  // namespace sa

@@ -1,0 +1,32 @@
+// Causal attention of packed sequences, forward, bf16: the ring step's workgroups (fwd_tiles.h), each on one 128-row tile of
+// one sequence (packed.h).
+//
+// A launch has a workgroup for every tile that the sequences can have, rows / 128 + n_seq of them a head, whatever the offsets
+// say (they are on the device); those behind the last tile end at once.
+#include "fwd_tiles.h"
+
+namespace sa {
+
+namespace {
+
+template <int DP, bool PART>
+hipError_t launch(const PackedArgs& p, hipStream_t st) {
+    hipLaunchKernelGGL((fwd_mfma_kernel<true, WALK_TRI, DP, PART, false, false, PackedArgs>), dim3((unsigned)p.n_ranks * p.H),
+                       dim3(64 * NW), 0, st, p, 0);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_packed_fwd(PackedArgs p, hipStream_t st) {
+    const int64_t workgroups = (int64_t)p.n_ranks * p.H;
+    p.by_rank = by_rank(true, workgroups, p.d > 128 ? MOST_BY_RANK<256, true> : p.d > 112 ? MOST_BY_RANK<128, true> : MOST_BY_RANK<64, true>);
+    const bool part = p.d % 8 != 0;
+    if (p.d > 128) return part ? launch<256, true>(p, st) : launch<256, false>(p, st);
+    if (p.d <= 32 && !part) return launch<32, false>(p, st);
+    if (p.d <= 64) return part ? launch<64, true>(p, st) : launch<64, false>(p, st);
+    if (p.d <= 112) return part ? launch<112, true>(p, st) : launch<112, false>(p, st);
+    return part ? launch<128, true>(p, st) : launch<128, false>(p, st);
+}
+
+}  // namespace sa

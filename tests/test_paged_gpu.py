@@ -1,0 +1,395 @@
+"""The paged key/value cache: appending rotated rows, attention of one new token, and both with the packed prompt, against 64 bits."""
+import pytest
+import torch
+
+from paper_2311_09431_amd import binding as sa
+from sequences import HALF_STEP, U, Head, check, lengths_to_offsets, normal
+
+pytestmark = pytest.mark.gpu
+
+BF16, F32 = torch.bfloat16, torch.float32
+ROUNDED = {BF16: 2.0 ** -17, F32: 0.0}          # a weight as two bf16 terms, or as it is
+
+
+def cache(pages, page, heads, d, dtype, order, fill=float("nan")):
+    """[pages, page, heads, d] on the GPU; order of the memory: heads inside a token's step, or apart.  What nobody wrote is NaN."""
+    if order == "shd":
+        return torch.full((pages, page, heads, d), fill, dtype=dtype, device="cuda")
+    return torch.full((pages, heads, page, d), fill, dtype=dtype, device="cuda").permute(0, 2, 1, 3)
+
+
+def tables(lens, page, seed, spare=2, width=None):
+    """Pages of a pool in no order; entries behind a sequence's last page are no page."""
+    n = [-(-x // page) for x in lens]
+    ids = torch.randperm(sum(n) + spare, generator=torch.Generator().manual_seed(seed)).to(torch.int32)
+    table = torch.full((len(lens), width or max(n + [1])), -1, dtype=torch.int32)
+    at = 0
+    for s, x in enumerate(n):
+        table[s, :x] = ids[at:at + x]
+        at += x
+    return table, len(ids)
+
+
+def fill(k_cache, v_cache, table, lens, seed):
+    """Gaussians in the slots that the sequences use; returns them, [tokens, heads, d] a sequence."""
+    page, (heads, d) = k_cache.shape[1], k_cache.shape[2:]
+    rows = []
+    for s, n in enumerate(lens):
+        kv = [normal((n, heads, d), seed + 2 * s + i, k_cache.dtype) for i in (0, 1)]
+        rows.append(kv)
+        t = torch.arange(n)
+        for c, x in zip((k_cache, v_cache), kv):
+            c[table[s][t // page].long().cuda(), (t % page).cuda()] = x.cuda()
+    return rows
+
+
+def decode(lens, H, H_kv, d, dtype, page=16, order="shd", seed=1, scale=None, mutate=None, width=None, with_lse=True):
+    table, pool = tables(lens, page, seed, width=width)
+    k_cache, v_cache = (cache(pool, page, H_kv, d, dtype, order) for _ in range(2))
+    rows = fill(k_cache, v_cache, table, lens, 10 * seed)
+    q = normal((len(lens), H, d), seed + 5, dtype)
+    if mutate:
+        mutate(q, rows, k_cache, v_cache, table)
+    out, lse = torch.full((len(lens), H, d), 7, dtype=dtype, device="cuda"), torch.full((len(lens), H), 7.0, device="cuda")
+    work = torch.full((sa.sa_attn_decode_workspace(q, k_cache),), 255, dtype=torch.uint8, device="cuda")       # NaN
+    sa.sa_attn_decode(q.cuda(), k_cache, v_cache, table.cuda(), torch.tensor(lens, dtype=torch.int32, device="cuda"), out, lse if with_lse else None,
+                      work, scale)
+    return q, rows, out.cpu(), lse.cpu()
+
+
+def compare(q, rows, out, lse, dtype, scale=None, heads=None):
+    B, H, d = q.shape
+    scale = scale or d ** -0.5
+    for b in range(B):
+        k, v = rows[b]
+        if k.shape[0] == 0:
+            assert (out[b] == 0).all() and (lse[b] == -torch.inf).all()
+            continue
+        G = H // k.shape[1]
+        for kvh in range(k.shape[1]):
+            if heads is not None and kvh not in heads:
+                continue
+            h = slice(kvh * G, (kvh + 1) * G)
+            x = Head(q[b, h], k[:, kvh], v[:, kvh], scale, False)
+            check(("out", b, kvh), out[b, h], x.out, x.out_off(dtype, ROUNDED[dtype]))
+            check(("lse", b, kvh), lse[b, h], x.lse, x.lse_off)
+
+
+LENS = [1, 15, 16, 0, 17, 31, 33, 128, 129, 500]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("d", [4, 20, 32, 64, 68, 100, 128, 132, 200, 256])
+def test_decode_head_dimensions(d, dtype):
+    compare(*decode(LENS, 4, 2, d, dtype), dtype)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("H,H_kv", [(1, 1), (5, 5), (12, 3), (16, 1), (17, 1), (32, 8), (40, 1), (66, 2)])
+@pytest.mark.parametrize("order", ["shd", "hsd"])
+def test_decode_heads_and_orders(H, H_kv, order, dtype):
+    compare(*decode([90, 1, 300], H, H_kv, 64, dtype, order=order), dtype)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("page", [16, 48, 64, 80, 256, 1024])
+def test_decode_page_sizes(page, dtype):
+    compare(*decode([1, 47, 200, 1100, 256], 8, 2, 128, dtype, page=page), dtype)
+
+
+# one sequence over many workgroups, many sequences in one workgroup, and both beside each other
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("lens", [[20000], [1] * 700, [0] * 70 + [9000] + [3] * 90, [130] * 65, list(range(1, 300, 7))])
+def test_decode_shares(lens, dtype):
+    compare(*decode(lens, 4, 2, 64, dtype, page=64), dtype)
+
+
+def test_decode_long():
+    lens = [70001, 5, 33333]
+    compare(*decode(lens, 8, 2, 128, BF16, page=128), BF16)
+
+
+def test_decode_offsets_beyond_32_bits():
+    """A cache of 6 GB: the pages used lie at its end."""
+    page, heads, d, pages = 256, 8, 128, 6000
+    lens = [700, 300]
+    k_cache, v_cache = (cache(pages, page, heads, d, BF16, "shd", 0) for _ in range(2))
+    assert k_cache.numel() > 2 ** 30 and k_cache.numel() * 2 > 2 ** 31
+    table = torch.tensor([[pages - 1, pages - 5, pages - 3], [pages - 2, 0, 0]], dtype=torch.int32)
+    table[1, 1] = pages - 4
+    rows = fill(k_cache, v_cache, table, lens, 3)
+    q = normal((2, 16, d), 9, BF16)
+    out, lse = torch.empty(2, 16, d, dtype=BF16, device="cuda"), torch.empty(2, 16, device="cuda")
+    work = torch.empty(sa.sa_attn_decode_workspace(q, k_cache), dtype=torch.uint8, device="cuda")
+    sa.sa_attn_decode(q.cuda(), k_cache, v_cache, table.cuda(), torch.tensor(lens, dtype=torch.int32, device="cuda"), out, lse, work)
+    compare(q, rows, out.cpu(), lse.cpu(), BF16)
+    # and appending there
+    slot = torch.tensor([(pages - 1) * page + 255, pages * page - 2, -1], dtype=torch.int32, device="cuda")
+    k, v = (normal((3, heads, d), s, BF16).cuda() for s in (20, 21))
+    sa.sa_cache_append(k, v, slot, k_cache, v_cache)
+    for c, x in ((k_cache, k), (v_cache, v)):
+        assert torch.equal(c[pages - 1, 255], x[0]) and torch.equal(c[pages - 1, 254], x[1])
+
+
+def test_decode_scale_and_no_lse():
+    q, rows, out, lse = decode([77, 200], 4, 2, 64, BF16, scale=0.5)
+    compare(q, rows, out, lse, BF16, scale=0.5)
+    again = decode([77, 200], 4, 2, 64, BF16, scale=0.5, with_lse=False)
+    assert torch.equal(again[2], out) and (again[3] == 7).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_decode_large_scores(dtype):
+    def mutate(q, rows, *_):
+        q.mul_(50)
+    compare(*decode([1, 300, 2000], 4, 2, 64, dtype, mutate=mutate), dtype)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_decode_pages_that_are_none(dtype):
+    """Tokens of a page number that is none of the cache's are left out, all of them: no token."""
+    page, lens = 32, [100, 200, 64]
+    table, pool = tables(lens, page, 4)
+    k_cache, v_cache = (cache(pool, page, 2, 64, dtype, "shd") for _ in range(2))
+    rows = fill(k_cache, v_cache, table, lens, 40)
+    table[0, 1], table[1, 0], table[1, 6] = pool, -2 ** 31, 2 ** 31 - 1
+    table[2, :2] = -1
+    gone = [torch.ones(n, dtype=torch.bool) for n in lens]
+    gone[0][32:64] = gone[1][0:32] = gone[1][192:] = gone[2][:] = False
+    rows = [[x[keep] for x in kv] for kv, keep in zip(rows, gone)]
+    q = normal((3, 4, 64), 6, dtype)
+    out, lse = torch.full_like(q, 7).cuda(), torch.full((3, 4), 7.0, device="cuda")
+    work = torch.empty(sa.sa_attn_decode_workspace(q, k_cache), dtype=torch.uint8, device="cuda")
+    sa.sa_attn_decode(q.cuda(), k_cache, v_cache, table.cuda(), torch.tensor(lens, dtype=torch.int32, device="cuda"), out, lse, work)
+    compare(q, rows, out.cpu(), lse.cpu(), dtype)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_decode_any_length_stays_within_the_table(dtype):
+    page = 16
+    table, pool = tables([40, 40, 40], page, 2)
+    k_cache, v_cache = (cache(pool, page, 1, 64, dtype, "shd") for _ in range(2))
+    rows = fill(k_cache, v_cache, table, [48, 48, 48], 4)
+    q = normal((3, 2, 64), 6, dtype)
+    out, lse = torch.empty_like(q).cuda(), torch.empty(3, 2, device="cuda")
+    work = torch.empty(sa.sa_attn_decode_workspace(q, k_cache), dtype=torch.uint8, device="cuda")
+    lens = torch.tensor([2 ** 31 - 1, -5, 49], dtype=torch.int32, device="cuda")
+    sa.sa_attn_decode(q.cuda(), k_cache, v_cache, table.cuda(), lens, out, lse, work)
+    rows[1] = [x[:0] for x in rows[1]]
+    compare(q, rows, out.cpu(), lse.cpu(), dtype)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("n", [20, 3000])
+def test_decode_infinities_and_nan(n, dtype):
+    """A key at -inf has no weight; alone, or beside NaN or +inf, the row is no number.  Other sequences do not notice."""
+    d, inf = 64, float("inf")
+    def mutate(q, rows, k_cache, v_cache, table):
+        q[:] = q.abs() + 0.1                    # a key of infinities has that score
+        page = k_cache.shape[1]
+        def put(s, t, value):
+            rows[s][0][t] = value
+            k_cache[int(table[s, t // page]), t % page] = value
+        for t in range(0, n, 2):
+            put(0, t, -inf)
+        for t in range(n):
+            put(1, t, -inf)
+        put(2, n - 1, inf)
+        put(3, n // 2, float("nan"))
+    q, rows, out, lse = decode([n] * 5, 2, 1, d, dtype, mutate=mutate)
+    keep = torch.arange(n) % 2 == 1
+    rows[0] = [x[keep] for x in rows[0]]
+    for s in (0, 4):
+        compare(q[s:s + 1], [rows[s]], out[s:s + 1], lse[s:s + 1], dtype)
+    assert out[1:4].isnan().all() and lse[1:4].isnan().all()
+
+
+def test_decode_captured_and_replayed():
+    """Lengths and tables are read when the graph is played."""
+    page, most = 32, 640
+    table, pool = tables([most] * 3, page, 8)
+    k_cache, v_cache = (cache(pool, page, 2, 128, BF16, "shd") for _ in range(2))
+    fill(k_cache, v_cache, table, [most] * 3, 5)
+    q = normal((3, 8, 128), 6, BF16).cuda()
+    table, lens = table.cuda(), torch.tensor([640, 5, 0], dtype=torch.int32, device="cuda")
+    out, lse = torch.empty_like(q), torch.empty(3, 8, device="cuda")
+    work = torch.empty(sa.sa_attn_decode_workspace(q, k_cache), dtype=torch.uint8, device="cuda")
+    call = lambda: sa.sa_attn_decode(q, k_cache, v_cache, table, lens, out, lse, work)
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for now in ([640, 5, 0], [0, 0, 640], [33, 640, 1]):
+        lens.copy_(torch.tensor(now, dtype=torch.int32))
+        call()
+        torch.cuda.synchronize()
+        want = out.clone(), lse.clone()
+        out.fill_(3), lse.fill_(3), work.fill_(255)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
+
+
+# ---------------------------------------------------------------- append
+
+
+def rotated(x, pos, base):
+    half = x.shape[-1] // 2
+    a = pos.double()[:, None] * base ** (-torch.arange(half, dtype=torch.float64) * 2 / x.shape[-1])
+    c, s = a.cos()[:, None], a.sin()[:, None]
+    lo, hi = x.double().split(half, -1)
+    return torch.cat([lo * c - hi * s, hi * c + lo * s], -1)
+
+
+def off_of(x, want, dtype):
+    """One rounding of the result; a sine or cosine in fp32 from an angle off by 2^-24 of half a turn (4 u in all), times both elements
+    of the pair; the two products and their sum in fp32."""
+    half = x.shape[-1] // 2
+    size = x.double().abs()
+    pair = size + torch.cat([size[..., half:], size[..., :half]], -1)
+    return HALF_STEP[dtype] * want.abs() + 8 * U * pair
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("d", [4, 12, 32, 64, 100, 112, 128, 256])
+@pytest.mark.parametrize("rows,order", [(1, "shd"), (37, "hsd"), (1500, "shd")])
+def test_append(rows, order, d, dtype):
+    H, H_kv, page = 6, 2, 32
+    pages = rows // page + 3
+    k_cache, v_cache = (cache(pages, page, H_kv, d, dtype, order, 7) for _ in range(2))
+    q, k, v = normal((rows, H, d), 1, dtype), normal((rows, H_kv, d), 2, dtype), normal((rows, H_kv, d), 3, dtype)
+    gen = torch.Generator().manual_seed(rows)
+    slot = torch.randperm(pages * page, generator=gen)[:rows].to(torch.int32)
+    pos = torch.randint(0, 1 << 20, (rows,), generator=gen).to(torch.int32)
+    padding = torch.arange(rows) % 5 == 4
+    slot[padding] = torch.tensor([-1, -2 ** 31, pages * page, 2 ** 31 - 1], dtype=torch.int32)[torch.arange(int(padding.sum())) % 4]
+    q_out, k_out = torch.empty_like(q).cuda(), torch.empty_like(k).cuda()
+    gq, gk, gv = q.cuda(), k.cuda(), v.cuda()
+    sa.sa_cache_append(gk, gv, slot.cuda(), k_cache, v_cache, pos=pos.cuda(), k_out=k_out, q=gq, q_out=q_out, base=5000.0)
+    assert torch.equal(gq.cpu(), q) and torch.equal(gk.cpu(), k)
+    for got, x in ((q_out, q), (k_out, k)):
+        want = rotated(x, pos, 5000.0)
+        check("rotated", got, want, off_of(x, want, dtype))
+    kept = slot[~padding].long()
+    for c, x in ((k_cache, k_out.cpu()), (v_cache, v)):
+        want = torch.full((pages * page, H_kv, d), 7, dtype=dtype)
+        want[kept] = x[~padding]
+        assert torch.equal(c.cpu().reshape(-1, H_kv, d), want)
+    # in place, and without what is not wanted
+    again = [cache(pages, page, H_kv, d, dtype, order, 7) for _ in range(2)]
+    sa.sa_cache_append(gk, gv, slot.cuda(), *again, pos=pos.cuda(), k_out=gk, q=gq, q_out=gq, base=5000.0)
+    assert torch.equal(gq, q_out) and torch.equal(gk, k_out) and torch.equal(again[0], k_cache) and torch.equal(again[1], v_cache)
+    again = [cache(pages, page, H_kv, d, dtype, order, 7) for _ in range(2)]
+    sa.sa_cache_append(k.cuda(), gv, slot.cuda(), *again, pos=pos.cuda(), base=5000.0)
+    assert torch.equal(again[0], k_cache) and torch.equal(again[1], v_cache)
+    # not rotated
+    sa.sa_cache_append(k.cuda(), gv, slot.cuda(), *again)
+    want = torch.full((pages * page, H_kv, d), 7, dtype=dtype)
+    want[kept] = k[~padding]
+    assert torch.equal(again[0].cpu().reshape(-1, H_kv, d), want)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_append_strided_rows(dtype):
+    """Rows as one projection writes them, q, k and v side by side; and with the heads apart."""
+    rows, H, H_kv, d, page = 21, 4, 2, 64, 16
+    for apart in (False, True):
+        x = normal((rows, H + 2 * H_kv, d), 4, dtype).cuda()
+        if apart:
+            x = x.permute(1, 0, 2).contiguous().permute(1, 0, 2)
+        q, k, v = x.split([H, H_kv, H_kv], 1)
+        kept = x.clone()
+        pos = torch.arange(rows, dtype=torch.int32, device="cuda") + 1000
+        slot = torch.arange(rows, dtype=torch.int32, device="cuda") + 5
+        got = [cache(3, page, H_kv, d, dtype, "shd", 0) for _ in range(2)]
+        sa.sa_cache_append(k, v, slot, *got, pos=pos, k_out=k, q=q, q_out=q)
+        plain = [t.contiguous() for t in kept.split([H, H_kv, H_kv], 1)]
+        want = [cache(3, page, H_kv, d, dtype, "shd", 0) for _ in range(2)]
+        sa.sa_cache_append(plain[1], plain[2], slot, *want, pos=pos, k_out=plain[1], q=plain[0], q_out=plain[0])
+        assert torch.equal(q, plain[0]) and torch.equal(k, plain[1]) and torch.equal(v, plain[2])
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+def test_append_rotates_as_rope_does():
+    rows, H, d = 200, 3, 128
+    k = normal((rows, H, d), 3, F32).cuda()
+    pos = torch.arange(rows, dtype=torch.int32, device="cuda") * 999
+    k_out, c = torch.empty_like(k), [cache(13, 16, H, d, F32, "shd", 0) for _ in range(2)]
+    sa.sa_cache_append(k, k, pos * 0 - 1, *c, pos=pos, k_out=k_out)
+    x = k.permute(1, 0, 2)[None]
+    y = torch.empty_like(x)
+    sa.sa_rope(x, y, pos, sa.shard_shape(x, rows))
+    # both: a sine in fp32, two products and a sum; 8 u of the pair each
+    assert (y[0].permute(1, 0, 2) - k_out).abs().max() <= 16 * U * 2 * k.abs().max()
+
+
+# ---------------------------------------------------------------- together
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("H,H_kv,d,page", [(4, 2, 64, 16), (8, 8, 100, 48), (8, 1, 128, 64)])
+def test_prompt_then_tokens(H, H_kv, d, page, dtype):
+    """Prompts of different lengths into the cache and through packed attention, then new tokens one at a time: each token's
+    attention is that of the whole sequence's last row."""
+    prompts, steps, n = [33, 1, 150], 3, 3
+    most = max(prompts) + steps
+    table, pool = tables([most] * n, page, 6)
+    k_cache, v_cache = (cache(pool, page, H_kv, d, dtype, "shd") for _ in range(2))
+    seqs = [[normal((x + steps, h, d), 7 * s + i, dtype) for i, h in enumerate((H, H_kv, H_kv))] for s, x in enumerate(prompts)]
+    slot_of = lambda s, t: (table[s][t // page].long() * page + t % page).to(torch.int32)
+    pos = torch.cat([torch.arange(x) for x in prompts])
+    slot = torch.cat([slot_of(s, torch.arange(x)) for s, x in enumerate(prompts)])
+    q, k, v = (torch.cat([x[i][:p] for x, p in zip(seqs, prompts)]).cuda() for i in range(3))
+    sa.sa_cache_append(k, v, slot.cuda(), k_cache, v_cache, pos=pos.to(torch.int32).cuda(), k_out=k, q=q, q_out=q)
+    off = lengths_to_offsets(prompts).cuda()
+    out, lse = torch.empty_like(q), torch.empty(H, q.shape[0], device="cuda")
+    sa.sa_attn_packed_fwd(q, k, v, off, out, lse, max(prompts))
+    at, keys = 0, []
+    for s, x in enumerate(prompts):
+        r = slice(at, at + x)
+        at += x
+        keys.append([k[r].cpu(), v[r].cpu()])
+        for h in range(H):
+            y = Head(q[r, h].cpu(), k[r, h // (H // H_kv)].cpu(), v[r, h // (H // H_kv)].cpu(), d ** -0.5, True)
+            check(("prompt", s, h), out[r, h], y.out, y.out_off(dtype, HALF_STEP[dtype] if dtype == BF16 else 0))
+    work = torch.empty(sa.sa_attn_decode_workspace(q, k_cache), dtype=torch.uint8, device="cuda")
+    for step in range(steps):
+        now = torch.tensor([x + step for x in prompts])
+        q, k, v = (torch.stack([x[i][p + step] for x, p in zip(seqs, prompts)]).cuda() for i in range(3))
+        slot = torch.cat([slot_of(s, now[s:s + 1]) for s in range(n)])
+        sa.sa_cache_append(k, v, slot.cuda(), k_cache, v_cache, pos=now.to(torch.int32).cuda(), k_out=k, q=q, q_out=q)
+        out, lse = torch.empty_like(q), torch.empty(n, H, device="cuda")
+        sa.sa_attn_decode(q, k_cache, v_cache, table.cuda(), (now + 1).to(torch.int32).cuda(), out, lse, work)
+        for s in range(n):
+            keys[s] = [torch.cat([old, x[s:s + 1].cpu()]) for old, x in zip(keys[s], (k, v))]
+        compare(q.cpu(), keys, out.cpu(), lse.cpu(), dtype)
+        # the rotated query and key are those of the token's place
+        for s in range(n):
+            x = seqs[s][0][prompts[s] + step][None]
+            want = rotated(x, now[s:s + 1], 10000.0)
+            check("query", q[s:s + 1], want, off_of(x, want, dtype))
+
+
+def test_other_stream():
+    want = decode([300, 4], 4, 2, 64, BF16)
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        got = decode([300, 4], 4, 2, 64, BF16)
+    assert torch.equal(got[2], want[2]) and torch.equal(got[3], want[3])
+
+
+def test_empty_calls():
+    k_cache = cache(2, 16, 2, 64, BF16, "shd", 0)
+    q = torch.empty(0, 2, 64, dtype=BF16, device="cuda")
+    none = torch.empty(0, dtype=torch.int32, device="cuda")
+    sa.sa_cache_append(q, q, none, k_cache, k_cache.clone())
+    work = torch.empty(sa.sa_attn_decode_workspace(q, k_cache), dtype=torch.uint8, device="cuda")
+    sa.sa_attn_decode(q, k_cache, k_cache, none.view(0, 0), none, q, torch.empty(0, 2, device="cuda"), work)
+    assert (k_cache == 0).all()
+    # a table without pages: no token
+    q = normal((2, 2, 64), 1, BF16).cuda()
+    out, lse = torch.empty_like(q), torch.empty(2, 2, device="cuda")
+    sa.sa_attn_decode(q, k_cache, k_cache, torch.empty(2, 0, dtype=torch.int32, device="cuda"), torch.full((2,), 9, dtype=torch.int32, device="cuda"), out,
+                      lse, work)
+    assert (out == 0).all() and (lse == -torch.inf).all()
