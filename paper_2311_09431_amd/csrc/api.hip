@@ -220,13 +220,11 @@ int play_packed(const sa_packed* s, const int32_t* offsets, sa::PackedArgs a, La
     a.scale = s->softmax_scale > 0.f ? s->softmax_scale : 1.0f / sqrtf((float)s->d);
     a.offsets = offsets; a.n_seq = s->n_seq; a.rows = s->rows; a.max_len = std::min(s->max_len, s->rows);
     a.es = (int)elt_size(s->dtype);
-    const int64_t each = ((int64_t)a.max_len + sa::PACKED_ROWS - 1) / sa::PACKED_ROWS;
-    const int64_t ranks = std::min((int64_t)s->rows / sa::PACKED_ROWS + s->n_seq, each * s->n_seq);
     const int group = s->H / s->H_kv;
-    // per key/value head at most a workgroup for each tile and query head, and two for its keys (above 128 columns)
-    const int64_t fit = kMostWorkgroups / (ranks * (group + 2));
+    // per key/value head at most two workgroups for each tile and query head (fp32 ones of 32 rows have 512 threads) and as many for
+    // its keys
+    const int64_t fit = kMostWorkgroups / (sa::most_tiles(a, s->dtype == SA_F32 ? 32 : 128) * 2 * (group + 1));
     if (fit < 1) return SA_ERR_SHAPE;
-    a.n_ranks = (int)ranks;
     const int heads = (int)std::min<int64_t>(fit, s->H_kv);
     for (int h = 0; h < s->H_kv; h += heads) {
         sa::PackedArgs part = a;

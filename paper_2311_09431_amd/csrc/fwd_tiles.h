@@ -255,7 +255,7 @@ fwd_mfma_kernel(Args p, int n_qtiles) {
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);      // wave-uniform, kept scalar
     int rank, bh, dev = p.q_dev;
     if constexpr (PACKED) {
-        if (!enter_sequence<true>(p, (int)blockIdx.x, p.H, n_qtiles, rank, bh)) return;
+        if (!enter_sequence<true, BM>(p, (int)blockIdx.x, p.H, n_qtiles, rank, bh)) return;
     } else {
         decode_block<true, BY_RANK>((int)blockIdx.x, RING ? n_qtiles * p.n_q : n_qtiles, p.B * p.H, rank, bh);
     }

@@ -11,12 +11,16 @@ namespace sa {
 struct PackedArgs : StepArgs {
     const int32_t* offsets;     // device, n_seq + 1
     int n_seq, rows, max_len;   // rows of the tensors; rows of a sequence beyond max_len are not looked at
-    int n_ranks;                // 128-row tiles of all sequences, at most
+    int n_ranks;                // tiles of all sequences, at most
     int es;                     // bytes of an element
     bool by_rank;               // workgroup order: by ranks over all heads, or in groups of heads (decode_block)
 };
 
-constexpr int PACKED_ROWS = 128;        // rows of a tile
+// Tiles of `tile` rows that the sequences can have, whatever their lengths
+inline int64_t most_tiles(const PackedArgs& p, int tile) {
+    const int64_t each = ((int64_t)p.max_len + tile - 1) / tile, by_rows = (int64_t)p.rows / tile + p.n_seq;
+    return each * p.n_seq < by_rows ? each * p.n_seq : by_rows;
+}
 
 // Rows first .. first + len - 1 of sequence s.  Whatever the offsets hold, they lie within the tensors: an offset below zero or
 // behind the last row is taken as the nearest one that is none, a sequence that ends before it begins is empty.
@@ -25,7 +29,8 @@ __device__ inline Span span_of(const PackedArgs& p, int s) {
     const int first = min(max(p.offsets[s], 0), p.rows), end = min(max(p.offsets[s + 1], first), p.rows);
     return {first, min(end - first, p.max_len)};
 }
-__device__ inline int tiles_of(Span x) { return (x.len + PACKED_ROWS - 1) / PACKED_ROWS; }
+template <int TILE>
+__device__ inline int tiles_of(Span x) { return (x.len + TILE - 1) / TILE; }
 
 __device__ inline int wave_add(int x) {
 #pragma unroll
@@ -38,22 +43,25 @@ hipError_t launch_packed_delta(const PackedArgs& p, const void* out, int dtype, 
 hipError_t launch_packed_bwd(const PackedArgs& p, hipStream_t st);
 hipError_t launch_packed_bwd_ring(const PackedArgs& p, hipStream_t st);       // dK and dV at 65 to 128 columns
 hipError_t launch_packed_f32(PackedArgs p, bool backward, hipStream_t st);
+hipError_t launch_packed_f32x3(PackedArgs p, bool backward, hipStream_t st);
+hipError_t launch_packed_f32x3_split(PackedArgs p, bool backward, hipStream_t st);
 
 // Tile `rank` of all sequences' tiles, the heaviest first: a sequence of t tiles has one of each weight 1 .. t (query tile i
 // walks i + 1 key tiles, key tile i is walked by t - i query tiles).  C(w) = sum over sequences of max(0, t - w + 1) tiles weigh w or
 // more; the tile's weight is the largest w with C(w) > rank, found by halving, and among the sequences that have one of it the tile is
 // that of number rank - C(w + 1).  Every wavefront looks for itself, 64 sequences at a time in its lanes.  False: fewer tiles than that.
+template <int TILE>
 __device__ inline bool find_tile(const PackedArgs& p, int rank, int& seq, int& weight) {
     const int lane = threadIdx.x & 63;
-    const int own = lane < p.n_seq ? tiles_of(span_of(p, lane)) : 0;      // of the first 64 sequences
+    const int own = lane < p.n_seq ? tiles_of<TILE>(span_of(p, lane)) : 0;      // of the first 64 sequences
     auto count = [&](int w) {
         int n = max(0, own - w + 1);
-        for (int s = 64 + lane; s < p.n_seq; s += 64) n += max(0, tiles_of(span_of(p, s)) - w + 1);
+        for (int s = 64 + lane; s < p.n_seq; s += 64) n += max(0, tiles_of<TILE>(span_of(p, s)) - w + 1);
         return __builtin_amdgcn_readfirstlane(wave_add(n));
     };
     int behind = count(1);
     if (rank >= behind) return false;
-    int lo = 1, hi = (p.max_len + PACKED_ROWS - 1) / PACKED_ROWS + 1;      // C(lo) > rank >= C(hi)
+    int lo = 1, hi = (p.max_len + TILE - 1) / TILE + 1;      // C(lo) > rank >= C(hi)
     behind = 0;
     while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1, c = count(mid);
@@ -66,7 +74,7 @@ __device__ inline bool find_tile(const PackedArgs& p, int rank, int& seq, int& w
     weight = lo;
     int left = rank - behind;           // so many sequences with such a tile come before it
     for (int s0 = 0; s0 < p.n_seq; s0 += 64) {
-        const int t = s0 == 0 ? own : s0 + lane < p.n_seq ? tiles_of(span_of(p, s0 + lane)) : 0;
+        const int t = s0 == 0 ? own : s0 + lane < p.n_seq ? tiles_of<TILE>(span_of(p, s0 + lane)) : 0;
         const uint64_t has = __builtin_amdgcn_ballot_w64(t >= lo);
         const int n = __builtin_popcountll(has);
         if (left < n) {
@@ -82,16 +90,16 @@ __device__ inline bool find_tile(const PackedArgs& p, int rank, int& seq, int& w
 
 // The workgroup's sequence, tile and head: p becomes the arguments of a launch on that sequence alone, n_tiles its tiles,
 // rank the tile's place among them (0: the heaviest).  False: none, the launch has more workgroups than there are tiles.
-template <bool SNAKE>
+template <bool SNAKE, int TILE>
 __device__ inline bool enter_sequence(PackedArgs& p, int linear, int n_heads, int& n_tiles, int& rank, int& head) {
     if (p.by_rank) decode_block<SNAKE, true>(linear, p.n_ranks, n_heads, rank, head);
     else decode_block<SNAKE, false>(linear, p.n_ranks, n_heads, rank, head);
     int seq, weight;
-    if (!find_tile(p, rank, seq, weight)) return false;
+    if (!find_tile<TILE>(p, rank, seq, weight)) return false;
     const Span x = span_of(p, seq);
     const int first = __builtin_amdgcn_readfirstlane(x.first);
     p.c = __builtin_amdgcn_readfirstlane(x.len);
-    n_tiles = (p.c + PACKED_ROWS - 1) / PACKED_ROWS;
+    n_tiles = (p.c + TILE - 1) / TILE;
     rank = n_tiles - weight;
     const int64_t q = p.es * p.stride_s * first, kv = p.es * p.kv_stride_s * first;         // bytes
     p.q = (const char*)p.q + q;
@@ -105,13 +113,6 @@ __device__ inline bool enter_sequence(PackedArgs& p, int linear, int n_heads, in
     p.lse += first;
     p.delta += first;
     return true;
-}
-
-// arguments of a row that is done over (f32_rows.h): of a packed sequence the workgroup's own, not the launch's
-template <bool PACKED>
-__device__ inline const StepArgs& row_args(const StepArgs& launch, const StepArgs& own) {
-    if constexpr (PACKED) return own;
-    else return launch;
 }
 
 }  // namespace sa

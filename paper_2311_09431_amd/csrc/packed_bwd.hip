@@ -42,7 +42,7 @@ packed_dq_kernel(PackedArgs p) {
     __shared__ __attribute__((aligned(1024))) char lds2[tile_bytes(DP) * halves_of(DP)];
     __shared__ __attribute__((aligned(1024))) char lds3[tile_bytes(DP) * halves_of(DP)];
     int n_tiles, rank, head;
-    if (!enter_sequence<true>(p, (int)blockIdx.x, p.H, n_tiles, rank, head)) return;
+    if (!enter_sequence<true, BM>(p, (int)blockIdx.x, p.H, n_tiles, rank, head)) return;
     bwd_dq<true, WALK_TRI, DP, PART, false, true>(p, n_tiles, rank * p.H + head, lds0, lds1, lds2, lds3);
 }
 
@@ -57,12 +57,13 @@ packed_dkdv_kernel(PackedArgs p) {
     __shared__ __attribute__((aligned(16))) float stat[KV_STAT_FLOATS];
     const int heads = p.H_kv * halves_of(DP);
     int n_tiles, rank, head;
-    if (!enter_sequence<false>(p, (int)blockIdx.x, heads, n_tiles, rank, head)) return;
+    if (!enter_sequence<false, BM>(p, (int)blockIdx.x, heads, n_tiles, rank, head)) return;
     bwd_dkdv<WALK_RING, true, DP, PART, false, true>(p, n_tiles, rank * heads + head, lds0, lds1, lds2, lds3, stat);
 }
 
 template <int DP, bool PART>
 hipError_t launch(PackedArgs p, hipStream_t st) {
+    p.n_ranks = (int)most_tiles(p, BM);
     const int64_t n_dq = (int64_t)p.n_ranks * p.H, n_dkdv = (int64_t)p.n_ranks * p.H_kv * halves_of(DP);
     p.by_rank = by_rank(true, n_dq, MOST_BY_RANK<DP, false>);
     hipLaunchKernelGGL((packed_dq_kernel<DP, PART>), dim3((unsigned)n_dq), dim3(256), 0, st, p);

@@ -13,7 +13,7 @@ packed_dkdv_ring_kernel(PackedArgs p) {
     __shared__ __attribute__((aligned(1024))) char lds[SLOTS * SLOT<DP>];
     __shared__ __attribute__((aligned(16))) float stat[STAT_FLOATS];
     int n_tiles, rank, head;
-    if (!enter_sequence<false>(p, (int)blockIdx.x, p.H_kv, n_tiles, rank, head)) return;
+    if (!enter_sequence<false, BM>(p, (int)blockIdx.x, p.H_kv, n_tiles, rank, head)) return;
     dkdv_ring<DP, PART, false, true>(p, n_tiles, rank * p.H_kv + head, lds, stat);
 }
 

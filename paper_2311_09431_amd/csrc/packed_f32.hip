@@ -1,5 +1,10 @@
-// Causal attention of packed sequences and its gradient, fp32 storage, on the fp32 matrix cores: the ring step's workgroups
-// (f32_tiles.h), each on one 128-row tile of one sequence (packed.h).
+// Causal attention of packed sequences and its gradient, fp32 storage: which kernels play a launch, and those on the fp32 matrix
+// cores, the ring step's workgroups (f32_tiles.h), each on one tile of one sequence (packed.h).
+//
+// Up to 128 columns three kinds of kernels compete, as for a ring step (f32_route.hip), and the same rule decides, for as many
+// sequences of their mean length: the lengths themselves are on the device.
+#include <algorithm>
+
 #include "f32_tiles.h"
 
 namespace sa {
@@ -7,38 +12,38 @@ namespace sa {
 namespace {
 
 // workgroups 0 .. n_dkdv - 1 own keys, the others queries; at 256 columns each kind in a launch of its own
-template <int DP, bool KEYS, bool QUERIES>
+template <int DP, int SPLIT, bool KEYS, bool QUERIES>
 __global__ void __launch_bounds__(64 * WAVES, DP > 64 ? 1 : 2)
 packed_bwd_f32_kernel(PackedArgs p, int n_dkdv) {
-    __shared__ __attribute__((aligned(16))) float lds[tile_floats<1, DP>()];
-    __shared__ float stats[KEYS ? 2 * tile_rows(1) : 1];
+    constexpr int ROWS = 32 * WAVES / SPLIT;
+    __shared__ __attribute__((aligned(16))) float lds[tile_floats<SPLIT, DP>()];
+    __shared__ float stats[KEYS ? 2 * tile_rows(SPLIT) : 1];        // LSE | delta of a tile's queries
     __shared__ uint32_t masks[WAVES];
     const int heads = p.H_kv * (DP > 128 ? 2 : 1);
     int n_tiles, rank, head;
     if (KEYS && (!QUERIES || (int)blockIdx.x < n_dkdv)) {
-        if (!enter_sequence<false>(p, (int)blockIdx.x, heads, n_tiles, rank, head)) return;
-        bwd_dkdv<float, DP, 1, true>(p, n_tiles, rank * heads + head, lds, stats, masks);
+        if (!enter_sequence<false, ROWS>(p, (int)blockIdx.x, heads, n_tiles, rank, head)) return;
+        bwd_dkdv<float, DP, SPLIT, true>(p, n_tiles, rank * heads + head, lds, stats, masks);
     } else if (QUERIES) {
-        if (!enter_sequence<true>(p, (int)blockIdx.x - (KEYS ? n_dkdv : 0), p.H, n_tiles, rank, head)) return;
-        bwd_dq<float, DP, 1, true>(p, n_tiles, rank * p.H + head, lds, masks);
+        if (!enter_sequence<true, ROWS>(p, (int)blockIdx.x - (KEYS ? n_dkdv : 0), p.H, n_tiles, rank, head)) return;
+        bwd_dq<float, DP, SPLIT, true>(p, n_tiles, rank * p.H + head, lds, masks);
     }
 }
 
-template <int DP>
-hipError_t fwd(const PackedArgs& p, hipStream_t st) {
-    hipLaunchKernelGGL((fwd_f32_kernel<float, DP, 1, PackedArgs>), dim3((unsigned)p.n_ranks * p.H), dim3(64 * WAVES), 0, st, p, 0);
-    return hipGetLastError();
-}
-template <int DP>
-hipError_t bwd(const PackedArgs& p, hipStream_t st) {
-    const unsigned n_dkdv = (unsigned)p.n_ranks * p.H_kv * (DP > 128 ? 2 : 1), n_dq = (unsigned)p.n_ranks * p.H;
+template <int DP, int SPLIT>
+hipError_t run(PackedArgs p, bool backward, hipStream_t st) {
+    const int64_t ranks = most_tiles(p, 32 * WAVES / SPLIT);
+    p.n_ranks = (int)ranks;
+    const unsigned n_dkdv = (unsigned)(ranks * p.H_kv) * (DP > 128 ? 2 : 1), n_dq = (unsigned)(ranks * p.H);
     const dim3 block(64 * WAVES);
-    if constexpr (DP <= 128) {
-        hipLaunchKernelGGL((packed_bwd_f32_kernel<DP, true, true>), dim3(n_dkdv + n_dq), block, 0, st, p, (int)n_dkdv);
+    if (!backward) {
+        hipLaunchKernelGGL((fwd_f32_kernel<float, DP, SPLIT, PackedArgs>), dim3(n_dq), block, 0, st, p, 0);
+    } else if constexpr (DP <= 128) {
+        hipLaunchKernelGGL((packed_bwd_f32_kernel<DP, SPLIT, true, true>), dim3(n_dkdv + n_dq), block, 0, st, p, (int)n_dkdv);
     } else {
-        hipLaunchKernelGGL((packed_bwd_f32_kernel<DP, false, true>), dim3(n_dq), block, 0, st, p, 0);
+        hipLaunchKernelGGL((packed_bwd_f32_kernel<DP, SPLIT, false, true>), dim3(n_dq), block, 0, st, p, 0);
         if (hipError_t e = hipGetLastError()) return e;
-        hipLaunchKernelGGL((packed_bwd_f32_kernel<DP, true, false>), dim3(n_dkdv), block, 0, st, p, (int)n_dkdv);
+        hipLaunchKernelGGL((packed_bwd_f32_kernel<DP, SPLIT, true, false>), dim3(n_dkdv), block, 0, st, p, (int)n_dkdv);
     }
     return hipGetLastError();
 }
@@ -47,10 +52,17 @@ hipError_t bwd(const PackedArgs& p, hipStream_t st) {
 
 hipError_t launch_packed_f32(PackedArgs p, bool backward, hipStream_t st) {
     p.by_rank = true;
-    if (p.d <= 32) return backward ? bwd<32>(p, st) : fwd<32>(p, st);
-    if (p.d <= 64) return backward ? bwd<64>(p, st) : fwd<64>(p, st);
-    if (p.d <= 128) return backward ? bwd<128>(p, st) : fwd<128>(p, st);
-    return backward ? bwd<256>(p, st) : fwd<256>(p, st);
+    StepArgs mean = p;
+    mean.B = p.n_seq;
+    mean.c = (int)std::min((int64_t)p.max_len, ((int64_t)p.rows + p.n_seq - 1) / p.n_seq);
+    if (p.d > 128) return few_row_tiles(mean, backward) ? run<256, 2>(p, backward, st) : run<256, 1>(p, backward, st);
+    StepArgs longest = p;
+    longest.c = p.max_len;
+    F32Route route = f32_route(mean, backward);
+    if (route == F32_SPLIT && !f32x3_split_supported(longest, backward)) route = F32_TERMS;
+    if (route == F32_SPLIT) return launch_packed_f32x3_split(p, backward, st);
+    if (route != F32_INSTRUCTION) return launch_packed_f32x3(p, backward, st);
+    return p.d <= 32 ? run<32, 4>(p, backward, st) : p.d <= 64 ? run<64, 4>(p, backward, st) : run<128, 4>(p, backward, st);
 }
 
 }  // namespace sa

@@ -19,6 +19,7 @@ hipError_t launch(const PackedArgs& p, hipStream_t st) {
 }  // namespace
 
 hipError_t launch_packed_fwd(PackedArgs p, hipStream_t st) {
+    p.n_ranks = (int)most_tiles(p, BM);
     const int64_t workgroups = (int64_t)p.n_ranks * p.H;
     p.by_rank = by_rank(true, workgroups, p.d > 128 ? MOST_BY_RANK<256, true> : p.d > 112 ? MOST_BY_RANK<128, true> : MOST_BY_RANK<64, true>);
     const bool part = p.d % 8 != 0;
