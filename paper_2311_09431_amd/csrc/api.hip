@@ -259,6 +259,8 @@ int check_decode(const sa_decode* s, const sa_cache* c) {
     if (int e = check_cache(c)) return e;
     if (s->B < 0 || s->H < 1 || s->H % c->H_kv || s->max_pages < 0) return SA_ERR_SHAPE;
     if ((int64_t)s->B * s->H > kMostWorkgroups || (int64_t)s->max_pages * c->page_size > (int64_t(1) << 30)) return SA_ERR_SHAPE;
+    // (chunks of all units are numbered in 31 bits)
+    if (((int64_t)s->max_pages * c->page_size / 64 + 1) * s->B * s->H >= (int64_t(1) << 31)) return SA_ERR_SHAPE;
     if (s->stride_h < c->d || (s->B > 1 && (s->stride_b < s->H * s->stride_h || s->stat_stride_b < s->H))) return SA_ERR_SHAPE;
     if (s->B > 1 && s->table_stride < s->max_pages) return SA_ERR_SHAPE;
     return s->stride_b % 4 || s->stride_h % 4 ? SA_ERR_ALIGN : SA_OK;
@@ -548,7 +550,6 @@ int sa_attn_packed_bwd(const void* q, const void* k, const void* v, const void* 
     a.o = (float*)const_cast<void*>(out);
     a.dq = (float*)dq; a.dk = (float*)dk; a.dv = (float*)dv;
     return play_packed(shape, offsets, a, [&](const sa::PackedArgs& p) {
-        if (hipError_t e = sa::launch_packed_delta(p, p.o, shape->dtype, st)) return e;
         return shape->dtype == SA_F32 ? sa::launch_packed_f32(p, true, st) : sa::launch_packed_bwd(p, st);
     });
 }

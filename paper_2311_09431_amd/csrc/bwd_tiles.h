@@ -216,7 +216,21 @@ __device__ __forceinline__ void bwd_dq(const StepArgs& p, int n_tiles, int linea
     load_b_frags<8 * NH>(gf, G + (int64_t)a * ss, h, d);
     const float kappa = p.scale * LOG2E;
     float lse2 = p.lse[sbase + a] * LOG2E;
-    float delta = p.delta[sbase + a];
+    float delta;
+    if constexpr (PACKED) {
+        // formed here, from the rows that the lane holds anyway, and stored for the key-owning workgroups behind this launch
+        bf16x8 of[8 * NH];
+        load_b_frags<8 * NH>(of, (const __bf16*)p.o + base + (int64_t)a * ss, h, d);
+        float x = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8 * NH; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x = fmaf((float)of[i][e], (float)gf[i][e], x);
+        delta = half_wave_sum(x);
+        if (h == 0 && row_ok) const_cast<float*>(p.delta)[sbase + a] = delta;
+    } else {
+        delta = p.delta[sbase + a];
+    }
     f32x16 acc[4 * NH];
 #pragma unroll
     for (int mb = 0; mb < 4 * NH; ++mb)

@@ -27,6 +27,7 @@
 
 #include "mfma_tiles.h"
 #include "paged.h"
+#include "wave.h"
 
 namespace sa {
 
@@ -72,49 +73,39 @@ __device__ inline void add_sum(float& sum, bool& weightless, float l, float fact
     sum += (l < 0.f ? 0.f : l) * factor;
 }
 __device__ inline int scalar(int x) { return __builtin_amdgcn_readfirstlane(x); }
-__device__ inline int64_t scalar64(int64_t x) {
-    return (int64_t)((uint64_t)(uint32_t)scalar((int)(x >> 32)) << 32 | (uint32_t)scalar((int)x));
-}
-
 template <typename T>
 __device__ inline int chunks_of(const DecodeArgs& p, int b) {
-    const int64_t room = (int64_t)p.max_pages * p.page_size;
-    const int len = (int)min((int64_t)max(p.lens[b], 0), room);
+    const int len = min(max(p.lens[b], 0), p.max_pages * p.page_size);
     return (len + CHUNK<T> - 1) / CHUNK<T>;
-}
-__device__ inline int wave_scan(int x, int lane) {          // inclusive
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const int y = __shfl_up(x, o);
-        if (lane >= o) x += y;
-    }
-    return x;
 }
 // units of a sequence
 __device__ inline int units_of(const DecodeArgs& p) { return p.H_kv * ((p.H / p.H_kv + HEADS - 1) / HEADS); }
 
-// Chunks of all sequences (a wavefront's lanes take them in turn), and the sequence in which chunk number `at` of them lies with the
-// chunks before it; found: at >= 0 and there is one.
-struct Where { int64_t all, before; int seq; };
+// Where chunk number `at` of all units' chunks lies: the sequence, the chunks of the sequences before it (of one unit); and the share of a
+// workgroup.  A wavefront's lanes take the sequences in turn.  (All counts are below 2^31: check_decode.)
+struct Shares { int all, each; };
 template <typename T>
-__device__ inline int64_t all_chunks(const DecodeArgs& p, int lane) {
-    int64_t n = 0;
-    for (int b0 = 0; b0 < p.B; b0 += 64) n += __shfl(wave_scan(b0 + lane < p.B ? chunks_of<T>(p, b0 + lane) : 0, lane), 63);
-    return n;
+__device__ inline Shares shares_of(const DecodeArgs& p, int units, int lane) {
+    int n = 0;
+    for (int b0 = 0; b0 < p.B; b0 += 64) n += b0 + lane < p.B ? chunks_of<T>(p, b0 + lane) : 0;
+    const int all = wave_total(wave_scan(n)) * units;
+    return {all, max(1, (int)(((uint32_t)all + (uint32_t)p.n_wgs - 1) / (uint32_t)p.n_wgs))};
 }
 template <typename T>
-__device__ inline Where find_chunk(const DecodeArgs& p, int64_t at, int lane) {
-    int64_t before = 0;
+__device__ inline void find_chunk(const DecodeArgs& p, int at, int units, int lane, int& seq, int& before) {
+    before = 0;
     for (int b0 = 0; b0 < p.B; b0 += 64) {
-        const int own = b0 + lane < p.B ? chunks_of<T>(p, b0 + lane) : 0, upto = wave_scan(own, lane);
-        const uint64_t past = __builtin_amdgcn_ballot_w64(before + upto > at);
+        const int own = b0 + lane < p.B ? chunks_of<T>(p, b0 + lane) : 0, upto = wave_scan(own);
+        const uint64_t past = __builtin_amdgcn_ballot_w64((before + upto) * units > at);
         if (past) {
             const int l = (int)__builtin_ctzll(past);
-            return {0, before + __shfl(upto - own, l), b0 + l};
+            before += __builtin_amdgcn_readlane(upto - own, l);
+            seq = b0 + l;
+            return;
         }
-        before += __shfl(upto, 63);
+        before += wave_total(upto);
     }
-    return {0, before, p.B};
+    seq = p.B;              // (not reached: `at` is one of them)
 }
 
 // A unit's piece in the workspace: HEADS rows (as many as the group has) of DP columns, then references and row sums.
@@ -135,26 +126,25 @@ decode_kernel(DecodeArgs p) {
     const int lane = threadIdx.x & 63, n = lane & 15, j = lane >> 4;
     const int wave = scalar((int)threadIdx.x >> 6);
     const int group = p.H / p.H_kv, blocks = (group + HEADS - 1) / HEADS, units = p.H_kv * blocks, d = p.d;
-    const int64_t all = scalar64(all_chunks<T>(p, lane)) * units;
-    const int64_t share = (all + p.n_wgs - 1) / p.n_wgs;
-    int64_t at = (int64_t)blockIdx.x * share;
-    const int64_t end = min(at + share, all);
-    if (at >= end) return;
+    const Shares shares = shares_of<T>(p, units, lane);
+    if ((int64_t)blockIdx.x * shares.each >= shares.all) return;
+    int at = (int)blockIdx.x * shares.each;
+    const int end = at + min(shares.each, shares.all - at);
     // where the share begins: sequence, unit of it, chunk of that
     int b, unit, chunk, n_chunks, len;
-    const int64_t room = (int64_t)p.max_pages * p.page_size;
+    const int room = p.max_pages * p.page_size;
     auto enter = [&]() {
-        len = scalar((int)min((int64_t)max(p.lens[b], 0), room));
+        len = scalar(min(max(p.lens[b], 0), room));
         n_chunks = (len + CHUNK<T> - 1) / CHUNK<T>;
     };
     {
         // (a sequence's chunks, unit by unit, follow those of all sequences before it)
-        const Where w = find_chunk<T>(p, at / units, lane);
-        b = scalar(w.seq);
+        int before;
+        find_chunk<T>(p, at, units, lane, b, before);
         enter();
-        const int64_t in = at - scalar64(w.before) * units;
-        unit = (int)(in / n_chunks);
-        chunk = (int)(in - (int64_t)unit * n_chunks);
+        const int in = at - before * units;
+        unit = (int)((uint32_t)in / (uint32_t)n_chunks);
+        chunk = in - unit * n_chunks;
     }
     const float kappa = p.scale * LOG2E;
     const int pitch = (int)p.stride_slot * ES;              // bytes between tokens of a page
@@ -178,7 +168,7 @@ decode_kernel(DecodeArgs p) {
     while (at < end) {
         const int kvh = unit / blocks, h0 = kvh * group + (unit - kvh * blocks) * HEADS;
         const int n_heads = min(HEADS, (kvh + 1) * group - h0);
-        const int first = chunk, last = (int)min((int64_t)n_chunks, chunk + (end - at));       // chunks of the unit in this share
+        const int first = chunk, last = min(n_chunks, chunk + (end - at));       // chunks of the unit in this share
         u32x4 q[KS];
         const bool has_head = n < n_heads;
         const T* q_row = (const T*)p.q + b * p.stride_b + (h0 + (has_head ? n : 0)) * p.stride_h;
@@ -465,17 +455,18 @@ decode_join_kernel(DecodeArgs p) {
     const int group = p.H / p.H_kv, blocks = (group + HEADS - 1) / HEADS, units = p.H_kv * blocks;
     const int b = (int)blockIdx.x / p.H, head = (int)blockIdx.x - b * p.H;
     const int kvh = head / group, in_group = head - kvh * group, unit = kvh * blocks + in_group / HEADS, row = in_group % HEADS;
-    int64_t before = 0, all = 0;
+    // (in one pass: the chunks of the sequences before b, and all)
+    int before = 0, all = 0;
     for (int b0 = 0; b0 < p.B; b0 += 64) {
-        const int own = b0 + lane < p.B ? chunks_of<T>(p, b0 + lane) : 0, upto = wave_scan(own, lane);
-        if (b >= b0 && b < b0 + 64) before = all + __shfl(upto - own, b - b0);
-        all += __shfl(upto, 63);
+        const int own = b0 + lane < p.B ? chunks_of<T>(p, b0 + lane) : 0;
+        all += own;
+        before += b0 + lane < b ? own : 0;
     }
-    before = scalar64(before);
-    all = scalar64(all) * units;
+    all = wave_total(wave_scan(all)) * units;
+    before = wave_total(wave_scan(before));
     const int n = scalar(chunks_of<T>(p, b));
-    const int64_t share = max((int64_t)1, (all + p.n_wgs - 1) / p.n_wgs);
-    const int64_t from = before * units + (int64_t)unit * n;
+    const uint32_t share = (uint32_t)max(1, (int)(((uint32_t)all + (uint32_t)p.n_wgs - 1) / (uint32_t)p.n_wgs));
+    const uint32_t from = (uint32_t)(before * units + unit * n);
     const int g0 = (int)(from / share), g1 = n ? (int)((from + n - 1) / share) : g0;
     if (n && g0 == g1) return;
     float m = -INFINITY, l = 0.f, acc[COLS] = {};

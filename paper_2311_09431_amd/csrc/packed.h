@@ -4,6 +4,7 @@
 #pragma once
 #include "mfma_tiles.h"
 #include "sa_internal.h"
+#include "wave.h"
 
 namespace sa {
 
@@ -32,16 +33,13 @@ __device__ inline Span span_of(const PackedArgs& p, int s) {
 template <int TILE>
 __device__ inline int tiles_of(Span x) { return (x.len + TILE - 1) / TILE; }
 
-__device__ inline int wave_add(int x) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o);
-    return x;
-}
-
 hipError_t launch_packed_fwd(PackedArgs p, hipStream_t st);
-hipError_t launch_packed_delta(const PackedArgs& p, const void* out, int dtype, hipStream_t st);
 hipError_t launch_packed_bwd(const PackedArgs& p, hipStream_t st);
 hipError_t launch_packed_bwd_ring(const PackedArgs& p, hipStream_t st);       // dK and dV at 65 to 128 columns
+// bf16 launches of few tiles (the backward's forms delta too)
+bool packed_split_wanted(const PackedArgs& p, bool backward);
+hipError_t launch_packed_split(PackedArgs p, bool backward, hipStream_t st);
+hipError_t launch_packed_delta(const PackedArgs& p, int dtype, hipStream_t st);
 hipError_t launch_packed_f32(PackedArgs p, bool backward, hipStream_t st);
 hipError_t launch_packed_f32x3(PackedArgs p, bool backward, hipStream_t st);
 hipError_t launch_packed_f32x3_split(PackedArgs p, bool backward, hipStream_t st);
@@ -57,7 +55,7 @@ __device__ inline bool find_tile(const PackedArgs& p, int rank, int& seq, int& w
     auto count = [&](int w) {
         int n = max(0, own - w + 1);
         for (int s = 64 + lane; s < p.n_seq; s += 64) n += max(0, tiles_of<TILE>(span_of(p, s)) - w + 1);
-        return __builtin_amdgcn_readfirstlane(wave_add(n));
+        return wave_total(wave_scan(n));
     };
     int behind = count(1);
     if (rank >= behind) return false;

@@ -1,38 +1,11 @@
 // Gradient of causal attention over packed sequences, bf16: the ring step's workgroups (bwd_tiles.h; dK and dV at 65 to 128 columns: packed_bwd_ring.hip), each on one
-// 128-row tile of one sequence (packed.h), and delta = rowsum(dO * O) before them.
+// 128-row tile of one sequence (packed.h).  The query-owning ones come first and form delta = rowsum(dO * O) of their rows for both.
 #include "bwd_tiles.h"
-#include "f32_rows.h"
 #include "packed.h"
 
 namespace sa {
 
 namespace {
-
-// 16 lanes a row and head, eight columns a lane and turn
-template <typename T>
-__global__ void __launch_bounds__(256)
-packed_delta_kernel(const T* __restrict__ o, const T* __restrict__ dout, float* __restrict__ delta, int rows, int H, int d, int64_t sh,
-                    int64_t ss, int64_t stat_sh) {
-    const int l = threadIdx.x & 15;
-    const int64_t n = (int64_t)rows * H;
-    for (int64_t i = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4); i < n; i += (int64_t)gridDim.x * 16) {
-        const int64_t row = i / H;
-        const int h = (int)(i - row * H);
-        const int64_t at = row * ss + h * sh;
-        float acc = 0.f;
-        for (int t = 8 * l; t < d; t += 128) {
-            float4 x = ld4<T>(o + at + t), y = ld4<T>(dout + at + t);
-            acc += x.x * y.x + x.y * y.y + x.z * y.z + x.w * y.w;
-            if (t + 4 >= d) break;
-            x = ld4<T>(o + at + t + 4);
-            y = ld4<T>(dout + at + t + 4);
-            acc += x.x * y.x + x.y * y.y + x.z * y.z + x.w * y.w;
-        }
-#pragma unroll
-        for (int by = 8; by > 0; by >>= 1) acc += __shfl_xor(acc, by, 16);
-        if (l == 0) delta[h * stat_sh + row] = acc;
-    }
-}
 
 template <int DP, bool PART>
 __global__ void __launch_bounds__(256, DP > 128 ? 1 : 2)
@@ -47,8 +20,9 @@ packed_dq_kernel(PackedArgs p) {
 }
 
 // up to 64 columns and above 128
-template <int DP, bool PART>
-__global__ void __launch_bounds__(256, DP > 64 ? 1 : 2)
+// WAVES: wavefronts a SIMD that the register budget is cut for; at 64 columns two spill 147 registers.
+template <int DP, bool PART, int WAVES>
+__global__ void __launch_bounds__(256, WAVES)
 packed_dkdv_kernel(PackedArgs p) {
     __shared__ __attribute__((aligned(1024))) char lds0[tile_bytes(DP) * halves_of(DP)];
     __shared__ __attribute__((aligned(1024))) char lds1[tile_bytes(DP) * halves_of(DP)];
@@ -61,35 +35,40 @@ packed_dkdv_kernel(PackedArgs p) {
     bwd_dkdv<WALK_RING, true, DP, PART, false, true>(p, n_tiles, rank * heads + head, lds0, lds1, lds2, lds3, stat);
 }
 
+// At 64 columns two wavefronts a SIMD are faster where many long walks hide each other's latency, whole training pass, us, one : two:
+// 2 x 8192 rows, 32 heads, 2506 : 2296, 8192, 16 heads, 688 : 677; but 6 of up to 4096, 16 heads, 713 : 717, 16 of up to 1000, 32
+// heads, 294 : 341, 4 of up to 500, 16 heads, 41 : 52, and with four query heads to a key/value head 8192, 32 heads, 1305 : 1415.
+template <int DP, bool PART>
+hipError_t launch_dkdv(const PackedArgs& p, hipStream_t st, int64_t n) {
+    if constexpr (DP <= 64) {
+        if (DP == 32 || (p.H == p.H_kv && p.max_len >= 8192 && n > 2 * N_CU)) {
+            hipLaunchKernelGGL((packed_dkdv_kernel<DP, PART, 2>), dim3((unsigned)n), dim3(256), 0, st, p);
+            return hipGetLastError();
+        }
+    }
+    if constexpr (DP != 32) hipLaunchKernelGGL((packed_dkdv_kernel<DP, PART, 1>), dim3((unsigned)n), dim3(256), 0, st, p);
+    return hipGetLastError();
+}
+
 template <int DP, bool PART>
 hipError_t launch(PackedArgs p, hipStream_t st) {
     p.n_ranks = (int)most_tiles(p, BM);
     const int64_t n_dq = (int64_t)p.n_ranks * p.H, n_dkdv = (int64_t)p.n_ranks * p.H_kv * halves_of(DP);
-    p.by_rank = by_rank(true, n_dq, MOST_BY_RANK<DP, false>);
+    // Query-owning workgroups in groups of heads, key-owning ones at 65 to 128 columns by ranks.  Whole training pass, us, queries and keys
+    // in groups, queries by ranks, keys, both: d 100, 6 sequences of up to 4096, 32 heads, 2258, 2331, 2253, 2335, 16 of up to 1000 467,
+    // 463, 456, 454; d 128 2332, 2381, 2342, 2391, 64 of up to 128, 16 heads, 97, 96, 95, 94; d 64 1481, 1482, 1503, 1498.
+    p.by_rank = false;
     hipLaunchKernelGGL((packed_dq_kernel<DP, PART>), dim3((unsigned)n_dq), dim3(256), 0, st, p);
     if (hipError_t e = hipGetLastError()) return e;
-    p.by_rank = by_rank(true, n_dkdv, MOST_BY_RANK<DP, false>);
+    p.by_rank = DP == 112 || DP == 128;
     if constexpr (DP == 112 || DP == 128) return launch_packed_bwd_ring(p, st);
-    else hipLaunchKernelGGL((packed_dkdv_kernel<DP, PART>), dim3((unsigned)n_dkdv), dim3(256), 0, st, p);
-    return hipGetLastError();
+    else return launch_dkdv<DP, PART>(p, st, n_dkdv);
 }
 
 }  // namespace
 
-hipError_t launch_packed_delta(const PackedArgs& p, const void* out, int dtype, hipStream_t st) {
-    int64_t g = ((int64_t)p.rows * p.H + 15) / 16;
-    if (g > 16384) g = 16384;
-    auto go = [&](auto* o) {
-        using T = std::remove_const_t<std::remove_pointer_t<decltype(o)>>;
-        hipLaunchKernelGGL(packed_delta_kernel<T>, dim3((unsigned)g), dim3(256), 0, st, o, (const T*)p.dout, const_cast<float*>(p.delta),
-                           p.rows, p.H, p.d, p.stride_h, p.stride_s, p.stat_stride_h);
-    };
-    if (dtype == SA_F32) go((const float*)out);
-    else go((const __hip_bfloat16*)out);
-    return hipGetLastError();
-}
-
 hipError_t launch_packed_bwd(const PackedArgs& p, hipStream_t st) {
+    if (packed_split_wanted(p, true)) return launch_packed_split(p, true, st);
     const bool part = p.d % 8 != 0;
     if (p.d > 128) return part ? launch<256, true>(p, st) : launch<256, false>(p, st);
     if (p.d <= 32 && !part) return launch<32, false>(p, st);

@@ -51,6 +51,8 @@ hipError_t run(PackedArgs p, bool backward, hipStream_t st) {
 }  // namespace
 
 hipError_t launch_packed_f32(PackedArgs p, bool backward, hipStream_t st) {
+    if (backward)
+        if (hipError_t e = launch_packed_delta(p, SA_F32, st)) return e;
     p.by_rank = true;
     StepArgs mean = p;
     mean.B = p.n_seq;

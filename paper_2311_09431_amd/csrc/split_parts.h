@@ -165,15 +165,16 @@ struct KeyCursor {
 
 // Forward, the end: the wavefronts' partial results (accumulators, base-2 reference m, half-wave row sum l) folded
 // into the running state of the lane's row (base: of the workgroup's rows' matrix, a: the row, clamped to the shard).
-// Returns the rows to do over (EXACT only; TERMS: V was three bf16 terms, masks are the words of RowsToRedo).
-template <int DP, int WAVES, bool EXACT, bool TERMS, typename Lane>
+// Returns the rows to do over (EXACT only; TERMS: V was three bf16 terms, masks are the words of RowsToRedo).  OutT: float, or __bf16
+// for rows that end here (packed sequences, p.fresh).
+template <int DP, int WAVES, bool EXACT, bool TERMS, typename Lane, typename OutT>
 __device__ __forceinline__ uint32_t fold_forward(const StepArgs& p, f32x16 (&acc)[4], float m, float l, char* lds, float* stats,
-                                                 uint32_t* masks, const Lane& ln, int dev, int a_own, int a, float* L, float* O) {
+                                                 uint32_t* masks, const Lane& ln, int dev, int a_own, int a, float* L, OutT* O) {
     constexpr int MB = blocks_of(DP), N = share_of(DP, WAVES);
     const int n = ln.n, h = ln.h, d = p.d;
     const float old = p.fresh ? -INFINITY : *L;
     float4 o_old[N];
-    load_old<DP, WAVES>(o_old, O, d, !p.fresh && a_own < p.c, ln);
+    if constexpr (sizeof(OutT) == 4) load_old<DP, WAVES>(o_old, O, d, !p.fresh && a_own < p.c, ln);
     const float top_acc = TERMS ? loudest<MB>(acc) : 0.f;           // (beside the loads)
     // the wavefronts' partial results against a common reference
     const float l_own = half_wave_sum(l);
@@ -218,17 +219,23 @@ __device__ __forceinline__ uint32_t fold_forward(const StepArgs& p, f32x16 (&acc
         for (int i = 0; i < N; ++i) {
             const int col = column_of<DP, WAVES>(i, ln);
             if (col >= d) continue;
-            float4* dst = reinterpret_cast<float4*>(O + col);
-            const float4 s = take_sum<DP, WAVES>(lds, i, ln);
-            float4 x = o_old[i];
-            if (f_old != 0.f) {
-                x.x *= f_old; x.y *= f_old; x.z *= f_old; x.w *= f_old;
-            } else {                    // an empty state: nothing of O is looked at
-                x = make_float4(0.f, 0.f, 0.f, 0.f);
+            if constexpr (sizeof(OutT) == 2) {
+                const float4 s = take_sum<DP, WAVES>(lds, i, ln);
+                const bf16x4 y = {(__bf16)(s.x * f_part), (__bf16)(s.y * f_part), (__bf16)(s.z * f_part), (__bf16)(s.w * f_part)};
+                *reinterpret_cast<bf16x4*>(O + col) = y;
+            } else {
+                float4* dst = reinterpret_cast<float4*>(O + col);
+                const float4 s = take_sum<DP, WAVES>(lds, i, ln);
+                float4 x = o_old[i];
+                if (f_old != 0.f) {
+                    x.x *= f_old; x.y *= f_old; x.z *= f_old; x.w *= f_old;
+                } else {                    // an empty state: nothing of O is looked at
+                    x = make_float4(0.f, 0.f, 0.f, 0.f);
+                }
+                x.x = fmaf(s.x, f_part, x.x); x.y = fmaf(s.y, f_part, x.y);
+                x.z = fmaf(s.z, f_part, x.z); x.w = fmaf(s.w, f_part, x.w);
+                *dst = x;
             }
-            x.x = fmaf(s.x, f_part, x.x); x.y = fmaf(s.y, f_part, x.y);
-            x.z = fmaf(s.z, f_part, x.z); x.w = fmaf(s.w, f_part, x.w);
-            *dst = x;
         }
         if (ln.wave == 0 && h == 0) *L = top + logf(w_sum);
     }
@@ -247,6 +254,19 @@ __device__ inline void add_rows(float* row, float4 (&x)[share_of(DP, WAVES)], co
         x[i].x = fmaf(scale, s.x, x[i].x); x[i].y = fmaf(scale, s.y, x[i].y);
         x[i].z = fmaf(scale, s.z, x[i].z); x[i].w = fmaf(scale, s.w, x[i].w);
         *reinterpret_cast<float4*>(row + col) = x[i];
+    }
+}
+
+// scale * (sum of the partial results at buf), rounded once, as the lane's row
+template <int DP, int WAVES, typename Lane>
+__device__ inline void set_rows(__bf16* row, const char* buf, float scale, int d, const Lane& ln) {
+#pragma unroll
+    for (int i = 0; i < share_of(DP, WAVES); ++i) {
+        const int col = column_of<DP, WAVES>(i, ln);
+        if (col >= d) continue;
+        const float4 s = take_sum<DP, WAVES>(buf, i, ln);
+        const bf16x4 y = {(__bf16)(scale * s.x), (__bf16)(scale * s.y), (__bf16)(scale * s.z), (__bf16)(scale * s.w)};
+        *reinterpret_cast<bf16x4*>(row + col) = y;
     }
 }
 

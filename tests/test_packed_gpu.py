@@ -297,3 +297,11 @@ def test_as_the_ring_step():
     # the step's state passes through fp32 once more before it is rounded
     assert (out.permute(1, 0, 2).float() - done[0].float()).abs().max() <= 2.0 ** -8 * done.float().abs().max()
     assert (lse - L[0]).abs().max() <= 1e-5
+
+
+# 32-row and 128-row workgroups, forward and backward each (launches of few and of many tiles), at every number of columns computed
+@pytest.mark.parametrize("d", [32, 64, 100, 128])
+@pytest.mark.parametrize("H,H_kv,lens", [(4, 1, [200, 31, 1, 65]), (24, 24, [500, 33, 257]), (32, 4, [900, 129, 64]), (48, 2, [257, 31])])
+def test_few_and_many_tiles(H, H_kv, lens, d):
+    r = run(lens, H, H_kv, d, BF16)
+    compare(lens, H, H_kv, d, BF16, 0, *r, heads={0, H_kv - 1})
