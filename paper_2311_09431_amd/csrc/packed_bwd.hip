@@ -1,6 +1,7 @@
 // Gradient of causal attention over packed sequences, bf16: the ring step's workgroups (bwd_tiles.h; dK and dV at 65 to 128 columns: packed_bwd_ring.hip), each on one
 // 128-row tile of one sequence (packed.h).  The query-owning ones come first and form delta = rowsum(dO * O) of their rows for both.
 #include "bwd_tiles.h"
+#include "bwd_wide_tiles.h"
 #include "packed.h"
 
 namespace sa {
@@ -38,11 +39,20 @@ packed_dkdv_kernel(PackedArgs p) {
 // At 64 columns two wavefronts a SIMD are faster where many long walks hide each other's latency, whole training pass, us, one : two:
 // 2 x 8192 rows, 32 heads, 2506 : 2296, 8192, 16 heads, 688 : 677; but 6 of up to 4096, 16 heads, 713 : 717, 16 of up to 1000, 32
 // heads, 294 : 341, 4 of up to 500, 16 heads, 41 : 52, and with four query heads to a key/value head 8192, 32 heads, 1305 : 1415.
+// Above 128 columns workgroups with all of them from 160 tiles on, whole training pass, d 256, us, halves : all: 4 of up to 500, 16 heads,
+// 110 : 104, 8 of up to 1000 267 : 219, 6 of up to 4096, 8 heads, 1568 : 1273; but (fewer tiles) 2 of up to 1000, 4 heads, 140 : 153, 8 of up
+// to 1000, 16 heads on 4, 308 : 342.
 template <int DP, bool PART>
 hipError_t launch_dkdv(const PackedArgs& p, hipStream_t st, int64_t n) {
     if constexpr (DP <= 64) {
         if (DP == 32 || (p.H == p.H_kv && p.max_len >= 8192 && n > 2 * N_CU)) {
             hipLaunchKernelGGL((packed_dkdv_kernel<DP, PART, 2>), dim3((unsigned)n), dim3(256), 0, st, p);
+            return hipGetLastError();
+        }
+    }
+    if constexpr (DP == 256 && !PART) {
+        if (n / 2 > 5 * N_CU / 8) {
+            hipLaunchKernelGGL((bwd_dkdv_wide_kernel<false, PackedArgs>), dim3((unsigned)(n / 2)), dim3(256), 0, st, p, 0);
             return hipGetLastError();
         }
     }

@@ -300,7 +300,8 @@ def test_as_the_ring_step():
 
 
 # 32-row and 128-row workgroups, forward and backward each (launches of few and of many tiles), at every number of columns computed
-@pytest.mark.parametrize("d", [32, 64, 100, 128])
+# (above 128 columns: halves of dK and dV, and all columns, in a workgroup)
+@pytest.mark.parametrize("d", [32, 64, 100, 128, 256])
 @pytest.mark.parametrize("H,H_kv,lens", [(4, 1, [200, 31, 1, 65]), (24, 24, [500, 33, 257]), (32, 4, [900, 129, 64]), (48, 2, [257, 31])])
 def test_few_and_many_tiles(H, H_kv, lens, d):
     r = run(lens, H, H_kv, d, BF16)
