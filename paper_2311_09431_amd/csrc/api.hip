@@ -582,7 +582,7 @@ int sa_cache_append(const void* q, void* q_out, const void* k, void* k_out, cons
 
 int64_t sa_attn_decode_workspace(const sa_decode* shape, const sa_cache* cache) {
     if (int e = check_decode(shape, cache)) return e;
-    return sa::decode_workspace(shape->H, cache->H_kv, cache->d, cache->dtype);
+    return sa::decode_workspace(shape->H, cache->H_kv, cache->d);
 }
 
 int sa_attn_decode(const void* q, const void* k_cache, const void* v_cache, const int32_t* table, const int32_t* lens, void* out,
@@ -590,7 +590,7 @@ int sa_attn_decode(const void* q, const void* k_cache, const void* v_cache, cons
     if (int e = check_decode(shape, cache)) return e;
     if (shape->B == 0) return SA_OK;
     if (!q || !k_cache || !v_cache || !lens || !out || !workspace || (!table && shape->max_pages > 0)) return SA_ERR_NULL;
-    if (workspace_bytes < sa::decode_workspace(shape->H, cache->H_kv, cache->d, cache->dtype)) return SA_ERR_SHAPE;
+    if (workspace_bytes < sa::decode_workspace(shape->H, cache->H_kv, cache->d)) return SA_ERR_SHAPE;
     for (const void* p : {q, k_cache, v_cache, (const void*)out, (const void*)workspace})
         if (!aligned16(p)) return SA_ERR_ALIGN;
     if ((reinterpret_cast<uintptr_t>(table) | reinterpret_cast<uintptr_t>(lens) | reinterpret_cast<uintptr_t>(lse)) & 3u) return SA_ERR_ALIGN;

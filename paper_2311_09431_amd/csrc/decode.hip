@@ -40,13 +40,13 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 constexpr int WAVES = 4, HEADS = 16;            // wavefronts a workgroup, query heads a unit
 constexpr float MOST = 16777216.f;              // 2^24: a lane's sum of a tile against a reference that stays
 
-// Of a storage type and DP columns computed: tokens a tile, columns of a V row a lane loads at once, loads a V row
+// Of a storage type and DP columns computed: tokens a tile, columns of a product over them, columns of a V row a lane loads at once
 template <typename T, int DP> struct Of;
 template <int DP> struct Of<__hip_bfloat16, DP> {
-    static constexpr int TILE = 32, STEP = 32, CW = DP >= 128 ? 8 : 4, ES = 2;
+    static constexpr int TILE = 32, STEP = 32, CW = DP >= 128 ? 8 : DP / 16, ES = 2;
 };
 template <int DP> struct Of<float, DP> {
-    static constexpr int TILE = 16, STEP = 16, CW = 4, ES = 4;
+    static constexpr int TILE = 16, STEP = 16, CW = DP >= 64 ? 4 : DP / 16, ES = 4;
 };
 template <typename T> constexpr int CHUNK = WAVES * Of<T, 64>::TILE;
 
@@ -112,7 +112,8 @@ __device__ inline void find_chunk(const DecodeArgs& p, int at, int units, int la
 __host__ __device__ inline int part_rows(int group) { return group < HEADS ? group : HEADS; }
 __host__ __device__ inline int64_t part_floats(int group, int DP) { return (int64_t)part_rows(group) * (DP + 2); }
 
-template <typename T, int DP>
+// WHOLE: a workgroup has one unit, all of it, and there is nothing to join.
+template <typename T, int DP, bool WHOLE>
 __global__ void __launch_bounds__(64 * WAVES, DP > 128 ? 1 : 2)
 decode_kernel(DecodeArgs p) {
     using O = Of<T, DP>;
@@ -126,18 +127,29 @@ decode_kernel(DecodeArgs p) {
     const int lane = threadIdx.x & 63, n = lane & 15, j = lane >> 4;
     const int wave = scalar((int)threadIdx.x >> 6);
     const int group = p.H / p.H_kv, blocks = (group + HEADS - 1) / HEADS, units = p.H_kv * blocks, d = p.d;
-    const Shares shares = shares_of<T>(p, units, lane);
-    if ((int64_t)blockIdx.x * shares.each >= shares.all) return;
-    int at = (int)blockIdx.x * shares.each;
-    const int end = at + min(shares.each, shares.all - at);
-    // where the share begins: sequence, unit of it, chunk of that
-    int b, unit, chunk, n_chunks, len;
+    int mine, at, end;                          // the share and its chunks
+    int b, unit, chunk, n_chunks, len;          // where it begins: sequence, unit of it, chunk of that
     const int room = p.max_pages * p.page_size;
     auto enter = [&]() {
         len = scalar(min(max(p.lens[b], 0), room));
         n_chunks = (len + CHUNK<T> - 1) / CHUNK<T>;
     };
-    {
+    if constexpr (WHOLE) {
+        mine = (int)blockIdx.x;
+        b = mine / units;
+        unit = mine - b * units;
+        enter();
+        chunk = at = 0;
+        end = n_chunks;
+    } else {
+        // neighbouring shares, which often read the same rows' other heads, on one XCD: consecutive workgroups go round-robin to the 8
+        const Shares shares = shares_of<T>(p, units, lane);
+        const int n_shares = (int)(((uint32_t)shares.all + (uint32_t)shares.each - 1) / (uint32_t)shares.each), per_xcd = (n_shares + 7) / 8;
+        if ((int)blockIdx.x / 8 >= per_xcd) return;
+        mine = (int)blockIdx.x % 8 * per_xcd + (int)blockIdx.x / 8;
+        if (mine >= n_shares) return;
+        at = mine * shares.each;
+        end = at + min(shares.each, shares.all - at);
         // (a sequence's chunks, unit by unit, follow those of all sequences before it)
         int before;
         find_chunk<T>(p, at, units, lane, b, before);
@@ -165,114 +177,128 @@ decode_kernel(DecodeArgs p) {
     // bf16, d % 8 == 4: the chunk that holds column d has four elements of whatever follows the row
     const int part_ks = BF16 && d % 8 && ((d >> 3) & 3) == j ? d >> 5 : -1;
 
-    while (at < end) {
+    // A piece: the chunks of a unit in this share.  Its first tile's rows and its queries are requested before the piece in front of it is
+    // joined and written (`ahead` they are those of the next piece).
+    struct Piece { int b, h0, n_heads, first, last, n_chunks, len; };
+    Piece now;
+    u32x4 q[KS], q_ahead[KS];
+    int t0;                                     // this wavefront's next tile: tokens t0 .. t0 + TILE - 1, CHUNK<T> further on the one after it
+    // page and place in it of each of its 16-token blocks
+    const int step_page = CHUNK<T> / p.page_size, step_in = CHUNK<T> - step_page * p.page_size;
+    int page[BLOCKS], in_page[BLOCKS];
+    const int32_t* table;
+    int64_t head_at;
+    u32x4 k[BLOCKS][KS];
+    uint32_t v[TOKENS][NM][CW * ES / 4];
+    int64_t at_k[BLOCKS], at_v[BLOCKS];         // bytes of the blocks in the caches, of the tile requested last / before it
+    int rows_k[BLOCKS], rows_v[BLOCKS];         // tokens that may be read (0: none)
+    auto place = [&](int t) {
+#pragma unroll
+        for (int i = 0; i < BLOCKS; ++i) {
+            const int token = t + 16 * i;
+            rows_k[i] = 0;
+            at_k[i] = 0;
+            if (token < len) {
+                const int id = scalar(table[page[i]]);
+                if (id >= 0 && id < p.n_pages) {
+                    rows_k[i] = min(16, len - token);
+                    at_k[i] = (id * p.stride_page + in_page[i] * p.stride_slot + head_at) * ES;
+                }
+            }
+            page[i] += step_page;
+            in_page[i] += step_in;
+            if (in_page[i] >= p.page_size) {
+                in_page[i] -= p.page_size;
+                ++page[i];
+            }
+        }
+    };
+    auto rsrc = [&](const void* cache, int64_t bytes, int rows) {
+        return __builtin_amdgcn_make_buffer_rsrc((void*)((const char*)cache + bytes), 0, rows ? (rows - 1) * pitch + ES * d : 0, 0x00020000);
+    };
+    auto load_k = [&]() {
+#pragma unroll
+        for (int i = 0; i < BLOCKS; ++i) {
+            const auto s = rsrc(p.k_cache, at_k[i], rows_k[i]);
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) k[i][ks] = __builtin_amdgcn_raw_buffer_load_b128(s, k_at[ks], 0, 0);
+        }
+    };
+    auto load_v = [&]() {
+#pragma unroll
+        for (int i = 0; i < BLOCKS; ++i) {
+            const auto s = rsrc(p.v_cache, at_v[i], rows_v[i]);
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int x = 0; x < NM; ++x) {
+                    uint32_t(&to)[CW * ES / 4] = v[4 * i + r][x];
+                    if constexpr (CW * ES == 16) {
+                        const u32x4 y = __builtin_amdgcn_raw_buffer_load_b128(s, v_at[r][x], 0, 0);
+                        to[0] = y[0]; to[1] = y[1]; to[2] = y[2]; to[3] = y[3];
+                    } else if constexpr (CW * ES == 8) {
+                        const u32x2 y = __builtin_amdgcn_raw_buffer_load_b64(s, v_at[r][x], 0, 0);
+                        to[0] = y[0]; to[1] = y[1];
+                    } else {
+                        to[0] = __builtin_amdgcn_raw_buffer_load_b32(s, v_at[r][x], 0, 0);
+                    }
+                }
+        }
+    };
+    auto keep_place = [&]() {
+#pragma unroll
+        for (int i = 0; i < BLOCKS; ++i) {
+            at_v[i] = at_k[i];
+            rows_v[i] = rows_k[i];
+        }
+    };
+    // the piece that begins with chunk `chunk` of (b, unit), `len` tokens long
+    auto request = [&]() {
         const int kvh = unit / blocks, h0 = kvh * group + (unit - kvh * blocks) * HEADS;
         const int n_heads = min(HEADS, (kvh + 1) * group - h0);
-        const int first = chunk, last = min(n_chunks, chunk + (end - at));       // chunks of the unit in this share
-        u32x4 q[KS];
+        const Piece next = {b, h0, n_heads, chunk, min(n_chunks, chunk + (end - at)), n_chunks, len};
         const bool has_head = n < n_heads;
         const T* q_row = (const T*)p.q + b * p.stride_b + (h0 + (has_head ? n : 0)) * p.stride_h;
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
             constexpr int E = BF16 ? 8 : 4;
             const int col = O::STEP * ks + E * j;
-            q[ks] = u32x4{0, 0, 0, 0};
+            q_ahead[ks] = u32x4{0, 0, 0, 0};
             if (has_head && col < d) {
-                if (!BF16 || col + 8 <= d) q[ks] = *reinterpret_cast<const u32x4*>(q_row + col);
+                if (!BF16 || col + 8 <= d) q_ahead[ks] = *reinterpret_cast<const u32x4*>(q_row + col);
                 else {
                     const u32x2 x = *reinterpret_cast<const u32x2*>(q_row + col);
-                    q[ks][0] = x[0];
-                    q[ks][1] = x[1];
+                    q_ahead[ks][0] = x[0];
+                    q_ahead[ks][1] = x[1];
                 }
             }
         }
-        f32x4 acc[NB];
-#pragma unroll
-        for (int i = 0; i < NB; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-        float m = -INFINITY, l = 0.f;
-        bool seen = false;                      // some token of a page that is one
-
-        // this wavefront's tiles of the unit: tokens t0, t0 + CHUNK, ..., each in BLOCKS blocks of 16
-        const int t_end = min(len, last * CHUNK<T>);
-        int t0 = first * CHUNK<T> + wave * TILE;
-        // page and place in it of each block, counted on by CHUNK a tile
-        const int step_page = CHUNK<T> / p.page_size, step_in = CHUNK<T> - step_page * p.page_size;
-        int page[BLOCKS], in_page[BLOCKS];
+        t0 = next.first * CHUNK<T> + wave * TILE;
 #pragma unroll
         for (int i = 0; i < BLOCKS; ++i) {
             page[i] = (t0 + 16 * i) / p.page_size;
             in_page[i] = t0 + 16 * i - page[i] * p.page_size;
         }
-        const int32_t* table = p.table + b * p.table_stride;
-        const int64_t head_at = (int64_t)kvh * p.stride_head;
-        u32x4 k[BLOCKS][KS];
-        uint32_t v[TOKENS][NM][CW * ES / 4];
-        int64_t at_k[BLOCKS], at_v[BLOCKS];         // bytes of the blocks in the caches, of the tile requested last / before it
-        int rows_k[BLOCKS], rows_v[BLOCKS];         // tokens that may be read (0: none)
-        auto place = [&](int t) {
-#pragma unroll
-            for (int i = 0; i < BLOCKS; ++i) {
-                const int token = t + 16 * i;
-                rows_k[i] = 0;
-                at_k[i] = 0;
-                if (token < len) {
-                    const int id = scalar(table[page[i]]);
-                    if (id >= 0 && id < p.n_pages) {
-                        rows_k[i] = min(16, len - token);
-                        at_k[i] = (id * p.stride_page + in_page[i] * p.stride_slot + head_at) * ES;
-                    }
-                }
-                page[i] += step_page;
-                in_page[i] += step_in;
-                if (in_page[i] >= p.page_size) {
-                    in_page[i] -= p.page_size;
-                    ++page[i];
-                }
-            }
-        };
-        auto rsrc = [&](const void* cache, int64_t bytes, int rows) {
-            return __builtin_amdgcn_make_buffer_rsrc((void*)((const char*)cache + bytes), 0, rows ? (rows - 1) * pitch + ES * d : 0, 0x00020000);
-        };
-        auto load_k = [&]() {
-#pragma unroll
-            for (int i = 0; i < BLOCKS; ++i) {
-                const auto s = rsrc(p.k_cache, at_k[i], rows_k[i]);
-#pragma unroll
-                for (int ks = 0; ks < KS; ++ks) k[i][ks] = __builtin_amdgcn_raw_buffer_load_b128(s, k_at[ks], 0, 0);
-            }
-        };
-        auto load_v = [&]() {
-#pragma unroll
-            for (int i = 0; i < BLOCKS; ++i) {
-                const auto s = rsrc(p.v_cache, at_v[i], rows_v[i]);
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-#pragma unroll
-                    for (int x = 0; x < NM; ++x) {
-                        uint32_t(&to)[CW * ES / 4] = v[4 * i + r][x];
-                        if constexpr (CW * ES == 16) {
-                            const u32x4 y = __builtin_amdgcn_raw_buffer_load_b128(s, v_at[r][x], 0, 0);
-                            to[0] = y[0]; to[1] = y[1]; to[2] = y[2]; to[3] = y[3];
-                        } else {
-                            const u32x2 y = __builtin_amdgcn_raw_buffer_load_b64(s, v_at[r][x], 0, 0);
-                            to[0] = y[0]; to[1] = y[1];
-                        }
-                    }
-            }
-        };
-        auto keep_place = [&]() {
-#pragma unroll
-            for (int i = 0; i < BLOCKS; ++i) {
-                at_v[i] = at_k[i];
-                rows_v[i] = rows_k[i];
-            }
-        };
-        if (t0 < t_end) {
+        table = p.table + b * p.table_stride;
+        head_at = (int64_t)kvh * p.stride_head;
+        if (t0 < min(len, next.last * CHUNK<T>)) {
             place(t0);
             load_k();
             keep_place();
             load_v();
         }
+        return next;
+    };
+    now = request();
+    for (;;) {
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) q[ks] = q_ahead[ks];
+        const int t_end = min(now.len, now.last * CHUNK<T>);
+        f32x4 acc[NB];
+#pragma unroll
+        for (int i = 0; i < NB; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+        float m = -INFINITY, l = 0.f;
+        bool seen = false;                      // some token of a page that is one
         for (; t0 < t_end; t0 += CHUNK<T>) {
             f32x4 s[BLOCKS];
 #pragma unroll
@@ -372,6 +398,22 @@ decode_kernel(DecodeArgs p) {
             }
         }
 
+        // on to the next piece: its first requests are on their way while this one is joined
+        const Piece done = now;
+        at += now.last - now.first;
+        const bool last_piece = WHOLE || at >= end;
+        if (!last_piece) {
+            chunk = 0;
+            if (++unit == units) {
+                unit = 0;
+                do {
+                    ++b;
+                    enter();
+                } while (n_chunks == 0);        // (there is one: `at` is before the end)
+            }
+            now = request();
+        }
+
         // the four wavefronts' parts
         l = quad_sum(l);
         if (l == 0.f && seen) l = -1.f;
@@ -389,17 +431,14 @@ decode_kernel(DecodeArgs p) {
 #pragma unroll
             for (int r = 0; r < 4; ++r)
 #pragma unroll
-                for (int c = 0; c < CW; c += 4) {
-                    float4 y;
-                    y.x = acc[x * CW + c][r] * own; y.y = acc[x * CW + c + 1][r] * own;
-                    y.z = acc[x * CW + c + 2][r] * own; y.w = acc[x * CW + c + 3][r] * own;
-                    *reinterpret_cast<float4*>(&o_lds[wave][n][16 * CW * x + CW * (4 * j + r) + c]) = y;
-                }
+                for (int c = 0; c < CW; c += 2)
+                    *reinterpret_cast<float2*>(&o_lds[wave][n][16 * CW * x + CW * (4 * j + r) + c]) =
+                        make_float2(acc[x * CW + c][r] * own, acc[x * CW + c + 1][r] * own);
         __syncthreads();
-        const bool complete = first == 0 && last == n_chunks;
+        const bool complete = done.first == 0 && done.last == done.n_chunks;
         // (a share's piece of a unit that began in another one is its first, of one that ends in another its last)
-        float* part = p.parts + ((int64_t)blockIdx.x * 2 + (first > 0 ? 0 : 1)) * part_floats(group, DP);
-        for (int i = threadIdx.x; i < n_heads * (DP / 4); i += 64 * WAVES) {
+        float* part = p.parts + ((int64_t)mine * 2 + (done.first > 0 ? 0 : 1)) * part_floats(group, DP);
+        for (int i = threadIdx.x; i < done.n_heads * (DP / 4); i += 64 * WAVES) {
             const int row = i / (DP / 4), col = 4 * (i - row * (DP / 4));
             if (col >= d) continue;
             float4 y = *reinterpret_cast<const float4*>(&o_lds[0][row][col]);
@@ -413,19 +452,20 @@ decode_kernel(DecodeArgs p) {
             float sum = 0.f;
             bool weightless = false;
 #pragma unroll
-            for (int w = 0; w < WAVES; ++w) add_sum(sum, weightless, l_lds[w][row], __builtin_amdgcn_exp2f(m_lds[w][row] - reference(mx)));
+            for (int w = 0; w < WAVES; ++w)
+                add_sum(sum, weightless, l_lds[w][row], __builtin_amdgcn_exp2f(m_lds[w][row] - reference(mx)));
             if (sum == 0.f && weightless) sum = -1.f;
             if (complete) {
                 // no token: zeros; tokens without any weight: no number
                 const float inv = sum < 0.f ? NAN : sum == 0.f ? 0.f : 1.f / sum;
-                T* to = (T*)p.out + b * p.stride_b + (h0 + row) * p.stride_h + col;
+                T* to = (T*)p.out + done.b * p.stride_b + (done.h0 + row) * p.stride_h + col;
                 if constexpr (BF16) {
                     bf16x4 z = {(__bf16)(y.x * inv), (__bf16)(y.y * inv), (__bf16)(y.z * inv), (__bf16)(y.w * inv)};
                     *reinterpret_cast<bf16x4*>(to) = z;
                 } else {
                     *reinterpret_cast<float4*>(to) = make_float4(y.x * inv, y.y * inv, y.z * inv, y.w * inv);
                 }
-                if (p.lse && col == 0) p.lse[b * p.stat_stride_b + h0 + row] = sum < 0.f ? NAN : (mx + __builtin_amdgcn_logf(sum)) * LN2;
+                if (p.lse && col == 0) p.lse[done.b * p.stat_stride_b + done.h0 + row] = sum < 0.f ? NAN : (mx + __builtin_amdgcn_logf(sum)) * LN2;
             } else {
                 *reinterpret_cast<float4*>(part + row * DP + col) = y;
                 if (col == 0) {
@@ -434,23 +474,19 @@ decode_kernel(DecodeArgs p) {
                 }
             }
         }
+        if (last_piece) break;
         __syncthreads();
-        at += last - first;
-        chunk = 0;
-        if (++unit == units) {
-            unit = 0;
-            do ++b; while (at < end && (enter(), n_chunks == 0));
-        }
     }
 }
 
 // Units whose pieces lie in several shares, and sequences without a token.  One workgroup a (sequence, unit, query head); its wavefronts
 // take the pieces in turn.
-template <typename T, int DP>
-__global__ void __launch_bounds__(64 * WAVES)
+constexpr int BATCH = 4;
+template <typename T, int DP, int JOIN_WAVES>
+__global__ void __launch_bounds__(64 * JOIN_WAVES)
 decode_join_kernel(DecodeArgs p) {
-    constexpr int COLS = DP / 64;
-    __shared__ float o_lds[WAVES][DP], m_lds[WAVES], l_lds[WAVES];
+    constexpr int COLS = (DP + 63) / 64;
+    __shared__ float o_lds[JOIN_WAVES][DP], m_lds[JOIN_WAVES], l_lds[JOIN_WAVES];
     const int lane = threadIdx.x & 63, wave = scalar((int)threadIdx.x >> 6);
     const int group = p.H / p.H_kv, blocks = (group + HEADS - 1) / HEADS, units = p.H_kv * blocks;
     const int b = (int)blockIdx.x / p.H, head = (int)blockIdx.x - b * p.H;
@@ -469,23 +505,35 @@ decode_join_kernel(DecodeArgs p) {
     const uint32_t from = (uint32_t)(before * units + unit * n);
     const int g0 = (int)(from / share), g1 = n ? (int)((from + n - 1) / share) : g0;
     if (n && g0 == g1) return;
+    // a wavefront's pieces, BATCH of them requested at a time (they come from other XCDs' workgroups: a round trip to memory each)
+    const int pieces = n ? g1 - g0 + 1 : 0, rows = part_rows(group);
     float m = -INFINITY, l = 0.f, acc[COLS] = {};
     bool weightless = false;
-    for (int g = n ? g0 + wave : g1 + 1; g <= g1; g += WAVES) {
-        const float* part = p.parts + ((int64_t)g * 2 + (g == g0 ? 1 : 0)) * part_floats(group, DP);
-        const float mg = part[part_rows(group) * DP + row], lg = part[part_rows(group) * (DP + 1) + row];
-        float x[COLS];
+    for (int i0 = wave * BATCH; i0 < pieces; i0 += JOIN_WAVES * BATCH) {
+        float mg[BATCH], lg[BATCH], x[BATCH][COLS];
 #pragma unroll
-        for (int c = 0; c < COLS; ++c) x[c] = lane + 64 * c < p.d ? part[row * DP + lane + 64 * c] : 0.f;
-        const float top = fmaxf(m, mg), a = __builtin_amdgcn_exp2f(m - reference(top)), f = __builtin_amdgcn_exp2f(mg - reference(top));
-        l *= a;
-        add_sum(l, weightless, lg, f);
+        for (int i = 0; i < BATCH; ++i) {
+            const int at = min(i0 + i, pieces - 1);
+            const float* part = p.parts + ((int64_t)(g0 + at) * 2 + (at == 0 ? 1 : 0)) * part_floats(group, DP);
+            mg[i] = part[rows * DP + row];
+            lg[i] = part[rows * (DP + 1) + row];
 #pragma unroll
-        for (int c = 0; c < COLS; ++c) acc[c] = acc[c] * a + x[c] * f;
-        m = top;
+            for (int c = 0; c < COLS; ++c) x[i][c] = lane + 64 * c < p.d ? part[row * DP + lane + 64 * c] : 0.f;
+        }
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) {
+            if (i0 + i >= pieces) break;
+            const float top = fmaxf(m, mg[i]), a = __builtin_amdgcn_exp2f(m - reference(top)), f = __builtin_amdgcn_exp2f(mg[i] - reference(top));
+            l *= a;
+            add_sum(l, weightless, lg[i], f);
+#pragma unroll
+            for (int c = 0; c < COLS; ++c) acc[c] = acc[c] * a + x[i][c] * f;
+            m = top;
+        }
     }
 #pragma unroll
-    for (int c = 0; c < COLS; ++c) o_lds[wave][lane + 64 * c] = acc[c];
+    for (int c = 0; c < COLS; ++c)
+        if (lane + 64 * c < DP) o_lds[wave][lane + 64 * c] = acc[c];
     if (lane == 0) {
         m_lds[wave] = m;
         l_lds[wave] = weightless && l == 0.f ? -1.f : l;
@@ -493,20 +541,20 @@ decode_join_kernel(DecodeArgs p) {
     __syncthreads();
     float top = m_lds[0];
 #pragma unroll
-    for (int w = 1; w < WAVES; ++w) top = fmaxf(top, m_lds[w]);
-    float f[WAVES], sum = 0.f;
+    for (int w = 1; w < JOIN_WAVES; ++w) top = fmaxf(top, m_lds[w]);
+    float f[JOIN_WAVES], sum = 0.f;
     weightless = false;
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w) {
+    for (int w = 0; w < JOIN_WAVES; ++w) {
         f[w] = __builtin_amdgcn_exp2f(m_lds[w] - reference(top));
         add_sum(sum, weightless, l_lds[w], f[w]);
     }
     if (sum == 0.f && weightless) sum = NAN;
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
-    for (int col = threadIdx.x; col < p.d; col += 64 * WAVES) {
+    for (int col = threadIdx.x; col < p.d; col += 64 * JOIN_WAVES) {
         float y = 0.f;
 #pragma unroll
-        for (int w = 0; w < WAVES; ++w) y += o_lds[w][col] * f[w];
+        for (int w = 0; w < JOIN_WAVES; ++w) y += o_lds[w][col] * f[w];
         T* to = (T*)p.out + b * p.stride_b + head * p.stride_h + col;
         if constexpr (sizeof(T) == 2) *reinterpret_cast<__bf16*>(to) = (__bf16)(y * inv);
         else *to = y * inv;
@@ -514,21 +562,35 @@ decode_join_kernel(DecodeArgs p) {
     if (p.lse && threadIdx.x == 0) p.lse[b * p.stat_stride_b + head] = (top + __builtin_amdgcn_logf(sum)) * LN2;
 }
 
-constexpr int columns(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
-// as many as the chip holds at once
-constexpr int workgroups(int DP) { return N_CU * (DP <= 128 ? 2 : 1); }
+constexpr int columns(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : d <= 128 ? 128 : 256; }
+// Shares: as many workgroups as the chip holds at once or nearly.  64 sequences of up to 8192 tokens, 8 key/value heads, us, 1, 2, 3, 4 a compute
+// unit: d 128 204, 208, 226, 208, 128 of up to 1000 72, 65, 73, 67, d 64 132, 117, 114, 122, d 32 (32 of up to 16384, 16 heads) 218, 192, 177, 179.
+constexpr int workgroups(int DP) { return N_CU * (DP <= 32 ? 3 : 2); }
 
 template <typename T, int DP>
 hipError_t launch(DecodeArgs a, hipStream_t st) {
+    // Where no sequence can have more than eight rounds (above 128 columns four), a unit to a workgroup and nothing to join, whatever the lengths
+    // are.  us, shares : units, 32 heads on 8, d 128, tables of up to 250 tokens, 16 sequences 13.6 : 11.0, 128 24.4 : 15.6, 500 38 : 30, 1000
+    // 61 : 58, 16 of 1000 16.5 : 13.9, but one of 1500 13.8 : 17.0, 64 of 2000 58 : 63; d 256, 8 heads on 2, 16 of 250 13.9 : 11.0, but 1000 13.9 : 23;
+    // fp32, 16 of 500 18.8 : 17.1, but 1000 22.6 : 29.  (11 us of these are the calls'.)
+    if ((int64_t)a.max_pages * a.page_size <= (DP > 128 ? 4 : 8) * CHUNK<T>) {
+        const int group = a.H / a.H_kv;
+        hipLaunchKernelGGL((decode_kernel<T, DP, true>), dim3((unsigned)(a.B * a.H_kv * ((group + HEADS - 1) / HEADS))), dim3(64 * WAVES), 0, st, a);
+        return hipGetLastError();
+    }
     a.n_wgs = workgroups(DP);
-    hipLaunchKernelGGL((decode_kernel<T, DP>), dim3((unsigned)a.n_wgs), dim3(64 * WAVES), 0, st, a);
+    hipLaunchKernelGGL((decode_kernel<T, DP, false>), dim3((unsigned)a.n_wgs), dim3(64 * WAVES), 0, st, a);
     if (hipError_t e = hipGetLastError()) return e;
-    hipLaunchKernelGGL((decode_join_kernel<T, DP>), dim3((unsigned)a.B * a.H), dim3(64 * WAVES), 0, st, a);
+    // eight wavefronts a head where there are few heads, whose units then have many pieces, us, two : eight: 8000 tokens, 32 heads, 18.5 : 15.0, 65536
+    // 61 : 57; 128 sequences of up to 300 28.5 : 35.6, of up to 1000 62 : 69
+    if ((int64_t)a.B * a.H <= 512) hipLaunchKernelGGL((decode_join_kernel<T, DP, 8>), dim3((unsigned)a.B * a.H), dim3(64 * 8), 0, st, a);
+    else hipLaunchKernelGGL((decode_join_kernel<T, DP, 2>), dim3((unsigned)a.B * a.H), dim3(64 * 2), 0, st, a);
     return hipGetLastError();
 }
 template <typename T>
 hipError_t launch(const DecodeArgs& a, hipStream_t st) {
     switch (columns(a.d)) {
+        case 32: return launch<T, 32>(a, st);
         case 64: return launch<T, 64>(a, st);
         case 128: return launch<T, 128>(a, st);
         default: return launch<T, 256>(a, st);
@@ -537,12 +599,12 @@ hipError_t launch(const DecodeArgs& a, hipStream_t st) {
 
 }  // namespace
 
-int64_t decode_workspace(int H, int H_kv, int d, int) {
+int64_t decode_workspace(int H, int H_kv, int d) {
     const int DP = columns(d);
     return (int64_t)workgroups(DP) * 2 * part_floats(H / H_kv, DP) * 4;
 }
 
-hipError_t launch_decode(DecodeArgs a, int dtype, hipStream_t st) {
+hipError_t launch_decode(const DecodeArgs& a, int dtype, hipStream_t st) {
     return dtype == SA_F32 ? launch<float>(a, st) : launch<__hip_bfloat16>(a, st);
 }
 

@@ -35,7 +35,7 @@ struct DecodeArgs {
     float scale;
     int n_wgs;                  // workgroups of the launch
 };
-int64_t decode_workspace(int H, int H_kv, int d, int dtype);
-hipError_t launch_decode(DecodeArgs a, int dtype, hipStream_t st);
+int64_t decode_workspace(int H, int H_kv, int d);
+hipError_t launch_decode(const DecodeArgs& a, int dtype, hipStream_t st);
 
 }  // namespace sa

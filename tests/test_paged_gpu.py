@@ -78,17 +78,23 @@ def compare(q, rows, out, lse, dtype, scale=None, heads=None):
 LENS = [1, 15, 16, 0, 17, 31, 33, 128, 129, 500]
 
 
+# Tables of so few pages that a workgroup takes a unit, and of so many that the tokens are dealt out in shares.
+WIDTHS = [None, 200]
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("d", [4, 20, 32, 64, 68, 100, 128, 132, 200, 256])
-def test_decode_head_dimensions(d, dtype):
-    compare(*decode(LENS, 4, 2, d, dtype), dtype)
+@pytest.mark.parametrize("width", WIDTHS)
+def test_decode_head_dimensions(width, d, dtype):
+    compare(*decode(LENS, 4, 2, d, dtype, width=width), dtype)
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("H,H_kv", [(1, 1), (5, 5), (12, 3), (16, 1), (17, 1), (32, 8), (40, 1), (66, 2)])
 @pytest.mark.parametrize("order", ["shd", "hsd"])
-def test_decode_heads_and_orders(H, H_kv, order, dtype):
-    compare(*decode([90, 1, 300], H, H_kv, 64, dtype, order=order), dtype)
+@pytest.mark.parametrize("width", WIDTHS)
+def test_decode_heads_and_orders(width, H, H_kv, order, dtype):
+    compare(*decode([90, 1, 300], H, H_kv, 64, dtype, order=order, width=width), dtype)
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
@@ -131,10 +137,11 @@ def test_decode_offsets_beyond_32_bits():
         assert torch.equal(c[pages - 1, 255], x[0]) and torch.equal(c[pages - 1, 254], x[1])
 
 
-def test_decode_scale_and_no_lse():
-    q, rows, out, lse = decode([77, 200], 4, 2, 64, BF16, scale=0.5)
+@pytest.mark.parametrize("width", WIDTHS)
+def test_decode_scale_and_no_lse(width):
+    q, rows, out, lse = decode([77, 200], 4, 2, 64, BF16, scale=0.5, width=width)
     compare(q, rows, out, lse, BF16, scale=0.5)
-    again = decode([77, 200], 4, 2, 64, BF16, scale=0.5, with_lse=False)
+    again = decode([77, 200], 4, 2, 64, BF16, scale=0.5, with_lse=False, width=width)
     assert torch.equal(again[2], out) and (again[3] == 7).all()
 
 
@@ -146,10 +153,11 @@ def test_decode_large_scores(dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
-def test_decode_pages_that_are_none(dtype):
+@pytest.mark.parametrize("width", [7, 200])
+def test_decode_pages_that_are_none(width, dtype):
     """Tokens of a page number that is none of the cache's are left out, all of them: no token."""
     page, lens = 32, [100, 200, 64]
-    table, pool = tables(lens, page, 4)
+    table, pool = tables(lens, page, 4, width=width)
     k_cache, v_cache = (cache(pool, page, 2, 64, dtype, "shd") for _ in range(2))
     rows = fill(k_cache, v_cache, table, lens, 40)
     table[0, 1], table[1, 0], table[1, 6] = pool, -2 ** 31, 2 ** 31 - 1
@@ -180,8 +188,8 @@ def test_decode_any_length_stays_within_the_table(dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
-@pytest.mark.parametrize("n", [20, 3000])
-def test_decode_infinities_and_nan(n, dtype):
+@pytest.mark.parametrize("n,width", [(20, None), (20, 200), (3000, None)])
+def test_decode_infinities_and_nan(n, width, dtype):
     """A key at -inf has no weight; alone, or beside NaN or +inf, the row is no number.  Other sequences do not notice."""
     d, inf = 64, float("inf")
     def mutate(q, rows, k_cache, v_cache, table):
@@ -196,7 +204,7 @@ def test_decode_infinities_and_nan(n, dtype):
             put(1, t, -inf)
         put(2, n - 1, inf)
         put(3, n // 2, float("nan"))
-    q, rows, out, lse = decode([n] * 5, 2, 1, d, dtype, mutate=mutate)
+    q, rows, out, lse = decode([n] * 5, 2, 1, d, dtype, mutate=mutate, width=width)
     keep = torch.arange(n) % 2 == 1
     rows[0] = [x[keep] for x in rows[0]]
     for s in (0, 4):
@@ -204,10 +212,11 @@ def test_decode_infinities_and_nan(n, dtype):
     assert out[1:4].isnan().all() and lse[1:4].isnan().all()
 
 
-def test_decode_captured_and_replayed():
+@pytest.mark.parametrize("width", [20, 200])
+def test_decode_captured_and_replayed(width):
     """Lengths and tables are read when the graph is played."""
     page, most = 32, 640
-    table, pool = tables([most] * 3, page, 8)
+    table, pool = tables([most] * 3, page, 8, width=width)
     k_cache, v_cache = (cache(pool, page, 2, 128, BF16, "shd") for _ in range(2))
     fill(k_cache, v_cache, table, [most] * 3, 5)
     q = normal((3, 8, 128), 6, BF16).cuda()
