@@ -15,6 +15,7 @@ struct AppendArgs {
     void* k_cache;
     void* v_cache;
     int rows, H, H_kv, d, page_size;
+    int wg_rows;                // rows a workgroup
     int64_t n_slots;
     int64_t stride_h, stride_s, kv_stride_h, kv_stride_s, stride_page, stride_slot, stride_head;
     double log2_base;
