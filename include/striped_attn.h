@@ -248,10 +248,12 @@ int sa_ring_bwd_tiled(const void* Q, const void* K, const void* V, const void* d
  * prompts in serving).  Row r of Q, O, dO, dQ is [r, head, 0..d) with d contiguous and strides stride_s (rows) and stride_h
  * (heads) in elements; K, V, dK, dV have H_kv heads (H_kv divides H; query head h reads head h / (H / H_kv)) and strides of
  * their own, under sa_shape's rules (heads apart or interleaved within a row step).  LSE and delta are fp32 [head, row], rows
- * contiguous, heads stat_stride_h apart.  offsets: DEVICE int32, n_seq + 1 of them: sequence s is rows offsets[s] ..
+ * contiguous, heads stat_stride_h apart.  No output overlaps an input or another output,
+ * here and below, but where it is said.  offsets: DEVICE int32, n_seq + 1 of them: sequence s is rows offsets[s] ..
  * offsets[s + 1] - 1 and attends causally to itself.  Empty sequences are allowed, and so are rows in front of the first and
- * behind the last sequence: nothing of them is read or written (but delta, which is scratch).  Offsets outside 0 .. rows count as
- * the nearest of these, a sequence that ends before it begins as empty.
+ * behind the last sequence: nothing of them has an effect, nothing of them is written (but delta, which is scratch).  Offsets
+ * outside 0 .. rows count as the nearest of these, a sequence that ends before it begins as empty; what rows hold afterwards that
+ * such offsets give to two sequences is not defined.
  * n_seq, rows or max_len 0: success, nothing launched, pointers not looked at.
  */
 typedef struct {
@@ -290,7 +292,7 @@ int sa_attn_packed_bwd(const void* q, const void* k, const void* v, const void* 
 typedef struct {
     int32_t n_pages;       /* n_pages * page_size below 2^31 */
     int32_t page_size;     /* tokens; a multiple of 16 */
-    int32_t H_kv, d;       /* d: any multiple of 4 up to 256 */
+    int32_t H_kv, d;       /* H_kv at most 65535; d: any multiple of 4 up to 256 */
     int64_t stride_page, stride_s, stride_h;       /* pages, tokens, heads; multiples of 4, stride_s below 2^24 */
     int32_t dtype;         /* sa_dtype of the cache and of what is appended to it or attends to it */
 } sa_cache;
@@ -319,7 +321,8 @@ int sa_cache_append(const void* q, void* q_out, const void* k, void* k_out, cons
  * cache's H_kv, query head h reads head h / (H / H_kv) */
 typedef struct {
     int32_t B, H;
-    int32_t max_pages;     /* page numbers a sequence in the table; max_pages * page_size at most 2^30 */
+    int32_t max_pages;     /* page numbers a sequence in the table; max_pages * page_size at most 2^30, and B * H times a 64th of
+                              that (plus 1) below 2^31 */
     int64_t stride_b, stride_h;        /* of q and out, multiples of 4 */
     int64_t stat_stride_b;
     int64_t table_stride;  /* page numbers between sequences in the table */
@@ -328,7 +331,7 @@ typedef struct {
 
 /*
  * Attention of one new token a sequence over its cached tokens 0 .. lens[b] - 1 (its own among them, appended before); token t lies
- * in page table[b, t / page_size].  lens: device int32 [B], taken as at most max_pages * page_size; of a sequence without a token
+ * in page table[b, t / page_size]; sequences may share pages.  lens: device int32 [B], taken as at most max_pages * page_size; of a sequence without a token
  * (0 or less) out is zero and LSE -inf.  A page number that is none of the cache's is not looked at: its tokens are left out.
  * Nothing behind a sequence's last token is read.  out is rounded once to the cache's dtype; lse may be NULL.  A key with score -inf has
  * no weight; a sequence with no other is NaN, and so is one with a NaN or +inf score.

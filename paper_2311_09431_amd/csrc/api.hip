@@ -245,7 +245,8 @@ int play_packed(const sa_packed* s, const int32_t* offsets, sa::PackedArgs a, La
 int check_cache(const sa_cache* c) {
     if (!c) return SA_ERR_NULL;
     if (c->dtype != SA_F32 && c->dtype != SA_BF16) return SA_ERR_DTYPE;
-    if (c->n_pages < 1 || c->page_size < 16 || c->page_size % 16 || c->H_kv < 1 || c->d < 1 || c->d > 256 || c->d % 4) return SA_ERR_SHAPE;
+    if (c->n_pages < 1 || c->page_size < 16 || c->page_size % 16 || c->H_kv < 1 || c->H_kv > 65535 || c->d < 1 || c->d > 256 || c->d % 4)
+        return SA_ERR_SHAPE;
     if ((int64_t)c->n_pages * c->page_size >= (int64_t(1) << 31)) return SA_ERR_SHAPE;
     if (int e = check_geom({c->H_kv, c->stride_page, c->stride_h, c->stride_s}, 1, c->page_size, c->d)) return e;
     // pages apart, and the tokens of a 16-row block within the 32-bit offsets of a descriptor

@@ -6,7 +6,7 @@
 // columns: a rotated one and its partner d/2 further on, 16 bytes each, or a piece of V.
 //
 // Bound by memory: (H + 2 H_kv) d elements a row are read and written (and H_kv d more written where rotated keys are kept).  16384 rows,
-// 32 heads on 8, d 128, bf16: 436 MB in 77 us, 5.7 TB/s (a copy reaches 4.9).  d = 100, whose halves are no whole 16-byte chunks, goes by
+// 32 heads on 8, d 128, bf16: 436 MB in 79 us, 5.5 TB/s (a copy reaches 4.9).  d = 100, whose halves are no whole 16-byte chunks, goes by
 // 8 bytes (bf16 4): 4.0 TB/s.
 #include <hip/hip_bf16.h>
 
@@ -16,7 +16,7 @@ namespace sa {
 
 namespace {
 
-constexpr int THREADS = 256, MOST_ROWS = 8;
+constexpr int THREADS = 256, MOST_ROWS = 8, MOST_WORKGROUPS = (1 << 24) - 1;
 
 // N elements, widened and back (one rounding)
 template <typename T, int N> struct Chunk;
@@ -108,8 +108,24 @@ template <typename T, int N>
 hipError_t launch(AppendArgs a, hipStream_t st) {
     const int per_row = ((a.q ? a.H : 0) + 2 * a.H_kv) * (a.d / 2 / N);
     a.wg_rows = THREADS / per_row < 1 ? 1 : THREADS / per_row > MOST_ROWS ? MOST_ROWS : THREADS / per_row;
-    hipLaunchKernelGGL((cache_append_kernel<T, N>), dim3((unsigned)(((int64_t)a.rows + a.wg_rows - 1) / a.wg_rows)), dim3(THREADS), 0, st, a);
-    return hipGetLastError();
+    // (a launch holds fewer than 2^32 threads: more rows go in several)
+    const int64_t all = a.rows, most = (int64_t)MOST_WORKGROUPS * a.wg_rows;
+    for (int64_t first = 0; first < all; first += most) {
+        AppendArgs p = a;
+        p.rows = (int)(all - first < most ? all - first : most);
+        p.k = (const T*)a.k + first * a.kv_stride_s;
+        p.v = (const T*)a.v + first * a.kv_stride_s;
+        if (a.k_out) p.k_out = (T*)a.k_out + first * a.kv_stride_s;
+        if (a.q) {
+            p.q = (const T*)a.q + first * a.stride_s;
+            p.q_out = (T*)a.q_out + first * a.stride_s;
+        }
+        if (a.pos) p.pos = a.pos + first;
+        p.slot = a.slot + first;
+        hipLaunchKernelGGL((cache_append_kernel<T, N>), dim3((unsigned)((p.rows + (int64_t)a.wg_rows - 1) / a.wg_rows)), dim3(THREADS), 0, st, p);
+        if (hipError_t e = hipGetLastError()) return e;
+    }
+    return hipSuccess;
 }
 
 // whole 16-byte chunks everywhere

@@ -1,7 +1,8 @@
 // Attention of one new token a sequence over its paged cache: O = softmax(scale q K^T) V over the sequence's cached rows.
 //
 // Bound by memory: the cache is read once, 2 d elements a token and key/value head, for 4 d operations of each of the G query
-// heads that share it.
+// heads that share it.  bf16, d 128: 2 sequences of 262144 tokens, 16 heads, 4.3 GB in 701 us, 6.1 TB/s; 64 of 1 to 8192, 32 heads on 8, 1.1 GB
+// in 207, 5.4; fp32, d 100, 160 MB in 41, 3.8.  (A copy reaches 4.9, a sum of a tensor 3.7.)
 //
 // Work.  A unit is (sequence, key/value head, 16 query heads of its group); its tokens come in chunks of CHUNK, and all chunks of all
 // units, in order, are cut into equal shares, one a workgroup, however the lengths differ.  What a workgroup holds of a unit it
@@ -479,20 +480,22 @@ decode_kernel(DecodeArgs p) {
     }
 }
 
-// Units whose pieces lie in several shares, and sequences without a token.  One workgroup a (sequence, unit, query head); its wavefronts
-// take the pieces in turn.
+// Units whose pieces lie in several shares, and sequences without a token.  JOIN_WAVES wavefronts take the pieces of a (sequence, query head) in
+// turn; a workgroup has eight wavefronts or, where one is enough for a head, four, of which each has a head of its own.
 constexpr int BATCH = 4;
 template <typename T, int DP, int JOIN_WAVES>
-__global__ void __launch_bounds__(64 * JOIN_WAVES)
+__global__ void __launch_bounds__(JOIN_WAVES == 1 ? 256 : 64 * JOIN_WAVES)
 decode_join_kernel(DecodeArgs p) {
-    constexpr int COLS = (DP + 63) / 64;
+    constexpr int COLS = (DP + 63) / 64, EACH = JOIN_WAVES == 1 ? 4 : 1;
     __shared__ float o_lds[JOIN_WAVES][DP], m_lds[JOIN_WAVES], l_lds[JOIN_WAVES];
-    const int lane = threadIdx.x & 63, wave = scalar((int)threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63, own_wave = scalar((int)threadIdx.x >> 6), wave = EACH == 1 ? own_wave : 0;
     const int group = p.H / p.H_kv, blocks = (group + HEADS - 1) / HEADS, units = p.H_kv * blocks;
-    const int b = (int)blockIdx.x / p.H, head = (int)blockIdx.x - b * p.H;
+    const int at_head = (int)blockIdx.x * EACH + (EACH == 1 ? 0 : own_wave), b = at_head / p.H, head = at_head - b * p.H;
+    if (b >= p.B) return;
     const int kvh = head / group, in_group = head - kvh * group, unit = kvh * blocks + in_group / HEADS, row = in_group % HEADS;
     // (in one pass: the chunks of the sequences before b, and all)
     int before = 0, all = 0;
+#pragma unroll 4
     for (int b0 = 0; b0 < p.B; b0 += 64) {
         const int own = b0 + lane < p.B ? chunks_of<T>(p, b0 + lane) : 0;
         all += own;
@@ -531,6 +534,19 @@ decode_join_kernel(DecodeArgs p) {
             m = top;
         }
     }
+    T* const to = (T*)p.out + b * p.stride_b + head * p.stride_h;
+    if constexpr (JOIN_WAVES == 1) {
+        if (weightless && l == 0.f) l = NAN;
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+        for (int c = 0; c < COLS; ++c)
+            if (lane + 64 * c < p.d) {
+                if constexpr (sizeof(T) == 2) reinterpret_cast<__bf16*>(to)[lane + 64 * c] = (__bf16)(acc[c] * inv);
+                else to[lane + 64 * c] = acc[c] * inv;
+            }
+        if (p.lse && lane == 0) p.lse[b * p.stat_stride_b + head] = (m + __builtin_amdgcn_logf(l)) * LN2;
+        return;
+    }
 #pragma unroll
     for (int c = 0; c < COLS; ++c)
         if (lane + 64 * c < DP) o_lds[wave][lane + 64 * c] = acc[c];
@@ -555,9 +571,8 @@ decode_join_kernel(DecodeArgs p) {
         float y = 0.f;
 #pragma unroll
         for (int w = 0; w < JOIN_WAVES; ++w) y += o_lds[w][col] * f[w];
-        T* to = (T*)p.out + b * p.stride_b + head * p.stride_h + col;
-        if constexpr (sizeof(T) == 2) *reinterpret_cast<__bf16*>(to) = (__bf16)(y * inv);
-        else *to = y * inv;
+        if constexpr (sizeof(T) == 2) reinterpret_cast<__bf16*>(to)[col] = (__bf16)(y * inv);
+        else to[col] = y * inv;
     }
     if (p.lse && threadIdx.x == 0) p.lse[b * p.stat_stride_b + head] = (top + __builtin_amdgcn_logf(sum)) * LN2;
 }
@@ -581,10 +596,11 @@ hipError_t launch(DecodeArgs a, hipStream_t st) {
     a.n_wgs = workgroups(DP);
     hipLaunchKernelGGL((decode_kernel<T, DP, false>), dim3((unsigned)a.n_wgs), dim3(64 * WAVES), 0, st, a);
     if (hipError_t e = hipGetLastError()) return e;
-    // eight wavefronts a head where there are few heads, whose units then have many pieces, us, two : eight: 8000 tokens, 32 heads, 18.5 : 15.0, 65536
-    // 61 : 57; 128 sequences of up to 300 28.5 : 35.6, of up to 1000 62 : 69
+    // Eight wavefronts a head where there are few heads, whose units then have many pieces, us, one : eight, 32 heads on 8: a sequence of
+    // 8000 tokens 25.0 : 14.9, of 65536 69 : 57, 4 of up to 100000 174 : 169, 16 of up to 4000 37.1 : 37.4; 32 of up to 2000 30.7 : 32.3, 128 of up to
+    // 1100 73 : 83.
     if ((int64_t)a.B * a.H <= 512) hipLaunchKernelGGL((decode_join_kernel<T, DP, 8>), dim3((unsigned)a.B * a.H), dim3(64 * 8), 0, st, a);
-    else hipLaunchKernelGGL((decode_join_kernel<T, DP, 2>), dim3((unsigned)a.B * a.H), dim3(64 * 2), 0, st, a);
+    else hipLaunchKernelGGL((decode_join_kernel<T, DP, 1>), dim3(((unsigned)(a.B * a.H) + 3) / 4), dim3(64 * 4), 0, st, a);
     return hipGetLastError();
 }
 template <typename T>

@@ -319,7 +319,7 @@ sa_cache cache_of(const at::Tensor& k) {
     if (k.size(3) > 1 && k.stride(3) != 1) refuse(PyExc_ValueError, "the head dimension must be contiguous");
     // (of a single head or page whatever fits)
     const int64_t h = k.size(2) == 1 ? k.size(3) : k.stride(2);
-    return {size(k, 0), size(k, 1), size(k, 2), size(k, 3), k.stride(0), k.stride(1), h, type_of(k)};
+    return {size(k, 0), size(k, 1), size(k, 2), size(k, 3), k.size(0) == 1 ? 0 : k.stride(0), k.stride(1), h, type_of(k)};
 }
 const at::Tensor* maybe(const Call& on, PyObject* o) { return o == Py_None ? nullptr : &on(o); }
 void* at_of(const at::Tensor* t) { return t ? t->data_ptr() : nullptr; }

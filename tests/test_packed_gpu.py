@@ -306,3 +306,26 @@ def test_as_the_ring_step():
 def test_few_and_many_tiles(H, H_kv, lens, d):
     r = run(lens, H, H_kv, d, BF16)
     compare(lens, H, H_kv, d, BF16, 0, *r, heads={0, H_kv - 1})
+
+
+def test_more_heads_than_a_launch_takes():
+    """Launches of whole key/value heads, 20971 of them in the first three."""
+    H, lens = 65535, [2, 1] * 100
+    r = run(lens, H, H, 4, BF16)
+    compare(lens, H, H, 4, BF16, 0, *r, heads=[0, 1, 20970, 20971, 41941, 41942, 50000, 62912, 62913, 65534])
+
+
+def test_two_streams_at_once():
+    lens = [700, 50, 333]
+    want = [run(lens, 8, 2, d, BF16) for d in (64, 128)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in want]
+    for _ in range(4):
+        got = []
+        for stream, d in zip(streams, (64, 128)):
+            with torch.cuda.stream(stream):
+                got.append(run(lens, 8, 2, d, BF16))
+        torch.cuda.synchronize()
+        for g, w in zip(got, want):
+            for x, y in zip((g[1], g[2], *g[3]), (w[1], w[2], *w[3])):
+                assert torch.equal(x, y)

@@ -240,6 +240,81 @@ def test_decode_captured_and_replayed(width):
         assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
 
 
+@pytest.mark.parametrize("width", WIDTHS)
+def test_decode_shared_pages(width):
+    """Sequences with the same beginning share its pages; a page may also stand twice in one sequence."""
+    page, lens = 16, [100, 90, 33]
+    table, pool = tables(lens, page, 3, width=width)
+    k_cache, v_cache = (cache(pool, page, 2, 64, BF16, "shd") for _ in range(2))
+    rows = fill(k_cache, v_cache, table, lens, 7)
+    table[1, :4], table[2, 1] = table[0, :4], table[2, 0]
+    rows[1] = [torch.cat([a[:64], b[64:]]) for a, b in zip(rows[0], rows[1])]
+    rows[2] = [torch.cat([x[:16], x[:16], x[32:]]) for x in rows[2]]
+    q = normal((3, 4, 64), 2, BF16)
+    out, lse = torch.empty_like(q, device="cuda"), torch.empty(3, 4, device="cuda")
+    work = torch.empty(sa.sa_attn_decode_workspace(q, k_cache), dtype=torch.uint8, device="cuda")
+    sa.sa_attn_decode(q.cuda(), k_cache, v_cache, table.cuda(), torch.tensor(lens, dtype=torch.int32, device="cuda"), out, lse, work)
+    compare(q, rows, out.cpu(), lse.cpu(), BF16)
+
+
+def test_decode_two_streams_at_once():
+    """A workspace each."""
+    lens = [3000, 4, 900]
+    want = [decode(lens, 8, 2, d, BF16) for d in (64, 128)]
+    streams = [torch.cuda.Stream() for _ in want]
+    for _ in range(4):
+        got = []
+        for stream, d in zip(streams, (64, 128)):
+            with torch.cuda.stream(stream):
+                got.append(decode(lens, 8, 2, d, BF16))
+        torch.cuda.synchronize()
+        for g, w in zip(got, want):
+            assert torch.equal(g[2], w[2]) and torch.equal(g[3], w[3])
+
+
+def test_two_captured_calls_with_a_workspace_each():
+    lens = torch.tensor([3000, 70], dtype=torch.int32)
+    table, pool = tables(lens.tolist(), 16, 8)
+    k_cache, v_cache = (cache(pool, 16, 2, 128, BF16, "shd") for _ in range(2))
+    fill(k_cache, v_cache, table, lens.tolist(), 5)
+    table, lens = table.cuda(), lens.cuda()
+    qs = [normal((2, 8, 128), seed, BF16).cuda() for seed in (6, 7)]
+    outs, lses = [torch.empty_like(q) for q in qs], [torch.empty(2, 8, device="cuda") for _ in qs]
+    works = [torch.empty(sa.sa_attn_decode_workspace(q, k_cache), dtype=torch.uint8, device="cuda") for q in qs]
+    calls = [lambda i=i: sa.sa_attn_decode(qs[i], k_cache, v_cache, table, lens, outs[i], lses[i], works[i]) for i in (0, 1)]
+    for call in calls:
+        call()
+    torch.cuda.synchronize()
+    want = [x.clone() for x in outs + lses]
+    graphs = [torch.cuda.CUDAGraph() for _ in calls]
+    for graph, call in zip(graphs, calls):
+        with torch.cuda.graph(graph):
+            call()
+    streams = [torch.cuda.Stream() for _ in calls]
+    for _ in range(3):
+        for x in outs + lses:
+            x.fill_(3)
+        torch.cuda.synchronize()
+        for graph, stream in zip(graphs, streams):
+            with torch.cuda.stream(stream):
+                graph.replay()
+        torch.cuda.synchronize()
+        for x, y in zip(outs + lses, want):
+            assert torch.equal(x, y)
+
+
+def test_a_single_page_of_any_page_stride():
+    """(nothing is a step of it away)"""
+    k, v = (normal((1, 48, 2, 64), s, BF16).cuda() for s in (1, 2))
+    odd = [x.as_strided(x.shape, (1, *x.stride()[1:])) for x in (k, v)]
+    q = normal((1, 4, 64), 3, BF16)
+    out, lse = torch.empty_like(q, device="cuda"), torch.empty(1, 4, device="cuda")
+    work = torch.empty(sa.sa_attn_decode_workspace(q, odd[0]), dtype=torch.uint8, device="cuda")
+    one = torch.zeros(1, 1, dtype=torch.int32, device="cuda")
+    sa.sa_attn_decode(q.cuda(), *odd, one, torch.full((1,), 41, dtype=torch.int32, device="cuda"), out, lse, work)
+    compare(q, [[x[0, :41].cpu() for x in (k, v)]], out.cpu(), lse.cpu(), BF16)
+
+
 # ---------------------------------------------------------------- append
 
 
@@ -318,6 +393,19 @@ def test_append_strided_rows(dtype):
         sa.sa_cache_append(plain[1], plain[2], slot, *want, pos=pos, k_out=plain[1], q=plain[0], q_out=plain[0])
         assert torch.equal(q, plain[0]) and torch.equal(k, plain[1]) and torch.equal(v, plain[2])
         assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+def test_append_more_rows_than_a_launch_takes():
+    """(2^24 - 1) * 8 rows go in the first one."""
+    n, page = (2 ** 24 - 1) * 8 + 21, 16
+    pages = -(-n // page)
+    k = torch.arange(4 * n, device="cuda").remainder_(251).to(BF16).view(n, 1, 4)
+    v = torch.arange(4 * n, device="cuda").remainder_(247).to(BF16).view(n, 1, 4)
+    k_cache, v_cache = (torch.zeros(pages, page, 1, 4, dtype=BF16, device="cuda") for _ in range(2))
+    slot = torch.arange(n - 1, -1, -1, dtype=torch.int32, device="cuda")
+    sa.sa_cache_append(k, v, slot, k_cache, v_cache)
+    for x, c in ((k, k_cache), (v, v_cache)):
+        assert torch.equal(c.view(-1, 1, 4)[:n], x.flip(0)) and (c.view(-1, 4)[n:] == 0).all()
 
 
 def test_append_rotates_as_rope_does():

@@ -97,7 +97,7 @@ def test_packed_nothing_to_do(kw):
 BAD_CACHE = [(dict(n_pages=0), E_SHAPE), (dict(page_size=0), E_SHAPE), (dict(page_size=8), E_SHAPE), (dict(page_size=40), E_SHAPE),
              (dict(H_kv=0), E_SHAPE), (dict(d=0), E_SHAPE), (dict(d=66), E_SHAPE), (dict(d=300), E_SHAPE), (dict(stride_s=120), E_SHAPE),
              (dict(stride_h=32), E_SHAPE), (dict(stride_page=32 * 128 - 4), E_SHAPE), (dict(stride_page=32 * 128 + 2), E_ALIGN),
-             (dict(stride_s=130, stride_page=1 << 20), E_ALIGN), (dict(dtype=5), E_DTYPE), (dict(n_pages=1 << 26), E_SHAPE),
+             (dict(stride_s=130, stride_page=1 << 20), E_ALIGN), (dict(dtype=5), E_DTYPE), (dict(n_pages=1 << 26), E_SHAPE), (dict(H_kv=65536), E_SHAPE),
              (dict(stride_s=1 << 24, stride_page=1 << 30), E_SHAPE)]
 
 
