@@ -4,7 +4,7 @@
 // A wavefront issues an instruction of any kind every four to five clocks (vector 5, exponential 9, wait and s_nop 4, dependent
 // scalar 8; LDS reads share the compute unit: a row read 4, a transposing one 2), a product of 32 x 32 x 16 takes the matrix core
 // 33, and behind a product there is room for about six others.  With all vector work beside the products of the scores and none
-// beside the others, as in bwd_mfma.hip, the first half of a sub-tile takes 760 clocks for 16 products and requests and walk 450
+// beside the others, as in bwd_tiles.h, the first half of a sub-tile takes 760 clocks for 16 products and requests and walk 450
 // a tile on top.  So here:
 //  * behind every product an even share of everything else; half of a sub-tile's exponentials run beside the last products of the
 //    one before it, where its scores are complete;
@@ -22,7 +22,7 @@
 // of a ring of 128-row shards with few heads, all of whose tiles are masked: 31 heads, 7 shards, d 120, 35.2 / 38.0, 32 on 16, 14, d 96,
 // 53.1 / 56.9.
 //
-// bwd_mfma.hip says what the products are; every sum has the order it has there, so the results have the same bits.
+// bwd_tiles.h says what the products are; every sum has the order it has there, so the results have the same bits.
 #pragma once
 #include <hip/hip_bf16.h>
 
@@ -238,7 +238,7 @@ __device__ __forceinline__ void keys_step(const f32x16& s_cur, const f32x16& dp_
 }
 
 // RAGGED without instantiations of its own: rows beyond the shard come in as zeros (clamped for the rows that stay), their LSE as
-// +inf, and they are not stored.  Pairs of (query head of the group, query shard) are blocks of one walk, as in bwd_mfma.hip.
+// +inf, and they are not stored.  Pairs of (query head of the group, query shard) are blocks of one walk, as in bwd_tiles.h.
 // PACKED: as in bwd_tiles.h.
 template <int DP, bool PART, bool BY_RANK, bool PACKED = false>
 __device__ __forceinline__ void dkdv_ring(const StepArgs& p, int n_tiles, int linear, char* lds, float* stat) {
@@ -263,7 +263,7 @@ __device__ __forceinline__ void dkdv_ring(const StepArgs& p, int n_tiles, int li
     const int dev0 = p.layout != SA_STRIPED ? max(p.q_dev, dev) : p.q_dev;
     auto first_tile = [&](int q_dev) {
         if (block_kind(q_dev, dev, p.layout) != MASK_TRI) return 0;
-        if (p.skip_bq > 0)      // emulated coarse skipping, as in bwd_mfma.hip
+        if (p.skip_bq > 0)      // emulated coarse skipping, as in bwd_tiles.h
             return ((k0 / p.skip_bk * p.skip_bk + block_off(q_dev, dev, p.layout)) / p.skip_bq) * p.skip_bq / DT_ROWS;
         return k0 / DT_ROWS;
     };

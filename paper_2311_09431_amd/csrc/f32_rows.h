@@ -1,8 +1,8 @@
 // Single rows of a ring step in plain fp32 arithmetic, one wavefront a row, looking at nothing but
 // the pairs that the mask allows.
 //
-// The fp32-precision matrix-core kernels (f32_step.hip, f32x3_step.hip, the exact ones of
-// split_mfma.hip) multiply whole 32 x 32 sub-tiles, masked pairs with a weight of zero, and two of
+// The fp32-precision matrix-core kernels (f32_tiles.h, f32x3_tiles.h, the exact ones of
+// split_tiles.h) multiply whole 32 x 32 sub-tiles, masked pairs with a weight of zero, and two of
 // them an operand as three terms.  For finite numbers that is the same sum; an infinite or NaN element
 // makes 0 * inf, inf - inf, or a sum of row weights that is no number.  All of these leave something
 // that is not finite in the row's accumulators or row sum, so a kernel looks there once, at its end,
@@ -32,7 +32,7 @@ __device__ inline float ld1(const __hip_bfloat16* p) {
     return __uint_as_float((uint32_t)(*reinterpret_cast<const uint16_t*>(p)) << 16);
 }
 
-// What f32_step.hip, f32x3_step.hip and split_mfma.hip share beside that.
+// What f32_tiles.h, f32x3_tiles.h and split_tiles.h share beside that.
 
 // streamed row (within a 32-row sub-tile) of register r of a 32 x 32 score tile, h = lane / 32
 __device__ inline int reg_row(int r, int h) { return 8 * (r / 4) + 4 * h + r % 4; }

@@ -297,7 +297,10 @@ fwd_f32_kernel(Args p, int n_tiles) {
         }
         if (kw == 0 && h == 0) *L = top + logf(w_sum);
     }
-    each_row<SPLIT>(odd_rows, kw, [&](const StepArgs& again, int i) { if constexpr (PACKED) fwd_row<T>(p, b, hd, dev_i, q0 + 32 * qw + i, lane); else fwd_row<T>(again, b, hd, dev_i, q0 + 32 * qw + i, lane); });
+    each_row<SPLIT>(odd_rows, kw, [&](const StepArgs& again, int i) {
+        if constexpr (PACKED) fwd_row<T>(p, b, hd, dev_i, q0 + 32 * qw + i, lane);
+        else fwd_row<T>(again, b, hd, dev_i, q0 + 32 * qw + i, lane);
+    });
 }
 
 // scale * acc to 32 owned rows (this lane's row at dst_row), added to what is there unless fresh
@@ -384,7 +387,10 @@ __device__ inline void bwd_dq(const StepArgs& p, int n_tiles, int linear, float*
         SPLIT > 1 ? combine<SPLIT, NB>(acc, lds + qw * SPLIT * NB * 16 * 64, masks + qw * SPLIT, odd, kw, lane) : row_mask(odd);
     if (a_own < p.c && !((odd_rows >> n) & 1))
         add_rows<SPLIT, NB>(p.dq + base + (int64_t)a * p.stride_s, acc, p.scale, 0, d, kw, h, p.fresh);
-    each_row<SPLIT>(odd_rows, kw, [&](const StepArgs& again, int i) { if constexpr (PACKED) dq_row<T>(p, b, hd, dev_i, q0 + 32 * qw + i, lane); else dq_row<T>(again, b, hd, dev_i, q0 + 32 * qw + i, lane); });
+    each_row<SPLIT>(odd_rows, kw, [&](const StepArgs& again, int i) {
+        if constexpr (PACKED) dq_row<T>(p, b, hd, dev_i, q0 + 32 * qw + i, lane);
+        else dq_row<T>(again, b, hd, dev_i, q0 + 32 * qw + i, lane);
+    });
 }
 
 // -------------------------------------------------------------------- dK/dV

@@ -1,4 +1,4 @@
-// What the three-term kernels (f32x3_step.hip, f32x3_split.hip) share: terms made in steps that go beside products, and
+// What the three-term kernels (f32x3_tiles.h, f32x3_split_tiles.h) share: terms made in steps that go beside products, and
 // the six products of two three-term operands.
 #pragma once
 #include "mfma_tiles.h"

@@ -1,5 +1,5 @@
 // Ring step for fp32 launches that leave much of the chip idle with 128-row workgroups, head dimension up to 128:
-// products of three bf16 terms a number, as in f32x3_step.hip, in the work split of split_mfma.hip.
+// products of three bf16 terms a number, as in f32x3_tiles.h, in the work split of split_tiles.h.
 //
 // What bounds such a launch is the walk of one workgroup, and in it the matrix cores and the vector instructions
 // that make terms of the streamed rows (5.5 an element, once for the products over the head dimension and once for
@@ -51,7 +51,7 @@ struct RawLane {
     }
 };
 
-// The loads of a streamed sub-tile, as split_mfma.hip's Loader: four pieces share one setting of m0.
+// The loads of a streamed sub-tile, as split_tiles.h's Loader: four pieces share one setting of m0.
 constexpr int AHEAD_BYTES = 4096;
 __device__ inline dt_rsrc stream_rsrc(const void* matrix, int rows, int pitch, int d) {
     dt_rsrc r = dt_make_rsrc((const char*)matrix - AHEAD_BYTES, rows, pitch, 2 * d);        // (2 d bf16 columns)
@@ -204,7 +204,7 @@ __device__ __forceinline__ f32x16 scores(const char* raw, const Own<DP>& own, co
     for (int r = 0; r < 16; ++r) hi[r] += lo[r];
     return hi;
 }
-// acc (32-column blocks x owned rows) += streamed^T w, the sub-tile's sum formed by itself (f32x3_step.hip)
+// acc (32-column blocks x owned rows) += streamed^T w, the sub-tile's sum formed by itself (f32x3_tiles.h)
 template <int DP>
 __device__ __forceinline__ void accumulate(f32x16 (&acc)[4], const char* raw, const f32x16& w, const RawLane<DP>& ln) {
     constexpr int N = 2 * blocks_of(DP);
@@ -344,7 +344,10 @@ fwd_f32x3_split_kernel(Args p, int n_tiles) {
     float* L = p.lse + b * p.stat_stride_b + hd * p.stat_stride_h + (int64_t)dev_i * p.c + a;
     const uint32_t odd_rows = fold_forward<DP, WAVES, true, true>(p, acc, m, l, lds, stats, masks, ln, dev, a_own, a, L,
                                                             p.o + base + (int64_t)a * p.stride_s);
-    each_row<WAVES>(odd_rows, ln.wave, [&](const StepArgs& again, int i) { if constexpr (PACKED) fwd_row<float>(p, b, hd, dev_i, q0 + i, ln.lane); else fwd_row<float>(again, b, hd, dev_i, q0 + i, ln.lane); });
+    each_row<WAVES>(odd_rows, ln.wave, [&](const StepArgs& again, int i) {
+        if constexpr (PACKED) fwd_row<float>(p, b, hd, dev_i, q0 + i, ln.lane);
+        else fwd_row<float>(again, b, hd, dev_i, q0 + i, ln.lane);
+    });
 }
 
 // ----------------------------------------------------------------------- dQ
@@ -438,7 +441,10 @@ __device__ inline void bwd_dq(const StepArgs& p, int n_tiles, int linear, char* 
     __syncthreads();
     const uint32_t odd_rows = redo.take(top, top);
     if (a_own < p.c && !((odd_rows >> n) & 1)) add_rows<DP, WAVES>(DQ, old, lds, p.scale, d, ln);
-    each_row<WAVES>(odd_rows, ln.wave, [&](const StepArgs& again, int i) { if constexpr (PACKED) dq_row<float>(p, b, hd, dev_i, q0 + i, ln.lane); else dq_row<float>(again, b, hd, dev_i, q0 + i, ln.lane); });
+    each_row<WAVES>(odd_rows, ln.wave, [&](const StepArgs& again, int i) {
+        if constexpr (PACKED) dq_row<float>(p, b, hd, dev_i, q0 + i, ln.lane);
+        else dq_row<float>(again, b, hd, dev_i, q0 + i, ln.lane);
+    });
 }
 
 // -------------------------------------------------------------------- dK/dV
@@ -571,7 +577,10 @@ __device__ inline void bwd_dkdv(const StepArgs& p, int n_tiles, int linear, char
         add_rows<DP, WAVES>(p.dv + row, old_v, lds, 1.f, d, ln);
         add_rows<DP, WAVES>(p.dk + row, old_k, lds + HALF, p.scale, d, ln);
     }
-    each_row<WAVES>(odd_rows, ln.wave, [&](const StepArgs& again, int i) { if constexpr (PACKED) dkdv_row<float>(p, b, kvh, dev_i, k0 + i, 0, d, ln.lane); else dkdv_row<float>(again, b, kvh, dev_i, k0 + i, 0, d, ln.lane); });
+    each_row<WAVES>(odd_rows, ln.wave, [&](const StepArgs& again, int i) {
+        if constexpr (PACKED) dkdv_row<float>(p, b, kvh, dev_i, k0 + i, 0, d, ln.lane);
+        else dkdv_row<float>(again, b, kvh, dev_i, k0 + i, 0, d, ln.lane);
+    });
 }
 
 }  // namespace

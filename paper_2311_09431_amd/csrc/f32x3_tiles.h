@@ -11,7 +11,7 @@
 // dQ 5.4e-7 -> 3.3e-7, dK 7.1e-7 -> 3.7e-7, dV 6.4e-7 -> 3.4e-7.  Whole ring, 16 heads, d 128,
 // 4 x 2048 tokens, forward + backward: 12.1 -> 6.5 ms.
 //
-// Everything else is as in f32_step.hip: transposed scores, a score register is the B operand of
+// Everything else is as in f32_tiles.h: transposed scores, a score register is the B operand of
 // the product over the streamed rows, one wavefront owns 32 rows (backward: two share 32), four (eight)
 // make a workgroup.  The owned rows sit in registers as three bf16 operands; the streamed ones go global -> registers
 // (a tile ahead) -> split -> three swizzled bf16 planes in LDS, two buffers, one barrier per 32-row
@@ -317,7 +317,10 @@ fwd_f32x3_kernel(Args p, int n_tiles) {
             }
         if (h == 0) *L = top + logf(w_sum);
     }
-    each_row<1>(odd_rows, 0, [&](const StepArgs& again, int i) { if constexpr (PACKED) fwd_row<float>(p, b, hd, dev_i, q0 + 32 * ln.wave + i, ln.lane); else fwd_row<float>(again, b, hd, dev_i, q0 + 32 * ln.wave + i, ln.lane); });
+    each_row<1>(odd_rows, 0, [&](const StepArgs& again, int i) {
+        if constexpr (PACKED) fwd_row<float>(p, b, hd, dev_i, q0 + 32 * ln.wave + i, ln.lane);
+        else fwd_row<float>(again, b, hd, dev_i, q0 + 32 * ln.wave + i, ln.lane);
+    });
 }
 
 // scale * acc to this lane's row, added to what is there unless fresh
@@ -479,7 +482,10 @@ __device__ inline void bwd_dq(const StepArgs& p, int n_tiles, int linear, char* 
                                           row_mask(top >= FAINT), ln.wave, ln.lane);
     if (a_own < p.c && !((odd_rows >> n) & 1))
         add_rows<NB>(p.dq + base + (int64_t)a * p.stride_s, acc, p.scale, 32 * NB * role, d, h, p.fresh);
-    each_row<2>(odd_rows, role, [&](const StepArgs& again, int i) { if constexpr (PACKED) dq_row<float>(p, b, hd, dev_i, q0 + 32 * group + i, ln.lane); else dq_row<float>(again, b, hd, dev_i, q0 + 32 * group + i, ln.lane); });
+    each_row<2>(odd_rows, role, [&](const StepArgs& again, int i) {
+        if constexpr (PACKED) dq_row<float>(p, b, hd, dev_i, q0 + 32 * group + i, ln.lane);
+        else dq_row<float>(again, b, hd, dev_i, q0 + 32 * group + i, ln.lane);
+    });
 }
 
 // dK (by the wavefront that forms dP) and dV (by the one that forms the probabilities).  Owned rows are keys, streamed
@@ -608,7 +614,10 @@ __device__ inline void bwd_dkdv(const StepArgs& p, int n_tiles, int linear, char
                                                      faint_rows(loudest<NB>(acc), key_own < p.c), 0, 0, ln.wave, ln.lane);
     if (key_own < p.c && !((odd_rows >> n) & 1))
         add_rows<NB>((role ? p.dk : p.dv) + row, acc, role ? p.scale : 1.f, 0, d, h, p.fresh);
-    each_row<2>(odd_rows, role, [&](const StepArgs& again, int i) { if constexpr (PACKED) dkdv_row<float>(p, b, kvh, dev_i, k0 + 32 * group + i, 0, d, ln.lane); else dkdv_row<float>(again, b, kvh, dev_i, k0 + 32 * group + i, 0, d, ln.lane); });
+    each_row<2>(odd_rows, role, [&](const StepArgs& again, int i) {
+        if constexpr (PACKED) dkdv_row<float>(p, b, kvh, dev_i, k0 + 32 * group + i, 0, d, ln.lane);
+        else dkdv_row<float>(again, b, kvh, dev_i, k0 + 32 * group + i, 0, d, ln.lane);
+    });
 }
 
 // Both in one launch, the kind with the longer walks first (they share nothing but the inputs; one compute unit each, so

@@ -402,8 +402,8 @@ ENTRY(decode) {
         void* st = stream(a[11]);
         const int64_t bytes = work.numel() * work.element_size();
         return run([&] {
-            return f(at_of(q), at_of(kc), at_of(vc), (const int32_t*)at_of(table), (const int32_t*)at_of(lens), at_of(out), (float*)at_of(lse), at_of(work), bytes,
-                     &s, &cache, st);
+            return f(at_of(q), at_of(kc), at_of(vc), (const int32_t*)at_of(table), (const int32_t*)at_of(lens), at_of(out), (float*)at_of(lse), at_of(work),
+                     bytes, &s, &cache, st);
         });
     });
 }
@@ -424,7 +424,8 @@ ENTRY(set_up) {
 
 #define FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(two), FAST(three), FAST(step_fwd), FAST(step_bwd), FAST(ring_fwd), FAST(ring_bwd), FAST(rope),
-                         FAST(permute), FAST(packed_fwd), FAST(packed_bwd), FAST(append), FAST(decode), FAST(decode_workspace), FAST(extent_of), FAST(set_up), {nullptr, nullptr, 0, nullptr}};
+                         FAST(permute), FAST(packed_fwd), FAST(packed_bwd), FAST(append), FAST(decode), FAST(decode_workspace),
+                         FAST(extent_of), FAST(set_up), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -36,6 +36,7 @@ __device__ inline int tiles_of(Span x) { return (x.len + TILE - 1) / TILE; }
 hipError_t launch_packed_fwd(PackedArgs p, hipStream_t st);
 hipError_t launch_packed_bwd(const PackedArgs& p, hipStream_t st);
 hipError_t launch_packed_bwd_ring(const PackedArgs& p, hipStream_t st);       // dK and dV at 65 to 128 columns
+hipError_t launch_packed_dkdv_wide(const PackedArgs& p, unsigned workgroups, hipStream_t st);         // above 128, all of them in a workgroup
 // bf16 launches of few tiles (the backward's forms delta too)
 bool packed_split_wanted(const PackedArgs& p, bool backward);
 hipError_t launch_packed_split(PackedArgs p, bool backward, hipStream_t st);

@@ -1,5 +1,5 @@
 // Causal attention of packed sequences and its gradient, bf16, launches of few tiles: the ring step's workgroups of 32 rows
-// (split_tiles.h), each on one tile of one sequence (packed.h).
+// (split_tiles.h), each on one tile of one sequence (packed.h).  Bound by the length of a walk, which several wavefronts share.
 #include "split_tiles.h"
 
 namespace sa {

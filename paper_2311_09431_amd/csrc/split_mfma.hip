@@ -47,7 +47,7 @@ hipError_t run(const StepArgs& a, Pass pass, hipStream_t st) {
     return run<128>(a, pass, st);
 }
 
-// Both sides' rows come through descriptors with 32-bit byte offsets (fwd_mfma.hip reads Q by 64-bit pointers, and
+// Both sides' rows come through descriptors with 32-bit byte offsets (fwd_tiles.h reads Q by 64-bit pointers, and
 // fwd_mfma_supported looks at the rows of K and V only).  Requests behind a walk's end name up to 32 rows behind the
 // block's last sub-tile: their offsets must not wrap into the matrix.
 bool rows_in_reach(const StepArgs& a) {

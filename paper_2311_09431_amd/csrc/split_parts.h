@@ -1,5 +1,5 @@
 // What the kernels share that give a workgroup 32 rows and split the streamed side over its wavefronts, each of
-// which streams by itself (split_mfma.hip: bf16, f32x3_split.hip: fp32): waits, the walks' order, and the meeting of
+// which streams by itself (split_tiles.h: bf16, f32x3_split_tiles.h: fp32): waits, the walks' order, and the meeting of
 // the partial results.
 #pragma once
 #include "f32_rows.h"

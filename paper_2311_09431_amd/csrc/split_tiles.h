@@ -1,5 +1,5 @@
 // Ring step for launches that leave most of the chip idle with 128-row workgroups (bf16 matrix cores,
-// head dimension up to 128): same operands and products as fwd_mfma.hip and bwd_mfma.hip, other split
+// head dimension up to 128): same operands and products as fwd_tiles.h and bwd_tiles.h, other split
 // of the work.
 //
 // What bounds such a launch is the walk of one workgroup.  Here a workgroup owns 32 rows and its
@@ -183,7 +183,7 @@ __device__ inline bool odd_sum(const float (&z)[2], const f32x16 (&ds_sum)[4]) {
 // ------------------------------------------------------------------ forward
 // Eight wavefronts, two to a SIMD: one's products run beside the other's vector instructions.  One stage each,
 // which is requested anew when the sub-tile has been read into registers.
-constexpr float RESCALE_SUM = 16777216.f;       // 2^24, see fwd_mfma.hip
+constexpr float RESCALE_SUM = 16777216.f;       // 2^24, see fwd_tiles.h
 // ROPE: the query rows are rotated by their position ids (d == DP).
 // Args: StepArgs, or PackedArgs for packed sequences (packed.h), whose rows are written in bf16
 template <int DP, bool PART, bool EXACT, bool ROPE = false, typename Args = StepArgs>
@@ -250,7 +250,7 @@ fwd_split_kernel(Args p, int n_tiles) {
     f32x16 acc[4];
 #pragma unroll
     for (int mb = 0; mb < 4; ++mb) acc[mb] = zero16();
-    // as in fwd_mfma.hip: a walk over striped shards sets its references anew at each
+    // as in fwd_tiles.h: a walk over striped shards sets its references anew at each
     const bool rebase_shards = !EXACT && p.n_kv > 1 && p.layout == SA_STRIPED;
     int kv_before = -1;
 
@@ -317,7 +317,7 @@ fwd_split_kernel(Args p, int n_tiles) {
             }
             m = m_new;
         } else {
-            // the reference moves when it has to, as in fwd_mfma.hip
+            // the reference moves when it has to, as in fwd_tiles.h
             f32x16 pr;
 #pragma unroll
             for (int r = 0; r < 16; ++r) {

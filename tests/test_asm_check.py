@@ -97,3 +97,21 @@ def test_every_source_with_such_statements_is_checked():
         if '"v_mfma' in text or "\\tv_mfma" in text or "mfma_vgpr_" in text:
             users.add(os.path.basename(path))
     assert users and users <= set(build.ASM_CHECKED)
+
+
+def test_every_source_that_includes_such_statements_is_checked():
+    """Statements in headers, other than the two that only define them."""
+    def texts(name, seen):
+        if name in seen:
+            return
+        seen.add(name)
+        with open(os.path.join(build.CSRC, name)) as f:
+            text = f.read()
+        if name not in ("mfma_tiles.h", "acc_file.h"):
+            yield text
+        for line in text.splitlines():
+            if line.startswith('#include "') and os.path.exists(os.path.join(build.CSRC, line.split('"')[1])):
+                yield from texts(line.split('"')[1], seen)
+
+    users = {s for s in build.SOURCES if any('"v_mfma' in t or "\\tv_mfma" in t or "mfma_vgpr_" in t for t in texts(s, set()))}
+    assert users == set(build.ASM_CHECKED)
