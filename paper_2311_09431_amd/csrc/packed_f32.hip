@@ -14,21 +14,22 @@ namespace sa {
 
 namespace {
 
-// workgroups 0 .. n_dkdv - 1 own keys, the others queries; at 256 columns each kind in a launch of its own
-template <int DP, int SPLIT, bool KEYS, bool QUERIES>
+// workgroups 0 .. n_dkdv - 1 own keys, the others queries.  In a launch each at 256 columns, whole training pass, us, together : apart: 4 sequences
+// of up to 1084 rows, 2 heads on 1, 776 : 1055, 16 heads 1705 : 1795, 3 of up to 500, 4 heads, 253 : 392, 8 of up to 1000, 32 on 8, 3232 : 3648.
+template <int DP, int SPLIT>
 __global__ void __launch_bounds__(64 * WAVES, DP > 64 ? 1 : 2)
 packed_bwd_f32_kernel(PackedArgs p, int n_dkdv) {
     constexpr int ROWS = 32 * WAVES / SPLIT;
     __shared__ __attribute__((aligned(16))) float lds[tile_floats<SPLIT, DP>()];
-    __shared__ float stats[KEYS ? 2 * tile_rows(SPLIT) : 1];        // LSE | delta of a tile's queries
+    __shared__ float stats[2 * tile_rows(SPLIT)];                   // LSE | delta of a tile's queries
     __shared__ uint32_t masks[WAVES];
     const int heads = p.H_kv * (DP > 128 ? 2 : 1);
     int n_tiles, rank, head;
-    if (KEYS && (!QUERIES || (int)blockIdx.x < n_dkdv)) {
+    if ((int)blockIdx.x < n_dkdv) {
         if (!enter_sequence<false, ROWS>(p, (int)blockIdx.x, heads, n_tiles, rank, head)) return;
         bwd_dkdv<float, DP, SPLIT, true>(p, n_tiles, rank * heads + head, lds, stats, masks);
-    } else if (QUERIES) {
-        if (!enter_sequence<true, ROWS>(p, (int)blockIdx.x - (KEYS ? n_dkdv : 0), p.H, n_tiles, rank, head)) return;
+    } else {
+        if (!enter_sequence<true, ROWS>(p, (int)blockIdx.x - n_dkdv, p.H, n_tiles, rank, head)) return;
         bwd_dq<float, DP, SPLIT, true>(p, n_tiles, rank * p.H + head, lds, masks);
     }
 }
@@ -39,15 +40,8 @@ hipError_t run(PackedArgs p, bool backward, hipStream_t st) {
     p.n_ranks = (int)ranks;
     const unsigned n_dkdv = (unsigned)(ranks * p.H_kv) * (DP > 128 ? 2 : 1), n_dq = (unsigned)(ranks * p.H);
     const dim3 block(64 * WAVES);
-    if (!backward) {
-        hipLaunchKernelGGL((fwd_f32_kernel<float, DP, SPLIT, PackedArgs>), dim3(n_dq), block, 0, st, p, 0);
-    } else if constexpr (DP <= 128) {
-        hipLaunchKernelGGL((packed_bwd_f32_kernel<DP, SPLIT, true, true>), dim3(n_dkdv + n_dq), block, 0, st, p, (int)n_dkdv);
-    } else {
-        hipLaunchKernelGGL((packed_bwd_f32_kernel<DP, SPLIT, false, true>), dim3(n_dq), block, 0, st, p, 0);
-        if (hipError_t e = hipGetLastError()) return e;
-        hipLaunchKernelGGL((packed_bwd_f32_kernel<DP, SPLIT, true, false>), dim3(n_dkdv), block, 0, st, p, (int)n_dkdv);
-    }
+    if (!backward) hipLaunchKernelGGL((fwd_f32_kernel<float, DP, SPLIT, PackedArgs>), dim3(n_dq), block, 0, st, p, 0);
+    else hipLaunchKernelGGL((packed_bwd_f32_kernel<DP, SPLIT>), dim3(n_dkdv + n_dq), block, 0, st, p, (int)n_dkdv);
     return hipGetLastError();
 }
 
