@@ -34,7 +34,7 @@ SOURCE_FLAGS = {name: ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]
 # Sources with matrix instructions in asm statements, and their kernels whose accumulators are registers by
 # number: the assembly of these is looked over (asm_check.py).
 ASM_CHECKED = {"bwd_mfma.hip": ["bwd_dkdv_wide_kernel"], "bwd_ring.hip": ["bwd_dkdv_ring_kernel", "bwd_both_ring_kernel"], "split_mfma.hip": [],
-               "packed_bwd.hip": [], "packed_split.hip": [], "packed_bwd_ring.hip": ["packed_dkdv_ring_kernel"]}
+               "packed_bwd.hip": [], "packed_split.hip": [], "packed_bwd_ring.hip": ["packed_dkdv_ring_kernel", "packed_both_ring_kernel"]}
 
 # packed fp32 VALU forms are switched off on purpose for the test machines
 FLAGS = ["-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC", "-fno-gpu-rdc",

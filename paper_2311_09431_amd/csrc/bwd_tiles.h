@@ -141,8 +141,8 @@ __device__ __forceinline__ void dq_step(f32x16& s_cur, f32x16& dp_cur, f32x16& s
 // k_lds0 .. v_lds1: the tile buffers (two 128-column halves each when DP = 256), LDS objects of their
 // own: as parts of one array the compiler arranges the d = 256 kernels otherwise and a full step of
 // 8 heads, 8192 rows, takes 2.197 instead of 2.177 ms
-// PACKED (packed sequences): linear is the tile's place and the head, dQ is written in bf16.
-template <bool RAGGED, int WALK, int DP, bool PART, bool BY_RANK, bool PACKED = false>
+// PACKED (packed sequences): linear is the tile's place and the head, dQ is written in bf16.  FORM_DELTA: delta is formed here.
+template <bool RAGGED, int WALK, int DP, bool PART, bool BY_RANK, bool PACKED = false, bool FORM_DELTA = PACKED>
 __device__ __forceinline__ void bwd_dq(const StepArgs& p, int n_tiles, int linear, char* k_lds0, char* k_lds1,
                                        char* v_lds0, char* v_lds1) {
     constexpr int NH = halves_of(DP), KS = ksteps_of(DP), MB = halves_of(DP) * blocks_of(DP);      // k-steps per half, column blocks
@@ -217,7 +217,7 @@ __device__ __forceinline__ void bwd_dq(const StepArgs& p, int n_tiles, int linea
     const float kappa = p.scale * LOG2E;
     float lse2 = p.lse[sbase + a] * LOG2E;
     float delta;
-    if constexpr (PACKED) {
+    if constexpr (FORM_DELTA) {
         // formed here, from the rows that the lane holds anyway, and stored for the key-owning workgroups behind this launch
         bf16x8 of[8 * NH];
         load_b_frags<8 * NH>(of, (const __bf16*)p.o + base + (int64_t)a * ss, h, d);

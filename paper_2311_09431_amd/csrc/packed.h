@@ -35,11 +35,13 @@ __device__ inline int tiles_of(Span x) { return (x.len + TILE - 1) / TILE; }
 
 hipError_t launch_packed_fwd(PackedArgs p, hipStream_t st);
 hipError_t launch_packed_bwd(const PackedArgs& p, hipStream_t st);
-hipError_t launch_packed_bwd_ring(const PackedArgs& p, hipStream_t st);       // dK and dV at 65 to 128 columns
+hipError_t launch_packed_bwd_ring(const PackedArgs& p, bool both, hipStream_t st);     // dK and dV at 65 to 128 columns; both: dQ too
 hipError_t launch_packed_dkdv_wide(const PackedArgs& p, unsigned workgroups, hipStream_t st);         // above 128, all of them in a workgroup
 // bf16 launches of few tiles (the backward's forms delta too)
 bool packed_split_wanted(const PackedArgs& p, bool backward);
 hipError_t launch_packed_split(PackedArgs p, bool backward, hipStream_t st);
+// (placed_kinds; as a ring step's, from 0.5 to 3 the same to 2 %)
+inline double packed_ratio(const PackedArgs& p) { return p.H == p.H_kv ? 1.45 : 0.; }
 hipError_t launch_packed_delta(const PackedArgs& p, int dtype, hipStream_t st);
 hipError_t launch_packed_f32(PackedArgs p, bool backward, hipStream_t st);
 hipError_t launch_packed_f32x3(PackedArgs p, bool backward, hipStream_t st);

@@ -39,6 +39,27 @@ packed_dkdv_kernel(PackedArgs p) {
     bwd_dkdv<WALK_RING, true, DP, PART, false, true>(p, n_tiles, rank * heads + head, lds0, lds1, lds2, lds3, stat);
 }
 
+// Both kinds of workgroups in a launch, delta formed by one in front of it.  Above 128 columns (65 to 128: packed_bwd_ring.hip).
+template <int DP, bool PART>
+__global__ void __launch_bounds__(256, 1)
+packed_both_kernel(PackedArgs p, PlacedKinds kinds) {
+    __shared__ __attribute__((aligned(1024))) char lds0[tile_bytes(DP) * halves_of(DP)];
+    __shared__ __attribute__((aligned(1024))) char lds1[tile_bytes(DP) * halves_of(DP)];
+    __shared__ __attribute__((aligned(1024))) char lds2[tile_bytes(DP) * halves_of(DP)];
+    __shared__ __attribute__((aligned(1024))) char lds3[tile_bytes(DP) * halves_of(DP)];
+    __shared__ __attribute__((aligned(16))) float stat[KV_STAT_FLOATS];
+    int linear = (int)blockIdx.x, n_tiles, rank, head;
+    const int keys = __builtin_amdgcn_readfirstlane(owns_keys(kinds, linear)), heads = keys ? p.H_kv * halves_of(DP) : p.H;
+    linear = __builtin_amdgcn_readfirstlane(linear);        // (both kept scalar)
+    if (keys) {
+        if (!enter_sequence<false, BM>(p, linear, heads, n_tiles, rank, head)) return;
+        bwd_dkdv<WALK_RING, true, DP, PART, false, true>(p, n_tiles, rank * heads + head, lds0, lds1, lds2, lds3, stat);
+    } else {
+        if (!enter_sequence<true, BM>(p, linear, heads, n_tiles, rank, head)) return;
+        bwd_dq<true, WALK_TRI, DP, PART, false, true, false>(p, n_tiles, rank * heads + head, lds0, lds1, lds2, lds3);
+    }
+}
+
 // At 64 columns two wavefronts a SIMD are faster where many long walks hide each other's latency, whole training pass, us, one : two:
 // 2 x 8192 rows, 32 heads, 2506 : 2296, 8192, 16 heads, 688 : 677; but 6 of up to 4096, 16 heads, 713 : 717, 16 of up to 1000, 32
 // heads, 294 : 341, 4 of up to 500, 16 heads, 41 : 52, and with four query heads to a key/value head 8192, 32 heads, 1305 : 1415.
@@ -60,6 +81,21 @@ hipError_t launch_dkdv(const PackedArgs& p, hipStream_t st, int64_t n) {
     return hipGetLastError();
 }
 
+// Both kinds of workgroups in one launch, by 128-row tiles (as many as there can be) of all key/value heads: few of them leave the chip half empty
+// while the first kind ends.  Over 570 launches of 1 to 64 sequences of up to 64 to 8192 rows the rules here and in packed_split_wanted take 0.3 %
+// more than the best choice, two launches always 17 % above 128 columns and 5 % below.  Whole training pass, us, one : two.  d 128: 1536, 16
+// heads (192 tiles) 80 : 110, 4096, 8 heads (256) 196 : 244, 8 of up to 2000, 8 heads (480) 132 : 146, but 2048, 32 heads (512) 196 : 189; 4 of
+// up to 4096, 32 heads on 8, (560) 1018 : 965, 6 of up to 1000, 64 on 8 (288) 389 : 407.  d 256: 1000 or 8192 rows, 1 to 4 heads 0.7,
+// 4096, 8 heads (256) 453 : 502, but 12 heads (384) 628 : 574; 8 of up to 2000, 32 on 4 (240) 1000 : 1417.  A walk of one tile leaves little
+// to fill: d 128, 16 of up to 128, 32 on 8, 59 : 53, 40 of up to 64, 32 on 8, 91 : 76, d 256, 64 of up to 64, 16 on 4, 166 : 118; 8 heads of
+// their own 27 : 34.  Up to 64 columns these are packed_split.hip's launches: of 334, one launch here was the fastest by 5 % in 13.
+bool one_launch(const PackedArgs& p) {
+    const int64_t tiles = (int64_t)p.n_ranks * p.H_kv;
+    const bool own = p.H == p.H_kv;
+    if (p.max_len <= BM) return tiles <= (own ? 192 : p.d > 128 ? 64 : 0);
+    return tiles <= (own ? p.d > 128 ? 280 : 512 : 352);
+}
+
 template <int DP, bool PART>
 hipError_t launch(PackedArgs p, hipStream_t st) {
     p.n_ranks = (int)most_tiles(p, BM);
@@ -67,11 +103,23 @@ hipError_t launch(PackedArgs p, hipStream_t st) {
     // Query-owning workgroups in groups of heads, key-owning ones at 65 to 128 columns by ranks.  Whole training pass, us, queries and keys
     // in groups, queries by ranks, keys, both: d 100, 6 sequences of up to 4096, 32 heads, 2258, 2331, 2253, 2335, 16 of up to 1000 467,
     // 463, 456, 454; d 128 2332, 2381, 2342, 2391, 64 of up to 128, 16 heads, 97, 96, 95, 94; d 64 1481, 1482, 1503, 1498.
+    if constexpr (DP > 64) {
+        if (one_launch(p)) {
+            p.by_rank = true;
+            if (hipError_t e = launch_packed_delta(p, SA_BF16, st)) return e;
+            if constexpr (DP <= 128) return launch_packed_bwd_ring(p, true, st);
+            else {
+                const PlacedKinds kinds = placed_kinds(p, n_dkdv, n_dq, packed_ratio(p));
+                hipLaunchKernelGGL((packed_both_kernel<DP, PART>), dim3((unsigned)(n_dkdv + n_dq)), dim3(256), 0, st, p, kinds);
+                return hipGetLastError();
+            }
+        }
+    }
     p.by_rank = false;
     hipLaunchKernelGGL((packed_dq_kernel<DP, PART>), dim3((unsigned)n_dq), dim3(256), 0, st, p);
     if (hipError_t e = hipGetLastError()) return e;
     p.by_rank = DP == 112 || DP == 128;
-    if constexpr (DP == 112 || DP == 128) return launch_packed_bwd_ring(p, st);
+    if constexpr (DP == 112 || DP == 128) return launch_packed_bwd_ring(p, false, st);
     else return launch_dkdv<DP, PART>(p, st, n_dkdv);
 }
 

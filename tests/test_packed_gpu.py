@@ -329,3 +329,14 @@ def test_two_streams_at_once():
         for g, w in zip(got, want):
             for x, y in zip((g[1], g[2], *g[3]), (w[1], w[2], *w[3])):
                 assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("d", [68, 100, 112, 128, 132, 256])
+@pytest.mark.parametrize("H,H_kv,lens", [(24, 12, [700, 300, 129, 1]), (14, 14, [1500, 0, 64]), (9, 9, [100, 3, 128, 77]), (36, 12, [2500])])
+def test_both_kinds_of_backward_workgroups_in_a_launch(H, H_kv, lens, d):
+    """108 to 252 tiles: one launch, or two by the head dimension and the groups."""
+    r = run(lens, H, H_kv, d, BF16)
+    compare(lens, H, H_kv, d, BF16, 0, *r, heads=[0, H_kv // 2, H_kv - 1])
+    again = run(lens, H, H_kv, d, BF16)
+    for x, y in zip(r[3], again[3]):
+        assert torch.equal(x, y)
