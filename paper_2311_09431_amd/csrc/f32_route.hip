@@ -41,8 +41,9 @@ constexpr Kind BWD_TERMS = {128, 32, {{5.12, 2.46, 1.23}, {4.98, 2.45, 1.09}, {1
 
 int up(int x, int by) { return (x - 1) / by + 1; }
 
-// waves: how many wavefronts share a walk by taking whole rounds in turn (1: all take part in each)
-double time_of(const Kind& k, const StepArgs& a, bool backward, int waves) {
+// waves: how many wavefronts share a walk by taking whole rounds in turn (1: all take part in each).  Of blocks that differ (packed
+// sequences): longest, the rows of the longest; blocks, how many of a.c rows there were
+double time_of(const Kind& k, const StepArgs& a, bool backward, int waves, int longest_rows, double blocks) {
     const Takes& t = k.by[a.d <= 32 ? 0 : a.d <= 64 ? 1 : a.d <= 112 ? 2 : 3];
     // contiguous layout: key shards behind the last played device are seen by nobody
     const int n_kv = a.layout == SA_STRIPED ? a.n_kv : a.q_dev + a.n_q - a.kv_dev < a.n_kv ? a.q_dev + a.n_q - a.kv_dev : a.n_kv;
@@ -56,13 +57,14 @@ double time_of(const Kind& k, const StepArgs& a, bool backward, int waves) {
     const int steps = up(a.c, k.rows > k.round ? k.rows : k.round);
     const double share = k.staged * mean((steps + 1) / (2. * steps)) + (1 - k.staged) * mean((m32 + 1) / (2. * m32));
     // the longest: of a triangular block the heaviest tile, whose wavefronts see nothing of the last rounds
-    const int own = k.rows / 32 < m32 ? k.rows / 32 : m32;
-    const double last = (m32 - (own - 1) / 2.) / m32;
+    const int long32 = up(longest_rows, 32), own = k.rows / 32 < long32 ? k.rows / 32 : long32;
+    const double last = (long32 - (own - 1) / 2.) / long32;
     const double seen = a.layout == SA_STRIPED ? last : a.n_q == 1 && a.kv_dev + n_kv <= a.q_dev ? 1. : (n_kv - 1 + last) / n_kv;
     const double longest_share = k.staged + (1 - k.staged) * seen;
-    const double queries = (double)a.B * a.H * a.n_q * tiles, keys = backward ? (double)a.B * a.H_kv * n_kv * tiles : 0.;
+    const double queries = blocks * a.H * a.n_q * tiles, keys = backward ? blocks * a.H_kv * n_kv * tiles : 0.;
     const double query_walk = (double)m * n_kv, key_walk = (double)m * a.n_q * (a.H / a.H_kv);
-    auto whole_rounds = [&](double walk) { return ceil(walk / waves) * waves; };
+    const double longer = (double)up(longest_rows, k.round) / m;
+    auto whole_rounds = [&](double walk) { return ceil(walk * longer / waves) * waves; };
     const double q = backward ? k.queries : 1.;
     double longest = q * (t.start + t.tile * longest_share * whole_rounds(query_walk));
     if (backward) longest = fmax(longest, t.start + t.tile * longest_share * whole_rounds(key_walk));
@@ -86,9 +88,9 @@ static bool alone_wanted(const StepArgs& a) {
 F32Route f32_route(const StepArgs& a, bool backward) {
     F32Route route = F32_TERMS;
     const bool wide = !backward && (int64_t)a.B * a.H * a.n_q * up(a.c, 128) >= 512;        // (as f32x3_step.hip decides)
-    double least = time_of(backward ? BWD_TERMS : wide ? FWD_TERMS_WIDE : FWD_TERMS, a, backward, 1);
+    double least = time_of(backward ? BWD_TERMS : wide ? FWD_TERMS_WIDE : FWD_TERMS, a, backward, 1, a.c, a.B);
     auto compete = [&](F32Route with, const Kind& k, int waves) {
-        const double t = time_of(k, a, backward, waves);
+        const double t = time_of(k, a, backward, waves, a.c, a.B);
         if (t < least) {
             least = t;
             route = with;
@@ -98,6 +100,23 @@ F32Route f32_route(const StepArgs& a, bool backward) {
     if (few_row_tiles(a, backward)) compete(F32_INSTRUCTION, backward ? BWD_INSTRUCTION : FWD_INSTRUCTION, 1);
     if (route == F32_TERMS && backward && alone_wanted(a)) route = F32_TERMS_ALONE;
     return route;
+}
+
+F32Route f32_packed_route(const StepArgs& a, int longest_rows, double blocks, bool wide, bool backward) {
+    const Kind* const kinds[] = {backward ? &BWD_INSTRUCTION : &FWD_INSTRUCTION, backward ? &BWD_SPLIT : &FWD_SPLIT,
+                                 backward ? &BWD_TERMS : wide ? &FWD_TERMS_WIDE : &FWD_TERMS};
+    const double tiles = blocks * up(a.c, 128);
+    const bool may[] = {tiles * a.H < 256 || (backward && tiles * a.H_kv <= 128) || (longest_rows <= 32 && a.d <= 64), longest_rows > 32, true};
+    int best = F32_TERMS;
+    double least = INFINITY;
+    for (int i : {F32_TERMS, F32_SPLIT, F32_INSTRUCTION}) {
+        const double t = may[i] ? time_of(*kinds[i], a, backward, i == F32_SPLIT ? a.d <= 64 ? 8 : 4 : 1, longest_rows, blocks) : INFINITY;
+        if (t < least) {
+            least = t;
+            best = i;
+        }
+    }
+    return (F32Route)best;
 }
 
 }  // namespace sa

@@ -1,11 +1,16 @@
 // Causal attention of packed sequences and its gradient, fp32 storage: which kernels play a launch, and those on the fp32 matrix
 // cores, the ring step's workgroups (f32_tiles.h), each on one tile of one sequence (packed.h).
 //
-// Up to 128 columns three kinds of kernels compete, as for a ring step (f32_route.hip), and the same rule decides, for as many rows in
-// sequences halfway between the mean and the longest: the lengths themselves are on the device.  Over 65 launches of 1 to 64 sequences
-// of up to 32 to 2048 rows what it picks takes 3 % more than the best kind (geometric mean; sequences of the mean length 4, of the longest
-// 5).  Sequences of one 32-row tile leave the wavefronts that share a walk without one: never those kernels.  64 of up to 32 rows, 16 heads,
-// d 32, forward 11 us on the fp32 instruction, 23 there, whole pass 53, 81; d 128, in terms 43, 60, 152, 256.
+// Up to 128 columns three kinds of kernels compete, as for a ring step, by the times that are put together there (f32_route.hip): the longest walk is
+// that of a sequence of max_len rows, the load that of as many rows in sequences a quarter of the way from the mean to the longest (the lengths
+// themselves are on the device).  Over 428 launches of 1 to 64 sequences of up to 32 to 4096 rows, d 64 and 128, forward and backward, what is picked
+// takes 0.03 to 0.6 % more than the best kind; with one length for both, halfway, 0.6 to 1.3 %: 5 of up to 777 rows, 16 heads on 4, d 64, forward
+// 53 : 43 us, 8 of up to 2000, 4 heads, backward 166 : 148, 5 of up to 777, 32 on 8, d 128, backward 506 : 373.
+// Sequences of one 32-row tile leave the wavefronts that share a walk without one: never those kernels, and up to 64 columns the fp32
+// instruction in launches of any size.  64 of up to 32 rows, 16 heads, d 32, forward 11 us on the fp32 instruction, 23 there, whole pass 53, 81; d
+// 128, in terms 43, 60, 152, 256.
+#include <math.h>
+
 #include <algorithm>
 
 #include "f32_tiles.h"
@@ -53,13 +58,15 @@ hipError_t launch_packed_f32(PackedArgs p, bool backward, hipStream_t st) {
     p.by_rank = true;
     const int64_t mean = std::min((int64_t)p.max_len, ((int64_t)p.rows + p.n_seq - 1) / p.n_seq);
     StepArgs like = p;
-    like.c = (int)((mean + p.max_len + 1) / 2);
-    like.B = (int)((p.rows + (int64_t)like.c - 1) / like.c);
-    if (p.d > 128) return few_row_tiles(like, backward) ? run<256, 2>(p, backward, st) : run<256, 1>(p, backward, st);
+    like.c = (int)((3 * mean + p.max_len + 2) / 4);
+    const double blocks = std::max(1., (double)p.rows / like.c);
+    if (p.d > 128) {
+        like.B = (int)ceil(blocks);
+        return few_row_tiles(like, backward) ? run<256, 2>(p, backward, st) : run<256, 1>(p, backward, st);
+    }
     StepArgs longest = p;
     longest.c = p.max_len;
-    F32Route route = f32_route(like, backward);
-    if (route == F32_SPLIT && p.max_len <= 32) route = p.d <= 64 ? F32_INSTRUCTION : F32_TERMS;
+    F32Route route = f32_packed_route(like, p.max_len, blocks, most_tiles(p, 128) * p.H >= 512, backward);
     if (route == F32_SPLIT && !f32x3_split_supported(longest, backward)) route = F32_TERMS;
     if (route == F32_SPLIT) return launch_packed_f32x3_split(p, backward, st);
     if (route != F32_INSTRUCTION) return launch_packed_f32x3(p, backward, st);

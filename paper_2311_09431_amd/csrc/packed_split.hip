@@ -38,7 +38,7 @@ hipError_t run(PackedArgs p, bool backward, hipStream_t st) {
 // By 128-row tiles (as many as there can be) of all query heads, and of all key/value heads in the backward.  us, 128-row kernels : these.
 // Forward, d 128: 3 sequences of up to 300 rows, 8 heads (48 tiles) 10.4 : 8.8, 2048, 8 heads (128) 34 : 25, 4 of up to 4096, 2 heads (144)
 // 60 : 35, 1000, 16 heads (128) 21 : 20, but 16 of up to 300, 4 heads (136) 10.8 : 13.5, 5 of up to 200, 16 heads (144) 9.9 : 14.6; 8192, 4 heads
-// (256) 114 : 106, but 4096, 8 heads (256) 62 : 66.  d 64 likewise.
+// (256) 114 : 106, but 4096, 8 heads (256) 62 : 66; 5 of up to 777, 4 heads (68) 18 : 11, 8 heads (136) 18 : 17.  d 64 likewise.
 // Backward, those kernels in one launch or two (packed_bwd.hip), the better, whole pass: d 128, 2000, 6 of up to, 16 heads on 2 (122) 426 : 312, 2
 // of up to 4096, 32 heads on 4 (184) 899 : 848, 4 of up to 2000, 6 heads (144) 82 : 77, but 16 of up to 128, 8 heads (128) 27 : 34, 3000, 6
 // heads (144) 120 : 122, 4 of up to 3000, 32 on 4 (212) 724 : 763; below 96 tiles to 0.5.  d 64, 16 of up to 1000, 32 on 4 (328) 290 : 256, 8 of up
@@ -48,7 +48,7 @@ bool packed_split_wanted(const PackedArgs& p, bool backward) {
     const int64_t widest = p.stride_s > p.kv_stride_s ? p.stride_s : p.kv_stride_s;
     if (p.d > TD || ((int64_t)(p.max_len + 127) / 128 * 128 + OWN) * 2 * widest + 2 * p.d >= (int64_t(1) << 31)) return false;
     const int64_t tiles = most_tiles(p, 128) * (backward ? p.H_kv : p.H);
-    if (!backward) return tiles <= 64 || (tiles <= 144 && p.max_len >= 1000) || (tiles <= 256 && p.max_len >= 8192);
+    if (!backward) return tiles <= 80 || (tiles <= 144 && p.max_len >= 700) || (tiles <= 256 && p.max_len >= 8192);
     if (p.d <= 64) return tiles <= (p.max_len >= 1000 ? 512 : p.max_len <= 64 || p.max_len > 128 ? 320 : 160);
     const int64_t walk = (int64_t)p.max_len * (p.H / p.H_kv);
     return tiles <= (walk >= 12000 ? 184 : walk >= 2000 ? 152 : 96);

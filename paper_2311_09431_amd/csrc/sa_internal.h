@@ -226,6 +226,8 @@ hipError_t launch_bwd_f32(const StepArgs& a, int dtype, hipStream_t st);
 // the backward's with one wavefront to 32 rows)
 enum F32Route : int { F32_INSTRUCTION = 0, F32_SPLIT = 1, F32_TERMS = 2, F32_TERMS_ALONE = 3 };
 F32Route f32_route(const StepArgs& a, bool backward);
+// packed sequences: `blocks` of a.c rows, the longest of longest_rows; wide: the forward's 128-row kind takes 256
+F32Route f32_packed_route(const StepArgs& a, int longest_rows, double blocks, bool wide, bool backward);
 hipError_t launch_f32x3(const StepArgs& a, bool backward, bool alone, hipStream_t st);
 bool f32x3_split_supported(const StepArgs& a, bool backward);
 hipError_t launch_f32x3_split(const StepArgs& a, bool backward, hipStream_t st);
