@@ -23,6 +23,17 @@ inline int64_t most_tiles(const PackedArgs& p, int tile) {
     return each * p.n_seq < by_rows ? each * p.n_seq : by_rows;
 }
 
+// Order of a bf16 launch's 128-row tiles: by ranks over all heads, which leaves the lightest tiles to the end, but in groups of heads, whose K and V
+// (Q and dO) an XCD's cache then serves, where those of all are too many for the cache behind it.  us, groups : ranks, forward: d 100, 6 sequences of
+// up to 4096, 32 heads (227 MB) 514 : 586, 64 (453 MB) .76, 2 of up to 8192, 32 heads (196 MB) 850 : 881; but 16 heads 1, 3 of up to 4096, 64
+// heads (168 MB, 54 tiles) 357 : 340, 64 of up to 300, 64 heads (258 MB) 1.08; four query heads share them: 8 of up to 4096, 32 on 8, d 128,
+// 564 : 554, 16 of up to 1000 100 : 96.  Over 336 forward launches, d 100 to 256, 0.3 % from the better of the two, ranks always 2.8.  Whole
+// training pass, d 128, 6 of up to 4096, 64 heads, 4763 : 5201, 2 of up to 8192 7868 : 8267, 3 of up to 4096 1596 : 1533, 64 of up to 300
+// 927 : 908, d 256 11048 : 12182, 18441 : 19421, 3560 : 3495, 1989 : 1863.
+inline bool by_rank_wanted(const PackedArgs& p) {
+    return 4. * p.rows * p.H_kv * p.d < 180e6 * (p.H / p.H_kv) || p.n_ranks < 64 || p.max_len < 400;
+}
+
 // Rows first .. first + len - 1 of sequence s.  Whatever the offsets hold, they lie within the tensors: an offset below zero or
 // behind the last row is taken as the nearest one that is none, a sequence that ends before it begins is empty.
 struct Span { int first, len; };

@@ -100,12 +100,9 @@ template <int DP, bool PART>
 hipError_t launch(PackedArgs p, hipStream_t st) {
     p.n_ranks = (int)most_tiles(p, BM);
     const int64_t n_dq = (int64_t)p.n_ranks * p.H, n_dkdv = (int64_t)p.n_ranks * p.H_kv * halves_of(DP);
-    // Query-owning workgroups in groups of heads, key-owning ones at 65 to 128 columns by ranks.  Whole training pass, us, queries and keys
-    // in groups, queries by ranks, keys, both: d 100, 6 sequences of up to 4096, 32 heads, 2258, 2331, 2253, 2335, 16 of up to 1000 467,
-    // 463, 456, 454; d 128 2332, 2381, 2342, 2391, 64 of up to 128, 16 heads, 97, 96, 95, 94; d 64 1481, 1482, 1503, 1498.
+    p.by_rank = by_rank_wanted(p);
     if constexpr (DP > 64) {
         if (one_launch(p)) {
-            p.by_rank = true;
             if (hipError_t e = launch_packed_delta(p, SA_BF16, st)) return e;
             if constexpr (DP <= 128) return launch_packed_bwd_ring(p, true, st);
             else {
@@ -115,10 +112,8 @@ hipError_t launch(PackedArgs p, hipStream_t st) {
             }
         }
     }
-    p.by_rank = false;
     hipLaunchKernelGGL((packed_dq_kernel<DP, PART>), dim3((unsigned)n_dq), dim3(256), 0, st, p);
     if (hipError_t e = hipGetLastError()) return e;
-    p.by_rank = DP == 112 || DP == 128;
     if constexpr (DP == 112 || DP == 128) return launch_packed_bwd_ring(p, false, st);
     else return launch_dkdv<DP, PART>(p, st, n_dkdv);
 }

@@ -25,9 +25,7 @@ hipError_t launch(const PackedArgs& p, hipStream_t st) {
 hipError_t launch_packed_fwd(PackedArgs p, hipStream_t st) {
     if (packed_split_wanted(p, false)) return launch_packed_split(p, false, st);
     p.n_ranks = (int)most_tiles(p, BM);
-    // by ranks over all heads: 8 sequences of up to 4096, 32 heads on 8, d 128, in groups of heads 592 us, so 581, 16 of up to 4096 829, 812,
-    // 16 of up to 1000 104, 100; 4 of up to 500 17.5, 18.0
-    p.by_rank = true;
+    p.by_rank = by_rank_wanted(p);
     const bool part = p.d % 8 != 0;
     if (p.d > 128) return part ? launch<256, true>(p, st) : launch<256, false>(p, st);
     if (p.d <= 32 && !part) return launch<32, false>(p, st);

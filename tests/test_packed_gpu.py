@@ -340,3 +340,12 @@ def test_both_kinds_of_backward_workgroups_in_a_launch(H, H_kv, lens, d):
     again = run(lens, H, H_kv, d, BF16)
     for x, y in zip(r[3], again[3]):
         assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("d", [100, 128, 256])
+def test_tiles_in_groups_of_heads(d):
+    """Over 180 MB of keys and values, as many as 100 tiles a head: the order of the workgroups is another."""
+    lens = [1900, 20, 700] + [20] * 58 + [2600]
+    assert 4 * sum(lens) * 80 * d > 180e6
+    r = run(lens, 80, 80, d, BF16)
+    compare(lens, 80, 80, d, BF16, 0, *r, heads=[0, 39, 79])
