@@ -349,3 +349,31 @@ def test_tiles_in_groups_of_heads(d):
     assert 4 * sum(lens) * 80 * d > 180e6
     r = run(lens, 80, 80, d, BF16)
     compare(lens, 80, 80, d, BF16, 0, *r, heads=[0, 39, 79])
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_parts_of_larger_tensors(dtype):
+    """Rows, heads and sums that are parts of larger tensors; what lies beside them stays."""
+    lens, H, H_kv, d = [200, 1, 60], 4, 2, 64
+    T = sum(lens)
+    (q, k, v, g), out, lse, grads = run(lens, H, H_kv, d, dtype)
+
+    def part(x, heads):
+        whole = torch.full((T + 3, heads + 3, d + 8), 9, dtype=dtype, device="cuda")
+        inside = whole[1:T + 1, 2:2 + heads, :d]
+        if x is not None:
+            inside.copy_(x)
+        return whole, inside
+
+    sums = [torch.full((H + 1, T + 5), 9.0, device="cuda") for _ in range(2)]
+    L, D = (x[:H, :T] for x in sums)
+    off = lengths_to_offsets(lens).cuda()
+    Q, G, O, DQ = (part(x, H) for x in (q, g, None, None))
+    K, V, DK, DV = (part(x, H_kv) for x in (k, v, None, None))
+    sa.sa_attn_packed_fwd(Q[1], K[1], V[1], off, O[1], L, 200)
+    sa.sa_attn_packed_bwd(Q[1], K[1], V[1], O[1], G[1], L, off, D, DQ[1], DK[1], DV[1], 200)
+    for (whole, got), want in ((O, out), (DQ, grads[0]), (DK, grads[1]), (DV, grads[2])):
+        assert torch.equal(got, want)
+        got.fill_(9)
+        assert (whole == 9).all()
+    assert torch.equal(L, lse) and (sums[0][H:] == 9).all() and (sums[0][:, T:] == 9).all()

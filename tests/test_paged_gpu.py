@@ -315,6 +315,29 @@ def test_a_single_page_of_any_page_stride():
     compare(q, [[x[0, :41].cpu() for x in (k, v)]], out.cpu(), lse.cpu(), BF16)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("width", WIDTHS)
+def test_decode_strided(width, dtype):
+    """Queries and results side by side with other heads, a table and sums that are parts of larger ones; nothing beside them changes."""
+    lens, H, H_kv, d, page = [77, 1, 0, 300], 4, 2, 68, 16
+    q, rows, out, lse = decode(lens, H, H_kv, d, dtype, page, width=width)
+    table, pool = tables(lens, page, 1, width=width)
+    k_cache, v_cache = (cache(pool, page, H_kv, d, dtype, "shd") for _ in range(2))
+    fill(k_cache, v_cache, table, lens, 10)
+    wide = torch.full((len(lens), H + 5, d + 4), 9, dtype=dtype, device="cuda")
+    q_wide = wide.clone()
+    q_wide[:, 1:1 + H, :d] = q.cuda()
+    pages = torch.full((len(lens), table.shape[1] + 3), 2 ** 30, dtype=torch.int32)
+    pages[:, 2:-1] = table
+    sums = torch.full((len(lens), H + 2), 9.0, device="cuda")
+    q_part, out_part = q_wide[:, :, :d][:, 1:1 + H], wide[:, :, :d][:, 1:1 + H]
+    work = torch.empty(sa.sa_attn_decode_workspace(q_part, k_cache), dtype=torch.uint8, device="cuda")
+    sa.sa_attn_decode(q_part, k_cache, v_cache, pages.cuda()[:, 2:-1], torch.tensor(lens, dtype=torch.int32, device="cuda"), out_part, sums[:, :H],
+                      work)
+    assert torch.equal(out_part.cpu(), out) and torch.equal(sums[:, :H].cpu(), lse)
+    assert (wide[:, 0] == 9).all() and (wide[:, 1 + H:] == 9).all() and (wide[..., d:] == 9).all() and (sums[:, H:] == 9).all()
+
+
 # ---------------------------------------------------------------- append
 
 
@@ -393,6 +416,16 @@ def test_append_strided_rows(dtype):
         sa.sa_cache_append(plain[1], plain[2], slot, *want, pos=pos, k_out=plain[1], q=plain[0], q_out=plain[0])
         assert torch.equal(q, plain[0]) and torch.equal(k, plain[1]) and torch.equal(v, plain[2])
         assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+@pytest.mark.parametrize("base", [1.5, 500000.0])
+def test_append_positions_of_any_sign(base):
+    x, v = normal((4, 2, 64), 1, F32), normal((4, 2, 64), 2, F32)
+    pos = torch.tensor([-3, 0, -100000, 7], dtype=torch.int32)
+    k_cache, v_cache = (cache(1, 16, 2, 64, F32, "shd", 0) for _ in range(2))
+    sa.sa_cache_append(x.cuda(), v.cuda(), torch.arange(4, dtype=torch.int32, device="cuda"), k_cache, v_cache, pos=pos.cuda(), base=base)
+    want = rotated(x, pos, base)
+    check("rotated", k_cache[0, :4], want, off_of(x, want, F32))
 
 
 def test_append_more_rows_than_a_launch_takes():
