@@ -269,7 +269,7 @@ typedef struct {
 /*
  * Forward: O = softmax(scale Q K^T, causal within a sequence) V rounded once to `dtype`, LSE = the rows' log-sum-exp.  Infinities
  * and NaN: as the ring step's blocks of 128 rows and more (fp32: as its fp32 storage); nothing of one sequence reaches another.
- * Errors: NULL, DTYPE, ALIGN, SHAPE (also: bf16 and a sequence of max_len rows reaches over 2^31 bytes, or more workgroups than
+ * Errors: NULL, DTYPE, ALIGN, SHAPE (also: bf16 and a sequence of max_len rows reaches over 2^31 bytes or 128 rows do, or more workgroups than
  * a launch takes for a single key/value head), HIP.
  */
 int sa_attn_packed_fwd(const void* q, const void* k, const void* v, const int32_t* offsets, void* out, float* lse,

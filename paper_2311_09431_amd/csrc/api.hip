@@ -524,7 +524,8 @@ int sa_attn_packed_fwd(const void* q, const void* k, const void* v, const int32_
     if (int e = check_packed(shape)) return e;
     if (shape->n_seq == 0 || shape->rows == 0 || shape->max_len == 0) return SA_OK;
     if (!q || !k || !v || !offsets || !out || !lse) return SA_ERR_NULL;
-    if (!packed_in_reach(shape, shape->kv_stride_s)) return SA_ERR_SHAPE;
+    // (queries: a tile's 128 rows)
+    if (!packed_in_reach(shape, shape->kv_stride_s) || (shape->dtype == SA_BF16 && shape->stride_s >= (1 << 23))) return SA_ERR_SHAPE;
     if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out) || (reinterpret_cast<uintptr_t>(offsets) & 3u) ||
         (reinterpret_cast<uintptr_t>(lse) & 3u))
         return SA_ERR_ALIGN;

@@ -59,6 +59,16 @@ struct Rows {
         load_b_frags<8>(b, row_b, h, d);
         asm volatile("" : : : "memory");
     }
+    // without branches: row `row` of matrices of `rows`
+    __device__ __forceinline__ Rows(const __bf16* of_a, const __bf16* of_b, int rows, int pitch, int row, int h, int d) {
+        load_b_frags<8>(a, of_a, rows, pitch, row, h, d);
+        load_b_frags<8>(b, of_b, rows, pitch, row, h, d);
+        asm volatile("" : : : "memory");
+    }
+    __device__ __forceinline__ void zero_beyond(int h, int d) {
+        zero_part<8>(a, h, d);
+        zero_part<8>(b, h, d);
+    }
     template <int N_ACC>
     __device__ __forceinline__ void keep() const {
         typedef int i32x4 __attribute__((ext_vector_type(4)));
@@ -97,13 +107,13 @@ struct OutRow {
 #pragma unroll
         for (int i = 0; i < 4 * blocks_of(DP); ++i) put(r + 4 * h, i, make_float4(0.f, 0.f, 0.f, 0.f), mul, first, h, d);
     }
-    __device__ __forceinline__ static void set(__bf16* r, float mul, int first, int h, int d) {
+    __device__ __forceinline__ static void set(__bf16* r, float mul, int first, bool row_ok, int h, int d) {
 #pragma unroll
-        for (int i = 0; i < 4 * blocks_of(DP); ++i) {
-            bf16x4 y;
+        for (int i = 0; i < 4 * blocks_of(DP); i += 2) {
+            bf16x4 y[2];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) y[e] = (__bf16)(mul * acc_read(first + 4 * i + e));
-            if (inside(i, h, d)) *reinterpret_cast<bf16x4*>(r + 8 * i + 4 * h) = y;
+            for (int e = 0; e < 8; ++e) y[e / 4][e % 4] = (__bf16)(mul * acc_read(first + 4 * i + e));
+            store_two_chunks(r, 8 * i, y[0], y[1], row_ok, h, d);
         }
     }
 };
@@ -257,7 +267,8 @@ __device__ __forceinline__ void dkdv_ring(const StepArgs& p, int n_tiles, int li
     const int pitch = 2 * (int)p.stride_s;
     const int k0 = ktile * BM, key_own = k0 + 32 * wave + n, key = min(key_own, p.c - 1);
 
-    const Rows rows_kv((const __bf16*)p.k + kv_base + (int64_t)key * ss, (const __bf16*)p.v + kv_base + (int64_t)key * ss, h, d);
+    Rows rows_kv = PACKED ? Rows((const __bf16*)p.k + kv_base, (const __bf16*)p.v + kv_base, p.c, 2 * (int)ss, key, h, d)
+                          : Rows((const __bf16*)p.k + kv_base + (int64_t)key * ss, (const __bf16*)p.v + kv_base + (int64_t)key * ss, h, d);
     const int group = p.H / p.H_kv, dev_end = p.q_dev + p.n_q, n_qt = (p.c + DT_ROWS - 1) / DT_ROWS;
     // contiguous layout: earlier devices' queries see nothing of these keys
     const int dev0 = p.layout != SA_STRIPED ? max(p.q_dev, dev) : p.q_dev;
@@ -335,6 +346,7 @@ __device__ __forceinline__ void dkdv_ring(const StepArgs& p, int n_tiles, int li
     };
     request();
     request();
+    if constexpr (PACKED && PART) rows_kv.zero_beyond(h, d);
     rows_kv.keep<128>();
     const float kappa = p.scale * LOG2E;
     uint32_t arow[8], tr0[4], tr1[4];
@@ -450,12 +462,12 @@ __device__ __forceinline__ void dkdv_ring(const StepArgs& p, int n_tiles, int li
     }
     wait_all_but<0>();  // (the last requests are on their way into this workgroup's slots)
     acc_settle();
-    if (key_own >= p.c) return;
     if constexpr (PACKED) {
-        OutRow<DP>::set((__bf16*)p.dv + kv_base + (int64_t)key * ss, 1.f, ACC_DV, h, d);
-        OutRow<DP>::set((__bf16*)p.dk + kv_base + (int64_t)key * ss, p.scale, ACC_DK, h, d);
+        OutRow<DP>::set((__bf16*)p.dv + kv_base + (int64_t)key * ss, 1.f, ACC_DV, key_own < p.c, h, d);
+        OutRow<DP>::set((__bf16*)p.dk + kv_base + (int64_t)key * ss, p.scale, ACC_DK, key_own < p.c, h, d);
         return;
     }
+    if (key_own >= p.c) return;
     float* const v_at = p.dv + kv_base + (int64_t)key * ss;
     float* const k_at = p.dk + kv_base + (int64_t)key * ss;
     if (p.fresh) {
@@ -565,7 +577,8 @@ __device__ __forceinline__ void dq_ring(const StepArgs& p, int n_tiles, int line
     const int pitch = 2 * (int)p.kv_stride_s;
     const int q0 = qt * BM, a_own = q0 + 32 * wave + n, a = min(a_own, p.c - 1);
 
-    const Rows rows_qg((const __bf16*)p.q + base + (int64_t)a * ss, (const __bf16*)p.dout + base + (int64_t)a * ss, h, d);
+    Rows rows_qg = PACKED ? Rows((const __bf16*)p.q + base, (const __bf16*)p.dout + base, p.c, 2 * (int)ss, a, h, d)
+                          : Rows((const __bf16*)p.q + base + (int64_t)a * ss, (const __bf16*)p.dout + base + (int64_t)a * ss, h, d);
     float lse2 = p.lse[sbase + a] * LOG2E, delta = p.delta[sbase + a];
     // contiguous layout: the blocks of devices further on are entirely masked
     const int kv_end = p.layout == SA_STRIPED ? p.kv_dev + p.n_kv : min(p.kv_dev + p.n_kv, dev + 1);
@@ -633,6 +646,7 @@ __device__ __forceinline__ void dq_ring(const StepArgs& p, int n_tiles, int line
     };
     request();
     request();
+    if constexpr (PACKED && PART) rows_qg.zero_beyond(h, d);
     rows_qg.keep<64>();
     const float kappa = p.scale * LOG2E;
     // (complete here: a load left pending would be waited for with the tile requested next)
@@ -713,11 +727,11 @@ __device__ __forceinline__ void dq_ring(const StepArgs& p, int n_tiles, int line
     queries_step<false, true, DP, PART>(s_b, dp_b, s_a, dp_a, kappa, lse2, delta, arow, tr0, tr1, pre, lds, lds + HALF, lim_at - 32, part_ks, none);
     wait_all_but<0>();
     acc_settle();
-    if (a_own >= p.c) return;
     if constexpr (PACKED) {
-        OutRow<DP>::set((__bf16*)p.dq + base + (int64_t)a * ss, p.scale, ACC_DQ, h, d);
+        OutRow<DP>::set((__bf16*)p.dq + base + (int64_t)a * ss, p.scale, ACC_DQ, a_own < p.c, h, d);
         return;
     }
+    if (a_own >= p.c) return;
     float* const q_at = p.dq + base + (int64_t)a * ss;
     if (p.fresh) OutRow<DP>::set(q_at, p.scale, ACC_DQ, h, d);
     else OutRow<DP>(q_at, h, d).add(p.scale, ACC_DQ, h, d);

@@ -37,11 +37,14 @@ constexpr int BN = TR;    // rows streamed per tile
 constexpr int D = TD;
 
 // four neighbouring columns of a row, rounded once
-__device__ inline void store_bf16(__bf16* to, const f32x16& x, int first, float mul) {
-    bf16x4 y;
+__device__ inline void store_bf16(__bf16* row, int col, const f32x16& x, float mul, bool row_ok, int h, int d) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) y[e] = (__bf16)(mul * x[first + e]);
-    *reinterpret_cast<bf16x4*>(to) = y;
+    for (int g = 0; g < 4; g += 2) {
+        bf16x4 y[2];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e / 4][e % 4] = (__bf16)(mul * x[4 * g + e]);
+        store_two_chunks(row, col + 8 * g, y[0], y[1], row_ok, h, d);
+    }
 }
 
 __device__ inline bf16x8 pack8(const f32x16& x, int first) {
@@ -212,15 +215,24 @@ __device__ __forceinline__ void bwd_dq(const StepArgs& p, int n_tiles, int linea
     load_tile(Vr, tile_pitch, v_lds1);
 
     bf16x8 qf[8 * NH], gf[8 * NH];
-    load_b_frags<8 * NH>(qf, Q + (int64_t)a * ss, h, d);
-    load_b_frags<8 * NH>(gf, G + (int64_t)a * ss, h, d);
+    if constexpr (PACKED) {
+        load_b_frags<8 * NH>(qf, Q, p.c, 2 * (int)ss, a, h, d);
+        load_b_frags<8 * NH>(gf, G, p.c, 2 * (int)ss, a, h, d);
+    } else {
+        load_b_frags<8 * NH>(qf, Q + (int64_t)a * ss, h, d);
+        load_b_frags<8 * NH>(gf, G + (int64_t)a * ss, h, d);
+    }
     const float kappa = p.scale * LOG2E;
     float lse2 = p.lse[sbase + a] * LOG2E;
     float delta;
     if constexpr (FORM_DELTA) {
         // formed here, from the rows that the lane holds anyway, and stored for the key-owning workgroups behind this launch
         bf16x8 of[8 * NH];
-        load_b_frags<8 * NH>(of, (const __bf16*)p.o + base + (int64_t)a * ss, h, d);
+        load_b_frags<8 * NH>(of, (const __bf16*)p.o + base, p.c, 2 * (int)ss, a, h, d);
+        if constexpr (PART) {
+            zero_part<8 * NH>(of, h, d);
+            zero_part<8 * NH>(gf, h, d);
+        }
         float x = 0.f;
 #pragma unroll
         for (int i = 0; i < 8 * NH; ++i)
@@ -230,6 +242,10 @@ __device__ __forceinline__ void bwd_dq(const StepArgs& p, int n_tiles, int linea
         if (h == 0 && row_ok) const_cast<float*>(p.delta)[sbase + a] = delta;
     } else {
         delta = p.delta[sbase + a];
+    }
+    if constexpr (PACKED && PART) {
+        zero_part<8 * NH>(qf, h, d);
+        if constexpr (!FORM_DELTA) zero_part<8 * NH>(gf, h, d);
     }
     f32x16 acc[4 * NH];
 #pragma unroll
@@ -326,16 +342,17 @@ __device__ __forceinline__ void bwd_dq(const StepArgs& p, int n_tiles, int linea
     trip(F{}, T{}, P0{}, F{}, t, Kr, Vr, 0);
     trip(T{}, T{}, P1{}, F{}, t + 1, Kr, Vr, 0);
 
+    if constexpr (PACKED) {
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb) store_bf16((__bf16*)p.dq + base + (int64_t)a * ss, 32 * mb, acc[mb], p.scale, row_ok, h, d);
+        return;
+    }
 #pragma unroll
     for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
             const int col = 32 * mb + 8 * g + 4 * h;
             if (col >= d || !row_ok) continue;            // padding columns, rows beyond the shard
-            if constexpr (PACKED) {
-                store_bf16((__bf16*)p.dq + base + (int64_t)a * ss + col, acc[mb], 4 * g, p.scale);
-                continue;
-            }
             float4* dst = reinterpret_cast<float4*>(DQ + (int64_t)a * ss + col);
             float4 x = RING && p.fresh ? make_float4(0.f, 0.f, 0.f, 0.f) : *dst;
             x.x = fmaf(p.scale, acc[mb][4 * g + 0], x.x); x.y = fmaf(p.scale, acc[mb][4 * g + 1], x.y);
@@ -600,8 +617,17 @@ __device__ __forceinline__ void bwd_dkdv(const StepArgs& p, int n_tiles, int lin
     float rstat = stat_fetch();         // statistics of the tile after the present one
 
     bf16x8 kf[8 * NH], vf[8 * NH];
-    load_b_frags<8 * NH>(kf, K + (int64_t)key * ss, h, d);
-    load_b_frags<8 * NH>(vf, V + (int64_t)key * ss, h, d);
+    if constexpr (PACKED) {
+        load_b_frags<8 * NH>(kf, K, p.c, 2 * (int)ss, key, h, d);
+        load_b_frags<8 * NH>(vf, V, p.c, 2 * (int)ss, key, h, d);
+        if constexpr (PART) {
+            zero_part<8 * NH>(kf, h, d);
+            zero_part<8 * NH>(vf, h, d);
+        }
+    } else {
+        load_b_frags<8 * NH>(kf, K + (int64_t)key * ss, h, d);
+        load_b_frags<8 * NH>(vf, V + (int64_t)key * ss, h, d);
+    }
     const float kappa = p.scale * LOG2E;
     f32x16 acck[4], accv[4];
 #pragma unroll
@@ -709,6 +735,15 @@ __device__ __forceinline__ void bwd_dkdv(const StepArgs& p, int n_tiles, int lin
     trip(M{}, P0{}, F{}, F{}, mask_base - 64 * t, 0);
     trip(M{}, P1{}, T{}, F{}, mask_base - 64 * t - 64, 0);
 
+    if constexpr (PACKED) {
+        const int64_t row = kv_base + (int64_t)key * ss;
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb) {
+            store_bf16((__bf16*)p.dv + row, 128 * ohalf + 32 * mb, accv[mb], 1.f, key_ok, h, d);
+            store_bf16((__bf16*)p.dk + row, 128 * ohalf + 32 * mb, acck[mb], p.scale, key_ok, h, d);
+        }
+        return;
+    }
 #pragma unroll
     for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
@@ -716,11 +751,6 @@ __device__ __forceinline__ void bwd_dkdv(const StepArgs& p, int n_tiles, int lin
             const int col = 128 * ohalf + 32 * mb + 8 * g + 4 * h;
             if (col >= d || !key_ok) continue;            // padding columns, keys beyond the shard
             const int64_t o = (int64_t)key * ss + col;
-            if constexpr (PACKED) {
-                store_bf16((__bf16*)p.dv + kv_base + o, accv[mb], 4 * g, 1.f);
-                store_bf16((__bf16*)p.dk + kv_base + o, acck[mb], 4 * g, p.scale);
-                continue;
-            }
             float4 x = make_float4(0.f, 0.f, 0.f, 0.f), y = x;
             if (!RING || !p.fresh) {
                 x = *reinterpret_cast<float4*>(DV + o);

@@ -369,7 +369,12 @@ fwd_mfma_kernel(Args p, int n_qtiles) {
     load_k(K, tile_pitch, k_lds1);     // n_kt >= 2 always
 
     bf16x8 qf[8 * NH];
-    load_b_frags<8 * NH>(qf, Q + (int64_t)a * ss, h, d);
+    if constexpr (PACKED) {
+        load_b_frags<8 * NH>(qf, Q + (int64_t)q0 * ss, min(BM, p.c - q0), 2 * (int)ss, a - q0, h, d);
+        if constexpr (PART) zero_part<8 * NH>(qf, h, d);
+    } else {
+        load_b_frags<8 * NH>(qf, Q + (int64_t)a * ss, h, d);
+    }
     int q_position = 0;
     if (ROPE) {
         q_position = p.q_pos[b * p.pos_stride_b + a];
@@ -537,13 +542,14 @@ fwd_mfma_kernel(Args p, int n_qtiles) {
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
             const int col = 32 * mb + 8 * g + 4 * h;
-            if (col >= d || !row_ok) continue;            // padding columns, rows beyond the shard
             if constexpr (PACKED) {
-                bf16x4 y;
+                if (g % 2) continue;
+                bf16x4 y[2];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) y[e] = (__bf16)(oacc[mb][4 * g + e] * a_part);
-                *reinterpret_cast<bf16x4*>(O + (int64_t)a * ss + col) = y;
+                for (int e = 0; e < 8; ++e) y[e / 4][e % 4] = (__bf16)(oacc[mb][4 * g + e] * a_part);
+                store_two_chunks(O + (int64_t)a * ss, col - 4 * h, y[0], y[1], row_ok, h, d);
             } else {
+                if (col >= d || !row_ok) continue;        // padding columns, rows beyond the shard
                 float4* dst = reinterpret_cast<float4*>(O + (int64_t)a * ss + col);
                 float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
                 if (a_old != 0.f) {

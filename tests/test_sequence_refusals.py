@@ -64,6 +64,11 @@ def test_packed_shapes(kw, status):
     assert L.sa_attn_packed_bwd(*[P] * 11, ctypes.byref(s), None) == status
 
 
+def test_packed_rows_too_far_apart():
+    """128 rows of queries beyond 2^31 bytes"""
+    assert sa.lib().sa_attn_packed_fwd(*[P] * 6, ctypes.byref(packed(stride_s=1 << 23)), None) == E_SHAPE
+
+
 def test_packed_pointers():
     L, s = sa.lib(), packed()
     assert L.sa_attn_packed_fwd(*[P] * 6, None, None) == E_NULL and L.sa_attn_packed_bwd(*[P] * 11, None, None) == E_NULL
