@@ -2,8 +2,8 @@
 // packed_bwd_ring.hip), each on one 128-row tile of one sequence (packed.h).  The query-owning ones come first and form delta =
 // rowsum(dO * O) of their rows for both.
 //
-// Bound as the ring step's backward is, by products and the vector work beside them: 6 sequences of up to 4096 rows, 32 heads, d 100, dQ 0.72 and
-// dK, dV 1.08 ms beside 0.55 forward; whole training pass, d 128, 2.34 ms, d 64 1.48.
+// Bound as the ring step's backward is, by products and the vector work beside them: 6 sequences of up to 4096 rows, 32 heads, d 100, dQ 0.67 and
+// dK, dV 1.01 ms beside 0.49 forward, whole training pass 2.19.
 #include "bwd_tiles.h"
 #include "packed.h"
 

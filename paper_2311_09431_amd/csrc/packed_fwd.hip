@@ -4,8 +4,8 @@
 // A launch has a workgroup for every tile that the sequences can have, rows / 128 + n_seq of them a head, whatever the offsets
 // say (they are on the device); those behind the last tile end at once.
 //
-// Bound as the ring step's forward is, by the products and the exponentials beside them: 8 sequences of up to 4096 rows, 32 heads on 8, d 128, 554
-// to 568 us, 0.95 to 0.98 PFLOP/s of allowed pairs, one of 16384, 16 heads, 938 to 947 us, 1.17; of the pairs computed, diagonal tiles whole and
+// Bound as the ring step's forward is, by the products and the exponentials beside them: 8 sequences of up to 4096 rows, 32 heads on 8, d 128, 538
+// to 556 us, 0.97 to 1.0 PFLOP/s of allowed pairs, 2 of 16384, 8 heads, 912 to 937 us, 1.17 to 1.2; of the pairs computed, diagonal tiles whole and
 // rows behind a sequence's end too, the former are 93 %.
 #include "fwd_tiles.h"
 
