@@ -175,14 +175,16 @@ bwd_dkdv_wide_kernel(Args p, int n_tiles) {
     char* const v_own = v_lds + wave * WIDE_V_LDS + lane * 16;
     {
         bf16x8 v_all[16];
-        load_b_frags<16>(v_all, (const __bf16*)p.v + kv_base + (int64_t)key * ss, h, d);
+        if constexpr (PACKED) load_b_frags<16>(v_all, (const __bf16*)p.v + kv_base, p.c, 2 * (int)ss, key, h, d);
+        else load_b_frags<16>(v_all, (const __bf16*)p.v + kv_base + (int64_t)key * ss, h, d);
 #pragma unroll
         for (int ks = 0; ks < 16; ++ks) {
             if (ks < WIDE_V_REGS) vf[ks % WIDE_V_REGS] = v_all[ks];
             else *reinterpret_cast<bf16x8*>(v_own + (ks - WIDE_V_REGS) * 1024) = v_all[ks];
         }
     }
-    load_b_frags<16>(kf, (const __bf16*)p.k + kv_base + (int64_t)key * ss, h, d);
+    if constexpr (PACKED) load_b_frags<16>(kf, (const __bf16*)p.k + kv_base, p.c, 2 * (int)ss, key, h, d);
+    else load_b_frags<16>(kf, (const __bf16*)p.k + kv_base + (int64_t)key * ss, h, d);
     request(0);
     const int lim_first = lim_req;
     stat_store(0);
@@ -248,26 +250,22 @@ bwd_dkdv_wide_kernel(Args p, int n_tiles) {
                      stat + stage * 2 * WIDE_ROWS, stat, h, lim_cur + n - 4 * h);
 
     acc_settle();
-    if (key_own >= p.c) return;
     if constexpr (PACKED) {
         const int64_t row = kv_base + (int64_t)key * ss;
 #pragma unroll
-        for (int mb = 0; mb < 8; ++mb)
+        for (int i = 0; i < 32; i += 2) {
+            bf16x4 x[2], y[2];
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const int col = 32 * mb + 8 * g + 4 * h;
-                if (col >= d) continue;
-                bf16x4 x, y;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    x[e] = (__bf16)acc_read(16 * mb + 4 * g + e);
-                    y[e] = (__bf16)(p.scale * acc_read(128 + 16 * mb + 4 * g + e));
-                }
-                *reinterpret_cast<bf16x4*>((__bf16*)p.dv + row + col) = x;
-                *reinterpret_cast<bf16x4*>((__bf16*)p.dk + row + col) = y;
+            for (int e = 0; e < 8; ++e) {
+                x[e / 4][e % 4] = (__bf16)acc_read(4 * i + e);
+                y[e / 4][e % 4] = (__bf16)(p.scale * acc_read(128 + 4 * i + e));
             }
+            store_two_chunks((__bf16*)p.dv + row, 8 * i, x[0], x[1], key_own < p.c, h, d);
+            store_two_chunks((__bf16*)p.dk + row, 8 * i, y[0], y[1], key_own < p.c, h, d);
+        }
         return;
     }
+    if (key_own >= p.c) return;
     float* DK = p.dk + kv_base + (int64_t)key * ss;
     float* DV = p.dv + kv_base + (int64_t)key * ss;
 #pragma unroll
