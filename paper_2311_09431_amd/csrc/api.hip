@@ -222,7 +222,7 @@ int play_packed(const sa_packed* s, const int32_t* offsets, sa::PackedArgs a, La
     a.es = (int)elt_size(s->dtype);
     const int group = s->H / s->H_kv;
     // per key/value head at most two workgroups for each tile and query head (fp32 ones of 32 rows have 512 threads) and as many for
-    // its keys
+    // its keys; bf16 launches of 32-row workgroups are kept small by their own rule (packed_split_wanted)
     const int64_t fit = kMostWorkgroups / (sa::most_tiles(a, s->dtype == SA_F32 ? 32 : 128) * 2 * (group + 1));
     if (fit < 1) return SA_ERR_SHAPE;
     const int heads = (int)std::min<int64_t>(fit, s->H_kv);

@@ -47,6 +47,8 @@ bool packed_split_wanted(const PackedArgs& p, bool backward) {
     // requests behind a walk's end name up to 32 rows behind the last sub-tile: their offsets must not wrap into the sequence
     const int64_t widest = p.stride_s > p.kv_stride_s ? p.stride_s : p.kv_stride_s;
     if (p.d > TD || ((int64_t)(p.max_len + 127) / 128 * 128 + OWN) * 2 * widest + 2 * p.d >= (int64_t(1) << 31)) return false;
+    // HIP takes fewer than 2^32 threads a launch: the backward's rule goes by key/value heads, of which each may have thousands of query heads
+    if (most_tiles(p, OWN) * (p.H + (backward ? p.H_kv : 0)) * 64 * (backward ? BWD_WAVES : FWD_WAVES) >= (int64_t(1) << 32)) return false;
     const int64_t tiles = most_tiles(p, 128) * (backward ? p.H_kv : p.H);
     if (!backward) return tiles <= 80 || (tiles <= 144 && p.max_len >= 700) || (tiles <= 256 && p.max_len >= 8192);
     if (p.d <= 64) return tiles <= (p.max_len >= 1000 ? 512 : p.max_len <= 64 || p.max_len > 128 ? 320 : 160);
