@@ -58,6 +58,14 @@ hipError_t launch_packed_f32(PackedArgs p, bool backward, hipStream_t st);
 hipError_t launch_packed_f32x3(PackedArgs p, bool backward, hipStream_t st);
 hipError_t launch_packed_f32x3_split(PackedArgs p, bool backward, hipStream_t st);
 
+// A lane's sum of tiles that weigh w or more, with those of one sequence more.  It stops above any rank (a launch has fewer workgroups):
+// offsets that give the same rows to many sequences could pass 2^31, and a search that goes by a wrapped sum could leave the table.
+constexpr int MOST_COUNTED = 1 << 24;
+__host__ __device__ inline int add_tiles(int sum, int tiles, int w) {
+    const int next = sum + (tiles >= w ? tiles - w + 1 : 0);
+    return next < MOST_COUNTED ? next : MOST_COUNTED;
+}
+
 // Tile `rank` of all sequences' tiles, the heaviest first: a sequence of t tiles has one of each weight 1 .. t (query tile i
 // walks i + 1 key tiles, key tile i is walked by t - i query tiles).  C(w) = sum over sequences of max(0, t - w + 1) tiles weigh w or
 // more; the tile's weight is the largest w with C(w) > rank, found by halving, and among the sequences that have one of it the tile is
@@ -67,8 +75,8 @@ __device__ inline bool find_tile(const PackedArgs& p, int rank, int& seq, int& w
     const int lane = threadIdx.x & 63;
     const int own = lane < p.n_seq ? tiles_of<TILE>(span_of(p, lane)) : 0;      // of the first 64 sequences
     auto count = [&](int w) {
-        int n = max(0, own - w + 1);
-        for (int s = 64 + lane; s < p.n_seq; s += 64) n += max(0, tiles_of<TILE>(span_of(p, s)) - w + 1);
+        int n = add_tiles(0, own, w);
+        for (int s = 64 + lane; s < p.n_seq; s += 64) n = add_tiles(n, tiles_of<TILE>(span_of(p, s)), w);
         return wave_total(wave_scan(n));
     };
     int behind = count(1);
