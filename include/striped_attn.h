@@ -252,8 +252,9 @@ int sa_ring_bwd_tiled(const void* Q, const void* K, const void* V, const void* d
  * here and below, but where it is said.  offsets: DEVICE int32, n_seq + 1 of them: sequence s is rows offsets[s] ..
  * offsets[s + 1] - 1 and attends causally to itself.  Empty sequences are allowed, and so are rows in front of the first and
  * behind the last sequence: nothing of them has an effect, nothing of them is written (but delta, which is scratch).  Offsets
- * outside 0 .. rows count as the nearest of these, a sequence that ends before it begins as empty; what rows hold afterwards that
- * such offsets give to two sequences is not defined.
+ * outside 0 .. rows count as the nearest of these, a sequence that ends before it begins as empty, and sequences may lie in any
+ * order.  No row may be in two sequences: a call with such offsets stays within the tensors and leaves rows of no sequence alone, but
+ * which of its other rows it writes, those of sequences that share none included, and what they then hold is not defined.
  * n_seq, rows or max_len 0: success, nothing launched, pointers not looked at.
  */
 typedef struct {

@@ -17,7 +17,8 @@ struct PackedArgs : StepArgs {
     bool by_rank;               // workgroup order: by ranks over all heads, or in groups of heads (decode_block)
 };
 
-// Tiles of `tile` rows that the sequences can have, whatever their lengths
+// Tiles of `tile` rows that sequences without a common row can have, whatever their lengths.  (Of sequences that share rows there can be more; a
+// launch then leaves out the lightest.)
 inline int64_t most_tiles(const PackedArgs& p, int tile) {
     const int64_t each = ((int64_t)p.max_len + tile - 1) / tile, by_rows = (int64_t)p.rows / tile + p.n_seq;
     return each * p.n_seq < by_rows ? each * p.n_seq : by_rows;

@@ -45,3 +45,17 @@ def test_sums_are_right_up_to_any_rank_and_stay_above_behind_it(host, n_seq, til
         got = host.counted(all_tiles.ctypes.data, n_seq, w)
         want = int(np.maximum(0, all_tiles.astype(np.int64) - w + 1).sum())
         assert got == want if want < RANKS else RANKS <= got < 1 << 31, (w, got, want)
+
+
+@pytest.mark.parametrize("seed", range(40))
+def test_a_launch_has_a_rank_for_every_tile_of_sequences_that_share_no_row(host, seed):
+    """In any order, with gaps, cut off at max_len."""
+    rng = np.random.default_rng(seed)
+    n, rows = int(rng.integers(1, 200)), int(rng.integers(1, 6000))
+    cuts = np.sort(rng.integers(0, rows + 1, 2 * n))
+    lens = np.diff(cuts)[::2] if seed % 2 else np.diff(np.concatenate([[0], cuts, [rows]]))
+    lens = rng.permutation(lens)
+    for max_len in {1, 31, 33, 128, 129, int(lens.max()) or 1, rows}:
+        kept = np.minimum(lens, max_len)
+        for tile in (32, 64, 128, 256):
+            assert int((-(-kept // tile)).sum()) <= host.most(len(lens), rows, min(max_len, rows), tile)
