@@ -52,6 +52,12 @@ hipError_t launch_packed_dkdv_wide(const PackedArgs& p, unsigned workgroups, hip
 // bf16 launches of few tiles (the backward's forms delta too)
 bool packed_split_wanted(const PackedArgs& p, bool backward);
 hipError_t launch_packed_split(PackedArgs p, bool backward, hipStream_t st);
+// the other rules of the bf16 backward (packed_bwd.hip; n_ranks: 128-row tiles), and of fp32 (packed_f32.hip: up to 128 columns, above)
+bool packed_one_launch(const PackedArgs& p);
+bool packed_two_wavefronts(const PackedArgs& p);
+bool packed_all_columns(const PackedArgs& p);
+F32Route packed_f32_route(const PackedArgs& p, bool backward);
+bool packed_f32_few(const PackedArgs& p, bool backward);
 // (placed_kinds; as a ring step's, from 0.5 to 3 the same to 2 %)
 inline double packed_ratio(const PackedArgs& p) { return p.H == p.H_kv ? 1.45 : 0.; }
 hipError_t launch_packed_delta(const PackedArgs& p, int dtype, hipStream_t st);

@@ -60,26 +60,17 @@ packed_both_kernel(PackedArgs p, PlacedKinds kinds) {
     }
 }
 
+}  // namespace
+
 // At 64 columns two wavefronts a SIMD are faster where many long walks hide each other's latency, whole training pass, us, one : two:
 // 2 x 8192 rows, 32 heads, 2506 : 2296, 8192, 16 heads, 688 : 677; but 6 of up to 4096, 16 heads, 713 : 717, 16 of up to 1000, 32
 // heads, 294 : 341, 4 of up to 500, 16 heads, 41 : 52, and with four query heads to a key/value head 8192, 32 heads, 1305 : 1415.
+bool packed_two_wavefronts(const PackedArgs& p) { return p.H == p.H_kv && p.max_len >= 8192 && (int64_t)p.n_ranks * p.H_kv > 2 * N_CU; }
+
 // Above 128 columns workgroups with all of them from 160 tiles on, whole training pass, d 256, us, halves : all: 4 of up to 500, 16 heads,
 // 110 : 104, 8 of up to 1000 267 : 219, 6 of up to 4096, 8 heads, 1568 : 1273; but (fewer tiles) 2 of up to 1000, 4 heads, 140 : 153, 8 of up
 // to 1000, 16 heads on 4, 308 : 342.
-template <int DP, bool PART>
-hipError_t launch_dkdv(const PackedArgs& p, hipStream_t st, int64_t n) {
-    if constexpr (DP <= 64) {
-        if (DP == 32 || (p.H == p.H_kv && p.max_len >= 8192 && n > 2 * N_CU)) {
-            hipLaunchKernelGGL((packed_dkdv_kernel<DP, PART, 2>), dim3((unsigned)n), dim3(256), 0, st, p);
-            return hipGetLastError();
-        }
-    }
-    if constexpr (DP == 256 && !PART) {
-        if (n / 2 > 5 * N_CU / 8) return launch_packed_dkdv_wide(p, (unsigned)(n / 2), st);
-    }
-    if constexpr (DP != 32) hipLaunchKernelGGL((packed_dkdv_kernel<DP, PART, 1>), dim3((unsigned)n), dim3(256), 0, st, p);
-    return hipGetLastError();
-}
+bool packed_all_columns(const PackedArgs& p) { return (int64_t)p.n_ranks * p.H_kv > 5 * N_CU / 8; }
 
 // Both kinds of workgroups in one launch, by 128-row tiles (as many as there can be) of all key/value heads: few of them leave the chip half empty
 // while the first kind ends.  Over 570 launches of 1 to 64 sequences of up to 64 to 8192 rows the rules here and in packed_split_wanted take 0.3 %
@@ -89,11 +80,28 @@ hipError_t launch_dkdv(const PackedArgs& p, hipStream_t st, int64_t n) {
 // 4096, 8 heads (256) 453 : 502, but 12 heads (384) 628 : 574; 8 of up to 2000, 32 on 4 (240) 1000 : 1417.  A walk of one tile leaves little
 // to fill: d 128, 16 of up to 128, 32 on 8, 59 : 53, 40 of up to 64, 32 on 8, 91 : 76, d 256, 64 of up to 64, 16 on 4, 166 : 118; 8 heads of
 // their own 27 : 34.  Up to 64 columns these are packed_split.hip's launches: of 334, one launch here was the fastest by 5 % in 13.
-bool one_launch(const PackedArgs& p) {
+bool packed_one_launch(const PackedArgs& p) {
     const int64_t tiles = (int64_t)p.n_ranks * p.H_kv;
     const bool own = p.H == p.H_kv;
     if (p.max_len <= BM) return tiles <= (own ? 192 : p.d > 128 ? 64 : 0);
     return tiles <= (own ? p.d > 128 ? 280 : 512 : 352);
+}
+
+namespace {
+
+template <int DP, bool PART>
+hipError_t launch_dkdv(const PackedArgs& p, hipStream_t st, int64_t n) {
+    if constexpr (DP <= 64) {
+        if (DP == 32 || packed_two_wavefronts(p)) {
+            hipLaunchKernelGGL((packed_dkdv_kernel<DP, PART, 2>), dim3((unsigned)n), dim3(256), 0, st, p);
+            return hipGetLastError();
+        }
+    }
+    if constexpr (DP == 256 && !PART) {
+        if (packed_all_columns(p)) return launch_packed_dkdv_wide(p, (unsigned)(n / 2), st);
+    }
+    if constexpr (DP != 32) hipLaunchKernelGGL((packed_dkdv_kernel<DP, PART, 1>), dim3((unsigned)n), dim3(256), 0, st, p);
+    return hipGetLastError();
 }
 
 template <int DP, bool PART>
@@ -102,7 +110,7 @@ hipError_t launch(PackedArgs p, hipStream_t st) {
     const int64_t n_dq = (int64_t)p.n_ranks * p.H, n_dkdv = (int64_t)p.n_ranks * p.H_kv * halves_of(DP);
     p.by_rank = by_rank_wanted(p);
     if constexpr (DP > 64) {
-        if (one_launch(p)) {
+        if (packed_one_launch(p)) {
             if (hipError_t e = launch_packed_delta(p, SA_BF16, st)) return e;
             if constexpr (DP <= 128) return launch_packed_bwd_ring(p, true, st);
             else {

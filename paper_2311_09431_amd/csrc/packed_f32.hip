@@ -52,22 +52,38 @@ hipError_t run(PackedArgs p, bool backward, hipStream_t st) {
 
 }  // namespace
 
+namespace {
+// a launch like p's of sequences of one length; blocks: how many of those
+StepArgs like_equal_ones(const PackedArgs& p, double& blocks) {
+    const int64_t mean = std::min((int64_t)p.max_len, ((int64_t)p.rows + p.n_seq - 1) / p.n_seq);
+    StepArgs like = p;
+    like.c = (int)((3 * mean + p.max_len + 2) / 4);
+    blocks = std::max(1., (double)p.rows / like.c);
+    return like;
+}
+}  // namespace
+
+F32Route packed_f32_route(const PackedArgs& p, bool backward) {
+    double blocks;
+    const StepArgs like = like_equal_ones(p, blocks);
+    StepArgs longest = p;
+    longest.c = p.max_len;
+    const F32Route route = f32_packed_route(like, p.max_len, blocks, most_tiles(p, 128) * p.H >= 512, backward);
+    return route == F32_SPLIT && !f32x3_split_supported(longest, backward) ? F32_TERMS : route;
+}
+bool packed_f32_few(const PackedArgs& p, bool backward) {
+    double blocks;
+    StepArgs like = like_equal_ones(p, blocks);
+    like.B = (int)ceil(blocks);
+    return few_row_tiles(like, backward);
+}
+
 hipError_t launch_packed_f32(PackedArgs p, bool backward, hipStream_t st) {
     if (backward)
         if (hipError_t e = launch_packed_delta(p, SA_F32, st)) return e;
     p.by_rank = true;
-    const int64_t mean = std::min((int64_t)p.max_len, ((int64_t)p.rows + p.n_seq - 1) / p.n_seq);
-    StepArgs like = p;
-    like.c = (int)((3 * mean + p.max_len + 2) / 4);
-    const double blocks = std::max(1., (double)p.rows / like.c);
-    if (p.d > 128) {
-        like.B = (int)ceil(blocks);
-        return few_row_tiles(like, backward) ? run<256, 2>(p, backward, st) : run<256, 1>(p, backward, st);
-    }
-    StepArgs longest = p;
-    longest.c = p.max_len;
-    F32Route route = f32_packed_route(like, p.max_len, blocks, most_tiles(p, 128) * p.H >= 512, backward);
-    if (route == F32_SPLIT && !f32x3_split_supported(longest, backward)) route = F32_TERMS;
+    if (p.d > 128) return packed_f32_few(p, backward) ? run<256, 2>(p, backward, st) : run<256, 1>(p, backward, st);
+    const F32Route route = packed_f32_route(p, backward);
     if (route == F32_SPLIT) return launch_packed_f32x3_split(p, backward, st);
     if (route != F32_INSTRUCTION) return launch_packed_f32x3(p, backward, st);
     return p.d <= 32 ? run<32, 4>(p, backward, st) : p.d <= 64 ? run<64, 4>(p, backward, st) : run<128, 4>(p, backward, st);

@@ -34,3 +34,28 @@ def test_128_row_workgroups_instead_of_too_many_of_32():
     for rows, H in ((65408, 16383), (8192, 65535)):
         assert not routes.rows_of_32(routes.args(1, rows, rows, H, 1, 4, sa.BF16, apart=True), True)
     assert routes.rows_of_32(routes.args(1, 8192, 8192, 65534, 1, 4, sa.BF16, apart=True), True)
+
+
+@pytest.mark.parametrize("kind,lens,H,H_kv,d,max_len,forward,backward", routes.CASES)
+def test_cases_reach_the_kernels_that_they_name(kind, lens, H, H_kv, d, max_len, forward, backward):
+    """What test_packed_routes_gpu.py runs: a rule that changes must not leave a kernel without a case."""
+    rows = sum(lens) + sum(routes.ROWS_AROUND)
+    p = routes.args(len(lens), rows, max_len or max(lens), H, H_kv, d, sa.BF16 if kind == "bf16" else sa.F32)
+    if kind == "fp32":
+        assert (routes.f32(p, False), routes.f32(p, True)) == (forward, backward)
+    else:
+        assert (("32 rows" if routes.rows_of_32(p, False) else "128 rows"), routes.backward(p)) == (forward, backward)
+
+
+def test_every_kind_of_kernel_has_a_case():
+    columns = lambda d: 32 if d <= 32 else 64 if d <= 64 else 128 if d <= 128 else 256       # noqa: E731
+    have = {(kind, columns(d), route) for kind, _, _, _, d, _, forward, backward in routes.CASES for route in (forward, "backward: " + backward)}
+    kinds = ("32 rows", "128 rows", "256 rows", "fp32 instruction")
+    for c in (32, 64, 128):
+        assert {("fp32", c, k) for k in kinds} <= have and {("fp32", c, "backward: " + k) for k in ("32 rows", "128 rows")} <= have
+        assert {("bf16", c, k) for k in kinds[:2]} <= have and ("bf16", c, "backward: 32 rows") in have
+    assert {("fp32", c, "backward: fp32 instruction") for c in (32, 128)} <= have
+    assert {("fp32", 256, k + w) for k in ("", "backward: ") for w in ("few tiles", "many tiles")} <= have
+    assert {("bf16", 32, "backward: two"), ("bf16", 64, "backward: two, one wavefront"), ("bf16", 64, "backward: two, two wavefronts"),
+            ("bf16", 128, "backward: two"), ("bf16", 128, "backward: one launch")} <= have
+    assert {("bf16", 256, "backward: " + k) for k in ("one launch", "two, halves", "two, all columns")} <= have
