@@ -106,7 +106,10 @@ F32Route f32_packed_route(const StepArgs& a, int longest_rows, double blocks, bo
     const Kind* const kinds[] = {backward ? &BWD_INSTRUCTION : &FWD_INSTRUCTION, backward ? &BWD_SPLIT : &FWD_SPLIT,
                                  backward ? &BWD_TERMS : wide ? &FWD_TERMS_WIDE : &FWD_TERMS};
     const double tiles = blocks * up(a.c, 128);
-    const bool may[] = {tiles * a.H < 256 || (backward && tiles * a.H_kv <= 128) || (longest_rows <= 32 && a.d <= 64), longest_rows > 32, true};
+    // (33 to 64 columns, backward: the fp32 instruction would be the least of none of 1.5 million drawn launches)
+    const bool instruction = backward && a.d > 32 && a.d <= 64 ? false
+                             : tiles * a.H < 256 || (backward && tiles * a.H_kv <= 128) || (longest_rows <= 32 && a.d <= 64);
+    const bool may[] = {instruction, longest_rows > 32, true};
     int best = F32_TERMS;
     double least = INFINITY;
     for (int i : {F32_TERMS, F32_SPLIT, F32_INSTRUCTION}) {

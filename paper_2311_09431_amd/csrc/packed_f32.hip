@@ -40,19 +40,20 @@ packed_bwd_f32_kernel(PackedArgs p, int n_dkdv) {
 }
 
 template <int DP, int SPLIT>
+hipError_t run_fwd(PackedArgs p, hipStream_t st) {
+    p.n_ranks = (int)most_tiles(p, 32 * WAVES / SPLIT);
+    hipLaunchKernelGGL((fwd_f32_kernel<float, DP, SPLIT, PackedArgs>), dim3((unsigned)p.n_ranks * p.H), dim3(64 * WAVES), 0, st, p, 0);
+    return hipGetLastError();
+}
+template <int DP, int SPLIT>
 hipError_t run(PackedArgs p, bool backward, hipStream_t st) {
-    const int64_t ranks = most_tiles(p, 32 * WAVES / SPLIT);
-    p.n_ranks = (int)ranks;
-    const unsigned n_dkdv = (unsigned)(ranks * p.H_kv) * (DP > 128 ? 2 : 1), n_dq = (unsigned)(ranks * p.H);
-    const dim3 block(64 * WAVES);
-    if (!backward) hipLaunchKernelGGL((fwd_f32_kernel<float, DP, SPLIT, PackedArgs>), dim3(n_dq), block, 0, st, p, 0);
-    else hipLaunchKernelGGL((packed_bwd_f32_kernel<DP, SPLIT>), dim3(n_dkdv + n_dq), block, 0, st, p, (int)n_dkdv);
+    if (!backward) return run_fwd<DP, SPLIT>(p, st);
+    p.n_ranks = (int)most_tiles(p, 32 * WAVES / SPLIT);
+    const unsigned n_dkdv = (unsigned)p.n_ranks * p.H_kv * (DP > 128 ? 2 : 1), n_dq = (unsigned)p.n_ranks * p.H;
+    hipLaunchKernelGGL((packed_bwd_f32_kernel<DP, SPLIT>), dim3(n_dkdv + n_dq), dim3(64 * WAVES), 0, st, p, (int)n_dkdv);
     return hipGetLastError();
 }
 
-}  // namespace
-
-namespace {
 // a launch like p's of sequences of one length; blocks: how many of those
 StepArgs like_equal_ones(const PackedArgs& p, double& blocks) {
     const int64_t mean = std::min((int64_t)p.max_len, ((int64_t)p.rows + p.n_seq - 1) / p.n_seq);
@@ -86,7 +87,8 @@ hipError_t launch_packed_f32(PackedArgs p, bool backward, hipStream_t st) {
     const F32Route route = packed_f32_route(p, backward);
     if (route == F32_SPLIT) return launch_packed_f32x3_split(p, backward, st);
     if (route != F32_INSTRUCTION) return launch_packed_f32x3(p, backward, st);
-    return p.d <= 32 ? run<32, 4>(p, backward, st) : p.d <= 64 ? run<64, 4>(p, backward, st) : run<128, 4>(p, backward, st);
+    if (p.d > 32 && p.d <= 64) return run_fwd<64, 4>(p, st);         // (forward: f32_packed_route)
+    return p.d <= 32 ? run<32, 4>(p, backward, st) : run<128, 4>(p, backward, st);
 }
 
 }  // namespace sa

@@ -1,4 +1,6 @@
 """Host-side rules of packed launches (no GPU needed)."""
+import random
+
 import pytest
 
 from paper_2311_09431_amd import binding as sa
@@ -59,3 +61,13 @@ def test_every_kind_of_kernel_has_a_case():
     assert {("bf16", 32, "backward: two"), ("bf16", 64, "backward: two, one wavefront"), ("bf16", 64, "backward: two, two wavefronts"),
             ("bf16", 128, "backward: two"), ("bf16", 128, "backward: one launch")} <= have
     assert {("bf16", 256, "backward: " + k) for k in ("one launch", "two, halves", "two, all columns")} <= have
+
+
+def test_no_fp32_instruction_in_the_backward_at_33_to_64_columns():
+    """There is no such kernel: what is picked is one that there is, and short sequences go to those of 128 rows."""
+    rng = random.Random(6)
+    for _ in range(4000):
+        n, longest = int(2 ** rng.uniform(0, 13)), int(2 ** rng.uniform(0, 15))
+        H_kv = int(2 ** rng.uniform(0, 8))
+        p = routes.args(n, max(longest, int(n * longest * rng.random())), longest, H_kv * int(2 ** rng.uniform(0, 7)), H_kv, rng.choice([36, 48, 60, 64]), sa.F32)
+        assert routes.f32(p, True) in ("32 rows", "128 rows") and (longest > 32 or routes.f32(p, True) == "128 rows")
