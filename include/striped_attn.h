@@ -256,6 +256,10 @@ int sa_ring_bwd_tiled(const void* Q, const void* K, const void* V, const void* d
  * order.  No row may be in two sequences: a call with such offsets stays within the tensors and leaves rows of no sequence alone, but
  * which of its other rows it writes, those of sequences that share none included, and what they then hold is not defined.
  * n_seq, rows or max_len 0: success, nothing launched, pointers not looked at.
+ * Which kernels play a call goes by max_len, so the longest sequence's own length is the fastest one to give: with all rows instead, 64
+ * sequences of up to 100 rows in fp32 take up to 1.75 times as long, of up to 300 in bf16 up to 1.35.  Every workgroup looks up its sequence among all: up
+ * to 64 sequences cost about 1 us at a workgroup's start, more of them longer (of 16 to 256 rows, 16 heads of 128, bf16, the forward takes 4.9 ns a row
+ * for 64 of them, 6.7 for 1000, 12.3 for 4000).
  */
 typedef struct {
     int32_t n_seq;         /* sequences */
@@ -270,8 +274,10 @@ typedef struct {
 /*
  * Forward: O = softmax(scale Q K^T, causal within a sequence) V rounded once to `dtype`, LSE = the rows' log-sum-exp.  Infinities
  * and NaN: as the ring step's blocks of 128 rows and more (fp32: as its fp32 storage); nothing of one sequence reaches another.
+ * bf16: probabilities meet V as bf16 (the backward: dO too, and dS K and Q), sums and LSE are fp32.
  * Errors: NULL, DTYPE, ALIGN, SHAPE (also: bf16 and a sequence of max_len rows reaches over 2^31 bytes or 128 rows do, or more workgroups than
- * a launch takes for a single key/value head), HIP.
+ * a launch takes for a single key/value head), HIP.  (The reach, 32 key/value heads of 128: a max_len above 262016 where a row's heads are
+ * interleaved, above 8.3 million where heads lie apart.  The backward looks at q's rows too.)
  */
 int sa_attn_packed_fwd(const void* q, const void* k, const void* v, const int32_t* offsets, void* out, float* lse,
                        const sa_packed* shape, void* stream);
@@ -309,7 +315,7 @@ typedef struct {
 /*
  * Append: row r of k, rotated by the angles of position id pos[r] (pairing, angles and double precision as sa_rope), and row r of
  * v are stored at slot[r]; each rotated value is rounded once.  Where slot[r] is no slot of the cache (negative: a padding row)
- * nothing of the row is stored.  No two rows may have the same slot: what it then holds is not defined.
+ * nothing of the row goes to the caches (q_out and k_out hold its rotated rows all the same).  No two rows may have the same slot: what it then holds is not defined.
  * q, q_out: rows of the same tokens' queries, rotated from one into the other (which may be the same); both NULL: none.
  * k_out: where the rotated keys are wanted beside the cache, in k's strides (may be k); NULL: nowhere.
  * pos: device int32 [rows]; NULL: nothing is rotated (q must be NULL then).  slot: device int32 [rows].

@@ -300,14 +300,16 @@ def sa_ring_bwd_tiled(Q, K, V, dO, O, LSE, delta, dQ, dK, dV, N, layout, shape, 
 
 
 def sa_attn_packed_fwd(q, k, v, offsets, out, lse, max_len, scale=None):
-    """Causal attention of sequences packed end to end: q, out [rows, H, d], k, v [rows, H_kv, d] (any strides, d contiguous),
-    offsets int32 [n_seq + 1] on the GPU, lse fp32 [H, rows]; no sequence is longer than max_len."""
+    """Causal attention of sequences packed end to end: q [rows, H, d], k, v [rows, H_kv, d] (any strides, d contiguous; v's are
+    k's), out in q's strides, offsets int32 [n_seq + 1] on the GPU, lse fp32 [H, rows]; no sequence is longer than max_len, and the
+    kernels are chosen by it."""
     _check(_marshal.packed_fwd(_entry["sa_attn_packed_fwd"], q, k, v, offsets, out, lse, max_len, scale or 0.0, _here, _stream),
            "sa_attn_packed_fwd")
 
 
 def sa_attn_packed_bwd(q, k, v, out, dout, lse, offsets, delta, dq, dk, dv, max_len, scale=None):
-    """The gradient of sa_attn_packed_fwd for the gradient dout of out; delta is scratch like lse."""
+    """The gradient of sa_attn_packed_fwd for the gradient dout of out; out, dout and dq in q's strides, dk and dv in k's; delta is scratch
+    like lse."""
     _check(_marshal.packed_bwd(_entry["sa_attn_packed_bwd"], q, k, v, out, dout, lse, offsets, delta, dq, dk, dv, max_len, scale or 0.0,
                                _here, _stream), "sa_attn_packed_bwd")
 
@@ -315,7 +317,7 @@ def sa_attn_packed_bwd(q, k, v, out, dout, lse, offsets, delta, dq, dk, dv, max_
 def sa_cache_append(k, v, slot, k_cache, v_cache, pos=None, k_out=None, q=None, q_out=None, base=10000.0):
     """Rows k, v [rows, H_kv, d] into the slots slot (int32 [rows], negative: none) of the caches [pages, page size, H_kv, d], keys
     rotated by their position ids pos (int32 [rows]; None: not rotated); the rotated keys also to k_out, q [rows, H, d] rotated
-    into q_out."""
+    into q_out, of rows without a slot too.  v and k_out have k's strides, q_out q's."""
     _check(_marshal.append(_entry["sa_cache_append"], k, v, slot, k_cache, v_cache, pos, k_out, q, q_out, float(base), _here, _stream),
            "sa_cache_append")
 
@@ -328,7 +330,7 @@ def sa_attn_decode_workspace(q, k_cache):
 
 
 def sa_attn_decode(q, k_cache, v_cache, table, lens, out, lse, workspace, scale=None):
-    """One new token a sequence, q, out [B, H, d], over the tokens 0 .. lens[b] - 1 in the pages table[b] (int32 [B, pages]) of the
+    """One new token a sequence, q [B, H, d] (out in its strides), over the tokens 0 .. lens[b] - 1 in the pages table[b] (int32 [B, pages]) of the
     caches [pages, page size, H_kv, d]; lse fp32 [B, H] or None."""
     _check(_marshal.decode(_entry["sa_attn_decode"], q, k_cache, v_cache, table, lens, out, lse, workspace, scale or 0.0, _here, _stream),
            "sa_attn_decode")
