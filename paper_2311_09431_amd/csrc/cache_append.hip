@@ -6,8 +6,9 @@
 // columns: a rotated one and its partner d/2 further on, 16 bytes each, or a piece of V.
 //
 // Bound by memory: (H + 2 H_kv) d elements a row are read and written (and H_kv d more written where rotated keys are kept).  16384 rows,
-// 32 heads on 8, d 128, bf16: 436 MB in 79 us, 5.5 TB/s (a copy reaches 4.9).  d = 100, whose halves are no whole 16-byte chunks and lie across
-// lines, 44 us, 4.0 TB/s (in pieces of 4 bytes throughout 54, 3.3).  Requesting two to four pairs of chunks at a time changes nothing.
+// 32 heads on 8, d 128, bf16, keys kept: 436 MB in 79 us, 5.5 TB/s (a copy reaches 4.9).  d = 100, whose halves are no whole 16-byte chunks and lie
+// across lines: 9265 rows of 32 heads on 8, bf16, 178 MB in 44 us, 4.0 TB/s (in pieces of 4 bytes throughout 54, 3.3), 2468 rows of 32 heads, fp32, keys
+// kept, 221 MB in 54 to 60, 3.7 to 4.1.  Requesting two to four pairs of chunks at a time changes nothing.
 #include <hip/hip_bf16.h>
 
 #include "paged.h"

@@ -7,7 +7,8 @@ namespace {
 
 // Both in one launch (KEYS and QUERIES): workgroups 0 .. n_dkdv - 1 own keys, the others queries.
 // They share nothing but the inputs; where neither fills the chip they run beside each other, and
-// a step is one launch less.  At 256 columns each by itself: together they spill registers.
+// a step is one launch less.  At 256 columns each by itself, with a register budget of its own (fp32: queries spill 149 registers and
+// keys 24 where two wavefronts share a walk, 21 and 26 where not).  Packed sequences take both in one launch there too (packed_f32.hip).
 template <typename T, int DP, int SPLIT, bool KEYS, bool QUERIES>
 __global__ void __launch_bounds__(64 * WAVES, DP > 64 ? 1 : 2)
 bwd_f32_kernel(StepArgs p, int n_tiles, int n_dkdv) {

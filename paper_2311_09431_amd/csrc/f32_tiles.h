@@ -149,7 +149,7 @@ template <int SPLIT, int DP>
 constexpr int tile_floats() { return 2 * tile_rows(SPLIT) * lds_pitch(DP); }
 
 // ------------------------------------------------------------------ forward
-// Args: StepArgs, or PackedArgs for packed sequences (packed.h), with SPLIT = 1
+// Args: StepArgs, or PackedArgs for packed sequences (packed.h)
 template <typename T, int DP, int SPLIT, typename Args = StepArgs>
 __global__ void __launch_bounds__(64 * WAVES, DP > 128 ? 1 : 2)
 fwd_f32_kernel(Args p, int n_tiles) {

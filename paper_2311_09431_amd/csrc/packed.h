@@ -77,6 +77,9 @@ __host__ __device__ inline int add_tiles(int sum, int tiles, int w) {
 // walks i + 1 key tiles, key tile i is walked by t - i query tiles).  C(w) = sum over sequences of max(0, t - w + 1) tiles weigh w or
 // more; the tile's weight is the largest w with C(w) > rank, found by halving, and among the sequences that have one of it the tile is
 // that of number rank - C(w + 1).  Every wavefront looks for itself, 64 sequences at a time in its lanes.  False: fewer tiles than that.
+// The first 64 sequences stay in registers: about 1 us.  Of more every sum reads the others' offsets again, n_seq / 64 rounds in turn, so a launch's
+// lookups grow with n_seq times its tiles.  ns a row, 64, 256, 1000, 4000 sequences of 16 to 256 rows, 16 heads: forward, d 128, 4.9, 5.5, 6.7,
+// 12.3, d 64 3.0, 2.7, 4.2, 8.4; backward 16.0, 17.2, 20.5, 38, d 64 10.4, 11.8, 16.3, 34; fp32, d 128, forward 17.9, 15.9, 16.3, 20.9.
 template <int TILE>
 __device__ inline bool find_tile(const PackedArgs& p, int rank, int& seq, int& weight) {
     const int lane = threadIdx.x & 63;

@@ -21,6 +21,7 @@ namespace {
 
 // workgroups 0 .. n_dkdv - 1 own keys, the others queries.  In a launch each at 256 columns, whole training pass, us, together : apart: 4 sequences
 // of up to 1084 rows, 2 heads on 1, 776 : 1055, 16 heads 1705 : 1795, 3 of up to 500, 4 heads, 253 : 392, 8 of up to 1000, 32 on 8, 3232 : 3648.
+// (There it spills 182 registers, 528 bytes of scratch a lane, with two wavefronts to a walk and 52, 116 bytes, with one.)
 template <int DP, int SPLIT>
 __global__ void __launch_bounds__(64 * WAVES, DP > 64 ? 1 : 2)
 packed_bwd_f32_kernel(PackedArgs p, int n_dkdv) {

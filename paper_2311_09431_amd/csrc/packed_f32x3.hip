@@ -1,7 +1,8 @@
 // Causal attention of packed sequences and its gradient, fp32 storage in three bf16 terms: the ring step's workgroups of 128 rows and
 // more (f32x3_tiles.h), each on one tile of one sequence (packed.h).  Bound by the longest walk or, in launches that fill the chip, the
 // splitting of rows into terms: 16 sequences of up to 1000 rows, 16 heads on 8, forward, d 128, 215 us, 120 TFLOP/s of allowed pairs (32-row
-// workgroups of three-term products 421, the fp32 instruction 543), d 64 112, 116 (209, 223).
+// workgroups of three-term products 421, the fp32 instruction 543), d 64 112, 116 (209, 223).  At 128 columns registers are spilled: 36 in the backward (148
+// bytes of scratch a lane), 11 (44 bytes) in the forward of 256 rows.
 #include "f32x3_tiles.h"
 
 namespace sa {

@@ -4,9 +4,12 @@
 // A launch has a workgroup for every tile that the sequences can have, rows / 128 + n_seq of them a head, whatever the offsets
 // say (they are on the device); those behind the last tile end at once.
 //
-// Bound as the ring step's forward is, by the products and the exponentials beside them: 8 sequences of up to 4096 rows, 32 heads on 8, d 128, 538
-// to 556 us, 0.97 to 1.0 PFLOP/s of allowed pairs, 2 of 16384, 8 heads, 912 to 937 us, 1.17 to 1.2; of the pairs computed, diagonal tiles whole and
+// Bound as the ring step's forward is, by the products and the exponentials beside them.  By the card, 8 sequences of up to 4096 rows, 32 heads on 8, d 128, 538
+// to 577 us, 0.94 to 1.0 PFLOP/s of allowed pairs, 2 of 16384, 8 heads, 912 to 997 us, 1.1 to 1.2; of the pairs computed, diagonal tiles whole and
 // rows behind a sequence's end too, the former are 93 %.
+//
+// A probability is rounded to one bf16 before it meets V, as in the ring step (row sums are of the unrounded ones): a second term would be half as many
+// products again in the kernel that products bound.  O is 0.0020 from 64 bits (2-norm, relative), of which its own rounding is 0.0016.
 #include "fwd_tiles.h"
 
 namespace sa {
