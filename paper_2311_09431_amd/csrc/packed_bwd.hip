@@ -3,7 +3,7 @@
 // rowsum(dO * O) of their rows for both.
 //
 // Bound as the ring step's backward is, by products and the vector work beside them: 6 sequences of up to 4096 rows, 32 heads, d 100, dQ 0.67 and
-// dK, dV 1.01 ms beside 0.49 forward, whole training pass 2.19 to 2.27 (by the card).  delta comes from O as it was stored, dS meets K and Q as bf16 (a second
+// dK, dV 1.01 ms beside 0.49 forward, whole training pass 2.19 to 2.28 (by the card).  delta comes from O as it was stored, dS meets K and Q as bf16 (a second
 // term would cost a third more products): gradients are 0.0025 to 0.0032 from 64 bits (2-norm, relative), their own rounding 0.0017.
 #include "bwd_tiles.h"
 #include "packed.h"
