@@ -291,6 +291,31 @@ int sa_attn_packed_bwd(const void* q, const void* k, const void* v, const void* 
                        const int32_t* offsets, float* delta, void* dq, void* dk, void* dv, const sa_packed* shape, void* stream);
 
 /*
+ * Packed sequences under a sliding window: row a of a sequence sees its keys b <= a with a - b < window, and the first `sinks` keys of the
+ * sequence (those up to a) however far back they lie.  A window of max_len or more is the causal attention above.
+ */
+typedef struct {
+    int32_t window;        /* 1 or more: a row's own key and the window - 1 before it */
+    int32_t sinks;         /* 0 or more */
+} sa_window;
+
+/*
+ * Forward and backward: as sa_attn_packed_fwd and sa_attn_packed_bwd, with their arguments, types, strides, roundings and errors, over the pairs
+ * that the window leaves.  The time goes by these pairs, in tiles of 128 rows and keys (fp32: 32), not by the sequences' lengths squared.
+ * Infinities and NaN: as in a sum over the pairs that a row sees alone, in both types.  A row with a NaN or +inf score is NaN in O and LSE, a key
+ * at -inf has no weight, a row that sees no other key is NaN; nothing of a key that a row does not see reaches it.
+ * workspace (backward): sa_attn_window_bwd_workspace(shape, window) bytes, 16-byte aligned, of any content; NULL where that is 0.  Calls that may run
+ * at the same time (other streams, captured graphs) need one each.
+ * Errors: as theirs, and SHAPE for a window below 1, sinks below 0, a workspace that is too small.
+ */
+int sa_attn_window_fwd(const void* q, const void* k, const void* v, const int32_t* offsets, void* out, float* lse,
+                       const sa_packed* shape, const sa_window* window, void* stream);
+int64_t sa_attn_window_bwd_workspace(const sa_packed* shape, const sa_window* window);      /* or a negative sa_status */
+int sa_attn_window_bwd(const void* q, const void* k, const void* v, const void* out, const void* dout, const float* lse,
+                       const int32_t* offsets, float* delta, void* dq, void* dk, void* dv, void* workspace, int64_t workspace_bytes,
+                       const sa_packed* shape, const sa_window* window, void* stream);
+
+/*
  * Paged key/value cache: two tensors (keys, values) of one geometry, each a pool of pages of page_size tokens,
  * [page, slot, head, 0..d) with d contiguous and strides in elements: heads interleaved within a token's step or apart.
  * Which page holds which tokens of which sequence is the caller's: sa_cache_append goes by slot numbers, page * page_size +

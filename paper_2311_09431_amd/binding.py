@@ -89,6 +89,9 @@ def lib():
             "sa_ring_bwd_tiled": (i32, [vp] * 10 + [i32, i32, shp, i32, i32, i32, vp, vp]),
             "sa_attn_packed_fwd": (i32, [vp] * 8),
             "sa_attn_packed_bwd": (i32, [vp] * 13),
+            "sa_attn_window_fwd": (i32, [vp] * 9),
+            "sa_attn_window_bwd_workspace": (i64, [vp, vp]),
+            "sa_attn_window_bwd": (i32, [vp] * 12 + [i64] + [vp] * 3),
             "sa_cache_append": (i32, [vp] * 12),
             "sa_attn_decode_workspace": (i64, [vp, vp]),
             "sa_attn_decode": (i32, [vp] * 8 + [i64] + [vp] * 3),
@@ -120,7 +123,8 @@ EXPORTS = ("sa_stripe_permute", "sa_unstripe_permute", "sa_rope", "sa_state_init
            "sa_attn_step_fwd_rope",
            "sa_finalize", "sa_bwd_preprocess", "sa_attn_step_bwd", "sa_ring_fwd", "sa_ring_bwd",
            "sa_attn_step_fwd_tiled", "sa_attn_step_bwd_tiled", "sa_ring_fwd_tiled", "sa_ring_bwd_tiled",
-           "sa_attn_packed_fwd", "sa_attn_packed_bwd", "sa_cache_append", "sa_attn_decode_workspace", "sa_attn_decode",
+           "sa_attn_packed_fwd", "sa_attn_packed_bwd", "sa_attn_window_fwd", "sa_attn_window_bwd_workspace",
+           "sa_attn_window_bwd", "sa_cache_append", "sa_attn_decode_workspace", "sa_attn_decode",
            "sa_step_tiles", "sa_step_mask", "sa_step_pairs", "sa_device_props", "sa_status_str")
 
 
@@ -312,6 +316,25 @@ def sa_attn_packed_bwd(q, k, v, out, dout, lse, offsets, delta, dq, dk, dv, max_
     like lse."""
     _check(_marshal.packed_bwd(_entry["sa_attn_packed_bwd"], q, k, v, out, dout, lse, offsets, delta, dq, dk, dv, max_len, scale or 0.0,
                                _here, _stream), "sa_attn_packed_bwd")
+
+
+def sa_attn_window_fwd(q, k, v, offsets, out, lse, max_len, window, sinks=0, scale=None):
+    """sa_attn_packed_fwd where a row sees the last `window` keys up to its own and the first `sinks` of its sequence."""
+    _check(_marshal.window_fwd(_entry["sa_attn_window_fwd"], q, k, v, offsets, out, lse, max_len, window, sinks, scale or 0.0, _here, _stream),
+           "sa_attn_window_fwd")
+
+
+def sa_attn_window_bwd_workspace(q, k, offsets, max_len, window, sinks=0):
+    """Bytes of workspace of sa_attn_window_bwd for such tensors; may be 0."""
+    size = _marshal.window_bwd_workspace(_entry["sa_attn_window_bwd_workspace"], q, k, offsets, max_len, window, sinks)
+    _check(min(size, 0), "sa_attn_window_bwd_workspace")
+    return size
+
+
+def sa_attn_window_bwd(q, k, v, out, dout, lse, offsets, delta, dq, dk, dv, workspace, max_len, window, sinks=0, scale=None):
+    """The gradient of sa_attn_window_fwd, arguments as sa_attn_packed_bwd's; workspace may be None where its size is 0."""
+    _check(_marshal.window_bwd(_entry["sa_attn_window_bwd"], q, k, v, out, dout, lse, offsets, delta, dq, dk, dv, workspace, max_len, window, sinks,
+                               scale or 0.0, _here, _stream), "sa_attn_window_bwd")
 
 
 def sa_cache_append(k, v, slot, k_cache, v_cache, pos=None, k_out=None, q=None, q_out=None, base=10000.0):

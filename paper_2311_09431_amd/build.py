@@ -22,7 +22,7 @@ OBJ_DIR = os.path.join(ROOT, "_build")
 SOURCES = ["api.hip", "permute.hip", "elementwise.hip", "f32_step.hip", "fwd_mfma.hip",
            "bwd_mfma.hip", "bwd_ring.hip", "split_mfma.hip", "f32x3_step.hip", "f32x3_split.hip", "f32_route.hip",
            "rows_step.hip", "packed_fwd.hip", "packed_bwd.hip", "packed_bwd_ring.hip", "packed_f32.hip", "packed_split.hip", "packed_delta.hip",
-           "packed_f32x3.hip", "packed_f32x3_split.hip", "cache_append.hip",
+           "packed_f32x3.hip", "packed_f32x3_split.hip", "window_fwd.hip", "window_bwd.hip", "window_f32.hip", "cache_append.hip",
            "decode.hip"]
 
 # Flags of single sources.  f32x3_step: score tiles are read by vector instructions right after
@@ -34,7 +34,7 @@ SOURCE_FLAGS = {name: ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]
 # Sources with matrix instructions in asm statements, and their kernels whose accumulators are registers by
 # number: the assembly of these is looked over (asm_check.py).
 ASM_CHECKED = {"bwd_mfma.hip": ["bwd_dkdv_wide_kernel"], "bwd_ring.hip": ["bwd_dkdv_ring_kernel", "bwd_both_ring_kernel"], "split_mfma.hip": [],
-               "packed_bwd.hip": [], "packed_split.hip": [], "packed_bwd_ring.hip": ["packed_dkdv_ring_kernel", "packed_both_ring_kernel"]}
+               "packed_bwd.hip": [], "window_bwd.hip": [], "packed_split.hip": [], "packed_bwd_ring.hip": ["packed_dkdv_ring_kernel", "packed_both_ring_kernel"]}
 
 # packed fp32 VALU forms are switched off on purpose for the test machines
 FLAGS = ["-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC", "-fno-gpu-rdc",

@@ -6,6 +6,7 @@
 #include <vector>
 
 #include "packed.h"
+#include "window.h"
 #include "paged.h"
 #include "sa_internal.h"
 
@@ -210,9 +211,33 @@ bool packed_in_reach(const sa_packed* s, int64_t stride) {
     const int64_t rows = ((int64_t)std::min(s->max_len, s->rows) + 127) / 128 * 128;
     return s->dtype == SA_F32 || stride < (int64_t(1) << 30) / (rows + 1);
 }
+// the pointers of a call, checked
+int packed_fwd_args(const void* q, const void* k, const void* v, const int32_t* offsets, void* out, float* lse, const sa_packed* shape,
+                    sa::PackedArgs& a) {
+    if (!q || !k || !v || !offsets || !out || !lse) return SA_ERR_NULL;
+    // (queries: a tile's 128 rows)
+    if (!packed_in_reach(shape, shape->kv_stride_s) || (shape->dtype == SA_BF16 && shape->stride_s >= (1 << 23))) return SA_ERR_SHAPE;
+    if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out) || (reinterpret_cast<uintptr_t>(offsets) & 3u) ||
+        (reinterpret_cast<uintptr_t>(lse) & 3u))
+        return SA_ERR_ALIGN;
+    a.q = q; a.k = k; a.v = v; a.o = (float*)out; a.lse = lse;
+    return SA_OK;
+}
+int packed_bwd_args(const void* q, const void* k, const void* v, const void* out, const void* dout, const float* lse, const int32_t* offsets,
+                    float* delta, void* dq, void* dk, void* dv, const sa_packed* shape, sa::PackedArgs& a) {
+    if (!q || !k || !v || !out || !dout || !lse || !offsets || !delta || !dq || !dk || !dv) return SA_ERR_NULL;
+    if (!packed_in_reach(shape, shape->kv_stride_s) || !packed_in_reach(shape, shape->stride_s)) return SA_ERR_SHAPE;
+    if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out) || !aligned16(dout) || !aligned16(dq) || !aligned16(dk) ||
+        !aligned16(dv) || ((reinterpret_cast<uintptr_t>(offsets) | reinterpret_cast<uintptr_t>(lse) | reinterpret_cast<uintptr_t>(delta)) & 3u))
+        return SA_ERR_ALIGN;
+    a.q = q; a.k = k; a.v = v; a.dout = dout; a.lse = const_cast<float*>(lse); a.delta = delta;
+    a.o = (float*)const_cast<void*>(out);
+    a.dq = (float*)dq; a.dk = (float*)dk; a.dv = (float*)dv;
+    return SA_OK;
+}
 // One launch, or several of whole key/value heads and their groups where a launch would hold too many workgroups.
-template <typename Launch>
-int play_packed(const sa_packed* s, const int32_t* offsets, sa::PackedArgs a, Launch launch) {
+template <typename Args, typename Launch>
+int play_packed(const sa_packed* s, const int32_t* offsets, Args a, Launch launch) {
     a.layout = SA_CONTIGUOUS; a.n_q = a.n_kv = 1; a.fresh = true;
     a.B = 1; a.H = s->H; a.H_kv = s->H_kv; a.d = s->d;
     a.stride_h = s->stride_h; a.stride_s = s->stride_s; a.kv_stride_h = s->kv_stride_h; a.kv_stride_s = s->kv_stride_s;
@@ -227,7 +252,7 @@ int play_packed(const sa_packed* s, const int32_t* offsets, sa::PackedArgs a, La
     if (fit < 1) return SA_ERR_SHAPE;
     const int heads = (int)std::min<int64_t>(fit, s->H_kv);
     for (int h = 0; h < s->H_kv; h += heads) {
-        sa::PackedArgs part = a;
+        Args part = a;
         part.H_kv = std::min(heads, s->H_kv - h);
         part.H = part.H_kv * group;
         const int64_t q = (int64_t)h * group * a.stride_h * a.es, kv = (int64_t)h * a.kv_stride_h * a.es;
@@ -239,6 +264,16 @@ int play_packed(const sa_packed* s, const int32_t* offsets, sa::PackedArgs a, La
         if (launch(part) != hipSuccess) return SA_ERR_HIP;
     }
     return SA_OK;
+}
+int check_window(const sa_window* w) {
+    if (!w) return SA_ERR_NULL;
+    return w->window < 1 || w->sinks < 0 ? SA_ERR_SHAPE : SA_OK;
+}
+// beyond the longest sequence neither says more
+void set_window(sa::WindowArgs& a, const sa_packed* s, const sa_window* w) {
+    const int most = std::min(s->max_len, s->rows);
+    a.window = std::min(w->window, most);
+    a.sinks = std::min(w->sinks, most);
 }
 
 // ---- paged cache
@@ -523,15 +558,9 @@ int sa_attn_packed_fwd(const void* q, const void* k, const void* v, const int32_
                        const sa_packed* shape, void* stream) {
     if (int e = check_packed(shape)) return e;
     if (shape->n_seq == 0 || shape->rows == 0 || shape->max_len == 0) return SA_OK;
-    if (!q || !k || !v || !offsets || !out || !lse) return SA_ERR_NULL;
-    // (queries: a tile's 128 rows)
-    if (!packed_in_reach(shape, shape->kv_stride_s) || (shape->dtype == SA_BF16 && shape->stride_s >= (1 << 23))) return SA_ERR_SHAPE;
-    if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out) || (reinterpret_cast<uintptr_t>(offsets) & 3u) ||
-        (reinterpret_cast<uintptr_t>(lse) & 3u))
-        return SA_ERR_ALIGN;
-    hipStream_t st = (hipStream_t)stream;
     sa::PackedArgs a{};
-    a.q = q; a.k = k; a.v = v; a.o = (float*)out; a.lse = lse;
+    if (int e = packed_fwd_args(q, k, v, offsets, out, lse, shape, a)) return e;
+    hipStream_t st = (hipStream_t)stream;
     return play_packed(shape, offsets, a, [&](const sa::PackedArgs& p) {
         return shape->dtype == SA_F32 ? sa::launch_packed_f32(p, false, st) : sa::launch_packed_fwd(p, st);
     });
@@ -541,18 +570,50 @@ int sa_attn_packed_bwd(const void* q, const void* k, const void* v, const void* 
                        const int32_t* offsets, float* delta, void* dq, void* dk, void* dv, const sa_packed* shape, void* stream) {
     if (int e = check_packed(shape)) return e;
     if (shape->n_seq == 0 || shape->rows == 0 || shape->max_len == 0) return SA_OK;
-    if (!q || !k || !v || !out || !dout || !lse || !offsets || !delta || !dq || !dk || !dv) return SA_ERR_NULL;
-    if (!packed_in_reach(shape, shape->kv_stride_s) || !packed_in_reach(shape, shape->stride_s)) return SA_ERR_SHAPE;
-    if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out) || !aligned16(dout) || !aligned16(dq) || !aligned16(dk) ||
-        !aligned16(dv) || ((reinterpret_cast<uintptr_t>(offsets) | reinterpret_cast<uintptr_t>(lse) | reinterpret_cast<uintptr_t>(delta)) & 3u))
-        return SA_ERR_ALIGN;
-    hipStream_t st = (hipStream_t)stream;
     sa::PackedArgs a{};
-    a.q = q; a.k = k; a.v = v; a.dout = dout; a.lse = const_cast<float*>(lse); a.delta = delta;
-    a.o = (float*)const_cast<void*>(out);
-    a.dq = (float*)dq; a.dk = (float*)dk; a.dv = (float*)dv;
+    if (int e = packed_bwd_args(q, k, v, out, dout, lse, offsets, delta, dq, dk, dv, shape, a)) return e;
+    hipStream_t st = (hipStream_t)stream;
     return play_packed(shape, offsets, a, [&](const sa::PackedArgs& p) {
         return shape->dtype == SA_F32 ? sa::launch_packed_f32(p, true, st) : sa::launch_packed_bwd(p, st);
+    });
+}
+
+int sa_attn_window_fwd(const void* q, const void* k, const void* v, const int32_t* offsets, void* out, float* lse,
+                       const sa_packed* shape, const sa_window* window, void* stream) {
+    if (int e = check_packed(shape)) return e;
+    if (int e = check_window(window)) return e;
+    if (shape->n_seq == 0 || shape->rows == 0 || shape->max_len == 0) return SA_OK;
+    sa::WindowArgs a{};
+    if (int e = packed_fwd_args(q, k, v, offsets, out, lse, shape, a)) return e;
+    set_window(a, shape, window);
+    hipStream_t st = (hipStream_t)stream;
+    return play_packed(shape, offsets, a, [&](const sa::WindowArgs& p) {
+        return shape->dtype == SA_F32 ? sa::launch_window_f32(p, false, st) : sa::launch_window_fwd(p, st);
+    });
+}
+
+int64_t sa_attn_window_bwd_workspace(const sa_packed* shape, const sa_window* window) {
+    if (int e = check_packed(shape)) return e;
+    if (int e = check_window(window)) return e;
+    return 0;
+}
+
+int sa_attn_window_bwd(const void* q, const void* k, const void* v, const void* out, const void* dout, const float* lse,
+                       const int32_t* offsets, float* delta, void* dq, void* dk, void* dv, void* workspace, int64_t workspace_bytes,
+                       const sa_packed* shape, const sa_window* window, void* stream) {
+    if (int e = check_packed(shape)) return e;
+    if (int e = check_window(window)) return e;
+    if (shape->n_seq == 0 || shape->rows == 0 || shape->max_len == 0) return SA_OK;
+    sa::WindowArgs a{};
+    if (int e = packed_bwd_args(q, k, v, out, dout, lse, offsets, delta, dq, dk, dv, shape, a)) return e;
+    const int64_t bytes = sa_attn_window_bwd_workspace(shape, window);
+    if (workspace_bytes < bytes) return SA_ERR_SHAPE;
+    if (bytes > 0 && !workspace) return SA_ERR_NULL;
+    if (!aligned16(workspace)) return SA_ERR_ALIGN;
+    set_window(a, shape, window);
+    hipStream_t st = (hipStream_t)stream;
+    return play_packed(shape, offsets, a, [&](const sa::WindowArgs& p) {
+        return shape->dtype == SA_F32 ? sa::launch_window_f32(p, true, st) : sa::launch_window_bwd(p, st);
     });
 }
 

@@ -27,6 +27,7 @@
 #include "acc_file.h"
 #include "mfma_tiles.h"
 #include "sa_internal.h"
+#include "window.h"
 
 namespace sa {
 
@@ -69,14 +70,14 @@ __device__ inline bf16x8 pack8(const f32x16& x, int first) {
 // (no k-step 7), 128, or 256 for head dimensions above 128: the K and V tiles then come as two 128-column halves, tile_bytes(DP) apart in
 // LDS, and every slice holds one MFMA of each product per half.  PART: d % 8 == 4, the K and V
 // fragments that hold column d are cleared beyond it (part_ks = the k-step, or -1 for the lanes
-// of the other half-wave).
-template <bool NEXT, bool MASK, int DP, bool PART>
+// of the other half-wave).  WINDOW: allowed is also only what is above mask_lim - window or below sink_lim (window.h).
+template <bool NEXT, bool MASK, int DP, bool PART, bool WINDOW = false>
 __device__ __forceinline__ void dq_step(f32x16& s_cur, f32x16& dp_cur, f32x16& s_next, f32x16& dp_next,
                                f32x16 (&acc)[4 * halves_of(DP)], const bf16x8 (&qf)[8 * halves_of(DP)],
                                const bf16x8 (&gf)[8 * halves_of(DP)], float kappa, float lse2, float delta,
                                const uint32_t (&arow)[8], const uint32_t (&tr0)[4], const uint32_t (&tr1)[4],
                                const char* k_next, const char* v_next, const char* k_cur, int mask_lim,
-                               int part_ks) {
+                               int part_ks, int window = 0, int sink_lim = 0) {
     constexpr int NH = halves_of(DP), KS = ksteps_of(DP), MB = blocks_of(DP);      // per half
     bf16x8 ka[NH][8], va[NH][8], kt[NH][8], dsb[2];
     auto fetch = [&](int i) {
@@ -118,7 +119,8 @@ __device__ __forceinline__ void dq_step(f32x16& s_cur, f32x16& dp_cur, f32x16& s
 #pragma unroll
         for (int r = 2 * i; r < 2 * i + 2; ++r) {
             float pr = __builtin_amdgcn_exp2f(fmaf(s_cur[r], kappa, -lse2));
-            if (MASK && 8 * (r / 4) + (r % 4) > mask_lim) pr = 0.f;
+            const int key = 8 * (r / 4) + (r % 4);
+            if (MASK && (key > mask_lim || (WINDOW && key <= mask_lim - window && key >= sink_lim))) pr = 0.f;
             dsb[r / 8][r % 8] = (__bf16)(pr * (dp_cur[r] - delta));
         }
     }
@@ -145,10 +147,12 @@ __device__ __forceinline__ void dq_step(f32x16& s_cur, f32x16& dp_cur, f32x16& s
 // own: as parts of one array the compiler arranges the d = 256 kernels otherwise and a full step of
 // 8 heads, 8192 rows, takes 2.197 instead of 2.177 ms
 // PACKED (packed sequences): linear is the tile's place and the head, dQ is written in bf16.  FORM_DELTA: delta is formed here.
-template <bool RAGGED, int WALK, int DP, bool PART, bool BY_RANK, bool PACKED = false, bool FORM_DELTA = PACKED>
-__device__ __forceinline__ void bwd_dq(const StepArgs& p, int n_tiles, int linear, char* k_lds0, char* k_lds1,
+// Args: StepArgs, or WindowArgs for packed sequences with a window
+template <bool RAGGED, int WALK, int DP, bool PART, bool BY_RANK, bool PACKED = false, bool FORM_DELTA = PACKED, typename Args = StepArgs>
+__device__ __forceinline__ void bwd_dq(const Args& p, int n_tiles, int linear, char* k_lds0, char* k_lds1,
                                        char* v_lds0, char* v_lds1) {
     constexpr int NH = halves_of(DP), KS = ksteps_of(DP), MB = halves_of(DP) * blocks_of(DP);      // k-steps per half, column blocks
+    constexpr bool WINDOW = std::is_same<Args, WindowArgs>::value;
 
     const int tid = threadIdx.x, lane = tid & 63, n = lane & 31, h = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);      // wave-uniform, kept scalar
@@ -209,10 +213,18 @@ __device__ __forceinline__ void bwd_dq(const StepArgs& p, int n_tiles, int linea
 #pragma unroll
         for (int hh = 0; hh < NH; ++hh) dt_load<DP>(m, tile_byte_offset, buf + hh * tile_bytes(DP), gl[hh], wave);
     };
-    load_tile(Kr, 0, k_lds0);
-    load_tile(Vr, 0, v_lds0);
-    load_tile(Kr, tile_pitch, k_lds1);       // n_kt >= 2 always
-    load_tile(Vr, tile_pitch, v_lds1);
+    WindowWalk<BM> walk;                     // as in the forward kernel
+    int window = 0, sink_base = 0;
+    if constexpr (WINDOW) {
+        walk = WindowWalk<BM>(p, q0, qt + 1);
+        window = p.window;
+        sink_base = p.sinks - 4 * h;
+    }
+    const int t_begin = WINDOW ? 2 * walk.at(0) : 0;
+    load_tile(Kr, t_begin * tile_pitch, k_lds0);
+    load_tile(Vr, t_begin * tile_pitch, v_lds0);
+    load_tile(Kr, (t_begin + 1) * tile_pitch, k_lds1);       // n_kt >= 2 always
+    load_tile(Vr, (t_begin + 1) * tile_pitch, v_lds1);
 
     bf16x8 qf[8 * NH], gf[8 * NH];
     if constexpr (PACKED) {
@@ -287,15 +299,16 @@ __device__ __forceinline__ void bwd_dq(const StepArgs& p, int n_tiles, int linea
         char* const v_cur = PAR ? v_lds1 : v_lds0;
         char* const k_nxt = PAR ? k_lds0 : k_lds1;
         char* const v_nxt = PAR ? v_lds0 : v_lds1;
-        dq_step<true, MASK, DP, PART>(s_a, dp_a, s_b, dp_b, acc, qf, gf, kappa, lse2, delta, arow, tr0, tr1,
+        dq_step<true, MASK, DP, PART, WINDOW>(s_a, dp_a, s_b, dp_b, acc, qf, gf, kappa, lse2, delta, arow, tr0, tr1,
                                       k_cur + tile_bytes(DP) / 2, v_cur + tile_bytes(DP) / 2, k_cur, mask_base - 64 * t,
-                                      part_ks);
+                                      part_ks, window, sink_base - 64 * t);
         if (!LAST) {
             __builtin_amdgcn_s_waitcnt(0);      // tile t+1, requested one iteration ago, has landed
             __syncthreads();
         }
-        dq_step<!LAST, MASK, DP, PART>(s_b, dp_b, s_a, dp_a, acc, qf, gf, kappa, lse2, delta, arow, tr0, tr1,
-                                       k_nxt, v_nxt, k_cur + tile_bytes(DP) / 2, mask_base - 64 * t - 32, part_ks);
+        dq_step<!LAST, MASK, DP, PART, WINDOW>(s_b, dp_b, s_a, dp_a, acc, qf, gf, kappa, lse2, delta, arow, tr0, tr1,
+                                       k_nxt, v_nxt, k_cur + tile_bytes(DP) / 2, mask_base - 64 * t - 32, part_ks, window,
+                                       sink_base - 64 * t - 32);
         if (REQ) {
             __syncthreads();                    // every wavefront is done with tile t
             load_tile(kr, at, k_cur);
@@ -308,8 +321,21 @@ __device__ __forceinline__ void bwd_dq(const StepArgs& p, int n_tiles, int linea
     using P1 = std::integral_constant<int, 1>;
     // per block: trips before the last tile pair of the fine walk without the element mask, then
     // masked trips: two, more under emulated coarse skipping (n_kt_fine and n_kt are even)
-    int t = 0;
-    for (;;) {
+    int t = t_begin;
+    if constexpr (WINDOW) {
+        int i = 0;
+        for (; i < walk.masked; ++i) {
+            const int next = 2 * walk.at(i + 1);
+            trip(F{}, T{}, P0{}, T{}, t, Kr, Vr, next * tile_pitch);
+            trip(F{}, T{}, P1{}, T{}, t + 1, Kr, Vr, (next + 1) * tile_pitch);
+            t = next;
+        }
+        for (; i < walk.n - 1; ++i, t += 2) {
+            trip(F{}, F{}, P0{}, T{}, t, Kr, Vr, (t + 2) * tile_pitch);
+            trip(F{}, F{}, P1{}, T{}, t + 1, Kr, Vr, (t + 3) * tile_pitch);
+        }
+    }
+    for (; !WINDOW;) {
         for (; t + 2 < n_kt_fine; t += 2) {
             trip(F{}, F{}, P0{}, T{}, t, Kr, Vr, (t + 2) * tile_pitch);
             trip(F{}, F{}, P1{}, T{}, t + 1, Kr, Vr, (t + 3) * tile_pitch);
@@ -343,8 +369,15 @@ __device__ __forceinline__ void bwd_dq(const StepArgs& p, int n_tiles, int linea
     trip(T{}, T{}, P1{}, F{}, t + 1, Kr, Vr, 0);
 
     if constexpr (PACKED) {
+        uint32_t odd = 0;       // rows to do over
+        if constexpr (WINDOW) odd = row_mask(row_ok && window_odd<MB, PART>(acc, h, d));
+        const bool stored = row_ok && (!WINDOW || !((odd >> n) & 1));
 #pragma unroll
-        for (int mb = 0; mb < MB; ++mb) store_bf16((__bf16*)p.dq + base + (int64_t)a * ss, 32 * mb, acc[mb], p.scale, row_ok, h, d);
+        for (int mb = 0; mb < MB; ++mb) store_bf16((__bf16*)p.dq + base + (int64_t)a * ss, 32 * mb, acc[mb], p.scale, stored, h, d);
+        if constexpr (WINDOW)
+            each_window_row<true, BM>(odd, (int)blockIdx.x, launch_args().H, 32 * wave, [&](const WindowArgs& again, int head, int row) {
+                window_dq_row<__hip_bfloat16>(again, head, row, threadIdx.x & 63);
+            });
         return;
     }
 #pragma unroll
@@ -408,15 +441,15 @@ __device__ inline void load_neg_delta(f32x16& dp, const float* neg_delta, int h)
 // tile_bytes(DP) apart in LDS.  S and dP contract over both; a workgroup accumulates only ONE half of
 // the columns of dK^T and dV^T (256 columns of both do not fit the register file beside K, V and
 // the score tiles), so tr0 / tr1 arrive with that half's LDS offset added and the other half is
-// another workgroup's, which computes S and dP again.
-template <bool NEXT, bool MASK, int DP, bool PART>
+// another workgroup's, which computes S and dP again.  WINDOW: allowed is also only what is at most `span` above mask_lim.
+template <bool NEXT, bool MASK, int DP, bool PART, bool WINDOW = false>
 __device__ __forceinline__ void dkdv_step(f32x16& s_cur, f32x16& dp_cur, f32x16& s_next, f32x16& dp_next,
                                  f32x16 (&acck)[4], f32x16 (&accv)[4], const bf16x8 (&kf)[8 * halves_of(DP)],
                                  const bf16x8 (&vf)[8 * halves_of(DP)], float kappa, const uint32_t (&arow)[8],
                                  const uint32_t (&tr0)[4], const uint32_t (&tr1)[4], const char* q_next,
                                  const char* g_next, const char* q_cur, const char* g_cur,
                                  const float* stat_cur, const float* stat_next, int h, int mask_lim,
-                                 int part_ks) {
+                                 int part_ks, int span = 0) {
     constexpr int NH = halves_of(DP), KS = ksteps_of(DP), MB = blocks_of(DP);      // per half
     bf16x8 qa[NH][8], ga[NH][8], qt[8], gt[8], pb[2], dsb[2];
     if (NEXT) load_neg_delta(dp_next, stat_next + DT_ROWS, h);
@@ -463,7 +496,8 @@ __device__ __forceinline__ void dkdv_step(f32x16& s_cur, f32x16& dp_cur, f32x16&
         auto score = [&](int r) {
             const float lr = (r & 1) ? lv[i].y : lv[i].x;
             float pr = __builtin_amdgcn_exp2f(fmaf(s_cur[r], kappa, -lr));
-            if (MASK && 8 * (r / 4) + (r % 4) < mask_lim) pr = 0.f;
+            const int query = 8 * (r / 4) + (r % 4);
+            if (MASK && (query < mask_lim || (WINDOW && query > mask_lim + span))) pr = 0.f;
             pb[r / 8][r % 8] = (__bf16)pr;
             dsb[r / 8][r % 8] = (__bf16)(pr * dp_cur[r]);
         };
@@ -506,11 +540,12 @@ __device__ __forceinline__ void dkdv_step(f32x16& s_cur, f32x16& dp_cur, f32x16&
 // first to the last: the query heads that share this key/value head, each with the query shards of
 // the devices that see these keys.
 // q_lds0 .. g_lds1: the tile buffers, as in the dQ kernel; stat: KV_STAT_FLOATS floats
-// PACKED: as in the dQ kernel
-template <int WALK, bool RAGGED, int DP, bool PART, bool BY_RANK, bool PACKED = false>
-__device__ __forceinline__ void bwd_dkdv(const StepArgs& p, int n_tiles, int linear, char* q_lds0, char* q_lds1,
+// PACKED, Args: as in the dQ kernel
+template <int WALK, bool RAGGED, int DP, bool PART, bool BY_RANK, bool PACKED = false, typename Args = StepArgs>
+__device__ __forceinline__ void bwd_dkdv(const Args& p, int n_tiles, int linear, char* q_lds0, char* q_lds1,
                                          char* g_lds0, char* g_lds1, float* stat) {
     constexpr int NH = halves_of(DP), KS = ksteps_of(DP), MB = blocks_of(DP);      // per half
+    constexpr bool WINDOW = std::is_same<Args, WindowArgs>::value;
 
     const int tid = threadIdx.x, lane = tid & 63, n = lane & 31, h = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);      // wave-uniform, kept scalar
@@ -539,7 +574,15 @@ __device__ __forceinline__ void bwd_dkdv(const StepArgs& p, int n_tiles, int lin
     const int k0 = ktile * BM, key_own = k0 + 32 * wave + n;
     const bool key_ok = !RAGGED || key_own < p.c;
     const int key = RAGGED ? min(key_own, p.c - 1) : key_own;     // the row this lane loads
-    const int n_qt = RAGGED ? 2 * n_tiles : p.c / DT_ROWS;
+    int n_qt = RAGGED ? 2 * n_tiles : p.c / DT_ROWS;
+    // WINDOW: up to the last pair of tiles with a row that sees a key of the tile; trips from t_low on carry the mask again, as some row no longer
+    // sees one
+    int t_low = 0x7fffffff, span = 0;
+    if constexpr (WINDOW) {
+        if (k0 >= p.sinks) n_qt = min(n_qt, 2 * ((k0 + BM - 2 + p.window) / BM + 1));
+        if (k0 + BM > p.sinks) t_low = (k0 + p.window) / BM * 2;
+        span = key_own < p.sinks ? 1 << 30 : p.window - 1;
+    }
     // The block being walked: query head q_head of the group and query shard q_dev.  Query tiles
     // holding at least one allowed pair (query a >= key + off) are those from k0 / 64 on; only the
     // first four 32-query sub-tiles of these can cross the diagonal for some wavefront, the trips
@@ -675,17 +718,17 @@ __device__ __forceinline__ void bwd_dkdv(const StepArgs& p, int n_tiles, int lin
         char* const g_nxt = PAR ? g_lds0 : g_lds1;
         const float* st = stat + PAR * 2 * DT_ROWS;
         const float* st_nxt = stat + (1 - PAR) * 2 * DT_ROWS;       // statistics of tile t + 1
-        dkdv_step<true, MASK, DP, PART>(s_a, dp_a, s_b, dp_b, acck, accv, kf, vf, kappa, arow, tr0, tr1,
+        dkdv_step<true, MASK, DP, PART, WINDOW>(s_a, dp_a, s_b, dp_b, acck, accv, kf, vf, kappa, arow, tr0, tr1,
                               q_cur + tile_bytes(DP) / 2, g_cur + tile_bytes(DP) / 2, q_cur, g_cur, st, st + 32, h,
-                              mask_at, part_ks);
+                              mask_at, part_ks, span);
         if (!last) {
             stat_store(1 - PAR, rstat);          // fetched at the end of the previous trip
             __builtin_amdgcn_s_waitcnt(0);       // tile t+1, requested one iteration ago, has landed
             __syncthreads();
         }
-        dkdv_step<!last, MASK, DP, PART>(s_b, dp_b, s_a, dp_a, acck, accv, kf, vf, kappa, arow, tr0, tr1, q_nxt,
+        dkdv_step<!last, MASK, DP, PART, WINDOW>(s_b, dp_b, s_a, dp_a, acck, accv, kf, vf, kappa, arow, tr0, tr1, q_nxt,
                               g_nxt, q_cur + tile_bytes(DP) / 2, g_cur + tile_bytes(DP) / 2, st + 32, st_nxt, h,
-                              mask_at - 32, part_ks);
+                              mask_at - 32, part_ks, span);
         if (REQ) {
             __syncthreads();                     // every wavefront is done with tile t
             load_tile(Qr, at, q_cur);
@@ -709,8 +752,8 @@ __device__ __forceinline__ void bwd_dkdv(const StepArgs& p, int n_tiles, int lin
     int t = t_first;
     for (;;) {
         int mask_at = mask_base - 64 * t, at = (t + 2) * tile_pitch;
-        if (t + 2 < n_qt && !ONE_FORM && t >= t_plain) {
-            for (; t + 2 < n_qt; t += 2) {              // the hot loop
+        if (t + 2 < n_qt && !ONE_FORM && t >= t_plain && (!WINDOW || t < t_low)) {
+            for (; t + 2 < n_qt && (!WINDOW || t < t_low); t += 2) {              // the hot loop
                 trip(F{}, P0{}, F{}, T{}, 0, (t + 2) * tile_pitch);
                 trip(F{}, P1{}, F{}, T{}, 0, (t + 3) * tile_pitch);
             }
@@ -737,11 +780,19 @@ __device__ __forceinline__ void bwd_dkdv(const StepArgs& p, int n_tiles, int lin
 
     if constexpr (PACKED) {
         const int64_t row = kv_base + (int64_t)key * ss;
+        uint32_t odd = 0;       // rows to do over
+        if constexpr (WINDOW) odd = row_mask(key_ok && (window_odd<MB, PART>(accv, h, d, 128 * ohalf) || window_odd<MB, PART>(acck, h, d, 128 * ohalf)));
+        const bool stored = key_ok && (!WINDOW || !((odd >> n) & 1));
 #pragma unroll
         for (int mb = 0; mb < MB; ++mb) {
-            store_bf16((__bf16*)p.dv + row, 128 * ohalf + 32 * mb, accv[mb], 1.f, key_ok, h, d);
-            store_bf16((__bf16*)p.dk + row, 128 * ohalf + 32 * mb, acck[mb], p.scale, key_ok, h, d);
+            store_bf16((__bf16*)p.dv + row, 128 * ohalf + 32 * mb, accv[mb], 1.f, stored, h, d);
+            store_bf16((__bf16*)p.dk + row, 128 * ohalf + 32 * mb, acck[mb], p.scale, stored, h, d);
         }
+        if constexpr (WINDOW)
+            each_window_row<false, BM>(odd, (int)blockIdx.x, launch_args().H_kv * NH, 32 * wave, [&](const WindowArgs& again, int head, int row) {
+                const int col0 = head % NH * 128;
+                window_dkdv_row<__hip_bfloat16>(again, head / NH, row, col0, NH > 1 ? min(again.d, col0 + 128) : again.d, threadIdx.x & 63);
+            });
         return;
     }
 #pragma unroll

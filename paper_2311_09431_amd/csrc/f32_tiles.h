@@ -33,6 +33,7 @@
 #include "f32_rows.h"
 #include "packed.h"
 #include "sa_internal.h"
+#include "window.h"
 
 namespace sa {
 
@@ -149,11 +150,17 @@ template <int SPLIT, int DP>
 constexpr int tile_floats() { return 2 * tile_rows(SPLIT) * lds_pitch(DP); }
 
 // ------------------------------------------------------------------ forward
-// Args: StepArgs, or PackedArgs for packed sequences (packed.h)
+// WINDOW's walk over key tiles of TK: where the tile after the one at t0 begins; start: the window's first sub-tile
+template <int TK>
+__device__ inline int next_tile(const WindowArgs& p, int t0, int start) {
+    const int t = t0 + TK;
+    return t >= p.sinks && t < start ? start : t;
+}
+// Args: StepArgs, or PackedArgs for packed sequences (packed.h), or WindowArgs with a window (window.h)
 template <typename T, int DP, int SPLIT, typename Args = StepArgs>
 __global__ void __launch_bounds__(64 * WAVES, DP > 128 ? 1 : 2)
 fwd_f32_kernel(Args p, int n_tiles) {
-    constexpr bool PACKED = !std::is_same<Args, StepArgs>::value;
+    constexpr bool PACKED = !std::is_same<Args, StepArgs>::value, WINDOW = std::is_same<Args, WindowArgs>::value;
     constexpr int OWN = WAVES / SPLIT, TK = tile_rows(SPLIT), SUB = subtiles(SPLIT), NB = DP / 32;
     __shared__ __attribute__((aligned(16))) float lds[tile_floats<SPLIT, DP>()];
     __shared__ uint32_t masks[WAVES];
@@ -183,6 +190,10 @@ fwd_f32_kernel(Args p, int n_tiles) {
     for (int mb = 0; mb < NB; ++mb) acc[mb] = zero16();
     float m = -INFINITY, l = 0.f;           // l: this half-wave's share of the row sum
 
+    auto sees = [&](int key, int last) {
+        if constexpr (WINDOW) return key <= last && (key > last - p.window || key < p.sinks);
+        else return key <= last;
+    };
     // the key shards one after the other; contiguous layout: none further on than the queries' own
     const int kv_end = last_shard(p, dev);
     for (int kv = p.kv_dev; kv < kv_end; ++kv) {
@@ -193,7 +204,13 @@ fwd_f32_kernel(Args p, int n_tiles) {
         const int last_key = full ? p.c - 1 : min(q0 + 32 * OWN, p.c) - 1 - off;          // for the workgroup
         const int wave_last = full ? p.c - 1 : min(q0 + 32 * qw + 31, p.c - 1) - off;     // for the wavefront
         const int lane_last = full ? p.c - 1 : a - off;
-        for (int t0 = 0; t0 <= last_key; t0 += TK) {
+        int t0 = 0, start = 0, wave_lo = 0;
+        if constexpr (WINDOW) {
+            start = window_start(p, q0) / 32 * 32;
+            wave_lo = window_start(p, q0 + 32 * qw);
+            if (p.sinks == 0) t0 = start;
+        }
+        for (; t0 <= last_key;) {
             __syncthreads();
             stage<T, DP, TK>(k_lds, K, p.kv_stride_s, t0, p.c, d);
             stage<T, DP, TK>(v_lds, V, p.kv_stride_s, t0, p.c, d);
@@ -202,11 +219,14 @@ fwd_f32_kernel(Args p, int n_tiles) {
             for (int s = 0; s < SUB; ++s) {
                 const int at = 32 * (SUB * kw + s), key0 = t0 + at;
                 if (key0 > wave_last) break;
+                if constexpr (WINDOW) {
+                    if (key0 + 31 < wave_lo && key0 >= p.sinks) continue;
+                }
                 f32x16 x = scores<DP>(k_lds + at * lds_pitch(DP), qf, n, h);
                 float mx = -INFINITY;
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
-                    x[r] = key0 + reg_row(r, h) <= lane_last ? x[r] * p.scale : -INFINITY;
+                    x[r] = sees(key0 + reg_row(r, h), lane_last) ? x[r] * p.scale : -INFINITY;
                     mx = fmaxf(mx, x[r]);
                 }
                 const float m_new = fmaxf(m, half_max(mx));
@@ -228,6 +248,8 @@ fwd_f32_kernel(Args p, int n_tiles) {
                 m = m_new;
                 accumulate<DP, NB>(acc, v_lds + at * lds_pitch(DP), x, n, h);
             }
+            if constexpr (WINDOW) t0 = next_tile<TK>(p, t0, start);
+            else t0 += TK;
         }
     }
 
@@ -298,7 +320,8 @@ fwd_f32_kernel(Args p, int n_tiles) {
         if (kw == 0 && h == 0) *L = top + logf(w_sum);
     }
     each_row<SPLIT>(odd_rows, kw, [&](const StepArgs& again, int i) {
-        if constexpr (PACKED) fwd_row<T>(p, b, hd, dev_i, q0 + 32 * qw + i, lane);
+        if constexpr (WINDOW) window_fwd_row<T>(p, hd, q0 + 32 * qw + i, lane);
+        else if constexpr (PACKED) fwd_row<T>(p, b, hd, dev_i, q0 + 32 * qw + i, lane);
         else fwd_row<T>(again, b, hd, dev_i, q0 + 32 * qw + i, lane);
     });
 }
@@ -325,8 +348,9 @@ __device__ inline void add_rows(float* dst_row, const f32x16 (&acc)[NB], float s
 
 // ----------------------------------------------------------------------- dQ
 // PACKED: linear is the tile's place and the head in a sequence that p is the arguments of
-template <typename T, int DP, int SPLIT, bool PACKED = false>
-__device__ inline void bwd_dq(const StepArgs& p, int n_tiles, int linear, float* lds, uint32_t* masks) {
+template <typename T, int DP, int SPLIT, bool PACKED = false, typename Args = StepArgs>
+__device__ inline void bwd_dq(const Args& p, int n_tiles, int linear, float* lds, uint32_t* masks) {
+    constexpr bool WINDOW = std::is_same<Args, WindowArgs>::value;
     constexpr int OWN = WAVES / SPLIT, TK = tile_rows(SPLIT), SUB = subtiles(SPLIT), NB = DP / 32;
     float* const k_lds = lds;
     float* const v_lds = lds + TK * lds_pitch(DP);
@@ -352,6 +376,10 @@ __device__ inline void bwd_dq(const StepArgs& p, int n_tiles, int linear, float*
 #pragma unroll
     for (int mb = 0; mb < NB; ++mb) acc[mb] = zero16();
 
+    auto sees = [&](int key, int last) {
+        if constexpr (WINDOW) return key <= last && (key > last - p.window || key < p.sinks);
+        else return key <= last;
+    };
     const int kv_end = last_shard(p, dev);
     for (int kv = p.kv_dev; kv < kv_end; ++kv) {
         const T* K = (const T*)p.k + kv_base + (kv - p.kv_dev) * p.kv_shard;
@@ -361,7 +389,13 @@ __device__ inline void bwd_dq(const StepArgs& p, int n_tiles, int linear, float*
         const int last_key = full ? p.c - 1 : min(q0 + 32 * OWN, p.c) - 1 - off;
         const int wave_last = full ? p.c - 1 : min(q0 + 32 * qw + 31, p.c - 1) - off;
         const int lane_last = full ? p.c - 1 : a - off;
-        for (int t0 = 0; t0 <= last_key; t0 += TK) {
+        int t0 = 0, start = 0, wave_lo = 0;
+        if constexpr (WINDOW) {
+            start = window_start(p, q0) / 32 * 32;
+            wave_lo = window_start(p, q0 + 32 * qw);
+            if (p.sinks == 0) t0 = start;
+        }
+        for (; t0 <= last_key;) {
             __syncthreads();
             stage<T, DP, TK>(k_lds, K, p.kv_stride_s, t0, p.c, d);
             stage<T, DP, TK>(v_lds, V, p.kv_stride_s, t0, p.c, d);
@@ -370,15 +404,20 @@ __device__ inline void bwd_dq(const StepArgs& p, int n_tiles, int linear, float*
             for (int s = 0; s < SUB; ++s) {
                 const int at = 32 * (SUB * kw + s), key0 = t0 + at;
                 if (key0 > wave_last) break;
+                if constexpr (WINDOW) {
+                    if (key0 + 31 < wave_lo && key0 >= p.sinks) continue;
+                }
                 f32x16 x = scores<DP>(k_lds + at * lds_pitch(DP), qf, n, h);
                 const f32x16 dp = scores<DP>(v_lds + at * lds_pitch(DP), gf, n, h);
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
-                    const float pr = key0 + reg_row(r, h) <= lane_last ? expf(x[r] * p.scale - lse) : 0.f;
+                    const float pr = sees(key0 + reg_row(r, h), lane_last) ? expf(x[r] * p.scale - lse) : 0.f;
                     x[r] = pr * (dp[r] - delta);
                 }
                 accumulate<DP, NB>(acc, k_lds + at * lds_pitch(DP), x, n, h);
             }
+            if constexpr (WINDOW) t0 = next_tile<TK>(p, t0, start);
+            else t0 += TK;
         }
     }
     const bool odd = a_own < p.c && not_finite<NB>(acc);
@@ -388,7 +427,8 @@ __device__ inline void bwd_dq(const StepArgs& p, int n_tiles, int linear, float*
     if (a_own < p.c && !((odd_rows >> n) & 1))
         add_rows<SPLIT, NB>(p.dq + base + (int64_t)a * p.stride_s, acc, p.scale, 0, d, kw, h, p.fresh);
     each_row<SPLIT>(odd_rows, kw, [&](const StepArgs& again, int i) {
-        if constexpr (PACKED) dq_row<T>(p, b, hd, dev_i, q0 + 32 * qw + i, lane);
+        if constexpr (WINDOW) window_dq_row<T>(p, hd, q0 + 32 * qw + i, lane);
+        else if constexpr (PACKED) dq_row<T>(p, b, hd, dev_i, q0 + 32 * qw + i, lane);
         else dq_row<T>(again, b, hd, dev_i, q0 + 32 * qw + i, lane);
     });
 }
@@ -398,8 +438,9 @@ __device__ inline void bwd_dq(const StepArgs& p, int n_tiles, int linear, float*
 // key/value head come one after the other.  DP = 256: a workgroup accumulates one 128-column
 // half of dK and dV (both halves beside K and V do not fit the registers) and scores are formed
 // once per half.
-template <typename T, int DP, int SPLIT, bool PACKED = false>
-__device__ inline void bwd_dkdv(const StepArgs& p, int n_tiles, int linear, float* lds, float* stats, uint32_t* masks) {
+template <typename T, int DP, int SPLIT, bool PACKED = false, typename Args = StepArgs>
+__device__ inline void bwd_dkdv(const Args& p, int n_tiles, int linear, float* lds, float* stats, uint32_t* masks) {
+    constexpr bool WINDOW = std::is_same<Args, WindowArgs>::value;
     constexpr int OWN = WAVES / SPLIT, TK = tile_rows(SPLIT), SUB = subtiles(SPLIT);
     constexpr int HALVES = DP > 128 ? 2 : 1, NB = DP / HALVES / 32;
     float* const q_lds = lds;
@@ -440,7 +481,13 @@ __device__ inline void bwd_dkdv(const StepArgs& p, int n_tiles, int linear, floa
             const int first_query = full ? 0 : k0 + off;
             const int wave_first = full ? 0 : k0 + 32 * own + off;
             const int lane_first = full ? 0 : key_own + off;
-            for (int t0 = first_query / 32 * 32; t0 < p.c; t0 += TK) {
+            int t_end = p.c, wave_end = p.c, lane_end = p.c;         // one past the last query
+            if constexpr (WINDOW) {
+                t_end = k0 < p.sinks ? p.c : window_end(p, k0 + 32 * OWN - 1);
+                wave_end = k0 + 32 * own < p.sinks ? p.c : window_end(p, k0 + 32 * own + 31);
+                lane_end = window_end(p, key_own);
+            }
+            for (int t0 = first_query / 32 * 32; t0 < t_end; t0 += TK) {
                 __syncthreads();
                 stage<T, DP, TK>(q_lds, Q, p.stride_s, t0, p.c, d);
                 stage<T, DP, TK>(g_lds, G, p.stride_s, t0, p.c, d);
@@ -452,14 +499,14 @@ __device__ inline void bwd_dkdv(const StepArgs& p, int n_tiles, int linear, floa
 #pragma unroll 1
                 for (int s = 0; s < SUB; ++s) {
                     const int at = 32 * (SUB * qsub + s), a0 = t0 + at;
-                    if (a0 >= p.c) break;
+                    if (a0 >= wave_end) break;
                     if (a0 + 31 < wave_first) continue;
                     const f32x16 x = scores<DP>(q_lds + at * lds_pitch(DP), kf, n, h);
                     f32x16 dp = scores<DP>(g_lds + at * lds_pitch(DP), vf, n, h), pr;
 #pragma unroll
                     for (int r = 0; r < 16; ++r) {
                         const int row = reg_row(r, h), a = a0 + row;
-                        pr[r] = a >= lane_first && a < p.c ? expf(x[r] * p.scale - stats[at + row]) : 0.f;
+                        pr[r] = a >= lane_first && a < lane_end ? expf(x[r] * p.scale - stats[at + row]) : 0.f;
                         dp[r] = pr[r] * (dp[r] - stats[TK + at + row]);
                     }
                     accumulate<DP, NB>(accv, g_lds + at * lds_pitch(DP) + col0, pr, n, h);
@@ -483,7 +530,8 @@ __device__ inline void bwd_dkdv(const StepArgs& p, int n_tiles, int linear, floa
         add_rows<SPLIT, NB>(p.dk + row, acck, p.scale, col0, d, qsub, h, p.fresh);
     }
     each_row<SPLIT>(odd_rows, qsub, [&](const StepArgs& again, int i) {
-        if constexpr (PACKED) dkdv_row<T>(p, b, kvh, dev_i, k0 + 32 * own + i, col0, HALVES > 1 ? min(d, col0 + 128) : d, lane);
+        if constexpr (WINDOW) window_dkdv_row<T>(p, kvh, k0 + 32 * own + i, col0, HALVES > 1 ? min(d, col0 + 128) : d, lane);
+        else if constexpr (PACKED) dkdv_row<T>(p, b, kvh, dev_i, k0 + 32 * own + i, col0, HALVES > 1 ? min(d, col0 + 128) : d, lane);
         else dkdv_row<T>(again, b, kvh, dev_i, k0 + 32 * own + i, col0, HALVES > 1 ? min(d, col0 + 128) : d, lane);
     });
 }

@@ -55,6 +55,7 @@
 #include "mfma_tiles.h"
 #include "packed.h"
 #include "sa_internal.h"
+#include "window.h"
 
 namespace sa {
 
@@ -114,14 +115,15 @@ __device__ inline bf16x8 lds_read_tr(const char* lds, uint32_t addr, uint32_t ad
 // halves, TILE_BYTES apart in LDS, and every slice holds one MFMA of each product per half.  PART: d % 8 == 4, the K fragment that holds
 // column d is cleared beyond it (part_ks = its k-step, or -1 for the lanes of the other
 // half-wave).
+// WINDOW: allowed is also only what is above mask_lim - window or below sink_lim (csrc/window.h).
 // REBASE and rebase (wave-uniform): the rows take the maximum of this sub-tile as their reference, above
 // or below the old one.
-template <bool QK, bool SM, bool PV, bool MASK, int DP, bool PART, bool REBASE = false>
+template <bool QK, bool SM, bool PV, bool MASK, int DP, bool PART, bool REBASE = false, bool WINDOW = false>
 __device__ __forceinline__ void step(f32x16& s_cur, f32x16& s_next, bf16x8 (&p_cur)[2], bf16x8 (&p_prev)[2],
                             f32x16 (&oacc)[4 * halves_of(DP)], const bf16x8 (&qf)[8 * halves_of(DP)], float& m,
                             float& l, float kappa, const uint32_t (&kaddr)[8], const uint32_t (&vaddr)[4],
                             const char* k_next, const char* v_prev, int mask_lim, int part_ks,
-                            bool rebase = false) {
+                            bool rebase = false, int window = 0, int sink_lim = 0) {
     constexpr int NH = halves_of(DP), KS = ksteps_of(DP), MB = blocks_of(DP);      // per half
     // Operands of slice i are requested from LDS two slices ahead, so only a few of
     // them are live at a time; slice i holds, per half, QK MFMA i (k-step i) and PV MFMA i
@@ -143,8 +145,10 @@ __device__ __forceinline__ void step(f32x16& s_cur, f32x16& s_next, bf16x8 (&p_c
     for (int i = 0; i < AHEAD; ++i) fetch(i);
     if (SM && MASK) {
 #pragma unroll
-        for (int r = 0; r < 16; ++r)
-            if (8 * (r / 4) + (r % 4) > mask_lim) s_cur[r] = -INFINITY;
+        for (int r = 0; r < 16; ++r) {
+            const int key = 8 * (r / 4) + (r % 4);
+            if (key > mask_lim || (WINDOW && key <= mask_lim - window && key >= sink_lim)) s_cur[r] = -INFINITY;
+        }
     }
     if (QK) {
 #pragma unroll
@@ -236,11 +240,11 @@ __device__ __forceinline__ void step(f32x16& s_cur, f32x16& s_next, bf16x8 (&p_c
 // d 128, forward: 5.93 -> 4.03 ms; 4 x 1024 tokens, 2 heads, forward + backward: 1.42 -> 0.27 ms.
 // ROPE: the query rows are rotated by their position ids as they are loaded (d == DP).
 // Args: StepArgs, or PackedArgs for packed sequences (packed.h): the workgroup then looks up its sequence and plays one
-// triangular block of it, the rows are written in bf16 and nothing is read of them.
+// triangular block of it, the rows are written in bf16 and nothing is read of them.  WindowArgs (window.h): the same with a window.
 template <bool RAGGED, int WALK, int DP, bool PART, bool BY_RANK, bool ROPE = false, typename Args = StepArgs>
 __global__ void __launch_bounds__(64 * NW, DP > 128 ? 1 : 2)
 fwd_mfma_kernel(Args p, int n_qtiles) {
-    constexpr bool PACKED = !std::is_same<Args, StepArgs>::value;
+    constexpr bool PACKED = !std::is_same<Args, StepArgs>::value, WINDOW = std::is_same<Args, WindowArgs>::value;
     using OutT = std::conditional_t<PACKED, __bf16, float>;
     constexpr int NH = halves_of(DP), KS = ksteps_of(DP), MB = halves_of(DP) * blocks_of(DP);      // k-steps per half, column blocks
     constexpr bool RING = WALK == WALK_RING;
@@ -363,10 +367,20 @@ fwd_mfma_kernel(Args p, int n_qtiles) {
         for (int hh = 0; hh < NH; ++hh)
             load_v_tile_direct(V, tile_byte_offset, buf + hh * TILE_BYTES, vg0[hh], wave, pitch);
     };
+    // The walk, WINDOW: pairs of tiles, those with first keys and those of the rows' windows; every pair carries the mask but those that all rows
+    // see.
+    WindowWalk<BM> walk;
+    int window = 0, sink_base = 0;          // of sub-tile v, register r is a first key iff 8 (r/4) + r%4 < sink_base - 32 v
+    if constexpr (WINDOW) {
+        walk = WindowWalk<BM>(p, q0, qt + 1);
+        window = p.window;
+        sink_base = p.sinks - 4 * h;
+    }
+    const int t_begin = WINDOW ? 2 * walk.at(0) : 0;
     // first tiles on their way while the running state is loaded
-    load_k(K, 0, k_lds0);
-    load_v(V, 0, v_lds0);
-    load_k(K, tile_pitch, k_lds1);     // n_kt >= 2 always
+    load_k(K, t_begin * tile_pitch, k_lds0);
+    load_v(V, t_begin * tile_pitch, v_lds0);
+    load_k(K, (t_begin + 1) * tile_pitch, k_lds1);     // n_kt >= 2 always
 
     bf16x8 qf[8 * NH];
     if constexpr (PACKED) {
@@ -437,15 +451,15 @@ fwd_mfma_kernel(Args p, int n_qtiles) {
         char* const k_nxt = PAR ? k_lds0 : k_lds1;
         char* const v_cur = PAR ? v_lds1 : v_lds0;
         char* const v_prv = PAR ? v_lds0 : v_lds1;
-        step<true, true, !FIRST, MASK, DP, PART, RING && PAR == 0 && MASK && !FIRST>(s_a, s_b, p_a, p_b, oacc, qf, m, l, kappa, kaddr, vaddr,
+        step<true, true, !FIRST, MASK, DP, PART, RING && PAR == 0 && MASK && !FIRST, WINDOW>(s_a, s_b, p_a, p_b, oacc, qf, m, l, kappa, kaddr, vaddr,
                                                  k_cur + tile_bytes(DP) / 2, v_prv + tile_bytes(DP) / 2,
-                                                 mask_base - 64 * t, part_ks, rebase && t == 0);
+                                                 mask_base - 64 * t, part_ks, rebase && t == 0, window, sink_base - 64 * t);
         __builtin_amdgcn_s_waitcnt(0);
         __syncthreads();
         if (LD >= 2) load_k(kr, k_at, k_cur);
         if (LD >= 1) load_v(vr, v_at, v_prv);
-        step<!LAST, true, true, MASK, DP, PART>(s_b, s_a, p_b, p_a, oacc, qf, m, l, kappa, kaddr, vaddr, k_nxt,
-                                                v_cur, mask_base - 64 * t - 32, part_ks);
+        step<!LAST, true, true, MASK, DP, PART, false, WINDOW>(s_b, s_a, p_b, p_a, oacc, qf, m, l, kappa, kaddr, vaddr, k_nxt,
+                                                v_cur, mask_base - 64 * t - 32, part_ks, false, window, sink_base - 64 * t - 32);
     };
     using T = std::true_type;
     using F = std::false_type;
@@ -489,7 +503,21 @@ fwd_mfma_kernel(Args p, int n_qtiles) {
         trip(first_c, F{}, T{}, P0{}, t, L1{}, K, 0, V, (t + 1) * tile_pitch);
         trip(F{}, T{}, T{}, P1{}, t + 1, L0{}, K, 0, V, 0);
     };
-    if (n_kt == 2 && kv + 1 == kv_end) {                   // a single pair (triangular: the first query tile)
+    if constexpr (WINDOW) {
+        t = t_begin;
+        if (walk.n > 1) {
+            pair(T{}, T{}, K, V, 2 * walk.at(1) * tile_pitch);
+            int i = 1;
+            for (; i < walk.masked; ++i) {
+                t = 2 * walk.at(i);
+                pair(F{}, T{}, K, V, 2 * walk.at(i + 1) * tile_pitch);
+            }
+            for (t = 2 * walk.at(i); i < walk.n - 1; ++i, t += 2) pair(F{}, F{}, K, V, (t + 2) * tile_pitch);      // the hot loop
+            last_pair(F{});
+        } else {
+            last_pair(T{});
+        }
+    } else if (n_kt == 2 && kv + 1 == kv_end) {                   // a single pair (triangular: the first query tile)
         last_pair(T{});
     } else {
         if (t_mask == 0) {          // masked from the start: a one-pair block or emulated coarse skipping
@@ -537,6 +565,9 @@ fwd_mfma_kernel(Args p, int n_qtiles) {
     const float inv = w_sum > 0.f ? 1.f / w_sum : 0.f;
     const float a_old = w_old * inv;
     const float a_part = l_tot > 0.f ? w_part * inv / l_tot : 0.f;
+    uint32_t odd = 0;           // rows to do over
+    if constexpr (WINDOW) odd = row_mask(row_ok && (!(l_tot > 0.f && l_tot < INFINITY) || window_odd<MB, PART>(oacc, h, d)));
+    const bool stored = row_ok && (!WINDOW || !((odd >> n) & 1));
 #pragma unroll
     for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
@@ -547,7 +578,7 @@ fwd_mfma_kernel(Args p, int n_qtiles) {
                 bf16x4 y[2];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) y[e / 4][e % 4] = (__bf16)(oacc[mb][4 * g + e] * a_part);
-                store_two_chunks(O + (int64_t)a * ss, col - 4 * h, y[0], y[1], row_ok, h, d);
+                store_two_chunks(O + (int64_t)a * ss, col - 4 * h, y[0], y[1], stored, h, d);
             } else {
                 if (col >= d || !row_ok) continue;        // padding columns, rows beyond the shard
                 float4* dst = reinterpret_cast<float4*>(O + (int64_t)a * ss + col);
@@ -561,7 +592,11 @@ fwd_mfma_kernel(Args p, int n_qtiles) {
                 *dst = x;
             }
         }
-    if (h == 0 && row_ok) L[a] = (top + __builtin_amdgcn_logf(w_sum)) * LN2;
+    if (h == 0 && stored) L[a] = (top + __builtin_amdgcn_logf(w_sum)) * LN2;
+    if constexpr (WINDOW)
+        each_window_row<true, BM>(odd, (int)blockIdx.x, launch_args().H, 32 * wave, [&](const WindowArgs& again, int head, int row) {
+            window_fwd_row<__hip_bfloat16>(again, head, row, threadIdx.x & 63);
+        });
 }
 
 }  // namespace

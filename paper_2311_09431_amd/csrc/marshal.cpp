@@ -271,6 +271,8 @@ void statistics(const at::Tensor& t, int64_t n0, int64_t n1, const char* why) {
         refuse(PyExc_ValueError, why);
 }
 void* at_of(const at::Tensor& t) { return t.data_ptr(); }
+const at::Tensor* maybe(const Call& on, PyObject* o) { return o == Py_None ? nullptr : &on(o); }
+void* at_of(const at::Tensor* t) { return t ? t->data_ptr() : nullptr; }
 sa_packed packed_of(const at::Tensor& q, const at::Tensor& k, const at::Tensor& v, const at::Tensor& offsets, const at::Tensor& lse, PyObject* max_len,
                     PyObject* scale) {
     const Strides qs = strides(q), ks = strides(k);
@@ -313,6 +315,53 @@ ENTRY(packed_bwd) {
         });
     });
 }
+// (function address, q, k, v, offsets, out, lse, max_len, window, sinks, scale, device, stream)
+ENTRY(window_fwd) {
+    return guarded(n, 13, [&] {
+        const auto f = reinterpret_cast<decltype(&sa_attn_window_fwd)>(address(a[0]));
+        const Call on(a[11]);
+        const at::Tensor &q = on(a[1]), &k = on(a[2]), &v = on(a[3]), &off = on.ids(a[4], OFFSETS), &out = on(a[5]), &lse = on(a[6]);
+        const sa_packed s = packed_of(q, k, v, off, lse, a[7], a[10]);
+        const sa_window w = {int32(a[8]), int32(a[9])};
+        same(out, q, "out must have q's shape, type and strides");
+        void* st = stream(a[12]);
+        return run([&] { return f(at_of(q), at_of(k), at_of(v), (const int32_t*)at_of(off), at_of(out), (float*)at_of(lse), &s, &w, st); });
+    });
+}
+// (function address, q, k, offsets, max_len, window, sinks): bytes
+ENTRY(window_bwd_workspace) {
+    return guarded(n, 7, [&] {
+        const auto f = reinterpret_cast<decltype(&sa_attn_window_bwd_workspace)>(address(a[0]));
+        const at::Tensor &q = tensor(a[1]), &k = tensor(a[2]), &off = tensor(a[3]);
+        const Strides qs = strides(q), ks = strides(k);
+        if (off.dim() != 1 || off.size(0) < 1) refuse(PyExc_ValueError, "offsets must hold one more number than there are sequences");
+        const sa_packed s = {size(off, 0) - 1, size(q, 0), int32(a[4]), size(q, 1), size(k, 1), size(q, 2), qs.h, qs.s, ks.h, ks.s, q.size(0), type_of(q), 0.f};
+        const sa_window w = {int32(a[5]), int32(a[6])};
+        return PyLong_FromLongLong(f(&s, &w));
+    });
+}
+// (function address, q, k, v, out, dout, lse, offsets, delta, dq, dk, dv, workspace, max_len, window, sinks, scale, device, stream)
+ENTRY(window_bwd) {
+    return guarded(n, 19, [&] {
+        const auto f = reinterpret_cast<decltype(&sa_attn_window_bwd)>(address(a[0]));
+        const Call on(a[17]);
+        const at::Tensor &q = on(a[1]), &k = on(a[2]), &v = on(a[3]), &out = on(a[4]), &dout = on(a[5]), &lse = on(a[6]), &off = on.ids(a[7], OFFSETS),
+                         &delta = on(a[8]), &dq = on(a[9]), &dk = on(a[10]), &dv = on(a[11]);
+        const at::Tensor* work = maybe(on, a[12]);
+        const sa_packed s = packed_of(q, k, v, off, lse, a[13], a[16]);
+        const sa_window w = {int32(a[14]), int32(a[15])};
+        for (const at::Tensor* t : {&out, &dout, &dq}) same(*t, q, "out, dout and dq must have q's shape, type and strides");
+        for (const at::Tensor* t : {&dk, &dv}) same(*t, k, "dk and dv must have k's shape, type and strides");
+        same(delta, lse, "delta must have lse's shape, type and strides");
+        if (work && !work->is_contiguous()) refuse(PyExc_ValueError, "workspace must be contiguous");
+        const int64_t bytes = work ? work->numel() * work->element_size() : 0;
+        void* st = stream(a[18]);
+        return run([&] {
+            return f(at_of(q), at_of(k), at_of(v), at_of(out), at_of(dout), (const float*)at_of(lse), (const int32_t*)at_of(off), (float*)at_of(delta),
+                     at_of(dq), at_of(dk), at_of(dv), at_of(work), bytes, &s, &w, st);
+        });
+    });
+}
 // [pages, page_size, heads, d]
 sa_cache cache_of(const at::Tensor& k) {
     if (k.dim() != 4) refuse(PyExc_ValueError, "a cache is [pages, page size, heads, d]");
@@ -321,8 +370,6 @@ sa_cache cache_of(const at::Tensor& k) {
     const int64_t h = k.size(2) == 1 ? k.size(3) : k.stride(2);
     return {size(k, 0), size(k, 1), size(k, 2), size(k, 3), k.size(0) == 1 ? 0 : k.stride(0), k.stride(1), h, type_of(k)};
 }
-const at::Tensor* maybe(const Call& on, PyObject* o) { return o == Py_None ? nullptr : &on(o); }
-void* at_of(const at::Tensor* t) { return t ? t->data_ptr() : nullptr; }
 // (function address, k, v, slot, k_cache, v_cache, pos, k_out, q, q_out, base, device, stream)
 ENTRY(append) {
     return guarded(n, 13, [&] {
@@ -424,7 +471,7 @@ ENTRY(set_up) {
 
 #define FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(two), FAST(three), FAST(step_fwd), FAST(step_bwd), FAST(ring_fwd), FAST(ring_bwd), FAST(rope),
-                         FAST(permute), FAST(packed_fwd), FAST(packed_bwd), FAST(append), FAST(decode), FAST(decode_workspace),
+                         FAST(permute), FAST(packed_fwd), FAST(packed_bwd), FAST(window_fwd), FAST(window_bwd), FAST(window_bwd_workspace), FAST(append), FAST(decode), FAST(decode_workspace),
                          FAST(extent_of), FAST(set_up), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

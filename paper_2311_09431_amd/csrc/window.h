@@ -1,0 +1,161 @@
+// Attention with a sliding window and a few first tokens that stay visible, over packed sequences (packed.h): row a of a sequence sees key b where
+// b <= a and (a - b < window or b < sinks).  The packed kernels' workgroups, whose walk leaves out the tiles that no row of theirs sees: a
+// query-owning one's goes over the tiles with first keys, then on to those of its rows' windows; a key-owning one's ends with the last row
+// whose window reaches back to its keys, of a tile with first keys with the sequence.
+#pragma once
+#include "f32_rows.h"
+#include "packed.h"
+
+namespace sa {
+
+struct WindowArgs : PackedArgs {
+    int window, sinks;          // 1 .. max_len, 0 .. max_len
+};
+hipError_t launch_window_fwd(WindowArgs p, hipStream_t st);
+hipError_t launch_window_bwd(WindowArgs p, hipStream_t st);
+hipError_t launch_window_f32(WindowArgs p, bool backward, hipStream_t st);
+
+// the first key of row a's window
+__device__ inline int window_start(const WindowArgs& p, int a) { return max(0, a - p.window + 1); }
+// one past the last row that sees `key`, of c
+__device__ inline int window_end(const WindowArgs& p, int key) { return key < p.sinks ? p.c : min(p.c, key + p.window); }
+
+// The walk of a query-owning workgroup of PAIR rows from q0 on, over tiles of PAIR keys, `tiles` of them up to its own.
+template <int PAIR>
+struct WindowWalk {
+    int firsts = 0, start = 0, masked = 0, n = 0;      // tiles with first keys; the window's first one; up to where some row does not see a key; all
+    __device__ WindowWalk() {}
+    __device__ WindowWalk(const WindowArgs& p, int q0, int tiles) {
+        start = window_start(p, q0) / PAIR;
+        firsts = min(start, (p.sinks + PAIR - 1) / PAIR);
+        n = firsts + tiles - start;
+        // (the last row's window begins above this; those with first keys are few, and masked too)
+        const int below = q0 + PAIR - 1 - p.window;
+        masked = below < 0 ? 0 : min(n - 1, firsts + below / PAIR + 1 - start);
+    }
+    __device__ int at(int i) const { return i < firsts ? i : i - firsts + start; }
+};
+
+// Rows done over, as f32_rows.h has them: nothing but the pairs that the mask allows, one wavefront a row.  The tiles multiply masked pairs with
+// a weight of zero, of which an infinite or NaN element makes a NaN.
+__device__ inline void store1(float* to, float x) { *to = x; }
+__device__ inline void store1(__hip_bfloat16* to, float x) { *reinterpret_cast<__bf16*>(to) = (__bf16)x; }
+
+// Some register of NB 32-column blocks from column col0 on is infinite or NaN.  PART: columns from d on hold what follows the rows, and are not
+// looked at.
+template <int NB, bool PART, typename Acc>
+__device__ inline bool window_odd(const Acc& acc, int h, int d, int col0 = 0) {
+    if constexpr (!PART) return not_finite<NB>(acc);
+    float z = 0.f;
+#pragma unroll
+    for (int mb = 0; mb < NB; ++mb)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) z = fmaf(col0 + 32 * mb + reg_row(r, h) < d ? acc[mb][r] : 0.f, 0.f, z);
+    return z != 0.f;
+}
+// the keys of row a in ranges: body(first, end)
+template <typename Body>
+__device__ inline void window_ranges(const WindowArgs& p, int a, Body body) {
+    const int lo = window_start(p, a);
+#pragma unroll 1
+    for (int i = 0; i < 2; ++i) body(i ? lo : 0, i ? a + 1 : min(p.sinks, lo));
+}
+template <typename T>
+__device__ inline void window_fwd_row(const WindowArgs& p, int hd, int a, int lane) {
+    const int64_t row = hd * p.stride_h + (int64_t)a * p.stride_s, kv_base = (hd / (p.H / p.H_kv)) * p.kv_stride_h;
+    const T* q = (const T*)p.q + row;
+    T* O = (T*)p.o + row;
+    float m = -INFINITY, l = 0.f, acc[ROW_COLS] = {};
+    window_ranges(p, a, [&](int first, int end) {
+#pragma unroll 1
+        for (int k0 = first; k0 < end; k0 += 64) {
+            const T* K = (const T*)p.k + kv_base + (int64_t)k0 * p.kv_stride_s;
+            const T* V = (const T*)p.v + kv_base + (int64_t)k0 * p.kv_stride_s;
+            const bool valid = k0 + lane < end;
+            const float s = valid ? p.scale * dot_rows<T>(q, K + lane * p.kv_stride_s, p.d) : -INFINITY;
+            const float m_new = fmaxf(m, wave_max(s)), ref = m_new == -INFINITY ? 0.f : m_new;
+            const float alpha = m == -INFINITY ? 0.f : expf(m - m_new);
+            const float pr = valid ? expf(s - ref) : 0.f;
+            l = l * alpha + wave_sum(pr);
+#pragma unroll
+            for (int k = 0; k < ROW_COLS; ++k) acc[k] *= alpha;
+            add_weighted<T>(acc, pr, V, p.kv_stride_s, min(64, end - k0), 0, p.d, lane);
+            m = m_new;
+        }
+    });
+    const float inv = 1.f / l;          // every key it sees at -inf: no number
+#pragma unroll
+    for (int k = 0; k < ROW_COLS; ++k)
+        if (lane + 64 * k < p.d) store1(O + lane + 64 * k, acc[k] * inv);
+    if (lane == 0) p.lse[hd * p.stat_stride_h + a] = l == 0.f ? NAN : m + logf(l);
+}
+template <typename T>
+__device__ inline void window_dq_row(const WindowArgs& p, int hd, int a, int lane) {
+    const int64_t row = hd * p.stride_h + (int64_t)a * p.stride_s, kv_base = (hd / (p.H / p.H_kv)) * p.kv_stride_h;
+    const T* q = (const T*)p.q + row;
+    const T* g = (const T*)p.dout + row;
+    const float lse = p.lse[hd * p.stat_stride_h + a], delta = p.delta[hd * p.stat_stride_h + a];
+    float acc[ROW_COLS] = {};
+    window_ranges(p, a, [&](int first, int end) {
+#pragma unroll 1
+        for (int k0 = first; k0 < end; k0 += 64) {
+            const T* K = (const T*)p.k + kv_base + (int64_t)k0 * p.kv_stride_s;
+            const T* V = (const T*)p.v + kv_base + (int64_t)k0 * p.kv_stride_s;
+            float ds = 0.f;
+            if (k0 + lane < end) {
+                const float pr = expf(p.scale * dot_rows<T>(q, K + lane * p.kv_stride_s, p.d) - lse);
+                ds = pr * (dot_rows<T>(g, V + lane * p.kv_stride_s, p.d) - delta);
+            }
+            add_weighted<T>(acc, ds, K, p.kv_stride_s, min(64, end - k0), 0, p.d, lane);
+        }
+    });
+#pragma unroll
+    for (int k = 0; k < ROW_COLS; ++k)
+        if (lane + 64 * k < p.d) store1((T*)p.dq + row + lane + 64 * k, p.scale * acc[k]);
+}
+// columns col0 .. end_col - 1 of dK and dV
+template <typename T>
+__device__ inline void window_dkdv_row(const WindowArgs& p, int kvh, int key, int col0, int end_col, int lane) {
+    const int group = p.H / p.H_kv, end = window_end(p, key);
+    const int64_t row = kvh * p.kv_stride_h + (int64_t)key * p.kv_stride_s;
+    float acck[ROW_COLS] = {}, accv[ROW_COLS] = {};
+#pragma unroll 1
+    for (int hd = kvh * group; hd < (kvh + 1) * group; ++hd) {
+        const float* lse = p.lse + hd * p.stat_stride_h;
+        const float* delta = p.delta + hd * p.stat_stride_h;
+#pragma unroll 1
+        for (int a0 = key; a0 < end; a0 += 64) {
+            const T* Q = (const T*)p.q + hd * p.stride_h + (int64_t)a0 * p.stride_s;
+            const T* G = (const T*)p.dout + hd * p.stride_h + (int64_t)a0 * p.stride_s;
+            float pr = 0.f, ds = 0.f;
+            if (a0 + lane < end) {
+                pr = expf(p.scale * dot_rows<T>((const T*)p.k + row, Q + lane * p.stride_s, p.d) - lse[a0 + lane]);
+                ds = pr * (dot_rows<T>((const T*)p.v + row, G + lane * p.stride_s, p.d) - delta[a0 + lane]);
+            }
+            add_weighted<T>(accv, pr, G, p.stride_s, min(64, end - a0), col0, end_col, lane);
+            add_weighted<T>(acck, ds, Q, p.stride_s, min(64, end - a0), col0, end_col, lane);
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < ROW_COLS; ++k) {
+        const int col = col0 + lane + 64 * k;
+        if (col >= end_col) continue;
+        store1((T*)p.dv + row + col, accv[k]);
+        store1((T*)p.dk + row + col, p.scale * acck[k]);
+    }
+}
+// The rows set in a mask, as each_row has them: the launch's arguments are read and its sequence looked up anew, so that nothing of either has to be
+// kept until here (39 registers spilled in the forward at 128 columns, 128 in dQ's).  first_row: of the wavefront within its workgroup's tile.
+// row(arguments, head, row of the sequence).
+template <bool SNAKE, int TILE, typename Row>
+__device__ inline void each_window_row(uint32_t rows, int linear, int n_heads, int first_row, Row row) {
+    if (rows == 0) return;
+    WindowArgs p = static_cast<const WindowArgs&>(launch_args());
+    int n_tiles, rank, head;
+    if (!enter_sequence<SNAKE, TILE>(p, linear, n_heads, n_tiles, rank, head)) return;
+    first_row += TILE * (SNAKE ? n_tiles - 1 - rank : rank);        // (query tiles: the heaviest, the first in order, is the last)
+#pragma unroll 1
+    for (; rows != 0; rows &= rows - 1) row(p, head, first_row + __builtin_ctz(rows));
+}
+
+}  // namespace sa
