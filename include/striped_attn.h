@@ -377,6 +377,70 @@ int sa_attn_decode(const void* q, const void* k_cache, const void* v_cache, cons
                    float* lse, void* workspace, int64_t workspace_bytes, const sa_decode* shape, const sa_cache* cache, void* stream);
 
 /*
+ * The same where the new token sees the last `window` of its sequence's cached tokens, its own among them, and the first `window->sinks`.  Of a page
+ * that holds no token it sees neither the number in the table nor the content is looked at (such pages may be given away), and of 16 tokens in
+ * a row that it sees none of no content.  Otherwise as sa_attn_decode, with its workspace, its errors, and SHAPE for a window below 1, sinks below 0.
+ */
+int sa_attn_window_decode(const void* q, const void* k_cache, const void* v_cache, const int32_t* table, const int32_t* lens, void* out,
+                          float* lse, void* workspace, int64_t workspace_bytes, const sa_decode* shape, const sa_cache* cache,
+                          const sa_window* window, void* stream);
+
+/* Drafted tokens of each of B sequences: q and out are [B, T, H, 0..d), LSE fp32 [B, T, H] (heads contiguous); heads as sa_decode's */
+typedef struct {
+    int32_t B, T, H;       /* T: 1 to 64; B * T * H below 2^24 */
+    int32_t max_pages;     /* as sa_decode's; the key/value heads of all sequences times T * H / H_kv, in 16s, times a 64th of the tokens that
+                              they name (plus 1) below 2^31 */
+    int64_t stride_b, stride_t, stride_h;          /* of q and out, multiples of 4 */
+    int64_t stat_stride_b, stat_stride_t;
+    int64_t table_stride;  /* page numbers between sequences in the table */
+    int64_t seen_stride;   /* masks between sequences */
+    float softmax_scale;   /* <= 0 selects 1/sqrt(d) */
+} sa_tree;
+
+/*
+ * Attention of a tree of drafted tokens (to verify a draft in one pass): token i of sequence b's draft lies in the cache as token lens[b] + i (appended
+ * before, its key rotated by whatever position id it has in the tree).  It sees the tokens 0 .. lens[b] - 1 in front of the draft, and those
+ * of the draft whose bits are set in seen[b, i], token j's being bit j: whom it descends from and, as a rule, itself.  Bits of tokens that the draft
+ * does not have are not looked at.  drafts: device int32 [B], the tokens of each draft (taken as 0 .. T); NULL: T each.  Rows of out and lse behind a
+ * sequence's draft are left as they are.  lens: device int32 [B], 0 or more; tokens behind max_pages * page_size are left out.
+ * A token that sees none is zero with LSE -inf; infinities and NaN as in sa_attn_decode, and nothing of a drafted token reaches one that does not see it.
+ * Pages, workspace (sa_attn_tree_workspace(shape, cache) bytes: it depends on T, H, H_kv, d), rounding and errors as sa_attn_decode; lengths, drafts,
+ * masks and the table are read on the device.
+ */
+int64_t sa_attn_tree_workspace(const sa_tree* shape, const sa_cache* cache);       /* or a negative sa_status */
+int sa_attn_tree(const void* q, const void* k_cache, const void* v_cache, const int32_t* table, const int32_t* lens, const int32_t* drafts,
+                 const int64_t* seen, void* out, float* lse, void* workspace, int64_t workspace_bytes, const sa_tree* shape,
+                 const sa_cache* cache, void* stream);
+
+/*
+ * The accepted tokens of drafts moved up behind the tokens in front of them, keys and values: token lens[b] + chosen[b, i] becomes token
+ * lens[b] + i, for i below accepted[b] (taken as 0 .. T).  chosen: device int32 [B, T], chosen_stride apart; a sequence's accepted ones ascend (as a
+ * branch of a tree does whose tokens come after those they descend from).  lens_after[b] = lens[b] + accepted[b] (a length below 0 counts as 0); may be
+ * lens, or NULL.  The other drafted tokens stay where they are.  A token whose page is none of the cache's or which lies behind max_pages *
+ * page_size, as source or destination, and a chosen number outside 0 .. T - 1 are left out.  Where chosen does not ascend, what the tokens
+ * lens[b] .. lens[b] + accepted[b] - 1 then hold is not defined; so it is where two sequences share a page that is written.
+ * B 0: success, nothing launched.  Errors: NULL, DTYPE, SHAPE (T outside 1 .. 64, B above 2^22), ALIGN, HIP.
+ */
+typedef struct {
+    int32_t B, T;
+    int32_t max_pages;     /* page numbers a sequence in the table; max_pages * page_size at most 2^30 */
+    int64_t table_stride, chosen_stride;
+} sa_accept;
+int sa_cache_accept(void* k_cache, void* v_cache, const int32_t* table, const int32_t* lens, const int32_t* chosen, const int32_t* accepted,
+                    int32_t* lens_after, const sa_accept* shape, const sa_cache* cache, void* stream);
+
+/*
+ * Pages copied, keys and values: page to[i] becomes page from[i], of n pairs of page numbers (device int32); with tokens (device int32 [n], taken as
+ * 0 .. page_size) its first tokens[i] tokens alone, the others stay.  What a fork of a sequence needs of its last, partly filled page (the
+ * others are shared by the tables), and what pushing the used pages of a pool together needs; which page is whose and which is free is the caller's.
+ * A pair with a number that is none of the cache's, or twice the same, is left out.  What a page then holds that is `to` of two pairs, or `to` of one and
+ * `from` of another, is not defined.
+ * n 0: success, nothing launched.  Errors: NULL, DTYPE, SHAPE (n below 0 or above 2^22, a page of 2^34 bytes or more), ALIGN, HIP.
+ */
+int sa_cache_copy(void* k_cache, void* v_cache, const int32_t* from, const int32_t* to, const int32_t* tokens, int32_t n,
+                  const sa_cache* cache, void* stream);
+
+/*
  * Host-only helpers (no GPU work).
  * sa_step_mask: the step's mask, GetMask(q_dev, kv_dev) of Sec. 2.2 / 2.3 in local
  * indices.  Writes both outputs: *kind = 0 empty (nothing allowed) / 1 triangular (key b

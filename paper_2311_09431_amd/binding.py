@@ -95,6 +95,11 @@ def lib():
             "sa_cache_append": (i32, [vp] * 12),
             "sa_attn_decode_workspace": (i64, [vp, vp]),
             "sa_attn_decode": (i32, [vp] * 8 + [i64] + [vp] * 3),
+            "sa_attn_window_decode": (i32, [vp] * 8 + [i64] + [vp] * 4),
+            "sa_attn_tree_workspace": (i64, [vp, vp]),
+            "sa_attn_tree": (i32, [vp] * 10 + [i64] + [vp] * 3),
+            "sa_cache_accept": (i32, [vp] * 10),
+            "sa_cache_copy": (i32, [vp] * 5 + [i32] + [vp] * 2),
             "sa_step_tiles": (i32, [i32, i32, i32, i32, i64, i64, i64, ctypes.POINTER(i64),
                                     ctypes.POINTER(i64)]),
             "sa_step_mask": (i32, [i32, i32, i32, i32, ctypes.POINTER(i32), ctypes.POINTER(i32)]),
@@ -125,6 +130,7 @@ EXPORTS = ("sa_stripe_permute", "sa_unstripe_permute", "sa_rope", "sa_state_init
            "sa_attn_step_fwd_tiled", "sa_attn_step_bwd_tiled", "sa_ring_fwd_tiled", "sa_ring_bwd_tiled",
            "sa_attn_packed_fwd", "sa_attn_packed_bwd", "sa_attn_window_fwd", "sa_attn_window_bwd_workspace",
            "sa_attn_window_bwd", "sa_cache_append", "sa_attn_decode_workspace", "sa_attn_decode",
+           "sa_attn_window_decode", "sa_attn_tree_workspace", "sa_attn_tree", "sa_cache_accept", "sa_cache_copy",
            "sa_step_tiles", "sa_step_mask", "sa_step_pairs", "sa_device_props", "sa_status_str")
 
 
@@ -357,6 +363,38 @@ def sa_attn_decode(q, k_cache, v_cache, table, lens, out, lse, workspace, scale=
     caches [pages, page size, H_kv, d]; lse fp32 [B, H] or None."""
     _check(_marshal.decode(_entry["sa_attn_decode"], q, k_cache, v_cache, table, lens, out, lse, workspace, scale or 0.0, _here, _stream),
            "sa_attn_decode")
+
+
+def sa_attn_window_decode(q, k_cache, v_cache, table, lens, out, lse, workspace, window, sinks=0, scale=None):
+    """sa_attn_decode where the new token sees the last `window` cached tokens, its own among them, and the first `sinks`."""
+    _check(_marshal.window_decode(_entry["sa_attn_window_decode"], q, k_cache, v_cache, table, lens, out, lse, workspace, window, sinks, scale or 0.0,
+                                  _here, _stream), "sa_attn_window_decode")
+
+
+def sa_attn_tree_workspace(q, k_cache):
+    """Bytes of workspace of sa_attn_tree for such q and cache; the same for any number of sequences."""
+    size = _marshal.tree_workspace(_entry["sa_attn_tree_workspace"], q, k_cache)
+    _check(min(size, 0), "sa_attn_tree_workspace")
+    return size
+
+
+def sa_attn_tree(q, k_cache, v_cache, table, lens, seen, out, lse, workspace, drafts=None, scale=None):
+    """The drafted tokens of each sequence, q [B, T, H, d] (out in its strides, T up to 64), cached as tokens lens[b] + i: each over the tokens 0 .. lens[b] - 1
+    and those of the draft whose bits are set in seen (int64 [B, T], bit j: token j).  drafts: int32 [B], how many each has (None: T); lse fp32
+    [B, T, H] or None.  Rows behind a draft stay as they are."""
+    _check(_marshal.tree(_entry["sa_attn_tree"], q, k_cache, v_cache, table, lens, drafts, seen, out, lse, workspace, scale or 0.0, _here, _stream),
+           "sa_attn_tree")
+
+
+def sa_cache_accept(k_cache, v_cache, table, lens, chosen, accepted, lens_after=None):
+    """Cached token lens[b] + chosen[b, i] (int32 [B, T], ascending) becomes token lens[b] + i, for i < accepted[b] (int32 [B]); lens_after <- lens + accepted
+    (may be lens)."""
+    _check(_marshal.accept(_entry["sa_cache_accept"], k_cache, v_cache, table, lens, chosen, accepted, lens_after, _here, _stream), "sa_cache_accept")
+
+
+def sa_cache_copy(k_cache, v_cache, src, dst, tokens=None):
+    """Page dst[i] of the caches <- page src[i] (int32 [n] each), of it the first tokens[i] tokens (int32 [n]; None: all)."""
+    _check(_marshal.copy(_entry["sa_cache_copy"], k_cache, v_cache, src, dst, tokens, _here, _stream), "sa_cache_copy")
 
 
 def sa_step_tiles(q_dev, kv_dev, N, layout, c, skip_bq, skip_bk):

@@ -23,7 +23,7 @@ SOURCES = ["api.hip", "permute.hip", "elementwise.hip", "f32_step.hip", "fwd_mfm
            "bwd_mfma.hip", "bwd_ring.hip", "split_mfma.hip", "f32x3_step.hip", "f32x3_split.hip", "f32_route.hip",
            "rows_step.hip", "packed_fwd.hip", "packed_bwd.hip", "packed_bwd_ring.hip", "packed_f32.hip", "packed_split.hip", "packed_delta.hip",
            "packed_f32x3.hip", "packed_f32x3_split.hip", "window_fwd.hip", "window_bwd.hip", "window_f32.hip", "cache_append.hip",
-           "decode.hip"]
+           "decode.hip", "tree.hip", "cache_move.hip"]
 
 # Flags of single sources.  f32x3_step: score tiles are read by vector instructions right after
 # their products, so MFMA results stay out of the accumulation registers (forward 2.20 -> 2.10 ms,

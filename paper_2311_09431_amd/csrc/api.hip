@@ -302,6 +302,41 @@ int check_decode(const sa_decode* s, const sa_cache* c) {
     return s->stride_b % 4 || s->stride_h % 4 ? SA_ERR_ALIGN : SA_OK;
 }
 
+template <typename Args>
+void set_cache(Args& a, const sa_cache* c) {
+    a.H_kv = c->H_kv; a.d = c->d; a.n_pages = c->n_pages; a.page_size = c->page_size;
+    a.stride_page = c->stride_page; a.stride_slot = c->stride_s; a.stride_head = c->stride_h;
+}
+// the pointers of a call, checked
+int decode_args(const void* q, const void* k_cache, const void* v_cache, const int32_t* table, const int32_t* lens, void* out, float* lse, void* workspace,
+                int64_t workspace_bytes, const sa_decode* shape, const sa_cache* cache, sa::DecodeArgs& a) {
+    if (!q || !k_cache || !v_cache || !lens || !out || !workspace || (!table && shape->max_pages > 0)) return SA_ERR_NULL;
+    if (workspace_bytes < sa::decode_workspace(shape->H, cache->H_kv, cache->d)) return SA_ERR_SHAPE;
+    for (const void* p : {q, k_cache, v_cache, (const void*)out, (const void*)workspace})
+        if (!aligned16(p)) return SA_ERR_ALIGN;
+    if ((reinterpret_cast<uintptr_t>(table) | reinterpret_cast<uintptr_t>(lens) | reinterpret_cast<uintptr_t>(lse)) & 3u) return SA_ERR_ALIGN;
+    a.q = q; a.k_cache = k_cache; a.v_cache = v_cache; a.table = table; a.lens = lens; a.out = out; a.lse = lse;
+    a.parts = (float*)workspace;
+    a.B = shape->B; a.H = shape->H; a.max_pages = shape->max_pages;
+    a.stride_b = shape->stride_b; a.stride_h = shape->stride_h; a.stat_stride_b = shape->stat_stride_b; a.table_stride = shape->table_stride;
+    set_cache(a, cache);
+    a.scale = shape->softmax_scale > 0.f ? shape->softmax_scale : 1.0f / sqrtf((float)cache->d);
+    return SA_OK;
+}
+int check_tree(const sa_tree* s, const sa_cache* c) {
+    if (!s) return SA_ERR_NULL;
+    if (int e = check_cache(c)) return e;
+    if (s->B < 0 || s->T < 1 || s->T > 64 || s->H < 1 || s->H % c->H_kv || s->max_pages < 0) return SA_ERR_SHAPE;
+    if ((int64_t)s->B * s->T * s->H > kMostWorkgroups || (int64_t)s->max_pages * c->page_size > (int64_t(1) << 30)) return SA_ERR_SHAPE;
+    // (chunks of all units are numbered in 31 bits)
+    const int64_t units = (int64_t)c->H_kv * (((int64_t)s->T * (s->H / c->H_kv) + 15) / 16) * s->B;
+    if (((int64_t)s->max_pages * c->page_size / 64 + 1) >= (int64_t(1) << 31) / std::max<int64_t>(units, 1)) return SA_ERR_SHAPE;
+    if (s->stride_h < c->d || (s->T > 1 && (s->stride_t < s->H * s->stride_h || s->stat_stride_t < s->H))) return SA_ERR_SHAPE;
+    if (s->B > 1 && (s->stride_b < (s->T - 1) * s->stride_t + s->H * s->stride_h || s->stat_stride_b < (s->T - 1) * s->stat_stride_t + s->H)) return SA_ERR_SHAPE;
+    if (s->B > 1 && (s->table_stride < s->max_pages || s->seen_stride < s->T)) return SA_ERR_SHAPE;
+    return s->stride_b % 4 || s->stride_t % 4 || s->stride_h % 4 ? SA_ERR_ALIGN : SA_OK;
+}
+
 // Event bookkeeping for the drivers' optional per-step timings.
 struct StepTimer {
     std::vector<hipEvent_t> ev;
@@ -652,20 +687,87 @@ int sa_attn_decode(const void* q, const void* k_cache, const void* v_cache, cons
                    float* lse, void* workspace, int64_t workspace_bytes, const sa_decode* shape, const sa_cache* cache, void* stream) {
     if (int e = check_decode(shape, cache)) return e;
     if (shape->B == 0) return SA_OK;
-    if (!q || !k_cache || !v_cache || !lens || !out || !workspace || (!table && shape->max_pages > 0)) return SA_ERR_NULL;
-    if (workspace_bytes < sa::decode_workspace(shape->H, cache->H_kv, cache->d)) return SA_ERR_SHAPE;
+    sa::DecodeArgs a{};
+    if (int e = decode_args(q, k_cache, v_cache, table, lens, out, lse, workspace, workspace_bytes, shape, cache, a)) return e;
+    return sa::launch_decode(a, cache->dtype, (hipStream_t)stream) == hipSuccess ? SA_OK : SA_ERR_HIP;
+}
+
+int sa_attn_window_decode(const void* q, const void* k_cache, const void* v_cache, const int32_t* table, const int32_t* lens, void* out,
+                          float* lse, void* workspace, int64_t workspace_bytes, const sa_decode* shape, const sa_cache* cache,
+                          const sa_window* window, void* stream) {
+    if (int e = check_decode(shape, cache)) return e;
+    if (int e = check_window(window)) return e;
+    if (shape->B == 0) return SA_OK;
+    sa::WindowDecodeArgs a{};
+    if (int e = decode_args(q, k_cache, v_cache, table, lens, out, lse, workspace, workspace_bytes, shape, cache, a)) return e;
+    const int room = std::max(1, shape->max_pages * cache->page_size);         // (beyond it neither says more)
+    a.window = std::min(window->window, room);
+    a.sinks = std::min(window->sinks, room);
+    return sa::launch_window_decode(a, cache->dtype, (hipStream_t)stream) == hipSuccess ? SA_OK : SA_ERR_HIP;
+}
+
+int64_t sa_attn_tree_workspace(const sa_tree* shape, const sa_cache* cache) {
+    if (int e = check_tree(shape, cache)) return e;
+    return sa::tree_workspace(shape->T * (shape->H / cache->H_kv), cache->d);
+}
+
+int sa_attn_tree(const void* q, const void* k_cache, const void* v_cache, const int32_t* table, const int32_t* lens, const int32_t* drafts,
+                 const int64_t* seen, void* out, float* lse, void* workspace, int64_t workspace_bytes, const sa_tree* shape,
+                 const sa_cache* cache, void* stream) {
+    if (int e = check_tree(shape, cache)) return e;
+    if (shape->B == 0) return SA_OK;
+    if (!q || !k_cache || !v_cache || !lens || !seen || !out || !workspace || (!table && shape->max_pages > 0)) return SA_ERR_NULL;
+    if (workspace_bytes < sa_attn_tree_workspace(shape, cache)) return SA_ERR_SHAPE;
     for (const void* p : {q, k_cache, v_cache, (const void*)out, (const void*)workspace})
         if (!aligned16(p)) return SA_ERR_ALIGN;
-    if ((reinterpret_cast<uintptr_t>(table) | reinterpret_cast<uintptr_t>(lens) | reinterpret_cast<uintptr_t>(lse)) & 3u) return SA_ERR_ALIGN;
-    sa::DecodeArgs a{};
-    a.q = q; a.k_cache = k_cache; a.v_cache = v_cache; a.table = table; a.lens = lens; a.out = out; a.lse = lse;
+    for (const void* p : {(const void*)table, (const void*)lens, (const void*)drafts, (const void*)lse})
+        if (reinterpret_cast<uintptr_t>(p) & 3u) return SA_ERR_ALIGN;
+    if (reinterpret_cast<uintptr_t>(seen) & 7u) return SA_ERR_ALIGN;
+    sa::TreeArgs a{};
+    a.q = q; a.k_cache = k_cache; a.v_cache = v_cache; a.table = table; a.lens = lens; a.drafts = drafts; a.seen = seen; a.out = out; a.lse = lse;
     a.parts = (float*)workspace;
-    a.B = shape->B; a.H = shape->H; a.H_kv = cache->H_kv; a.d = cache->d; a.n_pages = cache->n_pages; a.page_size = cache->page_size;
-    a.max_pages = shape->max_pages;
-    a.stride_b = shape->stride_b; a.stride_h = shape->stride_h; a.stat_stride_b = shape->stat_stride_b; a.table_stride = shape->table_stride;
-    a.stride_page = cache->stride_page; a.stride_slot = cache->stride_s; a.stride_head = cache->stride_h;
+    a.B = shape->B; a.T = shape->T; a.H = shape->H; a.max_pages = shape->max_pages;
+    a.stride_b = shape->stride_b; a.stride_t = shape->stride_t; a.stride_h = shape->stride_h;
+    a.stat_stride_b = shape->stat_stride_b; a.stat_stride_t = shape->stat_stride_t;
+    a.table_stride = shape->table_stride; a.seen_stride = shape->seen_stride;
+    set_cache(a, cache);
     a.scale = shape->softmax_scale > 0.f ? shape->softmax_scale : 1.0f / sqrtf((float)cache->d);
-    return sa::launch_decode(a, cache->dtype, (hipStream_t)stream) == hipSuccess ? SA_OK : SA_ERR_HIP;
+    return sa::launch_tree(a, cache->dtype, (hipStream_t)stream) == hipSuccess ? SA_OK : SA_ERR_HIP;
+}
+
+int sa_cache_accept(void* k_cache, void* v_cache, const int32_t* table, const int32_t* lens, const int32_t* chosen, const int32_t* accepted,
+                    int32_t* lens_after, const sa_accept* shape, const sa_cache* cache, void* stream) {
+    if (!shape) return SA_ERR_NULL;
+    if (int e = check_cache(cache)) return e;
+    if (shape->B < 0 || shape->B > 1 << 22 || shape->T < 1 || shape->T > 64 || shape->max_pages < 0) return SA_ERR_SHAPE;
+    if ((int64_t)shape->max_pages * cache->page_size > (int64_t(1) << 30)) return SA_ERR_SHAPE;
+    if (shape->B > 1 && (shape->table_stride < shape->max_pages || shape->chosen_stride < shape->T)) return SA_ERR_SHAPE;
+    if (shape->B == 0) return SA_OK;
+    if (!k_cache || !v_cache || !lens || !chosen || !accepted || (!table && shape->max_pages > 0)) return SA_ERR_NULL;
+    if (!aligned16(k_cache) || !aligned16(v_cache)) return SA_ERR_ALIGN;
+    for (const void* p : {(const void*)table, (const void*)lens, (const void*)chosen, (const void*)accepted, (const void*)lens_after})
+        if (reinterpret_cast<uintptr_t>(p) & 3u) return SA_ERR_ALIGN;
+    sa::AcceptArgs a{};
+    a.k_cache = k_cache; a.v_cache = v_cache; a.table = table; a.lens = lens; a.chosen = chosen; a.accepted = accepted; a.lens_after = lens_after;
+    a.B = shape->B; a.T = shape->T; a.max_pages = shape->max_pages; a.table_stride = shape->table_stride; a.chosen_stride = shape->chosen_stride;
+    set_cache(a, cache);
+    return sa::launch_cache_accept(a, cache->dtype, (hipStream_t)stream) == hipSuccess ? SA_OK : SA_ERR_HIP;
+}
+
+int sa_cache_copy(void* k_cache, void* v_cache, const int32_t* from, const int32_t* to, const int32_t* tokens, int32_t n,
+                  const sa_cache* cache, void* stream) {
+    if (int e = check_cache(cache)) return e;
+    if (n < 0 || n > 1 << 22) return SA_ERR_SHAPE;
+    // (a page's units of 8 bytes are numbered in 31 bits)
+    if ((double)cache->page_size * cache->H_kv * cache->d * (double)elt_size(cache->dtype) >= 17179869184.) return SA_ERR_SHAPE;
+    if (n == 0) return SA_OK;
+    if (!k_cache || !v_cache || !from || !to) return SA_ERR_NULL;
+    if (!aligned16(k_cache) || !aligned16(v_cache)) return SA_ERR_ALIGN;
+    if ((reinterpret_cast<uintptr_t>(from) | reinterpret_cast<uintptr_t>(to) | reinterpret_cast<uintptr_t>(tokens)) & 3u) return SA_ERR_ALIGN;
+    sa::CopyArgs a{};
+    a.k_cache = k_cache; a.v_cache = v_cache; a.from = from; a.to = to; a.tokens = tokens; a.n = n;
+    set_cache(a, cache);
+    return sa::launch_cache_copy(a, cache->dtype, (hipStream_t)stream) == hipSuccess ? SA_OK : SA_ERR_HIP;
 }
 
 int sa_step_mask(int32_t q_dev, int32_t kv_dev, int32_t N, int32_t layout, int32_t* kind, int32_t* off) {

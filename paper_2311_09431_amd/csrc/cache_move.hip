@@ -1,0 +1,149 @@
+// Moving what a paged cache holds: pages, or their first tokens, onto other pages; the accepted tokens of drafts up behind the tokens in front of them.
+//
+// Bound by memory: each byte is read and written once.  Rows are moved in units of 16 bytes where all rows begin at multiples of that, otherwise of 8
+// (a row is a multiple of four elements).
+#include "paged.h"
+
+namespace sa {
+
+namespace {
+
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+template <int BYTES> struct UnitOf { typedef u32x4 Type; };
+template <> struct UnitOf<8> { typedef u32x2 Type; };
+
+constexpr int THREADS = 256, EACH = 4;          // copy: units a thread requests at a time
+
+// sizes and strides in units
+struct Units { int row; int64_t page, slot, head; };
+template <int BYTES, typename Args>
+Units units_of(const Args& a, int es) {
+    return {a.d * es / BYTES, a.stride_page * es / BYTES, a.stride_slot * es / BYTES, a.stride_head * es / BYTES};
+}
+template <typename Args>
+bool in_16_bytes(const Args& a, int es) {
+    return a.d * es % 16 == 0 && a.stride_page * es % 16 == 0 && a.stride_slot * es % 16 == 0 && a.stride_head * es % 16 == 0;
+}
+
+// A workgroup: EACH * THREADS units of a page's keys or values.  A unit's number counts along memory: `inner` units one after the other, then slots or
+// heads (heads_apart: slots first), then the others.
+template <int BYTES>
+__global__ void __launch_bounds__(THREADS)
+cache_copy_kernel(CopyArgs p, Units s, bool heads_apart) {
+    typedef typename UnitOf<BYTES>::Type Unit;
+    const int i = (int)blockIdx.x;
+    const int from = p.from[i], to = p.to[i], tokens = p.tokens ? min(max(p.tokens[i], 0), p.page_size) : p.page_size;
+    if (from < 0 || from >= p.n_pages || to < 0 || to >= p.n_pages || from == to) return;
+    Unit* const cache = (Unit*)(blockIdx.z ? p.v_cache : p.k_cache);
+    const Unit* const src = cache + from * s.page;
+    Unit* const dst = cache + to * s.page;
+    // rows that lie one behind the other are one run
+    const uint32_t runs_inner = heads_apart ? tokens : p.H_kv, outer = heads_apart ? p.H_kv : tokens;
+    const int64_t stride_inner = heads_apart ? s.slot : s.head, stride_outer = heads_apart ? s.head : s.slot;
+    uint32_t run = s.row, inner = runs_inner, n_outer = outer;
+    if (stride_inner == run) {
+        run *= inner;
+        inner = 1;
+        if (stride_outer == run) {
+            run *= n_outer;
+            n_outer = 1;
+        }
+    }
+    const uint32_t all = run * inner * n_outer;
+    for (uint32_t u0 = blockIdx.y * EACH * THREADS; u0 < all; u0 += gridDim.y * EACH * THREADS) {
+        Unit x[EACH];
+        int64_t at[EACH];
+#pragma unroll
+        for (int e = 0; e < EACH; ++e) {
+            uint32_t u = u0 + e * THREADS + threadIdx.x;
+            at[e] = -1;
+            if (u >= all) continue;
+            if (inner * n_outer == 1) at[e] = u;
+            else {
+                const uint32_t r = u / run, o = r / inner;
+                at[e] = (int64_t)o * stride_outer + (int64_t)(r - o * inner) * stride_inner + (u - r * run);
+            }
+            x[e] = src[at[e]];
+        }
+#pragma unroll
+        for (int e = 0; e < EACH; ++e)
+            if (at[e] >= 0) dst[at[e]] = x[e];
+    }
+}
+
+// A workgroup: a sequence.  Its threads take units of the tokens' keys and values, and each moves its unit of BATCH tokens at a time: as the tokens
+// chosen ascend, none of a later batch has been written yet.
+constexpr int BATCH = 8;
+template <int BYTES>
+__global__ void cache_accept_kernel(AcceptArgs p, Units s) {
+    typedef typename UnitOf<BYTES>::Type Unit;
+    const int b = (int)blockIdx.x, room = p.max_pages * p.page_size;
+    const int lens = max(p.lens[b], 0), n = min(max(p.accepted[b], 0), p.T);
+    __syncthreads();            // (all have read the length before it may be written)
+    if (p.lens_after && threadIdx.x == 0) p.lens_after[b] = lens + n;
+    const int32_t* table = p.table + b * p.table_stride;
+    const int32_t* chosen = p.chosen + b * p.chosen_stride;
+    // where a token lies, -1: nowhere
+    auto place = [&](int64_t token) -> int64_t {
+        if (token >= room) return -1;
+        const int page = (int)token / p.page_size, id = table[page];
+        return id < 0 || id >= p.n_pages ? -1 : id * s.page + ((int)token - page * p.page_size) * s.slot;
+    };
+    const int per_cache = p.H_kv * s.row;
+    for (int u = threadIdx.x; u < 2 * per_cache; u += blockDim.x) {
+        Unit* const cache = (Unit*)(u < per_cache ? p.k_cache : p.v_cache);
+        const int in = u < per_cache ? u : u - per_cache, head = in / s.row;
+        Unit* const column = cache + head * s.head + (in - head * s.row);
+        for (int i0 = 0; i0 < n; i0 += BATCH) {
+            Unit x[BATCH];
+            int64_t to[BATCH];
+#pragma unroll
+            for (int i = 0; i < BATCH; ++i) {
+                to[i] = -1;
+                if (i0 + i >= n) continue;
+                const int which = chosen[i0 + i];
+                if (which < 0 || which >= p.T || which == i0 + i) continue;
+                const int64_t from = place((int64_t)lens + which);
+                to[i] = place((int64_t)lens + i0 + i);
+                if (from < 0) to[i] = -1;
+                if (to[i] >= 0) x[i] = column[from];
+            }
+#pragma unroll
+            for (int i = 0; i < BATCH; ++i)
+                if (to[i] >= 0) column[to[i]] = x[i];
+        }
+    }
+}
+
+template <int BYTES>
+hipError_t copy(const CopyArgs& a, int es, hipStream_t st) {
+    const Units s = units_of<BYTES>(a, es);
+    const bool heads_apart = a.stride_head >= a.page_size * a.stride_slot;
+    const int64_t most = (int64_t)a.page_size * a.H_kv * s.row, slices = (most + EACH * THREADS - 1) / (EACH * THREADS);
+    const int64_t most_slices = (1 << 22) / a.n;         // (a launch holds fewer than 2^32 threads; n: up to 2^22)
+    const unsigned y = (unsigned)(slices < most_slices ? slices : most_slices);
+    hipLaunchKernelGGL(cache_copy_kernel<BYTES>, dim3((unsigned)a.n, y, 2), dim3(THREADS), 0, st, a, s, heads_apart);
+    return hipGetLastError();
+}
+template <int BYTES>
+hipError_t accept(const AcceptArgs& a, int es, hipStream_t st) {
+    const Units s = units_of<BYTES>(a, es);
+    const int64_t all = 2ll * a.H_kv * s.row;
+    const unsigned threads = all >= 1024 ? 1024 : (unsigned)((all + 63) / 64 * 64);
+    hipLaunchKernelGGL(cache_accept_kernel<BYTES>, dim3((unsigned)a.B), dim3(threads), 0, st, a, s);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_cache_copy(const CopyArgs& a, int dtype, hipStream_t st) {
+    const int es = dtype == SA_F32 ? 4 : 2;
+    return in_16_bytes(a, es) ? copy<16>(a, es, st) : copy<8>(a, es, st);
+}
+hipError_t launch_cache_accept(const AcceptArgs& a, int dtype, hipStream_t st) {
+    const int es = dtype == SA_F32 ? 4 : 2;
+    return in_16_bytes(a, es) ? accept<16>(a, es, st) : accept<8>(a, es, st);
+}
+
+}  // namespace sa

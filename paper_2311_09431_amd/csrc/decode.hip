@@ -24,7 +24,14 @@
 //
 // What must not be read is not: a 16-token block's descriptor ends with the last cached token, and one whose page number is none
 // has a range of zero; both deliver zeros, and the scores are masked.
+//
+// Under a window (WindowDecodeArgs: a token sees the last `window` cached ones, its own among them, and the first `sinks`) a sequence's chunks are those with
+// tokens that are seen: those of its first tokens, then on from the window's first one.  A 16-token block that holds none is not looked at, nor its
+// page number; in one that holds others too these are masked, and their values taken as zeros.
 #include <hip/hip_bf16.h>
+
+#include <algorithm>
+#include <type_traits>
 
 #include "mfma_tiles.h"
 #include "paged.h"
@@ -74,26 +81,39 @@ __device__ inline void add_sum(float& sum, bool& weightless, float l, float fact
     sum += (l < 0.f ? 0.f : l) * factor;
 }
 __device__ inline int scalar(int x) { return __builtin_amdgcn_readfirstlane(x); }
-template <typename T>
-__device__ inline int chunks_of(const DecodeArgs& p, int b) {
-    const int len = min(max(p.lens[b], 0), p.max_pages * p.page_size);
-    return (len + CHUNK<T> - 1) / CHUNK<T>;
+// A sequence's tokens and chunks; WINDOW: the first token of the window, the chunks in front of it that hold first tokens, and how many behind those are
+// left out.
+struct Tokens { int len, n_chunks, low, firsts, skipped; };
+template <typename T, typename Args>
+__device__ inline Tokens tokens_of(const Args& p, int b) {
+    Tokens x = {min(max(p.lens[b], 0), p.max_pages * p.page_size), 0, 0, 0, 0};
+    x.n_chunks = (x.len + CHUNK<T> - 1) / CHUNK<T>;
+    if constexpr (std::is_same<Args, WindowDecodeArgs>::value) {
+        x.low = max(0, x.len - p.window);
+        const int start = x.low / CHUNK<T>;
+        x.firsts = min(start, (p.sinks + CHUNK<T> - 1) / CHUNK<T>);
+        x.skipped = start - x.firsts;
+        x.n_chunks -= x.skipped;
+    }
+    return x;
 }
+template <typename T, typename Args>
+__device__ inline int chunks_of(const Args& p, int b) { return tokens_of<T>(p, b).n_chunks; }
 // units of a sequence
 __device__ inline int units_of(const DecodeArgs& p) { return p.H_kv * ((p.H / p.H_kv + HEADS - 1) / HEADS); }
 
 // Where chunk number `at` of all units' chunks lies: the sequence, the chunks of the sequences before it (of one unit); and the share of a
 // workgroup.  A wavefront's lanes take the sequences in turn.  (All counts are below 2^31: check_decode.)
 struct Shares { int all, each; };
-template <typename T>
-__device__ inline Shares shares_of(const DecodeArgs& p, int units, int lane) {
+template <typename T, typename Args>
+__device__ inline Shares shares_of(const Args& p, int units, int lane) {
     int n = 0;
     for (int b0 = 0; b0 < p.B; b0 += 64) n += b0 + lane < p.B ? chunks_of<T>(p, b0 + lane) : 0;
     const int all = wave_total(wave_scan(n)) * units;
     return {all, max(1, (int)(((uint32_t)all + (uint32_t)p.n_wgs - 1) / (uint32_t)p.n_wgs))};
 }
-template <typename T>
-__device__ inline void find_chunk(const DecodeArgs& p, int at, int units, int lane, int& seq, int& before) {
+template <typename T, typename Args>
+__device__ inline void find_chunk(const Args& p, int at, int units, int lane, int& seq, int& before) {
     before = 0;
     for (int b0 = 0; b0 < p.B; b0 += 64) {
         const int own = b0 + lane < p.B ? chunks_of<T>(p, b0 + lane) : 0, upto = wave_scan(own);
@@ -114,9 +134,10 @@ __host__ __device__ inline int part_rows(int group) { return group < HEADS ? gro
 __host__ __device__ inline int64_t part_floats(int group, int DP) { return (int64_t)part_rows(group) * (DP + 2); }
 
 // WHOLE: a workgroup has one unit, all of it, and there is nothing to join.
-template <typename T, int DP, bool WHOLE>
+template <typename T, int DP, bool WHOLE, typename Args>
 __global__ void __launch_bounds__(64 * WAVES, DP > 128 ? 1 : 2)
-decode_kernel(DecodeArgs p) {
+decode_kernel(Args p) {
+    constexpr bool WINDOW = std::is_same<Args, WindowDecodeArgs>::value;
     using O = Of<T, DP>;
     constexpr int TILE = O::TILE, CW = O::CW, ES = O::ES, KS = DP / O::STEP, NM = DP / (16 * CW), NB = DP / 16;
     constexpr bool BF16 = ES == 2;
@@ -130,11 +151,19 @@ decode_kernel(DecodeArgs p) {
     const int group = p.H / p.H_kv, blocks = (group + HEADS - 1) / HEADS, units = p.H_kv * blocks, d = p.d;
     int mine, at, end;                          // the share and its chunks
     int b, unit, chunk, n_chunks, len;          // where it begins: sequence, unit of it, chunk of that
-    const int room = p.max_pages * p.page_size;
+    int low = 0, jump_at = 0, jump = 0;         // WINDOW: its first token; the token from which on chunks are left out, and how many tokens these have
     auto enter = [&]() {
-        len = scalar(min(max(p.lens[b], 0), room));
-        n_chunks = (len + CHUNK<T> - 1) / CHUNK<T>;
+        const Tokens x = tokens_of<T>(p, b);
+        len = scalar(x.len);
+        n_chunks = scalar(x.n_chunks);
+        if constexpr (WINDOW) {
+            low = scalar(x.low);
+            jump_at = scalar(x.firsts) * CHUNK<T>;
+            jump = scalar(x.skipped) * CHUNK<T>;
+        }
     };
+    // the first token of a chunk
+    auto token_of = [&](int chunk) { return chunk * CHUNK<T> + (WINDOW && chunk * CHUNK<T> >= jump_at ? jump : 0); };
     if constexpr (WHOLE) {
         mine = (int)blockIdx.x;
         b = mine / units;
@@ -180,7 +209,7 @@ decode_kernel(DecodeArgs p) {
 
     // A piece: the chunks of a unit in this share.  Its first tile's rows and its queries are requested before the piece in front of it is
     // joined and written (`ahead` they are those of the next piece).
-    struct Piece { int b, h0, n_heads, first, last, n_chunks, len; };
+    struct Piece { int b, h0, n_heads, first, last, n_chunks, len, end; };      // end: behind its last chunk
     Piece now;
     u32x4 q[KS], q_ahead[KS];
     int t0;                                     // this wavefront's next tile: tokens t0 .. t0 + TILE - 1, CHUNK<T> further on the one after it
@@ -193,13 +222,27 @@ decode_kernel(DecodeArgs p) {
     uint32_t v[TOKENS][NM][CW * ES / 4];
     int64_t at_k[BLOCKS], at_v[BLOCKS];         // bytes of the blocks in the caches, of the tile requested last / before it
     int rows_k[BLOCKS], rows_v[BLOCKS];         // tokens that may be read (0: none)
+    int hidden_k[BLOCKS], shown_k[BLOCKS];      // WINDOW: from the first to before the second they are not seen
+    auto at_token = [&](int t) {
+#pragma unroll
+        for (int i = 0; i < BLOCKS; ++i) {
+            page[i] = (t + 16 * i) / p.page_size;
+            in_page[i] = t + 16 * i - page[i] * p.page_size;
+        }
+    };
     auto place = [&](int t) {
 #pragma unroll
         for (int i = 0; i < BLOCKS; ++i) {
             const int token = t + 16 * i;
             rows_k[i] = 0;
             at_k[i] = 0;
-            if (token < len) {
+            bool looked_at = token < len;
+            if constexpr (WINDOW) {
+                hidden_k[i] = max(0, p.sinks - token);
+                shown_k[i] = min(16, low - token);
+                looked_at = looked_at && (token < p.sinks || token + 16 > low);
+            }
+            if (looked_at) {
                 const int id = scalar(table[page[i]]);
                 if (id >= 0 && id < p.n_pages) {
                     rows_k[i] = min(16, len - token);
@@ -257,7 +300,8 @@ decode_kernel(DecodeArgs p) {
     auto request = [&]() {
         const int kvh = unit / blocks, h0 = kvh * group + (unit - kvh * blocks) * HEADS;
         const int n_heads = min(HEADS, (kvh + 1) * group - h0);
-        const Piece next = {b, h0, n_heads, chunk, min(n_chunks, chunk + (end - at)), n_chunks, len};
+        Piece next = {b, h0, n_heads, chunk, min(n_chunks, chunk + (end - at)), n_chunks, len, 0};
+        next.end = WINDOW ? token_of(next.last - 1) + CHUNK<T> : next.last * CHUNK<T>;
         const bool has_head = n < n_heads;
         const T* q_row = (const T*)p.q + b * p.stride_b + (h0 + (has_head ? n : 0)) * p.stride_h;
 #pragma unroll
@@ -274,15 +318,11 @@ decode_kernel(DecodeArgs p) {
                 }
             }
         }
-        t0 = next.first * CHUNK<T> + wave * TILE;
-#pragma unroll
-        for (int i = 0; i < BLOCKS; ++i) {
-            page[i] = (t0 + 16 * i) / p.page_size;
-            in_page[i] = t0 + 16 * i - page[i] * p.page_size;
-        }
+        t0 = token_of(next.first) + wave * TILE;
+        at_token(t0);
         table = p.table + b * p.table_stride;
         head_at = (int64_t)kvh * p.stride_head;
-        if (t0 < min(len, next.last * CHUNK<T>)) {
+        if (t0 < min(len, next.end)) {
             place(t0);
             load_k();
             keep_place();
@@ -294,13 +334,19 @@ decode_kernel(DecodeArgs p) {
     for (;;) {
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) q[ks] = q_ahead[ks];
-        const int t_end = min(now.len, now.last * CHUNK<T>);
+        const int t_end = min(now.len, now.end);
         f32x4 acc[NB];
 #pragma unroll
         for (int i = 0; i < NB; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
         float m = -INFINITY, l = 0.f;
         bool seen = false;                      // some token of a page that is one
-        for (; t0 < t_end; t0 += CHUNK<T>) {
+        for (int t_next; t0 < t_end; t0 = t_next) {
+            t_next = t0 + CHUNK<T>;
+            bool jumped = false;
+            if constexpr (WINDOW) {
+                jumped = jump > 0 && t0 < jump_at && t_next >= jump_at;
+                if (jumped) t_next += jump;
+            }
             f32x4 s[BLOCKS];
 #pragma unroll
             for (int i = 0; i < BLOCKS; ++i) {
@@ -320,18 +366,24 @@ decode_kernel(DecodeArgs p) {
                     }
                 }
             }
-            int rows[BLOCKS];
-            bool whole = true;
+            int rows[BLOCKS], hidden[BLOCKS], shown[BLOCKS];
+            bool whole = true, edge = false;
 #pragma unroll
             for (int i = 0; i < BLOCKS; ++i) {
                 rows[i] = rows_k[i];
+                if constexpr (WINDOW) {
+                    hidden[i] = hidden_k[i];
+                    shown[i] = shown_k[i];
+                    edge = edge || hidden[i] < shown[i];
+                }
                 whole = whole && rows[i] == 16;
                 seen = seen || rows[i] > 0;
             }
             // the next tile's K rows (behind the last one: nothing, t0 is beyond the unit's tokens here)
-            const bool more = t0 + CHUNK<T> < t_end;
+            const bool more = t_next < t_end;
             if (more) {
-                place(t0 + CHUNK<T>);
+                if (WINDOW && jumped) at_token(t_next);
+                place(t_next);
                 load_k();
             }
             if (!whole) {
@@ -340,6 +392,19 @@ decode_kernel(DecodeArgs p) {
 #pragma unroll
                     for (int r = 0; r < 4; ++r)
                         if (4 * j + r >= rows[i]) s[i][r] = -INFINITY;
+            }
+            if (WINDOW && edge) {
+#pragma unroll
+                for (int i = 0; i < BLOCKS; ++i)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        if (4 * j + r >= hidden[i] && 4 * j + r < shown[i]) {
+                            s[i][r] = -INFINITY;
+#pragma unroll
+                            for (int x = 0; x < NM; ++x)
+#pragma unroll
+                                for (int c = 0; c < CW * ES / 4; ++c) v[4 * i + r][x][c] = 0;
+                        }
             }
             float pr[TOKENS], sum = 0.f;
 #pragma unroll
@@ -483,9 +548,9 @@ decode_kernel(DecodeArgs p) {
 // Units whose pieces lie in several shares, and sequences without a token.  JOIN_WAVES wavefronts take the pieces of a (sequence, query head) in
 // turn; a workgroup has eight wavefronts or, where one is enough for a head, four, of which each has a head of its own.
 constexpr int BATCH = 4;
-template <typename T, int DP, int JOIN_WAVES>
+template <typename T, int DP, int JOIN_WAVES, typename Args>
 __global__ void __launch_bounds__(JOIN_WAVES == 1 ? 256 : 64 * JOIN_WAVES)
-decode_join_kernel(DecodeArgs p) {
+decode_join_kernel(Args p) {
     constexpr int COLS = (DP + 63) / 64, EACH = JOIN_WAVES == 1 ? 4 : 1;
     __shared__ float o_lds[JOIN_WAVES][DP], m_lds[JOIN_WAVES], l_lds[JOIN_WAVES];
     const int lane = threadIdx.x & 63, own_wave = scalar((int)threadIdx.x >> 6), wave = EACH == 1 ? own_wave : 0;
@@ -582,29 +647,32 @@ constexpr int columns(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : d <= 128 ? 1
 // unit: d 128 204, 208, 226, 208, 128 of up to 1000 72, 65, 73, 67, d 64 132, 117, 114, 122, d 32 (32 of up to 16384, 16 heads) 218, 192, 177, 179.
 constexpr int workgroups(int DP) { return N_CU * (DP <= 32 ? 3 : 2); }
 
-template <typename T, int DP>
-hipError_t launch(DecodeArgs a, hipStream_t st) {
+template <typename T, int DP, typename Args>
+hipError_t launch(Args a, hipStream_t st) {
     // Where no sequence can have more than eight rounds (above 128 columns four), a unit to a workgroup and nothing to join, whatever the lengths
     // are.  us, shares : units, 32 heads on 8, d 128, tables of up to 250 tokens, 16 sequences 13.6 : 11.0, 128 24.4 : 15.6, 500 38 : 30, 1000
     // 61 : 58, 16 of 1000 16.5 : 13.9, but one of 1500 13.8 : 17.0, 64 of 2000 58 : 63; d 256, 8 heads on 2, 16 of 250 13.9 : 11.0, but 1000 13.9 : 23;
     // fp32, 16 of 500 18.8 : 17.1, but 1000 22.6 : 29.  (11 us of these are the calls'.)
-    if ((int64_t)a.max_pages * a.page_size <= (DP > 128 ? 4 : 8) * CHUNK<T>) {
+    int64_t most = (int64_t)a.max_pages * a.page_size;
+    if constexpr (std::is_same<Args, WindowDecodeArgs>::value)          // of the chunks with first tokens, and those that the window lies in
+        most = std::min<int64_t>(most, ((a.sinks + CHUNK<T> - 1ll) / CHUNK<T> + (a.window + CHUNK<T> - 2ll) / CHUNK<T> + 1) * CHUNK<T>);
+    if (most <= (DP > 128 ? 4 : 8) * CHUNK<T>) {
         const int group = a.H / a.H_kv;
-        hipLaunchKernelGGL((decode_kernel<T, DP, true>), dim3((unsigned)(a.B * a.H_kv * ((group + HEADS - 1) / HEADS))), dim3(64 * WAVES), 0, st, a);
+        hipLaunchKernelGGL((decode_kernel<T, DP, true, Args>), dim3((unsigned)(a.B * a.H_kv * ((group + HEADS - 1) / HEADS))), dim3(64 * WAVES), 0, st, a);
         return hipGetLastError();
     }
     a.n_wgs = workgroups(DP);
-    hipLaunchKernelGGL((decode_kernel<T, DP, false>), dim3((unsigned)a.n_wgs), dim3(64 * WAVES), 0, st, a);
+    hipLaunchKernelGGL((decode_kernel<T, DP, false, Args>), dim3((unsigned)a.n_wgs), dim3(64 * WAVES), 0, st, a);
     if (hipError_t e = hipGetLastError()) return e;
     // Eight wavefronts a head where there are few heads, whose units then have many pieces, us, one : eight, 32 heads on 8: a sequence of
     // 8000 tokens 25.0 : 14.9, of 65536 69 : 57, 4 of up to 100000 174 : 169, 16 of up to 4000 37.1 : 37.4; 32 of up to 2000 30.7 : 32.3, 128 of up to
     // 1100 73 : 83.
-    if ((int64_t)a.B * a.H <= 512) hipLaunchKernelGGL((decode_join_kernel<T, DP, 8>), dim3((unsigned)a.B * a.H), dim3(64 * 8), 0, st, a);
-    else hipLaunchKernelGGL((decode_join_kernel<T, DP, 1>), dim3(((unsigned)(a.B * a.H) + 3) / 4), dim3(64 * 4), 0, st, a);
+    if ((int64_t)a.B * a.H <= 512) hipLaunchKernelGGL((decode_join_kernel<T, DP, 8, Args>), dim3((unsigned)a.B * a.H), dim3(64 * 8), 0, st, a);
+    else hipLaunchKernelGGL((decode_join_kernel<T, DP, 1, Args>), dim3(((unsigned)(a.B * a.H) + 3) / 4), dim3(64 * 4), 0, st, a);
     return hipGetLastError();
 }
-template <typename T>
-hipError_t launch(const DecodeArgs& a, hipStream_t st) {
+template <typename T, typename Args>
+hipError_t launch(const Args& a, hipStream_t st) {
     switch (columns(a.d)) {
         case 32: return launch<T, 32>(a, st);
         case 64: return launch<T, 64>(a, st);
@@ -621,6 +689,9 @@ int64_t decode_workspace(int H, int H_kv, int d) {
 }
 
 hipError_t launch_decode(const DecodeArgs& a, int dtype, hipStream_t st) {
+    return dtype == SA_F32 ? launch<float>(a, st) : launch<__hip_bfloat16>(a, st);
+}
+hipError_t launch_window_decode(const WindowDecodeArgs& a, int dtype, hipStream_t st) {
     return dtype == SA_F32 ? launch<float>(a, st) : launch<__hip_bfloat16>(a, st);
 }
 

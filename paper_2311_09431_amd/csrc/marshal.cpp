@@ -423,34 +423,154 @@ ENTRY(decode_workspace) {
         return PyLong_FromLongLong(f(&s, &cache));
     });
 }
-// (function address, q, k_cache, v_cache, table, lens, out, lse, workspace, scale, device, stream)
-ENTRY(decode) {
-    return guarded(n, 12, [&] {
-        const auto f = reinterpret_cast<decltype(&sa_attn_decode)>(address(a[0]));
-        const Call on(a[10]);
-        const at::Tensor &q = on(a[1]), &kc = on(a[2]), &vc = on(a[3]), &table = on(a[4]), &lens = on.ids(a[5], "lens must be a contiguous int32 tensor"),
-                         &out = on(a[6]), &work = on(a[8]);
+const char* const CACHES = "the caches must have the same shape, type and strides";
+const char* const LENS = "lens must be a contiguous int32 tensor";
+// page numbers of n sequences
+void table_of(const at::Tensor& table, int64_t n, int32_t& max_pages, int64_t& stride) {
+    if (table.scalar_type() != at::kInt || table.dim() != 2 || table.size(0) != n || (table.size(1) > 1 && table.stride(1) != 1))
+        refuse(PyExc_ValueError, "table must be int32 [sequences, pages], pages contiguous");
+    max_pages = size(table, 1);
+    stride = n > 1 ? table.stride(0) : max_pages;
+}
+// one number for each of n
+void numbers(const at::Tensor& t, int64_t n, const char* why) {
+    if (t.dim() != 1 || t.size(0) != n) refuse(PyExc_ValueError, why);
+}
+int64_t bytes_of(const at::Tensor& work) {
+    if (!work.is_contiguous()) refuse(PyExc_ValueError, "workspace must be contiguous");
+    return work.numel() * work.element_size();
+}
+// (function address, q, k_cache, v_cache, table, lens, out, lse, workspace, scale, device, stream; with a window, window and sinks before scale)
+template <bool WINDOW>
+PyObject* decode_call(PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, WINDOW ? 14 : 12, [&] {
+        PyObject* const* z = a + (WINDOW ? 11 : 9);         // scale, device, stream
+        const Call on(z[1]);
+        const at::Tensor &q = on(a[1]), &kc = on(a[2]), &vc = on(a[3]), &table = on(a[4]), &lens = on.ids(a[5], LENS), &out = on(a[6]), &work = on(a[8]);
         const at::Tensor* lse = maybe(on, a[7]);
-        same(vc, kc, "the caches must have the same shape, type and strides");
+        same(vc, kc, CACHES);
         same(out, q, "out must have q's shape, type and strides");
         const sa_cache cache = cache_of(kc);
         sa_decode s = decode_of(q, cache);
-        if (table.scalar_type() != at::kInt || table.dim() != 2 || table.size(0) != q.size(0) || (table.size(1) > 1 && table.stride(1) != 1))
-            refuse(PyExc_ValueError, "table must be int32 [sequences, pages], pages contiguous");
-        if (lens.dim() != 1 || lens.size(0) != q.size(0)) refuse(PyExc_ValueError, "lens must hold one number a sequence");
+        table_of(table, q.size(0), s.max_pages, s.table_stride);
+        numbers(lens, q.size(0), "lens must hold one number a sequence");
         if (lse) {
             statistics(*lse, q.size(0), q.size(1), "lse must be float32 [sequences, heads], heads contiguous");
             if (q.size(0) > 1) s.stat_stride_b = lse->stride(0);
         }
-        if (!work.is_contiguous()) refuse(PyExc_ValueError, "workspace must be contiguous");
-        s.max_pages = size(table, 1);
-        s.table_stride = q.size(0) > 1 ? table.stride(0) : s.max_pages;
-        s.softmax_scale = real(a[9]);
-        void* st = stream(a[11]);
-        const int64_t bytes = work.numel() * work.element_size();
+        const int64_t bytes = bytes_of(work);
+        s.softmax_scale = real(z[0]);
+        sa_window w = {0, 0};
+        if (WINDOW) w = {int32(a[9]), int32(a[10])};
+        void* st = stream(z[2]);
         return run([&] {
-            return f(at_of(q), at_of(kc), at_of(vc), (const int32_t*)at_of(table), (const int32_t*)at_of(lens), at_of(out), (float*)at_of(lse), at_of(work),
-                     bytes, &s, &cache, st);
+            if constexpr (WINDOW)
+                return reinterpret_cast<decltype(&sa_attn_window_decode)>(address(a[0]))(
+                    at_of(q), at_of(kc), at_of(vc), (const int32_t*)at_of(table), (const int32_t*)at_of(lens), at_of(out), (float*)at_of(lse), at_of(work),
+                    bytes, &s, &cache, &w, st);
+            else
+                return reinterpret_cast<decltype(&sa_attn_decode)>(address(a[0]))(
+                    at_of(q), at_of(kc), at_of(vc), (const int32_t*)at_of(table), (const int32_t*)at_of(lens), at_of(out), (float*)at_of(lse), at_of(work),
+                    bytes, &s, &cache, st);
+        });
+    });
+}
+ENTRY(decode) { return decode_call<false>(a, n); }
+ENTRY(window_decode) { return decode_call<true>(a, n); }
+// q [sequences, drafted tokens, heads, d]
+sa_tree tree_of(const at::Tensor& q, const sa_cache& cache) {
+    if (q.dim() != 4) refuse(PyExc_ValueError, "expected [sequences, drafted tokens, heads, d]");
+    if (q.size(3) > 1 && q.stride(3) != 1) refuse(PyExc_ValueError, "the head dimension must be contiguous");
+    if (q.size(3) != cache.d || type_of(q) != cache.dtype) refuse(PyExc_ValueError, "q must have the cache's head dimension and type");
+    // (of a single sequence, token or head whatever fits)
+    const int64_t h = q.size(2) == 1 ? q.size(3) : q.stride(2), t = q.size(1) <= 1 ? h * q.size(2) : q.stride(1), b = q.size(0) <= 1 ? t * q.size(1) : q.stride(0);
+    return {size(q, 0), size(q, 1), size(q, 2), 0, b, t, h, q.size(1) * q.size(2), q.size(2), 0, q.size(1), 0.f};
+}
+// (function address, q, k_cache): bytes
+ENTRY(tree_workspace) {
+    return guarded(n, 3, [&] {
+        const auto f = reinterpret_cast<decltype(&sa_attn_tree_workspace)>(address(a[0]));
+        const sa_cache cache = cache_of(tensor(a[2]));
+        const sa_tree s = tree_of(tensor(a[1]), cache);
+        return PyLong_FromLongLong(f(&s, &cache));
+    });
+}
+// (function address, q, k_cache, v_cache, table, lens, drafts, seen, out, lse, workspace, scale, device, stream)
+ENTRY(tree) {
+    return guarded(n, 14, [&] {
+        const auto f = reinterpret_cast<decltype(&sa_attn_tree)>(address(a[0]));
+        const Call on(a[12]);
+        const at::Tensor &q = on(a[1]), &kc = on(a[2]), &vc = on(a[3]), &table = on(a[4]), &lens = on.ids(a[5], LENS), &seen = on(a[7]), &out = on(a[8]),
+                         &work = on(a[10]);
+        const at::Tensor* drafts = a[6] == Py_None ? nullptr : &on.ids(a[6], "drafts must be a contiguous int32 tensor");
+        const at::Tensor* lse = maybe(on, a[9]);
+        same(vc, kc, CACHES);
+        same(out, q, "out must have q's shape, type and strides");
+        const sa_cache cache = cache_of(kc);
+        sa_tree s = tree_of(q, cache);
+        const int64_t B = q.size(0), T = q.size(1), H = q.size(2);
+        table_of(table, B, s.max_pages, s.table_stride);
+        numbers(lens, B, "lens must hold one number a sequence");
+        if (drafts) numbers(*drafts, B, "drafts must hold one number a sequence");
+        if (seen.scalar_type() != at::kLong || seen.dim() != 2 || seen.size(0) != B || seen.size(1) != T || (T > 1 && seen.stride(1) != 1))
+            refuse(PyExc_ValueError, "seen must be int64 [sequences, drafted tokens], tokens contiguous");
+        if (B > 1) s.seen_stride = seen.stride(0);
+        if (lse) {
+            if (lse->scalar_type() != at::kFloat || lse->dim() != 3 || lse->size(0) != B || lse->size(1) != T || lse->size(2) != H || (H > 1 && lse->stride(2) != 1))
+                refuse(PyExc_ValueError, "lse must be float32 [sequences, drafted tokens, heads], heads contiguous");
+            if (T > 1) s.stat_stride_t = lse->stride(1);
+            s.stat_stride_b = B > 1 ? lse->stride(0) : T * s.stat_stride_t;
+        }
+        const int64_t bytes = bytes_of(work);
+        s.softmax_scale = real(a[11]);
+        void* st = stream(a[13]);
+        return run([&] {
+            return f(at_of(q), at_of(kc), at_of(vc), (const int32_t*)at_of(table), (const int32_t*)at_of(lens), (const int32_t*)at_of(drafts),
+                     (const int64_t*)at_of(seen), at_of(out), (float*)at_of(lse), at_of(work), bytes, &s, &cache, st);
+        });
+    });
+}
+// (function address, k_cache, v_cache, table, lens, chosen, accepted, lens_after, device, stream)
+ENTRY(accept) {
+    return guarded(n, 10, [&] {
+        const auto f = reinterpret_cast<decltype(&sa_cache_accept)>(address(a[0]));
+        const Call on(a[8]);
+        const at::Tensor &kc = on(a[1]), &vc = on(a[2]), &table = on(a[3]), &lens = on.ids(a[4], LENS), &chosen = on(a[5]),
+                         &accepted = on.ids(a[6], "accepted must be a contiguous int32 tensor");
+        const at::Tensor* after = a[7] == Py_None ? nullptr : &on.ids(a[7], "lens_after must be a contiguous int32 tensor");
+        same(vc, kc, CACHES);
+        const sa_cache cache = cache_of(kc);
+        const int64_t B = lens.dim() == 1 ? lens.size(0) : -1;
+        numbers(lens, B, "lens must hold one number a sequence");
+        numbers(accepted, B, "accepted must hold one number a sequence");
+        if (after) numbers(*after, B, "lens_after must hold one number a sequence");
+        if (chosen.scalar_type() != at::kInt || chosen.dim() != 2 || chosen.size(0) != B || (chosen.size(1) > 1 && chosen.stride(1) != 1))
+            refuse(PyExc_ValueError, "chosen must be int32 [sequences, drafted tokens], tokens contiguous");
+        sa_accept s = {size(lens, 0), size(chosen, 1), 0, 0, B > 1 ? chosen.stride(0) : chosen.size(1)};
+        table_of(table, B, s.max_pages, s.table_stride);
+        void* st = stream(a[9]);
+        return run([&] {
+            return f(at_of(kc), at_of(vc), (const int32_t*)at_of(table), (const int32_t*)at_of(lens), (const int32_t*)at_of(chosen),
+                     (const int32_t*)at_of(accepted), (int32_t*)at_of(after), &s, &cache, st);
+        });
+    });
+}
+// (function address, k_cache, v_cache, from, to, tokens, device, stream)
+ENTRY(copy) {
+    return guarded(n, 8, [&] {
+        const auto f = reinterpret_cast<decltype(&sa_cache_copy)>(address(a[0]));
+        const Call on(a[6]);
+        const at::Tensor &kc = on(a[1]), &vc = on(a[2]), &from = on.ids(a[3], "src must be a contiguous int32 tensor"),
+                         &to = on.ids(a[4], "dst must be a contiguous int32 tensor");
+        const at::Tensor* tokens = a[5] == Py_None ? nullptr : &on.ids(a[5], "tokens must be a contiguous int32 tensor");
+        same(vc, kc, CACHES);
+        const sa_cache cache = cache_of(kc);
+        numbers(to, from.dim() == 1 ? from.size(0) : -1, "src and dst must hold as many page numbers");
+        if (tokens) numbers(*tokens, from.size(0), "tokens must hold one number a page");
+        const int32_t pages = size(from, 0);
+        void* st = stream(a[7]);
+        return run([&] {
+            return f(at_of(kc), at_of(vc), (const int32_t*)at_of(from), (const int32_t*)at_of(to), (const int32_t*)at_of(tokens), pages, &cache, st);
         });
     });
 }
@@ -471,7 +591,7 @@ ENTRY(set_up) {
 
 #define FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(two), FAST(three), FAST(step_fwd), FAST(step_bwd), FAST(ring_fwd), FAST(ring_bwd), FAST(rope),
-                         FAST(permute), FAST(packed_fwd), FAST(packed_bwd), FAST(window_fwd), FAST(window_bwd), FAST(window_bwd_workspace), FAST(append), FAST(decode), FAST(decode_workspace),
+                         FAST(permute), FAST(packed_fwd), FAST(packed_bwd), FAST(window_fwd), FAST(window_bwd), FAST(window_bwd_workspace), FAST(append), FAST(decode), FAST(decode_workspace), FAST(window_decode), FAST(tree), FAST(tree_workspace), FAST(accept), FAST(copy),
                          FAST(extent_of), FAST(set_up), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -1,0 +1,732 @@
+// Attention of drafted tokens over the paged cache: each of a sequence's drafted tokens over all tokens in front of the draft and those of the draft that
+// its mask names.
+//
+// As decode.hip has it for one token, with the rows of a unit, its matrix products' right side, more than one block of 16: a unit is (sequence, key/value
+// head, 16 M of the sequence's rows), row i G + g being drafted token i and query head g of the group of G.  Tiles of tokens are loaded once for
+// all M blocks; units that share a key/value head are neighbours, so that what one reads of the cache lies near for the other.  Shares of
+// chunks, the four wavefronts' own references and sums and the joining of pieces are as there.
+//
+// What a row does not see has a score of -inf.  Its weight of zero would still make a NaN of an infinite or NaN value, so such tokens are taken out of the
+// products (`odd_values`) and added to the rows that see them by vector instructions; only tiles with drafted tokens are looked at for them.
+#include <hip/hip_bf16.h>
+
+#include "mfma_tiles.h"
+#include "paged.h"
+#include "wave.h"
+
+namespace sa {
+
+namespace {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int WAVES = 4;                        // wavefronts a workgroup
+constexpr float MOST = 16777216.f;              // 2^24: a lane's sum of a tile against a reference that stays
+
+// Of a storage type and DP columns computed: tokens a tile, columns of a product over them, columns of a V row a lane loads at once
+template <typename T, int DP> struct Of;
+template <int DP> struct Of<__hip_bfloat16, DP> {
+    static constexpr int TILE = 32, STEP = 32, CW = DP >= 128 ? 8 : DP / 16, ES = 2;
+};
+template <int DP> struct Of<float, DP> {
+    static constexpr int TILE = 16, STEP = 16, CW = DP >= 64 ? 4 : DP / 16, ES = 4;
+};
+template <typename T> constexpr int CHUNK = WAVES * Of<T, 64>::TILE;
+
+__device__ inline f32x4 mfma_bf16(u32x4 a, u32x4 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+__device__ inline f32x4 mfma_f32(uint32_t a, uint32_t b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a), __uint_as_float(b), c, 0, 0, 0);
+}
+// over the four lanes that hold a row
+__device__ inline float quad_max(float x) {
+    x = fmaxf(x, __shfl_xor(x, 16));
+    return fmaxf(x, __shfl_xor(x, 32));
+}
+__device__ inline float quad_sum(float x) {
+    x += __shfl_xor(x, 16);
+    return x + __shfl_xor(x, 32);
+}
+// Parts are joined against the largest reference, of parts without a token (or any weight) 0.  A row sum of -1 says that the row saw tokens, all
+// without weight (scores of -inf): nothing beside other parts, no number if there are none.
+__device__ inline float reference(float top) { return top == -INFINITY ? 0.f : top; }
+__device__ inline void add_sum(float& sum, bool& weightless, float l, float factor) {
+    weightless = weightless || l < 0.f;
+    sum += (l < 0.f ? 0.f : l) * factor;
+}
+__device__ inline int scalar(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
+// a sequence: tokens in front of its draft, all, rows
+struct Sequence { int before, len, rows; };
+__device__ inline Sequence sequence(const TreeArgs& p, int b) {
+    const int room = p.max_pages * p.page_size, drafted = p.drafts ? min(max(p.drafts[b], 0), p.T) : p.T;
+    const int before = min(max(p.lens[b], 0), room);
+    return {before, min(before + drafted, room), drafted * (p.H / p.H_kv)};
+}
+// its chunks, and its units
+template <typename T> __device__ inline int chunks_of(const Sequence& x) { return (x.len + CHUNK<T> - 1) / CHUNK<T>; }
+template <int ROWS> __device__ inline int units_of(const TreeArgs& p, const Sequence& x) { return p.H_kv * ((x.rows + ROWS - 1) / ROWS); }
+// the chunks of all its units
+template <typename T, int ROWS>
+__device__ inline int work_of(const TreeArgs& p, int b) {
+    const Sequence x = sequence(p, b);
+    return chunks_of<T>(x) * units_of<ROWS>(p, x);
+}
+
+// Where chunk number `at` of all units' chunks lies: the sequence, the chunks before it; and the share of a workgroup.  A wavefront's lanes take the
+// sequences in turn.  (All counts are below 2^31: check_tree.)
+__device__ inline int share_of(int all, int n_wgs) { return max(1, (int)(((uint32_t)all + (uint32_t)n_wgs - 1) / (uint32_t)n_wgs)); }
+template <typename T, int ROWS>
+__device__ inline int all_work(const TreeArgs& p, int lane) {
+    int n = 0;
+    for (int b0 = 0; b0 < p.B; b0 += 64) n += b0 + lane < p.B ? work_of<T, ROWS>(p, b0 + lane) : 0;
+    return wave_total(wave_scan(n));
+}
+template <typename T, int ROWS>
+__device__ inline void find_chunk(const TreeArgs& p, int at, int lane, int& seq, int& before) {
+    before = 0;
+    for (int b0 = 0; b0 < p.B; b0 += 64) {
+        const int own = b0 + lane < p.B ? work_of<T, ROWS>(p, b0 + lane) : 0, upto = wave_scan(own);
+        const uint64_t past = __builtin_amdgcn_ballot_w64(before + upto > at);
+        if (past) {
+            const int l = (int)__builtin_ctzll(past);
+            before += __builtin_amdgcn_readlane(upto - own, l);
+            seq = b0 + l;
+            return;
+        }
+        before += wave_total(upto);
+    }
+    seq = p.B;              // (not reached: `at` is one of them)
+}
+
+// A unit's piece in the workspace: its rows of DP columns, then references and row sums.
+__host__ __device__ inline int64_t part_floats(int rows, int DP) { return (int64_t)rows * (DP + 2); }
+
+// an infinite or NaN element of a dword
+template <int ES> __device__ inline bool odd_word(uint32_t w) {
+    return (w & 0x7f800000u) == 0x7f800000u || (ES == 2 && (w & 0x7f80u) == 0x7f80u);
+}
+template <int ES> __device__ inline float element(const uint32_t* words, int i) {
+    return __uint_as_float(ES == 4 ? words[i] : i % 2 ? words[i / 2] & 0xffff0000u : words[i / 2] << 16);
+}
+
+constexpr int waves_per_simd(int DP, int M) { return DP > 128 || M > 2 ? 1 : 2; }
+
+// WHOLE: a workgroup has one unit, all of it, and there is nothing to join.
+template <typename T, int DP, int M, bool WHOLE>
+__global__ void __launch_bounds__(64 * WAVES, waves_per_simd(DP, M))
+tree_kernel(TreeArgs p) {
+    using O = Of<T, DP>;
+    constexpr int TILE = O::TILE, CW = O::CW, ES = O::ES, KS = DP / O::STEP, NM = DP / (16 * CW), NB = DP / 16;
+    constexpr bool BF16 = ES == 2;
+    constexpr int BLOCKS = TILE / 16, TOKENS = 4 * BLOCKS;      // 16-token blocks of a tile, tokens a lane holds of it
+    constexpr int PITCH = DP + 4, ROWS = 16 * M;
+    __shared__ __attribute__((aligned(16))) float o_lds[WAVES][ROWS][PITCH];
+    __shared__ float m_lds[WAVES][ROWS], l_lds[WAVES][ROWS];
+
+    const int lane = threadIdx.x & 63, n = lane & 15, j = lane >> 4;
+    const int wave = scalar((int)threadIdx.x >> 6);
+    const int group = p.H / p.H_kv, d = p.d;
+    int mine, at, end;                          // the share and its chunks
+    int b, unit, chunk, n_chunks, units;        // where it begins: sequence, unit of it, chunk of that; the sequence's
+    Sequence seq;
+    auto enter = [&]() {
+        seq = sequence(p, b);
+        seq = {scalar(seq.before), scalar(seq.len), scalar(seq.rows)};
+        n_chunks = chunks_of<T>(seq);
+        units = units_of<ROWS>(p, seq);
+    };
+    if constexpr (WHOLE) {
+        mine = (int)blockIdx.x;
+        const int most = p.H_kv * ((p.T * group + ROWS - 1) / ROWS);
+        b = mine / most;
+        unit = mine - b * most;
+        enter();
+        if (unit >= units) return;
+        chunk = at = 0;
+        end = n_chunks;
+    } else {
+        // neighbouring shares, which often read the same rows for other ones, on one XCD: consecutive workgroups go round-robin to the 8
+        const int all = all_work<T, ROWS>(p, lane), each = share_of(all, p.n_wgs);
+        const int n_shares = (int)(((uint32_t)all + (uint32_t)each - 1) / (uint32_t)each), per_xcd = (n_shares + 7) / 8;
+        if ((int)blockIdx.x / 8 >= per_xcd) return;
+        mine = (int)blockIdx.x % 8 * per_xcd + (int)blockIdx.x / 8;
+        if (mine >= n_shares) return;
+        at = mine * each;
+        end = at + min(each, all - at);
+        // (a sequence's chunks, unit by unit, follow those of all sequences before it)
+        int before;
+        find_chunk<T, ROWS>(p, at, lane, b, before);
+        enter();
+        const int in = at - before;
+        unit = (int)((uint32_t)in / (uint32_t)n_chunks);
+        chunk = in - unit * n_chunks;
+    }
+    const float kappa = p.scale * LOG2E;
+    const int pitch = (int)p.stride_slot * ES;              // bytes between tokens of a page
+    // this lane's bytes of a K block (token n, its columns of each product) and of a V block (token 4 j + r, its columns)
+    uint32_t k_at[KS], v_at[4][NM];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+        const int col = O::STEP * ks + (BF16 ? 8 : 4) * j;
+        k_at[ks] = col < d ? n * pitch + col * ES : DT_OUT_OF_RANGE;
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int m = 0; m < NM; ++m) {
+            const int col = 16 * CW * m + CW * n;
+            v_at[r][m] = col < d ? (4 * j + r) * pitch + col * ES : DT_OUT_OF_RANGE;
+        }
+    // bf16, d % 8 == 4: the chunk that holds column d has four elements of whatever follows the row
+    const int part_ks = BF16 && d % 8 && ((d >> 3) & 3) == j ? d >> 5 : -1;
+
+    // A piece: the chunks of a unit in this share.  Its first tile's rows and its queries are requested before the piece in front of it is
+    // joined and written.
+    struct Piece { int b, kvh, row0, rows, first, last, n_chunks, before, len; };
+    Piece now;
+    u32x4 q[M][KS];
+    uint64_t sees[M];                           // the row's mask
+    int t0;                                     // this wavefront's next tile: tokens t0 .. t0 + TILE - 1, CHUNK<T> further on the one after it
+    // page and place in it of each of its 16-token blocks
+    const int step_page = CHUNK<T> / p.page_size, step_in = CHUNK<T> - step_page * p.page_size;
+    int page[BLOCKS], in_page[BLOCKS];
+    const int32_t* table;
+    int64_t head_at;
+    u32x4 k[BLOCKS][KS];
+    uint32_t v[TOKENS][NM][CW * ES / 4];
+    int64_t at_k[BLOCKS], at_v[BLOCKS];         // bytes of the blocks in the caches, of the tile requested last / before it
+    int rows_k[BLOCKS], rows_v[BLOCKS];         // tokens that may be read (0: none)
+    auto place = [&](int t) {
+#pragma unroll
+        for (int i = 0; i < BLOCKS; ++i) {
+            const int token = t + 16 * i;
+            rows_k[i] = 0;
+            at_k[i] = 0;
+            if (token < seq.len) {
+                const int id = scalar(table[page[i]]);
+                if (id >= 0 && id < p.n_pages) {
+                    rows_k[i] = min(16, seq.len - token);
+                    at_k[i] = (id * p.stride_page + in_page[i] * p.stride_slot + head_at) * ES;
+                }
+            }
+            page[i] += step_page;
+            in_page[i] += step_in;
+            if (in_page[i] >= p.page_size) {
+                in_page[i] -= p.page_size;
+                ++page[i];
+            }
+        }
+    };
+    auto rsrc = [&](const void* cache, int64_t bytes, int rows) {
+        return __builtin_amdgcn_make_buffer_rsrc((void*)((const char*)cache + bytes), 0, rows ? (rows - 1) * pitch + ES * d : 0, 0x00020000);
+    };
+    auto load_k = [&]() {
+#pragma unroll
+        for (int i = 0; i < BLOCKS; ++i) {
+            const auto s = rsrc(p.k_cache, at_k[i], rows_k[i]);
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) k[i][ks] = __builtin_amdgcn_raw_buffer_load_b128(s, k_at[ks], 0, 0);
+        }
+    };
+    auto load_v = [&]() {
+#pragma unroll
+        for (int i = 0; i < BLOCKS; ++i) {
+            const auto s = rsrc(p.v_cache, at_v[i], rows_v[i]);
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int x = 0; x < NM; ++x) {
+                    uint32_t(&to)[CW * ES / 4] = v[4 * i + r][x];
+                    if constexpr (CW * ES == 16) {
+                        const u32x4 y = __builtin_amdgcn_raw_buffer_load_b128(s, v_at[r][x], 0, 0);
+                        to[0] = y[0]; to[1] = y[1]; to[2] = y[2]; to[3] = y[3];
+                    } else if constexpr (CW * ES == 8) {
+                        const u32x2 y = __builtin_amdgcn_raw_buffer_load_b64(s, v_at[r][x], 0, 0);
+                        to[0] = y[0]; to[1] = y[1];
+                    } else {
+                        to[0] = __builtin_amdgcn_raw_buffer_load_b32(s, v_at[r][x], 0, 0);
+                    }
+                }
+        }
+    };
+    auto keep_place = [&]() {
+#pragma unroll
+        for (int i = 0; i < BLOCKS; ++i) {
+            at_v[i] = at_k[i];
+            rows_v[i] = rows_k[i];
+        }
+    };
+    // the piece that begins with chunk `chunk` of (b, unit)
+    auto request = [&]() {
+        const int blocks = units / p.H_kv, kvh = unit / blocks, row0 = (unit - kvh * blocks) * ROWS;
+        const Piece next = {b, kvh, row0, min(ROWS, seq.rows - row0), chunk, min(n_chunks, chunk + (end - at)), n_chunks, seq.before, seq.len};
+#pragma unroll
+        for (int m = 0; m < M; ++m) {
+            const bool has_row = 16 * m + n < next.rows;
+            const int row = row0 + (has_row ? 16 * m + n : 0), i = row / group, head = kvh * group + row - i * group;
+            const T* q_row = (const T*)p.q + b * p.stride_b + i * p.stride_t + head * p.stride_h;
+            sees[m] = has_row ? (uint64_t)p.seen[b * p.seen_stride + i] : 0;
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                constexpr int E = BF16 ? 8 : 4;
+                const int col = O::STEP * ks + E * j;
+                q[m][ks] = u32x4{0, 0, 0, 0};
+                if (has_row && col < d) {
+                    if (!BF16 || col + 8 <= d) q[m][ks] = *reinterpret_cast<const u32x4*>(q_row + col);
+                    else {
+                        const u32x2 x = *reinterpret_cast<const u32x2*>(q_row + col);
+                        q[m][ks][0] = x[0];
+                        q[m][ks][1] = x[1];
+                    }
+                }
+            }
+        }
+        t0 = next.first * CHUNK<T> + wave * TILE;
+#pragma unroll
+        for (int i = 0; i < BLOCKS; ++i) {
+            page[i] = (t0 + 16 * i) / p.page_size;
+            in_page[i] = t0 + 16 * i - page[i] * p.page_size;
+        }
+        table = p.table + b * p.table_stride;
+        head_at = (int64_t)kvh * p.stride_head;
+        if (t0 < min(seq.len, next.last * CHUNK<T>)) {
+            place(t0);
+            load_k();
+            keep_place();
+            load_v();
+        }
+        return next;
+    };
+    now = request();
+    for (;;) {
+        const int t_end = min(now.len, now.last * CHUNK<T>);
+        f32x4 acc[M][NB];
+        float top[M], l[M];
+        bool saw[M];                            // some token that the row sees, in a page that is one
+#pragma unroll
+        for (int m = 0; m < M; ++m) {
+#pragma unroll
+            for (int i = 0; i < NB; ++i) acc[m][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+            top[m] = -INFINITY;
+            l[m] = 0.f;
+            saw[m] = false;
+        }
+        for (; t0 < t_end; t0 += CHUNK<T>) {
+            f32x4 s[M][BLOCKS];
+#pragma unroll
+            for (int i = 0; i < BLOCKS; ++i) {
+#pragma unroll
+                for (int m = 0; m < M; ++m) s[m][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) {
+                    u32x4 x = k[i][ks];
+                    if (BF16 && d % 8) {
+                        x[2] = ks == part_ks ? 0 : x[2];
+                        x[3] = ks == part_ks ? 0 : x[3];
+                    }
+#pragma unroll
+                    for (int m = 0; m < M; ++m) {
+                        if constexpr (BF16) s[m][i] = mfma_bf16(x, q[m][ks], s[m][i]);
+                        else {
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) s[m][i] = mfma_f32(x[e], q[m][ks][e], s[m][i]);
+                        }
+                    }
+                }
+            }
+            int rows[BLOCKS];
+            bool whole = t0 + TILE <= now.before;
+#pragma unroll
+            for (int i = 0; i < BLOCKS; ++i) {
+                rows[i] = rows_k[i];
+                whole = whole && rows[i] == 16;
+            }
+            const bool drafted = t0 + TILE > now.before;
+            const int tile_at = t0;
+            // the next tile's K rows (behind the last one: nothing, t0 is beyond the unit's tokens here)
+            const bool more = t0 + CHUNK<T> < t_end;
+            if (more) {
+                place(t0 + CHUNK<T>);
+                load_k();
+            }
+            // a lane's token x of the tile is seen by its row of block m
+            auto seen = [&](int m, int x) {
+                const int row = 4 * j + x % 4, nth = tile_at + 16 * (x / 4) + row - now.before;        // of the draft; negative: before it
+                return row < rows[x / 4] && (nth < 0 || ((sees[m] >> (nth & 63)) & 1));
+            };
+            if (!whole) {
+#pragma unroll
+                for (int m = 0; m < M; ++m)
+#pragma unroll
+                    for (int x = 0; x < TOKENS; ++x) {
+                        const bool sees_it = seen(m, x);
+                        saw[m] = saw[m] || sees_it;
+                        if (!sees_it) s[m][x / 4][x % 4] = -INFINITY;
+                    }
+            } else {
+#pragma unroll
+                for (int m = 0; m < M; ++m) saw[m] = true;
+            }
+            float pr[M][TOKENS];
+#pragma unroll
+            for (int m = 0; m < M; ++m) {
+                float sum = 0.f;
+#pragma unroll
+                for (int x = 0; x < TOKENS; ++x) {
+                    pr[m][x] = __builtin_amdgcn_exp2f(fmaf(s[m][x / 4][x % 4], kappa, -top[m]));
+                    sum += pr[m][x];
+                }
+                if (__builtin_amdgcn_ballot_w64(!(sum < MOST)) != 0) {          // wave-uniform and rare but for the first tile
+                    float mx = s[m][0][0];
+#pragma unroll
+                    for (int x = 1; x < TOKENS; ++x) mx = fmaxf(mx, s[m][x / 4][x % 4]);
+                    const float m_new = fmaxf(top[m], quad_max(mx) * kappa), ref = m_new == -INFINITY ? 0.f : m_new;
+                    const float alpha = __builtin_amdgcn_exp2f(top[m] - ref);
+                    top[m] = m_new;
+                    l[m] *= alpha;
+#pragma unroll
+                    for (int i = 0; i < NB; ++i) acc[m][i] *= alpha;
+                    sum = 0.f;
+#pragma unroll
+                    for (int x = 0; x < TOKENS; ++x) {
+                        pr[m][x] = __builtin_amdgcn_exp2f(fmaf(s[m][x / 4][x % 4], kappa, -ref));
+                        sum += pr[m][x];
+                    }
+                }
+                l[m] += sum;
+            }
+            if (drafted) {
+                // values that are no numbers, of tokens that some rows do not see
+                bool odd_values = false;
+#pragma unroll
+                for (int x = 0; x < TOKENS; ++x)
+#pragma unroll
+                    for (int y = 0; y < NM; ++y)
+#pragma unroll
+                        for (int c = 0; c < CW * ES / 4; ++c) odd_values = odd_values || odd_word<ES>(v[x][y][c]);
+                if (__builtin_amdgcn_ballot_w64(odd_values) != 0) {
+#pragma unroll
+                    for (int x = 0; x < TOKENS; ++x) {
+                        bool odd = false;
+#pragma unroll
+                        for (int y = 0; y < NM; ++y)
+#pragma unroll
+                            for (int c = 0; c < CW * ES / 4; ++c) odd = odd || odd_word<ES>(v[x][y][c]);
+                        const uint64_t who = __builtin_amdgcn_ballot_w64(odd);
+#pragma unroll 1
+                        for (int jj = 0; jj < 4; ++jj) {
+                            if (!((who >> (16 * jj)) & 0xffff)) continue;
+#pragma unroll
+                            for (int m = 0; m < M; ++m) {
+                                const float w = __shfl(pr[m][x], 16 * jj + n);
+                                const bool sees_it = __shfl((int)seen(m, x), 16 * jj + n) != 0;
+#pragma unroll
+                                for (int y = 0; y < NM; ++y)
+#pragma unroll
+                                    for (int c = 0; c < CW; ++c)
+#pragma unroll
+                                        for (int r = 0; r < 4; ++r) {
+                                            const float value = __shfl(element<ES>(v[x][y], c), 16 * jj + 4 * j + r);
+                                            if (sees_it) acc[m][y * CW + c][r] += w * value;
+                                        }
+                            }
+                        }
+                        if ((who >> (16 * j)) & 0xffff) {
+#pragma unroll
+                            for (int y = 0; y < NM; ++y)
+#pragma unroll
+                                for (int c = 0; c < CW * ES / 4; ++c) v[x][y][c] = 0;
+                        }
+                    }
+                }
+            }
+            if constexpr (BF16) {
+                u32x4 ph[M], pl[M];
+#pragma unroll
+                for (int m = 0; m < M; ++m) {
+                    bf16x8 hi, lo;
+#pragma unroll
+                    for (int x = 0; x < 8; ++x) {
+                        hi[x] = (__bf16)pr[m][x];
+                        lo[x] = (__bf16)(pr[m][x] - (float)hi[x]);
+                    }
+                    ph[m] = __builtin_bit_cast(u32x4, hi);
+                    pl[m] = __builtin_bit_cast(u32x4, lo);
+                }
+#pragma unroll
+                for (int x = 0; x < NM; ++x)
+#pragma unroll
+                    for (int c = 0; c < CW; ++c) {
+                        u32x4 a;        // column c of the lane's, its eight tokens
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            a[e] = __builtin_amdgcn_perm(v[2 * e + 1][x][c / 2], v[2 * e][x][c / 2], c % 2 ? 0x07060302u : 0x05040100u);
+#pragma unroll
+                        for (int m = 0; m < M; ++m) acc[m][x * CW + c] = mfma_bf16(a, ph[m], acc[m][x * CW + c]);
+#pragma unroll
+                        for (int m = 0; m < M; ++m) acc[m][x * CW + c] = mfma_bf16(a, pl[m], acc[m][x * CW + c]);
+                    }
+            } else {
+#pragma unroll
+                for (int r = 0; r < TOKENS; ++r)
+#pragma unroll
+                    for (int x = 0; x < NM; ++x)
+#pragma unroll
+                        for (int c = 0; c < CW; ++c)
+#pragma unroll
+                            for (int m = 0; m < M; ++m)
+                                acc[m][x * CW + c] = mfma_f32(v[r][x][c], __float_as_uint(pr[m][r]), acc[m][x * CW + c]);
+            }
+            if (more) {
+                keep_place();
+                load_v();
+            }
+        }
+
+        // on to the next piece: its first requests are on their way while this one is joined
+        const Piece done = now;
+        at += now.last - now.first;
+        const bool last_piece = WHOLE || at >= end;
+        if (!last_piece) {
+            chunk = 0;
+            if (++unit == units) {
+                unit = 0;
+                do {
+                    ++b;
+                    enter();
+                } while (n_chunks == 0 || units == 0);        // (there is one: `at` is before the end)
+            }
+            now = request();
+        }
+
+        // the four wavefronts' parts
+#pragma unroll
+        for (int m = 0; m < M; ++m) {
+            l[m] = quad_sum(l[m]);
+            const uint64_t some = __builtin_amdgcn_ballot_w64(saw[m]);
+            if (l[m] == 0.f && (((some >> n) | (some >> (16 + n)) | (some >> (32 + n)) | (some >> (48 + n))) & 1)) l[m] = -1.f;
+            if (j == 0) {
+                m_lds[wave][16 * m + n] = top[m];
+                l_lds[wave][16 * m + n] = l[m];
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int m = 0; m < M; ++m) {
+            float all = m_lds[0][16 * m + n];
+#pragma unroll
+            for (int w = 1; w < WAVES; ++w) all = fmaxf(all, m_lds[w][16 * m + n]);
+            const float own = __builtin_amdgcn_exp2f(top[m] - reference(all));
+#pragma unroll
+            for (int x = 0; x < NM; ++x)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+#pragma unroll
+                    for (int c = 0; c < CW; c += 2)
+                        *reinterpret_cast<float2*>(&o_lds[wave][16 * m + n][16 * CW * x + CW * (4 * j + r) + c]) =
+                            make_float2(acc[m][x * CW + c][r] * own, acc[m][x * CW + c + 1][r] * own);
+        }
+        __syncthreads();
+        const bool complete = done.first == 0 && done.last == done.n_chunks;
+        // (a share's piece of a unit that began in another one is its first, of one that ends in another its last)
+        float* part = p.parts + ((int64_t)mine * 2 + (done.first > 0 ? 0 : 1)) * part_floats(ROWS, DP);
+        for (int i = threadIdx.x; i < done.rows * (DP / 4); i += 64 * WAVES) {
+            const int row = i / (DP / 4), col = 4 * (i - row * (DP / 4));
+            if (col >= d) continue;
+            float4 y = *reinterpret_cast<const float4*>(&o_lds[0][row][col]);
+            float mx = m_lds[0][row];
+#pragma unroll
+            for (int w = 1; w < WAVES; ++w) {
+                const float4 z = *reinterpret_cast<const float4*>(&o_lds[w][row][col]);
+                y.x += z.x; y.y += z.y; y.z += z.z; y.w += z.w;
+                mx = fmaxf(mx, m_lds[w][row]);
+            }
+            float sum = 0.f;
+            bool weightless = false;
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w)
+                add_sum(sum, weightless, l_lds[w][row], __builtin_amdgcn_exp2f(m_lds[w][row] - reference(mx)));
+            if (sum == 0.f && weightless) sum = -1.f;
+            if (complete) {
+                // no token: zeros; tokens without any weight: no number
+                const float inv = sum < 0.f ? NAN : sum == 0.f ? 0.f : 1.f / sum;
+                const int at_row = done.row0 + row, t = at_row / group, head = done.kvh * group + at_row - t * group;
+                T* to = (T*)p.out + done.b * p.stride_b + t * p.stride_t + head * p.stride_h + col;
+                if constexpr (BF16) {
+                    bf16x4 z = {(__bf16)(y.x * inv), (__bf16)(y.y * inv), (__bf16)(y.z * inv), (__bf16)(y.w * inv)};
+                    *reinterpret_cast<bf16x4*>(to) = z;
+                } else {
+                    *reinterpret_cast<float4*>(to) = make_float4(y.x * inv, y.y * inv, y.z * inv, y.w * inv);
+                }
+                if (p.lse && col == 0)
+                    p.lse[done.b * p.stat_stride_b + t * p.stat_stride_t + head] = sum < 0.f ? NAN : (mx + __builtin_amdgcn_logf(sum)) * LN2;
+            } else {
+                *reinterpret_cast<float4*>(part + row * DP + col) = y;
+                if (col == 0) {
+                    part[ROWS * DP + row] = mx;
+                    part[ROWS * (DP + 1) + row] = sum;
+                }
+            }
+        }
+        if (last_piece) break;
+        __syncthreads();
+    }
+}
+
+// Units whose pieces lie in several shares, and rows of sequences without a token.  JOIN_WAVES wavefronts take the pieces of a row in turn; a workgroup
+// has eight wavefronts or, where one is enough for a row, four, of which each has a row of its own.
+constexpr int BATCH = 4;
+template <typename T, int DP, int M, int JOIN_WAVES>
+__global__ void __launch_bounds__(JOIN_WAVES == 1 ? 256 : 64 * JOIN_WAVES)
+tree_join_kernel(TreeArgs p) {
+    constexpr int COLS = (DP + 63) / 64, EACH = JOIN_WAVES == 1 ? 4 : 1, ROWS = 16 * M;
+    __shared__ float o_lds[JOIN_WAVES][DP], m_lds[JOIN_WAVES], l_lds[JOIN_WAVES];
+    const int lane = threadIdx.x & 63, own_wave = scalar((int)threadIdx.x >> 6), wave = EACH == 1 ? own_wave : 0;
+    const int group = p.H / p.H_kv, at_row = (int)blockIdx.x * EACH + (EACH == 1 ? 0 : own_wave);
+    const int b = at_row / (p.T * p.H), t = (at_row - b * p.T * p.H) / p.H, head = at_row - (b * p.T + t) * p.H;
+    if (b >= p.B) return;
+    Sequence seq = sequence(p, b);
+    seq = {scalar(seq.before), scalar(seq.len), scalar(seq.rows)};
+    const int kvh = head / group, in_unit = t * group + head - kvh * group;
+    if (in_unit >= seq.rows) return;
+    const int n = chunks_of<T>(seq), unit = kvh * (units_of<ROWS>(p, seq) / p.H_kv) + in_unit / ROWS, row = in_unit % ROWS;
+    // (in one pass: the chunks of the sequences before b, and all)
+    int before = 0, all = 0;
+#pragma unroll 4
+    for (int b0 = 0; b0 < p.B; b0 += 64) {
+        const int own = b0 + lane < p.B ? work_of<T, ROWS>(p, b0 + lane) : 0;
+        all += own;
+        before += b0 + lane < b ? own : 0;
+    }
+    all = wave_total(wave_scan(all));
+    before = wave_total(wave_scan(before));
+    const uint32_t share = (uint32_t)share_of(all, p.n_wgs), from = (uint32_t)(before + unit * n);
+    const int g0 = (int)(from / share), g1 = n ? (int)((from + n - 1) / share) : g0;
+    if (n && g0 == g1) return;
+    // a wavefront's pieces, BATCH of them requested at a time (they come from other XCDs' workgroups: a round trip to memory each)
+    const int pieces = n ? g1 - g0 + 1 : 0;
+    float m = -INFINITY, l = 0.f, acc[COLS] = {};
+    bool weightless = false;
+    for (int i0 = wave * BATCH; i0 < pieces; i0 += JOIN_WAVES * BATCH) {
+        float mg[BATCH], lg[BATCH], x[BATCH][COLS];
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) {
+            const int at = min(i0 + i, pieces - 1);
+            const float* part = p.parts + ((int64_t)(g0 + at) * 2 + (at == 0 ? 1 : 0)) * part_floats(ROWS, DP);
+            mg[i] = part[ROWS * DP + row];
+            lg[i] = part[ROWS * (DP + 1) + row];
+#pragma unroll
+            for (int c = 0; c < COLS; ++c) x[i][c] = lane + 64 * c < p.d ? part[row * DP + lane + 64 * c] : 0.f;
+        }
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) {
+            if (i0 + i >= pieces) break;
+            const float top = fmaxf(m, mg[i]), a = __builtin_amdgcn_exp2f(m - reference(top)), f = __builtin_amdgcn_exp2f(mg[i] - reference(top));
+            l *= a;
+            add_sum(l, weightless, lg[i], f);
+#pragma unroll
+            for (int c = 0; c < COLS; ++c) acc[c] = acc[c] * a + x[i][c] * f;
+            m = top;
+        }
+    }
+    T* const to = (T*)p.out + b * p.stride_b + t * p.stride_t + head * p.stride_h;
+    float* const lse = p.lse ? p.lse + b * p.stat_stride_b + t * p.stat_stride_t + head : nullptr;
+    if constexpr (JOIN_WAVES == 1) {
+        if (weightless && l == 0.f) l = NAN;
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+        for (int c = 0; c < COLS; ++c)
+            if (lane + 64 * c < p.d) {
+                if constexpr (sizeof(T) == 2) reinterpret_cast<__bf16*>(to)[lane + 64 * c] = (__bf16)(acc[c] * inv);
+                else to[lane + 64 * c] = acc[c] * inv;
+            }
+        if (lse && lane == 0) *lse = (m + __builtin_amdgcn_logf(l)) * LN2;
+        return;
+    }
+#pragma unroll
+    for (int c = 0; c < COLS; ++c)
+        if (lane + 64 * c < DP) o_lds[wave][lane + 64 * c] = acc[c];
+    if (lane == 0) {
+        m_lds[wave] = m;
+        l_lds[wave] = weightless && l == 0.f ? -1.f : l;
+    }
+    __syncthreads();
+    float top = m_lds[0];
+#pragma unroll
+    for (int w = 1; w < JOIN_WAVES; ++w) top = fmaxf(top, m_lds[w]);
+    float f[JOIN_WAVES], sum = 0.f;
+    weightless = false;
+#pragma unroll
+    for (int w = 0; w < JOIN_WAVES; ++w) {
+        f[w] = __builtin_amdgcn_exp2f(m_lds[w] - reference(top));
+        add_sum(sum, weightless, l_lds[w], f[w]);
+    }
+    if (sum == 0.f && weightless) sum = NAN;
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    for (int col = threadIdx.x; col < p.d; col += 64 * JOIN_WAVES) {
+        float y = 0.f;
+#pragma unroll
+        for (int w = 0; w < JOIN_WAVES; ++w) y += o_lds[w][col] * f[w];
+        if constexpr (sizeof(T) == 2) reinterpret_cast<__bf16*>(to)[col] = (__bf16)(y * inv);
+        else to[col] = y * inv;
+    }
+    if (lse && threadIdx.x == 0) *lse = (top + __builtin_amdgcn_logf(sum)) * LN2;
+}
+
+constexpr int columns(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : d <= 128 ? 128 : 256; }
+// blocks of 16 rows a unit
+constexpr int blocks_for(int rows, int DP) { return rows <= 16 ? 1 : rows <= 32 || DP > 128 ? 2 : 4; }
+constexpr int workgroups(int DP, int M) { return N_CU * (DP > 128 || M > 2 ? 1 : 2); }
+
+template <typename T, int DP, int M>
+hipError_t launch(TreeArgs a, hipStream_t st) {
+    const int rows = a.T * (a.H / a.H_kv);
+    // (decode.hip's rule for units of a workgroup each)
+    if ((int64_t)a.max_pages * a.page_size <= (DP > 128 ? 4 : 8) * CHUNK<T>) {
+        hipLaunchKernelGGL((tree_kernel<T, DP, M, true>), dim3((unsigned)(a.B * a.H_kv * ((rows + 16 * M - 1) / (16 * M)))), dim3(64 * WAVES), 0, st, a);
+        return hipGetLastError();
+    }
+    a.n_wgs = workgroups(DP, M);
+    hipLaunchKernelGGL((tree_kernel<T, DP, M, false>), dim3((unsigned)a.n_wgs), dim3(64 * WAVES), 0, st, a);
+    if (hipError_t e = hipGetLastError()) return e;
+    const int64_t all = (int64_t)a.B * a.T * a.H;
+    if (all <= 512) hipLaunchKernelGGL((tree_join_kernel<T, DP, M, 8>), dim3((unsigned)all), dim3(64 * 8), 0, st, a);
+    else hipLaunchKernelGGL((tree_join_kernel<T, DP, M, 1>), dim3((unsigned)((all + 3) / 4)), dim3(64 * 4), 0, st, a);
+    return hipGetLastError();
+}
+template <typename T, int DP>
+hipError_t launch(const TreeArgs& a, hipStream_t st) {
+    switch (blocks_for(a.T * (a.H / a.H_kv), DP)) {
+        case 1: return launch<T, DP, 1>(a, st);
+        case 2: return launch<T, DP, 2>(a, st);
+        default:
+            if constexpr (DP <= 128) return launch<T, DP, 4>(a, st);
+            return hipErrorInvalidValue;        // (not reached: blocks_for)
+    }
+}
+template <typename T>
+hipError_t launch(const TreeArgs& a, hipStream_t st) {
+    switch (columns(a.d)) {
+        case 32: return launch<T, 32>(a, st);
+        case 64: return launch<T, 64>(a, st);
+        case 128: return launch<T, 128>(a, st);
+        default: return launch<T, 256>(a, st);
+    }
+}
+
+}  // namespace
+
+int64_t tree_workspace(int rows, int d) {
+    const int DP = columns(d), M = blocks_for(rows, DP);
+    return (int64_t)workgroups(DP, M) * 2 * part_floats(16 * M, DP) * 4;
+}
+
+hipError_t launch_tree(const TreeArgs& a, int dtype, hipStream_t st) {
+    return dtype == SA_F32 ? launch<float>(a, st) : launch<__hip_bfloat16>(a, st);
+}
+
+}  // namespace sa

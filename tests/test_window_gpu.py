@@ -176,7 +176,8 @@ def test_what_a_row_does_not_see_does_not_reach_it(bad, d, dtype):
     sees = (n >= at) & (n < at + window)        # rows that see the key
     for which in ((1,), (2,), (1, 2)):
         _, out, lse, _ = run(lens, 2, 2, d, dtype, window, sinks, mutate=poison(*which))
-        assert torch.equal(out.cpu()[~sees], clean[1].cpu()[~sees]) or (out.cpu()[~sees].float() - clean[1].cpu()[~sees].float()).abs().max() <= 2.0 ** -7 * 4
+        # (rows done over have the other rows' tolerance: two roundings, of values below 4)
+        assert (out.cpu()[~sees].float() - clean[1].cpu()[~sees].float()).abs().max() <= {BF16: 2.0 ** -7, F32: 2.0 ** -16}[dtype] * 4
         assert torch.isfinite(out.cpu()[~sees]).all() and torch.isfinite(lse.cpu()[:, ~sees]).all()
         assert not torch.isfinite(out.cpu()[sees]).all(1).any()
     # the gradient, with the statistics of the clean call
