@@ -404,7 +404,7 @@ typedef struct {
  * does not have are not looked at.  drafts: device int32 [B], the tokens of each draft (taken as 0 .. T); NULL: T each.  Rows of out and lse behind a
  * sequence's draft are left as they are.  lens: device int32 [B], 0 or more; tokens behind max_pages * page_size are left out.
  * A token that sees none is zero with LSE -inf; infinities and NaN as in sa_attn_decode, and nothing of a drafted token reaches one that does not see it.
- * Pages, workspace (sa_attn_tree_workspace(shape, cache) bytes: it depends on T, H, H_kv, d), rounding and errors as sa_attn_decode; lengths, drafts,
+ * Pages, workspace (sa_attn_tree_workspace(shape, cache) bytes: it depends on T, H, H_kv, d and the type), rounding and errors as sa_attn_decode; lengths, drafts,
  * masks and the table are read on the device.
  */
 int64_t sa_attn_tree_workspace(const sa_tree* shape, const sa_cache* cache);       /* or a negative sa_status */

@@ -708,7 +708,7 @@ int sa_attn_window_decode(const void* q, const void* k_cache, const void* v_cach
 
 int64_t sa_attn_tree_workspace(const sa_tree* shape, const sa_cache* cache) {
     if (int e = check_tree(shape, cache)) return e;
-    return sa::tree_workspace(shape->T * (shape->H / cache->H_kv), cache->d);
+    return sa::tree_workspace(shape->T * (shape->H / cache->H_kv), cache->d, cache->dtype);
 }
 
 int sa_attn_tree(const void* q, const void* k_cache, const void* v_cache, const int32_t* table, const int32_t* lens, const int32_t* drafts,

@@ -60,7 +60,7 @@ struct TreeArgs {
     float scale;
     int n_wgs;                  // workgroups of the launch
 };
-int64_t tree_workspace(int rows, int d);        // rows: T H / H_kv
+int64_t tree_workspace(int rows, int d, int dtype);         // rows: T H / H_kv
 hipError_t launch_tree(const TreeArgs& a, int dtype, hipStream_t st);
 
 // Whole pages, or their first tokens, onto others

@@ -33,7 +33,8 @@ template <int DP> struct Of<__hip_bfloat16, DP> {
 template <int DP> struct Of<float, DP> {
     static constexpr int TILE = 16, STEP = 16, CW = DP >= 64 ? 4 : DP / 16, ES = 4;
 };
-template <typename T> constexpr int CHUNK = WAVES * Of<T, 64>::TILE;
+template <typename T> constexpr int CHUNK = WAVES * Of<T, 64>::TILE;      // tree_kernel
+constexpr int TILE_CHUNK = DT_ROWS;                                        // tree_tiles_kernel
 
 __device__ inline f32x4 mfma_bf16(u32x4 a, u32x4 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
@@ -67,29 +68,29 @@ __device__ inline Sequence sequence(const TreeArgs& p, int b) {
     return {before, min(before + drafted, room), drafted * (p.H / p.H_kv)};
 }
 // its chunks, and its units
-template <typename T> __device__ inline int chunks_of(const Sequence& x) { return (x.len + CHUNK<T> - 1) / CHUNK<T>; }
+template <int CH> __device__ inline int chunks_of(const Sequence& x) { return (x.len + CH - 1) / CH; }
 template <int ROWS> __device__ inline int units_of(const TreeArgs& p, const Sequence& x) { return p.H_kv * ((x.rows + ROWS - 1) / ROWS); }
 // the chunks of all its units
-template <typename T, int ROWS>
+template <int CH, int ROWS>
 __device__ inline int work_of(const TreeArgs& p, int b) {
     const Sequence x = sequence(p, b);
-    return chunks_of<T>(x) * units_of<ROWS>(p, x);
+    return chunks_of<CH>(x) * units_of<ROWS>(p, x);
 }
 
 // Where chunk number `at` of all units' chunks lies: the sequence, the chunks before it; and the share of a workgroup.  A wavefront's lanes take the
 // sequences in turn.  (All counts are below 2^31: check_tree.)
 __device__ inline int share_of(int all, int n_wgs) { return max(1, (int)(((uint32_t)all + (uint32_t)n_wgs - 1) / (uint32_t)n_wgs)); }
-template <typename T, int ROWS>
+template <int CH, int ROWS>
 __device__ inline int all_work(const TreeArgs& p, int lane) {
     int n = 0;
-    for (int b0 = 0; b0 < p.B; b0 += 64) n += b0 + lane < p.B ? work_of<T, ROWS>(p, b0 + lane) : 0;
+    for (int b0 = 0; b0 < p.B; b0 += 64) n += b0 + lane < p.B ? work_of<CH, ROWS>(p, b0 + lane) : 0;
     return wave_total(wave_scan(n));
 }
-template <typename T, int ROWS>
+template <int CH, int ROWS>
 __device__ inline void find_chunk(const TreeArgs& p, int at, int lane, int& seq, int& before) {
     before = 0;
     for (int b0 = 0; b0 < p.B; b0 += 64) {
-        const int own = b0 + lane < p.B ? work_of<T, ROWS>(p, b0 + lane) : 0, upto = wave_scan(own);
+        const int own = b0 + lane < p.B ? work_of<CH, ROWS>(p, b0 + lane) : 0, upto = wave_scan(own);
         const uint64_t past = __builtin_amdgcn_ballot_w64(before + upto > at);
         if (past) {
             const int l = (int)__builtin_ctzll(past);
@@ -113,17 +114,15 @@ template <int ES> __device__ inline float element(const uint32_t* words, int i) 
     return __uint_as_float(ES == 4 ? words[i] : i % 2 ? words[i / 2] & 0xffff0000u : words[i / 2] << 16);
 }
 
-constexpr int waves_per_simd(int DP, int M) { return DP > 128 || M > 2 ? 1 : 2; }
-
 // WHOLE: a workgroup has one unit, all of it, and there is nothing to join.
 template <typename T, int DP, int M, bool WHOLE>
-__global__ void __launch_bounds__(64 * WAVES, waves_per_simd(DP, M))
+__global__ void __launch_bounds__(64 * WAVES, DP > 128 ? 1 : 2)
 tree_kernel(TreeArgs p) {
     using O = Of<T, DP>;
     constexpr int TILE = O::TILE, CW = O::CW, ES = O::ES, KS = DP / O::STEP, NM = DP / (16 * CW), NB = DP / 16;
     constexpr bool BF16 = ES == 2;
     constexpr int BLOCKS = TILE / 16, TOKENS = 4 * BLOCKS;      // 16-token blocks of a tile, tokens a lane holds of it
-    constexpr int PITCH = DP + 4, ROWS = 16 * M;
+    constexpr int PITCH = DP + 4, ROWS = 16 * M, CH = CHUNK<T>;
     __shared__ __attribute__((aligned(16))) float o_lds[WAVES][ROWS][PITCH];
     __shared__ float m_lds[WAVES][ROWS], l_lds[WAVES][ROWS];
 
@@ -136,7 +135,7 @@ tree_kernel(TreeArgs p) {
     auto enter = [&]() {
         seq = sequence(p, b);
         seq = {scalar(seq.before), scalar(seq.len), scalar(seq.rows)};
-        n_chunks = chunks_of<T>(seq);
+        n_chunks = chunks_of<CH>(seq);
         units = units_of<ROWS>(p, seq);
     };
     if constexpr (WHOLE) {
@@ -150,7 +149,7 @@ tree_kernel(TreeArgs p) {
         end = n_chunks;
     } else {
         // neighbouring shares, which often read the same rows for other ones, on one XCD: consecutive workgroups go round-robin to the 8
-        const int all = all_work<T, ROWS>(p, lane), each = share_of(all, p.n_wgs);
+        const int all = all_work<CH, ROWS>(p, lane), each = share_of(all, p.n_wgs);
         const int n_shares = (int)(((uint32_t)all + (uint32_t)each - 1) / (uint32_t)each), per_xcd = (n_shares + 7) / 8;
         if ((int)blockIdx.x / 8 >= per_xcd) return;
         mine = (int)blockIdx.x % 8 * per_xcd + (int)blockIdx.x / 8;
@@ -159,7 +158,7 @@ tree_kernel(TreeArgs p) {
         end = at + min(each, all - at);
         // (a sequence's chunks, unit by unit, follow those of all sequences before it)
         int before;
-        find_chunk<T, ROWS>(p, at, lane, b, before);
+        find_chunk<CH, ROWS>(p, at, lane, b, before);
         enter();
         const int in = at - before;
         unit = (int)((uint32_t)in / (uint32_t)n_chunks);
@@ -190,9 +189,9 @@ tree_kernel(TreeArgs p) {
     Piece now;
     u32x4 q[M][KS];
     uint64_t sees[M];                           // the row's mask
-    int t0;                                     // this wavefront's next tile: tokens t0 .. t0 + TILE - 1, CHUNK<T> further on the one after it
+    int t0;                                     // this wavefront's next tile: tokens t0 .. t0 + TILE - 1, CH further on the one after it
     // page and place in it of each of its 16-token blocks
-    const int step_page = CHUNK<T> / p.page_size, step_in = CHUNK<T> - step_page * p.page_size;
+    const int step_page = CH / p.page_size, step_in = CH - step_page * p.page_size;
     int page[BLOCKS], in_page[BLOCKS];
     const int32_t* table;
     int64_t head_at;
@@ -285,7 +284,7 @@ tree_kernel(TreeArgs p) {
                 }
             }
         }
-        t0 = next.first * CHUNK<T> + wave * TILE;
+        t0 = next.first * CH + wave * TILE;
 #pragma unroll
         for (int i = 0; i < BLOCKS; ++i) {
             page[i] = (t0 + 16 * i) / p.page_size;
@@ -293,7 +292,7 @@ tree_kernel(TreeArgs p) {
         }
         table = p.table + b * p.table_stride;
         head_at = (int64_t)kvh * p.stride_head;
-        if (t0 < min(seq.len, next.last * CHUNK<T>)) {
+        if (t0 < min(seq.len, next.last * CH)) {
             place(t0);
             load_k();
             keep_place();
@@ -303,7 +302,7 @@ tree_kernel(TreeArgs p) {
     };
     now = request();
     for (;;) {
-        const int t_end = min(now.len, now.last * CHUNK<T>);
+        const int t_end = min(now.len, now.last * CH);
         f32x4 acc[M][NB];
         float top[M], l[M];
         bool saw[M];                            // some token that the row sees, in a page that is one
@@ -315,7 +314,7 @@ tree_kernel(TreeArgs p) {
             l[m] = 0.f;
             saw[m] = false;
         }
-        for (; t0 < t_end; t0 += CHUNK<T>) {
+        for (; t0 < t_end; t0 += CH) {
             f32x4 s[M][BLOCKS];
 #pragma unroll
             for (int i = 0; i < BLOCKS; ++i) {
@@ -348,9 +347,9 @@ tree_kernel(TreeArgs p) {
             const bool drafted = t0 + TILE > now.before;
             const int tile_at = t0;
             // the next tile's K rows (behind the last one: nothing, t0 is beyond the unit's tokens here)
-            const bool more = t0 + CHUNK<T> < t_end;
+            const bool more = t0 + CH < t_end;
             if (more) {
-                place(t0 + CHUNK<T>);
+                place(t0 + CH);
                 load_k();
             }
             // a lane's token x of the tile is seen by its row of block m
@@ -577,13 +576,377 @@ tree_kernel(TreeArgs p) {
     }
 }
 
+// bf16, up to 128 columns, more than 32 rows a key/value head: as attention of whole blocks has it, tiles of 64 tokens go straight into LDS (mfma_tiles.h),
+// two buffers, and R groups of 32 rows read them; S^T = K Q^T and O^T += V^T P^T by 32 x 32 products, a lane holding 16 tokens of one row.  R = 4: a
+// wavefront each; R = 2: two wavefronts each, of which either takes 32 tokens of a tile, joined at the end of a piece.  A tile is requested while the one
+// before it is computed, each wavefront one 16-token block of it: its page, its descriptor.
+//
+// Bound by memory: a token costs a compute unit 512 bytes (d 128), 65 clocks at 4.9 TB/s, and 24 products of 32 clocks for each 32 tokens and rows, on
+// four SIMDs 24 clocks a token and 128 rows.
+template <int DP> constexpr int KV_BYTES = 2 * tile_bytes(DP);
+template <int DP, int R, bool PART, bool WHOLE>
+__global__ void __launch_bounds__(64 * WAVES, 2)
+tree_tiles_kernel(TreeArgs p) {
+    constexpr int ROWS = 32 * R, SHARING = WAVES / R, SUBS = 2 / SHARING, CH = TILE_CHUNK, KS = ksteps_of(DP), MB = blocks_of(DP);
+    static_assert(R == 2 || R == 4, "one or two wavefronts a row group");
+    __shared__ __attribute__((aligned(1024))) char lds[2][KV_BYTES<DP>];        // [buffer][K | V]
+    __shared__ int rows_lds[2][4];                                              // tokens of each 16-token block
+    __shared__ float stat_lds[R][2][32];
+
+    const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
+    const int wave = scalar((int)threadIdx.x >> 6), rg = wave / SHARING, part_of = wave % SHARING;      // row group; its tokens of a tile: SUBS sub-tiles
+    const int group = p.H / p.H_kv, d = p.d;
+    int mine, at, end, b, unit, chunk, n_chunks, units;       // as in tree_kernel
+    Sequence seq;
+    auto enter = [&]() {
+        seq = sequence(p, b);
+        seq = {scalar(seq.before), scalar(seq.len), scalar(seq.rows)};
+        n_chunks = chunks_of<CH>(seq);
+        units = units_of<ROWS>(p, seq);
+    };
+    if constexpr (WHOLE) {
+        mine = (int)blockIdx.x;
+        const int most = p.H_kv * ((p.T * group + ROWS - 1) / ROWS);
+        b = mine / most;
+        unit = mine - b * most;
+        enter();
+        if (unit >= units) return;
+        chunk = at = 0;
+        end = n_chunks;
+    } else {
+        const int all = all_work<CH, ROWS>(p, lane), each = share_of(all, p.n_wgs);
+        const int n_shares = (int)(((uint32_t)all + (uint32_t)each - 1) / (uint32_t)each), per_xcd = (n_shares + 7) / 8;
+        if ((int)blockIdx.x / 8 >= per_xcd) return;
+        mine = (int)blockIdx.x % 8 * per_xcd + (int)blockIdx.x / 8;
+        if (mine >= n_shares) return;
+        at = mine * each;
+        end = at + min(each, all - at);
+        int before;
+        find_chunk<CH, ROWS>(p, at, lane, b, before);
+        b = scalar(b);
+        enter();
+        const int in = at - before;
+        unit = scalar((int)((uint32_t)in / (uint32_t)n_chunks));
+        chunk = scalar(in - unit * n_chunks);
+    }
+    const float kappa = p.scale * LOG2E;
+    const int pitch = (int)p.stride_slot * 2;               // bytes between tokens of a page
+    uint32_t arow[8], tr0[4], tr1[4], g[4];                 // g: of a 16-token block, as of a tile's first one
+    dt_row_addrs<DP>(arow, n, h);
+    dt_tr_addrs<DP>(tr0, tr1, lane);
+    dt_load_offsets<DP>(g, lane, 0, pitch, d);
+    // PART, d % 8 == 4: the chunk that holds column d has four elements of whatever follows the row
+    const int part_ks = PART && ((d >> 3) & 1) == h ? d >> 4 : -1;
+
+    struct Piece { int b, kvh, row0, rows, first, last, n_chunks, before; };
+    Piece now;
+    bf16x8 q[8];
+    uint64_t sees;                              // the row's mask
+    const int step_page = CH / p.page_size, step_in = CH - step_page * p.page_size;
+    int page, in_page, token, id;               // of this wavefront's block of the tile to request next; its page's number in the cache
+    const int32_t* table;
+    int64_t head_at;
+    auto look_up = [&]() { id = token < seq.len ? table[page] : -1; };
+    auto request = [&](int buffer) {
+        const int page_id = scalar(id);
+        int rows = 0;
+        int64_t from = 0;
+        if (page_id >= 0 && page_id < p.n_pages) {
+            rows = min(16, seq.len - token);
+            from = (page_id * p.stride_page + in_page * p.stride_slot + head_at) * 2;
+        }
+        dt_rsrc k = dt_make_rsrc((const char*)p.k_cache + from, rows, pitch, d), v = dt_make_rsrc((const char*)p.v_cache + from, rows, pitch, d);
+        if (rows == 0) k[2] = v[2] = 0;         // nothing is in range: zeros
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {           // (kept scalar)
+            k[i] = scalar(k[i]);
+            v[i] = scalar(v[i]);
+        }
+        dt_load<DP>(k, 0, lds[buffer], g, wave);
+        dt_load<DP>(v, 0, lds[buffer] + tile_bytes(DP), g, wave);
+        if (lane == 0) rows_lds[buffer][wave] = rows;
+        token += CH;
+        page += step_page;
+        in_page += step_in;
+        if (in_page >= p.page_size) {
+            in_page -= p.page_size;
+            ++page;
+        }
+        look_up();
+    };
+    // the piece that begins with chunk `chunk` of (b, unit): its first tile and its queries
+    auto begin = [&]() {
+        const int blocks = units / p.H_kv, kvh = unit / blocks, row0 = (unit - kvh * blocks) * ROWS;
+        const Piece next = {b, kvh, row0, min(ROWS, seq.rows - row0), chunk, min(n_chunks, chunk + (end - at)), n_chunks, seq.before};
+        token = next.first * CH + 16 * wave;
+        page = token / p.page_size;
+        in_page = token - page * p.page_size;
+        table = p.table + b * p.table_stride;
+        head_at = (int64_t)kvh * p.stride_head;
+        look_up();
+        if (next.first < next.last) request(0);
+        const bool has_row = 32 * rg + n < next.rows;
+        const int row = row0 + (has_row ? 32 * rg + n : 0), i = row / group, head = kvh * group + row - i * group;
+        sees = has_row ? (uint64_t)p.seen[b * p.seen_stride + i] : 0;
+        const __bf16* const q_row = (const __bf16*)p.q + b * p.stride_b + i * p.stride_t + head * p.stride_h;
+        if (d < 8) load_b_frags<8>(q, q_row, h, d);
+        else {
+            // (all requested at once, without branches: from the row's last eight columns where a chunk goes beyond them)
+            typedef __bf16 Chunk __attribute__((ext_vector_type(8), aligned(8)));
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) q[ks] = *reinterpret_cast<const Chunk*>(q_row + min(16 * ks + 8 * h, d - 8));
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                const int beyond = 16 * ks + 8 * h + 8 - d;         // columns
+                const bf16x8 x = q[ks], z = {0, 0, 0, 0, 0, 0, 0, 0};
+                q[ks] = beyond <= 0 ? x : beyond == 4 ? __builtin_shufflevector(x, z, 4, 5, 6, 7, 8, 9, 10, 11) : z;
+            }
+        }
+        return next;
+    };
+    now = begin();
+    for (;;) {
+        f32x16 acc[MB];
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[mb][r] = 0.f;
+        float top = -INFINITY, l = 0.f;
+        bool saw = false;                       // some token that the row sees, in a page that is one
+        for (int t = now.first; t < now.last; ++t) {
+            const int buffer = scalar((t - now.first) & 1);
+            __builtin_amdgcn_s_waitcnt(0);      // this wavefront's loads have landed ...
+            __syncthreads();                    // ... and everyone's; the other buffer has been read
+            if (t + 1 < now.last) request(buffer ^ 1);
+            if (32 * rg >= now.rows) continue;  // no row here
+#pragma unroll 1
+            for (int sub = part_of * SUBS; sub < part_of * SUBS + SUBS; ++sub) {
+                const char* const k = lds[buffer] + sub * (tile_bytes(DP) / 2);
+                const char* const v = k + tile_bytes(DP);
+                const int t0 = t * CH + 32 * sub, rows0 = scalar(rows_lds[buffer][2 * sub]), rows1 = scalar(rows_lds[buffer][2 * sub + 1]);
+                if (rows0 + rows1 == 0) continue;
+                // operands are read from LDS this many products ahead of their use
+                constexpr int AHEAD_K = 3, AHEAD_V = 2;
+                bf16x8 ka[KS], va[2 * MB];
+                auto read_v = [&](int i) { va[i] = dt_read_tr(v + i / MB * 16 * row_bytes(DP), tr0[i % MB], tr1[i % MB]); };
+                f32x16 s;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[r] = 0.f;
+#pragma unroll
+                for (int ks = 0; ks < AHEAD_K; ++ks) ka[ks] = dt_read_row(k, arow[ks]);
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) {
+                    __builtin_amdgcn_sched_barrier(0);
+                    if (ks + AHEAD_K < KS) ka[ks + AHEAD_K] = dt_read_row(k, arow[ks + AHEAD_K]);
+                    s = mfma(PART ? zero_beyond_d(ka[ks], ks == part_ks) : ka[ks], q[ks], s);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int i = 0; i < AHEAD_V; ++i) read_v(i);
+                const bool drafted = t0 + 32 > now.before;
+                // register r is seen: a token that there is, in front of the draft or named by the mask
+                auto seen = [&](int r, uint64_t mask, int n0, int n1) {
+                    const int in = 8 * (r / 4) + 4 * h + r % 4, nth = t0 + in - now.before;
+                    return in % 16 < (r < 8 ? n0 : n1) && (nth < 0 || ((mask >> (nth & 63)) & 1));
+                };
+                if (drafted || rows0 + rows1 < 32) {
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const bool sees_it = seen(r, sees, rows0, rows1);
+                        saw = saw || sees_it;
+                        if (!sees_it) s[r] = -INFINITY;
+                    }
+                } else {
+                    saw = true;
+                }
+                float pr[16], sum = 0.f;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    pr[r] = __builtin_amdgcn_exp2f(fmaf(s[r], kappa, -top));
+                    sum += pr[r];
+                }
+                if (__builtin_amdgcn_ballot_w64(!(sum < MOST)) != 0) {          // wave-uniform and rare but for the first one
+                    float mx = s[0];
+#pragma unroll
+                    for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
+                    const float m_new = fmaxf(top, half_wave_max(mx) * kappa), ref = reference(m_new);
+                    const float alpha = __builtin_amdgcn_exp2f(top - ref);
+                    top = m_new;
+                    l *= alpha;
+#pragma unroll
+                    for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) acc[mb][r] *= alpha;
+                    sum = 0.f;
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        pr[r] = __builtin_amdgcn_exp2f(fmaf(s[r], kappa, -ref));
+                        sum += pr[r];
+                    }
+                }
+                l += sum;
+                // values that are no numbers, of tokens that some rows do not see
+                uint32_t odd = 0;               // tokens of the sub-tile
+                if (drafted) {
+#pragma unroll 1
+                    for (int y = 0; y < 32; y += 8) {       // eight tokens at a time, eight lanes each
+                        const int in = y + lane / 8;
+                        bool bad = false;
+#pragma unroll
+                        for (int c = 0; c < DP / 64; ++c) {
+                            typedef uint32_t u32x4a __attribute__((ext_vector_type(4)));
+                            const u32x4a w = *reinterpret_cast<const u32x4a*>(v + dt_chunk_at<DP>(in, lane % 8 + 8 * c));
+                            bad = bad || odd_word<2>(w[0]) || odd_word<2>(w[1]) || odd_word<2>(w[2]) || odd_word<2>(w[3]);
+                        }
+                        const uint64_t who = __builtin_amdgcn_ballot_w64(bad);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) odd |= ((who >> (8 * e)) & 0xff ? 1u : 0u) << (y + e);
+                    }
+                    odd = scalar(odd);
+                    if (odd) {
+                        // (what the masks need is formed anew here, not kept from above for this)
+                        uint32_t mask_lo = (uint32_t)sees, mask_hi = (uint32_t)(sees >> 32);
+                        int n0 = rows0, n1 = rows1;
+                        asm volatile("" : "+v"(mask_lo), "+v"(mask_hi), "+s"(n0), "+s"(n1));
+                        const uint64_t mask = (uint64_t)mask_hi << 32 | mask_lo;
+#pragma unroll 1
+                        for (uint32_t left = odd; left != 0; left &= left - 1) {
+                            const int in = __builtin_ctz(left);
+                            float w = 0.f;
+                            int sees_it = 0;
+#pragma unroll
+                            for (int r = 0; r < 16; ++r)
+                                if (8 * (r / 4) + 4 * h + r % 4 == in) {
+                                    w = pr[r];
+                                    sees_it = seen(r, mask, n0, n1);
+                                }
+                            const int owner = n + 32 * ((in >> 2) & 1);         // of the two lanes of a row the one that holds the token
+                            w = __shfl(w, owner);
+                            sees_it = __shfl(sees_it, owner);
+#pragma unroll
+                            for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+                                for (int r = 0; r < 16; ++r) {
+                                    const int column = 32 * mb + 8 * (r / 4) + 4 * h + r % 4;
+                                    const __bf16 value = *reinterpret_cast<const __bf16*>(v + dt_chunk_at<DP>(in, column / 8) + 2 * (column % 8));
+                                    if (sees_it) acc[mb][r] += w * (float)value;
+                                }
+                        }
+                    }
+                }
+                bf16x8 hi[2], lo[2];
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    hi[r / 8][r % 8] = (__bf16)pr[r];
+                    lo[r / 8][r % 8] = (__bf16)(pr[r] - (float)hi[r / 8][r % 8]);
+                }
+#pragma unroll
+                for (int i = 0; i < 2 * MB; ++i) {
+                    __builtin_amdgcn_sched_barrier(0);
+                    if (i + AHEAD_V < 2 * MB) read_v(i + AHEAD_V);
+                    if (odd) {                  // (wave-uniform)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            if ((odd >> (16 * (i / MB) + 8 * (e / 4) + 4 * h + e % 4)) & 1) va[i][e] = (__bf16)0.f;
+                    }
+                    acc[i % MB] = mfma(va[i], hi[i / MB], acc[i % MB]);
+                    acc[i % MB] = mfma(va[i], lo[i / MB], acc[i % MB]);
+                }
+            }
+        }
+
+        // on to the next piece: its first tile is on its way while this one is joined and written
+        const Piece done = now;
+        at += now.last - now.first;
+        const bool last_piece = WHOLE || at >= end;
+        __syncthreads();                        // everyone has read the last tile
+        if (!last_piece) {
+            chunk = 0;
+            if (++unit == units) {
+                unit = 0;
+                do {
+                    ++b;
+                    enter();
+                } while (n_chunks == 0 || units == 0);
+            }
+            now = begin();
+        }
+        l = half_wave_sum(l);
+        const uint64_t some = __builtin_amdgcn_ballot_w64(saw);
+        if (l == 0.f && (((some >> n) | (some >> (32 + n))) & 1)) l = -1.f;
+        if constexpr (SHARING == 2) {
+            // the second wavefront's part, through the buffer that the next tile does not go to
+            float* const other = reinterpret_cast<float*>(lds[1]) + rg * MB * 16 * 64;
+            if (part_of == 1) {
+#pragma unroll
+                for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) other[(mb * 16 + r) * 64 + lane] = acc[mb][r];
+                if (h == 0) {
+                    stat_lds[rg][0][n] = top;
+                    stat_lds[rg][1][n] = l;
+                }
+            }
+            meet();
+            if (part_of == 0) {
+                const float m1 = stat_lds[rg][0][n], l1 = stat_lds[rg][1][n], all = fmaxf(top, m1);
+                const float f0 = __builtin_amdgcn_exp2f(top - reference(all)), f1 = __builtin_amdgcn_exp2f(m1 - reference(all));
+                float sum = 0.f;
+                bool weightless = false;
+                add_sum(sum, weightless, l, f0);
+                add_sum(sum, weightless, l1, f1);
+                l = sum == 0.f && weightless ? -1.f : sum;
+                top = all;
+#pragma unroll
+                for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) acc[mb][r] = acc[mb][r] * f0 + other[(mb * 16 + r) * 64 + lane] * f1;
+            }
+        }
+        const int in_unit = 32 * rg + n;
+        if (part_of == 0 && in_unit < done.rows) {
+            if (done.first == 0 && done.last == done.n_chunks) {
+                // no token: zeros; tokens without any weight: no number
+                const float inv = l < 0.f ? NAN : l == 0.f ? 0.f : 1.f / l;
+                const int at_row = done.row0 + in_unit, i = at_row / group, head = done.kvh * group + at_row - i * group;
+                __bf16* const to = (__bf16*)p.out + done.b * p.stride_b + i * p.stride_t + head * p.stride_h;
+#pragma unroll
+                for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        const int column = 32 * mb + 8 * c + 4 * h;
+                        if (column >= d) continue;
+                        bf16x4 z;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) z[e] = (__bf16)(acc[mb][4 * c + e] * inv);
+                        *reinterpret_cast<bf16x4*>(to + column) = z;
+                    }
+                if (p.lse && h == 0) p.lse[done.b * p.stat_stride_b + i * p.stat_stride_t + head] = l < 0.f ? NAN : (top + __builtin_amdgcn_logf(l)) * LN2;
+            } else {
+                float* const part = p.parts + ((int64_t)mine * 2 + (done.first > 0 ? 0 : 1)) * part_floats(ROWS, DP);
+#pragma unroll
+                for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+                        *reinterpret_cast<float4*>(part + in_unit * DP + 32 * mb + 8 * c + 4 * h) =
+                            make_float4(acc[mb][4 * c], acc[mb][4 * c + 1], acc[mb][4 * c + 2], acc[mb][4 * c + 3]);
+                if (h == 0) {
+                    part[ROWS * DP + in_unit] = top;
+                    part[ROWS * (DP + 1) + in_unit] = l;
+                }
+            }
+        }
+        if (last_piece) break;
+    }
+}
+
 // Units whose pieces lie in several shares, and rows of sequences without a token.  JOIN_WAVES wavefronts take the pieces of a row in turn; a workgroup
 // has eight wavefronts or, where one is enough for a row, four, of which each has a row of its own.
 constexpr int BATCH = 4;
-template <typename T, int DP, int M, int JOIN_WAVES>
+template <typename T, int DP, int CH, int ROWS, int JOIN_WAVES>
 __global__ void __launch_bounds__(JOIN_WAVES == 1 ? 256 : 64 * JOIN_WAVES)
 tree_join_kernel(TreeArgs p) {
-    constexpr int COLS = (DP + 63) / 64, EACH = JOIN_WAVES == 1 ? 4 : 1, ROWS = 16 * M;
+    constexpr int COLS = (DP + 63) / 64, EACH = JOIN_WAVES == 1 ? 4 : 1;
     __shared__ float o_lds[JOIN_WAVES][DP], m_lds[JOIN_WAVES], l_lds[JOIN_WAVES];
     const int lane = threadIdx.x & 63, own_wave = scalar((int)threadIdx.x >> 6), wave = EACH == 1 ? own_wave : 0;
     const int group = p.H / p.H_kv, at_row = (int)blockIdx.x * EACH + (EACH == 1 ? 0 : own_wave);
@@ -593,12 +956,12 @@ tree_join_kernel(TreeArgs p) {
     seq = {scalar(seq.before), scalar(seq.len), scalar(seq.rows)};
     const int kvh = head / group, in_unit = t * group + head - kvh * group;
     if (in_unit >= seq.rows) return;
-    const int n = chunks_of<T>(seq), unit = kvh * (units_of<ROWS>(p, seq) / p.H_kv) + in_unit / ROWS, row = in_unit % ROWS;
+    const int n = chunks_of<CH>(seq), unit = kvh * (units_of<ROWS>(p, seq) / p.H_kv) + in_unit / ROWS, row = in_unit % ROWS;
     // (in one pass: the chunks of the sequences before b, and all)
     int before = 0, all = 0;
 #pragma unroll 4
     for (int b0 = 0; b0 < p.B; b0 += 64) {
-        const int own = b0 + lane < p.B ? work_of<T, ROWS>(p, b0 + lane) : 0;
+        const int own = b0 + lane < p.B ? work_of<CH, ROWS>(p, b0 + lane) : 0;
         all += own;
         before += b0 + lane < b ? own : 0;
     }
@@ -678,35 +1041,39 @@ tree_join_kernel(TreeArgs p) {
 }
 
 constexpr int columns(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : d <= 128 ? 128 : 256; }
-// blocks of 16 rows a unit
-constexpr int blocks_for(int rows, int DP) { return rows <= 16 ? 1 : rows <= 32 || DP > 128 ? 2 : 4; }
-constexpr int workgroups(int DP, int M) { return N_CU * (DP > 128 || M > 2 ? 1 : 2); }
+constexpr int tile_columns(int d) { return d <= 64 ? 64 : 128; }
+// tree_tiles_kernel's launches
+constexpr bool in_tiles(int rows, int d, int dtype) { return dtype == SA_BF16 && d <= 128 && rows > 32; }
+constexpr int row_groups(int rows) { return rows <= 64 ? 2 : 4; }
+// tree_kernel's: blocks of 16 rows a unit
+constexpr int blocks_for(int rows) { return rows <= 16 ? 1 : 2; }
+constexpr int workgroups(int DP) { return N_CU * (DP > 128 ? 1 : 2); }
+
+template <typename T, int DP, int CH, int ROWS>
+hipError_t join(const TreeArgs& a, hipStream_t st) {
+    const int64_t all = (int64_t)a.B * a.T * a.H;
+    if (all <= 512) hipLaunchKernelGGL((tree_join_kernel<T, DP, CH, ROWS, 8>), dim3((unsigned)all), dim3(64 * 8), 0, st, a);
+    else hipLaunchKernelGGL((tree_join_kernel<T, DP, CH, ROWS, 1>), dim3((unsigned)((all + 3) / 4)), dim3(64 * 4), 0, st, a);
+    return hipGetLastError();
+}
+template <int ROWS>
+unsigned all_units(const TreeArgs& a) { return (unsigned)(a.B * a.H_kv * ((a.T * (a.H / a.H_kv) + ROWS - 1) / ROWS)); }
 
 template <typename T, int DP, int M>
 hipError_t launch(TreeArgs a, hipStream_t st) {
-    const int rows = a.T * (a.H / a.H_kv);
     // (decode.hip's rule for units of a workgroup each)
     if ((int64_t)a.max_pages * a.page_size <= (DP > 128 ? 4 : 8) * CHUNK<T>) {
-        hipLaunchKernelGGL((tree_kernel<T, DP, M, true>), dim3((unsigned)(a.B * a.H_kv * ((rows + 16 * M - 1) / (16 * M)))), dim3(64 * WAVES), 0, st, a);
+        hipLaunchKernelGGL((tree_kernel<T, DP, M, true>), dim3(all_units<16 * M>(a)), dim3(64 * WAVES), 0, st, a);
         return hipGetLastError();
     }
-    a.n_wgs = workgroups(DP, M);
+    a.n_wgs = workgroups(DP);
     hipLaunchKernelGGL((tree_kernel<T, DP, M, false>), dim3((unsigned)a.n_wgs), dim3(64 * WAVES), 0, st, a);
     if (hipError_t e = hipGetLastError()) return e;
-    const int64_t all = (int64_t)a.B * a.T * a.H;
-    if (all <= 512) hipLaunchKernelGGL((tree_join_kernel<T, DP, M, 8>), dim3((unsigned)all), dim3(64 * 8), 0, st, a);
-    else hipLaunchKernelGGL((tree_join_kernel<T, DP, M, 1>), dim3((unsigned)((all + 3) / 4)), dim3(64 * 4), 0, st, a);
-    return hipGetLastError();
+    return join<T, DP, CHUNK<T>, 16 * M>(a, st);
 }
 template <typename T, int DP>
 hipError_t launch(const TreeArgs& a, hipStream_t st) {
-    switch (blocks_for(a.T * (a.H / a.H_kv), DP)) {
-        case 1: return launch<T, DP, 1>(a, st);
-        case 2: return launch<T, DP, 2>(a, st);
-        default:
-            if constexpr (DP <= 128) return launch<T, DP, 4>(a, st);
-            return hipErrorInvalidValue;        // (not reached: blocks_for)
-    }
+    return blocks_for(a.T * (a.H / a.H_kv)) == 1 ? launch<T, DP, 1>(a, st) : launch<T, DP, 2>(a, st);
 }
 template <typename T>
 hipError_t launch(const TreeArgs& a, hipStream_t st) {
@@ -717,16 +1084,36 @@ hipError_t launch(const TreeArgs& a, hipStream_t st) {
         default: return launch<T, 256>(a, st);
     }
 }
+template <int DP, int R, bool PART>
+hipError_t launch_tiles(TreeArgs a, hipStream_t st) {
+    if ((int64_t)a.max_pages * a.page_size <= 16 * TILE_CHUNK) {
+        hipLaunchKernelGGL((tree_tiles_kernel<DP, R, PART, true>), dim3(all_units<32 * R>(a)), dim3(64 * WAVES), 0, st, a);
+        return hipGetLastError();
+    }
+    a.n_wgs = workgroups(DP);
+    hipLaunchKernelGGL((tree_tiles_kernel<DP, R, PART, false>), dim3((unsigned)a.n_wgs), dim3(64 * WAVES), 0, st, a);
+    if (hipError_t e = hipGetLastError()) return e;
+    return join<__hip_bfloat16, DP, TILE_CHUNK, 32 * R>(a, st);
+}
+template <int DP, bool PART>
+hipError_t launch_tiles(const TreeArgs& a, hipStream_t st) {
+    return row_groups(a.T * (a.H / a.H_kv)) == 2 ? launch_tiles<DP, 2, PART>(a, st) : launch_tiles<DP, 4, PART>(a, st);
+}
 
 }  // namespace
 
-int64_t tree_workspace(int rows, int d) {
-    const int DP = columns(d), M = blocks_for(rows, DP);
-    return (int64_t)workgroups(DP, M) * 2 * part_floats(16 * M, DP) * 4;
+int64_t tree_workspace(int rows, int d, int dtype) {
+    if (in_tiles(rows, d, dtype)) return (int64_t)workgroups(tile_columns(d)) * 2 * part_floats(32 * row_groups(rows), tile_columns(d)) * 4;
+    return (int64_t)workgroups(columns(d)) * 2 * part_floats(16 * blocks_for(rows), columns(d)) * 4;
 }
 
 hipError_t launch_tree(const TreeArgs& a, int dtype, hipStream_t st) {
-    return dtype == SA_F32 ? launch<float>(a, st) : launch<__hip_bfloat16>(a, st);
+    if (dtype == SA_F32) return launch<float>(a, st);
+    if (in_tiles(a.T * (a.H / a.H_kv), a.d, dtype)) {
+        if (a.d <= 64) return a.d % 8 ? launch_tiles<64, true>(a, st) : launch_tiles<64, false>(a, st);
+        return a.d % 8 ? launch_tiles<128, true>(a, st) : launch_tiles<128, false>(a, st);
+    }
+    return launch<__hip_bfloat16>(a, st);
 }
 
 }  // namespace sa
