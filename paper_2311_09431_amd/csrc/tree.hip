@@ -1,13 +1,13 @@
 // Attention of drafted tokens over the paged cache: each of a sequence's drafted tokens over all tokens in front of the draft and those of the draft that
 // its mask names.
 //
-// As decode.hip has it for one token, with the rows of a unit, its matrix products' right side, more than one block of 16: a unit is (sequence, key/value
-// head, 16 M of the sequence's rows), row i G + g being drafted token i and query head g of the group of G.  Tiles of tokens are loaded once for
-// all M blocks; units that share a key/value head are neighbours, so that what one reads of the cache lies near for the other.  Shares of
-// chunks, the four wavefronts' own references and sums and the joining of pieces are as there.
+// As decode.hip has it for one token, with rows in the place of query heads: a unit is (sequence, key/value head, 16, 64 or 128 of the sequence's rows), row
+// i G + g being drafted token i and query head g of the group of G.  Shares of chunks, references and sums of their own for wavefronts and pieces,
+// and the joining of pieces in a second launch are as there; a sequence has as many units as its own draft needs.  Two kernels: tree_kernel takes 16 rows
+// with everything in registers, as a new token's heads; tree_tiles_kernel more, through LDS.
 //
 // What a row does not see has a score of -inf.  Its weight of zero would still make a NaN of an infinite or NaN value, so such tokens are taken out of the
-// products (`odd_values`) and added to the rows that see them by vector instructions; only tiles with drafted tokens are looked at for them.
+// products and added to the rows that see them by vector instructions; only tiles with drafted tokens are looked at for them.
 #include <hip/hip_bf16.h>
 
 #include "mfma_tiles.h"
@@ -115,14 +115,14 @@ template <int ES> __device__ inline float element(const uint32_t* words, int i) 
 }
 
 // WHOLE: a workgroup has one unit, all of it, and there is nothing to join.
-template <typename T, int DP, int M, bool WHOLE>
+template <typename T, int DP, bool WHOLE>
 __global__ void __launch_bounds__(64 * WAVES, DP > 128 ? 1 : 2)
 tree_kernel(TreeArgs p) {
     using O = Of<T, DP>;
     constexpr int TILE = O::TILE, CW = O::CW, ES = O::ES, KS = DP / O::STEP, NM = DP / (16 * CW), NB = DP / 16;
     constexpr bool BF16 = ES == 2;
     constexpr int BLOCKS = TILE / 16, TOKENS = 4 * BLOCKS;      // 16-token blocks of a tile, tokens a lane holds of it
-    constexpr int PITCH = DP + 4, ROWS = 16 * M, CH = CHUNK<T>;
+    constexpr int PITCH = DP + 4, ROWS = 16, CH = CHUNK<T>;
     __shared__ __attribute__((aligned(16))) float o_lds[WAVES][ROWS][PITCH];
     __shared__ float m_lds[WAVES][ROWS], l_lds[WAVES][ROWS];
 
@@ -187,8 +187,8 @@ tree_kernel(TreeArgs p) {
     // joined and written.
     struct Piece { int b, kvh, row0, rows, first, last, n_chunks, before, len; };
     Piece now;
-    u32x4 q[M][KS];
-    uint64_t sees[M];                           // the row's mask
+    u32x4 q[KS];
+    uint64_t sees;                              // the row's mask
     int t0;                                     // this wavefront's next tile: tokens t0 .. t0 + TILE - 1, CH further on the one after it
     // page and place in it of each of its 16-token blocks
     const int step_page = CH / p.page_size, step_in = CH - step_page * p.page_size;
@@ -263,27 +263,30 @@ tree_kernel(TreeArgs p) {
     auto request = [&]() {
         const int blocks = units / p.H_kv, kvh = unit / blocks, row0 = (unit - kvh * blocks) * ROWS;
         const Piece next = {b, kvh, row0, min(ROWS, seq.rows - row0), chunk, min(n_chunks, chunk + (end - at)), n_chunks, seq.before, seq.len};
+        const bool has_row = n < next.rows;
+        const int row = row0 + (has_row ? n : 0), i = row / group, head = kvh * group + row - i * group;
+        const T* q_row = (const T*)p.q + b * p.stride_b + i * p.stride_t + head * p.stride_h;
+        sees = has_row ? (uint64_t)p.seen[b * p.seen_stride + i] : 0;
+        // (all requested at once, without branches: from the row's last 16 bytes where a chunk goes beyond them; a row of eight bytes twice)
+        typedef uint32_t Chunk __attribute__((ext_vector_type(4), aligned(8)));
+        typedef uint32_t Half __attribute__((ext_vector_type(2)));
+        constexpr int E = BF16 ? 8 : 4;
 #pragma unroll
-        for (int m = 0; m < M; ++m) {
-            const bool has_row = 16 * m + n < next.rows;
-            const int row = row0 + (has_row ? 16 * m + n : 0), i = row / group, head = kvh * group + row - i * group;
-            const T* q_row = (const T*)p.q + b * p.stride_b + i * p.stride_t + head * p.stride_h;
-            sees[m] = has_row ? (uint64_t)p.seen[b * p.seen_stride + i] : 0;
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks) {
-                constexpr int E = BF16 ? 8 : 4;
-                const int col = O::STEP * ks + E * j;
-                q[m][ks] = u32x4{0, 0, 0, 0};
-                if (has_row && col < d) {
-                    if (!BF16 || col + 8 <= d) q[m][ks] = *reinterpret_cast<const u32x4*>(q_row + col);
-                    else {
-                        const u32x2 x = *reinterpret_cast<const u32x2*>(q_row + col);
-                        q[m][ks][0] = x[0];
-                        q[m][ks][1] = x[1];
-                    }
-                }
+        for (int ks = 0; ks < KS; ++ks) {
+            if (BF16 && d < 8) {
+                const Half x = *reinterpret_cast<const Half*>(q_row);
+                q[ks] = u32x4{x[0], x[1], 0, 0};
+            } else {
+                q[ks] = *reinterpret_cast<const Chunk*>(q_row + min(O::STEP * ks + E * j, d - E));
             }
         }
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                const int col = O::STEP * ks + (BF16 ? 8 : 4) * j;
+                const u32x4 x = q[ks];
+                if (col >= d) q[ks] = u32x4{0, 0, 0, 0};
+                else if (BF16 && col + 8 > d && d >= 8) q[ks] = u32x4{x[2], x[3], 0, 0};
+            }
         t0 = next.first * CH + wave * TILE;
 #pragma unroll
         for (int i = 0; i < BLOCKS; ++i) {
@@ -303,23 +306,16 @@ tree_kernel(TreeArgs p) {
     now = request();
     for (;;) {
         const int t_end = min(now.len, now.last * CH);
-        f32x4 acc[M][NB];
-        float top[M], l[M];
-        bool saw[M];                            // some token that the row sees, in a page that is one
+        f32x4 acc[NB];
+        float top = -INFINITY, l = 0.f;
+        bool saw = false;                       // some token that the row sees, in a page that is one
 #pragma unroll
-        for (int m = 0; m < M; ++m) {
-#pragma unroll
-            for (int i = 0; i < NB; ++i) acc[m][i] = f32x4{0.f, 0.f, 0.f, 0.f};
-            top[m] = -INFINITY;
-            l[m] = 0.f;
-            saw[m] = false;
-        }
+        for (int i = 0; i < NB; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
         for (; t0 < t_end; t0 += CH) {
-            f32x4 s[M][BLOCKS];
+            f32x4 s[BLOCKS];
 #pragma unroll
             for (int i = 0; i < BLOCKS; ++i) {
-#pragma unroll
-                for (int m = 0; m < M; ++m) s[m][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+                s[i] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int ks = 0; ks < KS; ++ks) {
                     u32x4 x = k[i][ks];
@@ -327,13 +323,10 @@ tree_kernel(TreeArgs p) {
                         x[2] = ks == part_ks ? 0 : x[2];
                         x[3] = ks == part_ks ? 0 : x[3];
                     }
+                    if constexpr (BF16) s[i] = mfma_bf16(x, q[ks], s[i]);
+                    else {
 #pragma unroll
-                    for (int m = 0; m < M; ++m) {
-                        if constexpr (BF16) s[m][i] = mfma_bf16(x, q[m][ks], s[m][i]);
-                        else {
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) s[m][i] = mfma_f32(x[e], q[m][ks][e], s[m][i]);
-                        }
+                        for (int e = 0; e < 4; ++e) s[i] = mfma_f32(x[e], q[ks][e], s[i]);
                     }
                 }
             }
@@ -352,52 +345,46 @@ tree_kernel(TreeArgs p) {
                 place(t0 + CH);
                 load_k();
             }
-            // a lane's token x of the tile is seen by its row of block m
-            auto seen = [&](int m, int x) {
+            // a lane's token x of the tile is seen by its row
+            auto seen = [&](int x) {
                 const int row = 4 * j + x % 4, nth = tile_at + 16 * (x / 4) + row - now.before;        // of the draft; negative: before it
-                return row < rows[x / 4] && (nth < 0 || ((sees[m] >> (nth & 63)) & 1));
+                return row < rows[x / 4] && (nth < 0 || ((sees >> (nth & 63)) & 1));
             };
             if (!whole) {
 #pragma unroll
-                for (int m = 0; m < M; ++m)
-#pragma unroll
                     for (int x = 0; x < TOKENS; ++x) {
-                        const bool sees_it = seen(m, x);
-                        saw[m] = saw[m] || sees_it;
-                        if (!sees_it) s[m][x / 4][x % 4] = -INFINITY;
+                        const bool sees_it = seen(x);
+                        saw = saw || sees_it;
+                        if (!sees_it) s[x / 4][x % 4] = -INFINITY;
                     }
             } else {
-#pragma unroll
-                for (int m = 0; m < M; ++m) saw[m] = true;
+                saw = true;
             }
-            float pr[M][TOKENS];
+            float pr[TOKENS];
+            float sum = 0.f;
 #pragma unroll
-            for (int m = 0; m < M; ++m) {
-                float sum = 0.f;
+            for (int x = 0; x < TOKENS; ++x) {
+                pr[x] = __builtin_amdgcn_exp2f(fmaf(s[x / 4][x % 4], kappa, -top));
+                sum += pr[x];
+            }
+            if (__builtin_amdgcn_ballot_w64(!(sum < MOST)) != 0) {          // wave-uniform and rare but for the first tile
+                float mx = s[0][0];
+#pragma unroll
+                for (int x = 1; x < TOKENS; ++x) mx = fmaxf(mx, s[x / 4][x % 4]);
+                const float m_new = fmaxf(top, quad_max(mx) * kappa), ref = m_new == -INFINITY ? 0.f : m_new;
+                const float alpha = __builtin_amdgcn_exp2f(top - ref);
+                top = m_new;
+                l *= alpha;
+#pragma unroll
+                for (int i = 0; i < NB; ++i) acc[i] *= alpha;
+                sum = 0.f;
 #pragma unroll
                 for (int x = 0; x < TOKENS; ++x) {
-                    pr[m][x] = __builtin_amdgcn_exp2f(fmaf(s[m][x / 4][x % 4], kappa, -top[m]));
-                    sum += pr[m][x];
+                    pr[x] = __builtin_amdgcn_exp2f(fmaf(s[x / 4][x % 4], kappa, -ref));
+                    sum += pr[x];
                 }
-                if (__builtin_amdgcn_ballot_w64(!(sum < MOST)) != 0) {          // wave-uniform and rare but for the first tile
-                    float mx = s[m][0][0];
-#pragma unroll
-                    for (int x = 1; x < TOKENS; ++x) mx = fmaxf(mx, s[m][x / 4][x % 4]);
-                    const float m_new = fmaxf(top[m], quad_max(mx) * kappa), ref = m_new == -INFINITY ? 0.f : m_new;
-                    const float alpha = __builtin_amdgcn_exp2f(top[m] - ref);
-                    top[m] = m_new;
-                    l[m] *= alpha;
-#pragma unroll
-                    for (int i = 0; i < NB; ++i) acc[m][i] *= alpha;
-                    sum = 0.f;
-#pragma unroll
-                    for (int x = 0; x < TOKENS; ++x) {
-                        pr[m][x] = __builtin_amdgcn_exp2f(fmaf(s[m][x / 4][x % 4], kappa, -ref));
-                        sum += pr[m][x];
-                    }
-                }
-                l[m] += sum;
             }
+            l += sum;
             if (drafted) {
                 // values that are no numbers, of tokens that some rows do not see
                 bool odd_values = false;
@@ -419,20 +406,17 @@ tree_kernel(TreeArgs p) {
 #pragma unroll 1
                         for (int jj = 0; jj < 4; ++jj) {
                             if (!((who >> (16 * jj)) & 0xffff)) continue;
+                            const float w = __shfl(pr[x], 16 * jj + n);
+                            const bool sees_it = __shfl((int)seen(x), 16 * jj + n) != 0;
 #pragma unroll
-                            for (int m = 0; m < M; ++m) {
-                                const float w = __shfl(pr[m][x], 16 * jj + n);
-                                const bool sees_it = __shfl((int)seen(m, x), 16 * jj + n) != 0;
+                            for (int y = 0; y < NM; ++y)
 #pragma unroll
-                                for (int y = 0; y < NM; ++y)
+                                for (int c = 0; c < CW; ++c)
 #pragma unroll
-                                    for (int c = 0; c < CW; ++c)
-#pragma unroll
-                                        for (int r = 0; r < 4; ++r) {
-                                            const float value = __shfl(element<ES>(v[x][y], c), 16 * jj + 4 * j + r);
-                                            if (sees_it) acc[m][y * CW + c][r] += w * value;
-                                        }
-                            }
+                                    for (int r = 0; r < 4; ++r) {
+                                        const float value = __shfl(element<ES>(v[x][y], c), 16 * jj + 4 * j + r);
+                                        if (sees_it) acc[y * CW + c][r] += w * value;
+                                    }
                         }
                         if ((who >> (16 * j)) & 0xffff) {
 #pragma unroll
@@ -444,18 +428,13 @@ tree_kernel(TreeArgs p) {
                 }
             }
             if constexpr (BF16) {
-                u32x4 ph[M], pl[M];
+                bf16x8 hi, lo;
 #pragma unroll
-                for (int m = 0; m < M; ++m) {
-                    bf16x8 hi, lo;
-#pragma unroll
-                    for (int x = 0; x < 8; ++x) {
-                        hi[x] = (__bf16)pr[m][x];
-                        lo[x] = (__bf16)(pr[m][x] - (float)hi[x]);
-                    }
-                    ph[m] = __builtin_bit_cast(u32x4, hi);
-                    pl[m] = __builtin_bit_cast(u32x4, lo);
+                for (int x = 0; x < 8; ++x) {
+                    hi[x] = (__bf16)pr[x];
+                    lo[x] = (__bf16)(pr[x] - (float)hi[x]);
                 }
+                const u32x4 ph = __builtin_bit_cast(u32x4, hi), pl = __builtin_bit_cast(u32x4, lo);
 #pragma unroll
                 for (int x = 0; x < NM; ++x)
 #pragma unroll
@@ -464,10 +443,8 @@ tree_kernel(TreeArgs p) {
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
                             a[e] = __builtin_amdgcn_perm(v[2 * e + 1][x][c / 2], v[2 * e][x][c / 2], c % 2 ? 0x07060302u : 0x05040100u);
-#pragma unroll
-                        for (int m = 0; m < M; ++m) acc[m][x * CW + c] = mfma_bf16(a, ph[m], acc[m][x * CW + c]);
-#pragma unroll
-                        for (int m = 0; m < M; ++m) acc[m][x * CW + c] = mfma_bf16(a, pl[m], acc[m][x * CW + c]);
+                        acc[x * CW + c] = mfma_bf16(a, ph, acc[x * CW + c]);
+                        acc[x * CW + c] = mfma_bf16(a, pl, acc[x * CW + c]);
                     }
             } else {
 #pragma unroll
@@ -476,9 +453,7 @@ tree_kernel(TreeArgs p) {
                     for (int x = 0; x < NM; ++x)
 #pragma unroll
                         for (int c = 0; c < CW; ++c)
-#pragma unroll
-                            for (int m = 0; m < M; ++m)
-                                acc[m][x * CW + c] = mfma_f32(v[r][x][c], __float_as_uint(pr[m][r]), acc[m][x * CW + c]);
+                                acc[x * CW + c] = mfma_f32(v[r][x][c], __float_as_uint(pr[r]), acc[x * CW + c]);
             }
             if (more) {
                 keep_place();
@@ -503,32 +478,26 @@ tree_kernel(TreeArgs p) {
         }
 
         // the four wavefronts' parts
-#pragma unroll
-        for (int m = 0; m < M; ++m) {
-            l[m] = quad_sum(l[m]);
-            const uint64_t some = __builtin_amdgcn_ballot_w64(saw[m]);
-            if (l[m] == 0.f && (((some >> n) | (some >> (16 + n)) | (some >> (32 + n)) | (some >> (48 + n))) & 1)) l[m] = -1.f;
-            if (j == 0) {
-                m_lds[wave][16 * m + n] = top[m];
-                l_lds[wave][16 * m + n] = l[m];
-            }
+        l = quad_sum(l);
+        const uint64_t some = __builtin_amdgcn_ballot_w64(saw);
+        if (l == 0.f && (((some >> n) | (some >> (16 + n)) | (some >> (32 + n)) | (some >> (48 + n))) & 1)) l = -1.f;
+        if (j == 0) {
+            m_lds[wave][n] = top;
+            l_lds[wave][n] = l;
         }
         __syncthreads();
+        float all = m_lds[0][n];
 #pragma unroll
-        for (int m = 0; m < M; ++m) {
-            float all = m_lds[0][16 * m + n];
+        for (int w = 1; w < WAVES; ++w) all = fmaxf(all, m_lds[w][n]);
+        const float own = __builtin_amdgcn_exp2f(top - reference(all));
 #pragma unroll
-            for (int w = 1; w < WAVES; ++w) all = fmaxf(all, m_lds[w][16 * m + n]);
-            const float own = __builtin_amdgcn_exp2f(top[m] - reference(all));
+        for (int x = 0; x < NM; ++x)
 #pragma unroll
-            for (int x = 0; x < NM; ++x)
+            for (int r = 0; r < 4; ++r)
 #pragma unroll
-                for (int r = 0; r < 4; ++r)
-#pragma unroll
-                    for (int c = 0; c < CW; c += 2)
-                        *reinterpret_cast<float2*>(&o_lds[wave][16 * m + n][16 * CW * x + CW * (4 * j + r) + c]) =
-                            make_float2(acc[m][x * CW + c][r] * own, acc[m][x * CW + c + 1][r] * own);
-        }
+                for (int c = 0; c < CW; c += 2)
+                    *reinterpret_cast<float2*>(&o_lds[wave][n][16 * CW * x + CW * (4 * j + r) + c]) =
+                        make_float2(acc[x * CW + c][r] * own, acc[x * CW + c + 1][r] * own);
         __syncthreads();
         const bool complete = done.first == 0 && done.last == done.n_chunks;
         // (a share's piece of a unit that began in another one is its first, of one that ends in another its last)
@@ -576,7 +545,7 @@ tree_kernel(TreeArgs p) {
     }
 }
 
-// bf16, up to 128 columns, more than 32 rows a key/value head: as attention of whole blocks has it, tiles of 64 tokens go straight into LDS (mfma_tiles.h),
+// bf16, up to 128 columns, more than 16 rows a key/value head: as attention of whole blocks has it, tiles of 64 tokens go straight into LDS (mfma_tiles.h),
 // two buffers, and R groups of 32 rows read them; S^T = K Q^T and O^T += V^T P^T by 32 x 32 products, a lane holding 16 tokens of one row.  R = 4: a
 // wavefront each; R = 2: two wavefronts each, of which either takes 32 tokens of a tile, joined at the end of a piece.  A tile is requested while the one
 // before it is computed, each wavefront one 16-token block of it: its page, its descriptor.
@@ -940,24 +909,13 @@ tree_tiles_kernel(TreeArgs p) {
     }
 }
 
-// Units whose pieces lie in several shares, and rows of sequences without a token.  JOIN_WAVES wavefronts take the pieces of a row in turn; a workgroup
-// has eight wavefronts or, where one is enough for a row, four, of which each has a row of its own.
-constexpr int BATCH = 4;
-template <typename T, int DP, int CH, int ROWS, int JOIN_WAVES>
-__global__ void __launch_bounds__(JOIN_WAVES == 1 ? 256 : 64 * JOIN_WAVES)
-tree_join_kernel(TreeArgs p) {
-    constexpr int COLS = (DP + 63) / 64, EACH = JOIN_WAVES == 1 ? 4 : 1;
-    __shared__ float o_lds[JOIN_WAVES][DP], m_lds[JOIN_WAVES], l_lds[JOIN_WAVES];
-    const int lane = threadIdx.x & 63, own_wave = scalar((int)threadIdx.x >> 6), wave = EACH == 1 ? own_wave : 0;
-    const int group = p.H / p.H_kv, at_row = (int)blockIdx.x * EACH + (EACH == 1 ? 0 : own_wave);
-    const int b = at_row / (p.T * p.H), t = (at_row - b * p.T * p.H) / p.H, head = at_row - (b * p.T + t) * p.H;
-    if (b >= p.B) return;
-    Sequence seq = sequence(p, b);
-    seq = {scalar(seq.before), scalar(seq.len), scalar(seq.rows)};
-    const int kvh = head / group, in_unit = t * group + head - kvh * group;
-    if (in_unit >= seq.rows) return;
-    const int n = chunks_of<CH>(seq), unit = kvh * (units_of<ROWS>(p, seq) / p.H_kv) + in_unit / ROWS, row = in_unit % ROWS;
-    // (in one pass: the chunks of the sequences before b, and all)
+// Units whose pieces lie in several shares, and rows of sequences without a token.
+
+// Where the pieces of a unit lie: shares g0 .. g1; the chunks before it and all, in one pass over the sequences.
+struct Pieces { int g0, g1, n; };       // n: chunks (0: no token)
+template <int CH, int ROWS>
+__device__ inline Pieces pieces_of(const TreeArgs& p, const Sequence& seq, int b, int kvh, int in_unit, int lane) {
+    const int n = chunks_of<CH>(seq), unit = kvh * (units_of<ROWS>(p, seq) / p.H_kv) + in_unit / ROWS;
     int before = 0, all = 0;
 #pragma unroll 4
     for (int b0 = 0; b0 < p.B; b0 += 64) {
@@ -968,22 +926,43 @@ tree_join_kernel(TreeArgs p) {
     all = wave_total(wave_scan(all));
     before = wave_total(wave_scan(before));
     const uint32_t share = (uint32_t)share_of(all, p.n_wgs), from = (uint32_t)(before + unit * n);
-    const int g0 = (int)(from / share), g1 = n ? (int)((from + n - 1) / share) : g0;
-    if (n && g0 == g1) return;
-    // a wavefront's pieces, BATCH of them requested at a time (they come from other XCDs' workgroups: a round trip to memory each)
-    const int pieces = n ? g1 - g0 + 1 : 0;
+    const int g0 = (int)(from / share);
+    return {g0, n ? (int)((from + n - 1) / share) : g0, n};
+}
+template <int DP, int ROWS>
+__device__ inline const float* piece(const TreeArgs& p, const Pieces& x, int i) {
+    return p.parts + ((int64_t)(x.g0 + i) * 2 + (i == 0 ? 1 : 0)) * part_floats(ROWS, DP);
+}
+
+// Few rows, whose units then have many pieces: eight wavefronts take a row's in turn, BATCH of them requested at a time (they come from other XCDs'
+// workgroups: a round trip to memory each).
+constexpr int BATCH = 4, JOIN_WAVES = 8;
+template <typename T, int DP, int CH, int ROWS>
+__global__ void __launch_bounds__(64 * JOIN_WAVES)
+tree_join_kernel(TreeArgs p) {
+    constexpr int COLS = (DP + 63) / 64;
+    __shared__ float o_lds[JOIN_WAVES][DP], m_lds[JOIN_WAVES], l_lds[JOIN_WAVES];
+    const int lane = threadIdx.x & 63, wave = scalar((int)threadIdx.x >> 6);
+    const int group = p.H / p.H_kv, at_row = (int)blockIdx.x;
+    const int b = at_row / (p.T * p.H), t = (at_row - b * p.T * p.H) / p.H, head = at_row - (b * p.T + t) * p.H;
+    Sequence seq = sequence(p, b);
+    seq = {scalar(seq.before), scalar(seq.len), scalar(seq.rows)};
+    const int kvh = head / group, in_unit = t * group + head - kvh * group, row = in_unit % ROWS;
+    if (in_unit >= seq.rows) return;
+    const Pieces x = pieces_of<CH, ROWS>(p, seq, b, kvh, in_unit, lane);
+    if (x.n && x.g0 == x.g1) return;
+    const int pieces = x.n ? x.g1 - x.g0 + 1 : 0;
     float m = -INFINITY, l = 0.f, acc[COLS] = {};
     bool weightless = false;
     for (int i0 = wave * BATCH; i0 < pieces; i0 += JOIN_WAVES * BATCH) {
-        float mg[BATCH], lg[BATCH], x[BATCH][COLS];
+        float mg[BATCH], lg[BATCH], y[BATCH][COLS];
 #pragma unroll
         for (int i = 0; i < BATCH; ++i) {
-            const int at = min(i0 + i, pieces - 1);
-            const float* part = p.parts + ((int64_t)(g0 + at) * 2 + (at == 0 ? 1 : 0)) * part_floats(ROWS, DP);
+            const float* part = piece<DP, ROWS>(p, x, min(i0 + i, pieces - 1));
             mg[i] = part[ROWS * DP + row];
             lg[i] = part[ROWS * (DP + 1) + row];
 #pragma unroll
-            for (int c = 0; c < COLS; ++c) x[i][c] = lane + 64 * c < p.d ? part[row * DP + lane + 64 * c] : 0.f;
+            for (int c = 0; c < COLS; ++c) y[i][c] = lane + 64 * c < p.d ? part[row * DP + lane + 64 * c] : 0.f;
         }
 #pragma unroll
         for (int i = 0; i < BATCH; ++i) {
@@ -992,23 +971,9 @@ tree_join_kernel(TreeArgs p) {
             l *= a;
             add_sum(l, weightless, lg[i], f);
 #pragma unroll
-            for (int c = 0; c < COLS; ++c) acc[c] = acc[c] * a + x[i][c] * f;
+            for (int c = 0; c < COLS; ++c) acc[c] = acc[c] * a + y[i][c] * f;
             m = top;
         }
-    }
-    T* const to = (T*)p.out + b * p.stride_b + t * p.stride_t + head * p.stride_h;
-    float* const lse = p.lse ? p.lse + b * p.stat_stride_b + t * p.stat_stride_t + head : nullptr;
-    if constexpr (JOIN_WAVES == 1) {
-        if (weightless && l == 0.f) l = NAN;
-        const float inv = l == 0.f ? 0.f : 1.f / l;
-#pragma unroll
-        for (int c = 0; c < COLS; ++c)
-            if (lane + 64 * c < p.d) {
-                if constexpr (sizeof(T) == 2) reinterpret_cast<__bf16*>(to)[lane + 64 * c] = (__bf16)(acc[c] * inv);
-                else to[lane + 64 * c] = acc[c] * inv;
-            }
-        if (lse && lane == 0) *lse = (m + __builtin_amdgcn_logf(l)) * LN2;
-        return;
     }
 #pragma unroll
     for (int c = 0; c < COLS; ++c)
@@ -1030,6 +995,7 @@ tree_join_kernel(TreeArgs p) {
     }
     if (sum == 0.f && weightless) sum = NAN;
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    T* const to = (T*)p.out + b * p.stride_b + t * p.stride_t + head * p.stride_h;
     for (int col = threadIdx.x; col < p.d; col += 64 * JOIN_WAVES) {
         float y = 0.f;
 #pragma unroll
@@ -1037,43 +1003,102 @@ tree_join_kernel(TreeArgs p) {
         if constexpr (sizeof(T) == 2) reinterpret_cast<__bf16*>(to)[col] = (__bf16)(y * inv);
         else to[col] = y * inv;
     }
-    if (lse && threadIdx.x == 0) *lse = (top + __builtin_amdgcn_logf(sum)) * LN2;
+    if (p.lse && threadIdx.x == 0) p.lse[b * p.stat_stride_b + t * p.stat_stride_t + head] = (top + __builtin_amdgcn_logf(sum)) * LN2;
+}
+
+// Many rows: a wavefront has four neighbouring ones of a unit, 16 lanes each, which have their pieces in common.  (A wavefront a row: 21 us for 32 sequences'
+// drafts of up to 32, 32 heads, where this takes JOIN_US.)
+template <typename T, int DP, int CH, int ROWS>
+__global__ void __launch_bounds__(256)
+tree_join_rows_kernel(TreeArgs p) {
+    constexpr int COLS = DP / 16, TWO = 2;      // columns a lane; pieces requested at a time
+    typedef float Floats __attribute__((ext_vector_type(COLS < 4 ? COLS : 4)));
+    constexpr int W = COLS < 4 ? COLS : 4, N = COLS / W;
+    const int lane = threadIdx.x & 63, group = p.H / p.H_kv, fours = (p.T * group + 3) / 4;
+    const int at = scalar((int)blockIdx.x * 4 + ((int)threadIdx.x >> 6)), b = at / (p.H_kv * fours), kvh = (at - b * p.H_kv * fours) / fours;
+    if (b >= p.B) return;
+    const int first = 4 * (at - (b * p.H_kv + kvh) * fours), in_unit = first + lane / 16, row = in_unit % ROWS;
+    Sequence seq = sequence(p, b);
+    seq = {scalar(seq.before), scalar(seq.len), scalar(seq.rows)};
+    if (first >= seq.rows) return;
+    const Pieces x = pieces_of<CH, ROWS>(p, seq, b, kvh, first, lane);
+    if (x.n && x.g0 == x.g1) return;
+    const int pieces = x.n ? x.g1 - x.g0 + 1 : 0;
+    float m = -INFINITY, l = 0.f;
+    Floats acc[N] = {};
+    bool weightless = false;
+    for (int i0 = 0; i0 < pieces; i0 += TWO) {
+        float mg[TWO], lg[TWO];
+        Floats y[TWO][N];
+#pragma unroll
+        for (int i = 0; i < TWO; ++i) {
+            const float* part = piece<DP, ROWS>(p, x, min(i0 + i, pieces - 1));
+            mg[i] = part[ROWS * DP + row];
+            lg[i] = part[ROWS * (DP + 1) + row];
+#pragma unroll
+            for (int c = 0; c < N; ++c) y[i][c] = *reinterpret_cast<const Floats*>(part + row * DP + W * (lane % 16 + 16 * c));
+        }
+#pragma unroll
+        for (int i = 0; i < TWO; ++i) {
+            if (i0 + i >= pieces) break;
+            const float top = fmaxf(m, mg[i]), a = __builtin_amdgcn_exp2f(m - reference(top)), f = __builtin_amdgcn_exp2f(mg[i] - reference(top));
+            l *= a;
+            add_sum(l, weightless, lg[i], f);
+#pragma unroll
+            for (int c = 0; c < N; ++c) acc[c] = acc[c] * a + y[i][c] * f;
+            m = top;
+        }
+    }
+    if (in_unit >= seq.rows) return;
+    if (weightless && l == 0.f) l = NAN;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const int t = in_unit / group, head = kvh * group + in_unit - t * group;
+    T* const to = (T*)p.out + b * p.stride_b + t * p.stride_t + head * p.stride_h;
+#pragma unroll
+    for (int c = 0; c < N; ++c) {
+        const int col = W * (lane % 16 + 16 * c);
+        if (col >= p.d) continue;
+        if constexpr (sizeof(T) == 2) {
+            typedef __bf16 Out __attribute__((ext_vector_type(W)));
+            Out z;
+#pragma unroll
+            for (int e = 0; e < W; ++e) z[e] = (__bf16)(acc[c][e] * inv);
+            *reinterpret_cast<Out*>(to + col) = z;
+        } else {
+            *reinterpret_cast<Floats*>(to + col) = acc[c] * inv;
+        }
+    }
+    if (p.lse && lane % 16 == 0) p.lse[b * p.stat_stride_b + t * p.stat_stride_t + head] = (m + __builtin_amdgcn_logf(l)) * LN2;
 }
 
 constexpr int columns(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : d <= 128 ? 128 : 256; }
 constexpr int tile_columns(int d) { return d <= 64 ? 64 : 128; }
 // tree_tiles_kernel's launches
-constexpr bool in_tiles(int rows, int d, int dtype) { return dtype == SA_BF16 && d <= 128 && rows > 32; }
+constexpr bool in_tiles(int rows, int d, int dtype) { return dtype == SA_BF16 && d <= 128 && rows > 16; }
 constexpr int row_groups(int rows) { return rows <= 64 ? 2 : 4; }
-// tree_kernel's: blocks of 16 rows a unit
-constexpr int blocks_for(int rows) { return rows <= 16 ? 1 : 2; }
 constexpr int workgroups(int DP) { return N_CU * (DP > 128 ? 1 : 2); }
 
 template <typename T, int DP, int CH, int ROWS>
 hipError_t join(const TreeArgs& a, hipStream_t st) {
-    const int64_t all = (int64_t)a.B * a.T * a.H;
-    if (all <= 512) hipLaunchKernelGGL((tree_join_kernel<T, DP, CH, ROWS, 8>), dim3((unsigned)all), dim3(64 * 8), 0, st, a);
-    else hipLaunchKernelGGL((tree_join_kernel<T, DP, CH, ROWS, 1>), dim3((unsigned)((all + 3) / 4)), dim3(64 * 4), 0, st, a);
+    const int64_t all = (int64_t)a.B * a.T * a.H, fours = (int64_t)a.B * a.H_kv * ((a.T * (a.H / a.H_kv) + 3) / 4);
+    if (all <= 512) hipLaunchKernelGGL((tree_join_kernel<T, DP, CH, ROWS>), dim3((unsigned)all), dim3(64 * JOIN_WAVES), 0, st, a);
+    else hipLaunchKernelGGL((tree_join_rows_kernel<T, DP, CH, ROWS>), dim3((unsigned)((fours + 3) / 4)), dim3(64 * 4), 0, st, a);
     return hipGetLastError();
 }
 template <int ROWS>
 unsigned all_units(const TreeArgs& a) { return (unsigned)(a.B * a.H_kv * ((a.T * (a.H / a.H_kv) + ROWS - 1) / ROWS)); }
 
-template <typename T, int DP, int M>
+template <typename T, int DP>
 hipError_t launch(TreeArgs a, hipStream_t st) {
     // (decode.hip's rule for units of a workgroup each)
     if ((int64_t)a.max_pages * a.page_size <= (DP > 128 ? 4 : 8) * CHUNK<T>) {
-        hipLaunchKernelGGL((tree_kernel<T, DP, M, true>), dim3(all_units<16 * M>(a)), dim3(64 * WAVES), 0, st, a);
+        hipLaunchKernelGGL((tree_kernel<T, DP, true>), dim3(all_units<16>(a)), dim3(64 * WAVES), 0, st, a);
         return hipGetLastError();
     }
     a.n_wgs = workgroups(DP);
-    hipLaunchKernelGGL((tree_kernel<T, DP, M, false>), dim3((unsigned)a.n_wgs), dim3(64 * WAVES), 0, st, a);
+    hipLaunchKernelGGL((tree_kernel<T, DP, false>), dim3((unsigned)a.n_wgs), dim3(64 * WAVES), 0, st, a);
     if (hipError_t e = hipGetLastError()) return e;
-    return join<T, DP, CHUNK<T>, 16 * M>(a, st);
-}
-template <typename T, int DP>
-hipError_t launch(const TreeArgs& a, hipStream_t st) {
-    return blocks_for(a.T * (a.H / a.H_kv)) == 1 ? launch<T, DP, 1>(a, st) : launch<T, DP, 2>(a, st);
+    return join<T, DP, CHUNK<T>, 16>(a, st);
 }
 template <typename T>
 hipError_t launch(const TreeArgs& a, hipStream_t st) {
@@ -1104,7 +1129,7 @@ hipError_t launch_tiles(const TreeArgs& a, hipStream_t st) {
 
 int64_t tree_workspace(int rows, int d, int dtype) {
     if (in_tiles(rows, d, dtype)) return (int64_t)workgroups(tile_columns(d)) * 2 * part_floats(32 * row_groups(rows), tile_columns(d)) * 4;
-    return (int64_t)workgroups(columns(d)) * 2 * part_floats(16 * blocks_for(rows), columns(d)) * 4;
+    return (int64_t)workgroups(columns(d)) * 2 * part_floats(16, columns(d)) * 4;
 }
 
 hipError_t launch_tree(const TreeArgs& a, int dtype, hipStream_t st) {
