@@ -271,9 +271,12 @@ int check_window(const sa_window* w) {
 }
 // beyond the longest sequence neither says more
 void set_window(sa::WindowArgs& a, const sa_packed* s, const sa_window* w) {
-    const int most = std::min(s->max_len, s->rows);
-    a.window = std::min(w->window, most);
-    a.sinks = std::min(w->sinks, most);
+    a.n_seq = s->n_seq; a.rows = s->rows; a.max_len = std::min(s->max_len, s->rows);
+    a.H = s->H; a.H_kv = s->H_kv; a.d = s->d; a.es = (int)elt_size(s->dtype);
+    a.window = std::min(w->window, std::max(a.max_len, 1));
+    a.sinks = std::min(w->sinks, a.max_len);
+    sa::set_far(a);
+    a.slot = -1;
 }
 
 // ---- paged cache
@@ -630,7 +633,9 @@ int sa_attn_window_fwd(const void* q, const void* k, const void* v, const int32_
 int64_t sa_attn_window_bwd_workspace(const sa_packed* shape, const sa_window* window) {
     if (int e = check_packed(shape)) return e;
     if (int e = check_window(window)) return e;
-    return 0;
+    sa::WindowArgs a{};
+    set_window(a, shape, window);
+    return sa::far_bytes(a);
 }
 
 int sa_attn_window_bwd(const void* q, const void* k, const void* v, const void* out, const void* dout, const float* lse,
@@ -646,6 +651,7 @@ int sa_attn_window_bwd(const void* q, const void* k, const void* v, const void* 
     if (bytes > 0 && !workspace) return SA_ERR_NULL;
     if (!aligned16(workspace)) return SA_ERR_ALIGN;
     set_window(a, shape, window);
+    a.work = (float*)workspace;
     hipStream_t st = (hipStream_t)stream;
     return play_packed(shape, offsets, a, [&](const sa::WindowArgs& p) {
         return shape->dtype == SA_F32 ? sa::launch_window_f32(p, true, st) : sa::launch_window_bwd(p, st);

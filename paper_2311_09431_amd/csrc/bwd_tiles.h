@@ -579,9 +579,9 @@ __device__ __forceinline__ void bwd_dkdv(const Args& p, int n_tiles, int linear,
     // sees one
     int t_low = 0x7fffffff, span = 0;
     if constexpr (WINDOW) {
-        if (k0 >= p.sinks) n_qt = min(n_qt, 2 * ((k0 + BM - 2 + p.window) / BM + 1));
-        if (k0 + BM > p.sinks) t_low = (k0 + p.window) / BM * 2;
-        span = key_own < p.sinks ? 1 << 30 : p.window - 1;
+        n_qt = min(n_qt, 2 * ((walk_end(p, k0, k0 + BM - 1) - 1) / BM + 1));
+        t_low = (k0 + p.window) / BM * 2;
+        span = p.n_slots == 0 && key_own < p.sinks ? 1 << 30 : p.window - 1;
     }
     // The block being walked: query head q_head of the group and query shard q_dev.  Query tiles
     // holding at least one allowed pair (query a >= key + off) are those from k0 / 64 on; only the
@@ -781,18 +781,33 @@ __device__ __forceinline__ void bwd_dkdv(const Args& p, int n_tiles, int linear,
     if constexpr (PACKED) {
         const int64_t row = kv_base + (int64_t)key * ss;
         uint32_t odd = 0;       // rows to do over
-        if constexpr (WINDOW) odd = row_mask(key_ok && (window_odd<MB, PART>(accv, h, d, 128 * ohalf) || window_odd<MB, PART>(acck, h, d, 128 * ohalf)));
-        const bool stored = key_ok && (!WINDOW || !((odd >> n) & 1));
+        if constexpr (WINDOW) odd = row_mask(key_ok && !is_far(p, key_own) && (window_odd<MB, PART>(accv, h, d, 128 * ohalf) || window_odd<MB, PART>(acck, h, d, 128 * ohalf)));
+        bool stored = key_ok;
+        if constexpr (WINDOW) stored = key_ok && !((odd >> n) & 1) && !is_far(p, key_own);
 #pragma unroll
         for (int mb = 0; mb < MB; ++mb) {
             store_bf16((__bf16*)p.dv + row, 128 * ohalf + 32 * mb, accv[mb], 1.f, stored, h, d);
             store_bf16((__bf16*)p.dk + row, 128 * ohalf + 32 * mb, acck[mb], p.scale, stored, h, d);
         }
-        if constexpr (WINDOW)
+        if constexpr (WINDOW) {
+            if (p.slot >= 0 && key_ok && is_far(p, key_own)) {
+                float* const to = slot_row(p, p.slot, kvh, key_own);
+#pragma unroll
+                for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) {
+                        const int col = 128 * ohalf + 32 * mb + 8 * g + 4 * h;
+                        if (col >= d) continue;
+                        *reinterpret_cast<float4*>(to + col) = make_float4(accv[mb][4 * g], accv[mb][4 * g + 1], accv[mb][4 * g + 2], accv[mb][4 * g + 3]);
+                        *reinterpret_cast<float4*>(to + d + col) = make_float4(p.scale * acck[mb][4 * g], p.scale * acck[mb][4 * g + 1],
+                                                                               p.scale * acck[mb][4 * g + 2], p.scale * acck[mb][4 * g + 3]);
+                    }
+            }
             each_window_row<false, BM>(odd, (int)blockIdx.x, launch_args().H_kv * NH, 32 * wave, [&](const WindowArgs& again, int head, int row) {
                 const int col0 = head % NH * 128;
                 window_dkdv_row<__hip_bfloat16>(again, head / NH, row, col0, NH > 1 ? min(again.d, col0 + 128) : again.d, threadIdx.x & 63);
             });
+        }
         return;
     }
 #pragma unroll

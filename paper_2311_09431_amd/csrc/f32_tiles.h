@@ -150,12 +150,6 @@ template <int SPLIT, int DP>
 constexpr int tile_floats() { return 2 * tile_rows(SPLIT) * lds_pitch(DP); }
 
 // ------------------------------------------------------------------ forward
-// WINDOW's walk over key tiles of TK: where the tile after the one at t0 begins; start: the window's first sub-tile
-template <int TK>
-__device__ inline int next_tile(const WindowArgs& p, int t0, int start) {
-    const int t = t0 + TK;
-    return t >= p.sinks && t < start ? start : t;
-}
 // Args: StepArgs, or PackedArgs for packed sequences (packed.h), or WindowArgs with a window (window.h)
 template <typename T, int DP, int SPLIT, typename Args = StepArgs>
 __global__ void __launch_bounds__(64 * WAVES, DP > 128 ? 1 : 2)
@@ -191,7 +185,7 @@ fwd_f32_kernel(Args p, int n_tiles) {
     float m = -INFINITY, l = 0.f;           // l: this half-wave's share of the row sum
 
     auto sees = [&](int key, int last) {
-        if constexpr (WINDOW) return key <= last && (key > last - p.window || key < p.sinks);
+        if constexpr (WINDOW) return key <= last && in_window(p, key, last);
         else return key <= last;
     };
     // the key shards one after the other; contiguous layout: none further on than the queries' own
@@ -208,7 +202,7 @@ fwd_f32_kernel(Args p, int n_tiles) {
         if constexpr (WINDOW) {
             start = window_start(p, q0) / 32 * 32;
             wave_lo = window_start(p, q0 + 32 * qw);
-            if (p.sinks == 0) t0 = start;
+            t0 = first_tile(p, start);
         }
         for (; t0 <= last_key;) {
             __syncthreads();
@@ -377,7 +371,7 @@ __device__ inline void bwd_dq(const Args& p, int n_tiles, int linear, float* lds
     for (int mb = 0; mb < NB; ++mb) acc[mb] = zero16();
 
     auto sees = [&](int key, int last) {
-        if constexpr (WINDOW) return key <= last && (key > last - p.window || key < p.sinks);
+        if constexpr (WINDOW) return key <= last && in_window(p, key, last);
         else return key <= last;
     };
     const int kv_end = last_shard(p, dev);
@@ -393,7 +387,7 @@ __device__ inline void bwd_dq(const Args& p, int n_tiles, int linear, float* lds
         if constexpr (WINDOW) {
             start = window_start(p, q0) / 32 * 32;
             wave_lo = window_start(p, q0 + 32 * qw);
-            if (p.sinks == 0) t0 = start;
+            t0 = first_tile(p, start);
         }
         for (; t0 <= last_key;) {
             __syncthreads();
@@ -483,9 +477,9 @@ __device__ inline void bwd_dkdv(const Args& p, int n_tiles, int linear, float* l
             const int lane_first = full ? 0 : key_own + off;
             int t_end = p.c, wave_end = p.c, lane_end = p.c;         // one past the last query
             if constexpr (WINDOW) {
-                t_end = k0 < p.sinks ? p.c : window_end(p, k0 + 32 * OWN - 1);
-                wave_end = k0 + 32 * own < p.sinks ? p.c : window_end(p, k0 + 32 * own + 31);
-                lane_end = window_end(p, key_own);
+                t_end = walk_end(p, k0, k0 + 32 * OWN - 1);
+                wave_end = walk_end(p, k0 + 32 * own, k0 + 32 * own + 31);
+                lane_end = walk_end(p, key_own);
             }
             for (int t0 = first_query / 32 * 32; t0 < t_end; t0 += TK) {
                 __syncthreads();
@@ -524,7 +518,19 @@ __device__ inline void bwd_dkdv(const Args& p, int n_tiles, int linear, float* l
         __syncthreads();
         combine<SPLIT, NB>(acck, buf, masks + own * SPLIT, odd, qsub, lane);
     }
-    if (key_own < p.c && !((odd_rows >> n) & 1)) {
+    bool stored = key_own < p.c;
+    if constexpr (WINDOW) {
+        // (keys that are seen from further on: to the workspace, whatever they are)
+        const bool far = key_own < p.c && is_far(p, key_own);
+        odd_rows &= ~row_mask(far);
+        if (far && p.slot >= 0) {
+            float* const to = slot_row(p, p.slot, kvh, key_own);
+            add_rows<SPLIT, NB>(to, accv, 1.f, col0, d, qsub, h, true);
+            add_rows<SPLIT, NB>(to + d, acck, p.scale, col0, d, qsub, h, true);
+        }
+        stored = key_own < p.c && !far;
+    }
+    if (stored && !((odd_rows >> n) & 1)) {
         const int64_t row = kv_base + (int64_t)key * p.kv_stride_s;
         add_rows<SPLIT, NB>(p.dv + row, accv, 1.f, col0, d, qsub, h, p.fresh);
         add_rows<SPLIT, NB>(p.dk + row, acck, p.scale, col0, d, qsub, h, p.fresh);

@@ -22,6 +22,7 @@
 #include "f32x3_parts.h"
 #include "packed.h"
 #include "sa_internal.h"
+#include "window.h"
 
 namespace sa {
 
@@ -175,22 +176,28 @@ __device__ inline void accumulate(f32x16 (&acc)[NB], const char* planes, const b
 }
 
 // The walk of a query-owning workgroup over the 32-key tiles of its shards, q0 its first query:
-// body(k, v, key0, full, off) on one tile.
-template <int DP, int WAVES, typename Body>
-__device__ inline void walk_keys(const StepArgs& p, int dev, int q0, int64_t kv_base, char* lds, Body body) {
+// body(k, v, key0, full, off) on one tile.  Args: StepArgs, or WindowArgs (window.h).
+template <int DP, int WAVES, typename Args, typename Body>
+__device__ inline void walk_keys(const Args& p, int dev, int q0, int64_t kv_base, char* lds, Body body) {
+    constexpr bool WINDOW = std::is_same<Args, WindowArgs>::value;
     const int kv_end = last_shard(p, dev), q_last = min(q0 + 32 * WAVES, p.c) - 1;
     const float* K = (const float*)p.k + kv_base;
     const float* V = (const float*)p.v + kv_base;
     Staged<DP, WAVES> sk, sv;
     // tile after tile of the walk: `ahead` is the next one to fetch
-    int kv_a = p.kv_dev, t_a = 0;
+    int kv_a = p.kv_dev, t_a = 0, start = 0;
+    if constexpr (WINDOW) {
+        start = window_start(p, q0) / TILE * TILE;
+        t_a = first_tile(p, start);
+    }
     auto last_key = [&](int kv) {
         return block_kind(dev, kv, p.layout) == MASK_FULL ? p.c - 1 : q_last - block_off(dev, kv, p.layout);
     };
     auto fetch = [&]() {
         sk.fetch(K + (kv_a - p.kv_dev) * p.kv_shard, p.kv_stride_s, t_a, p.c, p.d);
         sv.fetch(V + (kv_a - p.kv_dev) * p.kv_shard, p.kv_stride_s, t_a, p.c, p.d);
-        t_a += TILE;
+        if constexpr (WINDOW) t_a = next_tile<TILE>(p, t_a, start);
+        else t_a += TILE;
         if (t_a > last_key(kv_a)) {
             t_a = 0;
             ++kv_a;
@@ -218,11 +225,11 @@ __device__ inline void walk_keys(const StepArgs& p, int dev, int q0, int64_t kv_
 }
 
 // ------------------------------------------------------------------ forward
-// Args: StepArgs, or PackedArgs for packed sequences (packed.h)
+// Args: StepArgs, or PackedArgs for packed sequences (packed.h), or WindowArgs with a window
 template <int DP, int WAVES, typename Args = StepArgs>
 __global__ void __launch_bounds__(64 * WAVES, WAVES / 4)
 fwd_f32x3_kernel(Args p, int n_tiles) {
-    constexpr bool PACKED = !std::is_same<Args, StepArgs>::value;
+    constexpr bool PACKED = !std::is_same<Args, StepArgs>::value, WINDOW = std::is_same<Args, WindowArgs>::value;
     constexpr int KS = ksteps_of(DP), NB = blocks_of(DP);
     __shared__ __attribute__((aligned(1024))) char lds[2 * BUFFER];
 
@@ -254,8 +261,16 @@ fwd_f32x3_kernel(Args p, int n_tiles) {
     walk_keys<DP, WAVES>(p, dev, q0, kv_base, lds, [&](const char* k, const char* v, int key0, bool full, int off) {
         const int wave_last = full ? p.c - 1 : min(q0 + 32 * ln.wave + 31, p.c - 1) - off;
         if (key0 > wave_last) return;
+        if constexpr (WINDOW) {
+            if (key0 + TILE - 1 < window_start(p, q0 + 32 * ln.wave) && key0 >= p.sinks) return;
+        }
         const int lane_last = (full ? p.c - 1 : a - off) - key0;
         f32x16 x = scores<KS>(k, qf, ln);
+        if constexpr (WINDOW) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                if (!in_window(p, key0 + reg_row(r, h), a)) x[r] = -INFINITY;
+        }
         float mx = -INFINITY;
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
@@ -318,7 +333,8 @@ fwd_f32x3_kernel(Args p, int n_tiles) {
         if (h == 0) *L = top + logf(w_sum);
     }
     each_row<1>(odd_rows, 0, [&](const StepArgs& again, int i) {
-        if constexpr (PACKED) fwd_row<float>(p, b, hd, dev_i, q0 + 32 * ln.wave + i, ln.lane);
+        if constexpr (WINDOW) window_fwd_row<float>(p, hd, q0 + 32 * ln.wave + i, ln.lane);
+        else if constexpr (PACKED) fwd_row<float>(p, b, hd, dev_i, q0 + 32 * ln.wave + i, ln.lane);
         else fwd_row<float>(again, b, hd, dev_i, q0 + 32 * ln.wave + i, ln.lane);
     });
 }
@@ -381,8 +397,9 @@ __device__ inline uint32_t odd_of_pair(uint32_t* masks, uint32_t odd, uint32_t s
 
 // dQ.  The pair's wavefronts take half of its columns each.
 // PACKED: linear is the tile's place and the head in a sequence that p is the arguments of
-template <int DP, bool PACKED = false>
-__device__ inline void bwd_dq(const StepArgs& p, int n_tiles, int linear, char* lds, char* tiles, uint32_t* masks) {
+template <int DP, bool PACKED = false, typename Args = StepArgs>
+__device__ inline void bwd_dq(const Args& p, int n_tiles, int linear, char* lds, char* tiles, uint32_t* masks) {
+    constexpr bool WINDOW = std::is_same<Args, WindowArgs>::value;
     constexpr int KS = ksteps_of(DP), NB = blocks_of(DP) / 2;
     const Lane ln;
     const int n = ln.n, h = ln.h, group = ln.wave % GROUPS, role = ln.wave / GROUPS;
@@ -412,13 +429,22 @@ __device__ inline void bwd_dq(const StepArgs& p, int n_tiles, int linear, char* 
     }
     const Exchange own_tile(tiles + role * GROUPS * 4096, group, ln.lane), others_tile(tiles + (1 - role) * GROUPS * 4096, group, ln.lane);
 
+    auto reached = [&](int t0) {            // by some row's window, or one with first keys
+        if constexpr (WINDOW) return t0 + TILE - 1 >= window_start(p, q0 + 32 * group) || t0 < p.sinks;
+        else return true;
+    };
     const int kv_end = last_shard(p, dev), q_last = min(q0 + 32 * GROUPS, p.c) - 1;
     Staged<DP, 2 * GROUPS> sk, sv;
-    int kv_a = p.kv_dev, t_a = 0;               // the next tile to fetch
+    int kv_a = p.kv_dev, t_a = 0, start = 0;    // the next tile to fetch
+    if constexpr (WINDOW) {
+        start = window_start(p, q0) / TILE * TILE;
+        t_a = first_tile(p, start);
+    }
     auto fetch = [&]() {
         sk.fetch((const float*)p.k + kv_base + (kv_a - p.kv_dev) * p.kv_shard, p.kv_stride_s, t_a, p.c, d);
         sv.fetch((const float*)p.v + kv_base + (kv_a - p.kv_dev) * p.kv_shard, p.kv_stride_s, t_a, p.c, d);
-        t_a += TILE;
+        if constexpr (WINDOW) t_a = next_tile<TILE>(p, t_a, start);
+        else t_a += TILE;
         if (t_a > (block_kind(dev, kv_a, p.layout) == MASK_FULL ? p.c - 1 : q_last - block_off(dev, kv_a, p.layout))) {
             t_a = 0;
             ++kv_a;
@@ -435,7 +461,7 @@ __device__ inline void bwd_dq(const StepArgs& p, int n_tiles, int linear, char* 
         const char* k = lds + parity * BUFFER;
         const bool full = block_kind(dev, kv, p.layout) == MASK_FULL;
         const int off = block_off(dev, kv, p.layout);
-        const bool active = t0 <= (full ? p.c - 1 : min(q0 + 32 * group + 31, p.c - 1) - off);
+        const bool active = t0 <= (full ? p.c - 1 : min(q0 + 32 * group + 31, p.c - 1) - off) && reached(t0);
         const int kv_nn = kv_a, t_nn = t_a;
         auto stage = [&]() {
             sk.put(lds + (1 - parity) * BUFFER);
@@ -453,6 +479,12 @@ __device__ inline void bwd_dq(const StepArgs& p, int n_tiles, int linear, char* 
                 if (t0 + 31 > (full ? p.c - 1 : min(q0 + 32 * group, p.c) - 1 - off)) {        // some pair is masked
 #pragma unroll
                     for (int r = 0; r < 16; ++r) x[r] = reg_row(r, h) <= lane_last ? x[r] : 0.f;
+                }
+                if constexpr (WINDOW) {
+                    if (t0 <= q0 + 32 * group + 31 - p.window) {
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) x[r] = in_window(p, t0 + reg_row(r, h), a) ? x[r] : 0.f;
+                    }
                 }
             } else {
 #pragma unroll
@@ -483,7 +515,8 @@ __device__ inline void bwd_dq(const StepArgs& p, int n_tiles, int linear, char* 
     if (a_own < p.c && !((odd_rows >> n) & 1))
         add_rows<NB>(p.dq + base + (int64_t)a * p.stride_s, acc, p.scale, 32 * NB * role, d, h, p.fresh);
     each_row<2>(odd_rows, role, [&](const StepArgs& again, int i) {
-        if constexpr (PACKED) dq_row<float>(p, b, hd, dev_i, q0 + 32 * group + i, ln.lane);
+        if constexpr (WINDOW) window_dq_row<float>(p, hd, q0 + 32 * group + i, ln.lane);
+        else if constexpr (PACKED) dq_row<float>(p, b, hd, dev_i, q0 + 32 * group + i, ln.lane);
         else dq_row<float>(again, b, hd, dev_i, q0 + 32 * group + i, ln.lane);
     });
 }
@@ -491,8 +524,9 @@ __device__ inline void bwd_dq(const StepArgs& p, int n_tiles, int linear, char* 
 // dK (by the wavefront that forms dP) and dV (by the one that forms the probabilities).  Owned rows are keys, streamed
 // rows queries; the query heads of the group that shares the key/value head and the query shards that see it come one
 // after the other.
-template <int DP, bool PACKED = false>
-__device__ inline void bwd_dkdv(const StepArgs& p, int n_tiles, int linear, char* lds, char* tiles, float* stats, uint32_t* masks) {
+template <int DP, bool PACKED = false, typename Args = StepArgs>
+__device__ inline void bwd_dkdv(const Args& p, int n_tiles, int linear, char* lds, char* tiles, float* stats, uint32_t* masks) {
+    constexpr bool WINDOW = std::is_same<Args, WindowArgs>::value;
     constexpr int KS = ksteps_of(DP), NB = blocks_of(DP);
     const Lane ln;
     const int n = ln.n, h = ln.h, tid = threadIdx.x, group = ln.wave % GROUPS, role = ln.wave / GROUPS;
@@ -518,6 +552,16 @@ __device__ inline void bwd_dkdv(const StepArgs& p, int n_tiles, int linear, char
     auto first_tile = [&](int q_dev) {
         return block_kind(q_dev, dev, p.layout) == MASK_FULL ? 0 : (k0 + block_off(q_dev, dev, p.layout)) / TILE * TILE;
     };
+    int t_end = 0, group_end = 0, lane_end = 0;             // WINDOW: one past the last query that sees a key of the workgroup, of each of the 32, of the lane's
+    if constexpr (WINDOW) {
+        t_end = walk_end(p, k0, k0 + 32 * GROUPS - 1);
+        group_end = walk_end(p, k0 + 32 * group, k0 + 32 * group + 31);
+        lane_end = walk_end(p, key_own);
+    }
+    auto ends_within = [&](int t0) {        // some window, in the tile
+        if constexpr (WINDOW) return t0 + TILE > k0 + 32 * group + p.window;
+        else return false;
+    };
     Staged<DP, 2 * GROUPS> sq, sg;
     float stat = 0.f;           // LSE (threads 0 .. 31) or delta (32 .. 63) of a row of the tile
     int member_a = 0, dev_a = q_dev0, t_a = first_tile(q_dev0);
@@ -533,7 +577,7 @@ __device__ inline void bwd_dkdv(const StepArgs& p, int n_tiles, int linear, char
         }
         t_a += TILE;
         // a tile row may lie beyond the shard (last tile of a block) but a tile may not
-        if (t_a >= p.c) {
+        if (t_a >= (WINDOW ? t_end : p.c)) {
             if (++dev_a == p.q_dev + p.n_q) {
                 dev_a = q_dev0;
                 ++member_a;
@@ -570,16 +614,16 @@ __device__ inline void bwd_dkdv(const StepArgs& p, int n_tiles, int linear, char
         const int off = block_off(q_dev, dev, p.layout);
         const char* q = lds + parity * BUFFER;
         const float* st = stats + parity * 3 * TILE;
-        const bool active = full || t0 + 31 >= k0 + 32 * group + off;
+        const bool active = WINDOW ? t0 + 31 >= k0 + 32 * group && t0 < group_end : full || t0 + 31 >= k0 + 32 * group + off;
         f32x16 x;
         bf16x8x3 w[2];
         if (active) {
             x = scores<KS>(q + role * OPERAND, own, ln);
             if (role == 0) {
-                const int lane_first = (full ? 0 : key_own + off) - t0, rows = p.c - t0;
+                const int lane_first = (full ? 0 : key_own + off) - t0, rows = (WINDOW ? lane_end : p.c) - t0;
 #pragma unroll
                 for (int r = 0; r < 16; ++r) x[r] = kappa.exp2(x[r], st[reg_row(r, h)], st[TILE + reg_row(r, h)]);
-                if (t0 < (full ? 0 : k0 + 32 * group + 31 + off) || rows < TILE) {        // some pair is masked
+                if (t0 < (full ? 0 : k0 + 32 * group + 31 + off) || (WINDOW ? p.c - t0 : rows) < TILE || ends_within(t0)) {        // some pair is masked
 #pragma unroll
                     for (int r = 0; r < 16; ++r) x[r] = reg_row(r, h) >= lane_first && reg_row(r, h) < rows ? x[r] : 0.f;
                 }
@@ -610,12 +654,21 @@ __device__ inline void bwd_dkdv(const StepArgs& p, int n_tiles, int linear, char
         more = more_n;
     }
     // (each has all columns of its result)
-    const uint32_t odd_rows = odd_of_pair(masks, row_mask(key_own < p.c && not_finite<NB>(acc)) |
-                                                     faint_rows(loudest<NB>(acc), key_own < p.c), 0, 0, ln.wave, ln.lane);
-    if (key_own < p.c && !((odd_rows >> n) & 1))
+    uint32_t odd_rows = odd_of_pair(masks, row_mask(key_own < p.c && not_finite<NB>(acc)) |
+                                               faint_rows(loudest<NB>(acc), key_own < p.c), 0, 0, ln.wave, ln.lane);
+    bool stored = key_own < p.c;
+    if constexpr (WINDOW) {
+        // (keys that are seen from further on: to the workspace, whatever they are)
+        const bool far = key_own < p.c && is_far(p, key_own);
+        odd_rows &= ~row_mask(far);
+        if (far && p.slot >= 0) add_rows<NB>(slot_row(p, p.slot, kvh, key_own) + (role ? d : 0), acc, role ? p.scale : 1.f, 0, d, h, true);
+        stored = key_own < p.c && !far;
+    }
+    if (stored && !((odd_rows >> n) & 1))
         add_rows<NB>((role ? p.dk : p.dv) + row, acc, role ? p.scale : 1.f, 0, d, h, p.fresh);
     each_row<2>(odd_rows, role, [&](const StepArgs& again, int i) {
-        if constexpr (PACKED) dkdv_row<float>(p, b, kvh, dev_i, k0 + 32 * group + i, 0, d, ln.lane);
+        if constexpr (WINDOW) window_dkdv_row<float>(p, kvh, k0 + 32 * group + i, 0, d, ln.lane);
+        else if constexpr (PACKED) dkdv_row<float>(p, b, kvh, dev_i, k0 + 32 * group + i, 0, d, ln.lane);
         else dkdv_row<float>(again, b, kvh, dev_i, k0 + 32 * group + i, 0, d, ln.lane);
     });
 }

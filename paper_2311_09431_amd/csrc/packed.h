@@ -119,13 +119,14 @@ __device__ inline bool find_tile(const PackedArgs& p, int rank, int& seq, int& w
 }
 
 // The workgroup's sequence, tile and head: p becomes the arguments of a launch on that sequence alone, n_tiles its tiles,
-// rank the tile's place among them (0: the heaviest).  False: none, the launch has more workgroups than there are tiles.
+// rank the tile's place among them (0: the heaviest).  False: none, the launch has more workgroups than there are tiles.  which: gets the sequence.
 template <bool SNAKE, int TILE>
-__device__ inline bool enter_sequence(PackedArgs& p, int linear, int n_heads, int& n_tiles, int& rank, int& head) {
+__device__ inline bool enter_sequence(PackedArgs& p, int linear, int n_heads, int& n_tiles, int& rank, int& head, int* which = nullptr) {
     if (p.by_rank) decode_block<SNAKE, true>(linear, p.n_ranks, n_heads, rank, head);
     else decode_block<SNAKE, false>(linear, p.n_ranks, n_heads, rank, head);
     int seq, weight;
     if (!find_tile<TILE>(p, rank, seq, weight)) return false;
+    if (which) *which = seq;
     const Span x = span_of(p, seq);
     const int first = __builtin_amdgcn_readfirstlane(x.first);
     p.c = __builtin_amdgcn_readfirstlane(x.len);

@@ -1,7 +1,11 @@
 // Attention with a sliding window and a few first tokens that stay visible, over packed sequences (packed.h): row a of a sequence sees key b where
 // b <= a and (a - b < window or b < sinks).  The packed kernels' workgroups, whose walk leaves out the tiles that no row of theirs sees: a
 // query-owning one's goes over the tiles with first keys, then on to those of its rows' windows; a key-owning one's ends with the last row
-// whose window reaches back to its keys, of a tile with first keys with the sequence.
+// whose window reaches back to its keys.
+//
+// What the rows further on add to dK and dV of the first keys is, but for short ways, formed by workgroups of their own (window_far.hip), each for a part of
+// a sequence's rows: in the key-owning workgroup it would be a walk over the whole sequence beside others of a window's length.  Such keys'
+// sums stay in fp32 in the workspace, of the window's rows and of each part's, until they are put together.
 #pragma once
 #include "f32_rows.h"
 #include "packed.h"
@@ -10,15 +14,70 @@ namespace sa {
 
 struct WindowArgs : PackedArgs {
     int window, sinks;          // 1 .. max_len, 0 .. max_len
+    // backward, workspace: slots of H_kv x key_rows x (dV, dK) x d, one of a sequence's windows and one of each `part` of its rows behind
+    float* work;
+    int part, key_rows, n_slots;
+    int slot;                   // the sequence's first one, set by the workgroup; -1: none
 };
+// Whether there are such workgroups: two launches more, against the time of a walk, rows of all heads of a group.  FAR_RULE
+// The rows of a part (fewer parts where there are many first keys, whose blocks of 16 are workgroups too) and the slots that sequences
+// without a common row can have; 0: key-owning workgroups walk on.
+inline bool has_far(const WindowArgs& p) {
+    return p.sinks > 0 && (int64_t)(p.max_len - p.window) * (p.H / p.H_kv) > (p.es == 2 ? 1024 : 128);
+}
+inline void set_far(WindowArgs& p) {
+    p.key_rows = (p.sinks + 15) / 16 * 16;
+    p.part = (p.es == 2 ? 256 : 128) * (p.key_rows / 16 < 64 ? p.key_rows / 16 : 64);
+    const int64_t all = (int64_t)p.n_seq * p.max_len, rows = all < p.rows ? all : p.rows;
+    const int64_t longer = rows / (p.window + 1) < p.n_seq ? rows / (p.window + 1) : p.n_seq;      // sequences that are longer than the window
+    p.n_slots = has_far(p) ? (int)(2 * longer + rows / p.part) : 0;
+}
+inline int64_t far_bytes(const WindowArgs& p) { return (int64_t)p.n_slots * p.H_kv * p.key_rows * 2 * p.d * 4; }
+hipError_t launch_window_far(const WindowArgs& p, int dtype, hipStream_t st);
 hipError_t launch_window_fwd(WindowArgs p, hipStream_t st);
 hipError_t launch_window_bwd(WindowArgs p, hipStream_t st);
 hipError_t launch_window_f32(WindowArgs p, bool backward, hipStream_t st);
+bool window_in_terms(const WindowArgs& p);
+hipError_t launch_window_f32x3(WindowArgs p, bool backward, hipStream_t st);           // up to 128 columns
 
 // the first key of row a's window
 __device__ inline int window_start(const WindowArgs& p, int a) { return max(0, a - p.window + 1); }
-// one past the last row that sees `key`, of c
-__device__ inline int window_end(const WindowArgs& p, int key) { return key < p.sinks ? p.c : min(p.c, key + p.window); }
+// one past the last row that a key-owning workgroup walks to for keys first .. last
+__device__ inline int walk_end(const WindowArgs& p, int first, int last) { return p.n_slots == 0 && first < p.sinks ? p.c : min(p.c, last + p.window); }
+__device__ inline int walk_end(const WindowArgs& p, int key) { return walk_end(p, key, key); }
+// the key's sums are put together from those of its window's rows and those further on
+__device__ inline bool is_far(const WindowArgs& p, int key) { return p.n_slots > 0 && key < p.sinks && key + p.window < p.c; }
+// slots of a sequence of len rows; of those before sequence seq (a wavefront's lanes take the sequences in turn)
+__device__ inline int slots_of(const WindowArgs& p, int len) { return p.n_slots > 0 && len > p.window ? 1 + (len - p.window + p.part - 1) / p.part : 0; }
+__device__ inline int slots_before(const WindowArgs& p, int seq) {
+    const int lane = threadIdx.x & 63;
+    int n = 0;
+    for (int s = lane; s < seq; s += 64) {
+        const int next = n + slots_of(p, span_of(p, s).len);
+        n = next < MOST_COUNTED ? next : MOST_COUNTED;          // (as add_tiles)
+    }
+    return wave_total(wave_scan(n));
+}
+// A key-owning workgroup's slot, where its keys have one: sequences without a common row have n_slots, of others the last ones may have none.
+__device__ inline int find_slot(const WindowArgs& p, int seq, int k0) {
+    if (k0 >= p.sinks || p.c <= p.window) return -1;
+    const int slot = slots_before(p, seq);
+    return slot < p.n_slots ? slot : -1;
+}
+// a key's dV and dK, d columns each, in a slot
+__device__ inline float* slot_row(const WindowArgs& p, int slot, int kvh, int key) {
+    return p.work + (((int64_t)slot * p.H_kv + kvh) * p.key_rows + key) * 2 * p.d;
+}
+
+// A walk over key tiles of TK rows without pairs: where it begins, and the tile behind the one at t0; start: the window's first sub-tile of 32
+__device__ inline int first_tile(const WindowArgs& p, int start) { return p.sinks == 0 ? start : 0; }
+template <int TK>
+__device__ inline int next_tile(const WindowArgs& p, int t0, int start) {
+    const int t = t0 + TK;
+    return t >= p.sinks && t < start ? start : t;
+}
+// row a sees `key`, of those up to its own
+__device__ inline bool in_window(const WindowArgs& p, int key, int a) { return key > a - p.window || key < p.sinks; }
 
 // The walk of a query-owning workgroup of PAIR rows from q0 on, over tiles of PAIR keys, `tiles` of them up to its own.
 template <int PAIR>
@@ -113,10 +172,10 @@ __device__ inline void window_dq_row(const WindowArgs& p, int hd, int a, int lan
     for (int k = 0; k < ROW_COLS; ++k)
         if (lane + 64 * k < p.d) store1((T*)p.dq + row + lane + 64 * k, p.scale * acc[k]);
 }
-// columns col0 .. end_col - 1 of dK and dV
+// columns col0 .. end_col - 1 of dK and dV, of all rows that see the key
 template <typename T>
 __device__ inline void window_dkdv_row(const WindowArgs& p, int kvh, int key, int col0, int end_col, int lane) {
-    const int group = p.H / p.H_kv, end = window_end(p, key);
+    const int group = p.H / p.H_kv, end = key < p.sinks ? p.c : min(p.c, key + p.window);
     const int64_t row = kvh * p.kv_stride_h + (int64_t)key * p.kv_stride_s;
     float acck[ROW_COLS] = {}, accv[ROW_COLS] = {};
 #pragma unroll 1
@@ -145,8 +204,7 @@ __device__ inline void window_dkdv_row(const WindowArgs& p, int kvh, int key, in
     }
 }
 // The rows set in a mask, as each_row has them: the launch's arguments are read and its sequence looked up anew, so that nothing of either has to be
-// kept until here (39 registers spilled in the forward at 128 columns, 128 in dQ's).  first_row: of the wavefront within its workgroup's tile.
-// row(arguments, head, row of the sequence).
+// kept until here.  first_row: of the wavefront within its workgroup's tile.  row(arguments, head, row of the sequence).
 template <bool SNAKE, int TILE, typename Row>
 __device__ inline void each_window_row(uint32_t rows, int linear, int n_heads, int first_row, Row row) {
     if (rows == 0) return;

@@ -27,8 +27,9 @@ window_dkdv_kernel(WindowArgs p) {
     __shared__ __attribute__((aligned(1024))) char lds3[tile_bytes(DP) * halves_of(DP)];
     __shared__ __attribute__((aligned(16))) float stat[KV_STAT_FLOATS];
     const int heads = p.H_kv * halves_of(DP);
-    int n_tiles, rank, head;
-    if (!enter_sequence<false, BM>(p, (int)blockIdx.x, heads, n_tiles, rank, head)) return;
+    int n_tiles, rank, head, seq;
+    if (!enter_sequence<false, BM>(p, (int)blockIdx.x, heads, n_tiles, rank, head, &seq)) return;
+    p.slot = find_slot(p, seq, rank * BM);
     bwd_dkdv<WALK_RING, true, DP, PART, false, true, WindowArgs>(p, n_tiles, rank * heads + head, lds0, lds1, lds2, lds3, stat);
 }
 
@@ -39,7 +40,8 @@ hipError_t launch(WindowArgs p, hipStream_t st) {
     hipLaunchKernelGGL((window_dq_kernel<DP, PART>), dim3((unsigned)p.n_ranks * p.H), dim3(256), 0, st, p);
     if (hipError_t e = hipGetLastError()) return e;
     hipLaunchKernelGGL((window_dkdv_kernel<DP, PART>), dim3((unsigned)p.n_ranks * p.H_kv * halves_of(DP)), dim3(256), 0, st, p);
-    return hipGetLastError();
+    if (hipError_t e = hipGetLastError()) return e;
+    return launch_window_far(p, SA_BF16, st);
 }
 
 }  // namespace

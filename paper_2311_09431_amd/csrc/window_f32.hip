@@ -14,9 +14,10 @@ window_bwd_f32_kernel(WindowArgs p, int n_dkdv) {
     __shared__ float stats[2 * tile_rows(SPLIT)];                   // LSE | delta of a tile's queries
     __shared__ uint32_t masks[WAVES];
     const int heads = p.H_kv * (DP > 128 ? 2 : 1);
-    int n_tiles, rank, head;
+    int n_tiles, rank, head, seq;
     if ((int)blockIdx.x < n_dkdv) {
-        if (!enter_sequence<false, ROWS>(p, (int)blockIdx.x, heads, n_tiles, rank, head)) return;
+        if (!enter_sequence<false, ROWS>(p, (int)blockIdx.x, heads, n_tiles, rank, head, &seq)) return;
+        p.slot = find_slot(p, seq, rank * ROWS);
         bwd_dkdv<float, DP, SPLIT, true, WindowArgs>(p, n_tiles, rank * heads + head, lds, stats, masks);
     } else {
         if (!enter_sequence<true, ROWS>(p, (int)blockIdx.x - n_dkdv, p.H, n_tiles, rank, head)) return;
@@ -28,18 +29,30 @@ template <int DP, int SPLIT>
 hipError_t run(WindowArgs p, bool backward, hipStream_t st) {
     p.n_ranks = (int)most_tiles(p, 32 * WAVES / SPLIT);
     const unsigned n_dkdv = (unsigned)p.n_ranks * p.H_kv * (DP > 128 ? 2 : 1), n_dq = (unsigned)p.n_ranks * p.H;
-    if (backward) hipLaunchKernelGGL((window_bwd_f32_kernel<DP, SPLIT>), dim3(n_dkdv + n_dq), dim3(64 * WAVES), 0, st, p, (int)n_dkdv);
-    else hipLaunchKernelGGL((fwd_f32_kernel<float, DP, SPLIT, WindowArgs>), dim3(n_dq), dim3(64 * WAVES), 0, st, p, 0);
+    if (backward) {
+        hipLaunchKernelGGL((window_bwd_f32_kernel<DP, SPLIT>), dim3(n_dkdv + n_dq), dim3(64 * WAVES), 0, st, p, (int)n_dkdv);
+        if (hipError_t e = hipGetLastError()) return e;
+        return launch_window_far(p, SA_F32, st);
+    }
+    hipLaunchKernelGGL((fwd_f32_kernel<float, DP, SPLIT, WindowArgs>), dim3(n_dq), dim3(64 * WAVES), 0, st, p, 0);
     return hipGetLastError();
 }
 
 }  // namespace
+
+// Up to 128 columns in three bf16 terms, but in launches of few tiles (of 128 rows, as many as there can be, of all heads), whose workgroups on the fp32
+// instruction are four times as many.  us, instruction : terms, forward and backward, d 128: 5 sequences of up to 777 rows, 16 heads on 8, window 100
+// (d 100) 85, 256 : 42, 188, 4 of up to 2000, 16 heads, window 500, 209, 567 : 106, 298, a sequence of 4000, 8 heads, window 1000, 302, 772 : 137,
+// 401; but 2 heads on 1, window 2000 (64 tiles), 140, 465 : 241, 771, a sequence of 200, one head, 22, 48 : 27, 64; 8 of up to 1000, 8 heads, d 32,
+// window 64, 19, 72 : 21, 67.
+bool window_in_terms(const WindowArgs& p) { return p.d <= 128 && most_tiles(p, 128) * p.H > 64; }
 
 hipError_t launch_window_f32(WindowArgs p, bool backward, hipStream_t st) {
     if (backward)
         if (hipError_t e = launch_packed_delta(p, SA_F32, st)) return e;
     p.by_rank = true;
     if (p.d > 128) return run<256, 2>(p, backward, st);
+    if (window_in_terms(p)) return launch_window_f32x3(p, backward, st);
     if (p.d <= 32) return run<32, 4>(p, backward, st);
     return run<128, 4>(p, backward, st);
 }

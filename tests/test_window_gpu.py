@@ -96,6 +96,44 @@ def test_longer(dtype, n, window, sinks):
     compare(lens, 2, 1, 128, dtype, window, sinks, *run(lens, 2, 1, 128, dtype, window, sinks))
 
 
+# first keys that are seen from far: workgroups of their own, more than one part of the rows, more than one block of first keys, groups of heads, and
+# sequences with and without such rows
+@pytest.mark.parametrize("dtype,d", [(BF16, 4), (BF16, 32), (BF16, 60), (BF16, 64), (BF16, 100), (BF16, 128), (BF16, 132), (BF16, 256), (F32, 20), (F32, 64), (F32, 100),
+                                     (F32, 128), (F32, 256)])
+@pytest.mark.parametrize("H,H_kv,lens,window,sinks", [(2, 1, [1300, 40, 0, 700, 100], 70, 4), (8, 1, [33, 400], 5, 37), (2, 2, [1900], 800, 130)])
+def test_first_keys_seen_from_far(H, H_kv, lens, window, sinks, d, dtype):
+    r = run(lens, H, H_kv, d, dtype, window, sinks)
+    assert sa.sa_attn_window_bwd_workspace(r[0][0], r[0][1], lengths_to_offsets(lens), max(lens), window, sinks) > 0
+    compare(lens, H, H_kv, d, dtype, window, sinks, *r)
+    again = run(lens, H, H_kv, d, dtype, window, sinks)
+    for x, y in zip(r[3], again[3]):
+        assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_infinities_and_first_keys_seen_from_far(dtype):
+    """A query and its gradient that are no numbers, far behind a window: they reach dK and dV of the first keys and of its window, no other."""
+    lens, window, sinks, d, at = [1500], 60, 5, 64, 1200
+    (q, k, v, g), out, lse, clean = run(lens, 2, 1, d, dtype, window, sinks)
+    off, n = lengths_to_offsets(lens).cuda(), torch.arange(1500)
+    reached = (n < sinks) | ((n <= at) & (n > at - window))
+    for which in (0, 3):
+        ins = [x.clone() for x in (q, k, v, g)]
+        ins[which][at, 1, 3] = NAN
+        grads = [torch.full_like(x, 7) for x in (q, k, v)]
+        backward(ins, out, lse, off, grads, 1500, window, sinks)
+        for x, y in zip(grads[1:], clean[1:]):
+            x, y = x.cpu().float(), y.cpu().float()
+            assert torch.isfinite(x[~reached]).all() and (x[~reached] - y[~reached]).abs().max() <= 2.0 ** -6 * y.abs().max()
+        assert not torch.isfinite(grads[1].cpu()[reached]).all(2).any()
+    # another key's value: the first keys' own gradients know nothing of it
+    ins = [x.clone() for x in (q, k, v, g)]
+    ins[2][30] = NAN
+    grads = [torch.full_like(x, 7) for x in (q, k, v)]
+    backward(ins, out, lse, off, grads, 1500, window, sinks)
+    assert torch.isfinite(grads[1].cpu()[n != 30]).all() and torch.isfinite(grads[2].cpu()).all()
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("d", [32, 64, 100, 128, 256])
 def test_many_workgroups(d, dtype):

@@ -60,6 +60,7 @@ def test_pointers():
 def test_workspace():
     """Long sequences with first tokens take one; it is looked at."""
     s = packed(rows=20000, max_len=20000, stat_stride_h=20000)
+    assert bytes_of(s, Window(10, 2)) > 0 and bytes_of(s, Window(10, 0)) == 0 and bytes_of(s, Window(20000, 2)) == 0 and bytes_of(packed(), Window(10, 2)) == 0
     for w in (Window(10, 2), Window(500, 4), Window(20000, 4), Window(1, 0), Window(7, 20000)):
         size = bytes_of(s, w)
         assert 0 <= size < 1 << 31
