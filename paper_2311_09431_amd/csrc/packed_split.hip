@@ -56,6 +56,41 @@ bool packed_split_wanted(const PackedArgs& p, bool backward) {
     return tiles <= (walk >= 12000 ? 184 : walk >= 2000 ? 152 : 96);
 }
 
+// With a window, forward: four wavefronts a workgroup, or two, for walks that are no longer than the window.  Wavefronts of a workgroup (0: the
+// 128-row kernels), by 128-row tiles of all heads and by keys a walk goes over.  A small launch is latency, that of code read for the first time too:
+// 14 KB here, of which a tile passes all, 61 KB there.  us, 128-row : two wavefronts : four (: eight), first tokens 4.
+// d 128: 300 rows, 8 heads, window 64 (24 tiles) 17.0 : 8.0 : 7.4 : 7.9; 4096, 2 heads, 1024 (66) 29.8 : 17.2 : 14.1 : 13.7; 2000, 8 heads, 500
+// (136) 25.7 : 15.6 : 13.3 : 20.5; 4096, 4 heads, 2048 (132) 43 : 33 : 26 : 33; 2 of 2000, 8 heads, 500 (264) 26.3 : 24.0 : 23.3, but 4096, 8 heads,
+// 1024 (264) 30.9 : 35.6 : 32.3, 4 of 1000, 16 heads, 128 (576) 25.3 : 27.4 : 34.6; 100 of 20, 16 heads (1856) 32.9 : 17.7 : 23.2.
+// d 64: 5 of 200, 16 heads, 64 (208) 11.8 : 8.6 : 8.7 : 17.2; 4 of 1000, 16 heads, 512 (576) 20.8 : 20.1 : 24.5; 8 of 1000, 16 heads, 200 (1136)
+// 34.4 : 28.3 : 41.5, but 32 of 256, 32 heads, 64 (over 3000) 37.8 : 42.0 : 65.0.
+int window_split_waves(const WindowArgs& p) {
+    // (as above)
+    const int64_t widest = p.stride_s > p.kv_stride_s ? p.stride_s : p.kv_stride_s;
+    if (p.d > TD || ((int64_t)(p.max_len + 127) / 128 * 128 + OWN) * 2 * widest + 2 * p.d >= (int64_t(1) << 31)) return 0;
+    const int64_t tiles = most_tiles(p, 128) * p.H, reach = (int64_t)p.window + OWN + p.sinks, walk = p.max_len < reach ? p.max_len : reach;
+    if (most_tiles(p, OWN) * p.H * 64 * 4 >= (int64_t(1) << 32)) return 0;
+    if (tiles <= 144) return 4;
+    if (p.max_len <= OWN) return 2;
+    return (p.d <= 64 ? tiles <= 1600 && tiles * walk <= 320000 : tiles * walk <= 160000) ? 2 : 0;
+}
+template <int DP, bool PART>
+static hipError_t run_window(const WindowArgs& p, int waves, hipStream_t st) {
+    const dim3 grid((unsigned)p.n_ranks * p.H), block(64 * waves);
+    if (waves == 2) hipLaunchKernelGGL((fwd_split_kernel<DP, PART, false, false, WindowArgs, 2>), grid, block, 0, st, p, 0);
+    else hipLaunchKernelGGL((fwd_split_kernel<DP, PART, false, false, WindowArgs, 4>), grid, block, 0, st, p, 0);
+    return hipGetLastError();
+}
+hipError_t launch_window_split(WindowArgs p, int waves, hipStream_t st) {
+    p.n_ranks = (int)most_tiles(p, OWN);
+    p.by_rank = true;
+    const bool part = p.d % 8 != 0;
+    if (p.d <= 32 && !part) return run_window<32, false>(p, waves, st);
+    if (p.d <= 64) return part ? run_window<64, true>(p, waves, st) : run_window<64, false>(p, waves, st);
+    if (p.d <= 112) return part ? run_window<112, true>(p, waves, st) : run_window<112, false>(p, waves, st);
+    return part ? run_window<128, true>(p, waves, st) : run_window<128, false>(p, waves, st);
+}
+
 hipError_t launch_packed_split(PackedArgs p, bool backward, hipStream_t st) {
     if (backward)
         if (hipError_t e = launch_packed_delta(p, SA_BF16, st)) return e;

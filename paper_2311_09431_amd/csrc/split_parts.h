@@ -166,10 +166,11 @@ struct KeyCursor {
 // Forward, the end: the wavefronts' partial results (accumulators, base-2 reference m, half-wave row sum l) folded
 // into the running state of the lane's row (base: of the workgroup's rows' matrix, a: the row, clamped to the shard).
 // Returns the rows to do over (EXACT only; TERMS: V was three bf16 terms, masks are the words of RowsToRedo).  OutT: float, or __bf16
-// for rows that end here (packed sequences, p.fresh).
-template <int DP, int WAVES, bool EXACT, bool TERMS, typename Lane, typename OutT>
+// for rows that end here (packed sequences, p.fresh).  WINDOW: rows whose results are not finite (odd_acc: this wavefront's are not) are done over too.
+template <int DP, int WAVES, bool EXACT, bool TERMS, bool WINDOW = false, typename Lane, typename OutT>
 __device__ __forceinline__ uint32_t fold_forward(const StepArgs& p, f32x16 (&acc)[4], float m, float l, char* lds, float* stats,
-                                                 uint32_t* masks, const Lane& ln, int dev, int a_own, int a, float* L, OutT* O) {
+                                                 uint32_t* masks, const Lane& ln, int dev, int a_own, int a, float* L, OutT* O,
+                                                 bool odd_acc = false) {
     constexpr int MB = blocks_of(DP), N = share_of(DP, WAVES);
     const int n = ln.n, h = ln.h, d = p.d;
     const float old = p.fresh ? -INFINITY : *L;
@@ -198,12 +199,13 @@ __device__ __forceinline__ uint32_t fold_forward(const StepArgs& p, f32x16 (&acc
         for (int r = 0; r < 16; ++r) acc[mb][r] *= f;
     put_partial<DP>(lds, acc, ln);
     // a row sum that is no positive number although the row sees a key: see f32_rows.h
-    const RowsToRedo<WAVES> redo = {reinterpret_cast<uint4*>(masks), ln.lane, ln.wave, row_mask(a_own < p.c)};
+    const RowsToRedo<TERMS ? WAVES : 8> redo = {reinterpret_cast<uint4*>(masks), ln.lane, ln.wave, row_mask(a_own < p.c)};
     if (EXACT) {
         const bool odd = a_own < p.c && (not_finite<MB>(acc) || (!(l_tot > 0.f && l_tot < INFINITY) && sees_a_key(p, dev, a)));
         if (TERMS) redo.put(odd, top_acc * f, top_acc * f);
         else put_odd(masks, odd, ln.wave, ln.lane);
     }
+    if (WINDOW) put_odd(masks, a_own < p.c && (odd_acc || !(l_tot > 0.f && l_tot < INFINITY)), ln.wave, ln.lane);
 
     const float part = l_tot == 0.f ? -INFINITY : fmaf(m_all, LN2_HI, fmaf(m_all, LN2_LO, logf(l_tot)));
     const float top = fmaxf(old, part);
@@ -212,7 +214,7 @@ __device__ __forceinline__ uint32_t fold_forward(const StepArgs& p, f32x16 (&acc
     const float inv = w_sum > 0.f ? 1.f / w_sum : 0.f;
     const float f_old = w_old * inv, f_part = l_tot > 0.f ? w_part * inv / l_tot : 0.f;
     __syncthreads();
-    const uint32_t odd_rows = TERMS ? redo.take(top_acc * f, top_acc * f) : EXACT ? take_odd<WAVES>(masks) : 0;
+    const uint32_t odd_rows = TERMS ? redo.take(top_acc * f, top_acc * f) : EXACT || WINDOW ? take_odd<WAVES>(masks) : 0;
     // no row here, or no key seen: state unchanged
     if (a_own < p.c && !((odd_rows >> n) & 1) && (part != -INFINITY || p.fresh)) {
 #pragma unroll

@@ -23,6 +23,7 @@
 #pragma once
 #include "packed.h"
 #include "split_parts.h"
+#include "window.h"
 
 namespace sa {
 
@@ -185,13 +186,14 @@ __device__ inline bool odd_sum(const float (&z)[2], const f32x16 (&ds_sum)[4]) {
 // which is requested anew when the sub-tile has been read into registers.
 constexpr float RESCALE_SUM = 16777216.f;       // 2^24, see fwd_tiles.h
 // ROPE: the query rows are rotated by their position ids (d == DP).
-// Args: StepArgs, or PackedArgs for packed sequences (packed.h), whose rows are written in bf16
-template <int DP, bool PART, bool EXACT, bool ROPE = false, typename Args = StepArgs>
-__global__ void __launch_bounds__(64 * FWD_WAVES, 2)
+// Args: StepArgs, or PackedArgs for packed sequences (packed.h), whose rows are written in bf16, or WindowArgs for those with a window (window.h)
+// WAVES: fewer where walks are short, so that more workgroups share a compute unit
+template <int DP, bool PART, bool EXACT, bool ROPE = false, typename Args = StepArgs, int WAVES = FWD_WAVES>
+__global__ void __launch_bounds__(64 * WAVES, 2)
 fwd_split_kernel(Args p, int n_tiles) {
-    constexpr bool PACKED = !std::is_same<Args, StepArgs>::value;
+    constexpr bool PACKED = !std::is_same<Args, StepArgs>::value, WINDOW = std::is_same<Args, WindowArgs>::value;
     using OutT = std::conditional_t<PACKED, __bf16, float>;
-    constexpr int MB = blocks_of(DP), KS = ksteps_of(DP), WAVES = FWD_WAVES;
+    constexpr int MB = blocks_of(DP), KS = ksteps_of(DP);
     // the wavefronts' stages and the owned rows; at the end the statistics and partial results
     constexpr int TILES = WAVES * STAGE_BYTES<DP> > PARTIAL_BYTES<DP, WAVES> ? WAVES * STAGE_BYTES<DP> : PARTIAL_BYTES<DP, WAVES>;
     __shared__ __attribute__((aligned(1024))) char lds[TILES + SUB_BYTES<DP>];
@@ -225,8 +227,17 @@ fwd_split_kernel(Args p, int n_tiles) {
     dt_rsrc K = stream_rsrc((const __bf16*)p.k + kv_base, p.c, pitch, d);
     dt_rsrc V = stream_rsrc((const __bf16*)p.v + kv_base, p.c, pitch, d);
     int kv_loaded = at.kv, kv = 0, key0 = 0, shift = 0;
+    WindowWalk<OWN> walk;
+    if constexpr (WINDOW) walk = WindowWalk<OWN>(p, q0, min(q0 + OWN - 1, p.c - 1) / OWN + 1);
     // requests the next sub-tile
     auto request = [&]() {
+        if constexpr (WINDOW) {         // (at.v: its place in the walk; one behind it holds no more of anyone's keys)
+            key0 = 32 * walk.at(at.v);
+            kv = at.v < walk.n ? 0 : at.kv_end;
+            if (at.v < walk.n) loader.all(K, V, key0, k);
+            at.v += WAVES;
+            return;
+        }
         at.settle<WAVES>();
         kv = at.kv;
         key0 = 32 * at.v;
@@ -240,7 +251,8 @@ fwd_split_kernel(Args p, int n_tiles) {
         loader.all(K, V, key0, k);
         at.v += WAVES;
     };
-    at.enter<WAVES>();
+    if constexpr (WINDOW) at.v = ln.wave;
+    else at.template enter<WAVES>();
     request();
 
     float* L = p.lse + b * p.stat_stride_b + hd * p.stat_stride_h + (int64_t)dev_i * p.c + a;
@@ -279,7 +291,9 @@ fwd_split_kernel(Args p, int n_tiles) {
         for (int ks = 0; ks < 2; ++ks) score_product<PART, DP>(x, kr[ks], qf[ks], ks, part_ks);
         __builtin_amdgcn_sched_barrier(0);
         wait_lds();
-        const bool masked = key0 + 31 > min(p.c - 1, q0 + shift);          // some pair of the sub-tile is
+        bool masked = key0 + 31 > min(p.c - 1, q0 + shift);          // some pair of the sub-tile is
+        [[maybe_unused]] const int first = key0;
+        if constexpr (WINDOW) masked |= key0 <= q0 + 31 - p.window;
         const int lane_last = min(p.c - 1, a_own + shift) - key0;
         const bool rebase = rebase_shards && kv != kv_before;
         kv_before = kv;
@@ -291,6 +305,10 @@ fwd_split_kernel(Args p, int n_tiles) {
         if (masked) {
 #pragma unroll
             for (int r = 0; r < 16; ++r) x[r] = reg_row(r, h) <= lane_last ? x[r] : -INFINITY;
+            if constexpr (WINDOW) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) x[r] = in_window(p, first + reg_row(r, h), a_own) ? x[r] : -INFINITY;
+            }
         }
         auto highest = [&]() {
             float mx[2] = {x[0], x[1]};
@@ -353,8 +371,13 @@ fwd_split_kernel(Args p, int n_tiles) {
         }
     }
 
-    const uint32_t odd_rows = fold_forward<DP, WAVES, EXACT, false>(p, acc, m, l, lds, stats, masks, ln, dev, a_own, a, L,
-                                                             (OutT*)p.o + base + (int64_t)a * p.stride_s);
+    bool odd_acc = false;
+    if constexpr (WINDOW) odd_acc = window_odd<MB, PART>(acc, h, d);
+    const uint32_t odd_rows = fold_forward<DP, WAVES, EXACT, false, WINDOW>(p, acc, m, l, lds, stats, masks, ln, dev, a_own, a, L,
+                                                             (OutT*)p.o + base + (int64_t)a * p.stride_s, odd_acc);
+    if constexpr (WINDOW)
+        each_window_row<true, OWN>(odd_rows & 0xffffffffu / ((1u << WAVES) - 1) << ln.wave, (int)blockIdx.x, p.H, 0,
+                                   [&](const WindowArgs& again, int head, int row) { window_fwd_row<__hip_bfloat16>(again, head, row, ln.lane); });
     if (EXACT) each_row<WAVES>(odd_rows, ln.wave, [&](const StepArgs& again, int i) { fwd_row<__hip_bfloat16>(again, b, hd, dev_i, q0 + i, ln.lane); });
 }
 

@@ -19,11 +19,13 @@ struct WindowArgs : PackedArgs {
     int part, key_rows, n_slots;
     int slot;                   // the sequence's first one, set by the workgroup; -1: none
 };
-// Whether there are such workgroups: two launches more, against the time of a walk, rows of all heads of a group.  FAR_RULE
+// Whether there are such workgroups: two launches more, against the time of a walk, rows of all heads of a group.  (Gradient in
+// us, walking on / with them.  bf16: 1 x 1100 rows, 4 heads, 64 columns, window 64: 55.5 / 43.0; 4 x 1100, 8 heads, 128 columns, window 256: 80.5 /
+// 77.0; 1 x 600: 41.4 / 42.4; 8 x 300, 16 heads, 100 columns: 55.2 / 77.5.  fp32, the same four: 114 / 63, 221 / 193, 69.6 / 40.7, 137 / 157.)
 // The rows of a part (fewer parts where there are many first keys, whose blocks of 16 are workgroups too) and the slots that sequences
 // without a common row can have; 0: key-owning workgroups walk on.
 inline bool has_far(const WindowArgs& p) {
-    return p.sinks > 0 && (int64_t)(p.max_len - p.window) * (p.H / p.H_kv) > (p.es == 2 ? 1024 : 128);
+    return p.sinks > 0 && (int64_t)(p.max_len - p.window) * (p.H / p.H_kv) > (p.es == 2 ? 1024 : 256);
 }
 inline void set_far(WindowArgs& p) {
     p.key_rows = (p.sinks + 15) / 16 * 16;
@@ -35,6 +37,8 @@ inline void set_far(WindowArgs& p) {
 inline int64_t far_bytes(const WindowArgs& p) { return (int64_t)p.n_slots * p.H_kv * p.key_rows * 2 * p.d * 4; }
 hipError_t launch_window_far(const WindowArgs& p, int dtype, hipStream_t st);
 hipError_t launch_window_fwd(WindowArgs p, hipStream_t st);
+int window_split_waves(const WindowArgs& p);                                           // 32-row workgroups (packed_split.hip)
+hipError_t launch_window_split(WindowArgs p, int waves, hipStream_t st);
 hipError_t launch_window_bwd(WindowArgs p, hipStream_t st);
 hipError_t launch_window_f32(WindowArgs p, bool backward, hipStream_t st);
 bool window_in_terms(const WindowArgs& p);

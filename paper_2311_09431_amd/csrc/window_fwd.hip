@@ -14,6 +14,7 @@ hipError_t launch(const WindowArgs& p, hipStream_t st) {
 }  // namespace
 
 hipError_t launch_window_fwd(WindowArgs p, hipStream_t st) {
+    if (const int waves = window_split_waves(p)) return launch_window_split(p, waves, st);
     p.n_ranks = (int)most_tiles(p, BM);
     p.by_rank = true;
     const bool part = p.d % 8 != 0;

@@ -409,3 +409,34 @@ def test_empty_calls():
 def test_more_heads_than_a_launch_takes():
     H, lens = 65535, [2, 1] * 100
     compare(lens, H, H, 4, BF16, 1, 0, *run(lens, H, H, 4, BF16, 1, 0), heads=[0, 20970, 20971, 41942, 62912, 62913, 65534])
+
+
+# launches of few tiles, by workgroups of 32 rows of four wavefronts or two, and others
+@pytest.mark.parametrize("d", [8, 32, 52, 64, 100, 104, 128, 132])
+@pytest.mark.parametrize("H,H_kv,lens,window,sinks", [(2, 1, [300, 33, 0, 1, 95], 1, 0), (2, 2, [500, 64], 33, 40), (16, 4, [200, 190, 180, 170, 160], 64, 4),
+                                                      (48, 8, [31, 1, 17, 0, 32, 30], 7, 2), (48, 8, [700, 300], 130, 0)])
+def test_launches_of_few_tiles(H, H_kv, lens, window, sinks, d):
+    compare(lens, H, H_kv, d, BF16, window, sinks, *run(lens, H, H_kv, d, BF16, window, sinks))
+
+
+@pytest.mark.parametrize("d", [64, 100])
+@pytest.mark.parametrize("H", [2, 40])
+def test_infinities_in_launches_of_few_tiles(H, d):
+    """A value that is no number reaches the rows that see its key, of the heads that share it, and no others, whichever workgroups a launch has."""
+    lens, window, sinks, at = [300, 200], 50, 3, 260
+    (q, k, v, g), out, lse, clean = run(lens, H, H // 2, d, BF16, window, sinks)
+    off, n = lengths_to_offsets(lens).cuda(), torch.arange(500)
+    # rows beside them may be formed anew without rounding their probabilities: 2^-8 of the values, and both results' own rounding; lse, sums of up to
+    # 64 terms of either order
+    off_out, off_lse = 2.0 ** -8 * (v.float().abs().max() + 2 * out.float().abs().max()), 64 * 2.0 ** -24 * (1 + lse.abs().max())
+    for key, rows in ((at, (n >= at) & (n < 300)), (301, n >= 301)):
+        seen, other = rows.cuda(), ~rows.cuda()
+        for which in (1, 2):
+            ins = [q, k.clone(), v.clone()]
+            ins[which][key, 0, 5] = NAN
+            o2, lse2 = torch.full_like(out, 7), torch.full_like(lse, 7)
+            sa.sa_attn_window_fwd(*ins, off, o2, lse2, max(lens), window, sinks)
+            assert torch.isnan(o2[seen][:, :2, slice(None) if which == 1 else 5]).all()
+            assert torch.equal(torch.isnan(lse2[:2, seen]), torch.full_like(lse2[:2, seen], which == 1, dtype=torch.bool))
+            assert torch.equal(o2[:, 2:], out[:, 2:]) and torch.equal(lse2[2:], lse[2:])
+            assert (o2[other].float() - out[other].float()).abs().max() <= off_out and (lse2[:, other] - lse[:, other]).abs().max() <= off_lse
