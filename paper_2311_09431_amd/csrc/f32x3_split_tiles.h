@@ -13,6 +13,7 @@
 #include "f32x3_parts.h"
 #include "packed.h"
 #include "split_parts.h"
+#include "window.h"
 
 namespace sa {
 
@@ -242,11 +243,11 @@ __device__ __forceinline__ void accumulate(f32x16 (&acc)[4], const char* raw, co
 }
 
 // ------------------------------------------------------------------ forward
-// Args: StepArgs, or PackedArgs for packed sequences (packed.h)
+// Args: StepArgs, or PackedArgs for packed sequences (packed.h), or WindowArgs for those with a window (window.h)
 template <int DP, typename Args = StepArgs>
 __global__ void __launch_bounds__(64 * WAVES_OF<DP>, WAVES_OF<DP> / 4)
 fwd_f32x3_split_kernel(Args p, int n_tiles) {
-    constexpr bool PACKED = !std::is_same<Args, StepArgs>::value;
+    constexpr bool PACKED = !std::is_same<Args, StepArgs>::value, WINDOW = std::is_same<Args, WindowArgs>::value;
     constexpr int WAVES = WAVES_OF<DP>, MB = blocks_of(DP);
     static_assert(PARTIAL_BYTES<DP, WAVES> <= STAGES_BYTES<DP>, "partial results");
     __shared__ __attribute__((aligned(1024))) char lds[STAGES_BYTES<DP> + OWN_BYTES<DP>];
@@ -279,8 +280,16 @@ fwd_f32x3_split_kernel(Args p, int n_tiles) {
     // (behind the walk's end: rows beyond the matrix, whose loads deliver zeros without a look at memory)
     const int beyond = 32 * at.n_full;
     int key0, shift;                    // the sub-tile; key0 == beyond: none
+    WindowWalk<OWN> walk;
+    if constexpr (WINDOW) walk = WindowWalk<OWN>(p, q0, min(q0 + OWN - 1, p.c - 1) / OWN + 1);
     auto take = [&]() {
-        at.settle<WAVES>();
+        if constexpr (WINDOW) {         // (at.v: the sub-tile's place in the walk)
+            key0 = at.v < walk.n ? 32 * walk.at(at.v) : beyond;
+            shift = 0;
+            at.v += WAVES;
+            return;
+        }
+        at.template settle<WAVES>();
         key0 = at.kv < at.kv_end ? 32 * at.v : beyond;
         shift = at.shift;
         at.v += WAVES;
@@ -290,7 +299,8 @@ fwd_f32x3_split_kernel(Args p, int n_tiles) {
             kv_at = at.kv;
         }
     };
-    at.enter<WAVES>();
+    if constexpr (WINDOW) at.v = ln.wave;
+    else at.template enter<WAVES>();
     take();
     loader.load(K, key0, k);
     loader.load(V, key0, v);
@@ -305,7 +315,9 @@ fwd_f32x3_split_kernel(Args p, int n_tiles) {
     while (key0 != beyond) {
         wait_all_but<LOADS<DP>>();
         f32x16 x = scores<DP>(k, own[0], ln, [](int) {});
-        const bool masked = key0 + 31 > min(p.c - 1, q0 + shift);          // some pair of the sub-tile is
+        bool masked = key0 + 31 > min(p.c - 1, q0 + shift);          // some pair of the sub-tile is
+        [[maybe_unused]] const int first = key0;
+        if constexpr (WINDOW) masked |= key0 <= q0 + 31 - p.window;
         const int lane_last = min(p.c - 1, a_own + shift) - key0;
         take();
         wait_lds();
@@ -313,6 +325,10 @@ fwd_f32x3_split_kernel(Args p, int n_tiles) {
         if (masked) {
 #pragma unroll
             for (int r = 0; r < 16; ++r) x[r] = reg_row(r, h) <= lane_last ? x[r] : -INFINITY;
+            if constexpr (WINDOW) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) x[r] = in_window(p, first + reg_row(r, h), a_own) ? x[r] : -INFINITY;
+            }
         }
         float mx[2] = {x[0], x[1]};
 #pragma unroll
@@ -345,15 +361,17 @@ fwd_f32x3_split_kernel(Args p, int n_tiles) {
     const uint32_t odd_rows = fold_forward<DP, WAVES, true, true>(p, acc, m, l, lds, stats, masks, ln, dev, a_own, a, L,
                                                             p.o + base + (int64_t)a * p.stride_s);
     each_row<WAVES>(odd_rows, ln.wave, [&](const StepArgs& again, int i) {
-        if constexpr (PACKED) fwd_row<float>(p, b, hd, dev_i, q0 + i, ln.lane);
+        if constexpr (WINDOW) window_fwd_row<float>(p, hd, q0 + i, ln.lane);
+        else if constexpr (PACKED) fwd_row<float>(p, b, hd, dev_i, q0 + i, ln.lane);
         else fwd_row<float>(again, b, hd, dev_i, q0 + i, ln.lane);
     });
 }
 
 // ----------------------------------------------------------------------- dQ
 // PACKED: linear is the tile's place and the head in a sequence that p is the arguments of
-template <int DP, bool PACKED = false>
-__device__ inline void bwd_dq(const StepArgs& p, int n_tiles, int linear, char* lds, uint32_t* masks) {
+template <int DP, bool PACKED = false, typename Args = StepArgs>
+__device__ inline void bwd_dq(const Args& p, int n_tiles, int linear, char* lds, uint32_t* masks) {
+    constexpr bool WINDOW = std::is_same<Args, WindowArgs>::value;
     constexpr int WAVES = WAVES_OF<DP>, N = share_of(DP, WAVES);
     const RawLane<DP> ln;
     const int n = ln.n, h = ln.h;
@@ -378,8 +396,16 @@ __device__ inline void bwd_dq(const StepArgs& p, int n_tiles, int linear, char* 
     int kv_at = at.kv;
     const int beyond = 32 * at.n_full;          // as in the forward kernel
     int key0, shift;
+    WindowWalk<OWN> walk;
+    if constexpr (WINDOW) walk = WindowWalk<OWN>(p, q0, min(q0 + OWN - 1, p.c - 1) / OWN + 1);
     auto take = [&]() {
-        at.settle<WAVES>();
+        if constexpr (WINDOW) {         // (at.v: the sub-tile's place in the walk)
+            key0 = at.v < walk.n ? 32 * walk.at(at.v) : beyond;
+            shift = 0;
+            at.v += WAVES;
+            return;
+        }
+        at.template settle<WAVES>();
         key0 = at.kv < at.kv_end ? 32 * at.v : beyond;
         shift = at.shift;
         at.v += WAVES;
@@ -389,7 +415,8 @@ __device__ inline void bwd_dq(const StepArgs& p, int n_tiles, int linear, char* 
             kv_at = at.kv;
         }
     };
-    at.enter<WAVES>();
+    if constexpr (WINDOW) at.v = ln.wave;
+    else at.template enter<WAVES>();
     take();
     loader.load(V, key0, v);
     loader.load(K, key0, k);
@@ -408,7 +435,9 @@ __device__ inline void bwd_dq(const StepArgs& p, int n_tiles, int linear, char* 
     while (key0 != beyond) {
         wait_all_but<LOADS<DP>>();
         const f32x16 dp = scores<DP>(v, own[1], ln, [](int) {});
-        const bool masked = key0 + 31 > min(p.c - 1, q0 + shift);
+        bool masked = key0 + 31 > min(p.c - 1, q0 + shift);
+        [[maybe_unused]] const int first = key0;
+        if constexpr (WINDOW) masked |= key0 <= q0 + 31 - p.window;
         const int lane_last = min(p.c - 1, a_own + shift) - key0;
         take();
         wait_lds();
@@ -420,6 +449,10 @@ __device__ inline void bwd_dq(const StepArgs& p, int n_tiles, int linear, char* 
         if (masked) {
 #pragma unroll
             for (int r = 0; r < 16; ++r) x[r] = reg_row(r, h) <= lane_last ? x[r] : 0.f;
+            if constexpr (WINDOW) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) x[r] = in_window(p, first + reg_row(r, h), a_own) ? x[r] : 0.f;
+            }
         }
 #pragma unroll
         for (int r = 0; r < 16; ++r) x[r] *= dp[r] - delta;
@@ -442,7 +475,8 @@ __device__ inline void bwd_dq(const StepArgs& p, int n_tiles, int linear, char* 
     const uint32_t odd_rows = redo.take(top, top);
     if (a_own < p.c && !((odd_rows >> n) & 1)) add_rows<DP, WAVES>(DQ, old, lds, p.scale, d, ln);
     each_row<WAVES>(odd_rows, ln.wave, [&](const StepArgs& again, int i) {
-        if constexpr (PACKED) dq_row<float>(p, b, hd, dev_i, q0 + i, ln.lane);
+        if constexpr (WINDOW) window_dq_row<float>(p, hd, q0 + i, ln.lane);
+        else if constexpr (PACKED) dq_row<float>(p, b, hd, dev_i, q0 + i, ln.lane);
         else dq_row<float>(again, b, hd, dev_i, q0 + i, ln.lane);
     });
 }
@@ -450,8 +484,9 @@ __device__ inline void bwd_dq(const StepArgs& p, int n_tiles, int linear, char* 
 // -------------------------------------------------------------------- dK/dV
 // Owned rows are keys, the streamed ones queries with their LSE and delta beside them; the query heads that share
 // the key/value head and the query shards that see it come one after the other.
-template <int DP, bool PACKED = false>
-__device__ inline void bwd_dkdv(const StepArgs& p, int n_tiles, int linear, char* lds, char* stats, uint32_t* masks) {
+template <int DP, bool PACKED = false, typename Args = StepArgs>
+__device__ inline void bwd_dkdv(const Args& p, int n_tiles, int linear, char* lds, char* stats, uint32_t* masks) {
+    constexpr bool WINDOW = std::is_same<Args, WindowArgs>::value;
     constexpr int WAVES = WAVES_OF<DP>, KS = DP / 16, N = share_of(DP, WAVES);
     const RawLane<DP> ln;
     const int n = ln.n, h = ln.h;
@@ -474,7 +509,13 @@ __device__ inline void bwd_dkdv(const StepArgs& p, int n_tiles, int linear, char
     char* const g = q + RAW_BYTES<DP>;
     char* const stat = stats + ln.wave * STAT_BYTES;
     const int q_dev0 = p.layout == SA_STRIPED ? p.q_dev : max(p.q_dev, dev), q_end = p.q_dev + p.n_q;
-    const int n_sub = (p.c + 31) / 32;
+    int n_sub = (p.c + 31) / 32, lane_end = p.c, full_to = 0;       // one past the last query that sees the lane's key; WINDOW: all keys
+    const int beyond = 32 * n_sub;
+    if constexpr (WINDOW) {
+        n_sub = (walk_end(p, k0, k0 + OWN - 1) + 31) / 32;
+        lane_end = walk_end(p, key_own);
+        full_to = min(p.c, k0 + p.window);
+    }
     int member = q_dev0 < q_end ? 0 : group, q_dev = q_dev0, v = 0, turn = 0;
     int block_shift = 0;              // key b is seen by the block's queries from b + block_shift on
     dt_rsrc Q, G, S, E;
@@ -492,7 +533,6 @@ __device__ inline void bwd_dkdv(const StepArgs& p, int n_tiles, int linear, char
         S = dt_make_rsrc(p.lse + sbase, p.c, 4, 2);
         E = dt_make_rsrc(p.delta + sbase, p.c, 4, 2);
     };
-    const int beyond = 32 * n_sub;
     int a0, shift;                      // the sub-tile; a0 == beyond: none
     auto take = [&]() {
         while (v >= n_sub && member < group) {
@@ -538,8 +578,8 @@ __device__ inline void bwd_dkdv(const StepArgs& p, int n_tiles, int linear, char
                 pr[r + 1] = kappa.exp2(pr[r + 1], hi, lo);
             }
         });
-        if (a0 < k0 + OWN - 1 + shift || a0 + 32 > p.c) {       // some pair of the sub-tile is masked
-            const int lane_first = key_own + shift - a0, rows = p.c - a0;
+        if (a0 < k0 + OWN - 1 + shift || a0 + 32 > (WINDOW ? full_to : p.c)) {      // some pair of the sub-tile is masked
+            const int lane_first = key_own + shift - a0, rows = lane_end - a0;
 #pragma unroll
             for (int r = 0; r < 16; ++r) pr[r] = reg_row(r, h) >= lane_first && reg_row(r, h) < rows ? pr[r] : 0.f;
         }
@@ -564,21 +604,31 @@ __device__ inline void bwd_dkdv(const StepArgs& p, int n_tiles, int linear, char
     float4 old_v[N], old_k[N];
     load_old<DP, WAVES>(old_v, p.dv + row, d, !p.fresh && key_own < p.c, ln);
     load_old<DP, WAVES>(old_k, p.dk + row, d, !p.fresh && key_own < p.c, ln);
-    const RowsToRedo<WAVES> redo = {reinterpret_cast<uint4*>(masks), ln.lane, ln.wave, row_mask(key_own < p.c)};
+    bool ends = key_own < p.c;                  // the key's sums end here
+    if constexpr (WINDOW) ends = ends && !is_far(p, key_own);
+    const RowsToRedo<WAVES> redo = {reinterpret_cast<uint4*>(masks), ln.lane, ln.wave, row_mask(ends)};
     const float top_v = loudest<blocks_of(DP)>(accv), top_k = loudest<blocks_of(DP)>(acck);
-    const bool odd = key_own < p.c && (not_finite<blocks_of(DP)>(accv) || not_finite<blocks_of(DP)>(acck));
+    const bool odd = ends && (not_finite<blocks_of(DP)>(accv) || not_finite<blocks_of(DP)>(acck));
     __syncthreads();
     put_partial<DP>(lds, accv, ln);
     put_partial<DP>(lds + HALF, acck, ln);
     redo.put(odd, top_v, top_k);
     __syncthreads();
     const uint32_t odd_rows = redo.take(top_v, top_k);
-    if (key_own < p.c && !((odd_rows >> n) & 1)) {
+    if (ends && !((odd_rows >> n) & 1)) {
         add_rows<DP, WAVES>(p.dv + row, old_v, lds, 1.f, d, ln);
         add_rows<DP, WAVES>(p.dk + row, old_k, lds + HALF, p.scale, d, ln);
     }
+    if constexpr (WINDOW) {
+        if (p.slot >= 0 && key_own < p.c && !ends) {            // (the old ones: zeros)
+            float* const to = slot_row(p, p.slot, kvh, key_own);
+            add_rows<DP, WAVES>(to, old_v, lds, 1.f, d, ln);
+            add_rows<DP, WAVES>(to + d, old_k, lds + HALF, p.scale, d, ln);
+        }
+    }
     each_row<WAVES>(odd_rows, ln.wave, [&](const StepArgs& again, int i) {
-        if constexpr (PACKED) dkdv_row<float>(p, b, kvh, dev_i, k0 + i, 0, d, ln.lane);
+        if constexpr (WINDOW) window_dkdv_row<float>(p, kvh, k0 + i, 0, d, ln.lane);
+        else if constexpr (PACKED) dkdv_row<float>(p, b, kvh, dev_i, k0 + i, 0, d, ln.lane);
         else dkdv_row<float>(again, b, kvh, dev_i, k0 + i, 0, d, ln.lane);
     });
 }

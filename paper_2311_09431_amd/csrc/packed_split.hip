@@ -1,5 +1,6 @@
 // Causal attention of packed sequences and its gradient, bf16, launches of few tiles: the ring step's workgroups of 32 rows
-// (split_tiles.h), each on one tile of one sequence (packed.h).  Bound by the length of a walk, which several wavefronts share.
+// (split_tiles.h), each on one tile of one sequence (packed.h).  Bound by the length of a walk, which several wavefronts share.  The forward with a
+// window too (window.h).
 #include "split_tiles.h"
 
 namespace sa {

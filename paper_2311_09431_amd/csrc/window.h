@@ -41,8 +41,8 @@ int window_split_waves(const WindowArgs& p);                                    
 hipError_t launch_window_split(WindowArgs p, int waves, hipStream_t st);
 hipError_t launch_window_bwd(WindowArgs p, hipStream_t st);
 hipError_t launch_window_f32(WindowArgs p, bool backward, hipStream_t st);
-bool window_in_terms(const WindowArgs& p);
 hipError_t launch_window_f32x3(WindowArgs p, bool backward, hipStream_t st);           // up to 128 columns
+hipError_t launch_window_f32x3_split(WindowArgs p, bool backward, hipStream_t st);     // by workgroups of 32 rows
 
 // the first key of row a's window
 __device__ inline int window_start(const WindowArgs& p, int a) { return max(0, a - p.window + 1); }

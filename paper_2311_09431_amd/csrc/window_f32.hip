@@ -40,21 +40,25 @@ hipError_t run(WindowArgs p, bool backward, hipStream_t st) {
 
 }  // namespace
 
-// Up to 128 columns in three bf16 terms, but in launches of few tiles (of 128 rows, as many as there can be, of all heads), whose workgroups on the fp32
-// instruction are four times as many.  us, instruction : terms, forward and backward, d 128: 5 sequences of up to 777 rows, 16 heads on 8, window 100
-// (d 100) 85, 256 : 42, 188, 4 of up to 2000, 16 heads, window 500, 209, 567 : 106, 298, a sequence of 4000, 8 heads, window 1000, 302, 772 : 137,
-// 401; but 2 heads on 1, window 2000 (64 tiles), 140, 465 : 241, 771, a sequence of 200, one head, 22, 48 : 27, 64; 8 of up to 1000, 8 heads, d 32,
-// window 64, 19, 72 : 21, 67.
-bool window_in_terms(const WindowArgs& p) { return p.d <= 128 && most_tiles(p, 128) * p.H > 64; }
+// Up to 128 columns in three bf16 terms, launches of few tiles (of 128 rows, as many as there can be, of all heads) by workgroups of 32 rows.  us, fp32
+// instruction : 32 rows : 128 rows, forward and gradient.  d 128: a sequence of 4000 rows, 2 heads on 1, window 2000 (64 tiles) 140, 416 : 72, 255 :
+// 242, 728; of 200, one head, 22, 37 : 18, 39 : 27, 49; but of 1000, 16 heads, 128 (144) 59, 160 : 43, 158 : 40, 91; of 4000, 8 heads, 1000 (264)
+// 303, 754 : 172, 532 : 139, 378; 5 of up to 777, 16 heads on 8, 100 (d 100) 85, 209 : 71, 191 : 42, 141.  d 64: 2 of up to 1000, 2 heads, 300 (32)
+// 37, 60 : 12, 34 : 39, 59; 2000, 4 heads, 200 (68) 30, 86 : 13, 48 : 33, 55; but 5 of up to 777, 16 heads on 8, 100, 82, 193 : 37, 93 : 27, 75.
+static bool few_tiles(const WindowArgs& p, bool backward) {
+    StepArgs longest = p;
+    longest.c = p.max_len;
+    longest.B = 1;
+    const bool fits = most_tiles(p, 32) * p.H * 64 * 8 * 2 < (int64_t(1) << 32);
+    return most_tiles(p, 128) * p.H <= 96 && fits && f32x3_split_supported(longest, backward);
+}
 
 hipError_t launch_window_f32(WindowArgs p, bool backward, hipStream_t st) {
     if (backward)
         if (hipError_t e = launch_packed_delta(p, SA_F32, st)) return e;
     p.by_rank = true;
-    if (p.d > 128) return run<256, 2>(p, backward, st);
-    if (window_in_terms(p)) return launch_window_f32x3(p, backward, st);
-    if (p.d <= 32) return run<32, 4>(p, backward, st);
-    return run<128, 4>(p, backward, st);
+    if (p.d <= 128) return few_tiles(p, backward) ? launch_window_f32x3_split(p, backward, st) : launch_window_f32x3(p, backward, st);
+    return run<256, 2>(p, backward, st);
 }
 
 }  // namespace sa

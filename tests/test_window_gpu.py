@@ -100,7 +100,7 @@ def test_longer(dtype, n, window, sinks):
 # sequences with and without such rows
 @pytest.mark.parametrize("dtype,d", [(BF16, 4), (BF16, 32), (BF16, 60), (BF16, 64), (BF16, 100), (BF16, 128), (BF16, 132), (BF16, 256), (F32, 20), (F32, 64), (F32, 100),
                                      (F32, 128), (F32, 256)])
-@pytest.mark.parametrize("H,H_kv,lens,window,sinks", [(2, 1, [1300, 40, 0, 700, 100], 70, 4), (8, 1, [33, 400], 5, 37), (2, 2, [1900], 800, 130)])
+@pytest.mark.parametrize("H,H_kv,lens,window,sinks", [(2, 1, [1300, 40, 0, 700, 100], 70, 4), (8, 1, [33, 400], 5, 37), (2, 2, [1900], 800, 130), (16, 4, [700, 300, 128, 2], 100, 20)])
 def test_first_keys_seen_from_far(H, H_kv, lens, window, sinks, d, dtype):
     r = run(lens, H, H_kv, d, dtype, window, sinks)
     assert sa.sa_attn_window_bwd_workspace(r[0][0], r[0][1], lengths_to_offsets(lens), max(lens), window, sinks) > 0
@@ -411,12 +411,13 @@ def test_more_heads_than_a_launch_takes():
     compare(lens, H, H, 4, BF16, 1, 0, *run(lens, H, H, 4, BF16, 1, 0), heads=[0, 20970, 20971, 41942, 62912, 62913, 65534])
 
 
-# launches of few tiles, by workgroups of 32 rows of four wavefronts or two, and others
+# launches of few tiles, by workgroups of 32 rows, and others
+@pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("d", [8, 32, 52, 64, 100, 104, 128, 132])
 @pytest.mark.parametrize("H,H_kv,lens,window,sinks", [(2, 1, [300, 33, 0, 1, 95], 1, 0), (2, 2, [500, 64], 33, 40), (16, 4, [200, 190, 180, 170, 160], 64, 4),
                                                       (48, 8, [31, 1, 17, 0, 32, 30], 7, 2), (48, 8, [700, 300], 130, 0)])
-def test_launches_of_few_tiles(H, H_kv, lens, window, sinks, d):
-    compare(lens, H, H_kv, d, BF16, window, sinks, *run(lens, H, H_kv, d, BF16, window, sinks))
+def test_launches_of_few_tiles(H, H_kv, lens, window, sinks, d, dtype):
+    compare(lens, H, H_kv, d, dtype, window, sinks, *run(lens, H, H_kv, d, dtype, window, sinks))
 
 
 @pytest.mark.parametrize("d", [64, 100])
