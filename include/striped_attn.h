@@ -301,7 +301,7 @@ typedef struct {
 
 /*
  * Forward and backward: as sa_attn_packed_fwd and sa_attn_packed_bwd, with their arguments, types, strides, roundings and errors, over the pairs
- * that the window leaves.  The time goes by these pairs, in tiles of 128 rows and keys (fp32: 32), not by the sequences' lengths squared.
+ * that the window leaves.  The time goes by these pairs, in tiles of up to 128 rows and keys, not by the sequences' lengths squared.
  * Infinities and NaN: as in a sum over the pairs that a row sees alone, in both types.  A row with a NaN or +inf score is NaN in O and LSE, a key
  * at -inf has no weight, a row that sees no other key is NaN; nothing of a key that a row does not see reaches it.
  * workspace (backward): sa_attn_window_bwd_workspace(shape, window) bytes, 16-byte aligned, of any content; NULL where that is 0.  Calls that may run

@@ -4,7 +4,9 @@
 // As decode.hip has it for one token, with rows in the place of query heads: a unit is (sequence, key/value head, 16, 64 or 128 of the sequence's rows), row
 // i G + g being drafted token i and query head g of the group of G.  Shares of chunks, references and sums of their own for wavefronts and pieces,
 // and the joining of pieces in a second launch are as there; a sequence has as many units as its own draft needs.  Two kernels: tree_kernel takes 16 rows
-// with everything in registers, as a new token's heads; tree_tiles_kernel more, through LDS.
+// with everything in registers, as a new token's heads; tree_tiles_kernel more, through LDS.  Bound by memory where there is much of it: 32 sequences of 1 to
+// 8192 tokens, drafts of up to 32, 32 heads on 8 of 128 columns, 174 us, 3.5 TB/s, 12 of it the joining; else by a launch's latency: one of 1500, 8 drafted,
+// 13.5 us, both launches.
 //
 // What a row does not see has a score of -inf.  Its weight of zero would still make a NaN of an infinite or NaN value, so such tokens are taken out of the
 // products and added to the rows that see them by vector instructions; only tiles with drafted tokens are looked at for them.
@@ -1007,7 +1009,7 @@ tree_join_kernel(TreeArgs p) {
 }
 
 // Many rows: a wavefront has four neighbouring ones of a unit, 16 lanes each, which have their pieces in common.  (A wavefront a row: 21 us for 32 sequences'
-// drafts of up to 32, 32 heads, where this takes JOIN_US.)
+// drafts of up to 32, 32 heads, where this takes 12.)
 template <typename T, int DP, int CH, int ROWS>
 __global__ void __launch_bounds__(256)
 tree_join_rows_kernel(TreeArgs p) {
@@ -1075,6 +1077,14 @@ constexpr int columns(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : d <= 128 ? 1
 constexpr int tile_columns(int d) { return d <= 64 ? 64 : 128; }
 // tree_tiles_kernel's launches
 constexpr bool in_tiles(int rows, int d, int dtype) { return dtype == SA_BF16 && d <= 128 && rows > 16; }
+// of those, launches of few units and tokens, which 16 rows a unit take less time for although they read the cache once for each: more workgroups share
+// them, and code and parts are smaller.  us, tiles : 16 rows, d 128, 32 heads on 8 if not said: 8 drafted tokens (32 rows a unit), one sequence of 1500
+// 17.8 : 13.8, 6000 24.2 : 18.7, 16000 32.0 : 30.0, 24000 36.9 : 39.2, 60000 58 : 81; 32 drafted, 1500 x 4 34.6 : 29.3, 6000 48 : 30, 16000 62 : 85; 32 of 1500,
+// 8 heads on 1, 29.6 : 22.3; but 16 of 300, 32 drafted (1024 units) 24.6 : 35.1, 64 of 500, 16 drafted 34.6 : 86.9.
+bool in_few_rows(const TreeArgs& a) {
+    const int64_t units = (int64_t)a.B * a.H_kv * ((a.T * (a.H / a.H_kv) + 15) / 16);
+    return units <= 256 && units * a.max_pages * a.page_size <= 400000;
+}
 constexpr int row_groups(int rows) { return rows <= 64 ? 2 : 4; }
 constexpr int workgroups(int DP) { return N_CU * (DP > 128 ? 1 : 2); }
 
@@ -1134,7 +1144,7 @@ int64_t tree_workspace(int rows, int d, int dtype) {
 
 hipError_t launch_tree(const TreeArgs& a, int dtype, hipStream_t st) {
     if (dtype == SA_F32) return launch<float>(a, st);
-    if (in_tiles(a.T * (a.H / a.H_kv), a.d, dtype)) {
+    if (in_tiles(a.T * (a.H / a.H_kv), a.d, dtype) && !in_few_rows(a)) {
         if (a.d <= 64) return a.d % 8 ? launch_tiles<64, true>(a, st) : launch_tiles<64, false>(a, st);
         return a.d % 8 ? launch_tiles<128, true>(a, st) : launch_tiles<128, false>(a, st);
     }

@@ -1,4 +1,5 @@
-// Attention with a window (window.h) and its gradient, fp32 storage, on the fp32 matrix cores (f32_tiles.h).
+// Attention with a window (window.h) and its gradient, fp32 storage, on the fp32 matrix cores (f32_tiles.h): above 128 columns.  Up to
+// 128 by three bf16 terms a number (window_f32x3.hip, packed_f32x3_split.hip).
 #include "f32_tiles.h"
 
 namespace sa {

@@ -5,7 +5,8 @@
 // rows 4 j + r of key n) and once turned round in registers (dV^T += dO^T P, dK^T += Q^T dS).  P comes from the rows' LSE.  Four wavefronts take tiles of rows in
 // turn, their sums meet in LDS.  In bf16 P and dS meet dO and Q as bf16, as in the other kernels.
 //
-// Bound by memory: Q and dO are read once more, in both orders (the second from the caches).
+// Bound by the latency of its reads: Q and dO are read once more, in both orders (the second from the caches).  2 sequences of up to 16384 rows, 16 heads
+// on 8, bf16, 128 columns: 52 us, 2.9 TB/s; joining the parts' sums 17.
 #include <hip/hip_bf16.h>
 
 #include "mfma_tiles.h"

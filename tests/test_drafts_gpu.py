@@ -186,6 +186,9 @@ def test_window_decode_any_length_stays_within_the_table(dtype, width):
 
 # ---------------------------------------------------------------- drafted tokens
 
+# tables of few pages and of many, in small launches and beside so many sequences without a draft that the launch is a large one
+WAYS = WIDTHS + [(None, 260), (200, 260)]
+
 
 def trees(drafts, T, seed, empty=False):
     """int64 [B, T] masks of random trees, whose tokens see whom they descend from and themselves (empty: some see nothing), and as booleans."""
@@ -212,6 +215,8 @@ class Tree:
 
     def __init__(self, lens, drafts, T, H, H_kv, d, dtype, page=16, order="shd", seed=1, width=None, empty=False, scale=None, mutate=None, with_lse=True,
                  with_drafts=True):
+        width, others = width if isinstance(width, tuple) else (width, 0)
+        lens, drafts = list(lens) + [0] * others, list(drafts) + [0] * others
         self.lens, self.drafts, self.dtype, self.scale, self.shape = lens, drafts, dtype, scale, (len(lens), T, H, H_kv, d)
         total = [a + b for a, b in zip(lens, drafts)]
         self.table, pool = tables(total, page, seed, width=width)
@@ -249,7 +254,7 @@ class Tree:
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("d", [4, 20, 32, 64, 68, 100, 128, 132, 200, 256])
-@pytest.mark.parametrize("width", WIDTHS)
+@pytest.mark.parametrize("width", WAYS)
 def test_tree_head_dimensions(width, d, dtype):
     Tree([1, 0, 17, 300, 129, 14], [5, 3, 1, 0, 4, 5], 5, 4, 2, d, dtype, width=width).compare()
 
@@ -260,7 +265,7 @@ def test_tree_head_dimensions(width, d, dtype):
                                       (64, 1, 1), (64, 4, 1), (63, 12, 2), (5, 64, 1)])
 @pytest.mark.parametrize("order", ["shd", "hsd"])
 def test_tree_rows(order, T, H, H_kv, dtype):
-    for width in WIDTHS:
+    for width in WAYS:
         drafts = [T, max(1, T // 2), 0, 1]
         Tree([250, 33, 5, 0], drafts, T, H, H_kv, 64, dtype, order=order, width=width, seed=T + H).compare()
 
@@ -269,14 +274,14 @@ def test_tree_rows(order, T, H, H_kv, dtype):
 @pytest.mark.parametrize("d", [32, 128, 256])
 @pytest.mark.parametrize("T,H", [(4, 4), (9, 4), (30, 4)])
 def test_tree_rows_and_dimensions(T, H, d, dtype):
-    for width in WIDTHS:
+    for width in WAYS:
         Tree([300, 129], [T, T - 1], T, H, 1, d, dtype, width=width, seed=T).compare()
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("page", [16, 32, 48, 64, 256])
 def test_tree_page_sizes(page, dtype):
-    for width in WIDTHS:
+    for width in WAYS:
         Tree([500, 1, 129, 0, 64], [7, 20, 3, 20, 16], 20, 4, 2, 64, dtype, page=page, width=width).compare()
 
 
@@ -287,7 +292,7 @@ def test_tree_shares(lens, drafts, T, d):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
-@pytest.mark.parametrize("width", WIDTHS)
+@pytest.mark.parametrize("width", WAYS)
 def test_tree_rows_that_see_nothing(width, dtype):
     """Masks that leave a row empty, in front of which no token lies: zero and -inf; with tokens in front these are what it sees."""
     Tree([0, 40, 0], [6, 6, 1], 6, 4, 2, 64, dtype, width=width, empty=True, seed=4).compare()
@@ -317,7 +322,7 @@ def test_tree_random():
         lens, drafts = [rng.randint(0, 900) for _ in range(n)], [rng.randint(0, T) for _ in range(n)]
         H, page, width, order = H_kv * rng.choice([1, 2, 4, 8]), rng.choice([16, 48, 128]), rng.choice([None, 200]), rng.choice(["shd", "hsd"])
         print(i, dtype, d, H, H_kv, T, lens, drafts, page, width, order, flush=True)
-        Tree(lens, drafts, T, H, H_kv, d, dtype, page, order, seed=i, width=width, empty=rng.random() < 0.3).compare()
+        Tree(lens, drafts, T, H, H_kv, d, dtype, page, order, seed=i, width=(width, 0 if i % 2 else 260 // H_kv), empty=rng.random() < 0.3).compare()
 
 
 def test_tree_offsets_beyond_32_bits():
@@ -339,7 +344,7 @@ def test_tree_offsets_beyond_32_bits():
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
-@pytest.mark.parametrize("width", WIDTHS)
+@pytest.mark.parametrize("width", WAYS)
 @pytest.mark.parametrize("bad", [NAN, INF, -INF])
 @pytest.mark.parametrize("d", [64, 100, 256])
 def test_drafted_tokens_that_are_no_numbers(d, bad, width, dtype):
@@ -372,7 +377,7 @@ def test_drafted_tokens_that_are_no_numbers(d, bad, width, dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
-@pytest.mark.parametrize("width", WIDTHS)
+@pytest.mark.parametrize("width", WAYS)
 def test_tree_pages_that_are_none(width, dtype):
     """Tokens of a page that is none of the cache's are left out, drafted ones too."""
     lens, drafts, page = [100, 20], [10, 10], 16
@@ -388,18 +393,19 @@ def test_tree_pages_that_are_none(width, dtype):
 
 
 @pytest.mark.parametrize("width", [4, 200])
+@pytest.mark.parametrize("H,B", [(2, 4), (8, 4), (8, 300), (20, 300)])
 @pytest.mark.parametrize("dtype", [BF16, F32])
-def test_tree_any_numbers_stay_within_the_table(dtype, width):
+def test_tree_any_numbers_stay_within_the_table(dtype, H, B, width):
     """Lengths and drafts of any size; a table of 64 tokens (or whose other pages are none)."""
-    page, B, T = 16, 4, 6
+    page, T, none = 16, 6, [0] * (B - 4)
     table = torch.full((B, width), -1, dtype=torch.int32)
-    table[:, :4] = torch.arange(16).view(4, 4)
+    table[:4, :4] = torch.arange(16).view(4, 4)
     k_cache, v_cache = (cache(16, page, 1, 64, dtype, "shd", 0.5) for _ in range(2))
-    q = normal((B, T, 2, 64), 1, dtype).cuda()
-    out, lse = torch.full_like(q, 7), torch.full((B, T, 2), 7.0, device="cuda")
+    q = normal((B, T, H, 64), 1, dtype).cuda()
+    out, lse = torch.full_like(q, 7), torch.full((B, T, H), 7.0, device="cuda")
     work = torch.empty(sa.sa_attn_tree_workspace(q, k_cache), dtype=torch.uint8, device="cuda")
     seen = torch.full((B, T), -1, dtype=torch.int64, device="cuda")
-    sa.sa_attn_tree(q, k_cache, v_cache, table.cuda(), ints([-5, 2 ** 31 - 1, 62, 2 ** 31 - 3]), seen, out, lse, work, ints([3, 100, 5, -2]))
+    sa.sa_attn_tree(q, k_cache, v_cache, table.cuda(), ints([-5, 2 ** 31 - 1, 62, 2 ** 31 - 3] + none), seen, out, lse, work, ints([3, 100, 5, -2] + none))
     # (a length below zero is none: the draft itself is cached from token 0 on)
     assert (out[0, :3] == 0.5).all() and (out[1] == 0.5).all() and (out[2, :5] == 0.5).all()
     assert (out[0, 3:] == 7).all() and (out[2, 5:] == 7).all() and (out[3] == 7).all() and (lse[3] == 7).all()
@@ -418,30 +424,31 @@ def test_tree_without_pages():
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
-@pytest.mark.parametrize("width", WIDTHS)
+@pytest.mark.parametrize("width", WAYS)
 def test_tree_strided(width, dtype):
     """Everything a part of something larger; nothing beside it changes."""
     lens, drafts, T, H, H_kv, d = [77, 1, 0, 300], [5, 2, 4, 0], 5, 4, 2, 68
     x = Tree(lens, drafts, T, H, H_kv, d, dtype, width=width).compare()
-    wide = torch.full((4, T + 2, H + 3, d + 4), 9, dtype=dtype, device="cuda")
+    B = len(x.lens)
+    wide = torch.full((B, T + 2, H + 3, d + 4), 9, dtype=dtype, device="cuda")
     q_wide = torch.full_like(wide, NAN)
     part = lambda y: y[:, 1:1 + T, 2:2 + H, :d]      # noqa: E731
     part(q_wide).copy_(x.q)
     part(wide).fill_(7)
-    pages = torch.full((4, x.table.shape[1] + 3), 2 ** 30, dtype=torch.int32)
+    pages = torch.full((B, x.table.shape[1] + 3), 2 ** 30, dtype=torch.int32)
     pages[:, 2:-1] = x.table
-    seen = torch.full((4, T + 4), -1, dtype=torch.int64, device="cuda")
+    seen = torch.full((B, T + 4), -1, dtype=torch.int64, device="cuda")
     seen[:, 3:-1] = x.masks.cuda()
-    sums = torch.full((4, T + 1, H + 2), 9.0, device="cuda")
+    sums = torch.full((B, T + 1, H + 2), 9.0, device="cuda")
     sums[:, :T, :H] = 7
-    sa.sa_attn_tree(part(q_wide), x.k_cache, x.v_cache, pages.cuda()[:, 2:-1], ints(lens), seen[:, 3:-1], part(wide), sums[:, :T, :H], x.work, ints(drafts))
+    sa.sa_attn_tree(part(q_wide), x.k_cache, x.v_cache, pages.cuda()[:, 2:-1], ints(x.lens), seen[:, 3:-1], part(wide), sums[:, :T, :H], x.work, ints(x.drafts))
     assert torch.equal(part(wide), x.out) and torch.equal(sums[:, :T, :H], x.lse)
     part(wide).fill_(9)
     sums[:, :T, :H] = 9
     assert (wide == 9).all() and (sums == 9).all()
 
 
-@pytest.mark.parametrize("width", WIDTHS)
+@pytest.mark.parametrize("width", WAYS)
 def test_tree_captured_and_replayed(width):
     """Lengths, drafts and masks are read when the graph is played."""
     page, T = 32, 20
@@ -453,7 +460,7 @@ def test_tree_captured_and_replayed(width):
     with torch.cuda.graph(graph):
         call()
     for i, (a, b) in enumerate([([600, 600, 600], [20, 20, 20]), ([0, 5, 600], [3, 0, 20]), ([33, 590, 1], [20, 1, 9])]):
-        lens.copy_(ints(a)), drafts.copy_(ints(b)), seen.copy_(trees(b, T, 50 + i)[0])
+        lens[:3].copy_(ints(a)), drafts[:3].copy_(ints(b)), seen[:3].copy_(trees(b, T, 50 + i)[0])
         x.out.fill_(7), x.lse.fill_(7)
         call()
         torch.cuda.synchronize()
