@@ -306,7 +306,7 @@ typedef struct {
  * at -inf has no weight, a row that sees no other key is NaN; nothing of a key that a row does not see reaches it.
  * workspace (backward): sa_attn_window_bwd_workspace(shape, window) bytes, 16-byte aligned, of any content; NULL where that is 0.  Calls that may run
  * at the same time (other streams, captured graphs) need one each.
- * Errors: as theirs, and SHAPE for a window below 1, sinks below 0, a workspace that is too small.
+ * Errors: as theirs, and SHAPE for a window below 1, sinks below 0, a workspace that is too small, a max_len above 2^30.
  */
 int sa_attn_window_fwd(const void* q, const void* k, const void* v, const int32_t* offsets, void* out, float* lse,
                        const sa_packed* shape, const sa_window* window, void* stream);

@@ -269,6 +269,8 @@ int check_window(const sa_window* w) {
     if (!w) return SA_ERR_NULL;
     return w->window < 1 || w->sinks < 0 ? SA_ERR_SHAPE : SA_OK;
 }
+// (rows and windows behind them are added in 32 bits)
+bool too_long(const sa_packed* s) { return std::min(s->max_len, s->rows) > 1 << 30; }
 // beyond the longest sequence neither says more
 void set_window(sa::WindowArgs& a, const sa_packed* s, const sa_window* w) {
     a.n_seq = s->n_seq; a.rows = s->rows; a.max_len = std::min(s->max_len, s->rows);
@@ -621,6 +623,7 @@ int sa_attn_window_fwd(const void* q, const void* k, const void* v, const int32_
     if (int e = check_packed(shape)) return e;
     if (int e = check_window(window)) return e;
     if (shape->n_seq == 0 || shape->rows == 0 || shape->max_len == 0) return SA_OK;
+    if (too_long(shape)) return SA_ERR_SHAPE;
     sa::WindowArgs a{};
     if (int e = packed_fwd_args(q, k, v, offsets, out, lse, shape, a)) return e;
     set_window(a, shape, window);
@@ -633,6 +636,7 @@ int sa_attn_window_fwd(const void* q, const void* k, const void* v, const int32_
 int64_t sa_attn_window_bwd_workspace(const sa_packed* shape, const sa_window* window) {
     if (int e = check_packed(shape)) return e;
     if (int e = check_window(window)) return e;
+    if (too_long(shape)) return SA_ERR_SHAPE;
     sa::WindowArgs a{};
     set_window(a, shape, window);
     return sa::far_bytes(a);
@@ -644,6 +648,7 @@ int sa_attn_window_bwd(const void* q, const void* k, const void* v, const void* 
     if (int e = check_packed(shape)) return e;
     if (int e = check_window(window)) return e;
     if (shape->n_seq == 0 || shape->rows == 0 || shape->max_len == 0) return SA_OK;
+    if (too_long(shape)) return SA_ERR_SHAPE;
     sa::WindowArgs a{};
     if (int e = packed_bwd_args(q, k, v, out, dout, lse, offsets, delta, dq, dk, dv, shape, a)) return e;
     const int64_t bytes = sa_attn_window_bwd_workspace(shape, window);

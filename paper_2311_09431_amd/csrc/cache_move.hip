@@ -3,6 +3,8 @@
 // Bound by memory: each byte is read and written once.  Rows are moved in units of 16 bytes where all rows begin at multiples of that, otherwise of 8
 // (a row is a multiple of four elements).  2048 pages of 64 tokens, 8 heads of 128 columns, bf16: 215 us, 5.0 TB/s of reads and writes; a part of 64 pages: 4.4 us,
 // the launch.
+#include <algorithm>
+
 #include "paged.h"
 
 namespace sa {
@@ -123,7 +125,8 @@ hipError_t copy(const CopyArgs& a, int es, hipStream_t st) {
     const Units s = units_of<BYTES>(a, es);
     const bool heads_apart = a.stride_head >= a.page_size * a.stride_slot;
     const int64_t most = (int64_t)a.page_size * a.H_kv * s.row, slices = (most + EACH * THREADS - 1) / (EACH * THREADS);
-    const int64_t most_slices = (1 << 22) / a.n;         // (a launch holds fewer than 2^32 threads; n: up to 2^22)
+    // (a launch holds fewer than 2^32 threads, and fewer than 2^16 workgroups along y; n: up to 2^22)
+    const int64_t most_slices = std::min((1 << 22) / a.n, 65535);
     const unsigned y = (unsigned)(slices < most_slices ? slices : most_slices);
     hipLaunchKernelGGL(cache_copy_kernel<BYTES>, dim3((unsigned)a.n, y, 2), dim3(THREADS), 0, st, a, s, heads_apart);
     return hipGetLastError();

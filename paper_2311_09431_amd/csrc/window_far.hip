@@ -67,6 +67,12 @@ __device__ inline void load_columns(uint32_t (&to)[CW * sizeof(T) / 4], const T*
     }
 }
 
+// A workgroup's slot, key/value head and block of keys, slots first
+struct Place { int slot, kvh, block; };
+__device__ inline Place place_of(const WindowArgs& p, int block0) {
+    const int rest = (int)blockIdx.x / p.n_slots;
+    return {(int)blockIdx.x % p.n_slots, rest % p.H_kv, block0 + rest / p.H_kv};
+}
 // The sequence of a slot and the slot's place among its own (0: the windows' own).  False: none.
 __device__ inline bool find_sequence(const WindowArgs& p, int slot, int& seq, int& place) {
     const int lane = threadIdx.x & 63;
@@ -96,11 +102,12 @@ window_far_kernel(WindowArgs p, int block0) {
     __shared__ __attribute__((aligned(16))) float sums[WAVES][KEYS][PITCH];
 
     int seq, place;
-    if (!find_sequence(p, (int)blockIdx.x, seq, place) || place == 0) return;
+    const Place at_slot = place_of(p, block0);
+    if (!find_sequence(p, at_slot.slot, seq, place) || place == 0) return;
     const Span span = span_of(p, seq);
     const int first = __builtin_amdgcn_readfirstlane(span.first), c = __builtin_amdgcn_readfirstlane(span.len), d = p.d;
     const int a0 = p.window + (place - 1) * p.part, a1 = min(c, a0 + p.part);
-    const int kvh = (int)blockIdx.y, key0 = (block0 + (int)blockIdx.z) * KEYS, group = p.H / p.H_kv;
+    const int kvh = at_slot.kvh, key0 = at_slot.block * KEYS, group = p.H / p.H_kv;
     if (key0 + p.window >= c) return;           // no key of these is seen from further on
     const int lane = threadIdx.x & 63, n = lane & 15, j = lane >> 4, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int key = key0 + n;
@@ -225,7 +232,7 @@ window_far_kernel(WindowArgs p, int block0) {
                 const float4 z = *reinterpret_cast<const float4*>(&sums[w][row][col]);
                 y.x += z.x; y.y += z.y; y.z += z.z; y.w += z.w;
             }
-            *reinterpret_cast<float4*>(slot_row(p, (int)blockIdx.x, kvh, key0 + row) + which * d + col) = make_float4(mul * y.x, mul * y.y, mul * y.z, mul * y.w);
+            *reinterpret_cast<float4*>(slot_row(p, at_slot.slot, kvh, key0 + row) + which * d + col) = make_float4(mul * y.x, mul * y.y, mul * y.z, mul * y.w);
         }
     }
 }
@@ -236,19 +243,20 @@ template <typename T>
 __global__ void __launch_bounds__(64 * WAVES)
 window_join_kernel(WindowArgs p, int block0) {
     int seq, place;
-    if (!find_sequence(p, (int)blockIdx.x, seq, place) || place != 0) return;
+    const Place at_slot = place_of(p, block0);
+    if (!find_sequence(p, at_slot.slot, seq, place) || place != 0) return;
     const Span span = span_of(p, seq);
     const int first = __builtin_amdgcn_readfirstlane(span.first);
     p.c = __builtin_amdgcn_readfirstlane(span.len);
-    const int slots = min(slots_of(p, p.c), p.n_slots - (int)blockIdx.x);
-    const int lane = threadIdx.x & 63, kvh = (int)blockIdx.y, key = __builtin_amdgcn_readfirstlane((block0 + (int)blockIdx.z) * WAVES + ((int)threadIdx.x >> 6));
+    const int slots = min(slots_of(p, p.c), p.n_slots - at_slot.slot);
+    const int lane = threadIdx.x & 63, kvh = at_slot.kvh, key = __builtin_amdgcn_readfirstlane(at_slot.block * WAVES + ((int)threadIdx.x >> 6));
     if (!is_far(p, key)) return;
     float sum[2][ROW_COLS] = {};
     for (int s0 = 0; s0 < slots; s0 += BATCH) {         // (BATCH of them requested at a time)
         float x[BATCH][2][ROW_COLS];
 #pragma unroll
         for (int s = 0; s < BATCH; ++s) {
-            const float* from = slot_row(p, (int)blockIdx.x + min(s0 + s, slots - 1), kvh, key);
+            const float* from = slot_row(p, at_slot.slot + min(s0 + s, slots - 1), kvh, key);
 #pragma unroll
             for (int w = 0; w < 2; ++w)
 #pragma unroll
@@ -295,11 +303,11 @@ window_join_kernel(WindowArgs p, int block0) {
 
 template <typename T>
 hipError_t launch(const WindowArgs& p, hipStream_t st) {
-    // (slots and heads are fewer than 2^24, as the tiles of the other launches are; of keys as many blocks a launch as HIP takes)
-    const int64_t wide = (int64_t)p.n_slots * p.H_kv, most = ((1 << 24) - 1) / wide < 1 ? 1 : ((1 << 24) - 1) / wide < 65535 ? ((1 << 24) - 1) / wide : 65535;
+    // (slots and heads are fewer than 2^24, as the tiles of the other launches are; of keys as many blocks a launch as make no more than that)
+    const int64_t wide = (int64_t)p.n_slots * p.H_kv, fit = ((1 << 24) - 1) / wide, most = fit < 1 ? 1 : fit;
     auto each = [&](int blocks, auto launch) {
         for (int64_t b = 0; b < blocks; b += most) {
-            launch(dim3((unsigned)p.n_slots, (unsigned)p.H_kv, (unsigned)(blocks - b < most ? blocks - b : most)), (int)b);
+            launch(dim3((unsigned)(wide * (blocks - b < most ? blocks - b : most))), (int)b);
             if (hipError_t e = hipGetLastError()) return e;
         }
         return hipSuccess;

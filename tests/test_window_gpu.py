@@ -110,6 +110,16 @@ def test_first_keys_seen_from_far(H, H_kv, lens, window, sinks, d, dtype):
         assert torch.equal(x, y)
 
 
+# so many of them that all walk on
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("H,H_kv,lens,window,sinks", [(8, 8, [1500, 20], 40, 600), (16, 8, [500] * 6, 100, 330)])
+def test_many_first_keys(H, H_kv, lens, window, sinks, d, dtype):
+    r = run(lens, H, H_kv, d, dtype, window, sinks)
+    assert sa.sa_attn_window_bwd_workspace(r[0][0], r[0][1], lengths_to_offsets(lens), max(lens), window, sinks) == 0
+    compare(lens, H, H_kv, d, dtype, window, sinks, *r, heads=[0, H_kv - 1])
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
 def test_infinities_and_first_keys_seen_from_far(dtype):
     """A query and its gradient that are no numbers, far behind a window: they reach dK and dV of the first keys and of its window, no other."""

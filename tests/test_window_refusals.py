@@ -68,6 +68,17 @@ def test_workspace():
             assert bwd(s, w, size=size - 1) == E_SHAPE and bwd(s, w, at=[P] * 11 + [NULL], size=size) == E_NULL
 
 
+def test_longest_sequence():
+    n, w = 2 ** 30 + 1, Window(10, 2 ** 31 - 1)
+    for s in (packed(rows=n, max_len=n, stat_stride_h=n, dtype=1), packed(rows=2 ** 31 - 1, max_len=2 ** 31 - 1, stat_stride_h=2 ** 31, dtype=1)):
+        assert fwd(s, w) == E_SHAPE and bwd(s, w) == E_SHAPE and bytes_of(s, w) == E_SHAPE
+    for h, kv in ((1, 1), (64, 1), (65535, 65535)):
+        for n_seq in (1, 2 ** 20):
+            s = packed(rows=2 ** 30, max_len=2 ** 30, stat_stride_h=2 ** 30, dtype=1, H=h, H_kv=kv, n_seq=n_seq, stride_s=h * 64, kv_stride_s=kv * 64)
+            for window in (Window(1, 1), Window(1, 2 ** 30), Window(2 ** 29, 5)):
+                assert bytes_of(s, window) >= 0
+
+
 @pytest.mark.parametrize("kw", [dict(n_seq=0), dict(rows=0), dict(max_len=0)])
 def test_nothing_to_do(kw):
     s = packed(**kw)
