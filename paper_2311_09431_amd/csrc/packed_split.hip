@@ -1,6 +1,6 @@
 // Causal attention of packed sequences and its gradient, bf16, launches of few tiles: the ring step's workgroups of 32 rows
-// (split_tiles.h), each on one tile of one sequence (packed.h).  Bound by the length of a walk, which several wavefronts share.  The forward with a
-// window too (window.h).
+// (split_tiles.h), each on one tile of one sequence (packed.h).  Bound by the length of a walk, which several wavefronts share.  Those
+// with a window too (window.h).
 #include "split_tiles.h"
 
 namespace sa {
@@ -57,6 +57,13 @@ bool packed_split_wanted(const PackedArgs& p, bool backward) {
     return tiles <= (walk >= 12000 ? 184 : walk >= 2000 ? 152 : 96);
 }
 
+// offsets and threads fit their bits, as packed_split_wanted has it
+static bool in_reach(const WindowArgs& p) {
+    const int64_t widest = p.stride_s > p.kv_stride_s ? p.stride_s : p.kv_stride_s;
+    return p.d <= TD && ((int64_t)(p.max_len + 127) / 128 * 128 + OWN) * 2 * widest + 2 * p.d < (int64_t(1) << 31) &&
+           most_tiles(p, OWN) * (p.H + p.H_kv) * 64 * 4 < (int64_t(1) << 32);
+}
+
 // With a window, forward: four wavefronts a workgroup, or two, for walks that are no longer than the window.  Wavefronts of a workgroup (0: the
 // 128-row kernels), by 128-row tiles of all heads and by keys a walk goes over.  A small launch is latency, that of code read for the first time too:
 // 14 KB here, of which a tile passes all, 61 KB there.  us, 128-row : two wavefronts : four (: eight), first tokens 4.
@@ -66,11 +73,8 @@ bool packed_split_wanted(const PackedArgs& p, bool backward) {
 // d 64: 5 of 200, 16 heads, 64 (208) 11.8 : 8.6 : 8.7 : 17.2; 4 of 1000, 16 heads, 512 (576) 20.8 : 20.1 : 24.5; 8 of 1000, 16 heads, 200 (1136)
 // 34.4 : 28.3 : 41.5, but 32 of 256, 32 heads, 64 (over 3000) 37.8 : 42.0 : 65.0.
 int window_split_waves(const WindowArgs& p) {
-    // (as above)
-    const int64_t widest = p.stride_s > p.kv_stride_s ? p.stride_s : p.kv_stride_s;
-    if (p.d > TD || ((int64_t)(p.max_len + 127) / 128 * 128 + OWN) * 2 * widest + 2 * p.d >= (int64_t(1) << 31)) return 0;
+    if (!in_reach(p)) return 0;
     const int64_t tiles = most_tiles(p, 128) * p.H, reach = (int64_t)p.window + OWN + p.sinks, walk = p.max_len < reach ? p.max_len : reach;
-    if (most_tiles(p, OWN) * p.H * 64 * 4 >= (int64_t(1) << 32)) return 0;
     if (tiles <= 144) return 4;
     if (p.max_len <= OWN) return 2;
     return (p.d <= 64 ? tiles <= 1600 && tiles * walk <= 320000 : tiles * walk <= 160000) ? 2 : 0;
@@ -81,6 +85,48 @@ static hipError_t run_window(const WindowArgs& p, int waves, hipStream_t st) {
     if (waves == 2) hipLaunchKernelGGL((fwd_split_kernel<DP, PART, false, false, WindowArgs, 2>), grid, block, 0, st, p, 0);
     else hipLaunchKernelGGL((fwd_split_kernel<DP, PART, false, false, WindowArgs, 4>), grid, block, 0, st, p, 0);
     return hipGetLastError();
+}
+// The gradient, by four wavefronts, where there are few tiles of all key/value heads.  us, 128-row : these, whole call, first tokens 4.  d 128: 300 rows, 8 heads,
+// window 64 (24 tiles) 41 : 15; 8192, one head, 4096 (65) 225 : 90; 2 of 2000, 16 heads on 2, 500 (66) 278 : 177; 4 of 2000, 64 on 1, 500 (66) 2106 : 1290; 1000, 16
+// on 8, 200 (64) 83 : 54; 2000, 8 heads, 500 (128) 78 : 63; but 4 of 1000, 32 on 4, 128 (140) 200 : 222; 2500, 8 heads, 128 (160) 60 : 66; 4096, 8
+// heads, 1024 (264) 101 : 132.  d 64: 1000, 16 on 8, 200 (64) 65 : 36; 8 of 500, 16 on 2, 64 (78) 82 : 39; 4 of 1000, 6 heads, 128 (210) 53 : 30; 12 of 200,
+// 8 heads, 64 (240) 26.6 : 25.0; but 4 of 1000, 16 on 8, 256 (280) 69 : 74; 4000, 16 heads, 64 (512) 73 : 80.
+template <int DP, bool PART>
+__global__ void __launch_bounds__(64 * BWD_WAVES, DP <= 64 ? 2 : 1)
+window_bwd_split_kernel(WindowArgs p, int n_dkdv) {
+    __shared__ __attribute__((aligned(1024))) char lds[BWD_WAVES * 2 * STAGE_BYTES<DP> + 2 * SUB_BYTES<DP>];
+    __shared__ __attribute__((aligned(1024))) char stats[BWD_WAVES * 2 * STAT_BYTES];
+    __shared__ uint32_t masks[BWD_WAVES];
+    int n_tiles, rank, head, seq;
+    if ((int)blockIdx.x < n_dkdv) {
+        if (!enter_sequence<false, OWN>(p, (int)blockIdx.x, p.H_kv, n_tiles, rank, head, &seq)) return;
+        p.slot = find_slot(p, seq, rank * OWN);
+        bwd_dkdv<DP, PART, false, true, WindowArgs>(p, n_tiles, rank * p.H_kv + head, lds, stats, masks);
+    } else {
+        if (!enter_sequence<true, OWN>(p, (int)blockIdx.x - n_dkdv, p.H, n_tiles, rank, head)) return;
+        bwd_dq<DP, PART, false, true, WindowArgs>(p, n_tiles, rank * p.H + head, lds, stats, masks);
+    }
+}
+template <int DP, bool PART>
+static hipError_t run_window_bwd(const WindowArgs& p, hipStream_t st) {
+    const unsigned n_dkdv = (unsigned)p.n_ranks * p.H_kv, n_dq = (unsigned)p.n_ranks * p.H;
+    hipLaunchKernelGGL((window_bwd_split_kernel<DP, PART>), dim3(n_dkdv + n_dq), dim3(64 * BWD_WAVES), 0, st, p, (int)n_dkdv);
+    return hipGetLastError();
+}
+bool window_bwd_split_wanted(const WindowArgs& p) {
+    return in_reach(p) && most_tiles(p, 128) * p.H_kv <= (p.d <= 64 ? 240 : 128);
+}
+hipError_t launch_window_bwd_split(WindowArgs p, hipStream_t st) {
+    if (hipError_t e = launch_packed_delta(p, SA_BF16, st)) return e;
+    p.n_ranks = (int)most_tiles(p, OWN);
+    p.by_rank = true;
+    const bool part = p.d % 8 != 0;
+    hipError_t e;
+    if (p.d <= 32 && !part) e = run_window_bwd<32, false>(p, st);
+    else if (p.d <= 64) e = part ? run_window_bwd<64, true>(p, st) : run_window_bwd<64, false>(p, st);
+    else if (p.d <= 112) e = part ? run_window_bwd<112, true>(p, st) : run_window_bwd<112, false>(p, st);
+    else e = part ? run_window_bwd<128, true>(p, st) : run_window_bwd<128, false>(p, st);
+    return e != hipSuccess ? e : launch_window_far(p, SA_BF16, st);
 }
 hipError_t launch_window_split(WindowArgs p, int waves, hipStream_t st) {
     p.n_ranks = (int)most_tiles(p, OWN);

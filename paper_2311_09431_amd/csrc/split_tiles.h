@@ -416,8 +416,9 @@ __device__ inline bf16x8 negated(bf16x8 x) {
 
 // dQ: a workgroup owns queries
 // PACKED: linear is the tile's place and the head in a sequence that p is the arguments of; rows are written in bf16
-template <int DP, bool PART, bool EXACT, bool PACKED = false>
-__device__ inline void bwd_dq(const StepArgs& p, int n_tiles, int linear, char* lds, char* stats, uint32_t* masks) {
+template <int DP, bool PART, bool EXACT, bool PACKED = false, typename Args = StepArgs>
+__device__ inline void bwd_dq(const Args& p, int n_tiles, int linear, char* lds, char* stats, uint32_t* masks) {
+    constexpr bool WINDOW = std::is_same<Args, WindowArgs>::value;
     constexpr int KS = ksteps_of(DP), MB = blocks_of(DP), WAVES = BWD_WAVES, LOADS = 2 * PIECES<DP>, TERMS = EXACT ? 3 : 1;
     constexpr int LATE = KS > 2 ? KS - 2 : KS / 2, NEXT = MB > 1 ? 1 : 0;          // (32 columns: two k-steps, one block)
     const Lane<DP> ln;
@@ -451,8 +452,15 @@ __device__ inline void bwd_dq(const StepArgs& p, int n_tiles, int linear, char* 
     const int beyond = 32 * at.n_full;
     struct Tile { int key0, shift; };               // key0 == beyond: none
     // the walk's next sub-tile; K, V: of its block
+    WindowWalk<OWN> walk;
+    if constexpr (WINDOW) walk = WindowWalk<OWN>(p, q0, min(q0 + OWN - 1, p.c - 1) / OWN + 1);
     auto take = [&](Tile& t) {
-        at.settle<WAVES>();
+        if constexpr (WINDOW) {         // (at.v: the sub-tile's place in the walk)
+            t = {at.v < walk.n ? 32 * walk.at(at.v) : beyond, 0};
+            at.v += WAVES;
+            return;
+        }
+        at.template settle<WAVES>();
         t.key0 = at.kv < at.kv_end ? 32 * at.v : beyond;
         t.shift = at.shift;
         at.v += WAVES;
@@ -463,7 +471,8 @@ __device__ inline void bwd_dq(const StepArgs& p, int n_tiles, int linear, char* 
         }
     };
     Tile t0, t1 = {beyond, 0}, t2;
-    at.enter<WAVES>();
+    if constexpr (WINDOW) at.v = ln.wave;
+    else at.template enter<WAVES>();
 #pragma unroll 1
     for (int i = 0; i < 2; ++i) {
         t0 = t1;
@@ -521,10 +530,16 @@ __device__ inline void bwd_dq(const StepArgs& p, int n_tiles, int linear, char* 
         }
         asm volatile("" : "+v"(pr));            // there, beside the products
         __builtin_amdgcn_sched_barrier(0);
-        if (t0.key0 + 31 > min(p.c - 1, q0 + t0.shift)) {          // some pair of the sub-tile is masked
+        bool masked = t0.key0 + 31 > min(p.c - 1, q0 + t0.shift);          // some pair of the sub-tile is
+        if constexpr (WINDOW) masked |= t0.key0 <= q0 + 31 - p.window;
+        if (masked) {
             const int lane_last = min(p.c - 1, a_own + t0.shift) - t0.key0;
 #pragma unroll
             for (int r = 0; r < 16; ++r) pr[r] = reg_row(r, h) <= lane_last ? pr[r] : 0.f;
+            if constexpr (WINDOW) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) pr[r] = in_window(p, t0.key0 + reg_row(r, h), a_own) ? pr[r] : 0.f;
+            }
         }
         if (EXACT) look_at(z, s);
         mfma_results_to_valu(dp);
@@ -564,8 +579,12 @@ __device__ inline void bwd_dq(const StepArgs& p, int n_tiles, int linear, char* 
     if constexpr (PACKED) {
         __syncthreads();
         put_partial<DP>(lds, acc, ln);
+        if constexpr (WINDOW) put_odd(masks, a_own < p.c && window_odd<MB, PART>(acc, h, d), ln.wave, ln.lane);
         __syncthreads();
-        if (a_own < p.c) set_rows<DP, WAVES>((__bf16*)p.dq + base + (int64_t)a * p.stride_s, lds, p.scale, d, ln);
+        const uint32_t odd_rows = WINDOW ? take_odd<WAVES>(masks) : 0;
+        if (a_own < p.c && !((odd_rows >> n) & 1)) set_rows<DP, WAVES>((__bf16*)p.dq + base + (int64_t)a * p.stride_s, lds, p.scale, d, ln);
+        if constexpr (WINDOW)
+            each_row<WAVES>(odd_rows, ln.wave, [&](const StepArgs&, int i) { window_dq_row<__hip_bfloat16>(p, hd, q0 + i, ln.lane); });
         return;
     }
     float* const DQ = p.dq + base + (int64_t)a * p.stride_s;
@@ -585,8 +604,9 @@ __device__ inline void bwd_dq(const StepArgs& p, int n_tiles, int linear, char* 
 // that share the key/value head and the query shards that see it come one after the other.  The owned V is
 // negated, so that delta - dP comes out of the product that starts from delta; dK changes its sign
 // at the end.
-template <int DP, bool PART, bool EXACT, bool PACKED = false>
-__device__ inline void bwd_dkdv(const StepArgs& p, int n_tiles, int linear, char* lds, char* stats, uint32_t* masks) {
+template <int DP, bool PART, bool EXACT, bool PACKED = false, typename Args = StepArgs>
+__device__ inline void bwd_dkdv(const Args& p, int n_tiles, int linear, char* lds, char* stats, uint32_t* masks) {
+    constexpr bool WINDOW = std::is_same<Args, WindowArgs>::value;
     constexpr int KS = ksteps_of(DP), MB = blocks_of(DP), WAVES = BWD_WAVES, LOADS = 2 * PIECES<DP> + 2, TERMS = EXACT ? 3 : 1;
     constexpr int LATE = KS > 2 ? KS - 2 : KS / 2, NEXT = MB > 1 ? 1 : 0;          // as in bwd_dq
     const Lane<DP> ln;
@@ -613,7 +633,13 @@ __device__ inline void bwd_dkdv(const StepArgs& p, int n_tiles, int linear, char
     char* const tiles = lds + wave * 2 * STAGE_BYTES<DP>;
     char* const tile_stats = stats + wave * 2 * STAT_BYTES;
     const int q_dev0 = p.layout == SA_STRIPED ? p.q_dev : max(p.q_dev, dev), q_end = p.q_dev + p.n_q;
-    const int n_sub = (p.c + 31) / 32;
+    int n_sub = (p.c + 31) / 32, lane_end = p.c, full_to = p.c;            // one past the last query that sees the lane's key; all keys
+    const int beyond = 32 * n_sub;             // behind the walk's end, as above
+    if constexpr (WINDOW) {
+        n_sub = (walk_end(p, k0, k0 + OWN - 1) + 31) / 32;
+        lane_end = walk_end(p, key_own);
+        full_to = min(p.c, k0 + p.window);
+    }
     int member = q_dev0 < q_end ? 0 : group, q_dev = q_dev0, v = 0, turn = 0;
     int shift = 0;              // key b is seen by the block's queries from b + shift on
     dt_rsrc Q, G, S, E;
@@ -635,7 +661,6 @@ __device__ inline void bwd_dkdv(const StepArgs& p, int n_tiles, int linear, char
         S = dt_make_rsrc(p.lse + sbase, p.c, 4, 2);
         E = dt_make_rsrc(p.delta + sbase, p.c, 4, 2);
     };
-    const int beyond = 32 * n_sub;             // behind the walk's end, as above
     struct Tile { int a0, shift; };            // a0 == beyond: none
     // the walk's next sub-tile; Q, G, S, E: of its block
     auto take = [&](Tile& t) {
@@ -742,8 +767,8 @@ __device__ inline void bwd_dkdv(const StepArgs& p, int n_tiles, int linear, char
         }
         asm volatile("" : "+v"(pr));            // there, beside the products
         __builtin_amdgcn_sched_barrier(0);
-        if (t0.a0 < k0 + OWN - 1 + t0.shift || t0.a0 + 32 > p.c) {       // some pair of the sub-tile is masked
-            const int lane_first = key_own + t0.shift - t0.a0, rows = p.c - t0.a0;
+        if (t0.a0 < k0 + OWN - 1 + t0.shift || t0.a0 + 32 > full_to) {       // some pair of the sub-tile is masked
+            const int lane_first = key_own + t0.shift - t0.a0, rows = lane_end - t0.a0;
 #pragma unroll
             for (int r = 0; r < 16; ++r) pr[r] = reg_row(r, h) >= lane_first && reg_row(r, h) < rows ? pr[r] : 0.f;
         }
@@ -796,8 +821,25 @@ __device__ inline void bwd_dkdv(const StepArgs& p, int n_tiles, int linear, char
         __syncthreads();
         put_partial<DP>(lds, accv, ln);
         put_partial<DP>(lds + HALF, acck, ln);
+        bool ends = key_own < p.c;              // the key's sums end here
+        if constexpr (WINDOW) {
+            ends = ends && !is_far(p, key_own);
+            put_odd(masks, ends && (window_odd<MB, PART>(accv, h, d) || window_odd<MB, PART>(acck, h, d)), wave, ln.lane);
+        }
         __syncthreads();
-        if (key_own < p.c) {
+        const uint32_t odd_rows = WINDOW ? take_odd<WAVES>(masks) : 0;
+        if constexpr (WINDOW) {
+            if (p.slot >= 0 && key_own < p.c && !ends) {
+                float4 none[share_of(DP, WAVES)] = {};
+                float* const to = slot_row(p, p.slot, kvh, key_own);
+                add_rows<DP, WAVES>(to, none, lds, 1.f, d, ln);
+#pragma unroll
+                for (int i = 0; i < share_of(DP, WAVES); ++i) none[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+                add_rows<DP, WAVES>(to + d, none, lds + HALF, -p.scale, d, ln);
+            }
+            each_row<WAVES>(odd_rows, wave, [&](const StepArgs&, int i) { window_dkdv_row<__hip_bfloat16>(p, kvh, k0 + i, 0, d, ln.lane); });
+        }
+        if (ends && !((odd_rows >> n) & 1)) {
             set_rows<DP, WAVES>((__bf16*)p.dv + row, lds, 1.f, d, ln);
             set_rows<DP, WAVES>((__bf16*)p.dk + row, lds + HALF, -p.scale, d, ln);
         }

@@ -47,8 +47,10 @@ inline void set_far(WindowArgs& p) {
 inline int64_t far_bytes(const WindowArgs& p) { return (int64_t)p.n_slots * p.H_kv * p.key_rows * 2 * p.d * 4; }
 hipError_t launch_window_far(const WindowArgs& p, int dtype, hipStream_t st);
 hipError_t launch_window_fwd(WindowArgs p, hipStream_t st);
-int window_split_waves(const WindowArgs& p);                                           // 32-row workgroups (packed_split.hip)
+int window_split_waves(const WindowArgs& p);                                           // workgroups of 32 rows (packed_split.hip); 0: not wanted
 hipError_t launch_window_split(WindowArgs p, int waves, hipStream_t st);
+bool window_bwd_split_wanted(const WindowArgs& p);
+hipError_t launch_window_bwd_split(WindowArgs p, hipStream_t st);
 hipError_t launch_window_bwd(WindowArgs p, hipStream_t st);
 hipError_t launch_window_f32(WindowArgs p, bool backward, hipStream_t st);
 hipError_t launch_window_f32x3(WindowArgs p, bool backward, hipStream_t st);           // up to 128 columns

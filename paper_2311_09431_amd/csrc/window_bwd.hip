@@ -50,6 +50,7 @@ hipError_t launch(WindowArgs p, hipStream_t st) {
 }  // namespace
 
 hipError_t launch_window_bwd(WindowArgs p, hipStream_t st) {
+    if (window_bwd_split_wanted(p)) return launch_window_bwd_split(p, st);
     const bool part = p.d % 8 != 0;
     if (p.d > 128) return part ? launch<256, true>(p, st) : launch<256, false>(p, st);
     if (p.d <= 32 && !part) return launch<32, false>(p, st);
