@@ -4,15 +4,29 @@ import random
 import pytest
 import torch
 
+import sequences
 from paper_2311_09431_amd import binding as sa
 from seen import Seen, window_mask
-from sequences import check, lengths_to_offsets, normal
+from sequences import check, normal
 
 pytestmark = pytest.mark.gpu
 
 BF16, F32 = torch.bfloat16, torch.float32
 ROUNDED = {BF16: 2.0 ** -8, F32: 0.0}           # how far a weight is rounded before it meets V
 NAN, INF = float("nan"), float("inf")
+EMPTY = [0]
+
+
+@pytest.fixture(autouse=True, params=[0, 300])
+def empty_ones(request):
+    """How many sequences without a row follow those of a test: with many a launch has as many tiles as the large ones."""
+    EMPTY[0] = request.param
+    yield
+    EMPTY[0] = 0
+
+
+def lengths_to_offsets(lens, first=0):
+    return sequences.lengths_to_offsets(list(lens) + [0] * EMPTY[0], first)
 
 
 def rows(shape, seed, dtype, order="shd"):
@@ -196,7 +210,7 @@ def test_any_offsets_stay_within_the_tensors(offsets, window, sinks, dtype):
     T = 256
     q, k, v, g = (rows((T, 2, 64), s, dtype) for s in (1, 2, 3, 4))
     out, lse = torch.full_like(q, 7), torch.full((2, T), 7.0, device="cuda")
-    off = torch.tensor(offsets, dtype=torch.int32, device="cuda")
+    off = torch.tensor(offsets + offsets[-1:] * EMPTY[0], dtype=torch.int32, device="cuda")
     sa.sa_attn_window_fwd(q, k, v, off, out, lse, 256, window, sinks)
     grads = [torch.full_like(x, 7) for x in (q, k, v)]
     backward((q, k, v, g), out, lse, off, grads, 256, window, sinks)
