@@ -22,11 +22,12 @@ struct WindowArgs : PackedArgs {
 // Whether there are such workgroups: two launches more, against the time of a walk, rows of all heads of a group.  (Gradient in
 // us, walking on / with them.  bf16: 1 x 1100 rows, 4 heads, 64 columns, window 64: 55.5 / 43.0; 4 x 1100, 8 heads, 128 columns, window 256: 80.5 /
 // 77.0; 1 x 600: 41.4 / 42.4; 8 x 300, 16 heads, 100 columns: 55.2 / 77.5.  fp32, the same four: 114 / 63, 221 / 193, 69.6 / 40.7, 137 / 157.)
-// The rows of a part (fewer parts where there are many first keys, whose blocks of 16 are workgroups too) and the slots that sequences
-// without a common row can have; 0: key-owning workgroups walk on.
+// The rows of a part, as many as make about 1024 workgroups of all (key/value heads and blocks of 16 first keys are workgroups too) but two tiles a
+// wavefront, one with groups of four heads or more (3449 rows, 16 heads on 2, window 18, 130 first keys, gradient: 183 us, of 256 a block 878; 7921, 4 on 1, 44, 130: 148,
+// 447), and the slots that sequences without a common row can have; 0: key-owning workgroups walk on.
 //
 // Many first keys fill the chip by themselves while all walk on, where blocks of 16 have work in proportion: key/value heads times blocks times all
-// rows, against the longest walk's.  (1 x 16384, 8 heads, 128 columns, window 1024, first keys 64, 256, 512, 2048, walking on / with them: 741 / 394, 750 / 613,
+// rows, against the longest walk's.  (With parts of 256 rows a block, fp32 128: 1 x 16384, 8 heads, 128 columns, window 1024, first keys 64, 256, 512, 2048, walking on / with them: 741 / 394, 750 / 613,
 // 762 / 1169, 892 / 2449, fp32 3065 / 1677, 3139 / 2334, 3090 / 3218, 3677 / 11938; 4 of up to 4000, 32 heads on 8, 500, first keys 64, 256: 792 / 615,
 // 794 / 1455; 1 x 8000, 8 heads on 2, 64 columns, 500, 1024, 3000: 928 / 530, 1005 / 1271.)
 inline bool has_far(const WindowArgs& p) {
@@ -38,8 +39,10 @@ inline void set_far(WindowArgs& p) {
     p.key_rows = (int)(((int64_t)p.sinks + 15) / 16 * 16);
     p.n_slots = 0;
     if (!has_far(p)) return;
-    p.part = (p.es == 2 ? 256 : 128) * (p.key_rows / 16 < 64 ? p.key_rows / 16 : 64);
     const int64_t all = (int64_t)p.n_seq * p.max_len, rows = all < p.rows ? all : p.rows;
+    const int least = (p.es == 2 ? 128 : 64) * (p.H / p.H_kv < 4 ? 2 : 1);
+    const int64_t each = rows * p.H_kv * (p.key_rows / 16) / 1024;
+    p.part = (int)((each / least + 1) * least);
     const int64_t longer = rows / (p.window + 1) < p.n_seq ? rows / (p.window + 1) : p.n_seq;      // sequences that are longer than the window
     const int64_t slots = 2 * longer + rows / p.part;
     p.n_slots = slots < (1 << 24) ? (int)slots : 0;         // (more: more than a launch takes)

@@ -46,12 +46,14 @@ hipError_t run(WindowArgs p, bool backward, hipStream_t st) {
 // 242, 728; of 200, one head, 22, 37 : 18, 39 : 27, 49; but of 1000, 16 heads, 128 (144) 59, 160 : 43, 158 : 40, 91; of 4000, 8 heads, 1000 (264)
 // 303, 754 : 172, 532 : 139, 378; 5 of up to 777, 16 heads on 8, 100 (d 100) 85, 209 : 71, 191 : 42, 141.  d 64: 2 of up to 1000, 2 heads, 300 (32)
 // 37, 60 : 12, 34 : 39, 59; 2000, 4 heads, 200 (68) 30, 86 : 13, 48 : 33, 55; but 5 of up to 777, 16 heads on 8, 100, 82, 193 : 37, 93 : 27, 75.
+// (Of the gradient those of all key/value heads, 128 : 32 rows: 2 of 625, 16 heads on 2, 100 (22 tiles) 393 : 170; 5 of 454, 8 on 1, d 96, window 2 (22) 262 : 132; 2 of
+// 2000, 16 on 2, 500 (66) 900 : 602; 1000, 64 on 8, 100 (64) 415 : 384; d 64, 2 of 1000, 32 on 4, 100 (68) 184 : 140; d 32, 4 of 777, 8 on 2, 100 (56) 109 : 61.)
 static bool few_tiles(const WindowArgs& p, bool backward) {
     StepArgs longest = p;
     longest.c = p.max_len;
     longest.B = 1;
     const bool fits = most_tiles(p, 32) * p.H * 64 * 8 * 2 < (int64_t(1) << 32);
-    return most_tiles(p, 128) * p.H <= 96 && fits && f32x3_split_supported(longest, backward);
+    return most_tiles(p, 128) * (backward ? p.H_kv : p.H) <= 96 && fits && f32x3_split_supported(longest, backward);
 }
 
 hipError_t launch_window_f32(WindowArgs p, bool backward, hipStream_t st) {
