@@ -48,12 +48,17 @@ hipError_t run(WindowArgs p, bool backward, hipStream_t st) {
 // 37, 60 : 12, 34 : 39, 59; 2000, 4 heads, 200 (68) 30, 86 : 13, 48 : 33, 55; but 5 of up to 777, 16 heads on 8, 100, 82, 193 : 37, 93 : 27, 75.
 // (Of the gradient those of all key/value heads, 128 : 32 rows: 2 of 625, 16 heads on 2, 100 (22 tiles) 393 : 170; 5 of 454, 8 on 1, d 96, window 2 (22) 262 : 132; 2 of
 // 2000, 16 on 2, 500 (66) 900 : 602; 1000, 64 on 8, 100 (64) 415 : 384; d 64, 2 of 1000, 32 on 4, 100 (68) 184 : 140; d 32, 4 of 777, 8 on 2, 100 (56) 109 : 61.)
+// (Forward, longer walks, 128 : 32 rows: d 32, 2 of up to 2768 rows, 4 heads, 2395, 182 : 38; 3000, 16 heads, 1000 (400) 156 : 73; 4000, 8 heads, 300 (264) 39 : 32; d 64, 3000, 16
+// heads, 1000 159 : 119; 4 of up to 2000, 8 heads, 800, 72 : 41; but 8000, 4 heads, 500 (252) 55 : 60.)
 static bool few_tiles(const WindowArgs& p, bool backward) {
     StepArgs longest = p;
     longest.c = p.max_len;
     longest.B = 1;
     const bool fits = most_tiles(p, 32) * p.H * 64 * 8 * 2 < (int64_t(1) << 32);
-    return most_tiles(p, 128) * (backward ? p.H_kv : p.H) <= 96 && fits && f32x3_split_supported(longest, backward);
+    if (!fits || !f32x3_split_supported(longest, backward)) return false;
+    const int64_t tiles = most_tiles(p, 128), reach = (int64_t)p.window + 32 + p.sinks, walk = p.max_len < reach ? p.max_len : reach;
+    if (!backward && p.d <= 64 && tiles * p.H <= 512 && walk >= (p.d <= 32 ? 300 : 800)) return true;
+    return tiles * (backward ? p.H_kv : p.H) <= 96;
 }
 
 hipError_t launch_window_f32(WindowArgs p, bool backward, hipStream_t st) {
