@@ -136,8 +136,20 @@ hipError_t accept(const AcceptArgs& a, int es, hipStream_t st) {
     const Units s = units_of<BYTES>(a, es);
     const int64_t all = 2ll * a.H_kv * s.row;
     const unsigned threads = all >= 1024 ? 1024 : (unsigned)((all + 63) / 64 * 64);
-    hipLaunchKernelGGL(cache_accept_kernel<BYTES>, dim3((unsigned)a.B), dim3(threads), 0, st, a, s);
-    return hipGetLastError();
+    // (a launch holds fewer than 2^32 threads: of 2^22 sequences of 1024 the last one goes in a launch of its own)
+    const int most = (int)(((int64_t(1) << 32) - 1) / threads);
+    for (int64_t first = 0; first < a.B; first += most) {
+        AcceptArgs p = a;
+        p.B = (int)std::min<int64_t>(a.B - first, most);
+        if (a.table) p.table = a.table + first * a.table_stride;
+        p.lens = a.lens + first;
+        p.chosen = a.chosen + first * a.chosen_stride;
+        p.accepted = a.accepted + first;
+        if (a.lens_after) p.lens_after = a.lens_after + first;
+        hipLaunchKernelGGL(cache_accept_kernel<BYTES>, dim3((unsigned)p.B), dim3(threads), 0, st, p, s);
+        if (hipError_t e = hipGetLastError()) return e;
+    }
+    return hipSuccess;
 }
 
 }  // namespace
