@@ -306,7 +306,8 @@ def sa_ring_bwd_tiled(Q, K, V, dO, O, LSE, delta, dQ, dK, dV, N, layout, shape, 
 
 
 # ---- packed sequences and the paged cache: no shape structure, sizes and strides are the tensors'.  Tensors lie on the current
-# device (ValueError otherwise: the call goes to that device's stream).
+# device (ValueError otherwise: the call goes to that device's stream).  max_len, window and sinks beyond 32 bits are as the nearest
+# number that these hold.
 
 
 def sa_attn_packed_fwd(q, k, v, offsets, out, lse, max_len, scale=None):

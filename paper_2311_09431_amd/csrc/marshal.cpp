@@ -7,6 +7,7 @@
 // a function that gives the stream's handle.
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <algorithm>
 #include <cstdint>
 
 #include "striped_attn.h"
@@ -39,6 +40,17 @@ uint64_t integer(PyObject* o) {
     return v;
 }
 int32_t int32(PyObject* o) { return (int32_t)(uint32_t)integer(o); }
+// A length that bounds others, for which the largest number that 32 bits hold says as much as any beyond it: the nearest one (of a window of 2^32 + 5
+// the bits dropped would leave one of 5).
+int32_t bound(PyObject* o) {
+    PyObject* const whole = PyIndex_Check(o) ? PyNumber_Index(o) : PyObject_CallOneArg(other_integer, o);
+    if (!whole) throw ToStop();
+    int beyond = 0;
+    const long long v = PyLong_AsLongLongAndOverflow(whole, &beyond);
+    Py_DECREF(whole);
+    if (beyond) return beyond > 0 ? INT32_MAX : INT32_MIN;
+    return (int32_t)std::min<long long>(std::max<long long>(v, INT32_MIN), INT32_MAX);
+}
 // asked when the tensors have been looked at
 void* stream(PyObject* ask) {
     PyObject* o = PyObject_CallNoArgs(ask);
@@ -281,7 +293,7 @@ sa_packed packed_of(const at::Tensor& q, const at::Tensor& k, const at::Tensor& 
         refuse(PyExc_ValueError, "q and k must have the same rows, head dimension and type");
     if (offsets.dim() != 1 || offsets.size(0) < 1) refuse(PyExc_ValueError, "offsets must hold one more number than there are sequences");
     statistics(lse, q.size(1), q.size(0), "lse must be float32 [heads, rows], rows contiguous");
-    return {size(offsets, 0) - 1, size(q, 0), int32(max_len), size(q, 1), size(k, 1), size(q, 2), qs.h, qs.s, ks.h, ks.s,
+    return {size(offsets, 0) - 1, size(q, 0), bound(max_len), size(q, 1), size(k, 1), size(q, 2), qs.h, qs.s, ks.h, ks.s,
             q.size(1) == 1 ? q.size(0) : lse.stride(0), type_of(q), real(scale)};
 }
 const char* const OFFSETS = "offsets must be a contiguous int32 tensor";
@@ -322,7 +334,7 @@ ENTRY(window_fwd) {
         const Call on(a[11]);
         const at::Tensor &q = on(a[1]), &k = on(a[2]), &v = on(a[3]), &off = on.ids(a[4], OFFSETS), &out = on(a[5]), &lse = on(a[6]);
         const sa_packed s = packed_of(q, k, v, off, lse, a[7], a[10]);
-        const sa_window w = {int32(a[8]), int32(a[9])};
+        const sa_window w = {bound(a[8]), bound(a[9])};
         same(out, q, "out must have q's shape, type and strides");
         void* st = stream(a[12]);
         return run([&] { return f(at_of(q), at_of(k), at_of(v), (const int32_t*)at_of(off), at_of(out), (float*)at_of(lse), &s, &w, st); });
@@ -335,8 +347,8 @@ ENTRY(window_bwd_workspace) {
         const at::Tensor &q = tensor(a[1]), &k = tensor(a[2]), &off = tensor(a[3]);
         const Strides qs = strides(q), ks = strides(k);
         if (off.dim() != 1 || off.size(0) < 1) refuse(PyExc_ValueError, "offsets must hold one more number than there are sequences");
-        const sa_packed s = {size(off, 0) - 1, size(q, 0), int32(a[4]), size(q, 1), size(k, 1), size(q, 2), qs.h, qs.s, ks.h, ks.s, q.size(0), type_of(q), 0.f};
-        const sa_window w = {int32(a[5]), int32(a[6])};
+        const sa_packed s = {size(off, 0) - 1, size(q, 0), bound(a[4]), size(q, 1), size(k, 1), size(q, 2), qs.h, qs.s, ks.h, ks.s, q.size(0), type_of(q), 0.f};
+        const sa_window w = {bound(a[5]), bound(a[6])};
         return PyLong_FromLongLong(f(&s, &w));
     });
 }
@@ -349,7 +361,7 @@ ENTRY(window_bwd) {
                          &delta = on(a[8]), &dq = on(a[9]), &dk = on(a[10]), &dv = on(a[11]);
         const at::Tensor* work = maybe(on, a[12]);
         const sa_packed s = packed_of(q, k, v, off, lse, a[13], a[16]);
-        const sa_window w = {int32(a[14]), int32(a[15])};
+        const sa_window w = {bound(a[14]), bound(a[15])};
         for (const at::Tensor* t : {&out, &dout, &dq}) same(*t, q, "out, dout and dq must have q's shape, type and strides");
         for (const at::Tensor* t : {&dk, &dv}) same(*t, k, "dk and dv must have k's shape, type and strides");
         same(delta, lse, "delta must have lse's shape, type and strides");
@@ -461,7 +473,7 @@ PyObject* decode_call(PyObject* const* a, Py_ssize_t n) {
         const int64_t bytes = bytes_of(work);
         s.softmax_scale = real(z[0]);
         sa_window w = {0, 0};
-        if (WINDOW) w = {int32(a[9]), int32(a[10])};
+        if (WINDOW) w = {bound(a[9]), bound(a[10])};
         void* st = stream(z[2]);
         return run([&] {
             if constexpr (WINDOW)

@@ -133,3 +133,22 @@ def test_tensors_of_another_device_are_refused(monkeypatch):
     for call in (lambda: sa.sa_attn_window_fwd(x, x, x, i, x, lse, 4, 2), lambda: sa.sa_attn_window_bwd(x, x, x, x, x, lse, i, lse, x, x, x, None, 4, 2)):
         with pytest.raises(ValueError, match="current device"):
             call()
+
+
+def test_lengths_beyond_32_bits():
+    """The binding's max_len, window and sinks: a number that 32 bits do not hold is the nearest one that they do, none of its bits are dropped."""
+    q, k, off = torch.empty(20000, 4, 64, dtype=torch.bfloat16), torch.empty(20000, 2, 64, dtype=torch.bfloat16), torch.zeros(3, dtype=torch.int32)
+    size = lambda *a: sa.sa_attn_window_bwd_workspace(q, k, off, *a)      # noqa: E731
+    assert size(20000, 10, 2) > 0 and size(20000, 20000, 2) == 0
+    for beyond in (2 ** 31, 2 ** 32, 2 ** 32 + 10, 2 ** 63 - 1, 2 ** 63, 2 ** 64 + 10, 10 ** 40):
+        assert size(20000, beyond, 2) == 0                              # no window: nothing is seen from far
+        assert size(beyond, 10, 2) == size(20000, 10, 2)                # as long as the tensors
+        assert size(20000, 10, beyond) == size(20000, 10, 20000)        # every key is a first one
+        for low in ((20000, -beyond, 2), (20000, 10, -beyond), (-beyond, 10, 2)):
+            with pytest.raises(sa.StripedAttnError) as e:
+                size(*low)
+            assert e.value.status == E_SHAPE
+    for bad in (10.0, "10", None):
+        with pytest.raises((TypeError, ctypes.ArgumentError)):
+            size(20000, bad, 2)
+    assert size(20000, ctypes.c_int32(10), 2) == size(20000, 10, 2)
