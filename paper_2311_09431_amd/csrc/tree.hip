@@ -912,10 +912,11 @@ tree_tiles_kernel(TreeArgs p) {
     }
 }
 
-// Units whose pieces lie in several shares, and rows of sequences without a token.
+// Units whose pieces lie in several shares.  (Each has a chunk: a row is one of a drafted token's, cached itself, and the launches that share chunks have room
+// for more than one.)
 
 // Where the pieces of a unit lie: shares g0 .. g1; the chunks before it and all, in one pass over the sequences.
-struct Pieces { int g0, g1, n; };       // n: chunks (0: no token)
+struct Pieces { int g0, g1; };
 template <int CH, int ROWS>
 __device__ inline Pieces pieces_of(const TreeArgs& p, const Sequence& seq, int b, int kvh, int in_unit, int lane) {
     const int n = chunks_of<CH>(seq), unit = kvh * (units_of<ROWS>(p, seq) / p.H_kv) + in_unit / ROWS;
@@ -929,8 +930,7 @@ __device__ inline Pieces pieces_of(const TreeArgs& p, const Sequence& seq, int b
     all = wave_total(wave_scan(all));
     before = wave_total(wave_scan(before));
     const uint32_t share = (uint32_t)share_of(all, p.n_wgs), from = (uint32_t)(before + unit * n);
-    const int g0 = (int)(from / share);
-    return {g0, n ? (int)((from + n - 1) / share) : g0, n};
+    return {(int)(from / share), (int)((from + n - 1) / share)};
 }
 template <int DP, int ROWS>
 __device__ inline const float* piece(const TreeArgs& p, const Pieces& x, int i) {
@@ -953,8 +953,8 @@ tree_join_kernel(TreeArgs p) {
     const int kvh = head / group, in_unit = t * group + head - kvh * group, row = in_unit % ROWS;
     if (in_unit >= seq.rows) return;
     const Pieces x = pieces_of<CH, ROWS>(p, seq, b, kvh, in_unit, lane);
-    if (x.n && x.g0 == x.g1) return;
-    const int pieces = x.n ? x.g1 - x.g0 + 1 : 0;
+    if (x.g0 == x.g1) return;
+    const int pieces = x.g1 - x.g0 + 1;
     float m = -INFINITY, l = 0.f, acc[COLS] = {};
     bool weightless = false;
     for (int i0 = wave * BATCH; i0 < pieces; i0 += JOIN_WAVES * BATCH) {
@@ -1025,8 +1025,8 @@ tree_join_rows_kernel(TreeArgs p) {
     seq = {scalar(seq.before), scalar(seq.len), scalar(seq.rows)};
     if (first >= seq.rows) return;
     const Pieces x = pieces_of<CH, ROWS>(p, seq, b, kvh, first, lane);
-    if (x.n && x.g0 == x.g1) return;
-    const int pieces = x.n ? x.g1 - x.g0 + 1 : 0;
+    if (x.g0 == x.g1) return;
+    const int pieces = x.g1 - x.g0 + 1;
     float m = -INFINITY, l = 0.f;
     Floats acc[N] = {};
     bool weightless = false;
