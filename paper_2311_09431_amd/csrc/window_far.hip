@@ -237,8 +237,23 @@ window_far_kernel(WindowArgs p, int block0) {
     }
 }
 
+// fp32 up to 128 columns: the windows' own sums come of three bf16 terms, and those of 32 keys that are all faint are too small for these (f32_rows.h).
+// which: dV or dK, as of a launch on the sequence alone.  The tile's keys that have no slot are where they end.
+__device__ inline bool faint_tile(const WindowArgs& p, int slot, int kvh, int key, int which, int lane) {
+    const float least = which ? FAINT * p.scale : FAINT;
+    const int end = min(p.c, key / 32 * 32 + 32);
+    for (int other = key / 32 * 32; other < end; ++other) {
+        const float* from = is_far(p, other) ? slot_row(p, slot, kvh, other) + which * p.d
+                                             : (which ? p.dk : p.dv) + kvh * p.kv_stride_h + (int64_t)other * p.kv_stride_s;
+        bool loud = false;
+        for (int col = lane; col < p.d; col += 64) loud = loud || fabsf(from[col]) >= least;
+        if (__builtin_amdgcn_ballot_w64(loud)) return false;
+    }
+    return true;
+}
+
 // dK and dV of a sequence's first keys put together, a wavefront a key: the windows' own sums and each part's, in order.  Where that is no number
-// (or, in fp32, faint: f32_rows.h) the row is done over.
+// (or, in fp32, faint, of a tile that is: a faint key alone is what peaked scores leave) the row is done over.
 template <typename T>
 __global__ void __launch_bounds__(64 * WAVES)
 window_join_kernel(WindowArgs p, int block0) {
@@ -279,8 +294,6 @@ window_join_kernel(WindowArgs p, int block0) {
             loud[w] = fmaxf(loud[w], fabsf(sum[w][i]));
         }
     bool odd = __builtin_amdgcn_ballot_w64(z != 0.f) != 0;
-    if (sizeof(T) == 4)
-        for (int w = 0; w < 2; ++w) odd = odd || (__builtin_amdgcn_ballot_w64(loud[w] >= FAINT) == 0 && __builtin_amdgcn_ballot_w64(loud[w] > 0.f) != 0);
     // the arguments of a launch on that sequence alone
     const int64_t q = first * p.stride_s, kv = first * p.kv_stride_s;
     p.q = (const T*)p.q + q;
@@ -291,6 +304,11 @@ window_join_kernel(WindowArgs p, int block0) {
     p.dv = (float*)((T*)p.dv + kv);
     p.lse += first;
     p.delta += first;
+    if constexpr (sizeof(T) == 4)
+        if (p.d <= 128)
+            for (int w = 0; w < 2; ++w)
+                odd = odd || (__builtin_amdgcn_ballot_w64(loud[w] >= FAINT) == 0 && __builtin_amdgcn_ballot_w64(loud[w] > 0.f) != 0 &&
+                              faint_tile(p, at_slot.slot, kvh, key, w, lane));
     if (odd) return window_dkdv_row<T>(p, kvh, key, 0, p.d, lane);
     const int64_t row = kvh * p.kv_stride_h + (int64_t)key * p.kv_stride_s;
 #pragma unroll

@@ -3,6 +3,7 @@ import pytest
 import torch
 
 from paper_2311_09431_amd import binding as sa
+from seen import window_mask
 from sequences import lengths_to_offsets, normal
 from test_window_gpu import compare
 
@@ -55,3 +56,52 @@ def test_workspace_is_as_large_as_it_says(lens, empty, d, dtype):
     out, lse, *grads = gradient(*ins, lengths_to_offsets(lens + [0] * empty).cuda(), max(lens), window, sinks)
     q, k, v, g = ins
     compare(lens, H, H_kv, d, dtype, window, sinks, (q, k, v, g), out, lse, grads)
+
+
+@pytest.mark.parametrize("small", ["q", "k", "v", "g"])
+@pytest.mark.parametrize("d,H,H_kv,sinks", [(64, 2, 1, 4), (100, 2, 2, 40), (128, 16, 8, 33), (256, 2, 1, 5)])
+def test_small_magnitudes_and_first_keys_seen_from_far(d, H, H_kv, sinks, small):
+    # as the ring step has it: three bf16 terms hold fewer than 24 bits of a number below 2^-109, and every output's error in the 2-norm is as without
+    n, window = 700, 100
+    see = window_mask(n, window, sinks).cuda()
+    for exponent in (-100, -105, -109, -112, -116, -120):
+        x = dict(zip("qkvg", tensors(n, H, H_kv, d, F32)))
+        x[small] = x[small] * 2.0 ** exponent
+        out, _, *grads = gradient(*x.values(), lengths_to_offsets([n]).cuda(), n, window, sinks)
+        q, k, v, g = (y.double().transpose(0, 1) for y in x.values())
+        k, v = (y.repeat_interleave(H // H_kv, 0) for y in (k, v))
+        t = lambda y: y.transpose(-1, -2).contiguous()      # noqa: E731
+        p = (q @ t(k) * d ** -0.5).masked_fill(~see, -float("inf")).softmax(-1)
+        ds = p * (g @ t(v) - (g * (p @ v)).sum(-1, keepdim=True)) * d ** -0.5
+        shared = lambda y: y.view(H_kv, H // H_kv, n, d).sum(1)      # noqa: E731
+        for name, got, want in (("O", out, p @ v), ("dQ", grads[0], ds @ k), ("dK", grads[1], shared(t(ds) @ q)), ("dV", grads[2], shared(t(p) @ g))):
+            got = got.double().transpose(0, 1)
+            # The first keys by themselves too.  (Not dQ of the first rows: dP - delta is a difference of two numbers that are alike, in row 0 the same, so
+            # that what both are rounded by, about sqrt(d) 2^-24 of them each, 1e-6 at 256 columns, is not small beside what is left.)
+            for rows in (slice(0, n), slice(0, sinks)) if name in ("dK", "dV") else (slice(0, n),):
+                error = float((got - want)[:, rows].norm() / want[:, rows].norm())
+                assert error <= 1e-6, (name, exponent, rows, error)
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_peaked_scores_and_first_keys_take_no_longer(d):
+    # scores of standard deviation 300 leave single first keys whose every probability is below 2^-105 beside others
+    n, H, window, sinks, off = 700, 8, 128, 130, lengths_to_offsets([700]).cuda()
+    times = []
+    for spread in (1, 300):
+        q, k, v, g = tensors(n, H, H, d, F32)
+        q *= spread
+        out, lse, *grads = gradient(q, k, v, g, off, n, window, sinks)
+        delta, work = torch.empty_like(lse), torch.empty(sa.sa_attn_window_bwd_workspace(q, k, off, n, window, sinks), dtype=torch.uint8, device="cuda")
+        taken = []
+        for _ in range(5):
+            start, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            start.record()
+            for _ in range(4):
+                sa.sa_attn_window_bwd(q, k, v, out, g, lse, off, delta, *grads, work, n, window, sinks)
+            end.record()
+            torch.cuda.synchronize()
+            taken.append(start.elapsed_time(end))
+        times.append(min(taken))
+        faint = [int(((x[:sinks].abs().amax(-1) < 2.0 ** -105) & (x[:sinks] != 0).any(-1)).sum()) for x in grads[1:]]
+    assert all(faint) and times[1] <= 2 * times[0], (faint, times)
