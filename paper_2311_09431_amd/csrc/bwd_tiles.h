@@ -376,7 +376,7 @@ __device__ __forceinline__ void bwd_dq(const Args& p, int n_tiles, int linear, c
         for (int mb = 0; mb < MB; ++mb) store_bf16((__bf16*)p.dq + base + (int64_t)a * ss, 32 * mb, acc[mb], p.scale, stored, h, d);
         if constexpr (WINDOW)
             each_window_row<true, BM>(odd, (int)blockIdx.x, launch_args().H, 32 * wave, [&](const WindowArgs& again, int head, int row) {
-                window_dq_row<__hip_bfloat16>(again, head, row, threadIdx.x & 63);
+                window_dq_row<__hip_bfloat16>(again, head, row);
             });
         return;
     }
@@ -805,7 +805,7 @@ __device__ __forceinline__ void bwd_dkdv(const Args& p, int n_tiles, int linear,
             }
             each_window_row<false, BM>(odd, (int)blockIdx.x, launch_args().H_kv * NH, 32 * wave, [&](const WindowArgs& again, int head, int row) {
                 const int col0 = head % NH * 128;
-                window_dkdv_row<__hip_bfloat16>(again, head / NH, row, col0, NH > 1 ? min(again.d, col0 + 128) : again.d, threadIdx.x & 63);
+                window_dkdv_row<__hip_bfloat16>(again, head / NH, row, col0, NH > 1 ? min(again.d, col0 + 128) : again.d);
             });
         }
         return;

@@ -314,7 +314,7 @@ fwd_f32_kernel(Args p, int n_tiles) {
         if (kw == 0 && h == 0) *L = top + logf(w_sum);
     }
     each_row<SPLIT>(odd_rows, kw, [&](const StepArgs& again, int i) {
-        if constexpr (WINDOW) window_fwd_row<T>(p, hd, q0 + 32 * qw + i, lane);
+        if constexpr (WINDOW) window_fwd_row<T>(p, hd, q0 + 32 * qw + i);
         else if constexpr (PACKED) fwd_row<T>(p, b, hd, dev_i, q0 + 32 * qw + i, lane);
         else fwd_row<T>(again, b, hd, dev_i, q0 + 32 * qw + i, lane);
     });
@@ -421,7 +421,7 @@ __device__ inline void bwd_dq(const Args& p, int n_tiles, int linear, float* lds
     if (a_own < p.c && !((odd_rows >> n) & 1))
         add_rows<SPLIT, NB>(p.dq + base + (int64_t)a * p.stride_s, acc, p.scale, 0, d, kw, h, p.fresh);
     each_row<SPLIT>(odd_rows, kw, [&](const StepArgs& again, int i) {
-        if constexpr (WINDOW) window_dq_row<T>(p, hd, q0 + 32 * qw + i, lane);
+        if constexpr (WINDOW) window_dq_row<T>(p, hd, q0 + 32 * qw + i);
         else if constexpr (PACKED) dq_row<T>(p, b, hd, dev_i, q0 + 32 * qw + i, lane);
         else dq_row<T>(again, b, hd, dev_i, q0 + 32 * qw + i, lane);
     });
@@ -536,7 +536,7 @@ __device__ inline void bwd_dkdv(const Args& p, int n_tiles, int linear, float* l
         add_rows<SPLIT, NB>(p.dk + row, acck, p.scale, col0, d, qsub, h, p.fresh);
     }
     each_row<SPLIT>(odd_rows, qsub, [&](const StepArgs& again, int i) {
-        if constexpr (WINDOW) window_dkdv_row<T>(p, kvh, k0 + 32 * own + i, col0, HALVES > 1 ? min(d, col0 + 128) : d, lane);
+        if constexpr (WINDOW) window_dkdv_row<T>(p, kvh, k0 + 32 * own + i, col0, HALVES > 1 ? min(d, col0 + 128) : d);
         else if constexpr (PACKED) dkdv_row<T>(p, b, kvh, dev_i, k0 + 32 * own + i, col0, HALVES > 1 ? min(d, col0 + 128) : d, lane);
         else dkdv_row<T>(again, b, kvh, dev_i, k0 + 32 * own + i, col0, HALVES > 1 ? min(d, col0 + 128) : d, lane);
     });

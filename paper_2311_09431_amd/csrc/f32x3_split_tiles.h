@@ -361,7 +361,7 @@ fwd_f32x3_split_kernel(Args p, int n_tiles) {
     const uint32_t odd_rows = fold_forward<DP, WAVES, true, true>(p, acc, m, l, lds, stats, masks, ln, dev, a_own, a, L,
                                                             p.o + base + (int64_t)a * p.stride_s);
     each_row<WAVES>(odd_rows, ln.wave, [&](const StepArgs& again, int i) {
-        if constexpr (WINDOW) window_fwd_row<float>(p, hd, q0 + i, ln.lane);
+        if constexpr (WINDOW) window_fwd_row<float>(p, hd, q0 + i);
         else if constexpr (PACKED) fwd_row<float>(p, b, hd, dev_i, q0 + i, ln.lane);
         else fwd_row<float>(again, b, hd, dev_i, q0 + i, ln.lane);
     });
@@ -475,7 +475,7 @@ __device__ inline void bwd_dq(const Args& p, int n_tiles, int linear, char* lds,
     const uint32_t odd_rows = redo.take(top, top);
     if (a_own < p.c && !((odd_rows >> n) & 1)) add_rows<DP, WAVES>(DQ, old, lds, p.scale, d, ln);
     each_row<WAVES>(odd_rows, ln.wave, [&](const StepArgs& again, int i) {
-        if constexpr (WINDOW) window_dq_row<float>(p, hd, q0 + i, ln.lane);
+        if constexpr (WINDOW) window_dq_row<float>(p, hd, q0 + i);
         else if constexpr (PACKED) dq_row<float>(p, b, hd, dev_i, q0 + i, ln.lane);
         else dq_row<float>(again, b, hd, dev_i, q0 + i, ln.lane);
     });
@@ -627,7 +627,7 @@ __device__ inline void bwd_dkdv(const Args& p, int n_tiles, int linear, char* ld
         }
     }
     each_row<WAVES>(odd_rows, ln.wave, [&](const StepArgs& again, int i) {
-        if constexpr (WINDOW) window_dkdv_row<float>(p, kvh, k0 + i, 0, d, ln.lane);
+        if constexpr (WINDOW) window_dkdv_row<float>(p, kvh, k0 + i, 0, d);
         else if constexpr (PACKED) dkdv_row<float>(p, b, kvh, dev_i, k0 + i, 0, d, ln.lane);
         else dkdv_row<float>(again, b, kvh, dev_i, k0 + i, 0, d, ln.lane);
     });

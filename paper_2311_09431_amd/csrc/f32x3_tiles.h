@@ -333,7 +333,7 @@ fwd_f32x3_kernel(Args p, int n_tiles) {
         if (h == 0) *L = top + logf(w_sum);
     }
     each_row<1>(odd_rows, 0, [&](const StepArgs& again, int i) {
-        if constexpr (WINDOW) window_fwd_row<float>(p, hd, q0 + 32 * ln.wave + i, ln.lane);
+        if constexpr (WINDOW) window_fwd_row<float>(p, hd, q0 + 32 * ln.wave + i);
         else if constexpr (PACKED) fwd_row<float>(p, b, hd, dev_i, q0 + 32 * ln.wave + i, ln.lane);
         else fwd_row<float>(again, b, hd, dev_i, q0 + 32 * ln.wave + i, ln.lane);
     });
@@ -515,7 +515,7 @@ __device__ inline void bwd_dq(const Args& p, int n_tiles, int linear, char* lds,
     if (a_own < p.c && !((odd_rows >> n) & 1))
         add_rows<NB>(p.dq + base + (int64_t)a * p.stride_s, acc, p.scale, 32 * NB * role, d, h, p.fresh);
     each_row<2>(odd_rows, role, [&](const StepArgs& again, int i) {
-        if constexpr (WINDOW) window_dq_row<float>(p, hd, q0 + 32 * group + i, ln.lane);
+        if constexpr (WINDOW) window_dq_row<float>(p, hd, q0 + 32 * group + i);
         else if constexpr (PACKED) dq_row<float>(p, b, hd, dev_i, q0 + 32 * group + i, ln.lane);
         else dq_row<float>(again, b, hd, dev_i, q0 + 32 * group + i, ln.lane);
     });
@@ -667,7 +667,7 @@ __device__ inline void bwd_dkdv(const Args& p, int n_tiles, int linear, char* ld
     if (stored && !((odd_rows >> n) & 1))
         add_rows<NB>((role ? p.dk : p.dv) + row, acc, role ? p.scale : 1.f, 0, d, h, p.fresh);
     each_row<2>(odd_rows, role, [&](const StepArgs& again, int i) {
-        if constexpr (WINDOW) window_dkdv_row<float>(p, kvh, k0 + 32 * group + i, 0, d, ln.lane);
+        if constexpr (WINDOW) window_dkdv_row<float>(p, kvh, k0 + 32 * group + i, 0, d);
         else if constexpr (PACKED) dkdv_row<float>(p, b, kvh, dev_i, k0 + 32 * group + i, 0, d, ln.lane);
         else dkdv_row<float>(again, b, kvh, dev_i, k0 + 32 * group + i, 0, d, ln.lane);
     });

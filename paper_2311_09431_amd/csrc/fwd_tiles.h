@@ -595,7 +595,7 @@ fwd_mfma_kernel(Args p, int n_qtiles) {
     if (h == 0 && stored) L[a] = (top + __builtin_amdgcn_logf(w_sum)) * LN2;
     if constexpr (WINDOW)
         each_window_row<true, BM>(odd, (int)blockIdx.x, launch_args().H, 32 * wave, [&](const WindowArgs& again, int head, int row) {
-            window_fwd_row<__hip_bfloat16>(again, head, row, threadIdx.x & 63);
+            window_fwd_row<__hip_bfloat16>(again, head, row);
         });
 }
 

@@ -377,7 +377,7 @@ fwd_split_kernel(Args p, int n_tiles) {
                                                              (OutT*)p.o + base + (int64_t)a * p.stride_s, odd_acc);
     if constexpr (WINDOW)
         each_window_row<true, OWN>(odd_rows & 0xffffffffu / ((1u << WAVES) - 1) << ln.wave, (int)blockIdx.x, p.H, 0,
-                                   [&](const WindowArgs& again, int head, int row) { window_fwd_row<__hip_bfloat16>(again, head, row, ln.lane); });
+                                   [&](const WindowArgs& again, int head, int row) { window_fwd_row<__hip_bfloat16>(again, head, row); });
     if (EXACT) each_row<WAVES>(odd_rows, ln.wave, [&](const StepArgs& again, int i) { fwd_row<__hip_bfloat16>(again, b, hd, dev_i, q0 + i, ln.lane); });
 }
 
@@ -584,7 +584,7 @@ __device__ inline void bwd_dq(const Args& p, int n_tiles, int linear, char* lds,
         const uint32_t odd_rows = WINDOW ? take_odd<WAVES>(masks) : 0;
         if (a_own < p.c && !((odd_rows >> n) & 1)) set_rows<DP, WAVES>((__bf16*)p.dq + base + (int64_t)a * p.stride_s, lds, p.scale, d, ln);
         if constexpr (WINDOW)
-            each_row<WAVES>(odd_rows, ln.wave, [&](const StepArgs&, int i) { window_dq_row<__hip_bfloat16>(p, hd, q0 + i, ln.lane); });
+            each_row<WAVES>(odd_rows, ln.wave, [&](const StepArgs&, int i) { window_dq_row<__hip_bfloat16>(p, hd, q0 + i); });
         return;
     }
     float* const DQ = p.dq + base + (int64_t)a * p.stride_s;
@@ -837,7 +837,7 @@ __device__ inline void bwd_dkdv(const Args& p, int n_tiles, int linear, char* ld
                 for (int i = 0; i < share_of(DP, WAVES); ++i) none[i] = make_float4(0.f, 0.f, 0.f, 0.f);
                 add_rows<DP, WAVES>(to + d, none, lds + HALF, -p.scale, d, ln);
             }
-            each_row<WAVES>(odd_rows, wave, [&](const StepArgs&, int i) { window_dkdv_row<__hip_bfloat16>(p, kvh, k0 + i, 0, d, ln.lane); });
+            each_row<WAVES>(odd_rows, wave, [&](const StepArgs&, int i) { window_dkdv_row<__hip_bfloat16>(p, kvh, k0 + i, 0, d); });
         }
         if (ends && !((odd_rows >> n) & 1)) {
             set_rows<DP, WAVES>((__bf16*)p.dv + row, lds, 1.f, d, ln);

@@ -309,7 +309,7 @@ window_join_kernel(WindowArgs p, int block0) {
             for (int w = 0; w < 2; ++w)
                 odd = odd || (__builtin_amdgcn_ballot_w64(loud[w] >= FAINT) == 0 && __builtin_amdgcn_ballot_w64(loud[w] > 0.f) != 0 &&
                               faint_tile(p, at_slot.slot, kvh, key, w, lane));
-    if (odd) return window_dkdv_row<T>(p, kvh, key, 0, p.d, lane);
+    if (odd) return window_dkdv_row<T>(p, kvh, key, 0, p.d);
     const int64_t row = kvh * p.kv_stride_h + (int64_t)key * p.kv_stride_s;
 #pragma unroll
     for (int i = 0; i < ROW_COLS; ++i)

@@ -3,9 +3,9 @@ import pytest
 import torch
 
 from paper_2311_09431_amd import binding as sa
-from seen import window_mask
-from sequences import lengths_to_offsets, normal
-from test_window_gpu import compare
+from seen import Seen, window_mask
+from sequences import check, lengths_to_offsets, normal
+from test_window_gpu import ROUNDED, compare
 
 pytestmark = pytest.mark.gpu
 
@@ -105,3 +105,73 @@ def test_peaked_scores_and_first_keys_take_no_longer(d):
         times.append(min(taken))
         faint = [int(((x[:sinks].abs().amax(-1) < 2.0 ** -105) & (x[:sinks] != 0).any(-1)).sum()) for x in grads[1:]]
     assert all(faint) and times[1] <= 2 * times[0], (faint, times)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("H,H_kv,d,window,sinks,few", [(2, 1, 4, 20, 3, True), (2, 2, 68, 20, 0, True), (4, 1, 100, 20, 3, True), (24, 12, 100, 20, 3, False),
+                                                        (2, 1, 128, 90, 3, True), (24, 12, 64, 90, 3, False), (24, 12, 128, 20, 3, False), (4, 2, 256, 90, 3, False)])
+def test_rows_done_over(H, H_kv, d, window, sinks, few, dtype):
+    """A value that is no number, of a key in the first tile: rows that do not see it, and keys that none of the rows sees that do, have the result of 64 bits."""
+    n, at = 430, 50
+    lens = [n] if few else [n, 700, 300]            # (few tiles, and many)
+    q, k, v, g = tensors(sum(lens), H, H_kv, d, dtype)
+    v[at] = float("nan")
+    off = lengths_to_offsets(lens).cuda()
+    out, lse, grads = torch.full_like(q, 7), torch.full((H, sum(lens)), 7.0, device="cuda"), [torch.full_like(x, 7) for x in (q, k, v)]
+    sa.sa_attn_window_fwd(q, k, v, off, out, lse, max(lens), window, sinks)
+    work = torch.empty(sa.sa_attn_window_bwd_workspace(q, k, off, max(lens), window, sinks), dtype=torch.uint8, device="cuda")
+    sa.sa_attn_window_bwd(q, k, v, out, g, lse, off, torch.empty_like(lse), *grads, work, max(lens), window, sinks)
+    q, k, v, g, out, lse, dq, dk, dv = (x.cpu() for x in (q, k, v, g, out, lse, *grads))
+    assert out[at:at + window].isnan().all() and torch.isfinite(lse).all()
+    v[at], r, G = 0, slice(0, n), H // H_kv
+    sees = window_mask(n, window, sinks)
+    rows, w = ~sees[:, at], ROUNDED[dtype]
+    keys = ~sees[~rows].any(0)
+    assert rows.any() and keys.any()
+    for kvh in {0, H_kv // 2, H_kv - 1}:
+        want_k = want_v = off_k = off_v = 0
+        for h in range(kvh * G, kvh * G + G):
+            x = Seen(q[r, h], k[r, kvh], v[r, kvh], d ** -0.5, sees, g[r, h])
+            dq_off, a, b = x.grad_off(dtype, w)
+            check(("out", h), out[r, h][rows], x.out[rows], x.out_off(dtype, w)[rows])
+            check(("lse", h), lse[h, r], x.lse, x.lse_off)
+            check(("dq", h), dq[r, h][rows], x.dq[rows], dq_off[rows])
+            want_k, want_v, off_k, off_v = want_k + x.dk, want_v + x.dv, off_k + a, off_v + b
+        check(("dk", kvh), dk[r, kvh][keys], want_k[keys], off_k[keys])
+        check(("dv", kvh), dv[r, kvh][keys], want_v[keys], off_v[keys])
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("H,H_kv,d", [(8, 4, 128), (16, 2, 64), (2, 2, 256)])
+def test_inputs_of_no_numbers_take_no_longer(H, H_kv, d, dtype):
+    """As a step that has diverged leaves them, or a first key that all rows see: every result is NaN, in at most ten times an ordinary call's time (walking
+    over every pair took 130 to 250 times)."""
+    n, window, sinks, off, times = 4096, 512, 4, lengths_to_offsets([4096]).cuda(), []
+    for which in ("none", "all", "key"):
+        q, k, v, g = tensors(n, H, H_kv, d, dtype)
+        if which == "all":
+            for x in (q, k, v, g):
+                x.fill_(float("nan"))
+        elif which == "key":
+            k[0] = float("nan")
+        out, lse, delta, grads = torch.empty_like(q), torch.empty(H, n, device="cuda"), torch.empty(H, n, device="cuda"), [torch.empty_like(x) for x in (q, k, v)]
+        work = torch.empty(sa.sa_attn_window_bwd_workspace(q, k, off, n, window, sinks), dtype=torch.uint8, device="cuda")
+        calls = (lambda: sa.sa_attn_window_fwd(q, k, v, off, out, lse, n, window, sinks),
+                 lambda: sa.sa_attn_window_bwd(q, k, v, out, g, lse, off, delta, *grads, work, n, window, sinks))
+        taken = []
+        for call in calls:
+            call()
+            least = []
+            for _ in range(3):
+                start, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+                start.record()
+                call()
+                call()
+                end.record()
+                torch.cuda.synchronize()
+                least.append(start.elapsed_time(end))
+            taken.append(min(least))
+        times.append(taken)
+        for x in (out, lse, *grads):
+            assert x.isnan().all() if which != "none" else torch.isfinite(x).all()
+    assert all(x <= 10 * y for slow in times[1:] for x, y in zip(slow, times[0])), times
