@@ -221,6 +221,8 @@ __device__ __forceinline__ void bwd_dq(const Args& p, int n_tiles, int linear, c
         sink_base = p.sinks - 4 * h;
     }
     const int t_begin = WINDOW ? 2 * walk.at(0) : 0;
+    [[maybe_unused]] const int whole_end = Kr[2];
+    if constexpr (WINDOW) Kr[2] = Vr[2] = walk.reach(p, 0, whole_end, pitch);
     load_tile(Kr, t_begin * tile_pitch, k_lds0);
     load_tile(Vr, t_begin * tile_pitch, v_lds0);
     load_tile(Kr, (t_begin + 1) * tile_pitch, k_lds1);       // n_kt >= 2 always
@@ -326,6 +328,7 @@ __device__ __forceinline__ void bwd_dq(const Args& p, int n_tiles, int linear, c
         int i = 0;
         for (; i < walk.masked; ++i) {
             const int next = 2 * walk.at(i + 1);
+            Kr[2] = Vr[2] = walk.reach(p, i + 1, whole_end, pitch);
             trip(F{}, T{}, P0{}, T{}, t, Kr, Vr, next * tile_pitch);
             trip(F{}, T{}, P1{}, T{}, t + 1, Kr, Vr, (next + 1) * tile_pitch);
             t = next;
@@ -375,7 +378,7 @@ __device__ __forceinline__ void bwd_dq(const Args& p, int n_tiles, int linear, c
 #pragma unroll
         for (int mb = 0; mb < MB; ++mb) store_bf16((__bf16*)p.dq + base + (int64_t)a * ss, 32 * mb, acc[mb], p.scale, stored, h, d);
         if constexpr (WINDOW)
-            each_window_row<true, BM>(odd, (int)blockIdx.x, launch_args().H, 32 * wave, [&](const WindowArgs& again, int head, int row) {
+            each_window_row<true, BM>(odd, (int)blockIdx.x, launch_args().H, 32 * wave, [&](const WindowArgs& again, int head, int row, int) {
                 window_dq_row<__hip_bfloat16>(again, head, row);
             });
         return;
@@ -780,13 +783,18 @@ __device__ __forceinline__ void bwd_dkdv(const Args& p, int n_tiles, int linear,
 
     if constexpr (PACKED) {
         const int64_t row = kv_base + (int64_t)key * ss;
-        uint32_t odd = 0;       // rows to do over
-        if constexpr (WINDOW) odd = row_mask(key_ok && !is_far(p, key_own) && (window_odd<MB, PART>(accv, h, d, 128 * ohalf) || window_odd<MB, PART>(acck, h, d, 128 * ohalf)));
-        bool stored = key_ok;
-        if constexpr (WINDOW) stored = key_ok && !((odd >> n) & 1) && !is_far(p, key_own);
+        uint32_t odd = 0, odd_v = 0;            // rows to do over, those whose dV is too
+        bool stored = key_ok, stored_v = key_ok;
+        if constexpr (WINDOW) {
+            stored = stored_v = key_ok && !is_far(p, key_own);
+            odd_v = row_mask(stored && window_odd<MB, PART>(accv, h, d, 128 * ohalf));
+            odd = odd_v | row_mask(stored && window_odd<MB, PART>(acck, h, d, 128 * ohalf));
+            stored = stored && !((odd >> n) & 1);
+            stored_v = stored_v && !((odd_v >> n) & 1);
+        }
 #pragma unroll
         for (int mb = 0; mb < MB; ++mb) {
-            store_bf16((__bf16*)p.dv + row, 128 * ohalf + 32 * mb, accv[mb], 1.f, stored, h, d);
+            store_bf16((__bf16*)p.dv + row, 128 * ohalf + 32 * mb, accv[mb], 1.f, stored_v, h, d);
             store_bf16((__bf16*)p.dk + row, 128 * ohalf + 32 * mb, acck[mb], p.scale, stored, h, d);
         }
         if constexpr (WINDOW) {
@@ -803,9 +811,9 @@ __device__ __forceinline__ void bwd_dkdv(const Args& p, int n_tiles, int linear,
                                                                                p.scale * acck[mb][4 * g + 2], p.scale * acck[mb][4 * g + 3]);
                     }
             }
-            each_window_row<false, BM>(odd, (int)blockIdx.x, launch_args().H_kv * NH, 32 * wave, [&](const WindowArgs& again, int head, int row) {
+            each_window_row<false, BM>(odd, (int)blockIdx.x, launch_args().H_kv * NH, 32 * wave, [&](const WindowArgs& again, int head, int row, int bit) {
                 const int col0 = head % NH * 128;
-                window_dkdv_row<__hip_bfloat16>(again, head / NH, row, col0, NH > 1 ? min(again.d, col0 + 128) : again.d);
+                window_dkdv_row<__hip_bfloat16>(again, head / NH, row, col0, NH > 1 ? min(again.d, col0 + 128) : again.d, (odd_v >> bit) & 1);
             });
         }
         return;

@@ -206,8 +206,10 @@ fwd_f32_kernel(Args p, int n_tiles) {
         }
         for (; t0 <= last_key;) {
             __syncthreads();
-            stage<T, DP, TK>(k_lds, K, p.kv_stride_s, t0, p.c, d);
-            stage<T, DP, TK>(v_lds, V, p.kv_stride_s, t0, p.c, d);
+            int rows = p.c;
+            if constexpr (WINDOW) rows = rows_to_read<TK>(p, t0, start);
+            stage<T, DP, TK>(k_lds, K, p.kv_stride_s, t0, rows, d);
+            stage<T, DP, TK>(v_lds, V, p.kv_stride_s, t0, rows, d);
             __syncthreads();
 #pragma unroll 1
             for (int s = 0; s < SUB; ++s) {
@@ -391,8 +393,10 @@ __device__ inline void bwd_dq(const Args& p, int n_tiles, int linear, float* lds
         }
         for (; t0 <= last_key;) {
             __syncthreads();
-            stage<T, DP, TK>(k_lds, K, p.kv_stride_s, t0, p.c, d);
-            stage<T, DP, TK>(v_lds, V, p.kv_stride_s, t0, p.c, d);
+            int rows = p.c;
+            if constexpr (WINDOW) rows = rows_to_read<TK>(p, t0, start);
+            stage<T, DP, TK>(k_lds, K, p.kv_stride_s, t0, rows, d);
+            stage<T, DP, TK>(v_lds, V, p.kv_stride_s, t0, rows, d);
             __syncthreads();
 #pragma unroll 1
             for (int s = 0; s < SUB; ++s) {

@@ -276,6 +276,7 @@ fwd_f32x3_split_kernel(Args p, int n_tiles) {
     char* const v = k + RAW_BYTES<DP>;
     dt_rsrc K = stream_rsrc((const float*)p.k + kv_base, p.c, pitch, d);
     dt_rsrc V = stream_rsrc((const float*)p.v + kv_base, p.c, pitch, d);
+    [[maybe_unused]] const int whole_end = K[2];
     int kv_at = at.kv;
     // (behind the walk's end: rows beyond the matrix, whose loads deliver zeros without a look at memory)
     const int beyond = 32 * at.n_full;
@@ -286,6 +287,7 @@ fwd_f32x3_split_kernel(Args p, int n_tiles) {
         if constexpr (WINDOW) {         // (at.v: the sub-tile's place in the walk)
             key0 = at.v < walk.n ? 32 * walk.at(at.v) : beyond;
             shift = 0;
+            K[2] = V[2] = walk.reach(p, at.v, whole_end, pitch);
             at.v += WAVES;
             return;
         }
@@ -393,6 +395,7 @@ __device__ inline void bwd_dq(const Args& p, int n_tiles, int linear, char* lds,
     char* const v = k + RAW_BYTES<DP>;
     dt_rsrc K = stream_rsrc((const float*)p.k + kv_base, p.c, pitch, d);
     dt_rsrc V = stream_rsrc((const float*)p.v + kv_base, p.c, pitch, d);
+    [[maybe_unused]] const int whole_end = K[2];
     int kv_at = at.kv;
     const int beyond = 32 * at.n_full;          // as in the forward kernel
     int key0, shift;
@@ -402,6 +405,7 @@ __device__ inline void bwd_dq(const Args& p, int n_tiles, int linear, char* lds,
         if constexpr (WINDOW) {         // (at.v: the sub-tile's place in the walk)
             key0 = at.v < walk.n ? 32 * walk.at(at.v) : beyond;
             shift = 0;
+            K[2] = V[2] = walk.reach(p, at.v, whole_end, pitch);
             at.v += WAVES;
             return;
         }

@@ -194,8 +194,10 @@ __device__ inline void walk_keys(const Args& p, int dev, int q0, int64_t kv_base
         return block_kind(dev, kv, p.layout) == MASK_FULL ? p.c - 1 : q_last - block_off(dev, kv, p.layout);
     };
     auto fetch = [&]() {
-        sk.fetch(K + (kv_a - p.kv_dev) * p.kv_shard, p.kv_stride_s, t_a, p.c, p.d);
-        sv.fetch(V + (kv_a - p.kv_dev) * p.kv_shard, p.kv_stride_s, t_a, p.c, p.d);
+        int rows = p.c;
+        if constexpr (WINDOW) rows = rows_to_read<TILE>(p, t_a, start);
+        sk.fetch(K + (kv_a - p.kv_dev) * p.kv_shard, p.kv_stride_s, t_a, rows, p.d);
+        sv.fetch(V + (kv_a - p.kv_dev) * p.kv_shard, p.kv_stride_s, t_a, rows, p.d);
         if constexpr (WINDOW) t_a = next_tile<TILE>(p, t_a, start);
         else t_a += TILE;
         if (t_a > last_key(kv_a)) {
@@ -441,8 +443,10 @@ __device__ inline void bwd_dq(const Args& p, int n_tiles, int linear, char* lds,
         t_a = first_tile(p, start);
     }
     auto fetch = [&]() {
-        sk.fetch((const float*)p.k + kv_base + (kv_a - p.kv_dev) * p.kv_shard, p.kv_stride_s, t_a, p.c, d);
-        sv.fetch((const float*)p.v + kv_base + (kv_a - p.kv_dev) * p.kv_shard, p.kv_stride_s, t_a, p.c, d);
+        int rows = p.c;
+        if constexpr (WINDOW) rows = rows_to_read<TILE>(p, t_a, start);
+        sk.fetch((const float*)p.k + kv_base + (kv_a - p.kv_dev) * p.kv_shard, p.kv_stride_s, t_a, rows, d);
+        sv.fetch((const float*)p.v + kv_base + (kv_a - p.kv_dev) * p.kv_shard, p.kv_stride_s, t_a, rows, d);
         if constexpr (WINDOW) t_a = next_tile<TILE>(p, t_a, start);
         else t_a += TILE;
         if (t_a > (block_kind(dev, kv_a, p.layout) == MASK_FULL ? p.c - 1 : q_last - block_off(dev, kv_a, p.layout))) {

@@ -377,6 +377,8 @@ fwd_mfma_kernel(Args p, int n_qtiles) {
         sink_base = p.sinks - 4 * h;
     }
     const int t_begin = WINDOW ? 2 * walk.at(0) : 0;
+    [[maybe_unused]] const int whole_end = K[2];
+    if constexpr (WINDOW) K[2] = V[2] = walk.reach(p, 0, whole_end, pitch);
     // first tiles on their way while the running state is loaded
     load_k(K, t_begin * tile_pitch, k_lds0);
     load_v(V, t_begin * tile_pitch, v_lds0);
@@ -505,12 +507,20 @@ fwd_mfma_kernel(Args p, int n_qtiles) {
     };
     if constexpr (WINDOW) {
         t = t_begin;
+        // a masked pair, which requests the one behind it
+        auto window_pair = [&](auto first_c, int i) __attribute__((always_inline)) {
+            dt_rsrc kr = K, vr = V;
+            kr[2] = vr[2] = walk.reach(p, i + 1, whole_end, pitch);
+            pair(first_c, T{}, kr, vr, 2 * walk.at(i + 1) * tile_pitch);
+            K = kr;
+            V = vr;
+        };
         if (walk.n > 1) {
-            pair(T{}, T{}, K, V, 2 * walk.at(1) * tile_pitch);
+            window_pair(T{}, 0);
             int i = 1;
             for (; i < walk.masked; ++i) {
                 t = 2 * walk.at(i);
-                pair(F{}, T{}, K, V, 2 * walk.at(i + 1) * tile_pitch);
+                window_pair(F{}, i);
             }
             for (t = 2 * walk.at(i); i < walk.n - 1; ++i, t += 2) pair(F{}, F{}, K, V, (t + 2) * tile_pitch);      // the hot loop
             last_pair(F{});
@@ -564,9 +574,11 @@ fwd_mfma_kernel(Args p, int n_qtiles) {
     const float w_sum = w_old + w_part;
     const float inv = w_sum > 0.f ? 1.f / w_sum : 0.f;
     const float a_old = w_old * inv;
-    const float a_part = l_tot > 0.f ? w_part * inv / l_tot : 0.f;
+    // WINDOW: a row sum that is no positive number says so of the row (scores that are not seen are no part of it)
+    const bool number = !WINDOW || (l_tot > 0.f && l_tot < INFINITY);
+    const float a_part = !number ? NAN : l_tot > 0.f ? w_part * inv / l_tot : 0.f;
     uint32_t odd = 0;           // rows to do over
-    if constexpr (WINDOW) odd = row_mask(row_ok && (!(l_tot > 0.f && l_tot < INFINITY) || window_odd<MB, PART>(oacc, h, d)));
+    if constexpr (WINDOW) odd = row_mask(row_ok && number && window_odd<MB, PART>(oacc, h, d));
     const bool stored = row_ok && (!WINDOW || !((odd >> n) & 1));
 #pragma unroll
     for (int mb = 0; mb < MB; ++mb)
@@ -592,9 +604,9 @@ fwd_mfma_kernel(Args p, int n_qtiles) {
                 *dst = x;
             }
         }
-    if (h == 0 && stored) L[a] = (top + __builtin_amdgcn_logf(w_sum)) * LN2;
+    if (h == 0 && row_ok) L[a] = number ? (top + __builtin_amdgcn_logf(w_sum)) * LN2 : NAN;
     if constexpr (WINDOW)
-        each_window_row<true, BM>(odd, (int)blockIdx.x, launch_args().H, 32 * wave, [&](const WindowArgs& again, int head, int row) {
+        each_window_row<true, BM>(odd, (int)blockIdx.x, launch_args().H, 32 * wave, [&](const WindowArgs& again, int head, int row, int) {
             window_fwd_row<__hip_bfloat16>(again, head, row);
         });
 }

@@ -96,7 +96,7 @@ __global__ void __launch_bounds__(64 * BWD_WAVES, DP <= 64 ? 2 : 1)
 window_bwd_split_kernel(WindowArgs p, int n_dkdv) {
     __shared__ __attribute__((aligned(1024))) char lds[BWD_WAVES * 2 * STAGE_BYTES<DP> + 2 * SUB_BYTES<DP>];
     __shared__ __attribute__((aligned(1024))) char stats[BWD_WAVES * 2 * STAT_BYTES];
-    __shared__ uint32_t masks[BWD_WAVES];
+    __shared__ uint32_t masks[2 * BWD_WAVES];
     int n_tiles, rank, head, seq;
     if ((int)blockIdx.x < n_dkdv) {
         if (!enter_sequence<false, OWN>(p, (int)blockIdx.x, p.H_kv, n_tiles, rank, head, &seq)) return;

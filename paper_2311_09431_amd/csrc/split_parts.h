@@ -166,7 +166,8 @@ struct KeyCursor {
 // Forward, the end: the wavefronts' partial results (accumulators, base-2 reference m, half-wave row sum l) folded
 // into the running state of the lane's row (base: of the workgroup's rows' matrix, a: the row, clamped to the shard).
 // Returns the rows to do over (EXACT only; TERMS: V was three bf16 terms, masks are the words of RowsToRedo).  OutT: float, or __bf16
-// for rows that end here (packed sequences, p.fresh).  WINDOW: rows whose results are not finite (odd_acc: this wavefront's are not) are done over too.
+// for rows that end here (packed sequences, p.fresh).  WINDOW: rows with a number for their sum and results that are not finite (odd_acc: this
+// wavefront's are not) are done over, but for their LSE; a sum that is no positive number says so of the row (scores that are not seen are no part of it).
 template <int DP, int WAVES, bool EXACT, bool TERMS, bool WINDOW = false, typename Lane, typename OutT>
 __device__ __forceinline__ uint32_t fold_forward(const StepArgs& p, f32x16 (&acc)[4], float m, float l, char* lds, float* stats,
                                                  uint32_t* masks, const Lane& ln, int dev, int a_own, int a, float* L, OutT* O,
@@ -205,14 +206,15 @@ __device__ __forceinline__ uint32_t fold_forward(const StepArgs& p, f32x16 (&acc
         if (TERMS) redo.put(odd, top_acc * f, top_acc * f);
         else put_odd(masks, odd, ln.wave, ln.lane);
     }
-    if (WINDOW) put_odd(masks, a_own < p.c && (odd_acc || !(l_tot > 0.f && l_tot < INFINITY)), ln.wave, ln.lane);
+    const bool number = !WINDOW || (l_tot > 0.f && l_tot < INFINITY);
+    if (WINDOW) put_odd(masks, a_own < p.c && odd_acc && number, ln.wave, ln.lane);
 
     const float part = l_tot == 0.f ? -INFINITY : fmaf(m_all, LN2_HI, fmaf(m_all, LN2_LO, logf(l_tot)));
     const float top = fmaxf(old, part);
     const float ref = top == -INFINITY ? 0.f : top;
     const float w_old = expf(old - ref), w_part = expf(part - ref), w_sum = w_old + w_part;
     const float inv = w_sum > 0.f ? 1.f / w_sum : 0.f;
-    const float f_old = w_old * inv, f_part = l_tot > 0.f ? w_part * inv / l_tot : 0.f;
+    const float f_old = w_old * inv, f_part = !number ? NAN : l_tot > 0.f ? w_part * inv / l_tot : 0.f;
     __syncthreads();
     const uint32_t odd_rows = TERMS ? redo.take(top_acc * f, top_acc * f) : EXACT || WINDOW ? take_odd<WAVES>(masks) : 0;
     // no row here, or no key seen: state unchanged
@@ -239,8 +241,9 @@ __device__ __forceinline__ uint32_t fold_forward(const StepArgs& p, f32x16 (&acc
                 *dst = x;
             }
         }
-        if (ln.wave == 0 && h == 0) *L = top + logf(w_sum);
+        if (!WINDOW && ln.wave == 0 && h == 0) *L = top + logf(w_sum);
     }
+    if (WINDOW && a_own < p.c && ln.wave == 0 && h == 0) *L = number ? top + logf(w_sum) : NAN;
     return odd_rows;
 }
 

@@ -226,6 +226,7 @@ fwd_split_kernel(Args p, int n_tiles) {
     const Loader<DP> loader(pitch, d, ln.lane);
     dt_rsrc K = stream_rsrc((const __bf16*)p.k + kv_base, p.c, pitch, d);
     dt_rsrc V = stream_rsrc((const __bf16*)p.v + kv_base, p.c, pitch, d);
+    [[maybe_unused]] const int whole_end = K[2];
     int kv_loaded = at.kv, kv = 0, key0 = 0, shift = 0;
     WindowWalk<OWN> walk;
     if constexpr (WINDOW) walk = WindowWalk<OWN>(p, q0, min(q0 + OWN - 1, p.c - 1) / OWN + 1);
@@ -234,6 +235,7 @@ fwd_split_kernel(Args p, int n_tiles) {
         if constexpr (WINDOW) {         // (at.v: its place in the walk; one behind it holds no more of anyone's keys)
             key0 = 32 * walk.at(at.v);
             kv = at.v < walk.n ? 0 : at.kv_end;
+            K[2] = V[2] = walk.reach(p, at.v, whole_end, pitch);
             if (at.v < walk.n) loader.all(K, V, key0, k);
             at.v += WAVES;
             return;
@@ -377,7 +379,7 @@ fwd_split_kernel(Args p, int n_tiles) {
                                                              (OutT*)p.o + base + (int64_t)a * p.stride_s, odd_acc);
     if constexpr (WINDOW)
         each_window_row<true, OWN>(odd_rows & 0xffffffffu / ((1u << WAVES) - 1) << ln.wave, (int)blockIdx.x, p.H, 0,
-                                   [&](const WindowArgs& again, int head, int row) { window_fwd_row<__hip_bfloat16>(again, head, row); });
+                                   [&](const WindowArgs& again, int head, int row, int) { window_fwd_row<__hip_bfloat16>(again, head, row); });
     if (EXACT) each_row<WAVES>(odd_rows, ln.wave, [&](const StepArgs& again, int i) { fwd_row<__hip_bfloat16>(again, b, hd, dev_i, q0 + i, ln.lane); });
 }
 
@@ -447,6 +449,7 @@ __device__ inline void bwd_dq(const Args& p, int n_tiles, int linear, char* lds,
     char* const tiles = lds + ln.wave * 2 * STAGE_BYTES<DP>;
     dt_rsrc K = stream_rsrc((const __bf16*)p.k + kv_base, p.c, pitch, d);
     dt_rsrc V = stream_rsrc((const __bf16*)p.v + kv_base, p.c, pitch, d);
+    [[maybe_unused]] const int whole_end = K[2];
     int kv_at = at.kv;
     // (behind the walk's end: rows beyond the matrix, whose loads deliver zeros without a look at memory)
     const int beyond = 32 * at.n_full;
@@ -457,6 +460,7 @@ __device__ inline void bwd_dq(const Args& p, int n_tiles, int linear, char* lds,
     auto take = [&](Tile& t) {
         if constexpr (WINDOW) {         // (at.v: the sub-tile's place in the walk)
             t = {at.v < walk.n ? 32 * walk.at(at.v) : beyond, 0};
+            K[2] = V[2] = walk.reach(p, at.v, whole_end, pitch);
             at.v += WAVES;
             return;
         }
@@ -824,10 +828,12 @@ __device__ inline void bwd_dkdv(const Args& p, int n_tiles, int linear, char* ld
         bool ends = key_own < p.c;              // the key's sums end here
         if constexpr (WINDOW) {
             ends = ends && !is_far(p, key_own);
-            put_odd(masks, ends && (window_odd<MB, PART>(accv, h, d) || window_odd<MB, PART>(acck, h, d)), wave, ln.lane);
+            const bool odd_v = ends && window_odd<MB, PART>(accv, h, d);
+            put_odd(masks + WAVES, odd_v, wave, ln.lane);
+            put_odd(masks, odd_v || (ends && window_odd<MB, PART>(acck, h, d)), wave, ln.lane);
         }
         __syncthreads();
-        const uint32_t odd_rows = WINDOW ? take_odd<WAVES>(masks) : 0;
+        const uint32_t odd_rows = WINDOW ? take_odd<WAVES>(masks) : 0, odd_v = WINDOW ? take_odd<WAVES>(masks + WAVES) : 0;      // to do over, dV too
         if constexpr (WINDOW) {
             if (p.slot >= 0 && key_own < p.c && !ends) {
                 float4 none[share_of(DP, WAVES)] = {};
@@ -837,12 +843,10 @@ __device__ inline void bwd_dkdv(const Args& p, int n_tiles, int linear, char* ld
                 for (int i = 0; i < share_of(DP, WAVES); ++i) none[i] = make_float4(0.f, 0.f, 0.f, 0.f);
                 add_rows<DP, WAVES>(to + d, none, lds + HALF, -p.scale, d, ln);
             }
-            each_row<WAVES>(odd_rows, wave, [&](const StepArgs&, int i) { window_dkdv_row<__hip_bfloat16>(p, kvh, k0 + i, 0, d); });
+            each_row<WAVES>(odd_rows, wave, [&](const StepArgs&, int i) { window_dkdv_row<__hip_bfloat16>(p, kvh, k0 + i, 0, d, (odd_v >> i) & 1); });
         }
-        if (ends && !((odd_rows >> n) & 1)) {
-            set_rows<DP, WAVES>((__bf16*)p.dv + row, lds, 1.f, d, ln);
-            set_rows<DP, WAVES>((__bf16*)p.dk + row, lds + HALF, -p.scale, d, ln);
-        }
+        if (ends && !((odd_v >> n) & 1)) set_rows<DP, WAVES>((__bf16*)p.dv + row, lds, 1.f, d, ln);
+        if (ends && !((odd_rows >> n) & 1)) set_rows<DP, WAVES>((__bf16*)p.dk + row, lds + HALF, -p.scale, d, ln);
         return;
     }
     float4 old_v[MB], old_k[MB];

@@ -112,7 +112,15 @@ struct WindowWalk {
         masked = below < 0 ? 0 : min(n - 1, firsts + below / PAIR + 1 - start);
     }
     __device__ int at(int i) const { return i < firsts ? i : i - firsts + start; }
+    // where the keys of its tile i end that some row can see (whole: bytes up to the last row's end, as a descriptor has them): in the tiles of first keys with
+    // the last of these.  The loads deliver zeros for those behind them, or one of these that is no number would send all later rows to be done over.
+    __device__ int reach(const WindowArgs& p, int i, int whole, int pitch) const {
+        return __builtin_amdgcn_readfirstlane(i < firsts ? whole - (p.c - min(p.sinks, p.c)) * pitch : whole);
+    }
 };
+// the same for tiles of TK rows, as a number of rows
+template <int TK>
+__device__ inline int rows_to_read(const WindowArgs& p, int t0, int start) { return t0 + TK <= start ? min(p.sinks, p.c) : p.c; }
 
 // Rows done over, as f32_rows.h has them: nothing but the pairs that the mask allows, one wavefront a row.  The tiles multiply masked pairs with
 // a weight of zero, of which an infinite or NaN element makes a NaN.
@@ -256,6 +264,7 @@ __device__ inline void window_ranges(const WindowArgs& p, int a, Body body) {
 #pragma unroll 1
     for (int i = 0; i < 2 && on; ++i) on = body(i ? lo : 0, i ? a + 1 : min(p.sinks, lo));
 }
+// (bf16: the tiles' LSE stays, and their row sum has told a row whose scores leave no number; fp32: terms of an infinite key are NaN, the tiles' say nothing)
 template <typename T>
 __device__ inline void window_fwd_row(const WindowArgs& p, int hd, int a) {
     const int lane = lane_anew();
@@ -285,12 +294,13 @@ __device__ inline void window_fwd_row(const WindowArgs& p, int hd, int a) {
             acc = make_float4(acc.x * alpha, acc.y * alpha, acc.z * alpha, acc.w * alpha);
             if (!no_values) window_add<T>(acc, pr, V, p.kv_stride_s, n, col);
             no_values = no_values || lost(acc);
+            if (sizeof(T) == 2 && no_values) return false;
             m = m_new;
         }
         return true;
     });
     window_store<T>(O, acc, 1.f / l, 0, p.d, lane);          // (every key it sees at -inf: no number)
-    if (lane == 0) p.lse[hd * p.stat_stride_h + a] = l == 0.f ? NAN : m + logf(l);
+    if (sizeof(T) == 4 && lane == 0) p.lse[hd * p.stat_stride_h + a] = l == 0.f ? NAN : m + logf(l);
 }
 template <typename T>
 __device__ inline void window_dq_row(const WindowArgs& p, int hd, int a) {
@@ -323,9 +333,9 @@ __device__ inline void window_dq_row(const WindowArgs& p, int hd, int a) {
     });
     window_store<T>((T*)p.dq + row, acc, p.scale, 0, p.d, lane);
 }
-// columns col0 .. end_col - 1 of dK and dV, of all rows that see the key
+// columns col0 .. end_col - 1 of dK and dV, of all rows that see the key; both: not dK alone, where dV's sums are numbers
 template <typename T>
-__device__ inline void window_dkdv_row(const WindowArgs& p, int kvh, int key, int col0, int end_col) {
+__device__ inline void window_dkdv_row(const WindowArgs& p, int kvh, int key, int col0, int end_col, bool both = true) {
     const int lane = lane_anew();
     const int group = p.H / p.H_kv, end = key < p.sinks ? p.c : min(p.c, key + p.window);
     const int64_t row = kvh * p.kv_stride_h + (int64_t)key * p.kv_stride_s;
@@ -340,6 +350,7 @@ __device__ inline void window_dkdv_row(const WindowArgs& p, int kvh, int key, in
             no_delta = no_delta || e != e;
         }
     bool no_v = __builtin_amdgcn_ballot_w64(no_lse) != 0, no_k = no_v || __builtin_amdgcn_ballot_w64(no_delta) != 0;
+    no_v = no_v || !both;
     const int col = window_col(col0, end_col, lane);
     float4 acck = make_float4(0.f, 0.f, 0.f, 0.f), accv = acck;
     if (no_k) acck = no_numbers();
@@ -363,11 +374,11 @@ __device__ inline void window_dkdv_row(const WindowArgs& p, int kvh, int key, in
             no_k = no_k || lost(acck);
         }
     }
-    window_store<T>((T*)p.dv + row, accv, 1.f, col0, end_col, lane);
+    if (both) window_store<T>((T*)p.dv + row, accv, 1.f, col0, end_col, lane);
     window_store<T>((T*)p.dk + row, acck, p.scale, col0, end_col, lane);
 }
 // The rows set in a mask, as each_row has them: the launch's arguments are read and its sequence looked up anew, so that nothing of either has to be
-// kept until here.  first_row: of the wavefront within its workgroup's tile.  row(arguments, head, row of the sequence).
+// kept until here.  first_row: of the wavefront within its workgroup's tile.  row(arguments, head, row of the sequence, its bit).
 template <bool SNAKE, int TILE, typename Row>
 __device__ inline void each_window_row(uint32_t rows, int linear, int n_heads, int first_row, Row row) {
     if (rows == 0) return;
@@ -376,7 +387,7 @@ __device__ inline void each_window_row(uint32_t rows, int linear, int n_heads, i
     if (!enter_sequence<SNAKE, TILE>(p, linear, n_heads, n_tiles, rank, head)) return;
     first_row += TILE * (SNAKE ? n_tiles - 1 - rank : rank);        // (query tiles: the heaviest, the first in order, is the last)
 #pragma unroll 1
-    for (; rows != 0; rows &= rows - 1) row(p, head, first_row + __builtin_ctz(rows));
+    for (; rows != 0; rows &= rows - 1) row(p, head, first_row + __builtin_ctz(rows), (int)__builtin_ctz(rows));
 }
 
 }  // namespace sa

@@ -285,15 +285,17 @@ window_join_kernel(WindowArgs p, int block0) {
 #pragma unroll
                     for (int i = 0; i < ROW_COLS; ++i) sum[w][i] += x[s][w][i];
     }
-    float z = 0.f, loud[2] = {0.f, 0.f};
+    float z[2] = {0.f, 0.f}, loud[2] = {0.f, 0.f};
 #pragma unroll
     for (int w = 0; w < 2; ++w)
 #pragma unroll
         for (int i = 0; i < ROW_COLS; ++i) {
-            z = fmaf(sum[w][i], 0.f, z);
+            z[w] = fmaf(sum[w][i], 0.f, z[w]);
             loud[w] = fmaxf(loud[w], fabsf(sum[w][i]));
         }
-    bool odd = __builtin_amdgcn_ballot_w64(z != 0.f) != 0;
+    bool odd[2];            // dV, dK
+#pragma unroll
+    for (int w = 0; w < 2; ++w) odd[w] = __builtin_amdgcn_ballot_w64(z[w] != 0.f) != 0;
     // the arguments of a launch on that sequence alone
     const int64_t q = first * p.stride_s, kv = first * p.kv_stride_s;
     p.q = (const T*)p.q + q;
@@ -307,16 +309,16 @@ window_join_kernel(WindowArgs p, int block0) {
     if constexpr (sizeof(T) == 4)
         if (p.d <= 128)
             for (int w = 0; w < 2; ++w)
-                odd = odd || (__builtin_amdgcn_ballot_w64(loud[w] >= FAINT) == 0 && __builtin_amdgcn_ballot_w64(loud[w] > 0.f) != 0 &&
-                              faint_tile(p, at_slot.slot, kvh, key, w, lane));
-    if (odd) return window_dkdv_row<T>(p, kvh, key, 0, p.d);
+                odd[w] = odd[w] || (__builtin_amdgcn_ballot_w64(loud[w] >= FAINT) == 0 && __builtin_amdgcn_ballot_w64(loud[w] > 0.f) != 0 &&
+                                    faint_tile(p, at_slot.slot, kvh, key, w, lane));
     const int64_t row = kvh * p.kv_stride_h + (int64_t)key * p.kv_stride_s;
 #pragma unroll
     for (int i = 0; i < ROW_COLS; ++i)
         if (lane + 64 * i < p.d) {
-            store1((T*)p.dv + row + lane + 64 * i, sum[0][i]);
-            store1((T*)p.dk + row + lane + 64 * i, sum[1][i]);
+            if (!odd[0]) store1((T*)p.dv + row + lane + 64 * i, sum[0][i]);
+            if (!odd[0] && !odd[1]) store1((T*)p.dk + row + lane + 64 * i, sum[1][i]);
         }
+    if (odd[0] || odd[1]) window_dkdv_row<T>(p, kvh, key, 0, p.d, odd[0]);
 }
 
 template <typename T>
