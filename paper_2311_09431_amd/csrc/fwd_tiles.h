@@ -579,7 +579,6 @@ fwd_mfma_kernel(Args p, int n_qtiles) {
     const float a_part = !number ? NAN : l_tot > 0.f ? w_part * inv / l_tot : 0.f;
     uint32_t odd = 0;           // rows to do over
     if constexpr (WINDOW) odd = row_mask(row_ok && number && window_odd<MB, PART>(oacc, h, d));
-    const bool stored = row_ok && (!WINDOW || !((odd >> n) & 1));
 #pragma unroll
     for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
@@ -590,7 +589,7 @@ fwd_mfma_kernel(Args p, int n_qtiles) {
                 bf16x4 y[2];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) y[e / 4][e % 4] = (__bf16)(oacc[mb][4 * g + e] * a_part);
-                store_two_chunks(O + (int64_t)a * ss, col - 4 * h, y[0], y[1], stored, h, d);
+                store_two_chunks(O + (int64_t)a * ss, col - 4 * h, y[0], y[1], row_ok, h, d);
             } else {
                 if (col >= d || !row_ok) continue;        // padding columns, rows beyond the shard
                 float4* dst = reinterpret_cast<float4*>(O + (int64_t)a * ss + col);
@@ -605,10 +604,12 @@ fwd_mfma_kernel(Args p, int n_qtiles) {
             }
         }
     if (h == 0 && row_ok) L[a] = number ? (top + __builtin_amdgcn_logf(w_sum)) * LN2 : NAN;
-    if constexpr (WINDOW)
+    if constexpr (WINDOW) {
+        if (odd) __threadfence_block();         // what is stored of them is read
         each_window_row<true, BM>(odd, (int)blockIdx.x, launch_args().H, 32 * wave, [&](const WindowArgs& again, int head, int row, int) {
-            window_fwd_row<__hip_bfloat16>(again, head, row);
+            window_fwd_row<BM>(again, head, row);
         });
+    }
 }
 
 }  // namespace

@@ -167,7 +167,7 @@ struct KeyCursor {
 // into the running state of the lane's row (base: of the workgroup's rows' matrix, a: the row, clamped to the shard).
 // Returns the rows to do over (EXACT only; TERMS: V was three bf16 terms, masks are the words of RowsToRedo).  OutT: float, or __bf16
 // for rows that end here (packed sequences, p.fresh).  WINDOW: rows with a number for their sum and results that are not finite (odd_acc: this
-// wavefront's are not) are done over, but for their LSE; a sum that is no positive number says so of the row (scores that are not seen are no part of it).
+// wavefront's are not), which are stored all the same; a sum that is no positive number says so of the row (scores that are not seen are no part of it).
 template <int DP, int WAVES, bool EXACT, bool TERMS, bool WINDOW = false, typename Lane, typename OutT>
 __device__ __forceinline__ uint32_t fold_forward(const StepArgs& p, f32x16 (&acc)[4], float m, float l, char* lds, float* stats,
                                                  uint32_t* masks, const Lane& ln, int dev, int a_own, int a, float* L, OutT* O,
@@ -218,7 +218,7 @@ __device__ __forceinline__ uint32_t fold_forward(const StepArgs& p, f32x16 (&acc
     __syncthreads();
     const uint32_t odd_rows = TERMS ? redo.take(top_acc * f, top_acc * f) : EXACT || WINDOW ? take_odd<WAVES>(masks) : 0;
     // no row here, or no key seen: state unchanged
-    if (a_own < p.c && !((odd_rows >> n) & 1) && (part != -INFINITY || p.fresh)) {
+    if (a_own < p.c && (WINDOW || !((odd_rows >> n) & 1)) && (part != -INFINITY || p.fresh)) {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int col = column_of<DP, WAVES>(i, ln);

@@ -377,9 +377,11 @@ fwd_split_kernel(Args p, int n_tiles) {
     if constexpr (WINDOW) odd_acc = window_odd<MB, PART>(acc, h, d);
     const uint32_t odd_rows = fold_forward<DP, WAVES, EXACT, false, WINDOW>(p, acc, m, l, lds, stats, masks, ln, dev, a_own, a, L,
                                                              (OutT*)p.o + base + (int64_t)a * p.stride_s, odd_acc);
-    if constexpr (WINDOW)
+    if constexpr (WINDOW) {
+        if (odd_rows) __syncthreads();          // what the wavefronts have stored of them is read
         each_window_row<true, OWN>(odd_rows & 0xffffffffu / ((1u << WAVES) - 1) << ln.wave, (int)blockIdx.x, p.H, 0,
-                                   [&](const WindowArgs& again, int head, int row, int) { window_fwd_row<__hip_bfloat16>(again, head, row); });
+                                   [&](const WindowArgs& again, int head, int row, int) { window_fwd_row<OWN>(again, head, row); });
+    }
     if (EXACT) each_row<WAVES>(odd_rows, ln.wave, [&](const StepArgs& again, int i) { fwd_row<__hip_bfloat16>(again, b, hd, dev_i, q0 + i, ln.lane); });
 }
 

@@ -264,7 +264,73 @@ __device__ inline void window_ranges(const WindowArgs& p, int a, Body body) {
 #pragma unroll 1
     for (int i = 0; i < 2 && on; ++i) on = body(i ? lo : 0, i ? a + 1 : min(p.sinks, lo));
 }
-// (bf16: the tiles' LSE stays, and their row sum has told a row whose scores leave no number; fp32: terms of an infinite key are NaN, the tiles' say nothing)
+// Every element of n rows is a number and finite.
+template <typename T>
+__device__ inline bool all_finite(const T* rows, int64_t ss, int n, int d, int lane) {
+    static_assert(AHEAD<T> == 16, "four rows a load, 64 of them");
+    float z = 0.f;
+#pragma unroll 1
+    for (int r0 = 0; r0 < n; r0 += 64)
+#pragma unroll 1
+        for (int col0 = 0; col0 < d; col0 += 64) {
+            const int at = min(col0 + 4 * (lane & 15), d - 4);
+            Four<T> y[AHEAD<T>];
+#pragma unroll
+            for (int i = 0; i < AHEAD<T>; ++i) y[i].load(rows + min(r0 + 4 * i + (lane >> 4), n - 1) * ss + at);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = 0; i < AHEAD<T>; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) z = fmaf(y[i].at(e), 0.f, z);
+        }
+    return __builtin_amdgcn_ballot_w64(z != 0.f) == 0;
+}
+// bf16, a row whose scores are numbers (its row sum is one) and some of whose results are not: what the tiles of PAIR rows and keys have stored of it stands, but
+// for columns that a value of a hidden key may have reached, one in the tile that the window begins in or in the row's own.  These are done over, up to where
+// all of them are NaN.
+template <int PAIR>
+__device__ inline void window_fwd_row(const WindowArgs& p, int hd, int a) {
+    typedef __hip_bfloat16 T;
+    const int lane = lane_anew();
+    const int64_t row = hd * p.stride_h + (int64_t)a * p.stride_s, kv_base = (hd / (p.H / p.H_kv)) * p.kv_stride_h;
+    const int q0 = a / PAIR * PAIR, lo = max(window_start(p, q0) / PAIR * PAIR, p.sinks), hi = min(p.c, q0 + PAIR);
+    const T* const V0 = (const T*)p.v + kv_base;
+    if (all_finite<T>(V0 + lo * p.kv_stride_s, p.kv_stride_s, window_start(p, a) - lo, p.d, lane) &&
+        all_finite<T>(V0 + (a + 1) * p.kv_stride_s, p.kv_stride_s, hi - a - 1, p.d, lane))
+        return;
+    const T* const q = (const T*)p.q + row;
+    T* const O = (T*)p.o + row;
+    const int col = window_col(0, p.d, lane);
+    Four<T> tiles;
+    tiles.load(O + col);
+    float m = -INFINITY, l = 0.f;
+    // (a column that stays is NaN here, and none to wait for)
+    float4 acc = make_float4(fabsf(tiles.at(0)) < INFINITY ? NAN : 0.f, fabsf(tiles.at(1)) < INFINITY ? NAN : 0.f,
+                             fabsf(tiles.at(2)) < INFINITY ? NAN : 0.f, fabsf(tiles.at(3)) < INFINITY ? NAN : 0.f);
+    window_ranges(p, a, [&](int first, int end) {
+#pragma unroll 1
+        for (int k0 = first; k0 < end; k0 += 64) {
+            const int n = min(64, end - k0);
+            const float dot = window_dots<T>(q, (const T*)p.k + kv_base + (int64_t)k0 * p.kv_stride_s, p.kv_stride_s, n, p.d, lane);
+            const float s = lane < n ? p.scale * dot : -INFINITY;
+            const float m_new = fmaxf(m, wave_max(s)), ref = m_new == -INFINITY ? 0.f : m_new;
+            const float alpha = m == -INFINITY ? 0.f : expf(m - m_new);
+            const float pr = lane < n ? expf(s - ref) : 0.f;
+            l = l * alpha + wave_sum(pr);
+            acc = make_float4(acc.x * alpha, acc.y * alpha, acc.z * alpha, acc.w * alpha);
+            window_add<T>(acc, pr, V0 + (int64_t)k0 * p.kv_stride_s, p.kv_stride_s, n, col);
+            if (lost(acc)) return false;
+            m = m_new;
+        }
+        return true;
+    });
+    if (4 * lane >= p.d) return;
+    const float inv = 1.f / l, got[4] = {acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv};
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (!(fabsf(tiles.at(e)) < INFINITY)) store1(O + col + e, got[e]);
+}
+// fp32 (terms of an infinite number are NaN: the tiles' results and row sum say nothing)
 template <typename T>
 __device__ inline void window_fwd_row(const WindowArgs& p, int hd, int a) {
     const int lane = lane_anew();
@@ -294,13 +360,12 @@ __device__ inline void window_fwd_row(const WindowArgs& p, int hd, int a) {
             acc = make_float4(acc.x * alpha, acc.y * alpha, acc.z * alpha, acc.w * alpha);
             if (!no_values) window_add<T>(acc, pr, V, p.kv_stride_s, n, col);
             no_values = no_values || lost(acc);
-            if (sizeof(T) == 2 && no_values) return false;
             m = m_new;
         }
         return true;
     });
     window_store<T>(O, acc, 1.f / l, 0, p.d, lane);          // (every key it sees at -inf: no number)
-    if (sizeof(T) == 4 && lane == 0) p.lse[hd * p.stat_stride_h + a] = l == 0.f ? NAN : m + logf(l);
+    if (lane == 0) p.lse[hd * p.stat_stride_h + a] = l == 0.f ? NAN : m + logf(l);
 }
 template <typename T>
 __device__ inline void window_dq_row(const WindowArgs& p, int hd, int a) {

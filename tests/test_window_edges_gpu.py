@@ -175,3 +175,63 @@ def test_inputs_of_no_numbers_take_no_longer(H, H_kv, d, dtype):
         for x in (out, lse, *grads):
             assert x.isnan().all() if which != "none" else torch.isfinite(x).all()
     assert all(x <= 10 * y for slow in times[1:] for x, y in zip(slow, times[0])), times
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("H,d,few", [(2, 4, True), (2, 36, True), (2, 128, True), (24, 64, False), (24, 100, False), (24, 256, False)])
+def test_values_that_are_no_numbers_in_a_column(H, d, few, dtype):
+    """Infinities of a first key and of one that few rows see, and NaN in every key: the column has what the sum over the keys that are seen has, the others are
+    those of 64 bits, LSE too."""
+    window, sinks, at, column = 40, 3, 50, 3
+    lens = [430] if few else [430, 700, 300]
+    n = torch.arange(lens[0])
+    sees_at = (n >= at) & (n < at + window)
+    for case in ("first", "both", "every"):
+        q, k, v, _ = tensors(sum(lens), H, H, d, dtype)
+        if case == "every":
+            v[:, :, column] = float("nan")
+        else:
+            v[0, :, column] = float("-inf")
+            if case == "both":
+                v[at, :, column] = float("inf")
+        out, lse = torch.full_like(q, 7), torch.full((H, sum(lens)), 7.0, device="cuda")
+        sa.sa_attn_window_fwd(q, k, v, lengths_to_offsets(lens).cuda(), out, lse, max(lens), window, sinks)
+        q, k, v, out, lse = (x.cpu()[:, :lens[0]] if x is lse else x.cpu()[:lens[0]] for x in (q, k, v, out, lse))
+        got = out[:, :, column]
+        if case == "every":
+            assert got.isnan().all()
+        else:
+            nan = sees_at if case == "both" else torch.zeros_like(sees_at)
+            assert got[nan].isnan().all() and (got[~nan] == float("-inf")).all()
+        v[:, :, column] = 0
+        sees, others = window_mask(lens[0], window, sinks), torch.arange(d) != column
+        for h in {0, H // 2, H - 1}:
+            x = Seen(q[:, h], k[:, h], v[:, h], d ** -0.5, sees)
+            check((case, "out", h), out[:, h][:, others], x.out[:, others], x.out_off(dtype, ROUNDED[dtype])[:, others])
+            check((case, "lse", h), lse[h], x.lse, x.lse_off)
+
+
+@pytest.mark.parametrize("H,d", [(8, 128), (2, 256), (2, 64)])
+def test_values_that_are_no_numbers_take_no_longer(H, d):
+    """bf16, forward: one that all rows see, and a column of them in every key."""
+    n, window, sinks, off, times = 4096, 512, 4, lengths_to_offsets([4096]).cuda(), []
+    for which in ("none", "first", "column"):
+        q, k, v, _ = tensors(n, H, H, d, BF16)
+        if which == "first":
+            v[0, :, 3] = float("inf")
+        elif which == "column":
+            v[:, :, 3] = float("nan")
+        out, lse = torch.empty_like(q), torch.empty(H, n, device="cuda")
+        call = lambda: sa.sa_attn_window_fwd(q, k, v, off, out, lse, n, window, sinks)       # noqa: E731
+        call()
+        least = []
+        for _ in range(3):
+            start, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            start.record()
+            call()
+            call()
+            end.record()
+            torch.cuda.synchronize()
+            least.append(start.elapsed_time(end))
+        times.append(min(least))
+    assert max(times[1:]) <= 20 * times[0], times
