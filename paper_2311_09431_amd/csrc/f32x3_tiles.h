@@ -518,9 +518,13 @@ __device__ inline void bwd_dq(const Args& p, int n_tiles, int linear, char* lds,
                                           row_mask(top >= FAINT), ln.wave, ln.lane);
     if (a_own < p.c && !((odd_rows >> n) & 1))
         add_rows<NB>(p.dq + base + (int64_t)a * p.stride_s, acc, p.scale, 32 * NB * role, d, h, p.fresh);
+    if constexpr (WINDOW) {
+        each_window_row<true, 32 * GROUPS>(odd_rows & 0x55555555u << role, (int)blockIdx.x - key_workgroups(), launch_args().H, 32 * group,
+                                           [&](const WindowArgs& again, int head, int row, int) { window_dq_row<float>(again, head, row); });
+        return;
+    }
     each_row<2>(odd_rows, role, [&](const StepArgs& again, int i) {
-        if constexpr (WINDOW) window_dq_row<float>(p, hd, q0 + 32 * group + i);
-        else if constexpr (PACKED) dq_row<float>(p, b, hd, dev_i, q0 + 32 * group + i, ln.lane);
+        if constexpr (PACKED) dq_row<float>(p, b, hd, dev_i, q0 + 32 * group + i, ln.lane);
         else dq_row<float>(again, b, hd, dev_i, q0 + 32 * group + i, ln.lane);
     });
 }
@@ -670,9 +674,13 @@ __device__ inline void bwd_dkdv(const Args& p, int n_tiles, int linear, char* ld
     }
     if (stored && !((odd_rows >> n) & 1))
         add_rows<NB>((role ? p.dk : p.dv) + row, acc, role ? p.scale : 1.f, 0, d, h, p.fresh);
+    if constexpr (WINDOW) {
+        each_window_row<false, 32 * GROUPS>(odd_rows & 0x55555555u << role, (int)blockIdx.x, launch_args().H_kv, 32 * group,
+                                            [&](const WindowArgs& again, int head, int row, int) { window_dkdv_row<float>(again, head, row, 0, again.d); });
+        return;
+    }
     each_row<2>(odd_rows, role, [&](const StepArgs& again, int i) {
-        if constexpr (WINDOW) window_dkdv_row<float>(p, kvh, k0 + 32 * group + i, 0, d);
-        else if constexpr (PACKED) dkdv_row<float>(p, b, kvh, dev_i, k0 + 32 * group + i, 0, d, ln.lane);
+        if constexpr (PACKED) dkdv_row<float>(p, b, kvh, dev_i, k0 + 32 * group + i, 0, d, ln.lane);
         else dkdv_row<float>(again, b, kvh, dev_i, k0 + 32 * group + i, 0, d, ln.lane);
     });
 }

@@ -423,6 +423,7 @@ __device__ inline bf16x8 negated(bf16x8 x) {
 template <int DP, bool PART, bool EXACT, bool PACKED = false, typename Args = StepArgs>
 __device__ inline void bwd_dq(const Args& p, int n_tiles, int linear, char* lds, char* stats, uint32_t* masks) {
     constexpr bool WINDOW = std::is_same<Args, WindowArgs>::value;
+    static_assert(BWD_WAVES == 4, "rows done over go round four wavefronts");
     constexpr int KS = ksteps_of(DP), MB = blocks_of(DP), WAVES = BWD_WAVES, LOADS = 2 * PIECES<DP>, TERMS = EXACT ? 3 : 1;
     constexpr int LATE = KS > 2 ? KS - 2 : KS / 2, NEXT = MB > 1 ? 1 : 0;          // (32 columns: two k-steps, one block)
     const Lane<DP> ln;
@@ -590,7 +591,8 @@ __device__ inline void bwd_dq(const Args& p, int n_tiles, int linear, char* lds,
         const uint32_t odd_rows = WINDOW ? take_odd<WAVES>(masks) : 0;
         if (a_own < p.c && !((odd_rows >> n) & 1)) set_rows<DP, WAVES>((__bf16*)p.dq + base + (int64_t)a * p.stride_s, lds, p.scale, d, ln);
         if constexpr (WINDOW)
-            each_row<WAVES>(odd_rows, ln.wave, [&](const StepArgs&, int i) { window_dq_row<__hip_bfloat16>(p, hd, q0 + i); });
+            each_window_row<true, OWN>(odd_rows & 0x11111111u << ln.wave, (int)blockIdx.x - key_workgroups(), launch_args().H, 0,
+                                       [&](const WindowArgs& again, int head, int row, int) { window_dq_row<__hip_bfloat16>(again, head, row); });
         return;
     }
     float* const DQ = p.dq + base + (int64_t)a * p.stride_s;
@@ -845,10 +847,13 @@ __device__ inline void bwd_dkdv(const Args& p, int n_tiles, int linear, char* ld
                 for (int i = 0; i < share_of(DP, WAVES); ++i) none[i] = make_float4(0.f, 0.f, 0.f, 0.f);
                 add_rows<DP, WAVES>(to + d, none, lds + HALF, -p.scale, d, ln);
             }
-            each_row<WAVES>(odd_rows, wave, [&](const StepArgs&, int i) { window_dkdv_row<__hip_bfloat16>(p, kvh, k0 + i, 0, d, (odd_v >> i) & 1); });
         }
         if (ends && !((odd_v >> n) & 1)) set_rows<DP, WAVES>((__bf16*)p.dv + row, lds, 1.f, d, ln);
         if (ends && !((odd_rows >> n) & 1)) set_rows<DP, WAVES>((__bf16*)p.dk + row, lds + HALF, -p.scale, d, ln);
+        if constexpr (WINDOW)
+            each_window_row<false, OWN>(odd_rows & 0x11111111u << wave, (int)blockIdx.x, launch_args().H_kv, 0, [&](const WindowArgs& again, int head, int row, int bit) {
+                window_dkdv_row<__hip_bfloat16>(again, head, row, 0, again.d, (odd_v >> bit) & 1);
+            });
         return;
     }
     float4 old_v[MB], old_k[MB];

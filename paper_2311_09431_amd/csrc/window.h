@@ -454,5 +454,10 @@ __device__ inline void each_window_row(uint32_t rows, int linear, int n_heads, i
 #pragma unroll 1
     for (; rows != 0; rows &= rows - 1) row(p, head, first_row + __builtin_ctz(rows), (int)__builtin_ctz(rows));
 }
+// of a launch with both kinds of workgroups those that own keys, which come first
+__device__ inline int key_workgroups() {
+    const WindowArgs& launched = static_cast<const WindowArgs&>(launch_args());
+    return launched.n_ranks * launched.H_kv;
+}
 
 }  // namespace sa
