@@ -304,6 +304,7 @@ typedef struct {
  * that the window leaves.  The time goes by these pairs, in tiles of up to 128 rows and keys, not by the sequences' lengths squared.
  * Infinities and NaN: as in a sum over the pairs that a row sees alone, in both types.  A row with a NaN or +inf score is NaN in O and LSE, a key
  * at -inf has no weight, a row that sees no other key is NaN; nothing of a key that a row does not see reaches it.
+ * (What is no number costs time: rows and keys within a tile of those that see it are formed one by one; in fp32 all that see an infinite one are.)
  * workspace (backward): sa_attn_window_bwd_workspace(shape, window) bytes, 16-byte aligned, of any content; NULL where that is 0.  Calls that may run
  * at the same time (other streams, captured graphs) need one each.
  * Errors: as theirs, and SHAPE for a window below 1, sinks below 0, a workspace that is too small, a max_len above 2^30.

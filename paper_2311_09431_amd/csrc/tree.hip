@@ -554,7 +554,8 @@ tree_kernel(TreeArgs p) {
 // where this takes 174, 32 sequences' drafts of up to 32.)
 //
 // Bound by memory: a token costs a compute unit 512 bytes (d 128), 65 clocks at 4.9 TB/s, and 24 products of 32 clocks for each 32 tokens and rows, on
-// four SIMDs 24 clocks a token and 128 rows.
+// four SIMDs 24 clocks a token and 128 rows.  It takes 1.4 times that (174 us): R goes by the longest draft that there can be, so a shorter one's unit leaves
+// wavefronts idle; every tile passes the tests for drafted tokens' values; shares spill 48 to 56 registers at 128 columns, between pieces.
 template <int DP> constexpr int KV_BYTES = 2 * tile_bytes(DP);
 template <int DP, int R, bool PART, bool WHOLE>
 __global__ void __launch_bounds__(64 * WAVES, 2)

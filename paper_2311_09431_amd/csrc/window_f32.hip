@@ -1,5 +1,7 @@
 // Attention with a window (window.h) and its gradient, fp32 storage, on the fp32 matrix cores (f32_tiles.h): above 128 columns.  Up to
-// 128 by three bf16 terms a number (window_f32x3.hip, packed_f32x3_split.hip).
+// 128 by three bf16 terms a number (window_f32x3.hip, packed_f32x3_split.hip).  Bound by walks that few workgroups take, each key-owning one a group's
+// heads in turn, with scores formed for either half of the columns: 3 sequences of up to 265 rows, 8 heads on 1, 256 columns, window 100, forward 58, gradient 582 us.  (The
+// gradient's kernel spills 113 registers, the forward's 21.)
 #include "f32_tiles.h"
 
 namespace sa {

@@ -1,7 +1,7 @@
 // Attention with a window (window.h) and its gradient, fp32 storage in three bf16 terms: the workgroups of 128 rows and more (f32x3_tiles.h).
 // Streamed tiles are of 32 rows, and a wavefront's 32 rows leave out those of which they see nothing.  Bound by the number of such tiles, each between
 // barriers, more than by products: 5 sequences of up to 777 rows, 16 heads on 8, 100 columns, window 100, forward 41 us (matrix cores 12 % busy),
-// gradient 111 (15 %, 53 % of cycles in waits), 105 keys a row seen of 288 walked over.
+// gradient 111 (15 %, 55 % of cycles in waits), 105 keys a row seen of 288 walked over.  (The gradient's kernel of 65 to 128 columns spills 39 registers.)
 #include "f32x3_tiles.h"
 
 namespace sa {

@@ -3,7 +3,7 @@
 // A workgroup takes 16 keys, a part of the sequence's rows and, one after the other, the query heads of its group, as decode.hip takes heads and cached
 // tokens: rows of Q and dO go from memory to the registers that the products want, once as they lie (S = Q K^T and dP = dO V^T, a lane holding
 // rows 4 j + r of key n) and once turned round in registers (dV^T += dO^T P, dK^T += Q^T dS).  P comes from the rows' LSE.  Four wavefronts take tiles of rows in
-// turn, their sums meet in LDS.  In bf16 P and dS meet dO and Q as bf16, as in the other kernels.
+// turn, their sums meet in LDS.  In bf16 P and dS meet dO and Q as bf16, as in the other kernels.  (At 256 columns 40 registers are spilled, in fp32 74.)
 //
 // Bound by the latency of its reads: Q and dO are read once more, in both orders (the second from the caches).  2 sequences of up to 16384 rows, 16 heads
 // on 8, bf16, 128 columns: 52 us, 2.9 TB/s; joining the parts' sums 17.
@@ -253,7 +253,8 @@ __device__ inline bool faint_tile(const WindowArgs& p, int slot, int kvh, int ke
 }
 
 // dK and dV of a sequence's first keys put together, a wavefront a key: the windows' own sums and each part's, in order.  Where that is no number
-// (or, in fp32, faint, of a tile that is: a faint key alone is what peaked scores leave) the row is done over.
+// (or, in fp32, faint, of a tile that is: a faint key alone is what peaked scores leave; all of them done over, 700 rows, 8 heads of 64 columns, 130 first
+// keys, 287 us, not 51) the row is done over.
 template <typename T>
 __global__ void __launch_bounds__(64 * WAVES)
 window_join_kernel(WindowArgs p, int block0) {
